@@ -349,6 +349,110 @@ ssgd_status ssgd_signsgd_step_noalloc(float* x, const float* g, float* m,
                                       size_t M, size_t d, size_t ld, float beta,
                                       float delta, void* stream);
 
+/* Element types of the tensors that the calls below read and write. */
+typedef enum { SSGD_F32 = 0, SSGD_BF16 = 1, SSGD_F16 = 2 } ssgd_dtype;
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Norm and clipping of gradients that come as many tensors.
+ *
+ * A model's gradient is hundreds of tensors of several types and odd sizes; the step above takes one float row per
+ * worker.  These calls find the norm of each worker's gradient over all its tensors, scale it down to max_norm where
+ * it is larger, and write it where it is wanted: into a worker's row (type conversion and layout in the same pass),
+ * or in place.  Clipping matters with a momentum (Algorithm 2), where one outsized gradient would stay in m for many
+ * steps; without one the sign does not feel it.
+ *
+ * The tensors are described once, on the host, by a table that the caller owns and copies to the device; it may be
+ * used for as long as the buffers stay where they are.
+ *   src      DEVICE, n elements, contiguous, aligned to its element
+ *   dst      DEVICE, n elements, or NULL (norm only); may equal src when the types are equal
+ *   group    the worker that the tensor belongs to; the tensors come in order of their groups                       */
+typedef struct {
+  const void* src;
+  void* dst;
+  size_t n;
+  unsigned src_type, dst_type; /* ssgd_dtype */
+  unsigned group;
+  unsigned reserved;           /* 0 */
+} ssgd_tensor;
+
+/* Sizes for a table of T tensors in `groups` groups (1 .. SSGD_MAX_WORKERS; a group may be empty): the number of
+ * tiles (pieces of at most 8192 elements, one per thread block), the bytes of the table, and the bytes of the
+ * workspace of the calls that use it.  Pure host arithmetic.                                                        */
+ssgd_status ssgd_table_size(const ssgd_tensor* tensors, size_t T, size_t groups, size_t* tiles, size_t* table_bytes,
+                            size_t* ws_bytes);
+
+/* Writes the table into HOST memory; copy its table_bytes to the device (16-byte aligned) before use.               */
+ssgd_status ssgd_table_build(const ssgd_tensor* tensors, size_t T, size_t groups, void* table_host, size_t table_bytes);
+
+/* Norm of each group: SSGD_NORM_TWO sqrt(sum g^2), summed in fp64; SSGD_NORM_MAX max |g|.  NaN and infinity carry
+ * through; an empty group has norm 0.  No atomics: equal inputs give equal bits.
+ *   table  DEVICE copy of the table; ws DEVICE, ws_bytes, 16-byte aligned;  norms out DEVICE float [groups]         */
+#define SSGD_NORM_TWO 0
+#define SSGD_NORM_MAX 1
+ssgd_status ssgd_tensors_norm(const void* table, size_t tiles, size_t groups, int kind, void* ws, float* norms,
+                              void* stream);
+
+/* ssgd_tensors_norm, then for every tensor with a dst
+ *   dst <- c * src,  c = max_norm / norm where norm > max_norm, else 1     (one fp32 rounding, one to dst's type)
+ * max_norm >= 0; infinity: no clipping, only the copy.  A norm that is not finite: with zero_nonfinite != 0 that
+ * group's dst becomes 0, so that a broken gradient does not enter the momentum; else c is what the formula gives
+ * (0 for infinity, NaN for NaN).                                                                                    */
+ssgd_status ssgd_tensors_clip(const void* table, size_t tiles, size_t groups, int kind, float max_norm,
+                              int zero_nonfinite, void* ws, float* norms, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point: the products that make the gradients, and the trained weights, in 4 bits.
+ *
+ * A value is 4 bits: sign, two exponent bits, one fraction bit (0, 0.5, 1, 1.5, 2, 3, 4, 6).  Blocks of values that
+ * follow one another along a row share a scale S:
+ *   SSGD_MXFP4  32 values; S a power of two, one byte, its exponent + 127 (255: NaN)
+ *   SSGD_NVFP4  16 values; S an E4M3 number, one byte (0x7F: NaN), times the tensor scale (one float for the operand)
+ * A packed operand of `rows` x `cols`:
+ *   codes   uint8 [rows][ssgd_fp4_row_bytes(cols)], two values a byte, the even column in the low half; codes beyond
+ *           cols are 0
+ *   scales  uint8 [ssgd_fp4_scale_bytes(format, rows, cols)]: tiles of 128 rows x 4 blocks, 512 bytes each, tiles of
+ *           the same rows following one another; byte (row % 32) * 16 + (row % 128) / 32 * 4 + block % 4 of a tile;
+ *           what lies beyond rows and cols in a tile is 0
+ *   both 16-byte aligned.  Sides go up to SSGD_FP4_MAX_SIDE.                                                        */
+typedef enum { SSGD_MXFP4 = 0, SSGD_NVFP4 = 1 } ssgd_fp4_format;
+#define SSGD_FP4_MAX_SIDE ((size_t)1 << 30)
+
+size_t ssgd_fp4_row_bytes(size_t cols);
+size_t ssgd_fp4_scale_bytes(int format, size_t rows, size_t cols); /* 0 for a bad format or side */
+
+/* Quantises a matrix by rows (codes, scales: blocks along its columns), by columns (codes_t, scales_t: the packed
+ * transpose, cols x rows, blocks along its rows), or both; the pair that is not wanted is NULL.
+ *   x         in   DEVICE [rows][ldx] of dtype, ldx >= cols, aligned to its element
+ *   mx: S = 2^(floor(log2 max|x|) - 2), exponent not below -127
+ *   nv: S = max(E4M3 nearest to max|x| / t / 6, 2^-9) * t, with t, the tensor scale, the least power of two for which
+ *       2688 t >= amax (1 when amax is 0 or not finite; exponent kept within -100 .. 120)
+ *   code = the value nearest to x / S (fp32 quotient), ties to the even code, magnitudes above 6 to 6.  A block with
+ *   an infinity or a NaN has the NaN scale and reads back as NaN.
+ *   amax          in   DEVICE float, nv only: max |x| of the operand, or NULL: the call finds it
+ *   tensor_scale  out  DEVICE float[2], nv only (may be NULL for mx): [0] = t; [1] = the amax found when amax is NULL  */
+ssgd_status ssgd_fp4_quantise(const void* x, int dtype, size_t rows, size_t cols, size_t ldx, int format,
+                              const float* amax, float* tensor_scale, uint8_t* codes, uint8_t* scales,
+                              uint8_t* codes_t, uint8_t* scales_t, void* stream);
+
+/* The values of a packed operand: out[r][c] = code * S, rounded once to dtype.
+ *   tensor_scale in DEVICE float or NULL (1);  out DEVICE [rows][ldo], ldo >= cols, aligned to its element           */
+ssgd_status ssgd_fp4_dequantise(const uint8_t* codes, const uint8_t* scales, const float* tensor_scale, int format,
+                                size_t rows, size_t cols, void* out, int dtype, size_t ldo, void* stream);
+
+/* Product of two packed operands of one format, A M x K and B N x K, blocks along K in both:
+ *   out[i][j] = tA tB sum_k A[i][k] B[j][k]      (fp32 accumulation, rounded once to dtype; K = 0 gives 0)
+ * A layer's forward product is y = x w^T (A = x, B = w by rows); its backward products take the packed transposes:
+ * dx = dy w (A = dy by rows, B = w by columns), dw = dy^T x (A = dy by columns, B = x by columns).
+ *   a_tensor_scale, b_tensor_scale  in DEVICE float or NULL (1)
+ *   out     out DEVICE [M][ldo] of dtype, ldo >= N, aligned to its element
+ *   status  in/out DEVICE unsigned, 0 before the first call: every wait in the kernel has an iteration limit, and a
+ *           block whose operands do not arrive within it sets bit 0 here and gives up its part of out; it stays 0 in
+ *           normal operation                                                                                         */
+ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_tensor_scale,
+                            const uint8_t* b_codes, const uint8_t* b_scales, const float* b_tensor_scale, size_t M,
+                            size_t N, size_t K, int format, void* out, int dtype, size_t ldo, unsigned* status,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,7 +7,7 @@ load the CUDA library; the first use of ``binding`` does, and fails loudly if th
 library has not been built.
 """
 
-__all__ = ["binding", "workloads"]
+__all__ = ["binding", "fp4", "workloads"]
 
 
 def __getattr__(name):

@@ -49,6 +49,10 @@ def lib() -> ctypes.CDLL:
     L.ssgd_warmup_steps.argtypes = [f32]
     L.ssgd_step_is_fused.restype = ci
     L.ssgd_step_is_fused.argtypes = [sz, sz, ci]
+    L.ssgd_fp4_row_bytes.restype = sz
+    L.ssgd_fp4_row_bytes.argtypes = [sz]
+    L.ssgd_fp4_scale_bytes.restype = sz
+    L.ssgd_fp4_scale_bytes.argtypes = [ci, sz, sz]
     L.ssgd_status_str.restype = ctypes.c_char_p
     L.ssgd_status_str.argtypes = [ci]
     sigs = {
@@ -71,6 +75,13 @@ def lib() -> ctypes.CDLL:
         "ssgd_signum_momentum_pack_scatter": [vp, vp, sz, f32, vp, sz, sz, sz, vp],
         "ssgd_majority_vote_staged": [vp, sz, sz, sz, vp, vp, vp],
         "ssgd_majority_vote_staged_wait_selftest": [vp, sz, sz, sz, vp, vp, vp],
+        "ssgd_table_size": [vp, sz, sz, vp, vp, vp],
+        "ssgd_table_build": [vp, sz, sz, vp, sz],
+        "ssgd_tensors_norm": [vp, sz, sz, ci, vp, vp, vp],
+        "ssgd_tensors_clip": [vp, sz, sz, ci, f32, ci, vp, vp, vp],
+        "ssgd_fp4_quantise": [vp, ci, sz, sz, sz, ci, vp, vp, vp, vp, vp, vp, vp],
+        "ssgd_fp4_dequantise": [vp, vp, vp, ci, sz, sz, vp, ci, sz, vp],
+        "ssgd_fp4_matmul": [vp, vp, vp, vp, vp, vp, sz, sz, sz, ci, vp, ci, sz, vp, vp],
     }
     for name, args in sigs.items():
         fn = getattr(L, name)
@@ -355,3 +366,148 @@ def signsgd_step_noalloc(x: torch.Tensor, g: torch.Tensor, m: Optional[torch.Ten
     _check(lib().ssgd_signsgd_step_noalloc(
         _ptr(x, torch.float32, "x"), _ptr(g, torch.float32, "g"), _ptr(m, torch.float32, "m"),
         M, d, ld, beta, delta, _stream(stream)), "ssgd_signsgd_step_noalloc")
+
+
+# --------------------------------------------------------------------------
+# gradients that come as many tensors; 4-bit operands
+
+DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_size_t), ("src_type", ctypes.c_uint),
+                ("dst_type", ctypes.c_uint), ("group", ctypes.c_uint), ("reserved", ctypes.c_uint)]
+
+
+def _typed_ptr(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or t.dtype not in DTYPE_CODE:
+        raise TypeError("%s must be a torch tensor of dtype float32, bfloat16 or float16" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must live in device memory" % name)
+    return t.data_ptr()
+
+
+def _need_rows(t: torch.Tensor, rows: int, cols: int, ld: int, name: str) -> None:
+    """t's memory, from its first element on, must hold `rows` rows of `cols` elements at a stride of ld."""
+    n = (rows - 1) * ld + cols if rows and cols else 0
+    if t.numel() < n and t.untyped_storage().nbytes() // t.element_size() - t.storage_offset() < n:
+        raise ValueError("%s is too small for %d x %d elements at a row stride of %d" % (name, rows, cols, ld))
+
+
+class TensorTable:
+    """The tensors of one or more workers' gradients, described once for `tensors_norm` and `tensors_clip`.
+
+    src     device tensors (float32, bfloat16, float16; contiguous), any number, any size
+    dst     where the clipped values go, one tensor of the same number of elements for each (None entries, or None
+            altogether: norm only); a tensor of `src` itself: in place.  Slices of a worker's flat row are the usual ones
+    groups  the worker of each tensor, not descending; None: all belong to worker 0
+
+    The table keeps the tensors alive and holds for as long as they stay where they are."""
+
+    def __init__(self, src, dst=None, groups=None, workers: Optional[int] = None):
+        src = list(src)
+        dst = [None] * len(src) if dst is None else list(dst)
+        groups = [0] * len(src) if groups is None else list(groups)
+        if len(dst) != len(src) or len(groups) != len(src):
+            raise ValueError("src, dst and groups must have one entry per tensor")
+        self.workers = (max(groups) + 1 if groups else 1) if workers is None else int(workers)
+        entries = (_Tensor * max(1, len(src)))()
+        device = None
+        for e, s, t, w in zip(entries, src, dst, groups):
+            e.src, e.n, e.src_type, e.group = _typed_ptr(s, "src"), s.numel(), DTYPE_CODE[s.dtype], int(w)
+            device = s.device if device is None else device
+            if s.device != device or (t is not None and t.device != device):
+                raise ValueError("all tensors must live on one device")
+            if not s.is_contiguous() or (t is not None and not t.is_contiguous()):
+                raise ValueError("src and dst must be contiguous")
+            if t is not None:
+                e.dst, e.dst_type = _typed_ptr(t, "dst"), DTYPE_CODE[t.dtype]
+                if t.numel() != s.numel():
+                    raise ValueError("a dst holds %d elements, its src %d" % (t.numel(), s.numel()))
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+        tiles, nbytes, ws = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
+        _check(lib().ssgd_table_size(entries, len(src), self.workers, ctypes.byref(tiles), ctypes.byref(nbytes), ctypes.byref(ws)),
+               "ssgd_table_size")
+        host = torch.zeros(nbytes.value, dtype=torch.uint8)
+        _check(lib().ssgd_table_build(entries, len(src), self.workers, host.data_ptr(), nbytes.value), "ssgd_table_build")
+        self.tiles = tiles.value
+        self.table = host.to(self.device)
+        self.ws = torch.zeros(ws.value, dtype=torch.uint8, device=self.device)
+        self._keep = (src, dst)
+
+
+NORM_KIND = {"two": 0, "max": 1}
+
+
+def tensors_norm(table: TensorTable, norms: torch.Tensor, kind: str = "two", stream=None) -> None:
+    """norms[w] <- norm of worker w's gradient over all its tensors ("two": sqrt of the sum of squares, "max")."""
+    _need(norms, table.workers, "norms")
+    _check(lib().ssgd_tensors_norm(table.table.data_ptr(), table.tiles, table.workers, NORM_KIND[kind], table.ws.data_ptr(),
+                                   _ptr(norms, torch.float32, "norms"), _stream(stream)), "ssgd_tensors_norm")
+
+
+def tensors_clip(table: TensorTable, max_norm: float, norms: torch.Tensor, kind: str = "two", zero_nonfinite: bool = False,
+                 stream=None) -> None:
+    """norms as `tensors_norm`; every dst <- src * (max_norm / norm where norm > max_norm, else 1).  With zero_nonfinite a
+    worker whose norm is not finite gets zeros."""
+    _need(norms, table.workers, "norms")
+    _check(lib().ssgd_tensors_clip(table.table.data_ptr(), table.tiles, table.workers, NORM_KIND[kind], max_norm,
+                                   1 if zero_nonfinite else 0, table.ws.data_ptr(), _ptr(norms, torch.float32, "norms"),
+                                   _stream(stream)), "ssgd_tensors_clip")
+
+
+FP4_FORMAT = {"mx": 0, "nv": 1}
+
+
+def fp4_row_bytes(cols: int) -> int:
+    """Bytes of one row of codes."""
+    return int(lib().ssgd_fp4_row_bytes(cols))
+
+
+def fp4_scale_bytes(fmt: str, rows: int, cols: int) -> int:
+    """Bytes of the scales of a packed operand."""
+    return int(lib().ssgd_fp4_scale_bytes(FP4_FORMAT[fmt], rows, cols))
+
+
+def fp4_quantise(x: torch.Tensor, rows: int, cols: int, ldx: int, fmt: str, amax: Optional[torch.Tensor],
+                 tensor_scale: Optional[torch.Tensor], codes: Optional[torch.Tensor], scales: Optional[torch.Tensor],
+                 codes_t: Optional[torch.Tensor], scales_t: Optional[torch.Tensor], stream=None) -> None:
+    """Packs x (its first element at x, rows of stride ldx) by rows, by columns, or both, into uint8 buffers."""
+    _need_rows(x, rows, cols, ldx, "x")
+    for name, c, s, r, k in (("codes", codes, scales, rows, cols), ("codes_t", codes_t, scales_t, cols, rows)):
+        if c is not None:
+            _need(c, r * ((k + 31) // 32 * 16), name); _need(s, fp4_scale_bytes(fmt, r, k), "scales of " + name)
+    if fmt == "nv":
+        _need(tensor_scale, 2, "tensor_scale")
+    u8, f32 = torch.uint8, torch.float32
+    _check(lib().ssgd_fp4_quantise(
+        _typed_ptr(x, "x"), DTYPE_CODE[x.dtype], rows, cols, ldx, FP4_FORMAT[fmt], _ptr(amax, f32, "amax"),
+        _ptr(tensor_scale, f32, "tensor_scale"), _ptr(codes, u8, "codes"), _ptr(scales, u8, "scales"),
+        _ptr(codes_t, u8, "codes_t"), _ptr(scales_t, u8, "scales_t"), _stream(stream)), "ssgd_fp4_quantise")
+
+
+def fp4_dequantise(codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Optional[torch.Tensor], fmt: str, rows: int,
+                   cols: int, out: torch.Tensor, ldo: int, stream=None) -> None:
+    """out <- the values of a packed operand (rows of stride ldo)."""
+    _need(codes, rows * ((cols + 31) // 32 * 16), "codes"); _need(scales, fp4_scale_bytes(fmt, rows, cols), "scales")
+    _need_rows(out, rows, cols, ldo, "out")
+    _check(lib().ssgd_fp4_dequantise(
+        _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), _ptr(tensor_scale, torch.float32, "tensor_scale"),
+        FP4_FORMAT[fmt], rows, cols, _typed_ptr(out, "out"), DTYPE_CODE[out.dtype], ldo, _stream(stream)), "ssgd_fp4_dequantise")
+
+
+def fp4_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, a_tensor_scale: Optional[torch.Tensor], b_codes: torch.Tensor,
+               b_scales: torch.Tensor, b_tensor_scale: Optional[torch.Tensor], M: int, N: int, K: int, fmt: str,
+               out: torch.Tensor, ldo: int, status: torch.Tensor, stream=None) -> None:
+    """out[i][j] <- sum_k A[i][k] B[j][k] of two packed operands (rows of out of stride ldo).  `status` is a one-element
+    int32 device tensor, zero at first, non-zero afterwards only if a bounded wait in the kernel ran out."""
+    row = (K + 31) // 32 * 16
+    _need(a_codes, M * row, "a_codes"); _need(b_codes, N * row, "b_codes"); _need(status, 1, "status")
+    _need(a_scales, fp4_scale_bytes(fmt, M, K), "a_scales"); _need(b_scales, fp4_scale_bytes(fmt, N, K), "b_scales")
+    _need_rows(out, M, N, ldo, "out")
+    u8, f32 = torch.uint8, torch.float32
+    _check(lib().ssgd_fp4_matmul(
+        _ptr(a_codes, u8, "a_codes"), _ptr(a_scales, u8, "a_scales"), _ptr(a_tensor_scale, f32, "a_tensor_scale"),
+        _ptr(b_codes, u8, "b_codes"), _ptr(b_scales, u8, "b_scales"), _ptr(b_tensor_scale, f32, "b_tensor_scale"), M, N, K,
+        FP4_FORMAT[fmt], _typed_ptr(out, "out"), DTYPE_CODE[out.dtype], ldo, _ptr(status, torch.int32, "status"),
+        _stream(stream)), "ssgd_fp4_matmul")
