@@ -123,6 +123,11 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_of(device: torch.device) -> int:
+    """The current stream of a tensor's device."""
+    return torch.cuda.current_stream(device).cuda_stream
+
+
 def _check(status: int, where: str) -> None:
     if status != 0:
         raise SignSGDError(status, where)

@@ -38,6 +38,14 @@ __device__ __forceinline__ float4 load4(const __half* p) {
   return make_float4(a.x, a.y, b.x, b.y);
 }
 
+// The two elements of a 32-bit word.
+__device__ __forceinline__ float low_to_float(__nv_bfloat16, unsigned w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_to_float(__nv_bfloat16, unsigned w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ float low_to_float(__half, unsigned w) { return __low2float(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ float high_to_float(__half, unsigned w) { return __high2float(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ float low_to_float(float, unsigned w) { return __uint_as_float(w); }
+__device__ __forceinline__ float high_to_float(float, unsigned w) { return __uint_as_float(w); }
+
 __device__ __forceinline__ unsigned pack2(__nv_bfloat16, float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const unsigned*>(&v);

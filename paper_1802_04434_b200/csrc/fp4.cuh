@@ -27,11 +27,11 @@ __host__ __device__ __forceinline__ size_t fp4_scale_index(size_t row, size_t bl
   return ((row >> 7) * tiles_k + (block >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
 }
 
-// Magnitude of a code as a float: codes 0 and 1 are 0 and 0.5, above it is (1 + f / 2) * 2^(e - 1).
-__device__ __forceinline__ float fp4_value(unsigned code) {
-  const unsigned m = code & 7u;
-  const float v = m < 2 ? 0.5f * (float)m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
-  return (code & 8u) ? -v : v;
+// The two values of a byte of codes, the low half's first.
+__device__ __forceinline__ float2 fp4_pair_value(unsigned byte) {
+  unsigned h;
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\t}" : "=r"(h) : "r"(byte));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
 __device__ __forceinline__ float e8m0_value(unsigned byte) {

@@ -12,31 +12,78 @@ import torch
 
 from . import binding as B
 
+_BLOCK = {"mx": 32, "nv": 16}
 
-class Packed(NamedTuple):
-    """A matrix in 4 bits, blocks along its columns."""
-    codes: torch.Tensor                     # uint8 [rows][row bytes]
-    scales: torch.Tensor                    # uint8, tiles of 128 rows x 4 blocks
-    tensor_scale: Optional[torch.Tensor]    # float32, its first element (None: 1)
-    rows: int
-    cols: int
-    fmt: str
+
+def _sizes(rows: int, cols: int, fmt: str) -> Tuple[int, int]:
+    """Bytes of the codes and of the scales of a packed operand."""
+    return rows * ((cols + 31) // 32 * 16), (rows + 127) // 128 * (((cols + _BLOCK[fmt] - 1) // _BLOCK[fmt] + 3) // 4) * 512
+
+
+class Packed:
+    """A matrix in 4 bits, blocks along its columns.
+
+    codes          uint8 [rows][row bytes], contiguous
+    scales         uint8, tiles of 128 rows x 4 blocks, contiguous
+    tensor_scale   float32, its first element (None: 1)
+
+    Its three parts may lie in one buffer, as `quantise` makes them; they are cut out of it when they are asked for."""
+    __slots__ = ("rows", "cols", "fmt", "device", "pointers", "_parts", "_buffer")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Optional[torch.Tensor], rows: int, cols: int, fmt: str):
+        if fmt not in _BLOCK:
+            raise ValueError("fmt must be 'mx' or 'nv'")
+        need = _sizes(rows, cols, fmt)
+        for name, t, n in (("codes", codes, need[0]), ("scales", scales, need[1])):
+            B._ptr(t, torch.uint8, name)
+            B._need(t, n, name)
+        self.rows, self.cols, self.fmt, self.device = rows, cols, fmt, codes.device
+        self.pointers = (codes.data_ptr(), scales.data_ptr(), B._ptr(tensor_scale, torch.float32, "tensor_scale"))
+        self._parts, self._buffer = (codes, scales, tensor_scale), None
+
+    @classmethod
+    def _in(cls, buffer: torch.Tensor, base: int, at: Tuple[int, int, Optional[int]], rows: int, cols: int, fmt: str) -> "Packed":
+        """Parts at the given byte offsets of one buffer whose address is `base`."""
+        p = cls.__new__(cls)
+        p.rows, p.cols, p.fmt, p.device = rows, cols, fmt, buffer.device
+        p.pointers = (base + at[0], base + at[1], None if at[2] is None else base + at[2])
+        p._parts, p._buffer = None, (buffer, at)
+        return p
+
+    def _cut(self):
+        if self._parts is None:
+            buffer, (c, s, t) = self._buffer
+            n, m = _sizes(self.rows, self.cols, self.fmt)
+            self._parts = (buffer[c:c + n].view(self.rows, -1) if n else buffer[:0].view(self.rows, (self.cols + 31) // 32 * 16), buffer[s:s + m],
+                           None if t is None else buffer[t:t + 8].view(torch.float32))
+        return self._parts
+
+    codes = property(lambda self: self._cut()[0])
+    scales = property(lambda self: self._cut()[1])
+    tensor_scale = property(lambda self: self._cut()[2])
+
+    def _replace(self, **parts) -> "Packed":
+        """A copy with some of codes, scales, tensor_scale, rows, cols, fmt replaced."""
+        names = ("codes", "scales", "tensor_scale", "rows", "cols", "fmt")
+        return Packed(*[parts.get(n, getattr(self, n)) for n in names])
 
 
 _status = {}
 
 
-def _status_of(device: torch.device) -> torch.Tensor:
+def _status_of(device: torch.device) -> Tuple[torch.Tensor, int]:
     s = _status.get(device)
     if s is None:
-        s = _status[device] = torch.zeros(1, dtype=torch.int32, device=device)
+        t = torch.zeros(1, dtype=torch.int32, device=device)
+        s = _status[device] = (t, t.data_ptr())
     return s
 
 
 def check(device="cuda") -> None:
     """Waits for the device and raises if a product since the last check had to give up a bounded wait."""
     device = torch.device("cuda", torch.cuda.current_device()) if torch.device(device).index is None else torch.device(device)
-    s = _status_of(device)
+    s = _status_of(device)[0]
+    torch.cuda.synchronize(device)
     if int(s.item()):
         s.zero_()
         raise RuntimeError("a 4-bit product did not receive its operands in time; its output is not valid")
@@ -45,31 +92,42 @@ def check(device="cuda") -> None:
 def _matrix(x: torch.Tensor) -> torch.Tensor:
     if x.dim() != 2:
         raise ValueError("a matrix is wanted, got %d dimensions" % x.dim())
+    if not x.is_cuda:
+        raise ValueError("the matrix must live in device memory")
+    if x.dtype not in B.DTYPE_CODE:
+        raise TypeError("the matrix must be of dtype float32, bfloat16 or float16")
     # rows at any stride; a single column, or a single row, has no stride of its own to look at
-    return x if (x.stride(1) == 1 or x.shape[1] <= 1) and x.stride(0) >= x.shape[1] else x.contiguous()
-
-
-def _empty(rows: int, cols: int, fmt: str, device) -> Tuple[torch.Tensor, torch.Tensor]:
-    return (torch.empty(rows, (cols + 31) // 32 * 16, dtype=torch.uint8, device=device),
-            torch.empty(B.fp4_scale_bytes(fmt, rows, cols), dtype=torch.uint8, device=device))
+    if x.is_contiguous() or ((x.stride(1) == 1 or x.shape[1] <= 1) and x.stride(0) >= x.shape[1]):
+        return x
+    return x.contiguous()
 
 
 def _quantise(x, fmt, amax, by_rows, by_columns):
-    if fmt not in B.FP4_FORMAT:
+    if fmt not in _BLOCK:
         raise ValueError("fmt must be 'mx' or 'nv'")
     x = _matrix(x)
     rows, cols = x.shape
-    codes = scales = codes_t = scales_t = ts = None
+    n = m = nt = mt = 0
     if by_rows:
-        codes, scales = _empty(rows, cols, fmt, x.device)
+        n, m = _sizes(rows, cols, fmt)
     if by_columns:
-        codes_t, scales_t = _empty(cols, rows, fmt, x.device)
-    if fmt == "nv":
-        ts = torch.empty(2, device=x.device) if rows and cols else torch.ones(2, device=x.device)
+        nt, mt = _sizes(cols, rows, fmt)
+    nv = fmt == "nv"
+    ts = n + m + nt + mt                      # all parts are multiples of 16 bytes
+    buffer = torch.empty(ts + 16, dtype=torch.uint8, device=x.device)
+    base = buffer.data_ptr()
     if rows and cols:
-        B.fp4_quantise(x, rows, cols, max(x.stride(0), cols), fmt, amax, ts, codes, scales, codes_t, scales_t)
-    return (Packed(codes, scales, ts, rows, cols, fmt) if by_rows else None,
-            Packed(codes_t, scales_t, ts, cols, rows, fmt) if by_columns else None)
+        status = B.lib().ssgd_fp4_quantise(
+            x.data_ptr(), B.DTYPE_CODE[x.dtype], rows, cols, max(x.stride(0), cols), B.FP4_FORMAT[fmt], B._ptr(amax, torch.float32, "amax"),
+            base + ts if nv else None, base if by_rows else None, base + n, base + n + m if by_columns else None, base + n + m + nt,
+            B._stream_of(x.device))
+        if status:
+            B._check(status, "ssgd_fp4_quantise")
+    elif nv:
+        buffer[ts:ts + 8].view(torch.float32).fill_(1.0)
+    at = ts if nv else None
+    return (Packed._in(buffer, base, (0, n, at), rows, cols, fmt) if by_rows else None,
+            Packed._in(buffer, base, (n + m, n + m + nt, at), cols, rows, fmt) if by_columns else None)
 
 
 def quantise(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor] = None) -> Packed:
@@ -90,25 +148,35 @@ def quantise_both(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor]
 
 def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """The values of a packed matrix."""
-    out = torch.empty(p.rows, p.cols, dtype=dtype, device=p.codes.device)
+    out = torch.empty(p.rows, p.cols, dtype=dtype, device=p.device)
     if p.rows and p.cols:
-        B.fp4_dequantise(p.codes, p.scales, p.tensor_scale, p.fmt, p.rows, p.cols, out, max(1, p.cols))
+        codes, scales, ts = p.pointers
+        status = B.lib().ssgd_fp4_dequantise(codes, scales, ts, B.FP4_FORMAT[p.fmt], p.rows, p.cols, out.data_ptr(), B.DTYPE_CODE[dtype],
+                                             p.cols, B._stream_of(p.device))
+        if status:
+            B._check(status, "ssgd_fp4_dequantise")
     return out
 
 
 def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """a b^T of two packed matrices of one format, fp32 accumulation; into `out` (rows at any stride) where given."""
-    if a.fmt != b.fmt or a.cols != b.cols:
-        raise ValueError("a product needs operands of one format and one length: got %s x %d and %s x %d" % (a.fmt, a.cols, b.fmt, b.cols))
+    if a.fmt != b.fmt or a.cols != b.cols or a.device != b.device:
+        raise ValueError("a product needs operands of one format, one length and one device: got %s x %d and %s x %d" % (a.fmt, a.cols, b.fmt, b.cols))
+    rows, cols = a.rows, b.rows
+    ldo = max(1, cols)
     if out is None:
-        out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
-    elif out.shape != (a.rows, b.rows) or (b.rows > 1 and out.stride(1) != 1) or (a.rows > 1 and out.stride(0) < b.rows):
-        raise ValueError("out must be %d x %d with unit column stride" % (a.rows, b.rows))
+        out = torch.empty(rows, cols, dtype=dtype, device=a.device)
+    else:
+        if out.shape != (rows, cols) or out.device != a.device or (cols > 1 and out.stride(1) != 1) or (rows > 1 and out.stride(0) < cols):
+            raise ValueError("out must be %d x %d with unit column stride, on the operands' device" % (rows, cols))
+        ldo = out.stride(0) if rows > 1 else ldo
     if a.cols == 0:
         return out.zero_()
-    if a.rows and b.rows:
-        B.fp4_matmul(a.codes, a.scales, a.tensor_scale, b.codes, b.scales, b.tensor_scale, a.rows, b.rows, a.cols, a.fmt, out,
-                     out.stride(0) if a.rows > 1 else max(1, b.rows), _status_of(a.codes.device))
+    if rows and cols:
+        status = B.lib().ssgd_fp4_matmul(*a.pointers, *b.pointers, rows, cols, a.cols, B.FP4_FORMAT[a.fmt], out.data_ptr(),
+                                         B.DTYPE_CODE[out.dtype], ldo, _status_of(a.device)[1], B._stream_of(a.device))
+        if status:
+            B._check(status, "ssgd_fp4_matmul")
     return out
 
 
