@@ -194,15 +194,24 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
   if (splits > 1) {
     __syncwarp();
     cluster.sync();
-    if (warp >= 2) {
-      const unsigned row = (warp & 3u) * 32 + lane, j = j0 + row;
-      const float ts = (p.a_ts ? __ldg(p.a_ts) : 1.0f) * (p.b_ts ? __ldg(p.b_ts) : 1.0f);
-      float* partial = reinterpret_cast<float*>(stage_mem);
-      for (unsigned c = split; c < NT && i0 + c < p.M; c += splits) {
-        float v = 0.0f;
-        for (unsigned r = 0; r < splits; ++r) v += cluster.map_shared_rank(partial, r)[c * kTileJ + row];
-        if (j < p.N) store_out(p, (size_t)(i0 + c) * p.ldo + j, v * ts);
-      }
+    // this CTA's columns are split, split + splits, ...: four rows of one column to a thread, all ranks' loads in flight
+    const float ts = (p.a_ts ? __ldg(p.a_ts) : 1.0f) * (p.b_ts ? __ldg(p.b_ts) : 1.0f);
+    const unsigned columns = min((unsigned)NT, p.M - i0);
+    for (unsigned i = threadIdx.x; split + i / 32 * splits < columns; i += kMmaThreads) {
+      const unsigned c = split + i / 32 * splits, row = i % 32 * 4, j = j0 + row;
+      float4 v[8];
+#pragma unroll
+      for (unsigned r = 0; r < 8; ++r)
+        if (r < splits) v[r] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(reinterpret_cast<float*>(stage_mem), r) + c * kTileJ + row);
+      float4 sum = v[0];
+#pragma unroll
+      for (unsigned r = 1; r < 8; ++r)
+        if (r < splits) sum = make_float4(sum.x + v[r].x, sum.y + v[r].y, sum.z + v[r].z, sum.w + v[r].w);
+      const size_t at = (size_t)(i0 + c) * p.ldo + j;
+      if (j < p.N) store_out(p, at, sum.x * ts);
+      if (j + 1 < p.N) store_out(p, at + 1, sum.y * ts);
+      if (j + 2 < p.N) store_out(p, at + 2, sum.z * ts);
+      if (j + 3 < p.N) store_out(p, at + 3, sum.w * ts);
     }
     __syncwarp();
     cluster.sync();                             // nobody leaves while its shared memory is still read
@@ -210,6 +219,203 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
   if (warp == 1) {
     tcgen05_fence_after();
     tmem_free(tmem, S::columns);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Many rows on both sides: persistent pairs of CTAs (cta_group::2), each pair a tile of 256 rows of B by NT rows of A.  A
+// CTA loads 128 rows of B and half of the rows of A, so an operand byte that reaches shared memory serves 256 rows instead
+// of 128, and what bounds the product, bytes from L2 to shared memory, is a third less than with single CTAs.
+//   accumulators   two, so that a tile is written out while the next one is multiplied.  Both and the scales' columns do not
+//                  fit beside one another at NT = 256: the second starts at kSecond < NT, the epilogue drains the shared
+//                  columns first and gives the go-ahead after them
+//   scales         two sets of columns in turn; a set is overwritten when the MMAs that read it are known to be done
+
+template <int FORMAT, int NT>
+struct PairShape {
+  static constexpr unsigned blocks = FORMAT == SSGD_MXFP4 ? 2 : 4;
+  static constexpr unsigned row_tiles = (NT + 127) / 128;
+  static constexpr unsigned b_bytes = 128 * 128, a_bytes = NT / 2 * 128;
+  static constexpr unsigned scale_bytes = blocks * 512;
+  static constexpr unsigned loaded = b_bytes + a_bytes + (1 + row_tiles) * scale_bytes;     // per CTA and stage
+  static constexpr unsigned stage_bytes = (loaded + 1023) / 1024 * 1024;
+  static constexpr unsigned stages = 225280 / stage_bytes < 8 ? 225280 / stage_bytes : 8;
+  static constexpr unsigned scale_columns = (1 + row_tiles) * blocks * 4;
+  static constexpr unsigned first_scale = 512 - 2 * scale_columns;
+  static constexpr unsigned room = (first_scale - NT) / 32 * 32;
+  static constexpr unsigned second = room < NT ? room : NT;              // column of the second accumulator
+  static constexpr unsigned smem = stages * stage_bytes + 1024;
+  static_assert(stages >= 3 && smem <= 231424, "shared memory");
+};
+
+struct PairArgs {
+  const float* a_ts;
+  const float* b_ts;
+  void* out;
+  unsigned* status;
+  size_t ldo;
+  unsigned M, N, k_chunks, tiles_i, tiles;
+};
+
+template <int FORMAT, int NT, typename T>
+__global__ void __launch_bounds__(kMmaThreads, 1)
+fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
+                       const __grid_constant__ CUtensorMap a_scale_map, const __grid_constant__ CUtensorMap b_scale_map, const PairArgs p) {
+  using S = PairShape<FORMAT, NT>;
+  constexpr bool kE8M0 = FORMAT == SSGD_MXFP4;
+  extern __shared__ unsigned char dynamic_smem[];
+  __shared__ __align__(8) uint64_t bars[2 * S::stages + 2];
+  __shared__ unsigned tmem_base, failed;
+  const unsigned rank = cluster_rank();
+  const unsigned stage0 = (smem_u32(dynamic_smem) + 1023u) & ~1023u;     // the same in both CTAs
+  const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 8;
+  const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const unsigned stages_k = (p.k_chunks + 3) / 4;
+  const unsigned pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+
+  if (threadIdx.x == 0) {
+    prefetch_tensor_map(&a_map);
+    prefetch_tensor_map(&b_map);
+    prefetch_tensor_map(&a_scale_map);
+    prefetch_tensor_map(&b_scale_map);
+    for (unsigned s = 0; s < S::stages; ++s) {
+      mbarrier_init(full + 8 * s, 1);
+      mbarrier_init(empty + 8 * s, 1);
+    }
+    mbarrier_init(acc_full, 1);
+    mbarrier_init(acc_free, 8);                 // one arrival from each of the two CTAs' four epilogue warps
+    mbarrier_init_fence();
+    failed = 0;
+  }
+  pdl_launch_dependents();
+  pdl_wait();                                   // before tensor memory is taken: its last holder has finished
+  if (warp == 1) tmem_alloc_pair(smem_u32(&tmem_base), 512);
+  tcgen05_fence_before();
+  __syncthreads();
+  cluster_sync();                               // the other CTA's barriers are ready too
+  tcgen05_fence_after();
+  const unsigned tmem = tmem_base;
+  bool ok = true;
+  unsigned n = 0;                               // stages so far, over all tiles
+
+  if (warp == 0) {
+    if (lane == 0) {
+      for (unsigned tile = pair; tile < p.tiles && ok; tile += pairs) {
+        const unsigned i0 = tile % p.tiles_i * NT, j0 = tile / p.tiles_i * 256 + rank * 128;
+        for (unsigned k = 0; k < stages_k; ++k, ++n) {
+          const unsigned s = n % S::stages;
+          if (n >= S::stages) ok = mbarrier_wait_cluster(empty + 8 * s, (n / S::stages - 1) & 1u, kPolls);
+          if (!ok) break;
+          const unsigned base = stage0 + s * S::stage_bytes, bar = cluster_address(full + 8 * s, 0);
+          if (rank == 0) mbarrier_expect(full + 8 * s, 2 * S::loaded);
+          tma_load_2d_pair(base, &b_map, (int)(k * 128), (int)j0, bar);
+          tma_load_2d_pair(base + S::b_bytes, &a_map, (int)(k * 128), (int)(i0 + rank * (NT / 2)), bar);
+          const unsigned sc = base + S::b_bytes + S::a_bytes;
+          tma_load_2d_pair(sc, &b_scale_map, (int)(k * S::blocks * 64), (int)(j0 / 128), bar);
+          tma_load_2d_pair(sc + S::scale_bytes, &a_scale_map, (int)(k * S::blocks * 64), (int)(i0 / 128), bar);
+        }
+      }
+      // the last stages' commits have to arrive before this CTA may go
+      for (unsigned m = n > S::stages ? n - S::stages : 0; m < n && ok; ++m)
+        ok = mbarrier_wait_cluster(empty + 8 * (m % S::stages), (m / S::stages) & 1u, kPolls);
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      unsigned t = 0;                           // tiles so far
+      for (unsigned tile = pair; tile < p.tiles && ok; tile += pairs, ++t) {
+        if (t > 0) ok = mbarrier_wait_cluster(acc_free, (t - 1) & 1u, kPolls);
+        if (!ok) break;
+        tcgen05_fence_after();
+        const unsigned d = tmem + (t & 1u) * S::second;
+        const unsigned half = (tile % p.tiles_i * NT % 128) / 32;        // NT = 64: where its rows' scales begin in their tile
+        for (unsigned k = 0; k < stages_k; ++k, ++n) {
+          const unsigned s = n % S::stages;
+          ok = mbarrier_wait_cluster(full + 8 * s, (n / S::stages) & 1u, kPolls) &&
+               (n < 2 || mbarrier_wait_cluster(empty + 8 * ((n - 2) % S::stages), ((n - 2) / S::stages) & 1u, kPolls));
+          if (!ok) break;
+          tcgen05_fence_after();
+          const unsigned base = stage0 + s * S::stage_bytes, sc = base + S::b_bytes + S::a_bytes;
+          const unsigned columns = tmem + S::first_scale + (n & 1u) * S::scale_columns;
+          const unsigned chunks = min(4u, p.k_chunks - k * 4);
+#pragma unroll
+          for (unsigned q = 0; q < S::blocks; ++q) {
+            tcgen05_copy_scales_pair(columns + q * 4, smem_descriptor(sc + q * 512, 128, 0));
+#pragma unroll
+            for (unsigned r = 0; r < S::row_tiles; ++r)
+              tcgen05_copy_scales_pair(columns + S::blocks * 4 + (q * S::row_tiles + r) * 4,
+                                       smem_descriptor(sc + (1 + r) * S::scale_bytes + q * 512, 128, 0));
+          }
+          const uint64_t b_desc = smem_descriptor(base, 1024, 2), a_desc = smem_descriptor(base + S::b_bytes, 1024, 2);
+          for (unsigned c = 0; c < chunks; ++c) {
+            const unsigned q = kE8M0 ? c / 2 : c, id = kE8M0 ? (c & 1u) * 2 : 0;
+            mma_fp4_pair<kE8M0>(d, b_desc + 2 * c, a_desc + 2 * c, mma_fp4_descriptor(256, NT, kE8M0, id), columns + q * 4,
+                                columns + S::blocks * 4 + q * S::row_tiles * 4 + half, k > 0 || c > 0);
+          }
+          tcgen05_commit_pair(empty + 8 * s);
+        }
+        if (ok) tcgen05_commit_pair(acc_full);
+      }
+      if (!ok) tcgen05_commit_pair(acc_full);   // what was issued has to end before tensor memory is freed
+    }
+  } else {
+    const unsigned quarter = warp & 3u;
+    const float ts = (p.a_ts ? __ldg(p.a_ts) : 1.0f) * (p.b_ts ? __ldg(p.b_ts) : 1.0f);
+    const unsigned go = cluster_address(acc_free, 0);
+    unsigned t = 0;
+    for (unsigned tile = pair; tile < p.tiles; tile += pairs, ++t) {
+      ok = mbarrier_wait_cluster(acc_full, t & 1u, 4 * kPolls + 64 * stages_k);
+      if (!ok) break;
+      tcgen05_fence_after();
+      const unsigned i0 = tile % p.tiles_i * NT, j = tile / p.tiles_i * 256 + rank * 128 + quarter * 32 + lane;
+      const unsigned lanes = tmem + (t & 1u) * S::second + (quarter << 21);
+      // the columns that both accumulators use come first: from kSecond on in the first, the front ones in the second
+      constexpr unsigned shared = NT - S::second;
+      const unsigned first = (t & 1u) ? 0u : S::second % NT;
+      if (shared == 0) {
+        if (lane == 0) mbarrier_arrive_cluster(go);
+      }
+#pragma unroll 1
+      for (unsigned done = 0; done < NT; done += 32) {
+        const unsigned c = (first + done) % NT;
+        unsigned v[32];
+        tmem_read32(lanes + c, v);
+        if (shared > 0 && done + 32 == shared) {
+          tcgen05_fence_before();
+          __syncwarp();
+          if (lane == 0) mbarrier_arrive_cluster(go);
+        }
+        T* o = static_cast<T*>(p.out) + (size_t)(i0 + c) * p.ldo + j;
+        const unsigned rows = i0 + c < p.M ? min(32u, p.M - (i0 + c)) : 0u;
+        if (j < p.N) {
+          if (rows == 32) {
+#pragma unroll
+            for (unsigned q = 0; q < 32; ++q) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+          } else {
+#pragma unroll
+            for (unsigned q = 0; q < 32; ++q)
+              if (q < rows) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+          }
+        }
+        __syncwarp();
+      }
+      tcgen05_fence_before();
+    }
+  }
+  if (!ok) atomicExch(&failed, 1u);
+  __syncwarp();
+  __syncthreads();
+  if (failed && threadIdx.x == 0) {
+    // copies that were asked for, here and by the other CTA, have to land before the memory is given up
+    atomicOr(p.status, 1u);
+    if (rank == 0)
+      for (unsigned m = n > S::stages ? n - S::stages : 0; m < n; ++m)
+        (void)mbarrier_wait_cluster(full + 8 * (m % S::stages), (m / S::stages) & 1u, kPolls);
+  }
+  __syncthreads();
+  cluster_sync();
+  if (warp == 1) {
+    tcgen05_fence_after();
+    tmem_free_pair(tmem, 512);
   }
 }
 
@@ -241,6 +447,16 @@ bool code_map(CUtensorMap* map, const uint8_t* codes, size_t rows, size_t row_by
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Scale tiles as a matrix of 64-bit words, a tile of 512 bytes 64 of them, in boxes of box_tiles x box_rows tiles.
+bool scale_map(CUtensorMap* map, const uint8_t* scales, size_t row_tiles, size_t tiles_k, unsigned box_tiles, unsigned box_rows) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const cuuint64_t dims[2] = {tiles_k * 64, row_tiles}, strides[1] = {tiles_k * 512};
+  const cuuint32_t box[2] = {box_tiles * 64, box_rows}, steps[2] = {1, 1};
+  return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT64, 2, const_cast<uint8_t*>(scales), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int FORMAT, int NT>
 ssgd_status launch_product(const CUtensorMap& a_map, const CUtensorMap& b_map, const ProductArgs& p, unsigned tiles, unsigned splits, cudaStream_t s) {
   using S = Shape<FORMAT, NT>;
@@ -263,38 +479,96 @@ ssgd_status launch_product(const CUtensorMap& a_map, const CUtensorMap& b_map, c
   return launch_status();
 }
 
+struct Operands {
+  const uint8_t *a, *a_scales, *b, *b_scales;
+  const float *a_ts, *b_ts;
+  size_t M, N, K;
+  void* out;
+  int dtype;
+  size_t ldo;
+  unsigned* status;
+};
+
 template <int FORMAT>
-ssgd_status product(const uint8_t* a, const uint8_t* as, const float* ats, const uint8_t* b, const uint8_t* bs, const float* bts, size_t M,
-                    size_t N, size_t K, void* out, int dtype, size_t ldo, unsigned* status, cudaStream_t s) {
-  DeviceInfo info;
-  if (!device_info(&info)) return SSGD_ERR_CUDA;
-  const size_t row_bytes = ssgd_fp4_row_bytes(K);
-  // widest tile that A's rows fill, 256 only where it still leaves every SM a tile
-  const size_t tiles_j = (N + kTileJ - 1) / kTileJ;
-  unsigned nt = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
-  const size_t tiles_i = (M + nt - 1) / nt;
-  if (tiles_j * tiles_i > (size_t)1 << 27) return SSGD_ERR_SIZE;
-  const unsigned tiles = (unsigned)(tiles_j * tiles_i);
-  const unsigned stages_k = (unsigned)((row_bytes + 127) / 128);
+ssgd_status product(const Operands& o, int sms, cudaStream_t s) {
+  const size_t row_bytes = ssgd_fp4_row_bytes(o.K);
+  const unsigned nt = o.M <= 16 ? 16 : o.M <= 32 ? 32 : o.M <= 64 ? 64 : 128;
+  const size_t tiles_i = (o.M + nt - 1) / nt, all = (o.N + kTileJ - 1) / kTileJ * tiles_i;
+  if (all > (size_t)1 << 27) return SSGD_ERR_SIZE;
+  const unsigned tiles = (unsigned)all, stages_k = (unsigned)((row_bytes + 127) / 128);
   unsigned splits = 1;
-  while (splits < 8 && tiles * splits * 2 <= (unsigned)info.sms && splits * 2 <= stages_k) splits *= 2;
+  while (splits < 8 && tiles * splits * 2 <= (unsigned)sms && splits * 2 <= stages_k) splits *= 2;
   CUtensorMap a_map, b_map;
-  if (!code_map(&a_map, a, M, row_bytes, nt) || !code_map(&b_map, b, N, row_bytes, kTileJ)) return SSGD_ERR_CUDA;
+  if (!code_map(&a_map, o.a, o.M, row_bytes, nt) || !code_map(&b_map, o.b, o.N, row_bytes, kTileJ)) return SSGD_ERR_CUDA;
   ProductArgs p;
-  p.a_scales = as; p.b_scales = bs; p.a_ts = ats; p.b_ts = bts; p.out = out; p.status = status; p.ldo = ldo;
-  p.M = (unsigned)M; p.N = (unsigned)N;
+  p.a_scales = o.a_scales; p.b_scales = o.b_scales; p.a_ts = o.a_ts; p.b_ts = o.b_ts; p.out = o.out; p.status = o.status; p.ldo = o.ldo;
+  p.M = (unsigned)o.M; p.N = (unsigned)o.N;
   p.k_chunks = (unsigned)((row_bytes + 31) / 32);
-  p.tiles_k = (unsigned)((fp4_block_count(FORMAT, K) + 3) / 4);
-  p.a_row_tiles = (unsigned)((M + 127) / 128);
+  p.tiles_k = (unsigned)((fp4_block_count(FORMAT, o.K) + 3) / 4);
+  p.a_row_tiles = (unsigned)((o.M + 127) / 128);
   p.tiles_i = (unsigned)tiles_i;
-  p.dtype = dtype;
+  p.dtype = o.dtype;
   switch (nt) {
     case 16: return launch_product<FORMAT, 16>(a_map, b_map, p, tiles, splits, s);
     case 32: return launch_product<FORMAT, 32>(a_map, b_map, p, tiles, splits, s);
     case 64: return launch_product<FORMAT, 64>(a_map, b_map, p, tiles, splits, s);
-    case 128: return launch_product<FORMAT, 128>(a_map, b_map, p, tiles, splits, s);
-    default: return launch_product<FORMAT, 256>(a_map, b_map, p, tiles, splits, s);
+    default: return launch_product<FORMAT, 128>(a_map, b_map, p, tiles, splits, s);
   }
+}
+
+template <int FORMAT, int NT, typename T>
+ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
+  using S = PairShape<FORMAT, NT>;
+  const size_t row_bytes = ssgd_fp4_row_bytes(o.K), tiles_k = (fp4_block_count(FORMAT, o.K) + 3) / 4;
+  const size_t tiles_i = (o.M + NT - 1) / NT, tiles = (o.N + 255) / 256 * tiles_i;
+  if (tiles > kMaxGrid) return SSGD_ERR_SIZE;
+  CUtensorMap a_map, b_map, a_scale_map, b_scale_map;
+  if (!code_map(&a_map, o.a, o.M, row_bytes, NT / 2) || !code_map(&b_map, o.b, o.N, row_bytes, 128) ||
+      !scale_map(&a_scale_map, o.a_scales, (o.M + 127) / 128, tiles_k, S::blocks, S::row_tiles) ||
+      !scale_map(&b_scale_map, o.b_scales, (o.N + 127) / 128, tiles_k, S::blocks, 1))
+    return SSGD_ERR_CUDA;
+  PairArgs p;
+  p.a_ts = o.a_ts; p.b_ts = o.b_ts; p.out = o.out; p.status = o.status; p.ldo = o.ldo;
+  p.M = (unsigned)o.M; p.N = (unsigned)o.N;
+  p.k_chunks = (unsigned)((row_bytes + 31) / 32);
+  p.tiles_i = (unsigned)tiles_i;
+  p.tiles = (unsigned)tiles;
+  auto kernel = fp4_matmul_pair_kernel<FORMAT, NT, T>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem) != cudaSuccess) return SSGD_ERR_CUDA;
+  const unsigned pairs = (unsigned)(tiles < (size_t)(sms / 2) ? tiles : (size_t)(sms / 2));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * pairs);
+  cfg.blockDim = dim3(kMmaThreads);
+  cfg.dynamicSmemBytes = S::smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, kernel, a_map, b_map, a_scale_map, b_scale_map, p);
+  return launch_status();
+}
+
+template <int FORMAT, int NT>
+ssgd_status pair_product(const Operands& o, int sms, cudaStream_t s) {
+  switch (o.dtype) {
+    case SSGD_F32: return launch_pair<FORMAT, NT, float>(o, sms, s);
+    case SSGD_BF16: return launch_pair<FORMAT, NT, __nv_bfloat16>(o, sms, s);
+    default: return launch_pair<FORMAT, NT, __half>(o, sms, s);
+  }
+}
+
+template <int FORMAT>
+ssgd_status any_product(const Operands& o, int sms, cudaStream_t s) {
+  if (o.M <= 128) return product<FORMAT>(o, sms, s);
+  const size_t tiles_j = (o.N + 255) / 256, pairs = (size_t)(sms / 2);
+  if (tiles_j * ((o.M + 255) / 256) >= pairs) return pair_product<FORMAT, 256>(o, sms, s);
+  if (tiles_j * ((o.M + 127) / 128) >= pairs) return pair_product<FORMAT, 128>(o, sms, s);
+  return pair_product<FORMAT, 64>(o, sms, s);
 }
 
 }  // namespace
@@ -318,9 +592,10 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
     const size_t e = dtype_bytes((unsigned)dtype);
     return cudaMemset2DAsync(out, ldo * e, 0, N * e, M, s) == cudaSuccess ? SSGD_OK : SSGD_ERR_CUDA;
   }
-  return format == SSGD_MXFP4
-             ? product<SSGD_MXFP4>(a_codes, a_scales, a_tensor_scale, b_codes, b_scales, b_tensor_scale, M, N, K, out, dtype, ldo, status, s)
-             : product<SSGD_NVFP4>(a_codes, a_scales, a_tensor_scale, b_codes, b_scales, b_tensor_scale, M, N, K, out, dtype, ldo, status, s);
+  DeviceInfo info;
+  if (!device_info(&info)) return SSGD_ERR_CUDA;
+  const Operands o = {a_codes, a_scales, b_codes, b_scales, a_tensor_scale, b_tensor_scale, M, N, K, out, dtype, ldo, status};
+  return format == SSGD_MXFP4 ? any_product<SSGD_MXFP4>(o, info.sms, s) : any_product<SSGD_NVFP4>(o, info.sms, s);
 }
 
 }  // extern "C"

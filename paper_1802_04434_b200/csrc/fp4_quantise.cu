@@ -15,39 +15,47 @@ __device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_
 // Largest magnitude of a matrix, as ordered bits (NaN above infinity); `out` starts at 0.  A maximum does not depend on
 // the order, so the atomic gives the same bits every time.
 template <typename T>
-__device__ __forceinline__ unsigned matrix_amax(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec,
-                                                unsigned first, unsigned step) {
+__device__ __forceinline__ unsigned piece_amax(const T* __restrict__ at, unsigned left, bool vec) {
   constexpr unsigned V = 16 / sizeof(T);
   unsigned top = 0;
-  if (vec) {
-    const unsigned per_row = (cols + V - 1) / V;
-    const size_t total = (size_t)rows * per_row;
-#pragma unroll 4
-    for (size_t i = first; i < total; i += step) {
-      const unsigned r = (unsigned)(i / per_row), c = (unsigned)(i % per_row) * V;
-      const T* at = x + (size_t)r * ldx + c;
-      if (c + V <= cols) {
-        const uint4 q = *reinterpret_cast<const uint4*>(at);
-        const T* e = reinterpret_cast<const T*>(&q);
+  if (vec && left >= V) {
+    const uint4 q = *reinterpret_cast<const uint4*>(at);
+    const unsigned* w = reinterpret_cast<const unsigned*>(&q);
 #pragma unroll
-        for (unsigned j = 0; j < V; ++j) top = max(top, magnitude_bits(to_float(e[j])));
-      } else {
-        for (unsigned j = 0; c + j < cols; ++j) top = max(top, magnitude_bits(to_float(at[j])));
-      }
+    for (int j = 0; j < 4; ++j) {
+      top = max(top, magnitude_bits(low_to_float(T(), w[j])));
+      if (sizeof(T) == 2) top = max(top, magnitude_bits(high_to_float(T(), w[j])));
     }
   } else {
-    const size_t total = (size_t)rows * cols;
-#pragma unroll 8
-    for (size_t i = first; i < total; i += step)
-      top = max(top, magnitude_bits(to_float(x[i / cols * ldx + i % cols])));
+    for (unsigned j = 0; j < V && j < left; ++j) top = max(top, magnitude_bits(to_float(at[j])));
   }
   return top;
 }
 
+// A CTA takes a rectangle of kAmaxRows rows by 256 pieces of 16 bytes, eight pieces of a thread in flight; rows that are
+// not 16-byte aligned are read element by element, lanes side by side.
+constexpr unsigned kAmaxRows = 8;
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, unsigned* __restrict__ out) {
-  const unsigned top = __reduce_max_sync(0xFFFFFFFFu, matrix_amax(x, rows, cols, ldx, vec, blockIdx.x * kThreads + threadIdx.x, gridDim.x * kThreads));
+fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, unsigned tiles_c, unsigned* __restrict__ out) {
+  constexpr unsigned V = 16 / sizeof(T), WIDE = kThreads * V;
+  const unsigned r0 = blockIdx.x / tiles_c * kAmaxRows, c0 = blockIdx.x % tiles_c * WIDE;
+  unsigned top = 0;
+  if (vec) {
+    const unsigned c = c0 + threadIdx.x * V;
+#pragma unroll
+    for (unsigned r = 0; r < kAmaxRows; ++r)
+      if (r0 + r < rows && c < cols) top = max(top, piece_amax(x + (size_t)(r0 + r) * ldx + c, cols - c, true));
+  } else {
+#pragma unroll 2
+    for (unsigned r = 0; r < kAmaxRows; ++r)
+#pragma unroll
+      for (unsigned q = 0; q < V; ++q) {
+        const unsigned c = c0 + q * kThreads + threadIdx.x;
+        if (r0 + r < rows && c < cols) top = max(top, magnitude_bits(to_float(x[(size_t)(r0 + r) * ldx + c])));
+      }
+  }
+  top = __reduce_max_sync(0xFFFFFFFFu, top);
   __shared__ unsigned part[kThreads / 32];
   if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = top;
   __syncthreads();
@@ -55,6 +63,20 @@ fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ld
     const unsigned all = __reduce_max_sync(0xFFFFFFFFu, threadIdx.x < kThreads / 32 ? part[threadIdx.x] : 0u);
     if (threadIdx.x == 0) atomicMax(out, all);
   }
+}
+
+// Largest magnitude of a small matrix, by one CTA.
+template <typename T>
+__device__ __forceinline__ unsigned small_amax(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec) {
+  constexpr unsigned V = 16 / sizeof(T);
+  const unsigned pieces = (cols + V - 1) / V, total = rows * pieces;
+  unsigned top = 0;
+#pragma unroll 4
+  for (unsigned i = threadIdx.x; i < total; i += kThreads) {
+    const unsigned r = i / pieces, c = i % pieces * V;
+    top = max(top, piece_amax(x + (size_t)r * ldx + c, cols - c, vec));
+  }
+  return top;
 }
 
 // x / s rounded to nearest, from the correctly rounded reciprocal r of s: one Newton correction of the product
@@ -195,7 +217,7 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
     if (amax) {
       top = __ldg(amax);
     } else {
-      const unsigned t = __reduce_max_sync(0xFFFFFFFFu, matrix_amax(x, rows, cols, ldx, vec, threadIdx.x, kThreads));
+      const unsigned t = __reduce_max_sync(0xFFFFFFFFu, small_amax(x, rows, cols, ldx, vec));
       if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = t;
       __syncthreads();
       unsigned all = 0;
@@ -291,51 +313,76 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
   }
 }
 
-// Eight values per thread, at places where the stores are 16-byte aligned: row by row the first group starts up to
-// seven columns before the row, and a group's codes are cut out of two words.
+// Eight values per thread and group, at places where the stores are 16-byte aligned: row by row the first group starts up
+// to seven columns before the row, and a group's codes are cut out of two words.  A CTA takes kGroups x 256 groups from
+// its place in the sequence of all rows' groups; the one 64-bit division is the CTA's.
+constexpr unsigned kGroups = 4;
+
 template <int FORMAT, typename T>
 __global__ void __launch_bounds__(kThreads)
 fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ tensor_scale,
                       unsigned rows, unsigned cols, T* __restrict__ out, size_t ldo, unsigned groups) {
   constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, V = 16 / sizeof(T);
+  __shared__ unsigned start[2];
+  if (threadIdx.x == 0) {
+    const size_t first = (size_t)blockIdx.x * (kThreads * kGroups);
+    start[0] = (unsigned)(first / groups);
+    start[1] = (unsigned)(first % groups);
+  }
+  __syncthreads();
   pdl_launch_dependents();
   pdl_wait();
   const float ts = FORMAT == SSGD_NVFP4 && tensor_scale ? __ldg(tensor_scale) : 1.0f;
   const unsigned row_words = (cols + 31) / 32 * 4;
-  const size_t tiles_k = ((cols + B - 1) / B + 3) / 4, total = (size_t)rows * groups;
-  const size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= total) return;
-  const unsigned row = (unsigned)(i / groups), g = (unsigned)(i % groups);
-  T* line = out + (size_t)row * ldo;
-  const unsigned back = (unsigned)(reinterpret_cast<uintptr_t>(line) / sizeof(T)) & (V - 1);   // columns before the row that complete 16 bytes
-  const int c = (int)(g * 8) - (int)back;                                                      // first column of the group
-  if (c >= (int)cols) return;
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(codes) + (size_t)row * row_words;
-  const int w = c >> 3;                                                                        // rounds down
-  const unsigned shift = ((unsigned)c & 7u) * 4;
-  const unsigned lo = w >= 0 ? words[w] : 0u, hi = shift && (unsigned)(w + 1) < row_words ? words[w + 1] : 0u;
-  const unsigned eight = __funnelshift_r(lo, hi, shift);
-  const unsigned b0 = (unsigned)max(c, 0) / B, b1 = min((unsigned)(c + 7), cols - 1) / B;
-  const float s0 = __fmul_rn(fp4_scale_value<FORMAT>(scales[fp4_scale_index(row, b0, tiles_k)]), ts);
-  const float s1 = b1 == b0 ? s0 : __fmul_rn(fp4_scale_value<FORMAT>(scales[fp4_scale_index(row, b1, tiles_k)]), ts);
-  float v[8];
+  const size_t tiles_k = ((cols + B - 1) / B + 3) / 4;
+  T* line[kGroups];
+  int column[kGroups];
+  unsigned lo[kGroups], hi[kGroups], byte0[kGroups], byte1[kGroups];
 #pragma unroll
-  for (int j = 0; j < 8; j += 2) {
-    const float2 two = fp4_pair_value(eight >> (4 * j));
-    v[j] = __fmul_rn(two.x, (unsigned)(c + j) / B == b0 || c + j < 0 ? s0 : s1);
-    v[j + 1] = __fmul_rn(two.y, (unsigned)(c + j + 1) / B == b0 || c + j + 1 < 0 ? s0 : s1);
-  }
-  if (c >= 0 && c + 8 <= (int)cols) {
-    if constexpr (sizeof(T) == 4) {
-      store4(line + c, make_float4(v[0], v[1], v[2], v[3]));
-      store4(line + c + 4, make_float4(v[4], v[5], v[6], v[7]));
-    } else {
-      __stcs(reinterpret_cast<uint4*>(line + c), make_uint4(pack2(T(), v[0], v[1]), pack2(T(), v[2], v[3]), pack2(T(), v[4], v[5]), pack2(T(), v[6], v[7])));
+  for (unsigned u = 0; u < kGroups; ++u) {
+    const unsigned from = start[1] + u * kThreads + threadIdx.x, row = start[0] + from / groups;
+    line[u] = out + (size_t)row * ldo;
+    const unsigned back = (unsigned)(reinterpret_cast<uintptr_t>(line[u]) / sizeof(T)) & (V - 1);   // columns before the row that complete 16 bytes
+    const int c = (int)(from % groups * 8) - (int)back;                                              // first column of the group
+    column[u] = row < rows ? c : (int)cols;
+    lo[u] = hi[u] = byte0[u] = byte1[u] = 0;
+    if (row < rows && c < (int)cols) {
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(codes) + (size_t)row * row_words;
+      const int w = c >> 3;                                                                          // rounds down
+      if (w >= 0) lo[u] = words[w];
+      if (((unsigned)c & 7u) && (unsigned)(w + 1) < row_words) hi[u] = words[w + 1];
+      const unsigned b0 = (unsigned)max(c, 0) / B, b1 = min((unsigned)(c + 7), cols - 1) / B;
+      byte0[u] = scales[fp4_scale_index(row, b0, tiles_k)];
+      byte1[u] = b1 == b0 ? byte0[u] : scales[fp4_scale_index(row, b1, tiles_k)];
     }
-  } else {
+  }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j >= 0 && c + j < (int)cols) line[c + j] = from_float<T>(v[j]);
+  for (unsigned u = 0; u < kGroups; ++u) {
+    const int c = column[u];
+    if (c >= (int)cols) continue;
+    const unsigned eight = __funnelshift_r(lo[u], hi[u], ((unsigned)c & 7u) * 4);
+    const float s0 = __fmul_rn(fp4_scale_value<FORMAT>(byte0[u]), ts), s1 = __fmul_rn(fp4_scale_value<FORMAT>(byte1[u]), ts);
+    const int change = (max(c, 0) / (int)B + 1) * (int)B - c;           // the group's place from which the second scale holds
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      const float2 two = fp4_pair_value(eight >> (4 * j));
+      v[j] = __fmul_rn(two.x, j < change ? s0 : s1);
+      v[j + 1] = __fmul_rn(two.y, j + 1 < change ? s0 : s1);
+    }
+    T* o = line[u] + c;
+    if (c >= 0 && c + 8 <= (int)cols) {
+      if constexpr (sizeof(T) == 4) {
+        store4(o, make_float4(v[0], v[1], v[2], v[3]));
+        store4(o + 4, make_float4(v[4], v[5], v[6], v[7]));
+      } else {
+        __stcs(reinterpret_cast<uint4*>(o), make_uint4(pack2(T(), v[0], v[1]), pack2(T(), v[2], v[3]), pack2(T(), v[4], v[5]), pack2(T(), v[6], v[7])));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j >= 0 && c + j < (int)cols) o[j] = from_float<T>(v[j]);
+    }
   }
 }
 
@@ -362,11 +409,10 @@ ssgd_status quantise_typed(const T* x, size_t rows, size_t cols, size_t ldx, con
                            uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, cudaStream_t s) {
   if (FORMAT == SSGD_NVFP4 && !amax && rows * cols > kFusedAmax) {
     if (cudaMemsetAsync(tensor_scale + 1, 0, sizeof(float), s) != cudaSuccess) return SSGD_ERR_CUDA;
-    DeviceInfo info;
-    if (!device_info(&info)) return SSGD_ERR_CUDA;
-    const size_t want = (rows * cols + kThreads * 32 - 1) / (kThreads * 32), most = (size_t)info.sms * 8;
-    fp4_amax_kernel<<<(unsigned)(want < most ? want : most), kThreads, 0, s>>>(x, (unsigned)rows, (unsigned)cols, ldx, rows_aligned(x, ldx),
-                                                                               reinterpret_cast<unsigned*>(tensor_scale + 1));
+    const size_t wide = kThreads * 16 / sizeof(T), tiles_c = (cols + wide - 1) / wide, ctas = (rows + kAmaxRows - 1) / kAmaxRows * tiles_c;
+    if (ctas > kMaxGrid) return SSGD_ERR_SIZE;
+    fp4_amax_kernel<<<(unsigned)ctas, kThreads, 0, s>>>(x, (unsigned)rows, (unsigned)cols, ldx, rows_aligned(x, ldx), (unsigned)tiles_c,
+                                                        reinterpret_cast<unsigned*>(tensor_scale + 1));
     amax = tensor_scale + 1;
   }
   if (codes && codes_t) return launch_quantise<FORMAT, true, true>(x, rows, cols, ldx, amax, tensor_scale, codes, scales, codes_t, scales_t, s);
@@ -383,7 +429,7 @@ ssgd_status quantise_format(const T* x, size_t rows, size_t cols, size_t ldx, in
 
 template <int FORMAT, typename T>
 ssgd_status launch_dequantise(const uint8_t* codes, const uint8_t* scales, const float* ts, size_t rows, size_t cols, T* out, size_t ldo, cudaStream_t s) {
-  const size_t groups = (cols + 7) / 8 + (rows_aligned(out, rows > 1 ? ldo : 16 / sizeof(T)) ? 0 : 1), ctas = (rows * groups + kThreads - 1) / kThreads;
+  const size_t groups = (cols + 7) / 8 + (rows_aligned(out, rows > 1 ? ldo : 16 / sizeof(T)) ? 0 : 1), ctas = (rows * groups + kThreads * kGroups - 1) / (kThreads * kGroups);
   if (ctas > kMaxGrid) return SSGD_ERR_SIZE;
   launch_kernel(fp4_dequantise_kernel<FORMAT, T>, dim3((unsigned)ctas), dim3(kThreads), 0, s, true, codes, scales, ts, (unsigned)rows, (unsigned)cols,
                 out, ldo, (unsigned)groups);
