@@ -107,7 +107,7 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
   unsigned issued = 0;                          // stages that this thread has asked for
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect_one()) {
       const unsigned jt = j0 / 128, it = i0 / 128;
       for (unsigned k = first; k < last && ok; ++k) {
         const unsigned n = k - first, s = n % S::stages;
@@ -127,7 +127,7 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (elect_one()) {
       for (unsigned k = first; k < last && ok; ++k) {
         const unsigned n = k - first, s = n % S::stages;
         ok = mbarrier_wait(full + 8 * s, (n / S::stages) & 1u, kPolls);
@@ -184,8 +184,8 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
   __syncthreads();
   if (failed) {
     // copies that were asked for have to land before the CTA gives its memory up
-    if (threadIdx.x == 0) {
-      atomicOr(p.status, 1u);
+    if (threadIdx.x == 0) atomicOr(p.status, 1u);
+    if (issued > 0) {
       for (unsigned n = issued > S::stages ? issued - S::stages : 0; n < issued; ++n)
         (void)mbarrier_wait(full + 8 * (n % S::stages), (n / S::stages) & 1u, kPolls);
     }
@@ -241,7 +241,8 @@ struct PairShape {
   static constexpr unsigned stage_bytes = (loaded + 1023) / 1024 * 1024;
   static constexpr unsigned stages = 225280 / stage_bytes < 8 ? 225280 / stage_bytes : 8;
   static constexpr unsigned scale_columns = (1 + row_tiles) * blocks * 4;
-  static constexpr unsigned first_scale = 512 - 2 * scale_columns;
+  static constexpr unsigned ring = 2;
+  static constexpr unsigned first_scale = 512 - ring * scale_columns;
   static constexpr unsigned room = (first_scale - NT) / 32 * 32;
   static constexpr unsigned second = room < NT ? room : NT;              // column of the second accumulator
   static constexpr unsigned smem = stages * stage_bytes + 1024;
@@ -299,7 +300,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
   unsigned n = 0;                               // stages so far, over all tiles
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect_one()) {
       for (unsigned tile = pair; tile < p.tiles && ok; tile += pairs) {
         const unsigned i0 = tile % p.tiles_i * NT, j0 = tile / p.tiles_i * 256 + rank * 128;
         for (unsigned k = 0; k < stages_k; ++k, ++n) {
@@ -320,7 +321,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
         ok = mbarrier_wait_cluster(empty + 8 * (m % S::stages), (m / S::stages) & 1u, kPolls);
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0 && elect_one()) {
       unsigned t = 0;                           // tiles so far
       for (unsigned tile = pair; tile < p.tiles && ok; tile += pairs, ++t) {
         if (t > 0) ok = mbarrier_wait_cluster(acc_free, (t - 1) & 1u, kPolls);
@@ -331,11 +332,11 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
         for (unsigned k = 0; k < stages_k; ++k, ++n) {
           const unsigned s = n % S::stages;
           ok = mbarrier_wait_cluster(full + 8 * s, (n / S::stages) & 1u, kPolls) &&
-               (n < 2 || mbarrier_wait_cluster(empty + 8 * ((n - 2) % S::stages), ((n - 2) / S::stages) & 1u, kPolls));
+               (n < S::ring || mbarrier_wait_cluster(empty + 8 * ((n - S::ring) % S::stages), ((n - S::ring) / S::stages) & 1u, kPolls));
           if (!ok) break;
           tcgen05_fence_after();
           const unsigned base = stage0 + s * S::stage_bytes, sc = base + S::b_bytes + S::a_bytes;
-          const unsigned columns = tmem + S::first_scale + (n & 1u) * S::scale_columns;
+          const unsigned columns = tmem + S::first_scale + n % S::ring * S::scale_columns;
           const unsigned chunks = min(4u, p.k_chunks - k * 4);
 #pragma unroll
           for (unsigned q = 0; q < S::blocks; ++q) {
@@ -404,10 +405,10 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
   if (!ok) atomicExch(&failed, 1u);
   __syncwarp();
   __syncthreads();
-  if (failed && threadIdx.x == 0) {
+  if (failed) {
     // copies that were asked for, here and by the other CTA, have to land before the memory is given up
-    atomicOr(p.status, 1u);
-    if (rank == 0)
+    if (threadIdx.x == 0) atomicOr(p.status, 1u);
+    if (rank == 0 && warp == 0)
       for (unsigned m = n > S::stages ? n - S::stages : 0; m < n; ++m)
         (void)mbarrier_wait_cluster(full + 8 * (m % S::stages), (m / S::stages) & 1u, kPolls);
   }
