@@ -223,11 +223,15 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Many rows on both sides: persistent pairs of CTAs (cta_group::2), each pair a tile of 256 rows of B by NT rows of A.  A
-// CTA loads 128 rows of B and half of the rows of A, so an operand byte that reaches shared memory serves 256 rows instead
-// of 128, and what bounds the product, bytes from L2 to shared memory, is a third less than with single CTAs.
+// Many rows on both sides: persistent pairs of CTAs (cta_group::2), each pair a tile of 256 rows of one operand, P (the
+// accumulator's lanes), by NT rows of the other, Q (its columns).  A CTA loads 128 rows of P and half of the rows of Q, so an
+// operand byte that reaches shared memory serves 256 rows instead of 128, and the bytes from L2 to shared memory are a third
+// less than with single CTAs.
+//   WIDE           P = A, Q = B: a lane holds neighbours of one row of out and stores 32 bytes at a time; for rows of out that
+//                  start at multiples of 32 bytes.  Otherwise P = B, Q = A: the lanes of a warp hold neighbours, stores of
+//                  one element, coalesced, wherever a row starts
 //   accumulators   two, so that a tile is written out while the next one is multiplied.  Both and the scales' columns do not
-//                  fit beside one another at NT = 256: the second starts at kSecond < NT, the epilogue drains the shared
+//                  fit beside one another at NT = 256: the second starts at `second` < NT, the epilogue drains the shared
 //                  columns first and gives the go-ahead after them
 //   scales         two sets of columns in turn; a set is overwritten when the MMAs that read it are known to be done
 
@@ -235,9 +239,9 @@ template <int FORMAT, int NT>
 struct PairShape {
   static constexpr unsigned blocks = FORMAT == SSGD_MXFP4 ? 2 : 4;
   static constexpr unsigned row_tiles = (NT + 127) / 128;
-  static constexpr unsigned b_bytes = 128 * 128, a_bytes = NT / 2 * 128;
+  static constexpr unsigned p_bytes = 128 * 128, q_bytes = NT / 2 * 128;
   static constexpr unsigned scale_bytes = blocks * 512;
-  static constexpr unsigned loaded = b_bytes + a_bytes + (1 + row_tiles) * scale_bytes;     // per CTA and stage
+  static constexpr unsigned loaded = p_bytes + q_bytes + (1 + row_tiles) * scale_bytes;     // per CTA and stage
   static constexpr unsigned stage_bytes = (loaded + 1023) / 1024 * 1024;
   static constexpr unsigned stages = 225280 / stage_bytes < 8 ? 225280 / stage_bytes : 8;
   static constexpr unsigned scale_columns = (1 + row_tiles) * blocks * 4;
@@ -250,18 +254,33 @@ struct PairShape {
 };
 
 struct PairArgs {
-  const float* a_ts;
-  const float* b_ts;
+  const float* p_ts;
+  const float* q_ts;
   void* out;
   unsigned* status;
   size_t ldo;
-  unsigned M, N, k_chunks, tiles_i, tiles;
+  unsigned P, Q, k_chunks, tiles_p, tiles_q;    // rows and tiles of either side
 };
 
-template <int FORMAT, int NT, typename T>
+// Tiles go through bands of eight of P's tiles, so that those in flight share rows of both operands.
+struct TilePlace { unsigned p0, q0; };
+template <int NT>
+__device__ __forceinline__ TilePlace tile_place(unsigned tile, const PairArgs& a) {
+  constexpr unsigned kBand = 8;
+  const unsigned band = tile / (kBand * a.tiles_q), in = tile - band * kBand * a.tiles_q, high = min(kBand, a.tiles_p - band * kBand);
+  return {(band * kBand + in % high) * 256, in / high * NT};
+}
+
+__device__ __forceinline__ void store32(void* at, const unsigned* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
+template <int FORMAT, int NT, typename T, bool WIDE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
-fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
-                       const __grid_constant__ CUtensorMap a_scale_map, const __grid_constant__ CUtensorMap b_scale_map, const PairArgs p) {
+fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_constant__ CUtensorMap q_map,
+                       const __grid_constant__ CUtensorMap p_scale_map, const __grid_constant__ CUtensorMap q_scale_map, const PairArgs p) {
   using S = PairShape<FORMAT, NT>;
   constexpr bool kE8M0 = FORMAT == SSGD_MXFP4;
   extern __shared__ unsigned char dynamic_smem[];
@@ -272,13 +291,13 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
   const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 8;
   const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const unsigned stages_k = (p.k_chunks + 3) / 4;
-  const unsigned pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+  const unsigned pair = blockIdx.x / 2, pairs = gridDim.x / 2, tiles = p.tiles_p * p.tiles_q;
 
   if (threadIdx.x == 0) {
-    prefetch_tensor_map(&a_map);
-    prefetch_tensor_map(&b_map);
-    prefetch_tensor_map(&a_scale_map);
-    prefetch_tensor_map(&b_scale_map);
+    prefetch_tensor_map(&q_map);
+    prefetch_tensor_map(&p_map);
+    prefetch_tensor_map(&q_scale_map);
+    prefetch_tensor_map(&p_scale_map);
     for (unsigned s = 0; s < S::stages; ++s) {
       mbarrier_init(full + 8 * s, 1);
       mbarrier_init(empty + 8 * s, 1);
@@ -301,41 +320,42 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
 
   if (warp == 0) {
     if (elect_one()) {
-      for (unsigned tile = pair; tile < p.tiles && ok; tile += pairs) {
-        const unsigned i0 = tile % p.tiles_i * NT, j0 = tile / p.tiles_i * 256 + rank * 128;
+      for (unsigned tile = pair; tile < tiles && ok; tile += pairs) {
+        const TilePlace at = tile_place<NT>(tile, p);
+        const unsigned p0 = at.p0 + rank * 128, q0 = at.q0;
         for (unsigned k = 0; k < stages_k; ++k, ++n) {
           const unsigned s = n % S::stages;
-          if (n >= S::stages) ok = mbarrier_wait_cluster(empty + 8 * s, (n / S::stages - 1) & 1u, kPolls);
+          if (n >= S::stages) ok = mbarrier_wait(empty + 8 * s, (n / S::stages - 1) & 1u, kPolls);
           if (!ok) break;
           const unsigned base = stage0 + s * S::stage_bytes, bar = cluster_address(full + 8 * s, 0);
           if (rank == 0) mbarrier_expect(full + 8 * s, 2 * S::loaded);
-          tma_load_2d_pair(base, &b_map, (int)(k * 128), (int)j0, bar);
-          tma_load_2d_pair(base + S::b_bytes, &a_map, (int)(k * 128), (int)(i0 + rank * (NT / 2)), bar);
-          const unsigned sc = base + S::b_bytes + S::a_bytes;
-          tma_load_2d_pair(sc, &b_scale_map, (int)(k * S::blocks * 64), (int)(j0 / 128), bar);
-          tma_load_2d_pair(sc + S::scale_bytes, &a_scale_map, (int)(k * S::blocks * 64), (int)(i0 / 128), bar);
+          tma_load_2d_pair(base, &p_map, (int)(k * 128), (int)p0, bar);
+          tma_load_2d_pair(base + S::p_bytes, &q_map, (int)(k * 128), (int)(q0 + rank * (NT / 2)), bar);
+          const unsigned sc = base + S::p_bytes + S::q_bytes;
+          tma_load_2d_pair(sc, &p_scale_map, (int)(k * S::blocks * 64), (int)(p0 / 128), bar);
+          tma_load_2d_pair(sc + S::scale_bytes, &q_scale_map, (int)(k * S::blocks * 64), (int)(q0 / 128), bar);
         }
       }
       // the last stages' commits have to arrive before this CTA may go
       for (unsigned m = n > S::stages ? n - S::stages : 0; m < n && ok; ++m)
-        ok = mbarrier_wait_cluster(empty + 8 * (m % S::stages), (m / S::stages) & 1u, kPolls);
+        ok = mbarrier_wait(empty + 8 * (m % S::stages), (m / S::stages) & 1u, kPolls);
     }
   } else if (warp == 1) {
     if (rank == 0 && elect_one()) {
       unsigned t = 0;                           // tiles so far
-      for (unsigned tile = pair; tile < p.tiles && ok; tile += pairs, ++t) {
+      for (unsigned tile = pair; tile < tiles && ok; tile += pairs, ++t) {
         if (t > 0) ok = mbarrier_wait_cluster(acc_free, (t - 1) & 1u, kPolls);
         if (!ok) break;
         tcgen05_fence_after();
         const unsigned d = tmem + (t & 1u) * S::second;
-        const unsigned half = (tile % p.tiles_i * NT % 128) / 32;        // NT = 64: where its rows' scales begin in their tile
+        const unsigned half = tile_place<NT>(tile, p).q0 % 128 / 32;           // NT = 64: where its rows' scales begin in their tile
         for (unsigned k = 0; k < stages_k; ++k, ++n) {
           const unsigned s = n % S::stages;
-          ok = mbarrier_wait_cluster(full + 8 * s, (n / S::stages) & 1u, kPolls) &&
-               (n < S::ring || mbarrier_wait_cluster(empty + 8 * ((n - S::ring) % S::stages), ((n - S::ring) / S::stages) & 1u, kPolls));
+          ok = mbarrier_wait(full + 8 * s, (n / S::stages) & 1u, kPolls) &&
+               (n < S::ring || mbarrier_wait(empty + 8 * ((n - S::ring) % S::stages), ((n - S::ring) / S::stages) & 1u, kPolls));
           if (!ok) break;
           tcgen05_fence_after();
-          const unsigned base = stage0 + s * S::stage_bytes, sc = base + S::b_bytes + S::a_bytes;
+          const unsigned base = stage0 + s * S::stage_bytes, sc = base + S::p_bytes + S::q_bytes;
           const unsigned columns = tmem + S::first_scale + n % S::ring * S::scale_columns;
           const unsigned chunks = min(4u, p.k_chunks - k * 4);
 #pragma unroll
@@ -346,10 +366,10 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
               tcgen05_copy_scales_pair(columns + S::blocks * 4 + (q * S::row_tiles + r) * 4,
                                        smem_descriptor(sc + (1 + r) * S::scale_bytes + q * 512, 128, 0));
           }
-          const uint64_t b_desc = smem_descriptor(base, 1024, 2), a_desc = smem_descriptor(base + S::b_bytes, 1024, 2);
+          const uint64_t p_desc = smem_descriptor(base, 1024, 2), q_desc = smem_descriptor(base + S::p_bytes, 1024, 2);
           for (unsigned c = 0; c < chunks; ++c) {
             const unsigned q = kE8M0 ? c / 2 : c, id = kE8M0 ? (c & 1u) * 2 : 0;
-            mma_fp4_pair<kE8M0>(d, b_desc + 2 * c, a_desc + 2 * c, mma_fp4_descriptor(256, NT, kE8M0, id), columns + q * 4,
+            mma_fp4_pair<kE8M0>(d, p_desc + 2 * c, q_desc + 2 * c, mma_fp4_descriptor(256, NT, kE8M0, id), columns + q * 4,
                                 columns + S::blocks * 4 + q * S::row_tiles * 4 + half, k > 0 || c > 0);
           }
           tcgen05_commit_pair(empty + 8 * s);
@@ -360,16 +380,17 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
     }
   } else {
     const unsigned quarter = warp & 3u;
-    const float ts = (p.a_ts ? __ldg(p.a_ts) : 1.0f) * (p.b_ts ? __ldg(p.b_ts) : 1.0f);
+    const float ts = (p.p_ts ? __ldg(p.p_ts) : 1.0f) * (p.q_ts ? __ldg(p.q_ts) : 1.0f);
     const unsigned go = cluster_address(acc_free, 0);
     unsigned t = 0;
-    for (unsigned tile = pair; tile < p.tiles; tile += pairs, ++t) {
-      ok = mbarrier_wait_cluster(acc_full, t & 1u, 4 * kPolls + 64 * stages_k);
+    for (unsigned tile = pair; tile < tiles; tile += pairs, ++t) {
+      ok = mbarrier_wait(acc_full, t & 1u, 4 * kPolls + 64 * stages_k);
       if (!ok) break;
       tcgen05_fence_after();
-      const unsigned i0 = tile % p.tiles_i * NT, j = tile / p.tiles_i * 256 + rank * 128 + quarter * 32 + lane;
+      const TilePlace at = tile_place<NT>(tile, p);
+      const unsigned row = at.p0 + rank * 128 + quarter * 32 + lane, q0 = at.q0;       // of P; the first of Q
       const unsigned lanes = tmem + (t & 1u) * S::second + (quarter << 21);
-      // the columns that both accumulators use come first: from kSecond on in the first, the front ones in the second
+      // the columns that both accumulators use come first: from `second` on in the first, the front ones in the second
       constexpr unsigned shared = NT - S::second;
       const unsigned first = (t & 1u) ? 0u : S::second % NT;
       if (shared == 0) {
@@ -385,16 +406,32 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
           __syncwarp();
           if (lane == 0) mbarrier_arrive_cluster(go);
         }
-        T* o = static_cast<T*>(p.out) + (size_t)(i0 + c) * p.ldo + j;
-        const unsigned rows = i0 + c < p.M ? min(32u, p.M - (i0 + c)) : 0u;
-        if (j < p.N) {
-          if (rows == 32) {
+        const unsigned left = q0 + c < p.Q ? min(32u, p.Q - (q0 + c)) : 0u;      // columns of the 32 that exist
+        if (row < p.P) {
+          if constexpr (WIDE) {
+            T* o = static_cast<T*>(p.out) + (size_t)row * p.ldo + q0 + c;
+            if (left == 32) {
+              if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (unsigned q = 0; q < 32; ++q) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+                for (unsigned q = 0; q < 32; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * ts);
+#pragma unroll
+                for (unsigned q = 0; q < 32; q += 8) store32(o + q, v + q);
+              } else {
+#pragma unroll
+                for (unsigned q = 0; q < 16; ++q) v[q] = pack2(T(), __uint_as_float(v[2 * q]) * ts, __uint_as_float(v[2 * q + 1]) * ts);
+                store32(o, v);
+                store32(o + 16, v + 8);
+              }
+            } else {
+#pragma unroll
+              for (unsigned q = 0; q < 32; ++q)
+                if (q < left) o[q] = from_float<T>(__uint_as_float(v[q]) * ts);
+            }
           } else {
+            T* o = static_cast<T*>(p.out) + (size_t)(q0 + c) * p.ldo + row;
 #pragma unroll
             for (unsigned q = 0; q < 32; ++q)
-              if (q < rows) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+              if (q < left) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
           }
         }
         __syncwarp();
@@ -410,7 +447,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_c
     if (threadIdx.x == 0) atomicOr(p.status, 1u);
     if (rank == 0 && warp == 0)
       for (unsigned m = n > S::stages ? n - S::stages : 0; m < n; ++m)
-        (void)mbarrier_wait_cluster(full + 8 * (m % S::stages), (m / S::stages) & 1u, kPolls);
+        (void)mbarrier_wait(full + 8 * (m % S::stages), (m / S::stages) & 1u, kPolls);
   }
   __syncthreads();
   cluster_sync();
@@ -517,25 +554,26 @@ ssgd_status product(const Operands& o, int sms, cudaStream_t s) {
   }
 }
 
-template <int FORMAT, int NT, typename T>
+template <int FORMAT, int NT, typename T, bool WIDE>
 ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
   using S = PairShape<FORMAT, NT>;
   const size_t row_bytes = ssgd_fp4_row_bytes(o.K), tiles_k = (fp4_block_count(FORMAT, o.K) + 3) / 4;
-  const size_t tiles_i = (o.M + NT - 1) / NT, tiles = (o.N + 255) / 256 * tiles_i;
-  if (tiles > kMaxGrid) return SSGD_ERR_SIZE;
-  CUtensorMap a_map, b_map, a_scale_map, b_scale_map;
-  if (!code_map(&a_map, o.a, o.M, row_bytes, NT / 2) || !code_map(&b_map, o.b, o.N, row_bytes, 128) ||
-      !scale_map(&a_scale_map, o.a_scales, (o.M + 127) / 128, tiles_k, S::blocks, S::row_tiles) ||
-      !scale_map(&b_scale_map, o.b_scales, (o.N + 127) / 128, tiles_k, S::blocks, 1))
+  const size_t P = WIDE ? o.M : o.N, Q = WIDE ? o.N : o.M, tiles_p = (P + 255) / 256, tiles_q = (Q + NT - 1) / NT;
+  if (tiles_p * tiles_q > kMaxGrid / 8) return SSGD_ERR_SIZE;
+  CUtensorMap p_map, q_map, p_scale_map, q_scale_map;
+  if (!code_map(&p_map, WIDE ? o.a : o.b, P, row_bytes, 128) || !code_map(&q_map, WIDE ? o.b : o.a, Q, row_bytes, NT / 2) ||
+      !scale_map(&p_scale_map, WIDE ? o.a_scales : o.b_scales, (P + 127) / 128, tiles_k, S::blocks, 1) ||
+      !scale_map(&q_scale_map, WIDE ? o.b_scales : o.a_scales, (Q + 127) / 128, tiles_k, S::blocks, S::row_tiles))
     return SSGD_ERR_CUDA;
   PairArgs p;
-  p.a_ts = o.a_ts; p.b_ts = o.b_ts; p.out = o.out; p.status = o.status; p.ldo = o.ldo;
-  p.M = (unsigned)o.M; p.N = (unsigned)o.N;
+  p.p_ts = o.a_ts; p.q_ts = o.b_ts; p.out = o.out; p.status = o.status; p.ldo = o.ldo;
+  p.P = (unsigned)P; p.Q = (unsigned)Q;
   p.k_chunks = (unsigned)((row_bytes + 31) / 32);
-  p.tiles_i = (unsigned)tiles_i;
-  p.tiles = (unsigned)tiles;
-  auto kernel = fp4_matmul_pair_kernel<FORMAT, NT, T>;
+  p.tiles_p = (unsigned)tiles_p;
+  p.tiles_q = (unsigned)tiles_q;
+  auto kernel = fp4_matmul_pair_kernel<FORMAT, NT, T, WIDE>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem) != cudaSuccess) return SSGD_ERR_CUDA;
+  const size_t tiles = tiles_p * tiles_q;
   const unsigned pairs = (unsigned)(tiles < (size_t)(sms / 2) ? tiles : (size_t)(sms / 2));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * pairs);
@@ -550,26 +588,33 @@ ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  (void)cudaLaunchKernelEx(&cfg, kernel, a_map, b_map, a_scale_map, b_scale_map, p);
+  (void)cudaLaunchKernelEx(&cfg, kernel, p_map, q_map, p_scale_map, q_scale_map, p);
   return launch_status();
 }
 
+template <int FORMAT, int NT, typename T>
+ssgd_status pair_typed(const Operands& o, bool wide, int sms, cudaStream_t s) {
+  return wide ? launch_pair<FORMAT, NT, T, true>(o, sms, s) : launch_pair<FORMAT, NT, T, false>(o, sms, s);
+}
+
 template <int FORMAT, int NT>
-ssgd_status pair_product(const Operands& o, int sms, cudaStream_t s) {
+ssgd_status pair_product(const Operands& o, bool wide, int sms, cudaStream_t s) {
   switch (o.dtype) {
-    case SSGD_F32: return launch_pair<FORMAT, NT, float>(o, sms, s);
-    case SSGD_BF16: return launch_pair<FORMAT, NT, __nv_bfloat16>(o, sms, s);
-    default: return launch_pair<FORMAT, NT, __half>(o, sms, s);
+    case SSGD_F32: return pair_typed<FORMAT, NT, float>(o, wide, sms, s);
+    case SSGD_BF16: return pair_typed<FORMAT, NT, __nv_bfloat16>(o, wide, sms, s);
+    default: return pair_typed<FORMAT, NT, __half>(o, wide, sms, s);
   }
 }
 
 template <int FORMAT>
 ssgd_status any_product(const Operands& o, int sms, cudaStream_t s) {
+  const size_t e = dtype_bytes((unsigned)o.dtype);
+  const bool wide = reinterpret_cast<uintptr_t>(o.out) % 32 == 0 && o.ldo * e % 32 == 0;
   if (o.M <= 128) return product<FORMAT>(o, sms, s);
-  const size_t tiles_j = (o.N + 255) / 256, pairs = (size_t)(sms / 2);
-  if (tiles_j * ((o.M + 255) / 256) >= pairs) return pair_product<FORMAT, 256>(o, sms, s);
-  if (tiles_j * ((o.M + 127) / 128) >= pairs) return pair_product<FORMAT, 128>(o, sms, s);
-  return pair_product<FORMAT, 64>(o, sms, s);
+  const size_t P = wide ? o.M : o.N, Q = wide ? o.N : o.M, tiles_p = (P + 255) / 256, pairs = (size_t)(sms / 2);
+  if (tiles_p * ((Q + 255) / 256) >= pairs) return pair_product<FORMAT, 256>(o, wide, sms, s);
+  if (tiles_p * ((Q + 127) / 128) >= pairs) return pair_product<FORMAT, 128>(o, wide, sms, s);
+  return pair_product<FORMAT, 64>(o, wide, sms, s);
 }
 
 }  // namespace

@@ -144,16 +144,18 @@ __device__ __forceinline__ unsigned cluster_address(unsigned addr, unsigned rank
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// An arrival at a barrier of another CTA that orders tensor memory only (between the two tcgen05 fences): relaxed, since a
+// release would first wait for all of this thread's stores to global memory (a third of the time of a short product).
 __device__ __forceinline__ void mbarrier_arrive_cluster(unsigned cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-// Like mbarrier_wait, for arrivals from the other CTA.
+// Like mbarrier_wait, for such arrivals.
 __device__ __forceinline__ bool mbarrier_wait_cluster(unsigned bar, unsigned parity, unsigned polls) {
   for (unsigned i = 0; i < polls; ++i) {
     unsigned done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
         : "r"(bar), "r"(parity), "r"(1000u)
