@@ -23,8 +23,40 @@
 namespace {
 
 constexpr int kMmaThreads = 192;
+constexpr int kPairThreads = 320;           // copies, MMAs, eight warps that write out
 constexpr unsigned kTileJ = 128;            // rows of B in a tile: lanes of the accumulator
 constexpr unsigned kPolls = 200000;         // bound of a wait, about 0.2 s
+
+// One stage's tensor-core work: its scales to tensor memory (4 columns for each tile of 128 rows x 4 blocks: the lanes'
+// operand first, then for each four blocks the columns' operand's row tiles side by side), then up to four MMAs of 64 of k.
+// Unrolled throughout: a loop over them costs the issuing thread more than the tensor cores take (B200: 530 clocks a
+// stage instead of 356 at NT = 64).
+//   p_desc, q_desc  codes of the lanes' and the columns' operand;  sc_desc  scale tiles, the columns' operand's behind
+//   half            column at which the scales of the columns' operand begin in their tile
+template <int FORMAT, int NT, bool PAIR>
+__device__ __forceinline__ void issue_stage(unsigned d, uint64_t p_desc, uint64_t q_desc, uint64_t sc_desc, unsigned columns, unsigned half,
+                                            unsigned chunks, bool first) {
+  constexpr bool kE8M0 = FORMAT == SSGD_MXFP4;
+  constexpr unsigned blocks = kE8M0 ? 2 : 4, row_tiles = (NT + 127) / 128;
+#pragma unroll
+  for (unsigned q = 0; q < blocks; ++q) {
+#pragma unroll
+    for (unsigned t = 0; t <= row_tiles; ++t) {
+      const unsigned to = columns + (t == 0 ? q * 4 : blocks * 4 + (q * row_tiles + t - 1) * 4);
+      if (PAIR) tcgen05_copy_scales_pair(to, sc_desc + (t * blocks + q) * 32);
+      else tcgen05_copy_scales(to, sc_desc + (t * blocks + q) * 32);
+    }
+  }
+#pragma unroll
+  for (unsigned c = 0; c < 4; ++c) {
+    const unsigned q = kE8M0 ? c / 2 : c, id = kE8M0 ? (c & 1u) * 2 : 0;
+    const unsigned idesc = mma_fp4_descriptor(PAIR ? 256 : 128, NT, kE8M0, id), ps = columns + q * 4, qs = columns + blocks * 4 + q * row_tiles * 4 + half;
+    if (c == 0 || c < chunks) {
+      if (PAIR) mma_fp4_pair<kE8M0>(d, p_desc + 2 * c, q_desc + 2 * c, idesc, ps, qs, c > 0 || !first);
+      else mma_fp4<kE8M0>(d, p_desc + 2 * c, q_desc + 2 * c, idesc, ps, qs, c > 0 || !first);
+    }
+  }
+}
 
 template <int FORMAT, int NT>
 struct Shape {
@@ -128,27 +160,20 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
     }
   } else if (warp == 1) {
     if (elect_one()) {
-      for (unsigned k = first; k < last && ok; ++k) {
-        const unsigned n = k - first, s = n % S::stages;
-        ok = mbarrier_wait(full + 8 * s, (n / S::stages) & 1u, kPolls);
+      const uint64_t p_desc = smem_descriptor(stage0, 1024, 2), q_desc = smem_descriptor(stage0 + S::b_bytes, 1024, 2),
+                     sc_desc = smem_descriptor(stage0 + S::b_bytes + S::a_bytes, 128, 0);
+      bool ready = false;                       // the stage's operands are known to be there
+      for (unsigned k = first, s = 0, parity = 0; k < last; ++k) {
+        ok = ready || mbarrier_wait(full + 8 * s, parity, kPolls);
         if (!ok) break;
         tcgen05_fence_after();
-        const unsigned base = stage0 + s * S::stage_bytes, sc = base + S::b_bytes + S::a_bytes;
-        const unsigned columns = tmem + NT + s * S::scale_columns;
-        const unsigned chunks = min(4u, p.k_chunks - k * 4), blocks = min(S::blocks, p.tiles_k - k * S::blocks);
-        // scales: 4 columns for each tile of 128 rows x 4 blocks; B's, then for each four blocks A's row tiles side by side
-        for (unsigned q = 0; q < blocks; ++q) {
-          tcgen05_copy_scales(columns + q * 4, smem_descriptor(sc + q * 512, 128, 0));
-          for (unsigned t = 0; t < S::row_tiles; ++t)
-            tcgen05_copy_scales(columns + S::blocks * 4 + (q * S::row_tiles + t) * 4, smem_descriptor(sc + (1 + t) * S::scale_bytes + q * 512, 128, 0));
-        }
-        const uint64_t b_desc = smem_descriptor(base, 1024, 2), a_desc = smem_descriptor(base + S::b_bytes, 1024, 2);
-        for (unsigned c = 0; c < chunks; ++c) {
-          const unsigned q = FORMAT == SSGD_MXFP4 ? c / 2 : c, id = FORMAT == SSGD_MXFP4 ? (c & 1u) * 2 : 0;
-          mma_fp4<FORMAT == SSGD_MXFP4>(tmem, b_desc + 2 * c, a_desc + 2 * c, mma_fp4_descriptor(kTileJ, NT, FORMAT == SSGD_MXFP4, id),
-                                        columns + q * 4, columns + S::blocks * 4 + q * S::row_tiles * 4, n > 0 || c > 0);
-        }
+        const unsigned next = s + 1 == S::stages ? 0 : s + 1, next_parity = parity ^ (next == 0);
+        ready = mbarrier_test(full + 8 * next, next_parity);      // its answer comes while this stage is issued
+        const unsigned at = s * (S::stage_bytes >> 4);
+        issue_stage<FORMAT, NT, false>(tmem, p_desc + at, q_desc + at, sc_desc + at, tmem + NT + s * S::scale_columns, 0, p.k_chunks - k * 4, k == first);
         tcgen05_commit(empty + 8 * s);
+        s = next;
+        parity = next_parity;
       }
       if (!ok) atomicExch(&failed, 1u);        // the epilogue looks at it once `done` has come
       tcgen05_commit(done);
@@ -233,7 +258,8 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
 //   accumulators   two, so that a tile is written out while the next one is multiplied.  Both and the scales' columns do not
 //                  fit beside one another at NT = 256: the second starts at `second` < NT, the epilogue drains the shared
 //                  columns first and gives the go-ahead after them
-//   scales         two sets of columns in turn; a set is overwritten when the MMAs that read it are known to be done
+//   scales         a set of columns for every stage, or at NT = 256 two in turn: a set is overwritten when the MMAs that
+//                  read it are known to be done
 
 template <int FORMAT, int NT>
 struct PairShape {
@@ -245,12 +271,13 @@ struct PairShape {
   static constexpr unsigned stage_bytes = (loaded + 1023) / 1024 * 1024;
   static constexpr unsigned stages = 225280 / stage_bytes < 8 ? 225280 / stage_bytes : 8;
   static constexpr unsigned scale_columns = (1 + row_tiles) * blocks * 4;
-  static constexpr unsigned ring = 2;
+  static constexpr unsigned ring = NT == 256 ? 2 : stages;              // sets of scale columns
   static constexpr unsigned first_scale = 512 - ring * scale_columns;
   static constexpr unsigned room = (first_scale - NT) / 32 * 32;
   static constexpr unsigned second = room < NT ? room : NT;              // column of the second accumulator
   static constexpr unsigned smem = stages * stage_bytes + 1024;
   static_assert(stages >= 3 && smem <= 231424, "shared memory");
+  static_assert(second + NT <= first_scale && (NT == 256 || second == NT), "tensor memory");
 };
 
 struct PairArgs {
@@ -278,11 +305,10 @@ __device__ __forceinline__ void store32(void* at, const unsigned* w) {
 }
 
 template <int FORMAT, int NT, typename T, bool WIDE>
-__global__ void __launch_bounds__(kMmaThreads, 1)
+__global__ void __launch_bounds__(kPairThreads, 1)
 fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_constant__ CUtensorMap q_map,
                        const __grid_constant__ CUtensorMap p_scale_map, const __grid_constant__ CUtensorMap q_scale_map, const PairArgs p) {
   using S = PairShape<FORMAT, NT>;
-  constexpr bool kE8M0 = FORMAT == SSGD_MXFP4;
   extern __shared__ unsigned char dynamic_smem[];
   __shared__ __align__(8) uint64_t bars[2 * S::stages + 2];
   __shared__ unsigned tmem_base, failed;
@@ -303,7 +329,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
       mbarrier_init(empty + 8 * s, 1);
     }
     mbarrier_init(acc_full, 1);
-    mbarrier_init(acc_free, 8);                 // one arrival from each of the two CTAs' four epilogue warps
+    mbarrier_init(acc_free, 16);                // one arrival from each of the two CTAs' eight epilogue warps
     mbarrier_init_fence();
     failed = 0;
   }
@@ -342,6 +368,11 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
     }
   } else if (warp == 1) {
     if (rank == 0 && elect_one()) {
+      const uint64_t p_desc = smem_descriptor(stage0, 1024, 2), q_desc = smem_descriptor(stage0 + S::p_bytes, 1024, 2),
+                     sc_desc = smem_descriptor(stage0 + S::p_bytes + S::q_bytes, 128, 0);
+      unsigned s = 0, parity = 0, ring = 0;     // place among the stages and the sets of scale columns
+      unsigned behind = 0, behind_parity = 0;   // the stage whose MMAs read the next stage's scale columns last
+      bool ready = false, ring_free = true;     // what is known of the next stage's operands and scale columns
       unsigned t = 0;                           // tiles so far
       for (unsigned tile = pair; tile < tiles && ok; tile += pairs, ++t) {
         if (t > 0) ok = mbarrier_wait_cluster(acc_free, (t - 1) & 1u, kPolls);
@@ -350,36 +381,32 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
         const unsigned d = tmem + (t & 1u) * S::second;
         const unsigned half = tile_place<NT>(tile, p).q0 % 128 / 32;           // NT = 64: where its rows' scales begin in their tile
         for (unsigned k = 0; k < stages_k; ++k, ++n) {
-          const unsigned s = n % S::stages;
-          ok = mbarrier_wait(full + 8 * s, (n / S::stages) & 1u, kPolls) &&
-               (n < S::ring || mbarrier_wait(empty + 8 * ((n - S::ring) % S::stages), ((n - S::ring) / S::stages) & 1u, kPolls));
+          ok = (ready || mbarrier_wait(full + 8 * s, parity, kPolls)) && (ring_free || mbarrier_wait(empty + 8 * behind, behind_parity, kPolls));
           if (!ok) break;
           tcgen05_fence_after();
-          const unsigned base = stage0 + s * S::stage_bytes, sc = base + S::p_bytes + S::q_bytes;
-          const unsigned columns = tmem + S::first_scale + n % S::ring * S::scale_columns;
-          const unsigned chunks = min(4u, p.k_chunks - k * 4);
-#pragma unroll
-          for (unsigned q = 0; q < S::blocks; ++q) {
-            tcgen05_copy_scales_pair(columns + q * 4, smem_descriptor(sc + q * 512, 128, 0));
-#pragma unroll
-            for (unsigned r = 0; r < S::row_tiles; ++r)
-              tcgen05_copy_scales_pair(columns + S::blocks * 4 + (q * S::row_tiles + r) * 4,
-                                       smem_descriptor(sc + (1 + r) * S::scale_bytes + q * 512, 128, 0));
+          const unsigned next = s + 1 == S::stages ? 0 : s + 1, next_parity = parity ^ (next == 0);
+          ready = mbarrier_test(full + 8 * next, next_parity);    // its answer comes while this stage is issued
+          if (S::ring < S::stages && n + 1 >= S::ring) {          // the scale columns of the next stage were last read `ring` stages before it
+            if (n + 1 > S::ring) {
+              behind_parity ^= behind + 1 == S::stages;
+              behind = behind + 1 == S::stages ? 0 : behind + 1;
+            }
+            ring_free = mbarrier_test(empty + 8 * behind, behind_parity);
           }
-          const uint64_t p_desc = smem_descriptor(base, 1024, 2), q_desc = smem_descriptor(base + S::p_bytes, 1024, 2);
-          for (unsigned c = 0; c < chunks; ++c) {
-            const unsigned q = kE8M0 ? c / 2 : c, id = kE8M0 ? (c & 1u) * 2 : 0;
-            mma_fp4_pair<kE8M0>(d, p_desc + 2 * c, q_desc + 2 * c, mma_fp4_descriptor(256, NT, kE8M0, id), columns + q * 4,
-                                columns + S::blocks * 4 + q * S::row_tiles * 4 + half, k > 0 || c > 0);
-          }
+          const unsigned at = s * (S::stage_bytes >> 4);
+          issue_stage<FORMAT, NT, true>(d, p_desc + at, q_desc + at, sc_desc + at, tmem + S::first_scale + ring * S::scale_columns, half,
+                                        p.k_chunks - k * 4, k == 0);
           tcgen05_commit_pair(empty + 8 * s);
+          s = next;
+          parity = next_parity;
+          ring = ring + 1 == S::ring ? 0 : ring + 1;
         }
         if (ok) tcgen05_commit_pair(acc_full);
       }
       if (!ok) tcgen05_commit_pair(acc_full);   // what was issued has to end before tensor memory is freed
     }
   } else {
-    const unsigned quarter = warp & 3u;
+    const unsigned quarter = warp & 3u, odd = warp >= 6;      // two warps share a quarter of the lanes, 32 columns in turn
     const float ts = (p.p_ts ? __ldg(p.p_ts) : 1.0f) * (p.q_ts ? __ldg(p.q_ts) : 1.0f);
     const unsigned go = cluster_address(acc_free, 0);
     unsigned t = 0;
@@ -397,11 +424,11 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
         if (lane == 0) mbarrier_arrive_cluster(go);
       }
 #pragma unroll 1
-      for (unsigned done = 0; done < NT; done += 32) {
+      for (unsigned done = odd * 32; done < NT; done += 64) {
         const unsigned c = (first + done) % NT;
         unsigned v[32];
         tmem_read32(lanes + c, v);
-        if (shared > 0 && done + 32 == shared) {
+        if (shared > 0 && done < shared && done + 64 >= shared) {          // this warp's last shared columns
           tcgen05_fence_before();
           __syncwarp();
           if (lane == 0) mbarrier_arrive_cluster(go);
@@ -429,9 +456,14 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
             }
           } else {
             T* o = static_cast<T*>(p.out) + (size_t)(q0 + c) * p.ldo + row;
+            if (left == 32) {
 #pragma unroll
-            for (unsigned q = 0; q < 32; ++q)
-              if (q < left) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+              for (unsigned q = 0; q < 32; ++q) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+            } else {
+#pragma unroll
+              for (unsigned q = 0; q < 32; ++q)
+                if (q < left) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+            }
           }
         }
         __syncwarp();
@@ -577,7 +609,7 @@ ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
   const unsigned pairs = (unsigned)(tiles < (size_t)(sms / 2) ? tiles : (size_t)(sms / 2));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * pairs);
-  cfg.blockDim = dim3(kMmaThreads);
+  cfg.blockDim = dim3(kPairThreads);
   cfg.dynamicSmemBytes = S::smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];

@@ -42,6 +42,18 @@ __device__ __forceinline__ bool mbarrier_poll(unsigned bar, unsigned parity) {
       : "memory");
   return done != 0;
 }
+// The same without suspension: what is true now.
+__device__ __forceinline__ bool mbarrier_test(unsigned bar, unsigned parity) {
+  unsigned done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
 // Waits for the phase of the given parity; false when it has not completed within `polls` polls.
 __device__ __forceinline__ bool mbarrier_wait(unsigned bar, unsigned parity, unsigned polls) {
   for (unsigned i = 0; i < polls; ++i)
