@@ -8,7 +8,7 @@
 //   warp 0      one thread brings a stage, 256 of k: 128 x 128 and NT x 128 bytes of codes (tiled copies, 128-byte
 //               swizzle, out-of-range rows and columns filled with zero codes) and their scale tiles (bulk copies)
 //   warp 1      one thread copies the scales into tensor memory and issues four MMAs of 64 of k per stage
-//   warps 2..5  read the accumulators and write out
+//   warps 2..9  read the accumulators and write out, two warps to a quarter of the lanes, 32 columns in turn
 // Every stage has scale columns of its own, so that nothing is overwritten before the commit that frees the stage.
 // Few output tiles: a cluster of 2, 4 or 8 CTAs splits k, the partial tiles meet in shared memory and each CTA adds up
 // its share of the columns over the cluster, in rank order: no atomics, equal inputs give equal bits.
@@ -22,8 +22,7 @@
 
 namespace {
 
-constexpr int kMmaThreads = 192;
-constexpr int kPairThreads = 320;           // copies, MMAs, eight warps that write out
+constexpr int kMmaThreads = 320;            // copies, MMAs, eight warps that write out
 constexpr unsigned kTileJ = 128;            // rows of B in a tile: lanes of the accumulator
 constexpr unsigned kPolls = 200000;         // bound of a wait, about 0.2 s
 
@@ -88,16 +87,22 @@ struct ProductArgs {
   unsigned tiles_k;       // scale tiles along k of one row of tiles
   unsigned a_row_tiles;   // scale row tiles of A
   unsigned tiles_i;
-  int dtype;
 };
 
-__device__ __forceinline__ void store_out(const ProductArgs& p, size_t at, float v) {
-  if (p.dtype == SSGD_F32) static_cast<float*>(p.out)[at] = v;
-  else if (p.dtype == SSGD_BF16) static_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(v);
-  else static_cast<__half*>(p.out)[at] = __float2half_rn(v);
+// 32 accumulators of one lane to a column of out (rows of stride ldo), `left` of them wanted.
+template <typename T>
+__device__ __forceinline__ void store_column(T* o, size_t ldo, const unsigned (&v)[32], unsigned left, float ts) {
+  if (left >= 32) {
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) o[q * ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+  } else {
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q)
+      if (q < left) o[q * ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
+  }
 }
 
-template <int FORMAT, int NT>
+template <int FORMAT, int NT, typename T>
 __global__ void __launch_bounds__(kMmaThreads, 1)
 fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map, const ProductArgs p) {
   using S = Shape<FORMAT, NT>;
@@ -187,18 +192,17 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
     float* partial = reinterpret_cast<float*>(stage_mem);       // [NT][128]; the stages are used up by now
     if (ok) {
 #pragma unroll 1
-      for (unsigned c = 0; c < NT; c += 16) {
+      for (unsigned c = (warp >= 6) * 32; c < NT; c += 64) {
         if (i0 + c >= p.M) break;
-        unsigned v[16];
-        tmem_load16(lanes + c, v);
-        tmem_load_wait(v);
+        unsigned v[32];
+        tmem_read32(lanes + c, v);                              // at NT = 16 the columns from 16 on are other data, not wanted
+        const unsigned left = min((unsigned)NT - c, p.M - (i0 + c));
         if (splits == 1) {
-#pragma unroll
-          for (unsigned q = 0; q < 16; ++q)
-            if (i0 + c + q < p.M && j < p.N) store_out(p, (size_t)(i0 + c + q) * p.ldo + j, __uint_as_float(v[q]) * ts);
+          if (j < p.N) store_column(static_cast<T*>(p.out) + (size_t)(i0 + c) * p.ldo + j, p.ldo, v, left, ts);
         } else {
 #pragma unroll
-          for (unsigned q = 0; q < 16; ++q) partial[(c + q) * kTileJ + quarter * 32 + lane] = __uint_as_float(v[q]);
+          for (unsigned q = 0; q < 32; ++q)
+            if (q < left) partial[(c + q) * kTileJ + quarter * 32 + lane] = __uint_as_float(v[q]);
         }
       }
       tcgen05_fence_before();
@@ -233,10 +237,11 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
       for (unsigned r = 1; r < 8; ++r)
         if (r < splits) sum = make_float4(sum.x + v[r].x, sum.y + v[r].y, sum.z + v[r].z, sum.w + v[r].w);
       const size_t at = (size_t)(i0 + c) * p.ldo + j;
-      if (j < p.N) store_out(p, at, sum.x * ts);
-      if (j + 1 < p.N) store_out(p, at + 1, sum.y * ts);
-      if (j + 2 < p.N) store_out(p, at + 2, sum.z * ts);
-      if (j + 3 < p.N) store_out(p, at + 3, sum.w * ts);
+      T* o = static_cast<T*>(p.out) + at;
+      if (j < p.N) o[0] = from_float<T>(sum.x * ts);
+      if (j + 1 < p.N) o[1] = from_float<T>(sum.y * ts);
+      if (j + 2 < p.N) o[2] = from_float<T>(sum.z * ts);
+      if (j + 3 < p.N) o[3] = from_float<T>(sum.w * ts);
     }
     __syncwarp();
     cluster.sync();                             // nobody leaves while its shared memory is still read
@@ -305,7 +310,7 @@ __device__ __forceinline__ void store32(void* at, const unsigned* w) {
 }
 
 template <int FORMAT, int NT, typename T, bool WIDE>
-__global__ void __launch_bounds__(kPairThreads, 1)
+__global__ void __launch_bounds__(kMmaThreads, 1)
 fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_constant__ CUtensorMap q_map,
                        const __grid_constant__ CUtensorMap p_scale_map, const __grid_constant__ CUtensorMap q_scale_map, const PairArgs p) {
   using S = PairShape<FORMAT, NT>;
@@ -456,14 +461,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
             }
           } else {
             T* o = static_cast<T*>(p.out) + (size_t)(q0 + c) * p.ldo + row;
-            if (left == 32) {
-#pragma unroll
-              for (unsigned q = 0; q < 32; ++q) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
-            } else {
-#pragma unroll
-              for (unsigned q = 0; q < 32; ++q)
-                if (q < left) o[q * p.ldo] = from_float<T>(__uint_as_float(v[q]) * ts);
-            }
+            store_column(o, p.ldo, v, left, ts);
           }
         }
         __syncwarp();
@@ -527,10 +525,10 @@ bool scale_map(CUtensorMap* map, const uint8_t* scales, size_t row_tiles, size_t
            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int FORMAT, int NT>
+template <int FORMAT, int NT, typename T>
 ssgd_status launch_product(const CUtensorMap& a_map, const CUtensorMap& b_map, const ProductArgs& p, unsigned tiles, unsigned splits, cudaStream_t s) {
   using S = Shape<FORMAT, NT>;
-  auto kernel = fp4_matmul_kernel<FORMAT, NT>;
+  auto kernel = fp4_matmul_kernel<FORMAT, NT, T>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem) != cudaSuccess) return SSGD_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(tiles * splits);
@@ -559,15 +557,33 @@ struct Operands {
   unsigned* status;
 };
 
+template <int FORMAT, int NT>
+ssgd_status launch_product_typed(const CUtensorMap& a_map, const CUtensorMap& b_map, const ProductArgs& p, int dtype, unsigned tiles, unsigned splits,
+                                 cudaStream_t s) {
+  switch (dtype) {
+    case SSGD_F32: return launch_product<FORMAT, NT, float>(a_map, b_map, p, tiles, splits, s);
+    case SSGD_BF16: return launch_product<FORMAT, NT, __nv_bfloat16>(a_map, b_map, p, tiles, splits, s);
+    default: return launch_product<FORMAT, NT, __half>(a_map, b_map, p, tiles, splits, s);
+  }
+}
+
+// CTAs that share one tile's k.  A stage costs 0.12 to 0.2 us, joining the parts about 1 us (B200; one row against 4096 x K,
+// one / two / four CTAs: 3.6 / 4.4 / 4.6 us at K = 1024, 5.9 / 5.6 / 5.5 at 4096, 9.5 / 7.8 / 7.3 at 8192).  Clusters have to
+// find their place at the same time: four CTAs fit 32 times, eight 12 times; one tile more doubles the time.
+inline unsigned k_splits(unsigned tiles, unsigned stages_k, int sms) {
+  if (stages_k >= 16 && tiles * 12 <= (unsigned)sms) return 8;
+  if (stages_k >= 12 && tiles * 37 <= (unsigned)sms * 8) return 4;
+  if (stages_k >= 14 && tiles * 2 <= (unsigned)sms) return 2;
+  return 1;
+}
+
 template <int FORMAT>
 ssgd_status product(const Operands& o, int sms, cudaStream_t s) {
   const size_t row_bytes = ssgd_fp4_row_bytes(o.K);
   const unsigned nt = o.M <= 16 ? 16 : o.M <= 32 ? 32 : o.M <= 64 ? 64 : 128;
   const size_t tiles_i = (o.M + nt - 1) / nt, all = (o.N + kTileJ - 1) / kTileJ * tiles_i;
   if (all > (size_t)1 << 27) return SSGD_ERR_SIZE;
-  const unsigned tiles = (unsigned)all, stages_k = (unsigned)((row_bytes + 127) / 128);
-  unsigned splits = 1;
-  while (splits < 8 && tiles * splits * 2 <= (unsigned)sms && splits * 2 <= stages_k) splits *= 2;
+  const unsigned tiles = (unsigned)all, stages_k = (unsigned)((row_bytes + 127) / 128), splits = k_splits(tiles, stages_k, sms);
   CUtensorMap a_map, b_map;
   if (!code_map(&a_map, o.a, o.M, row_bytes, nt) || !code_map(&b_map, o.b, o.N, row_bytes, kTileJ)) return SSGD_ERR_CUDA;
   ProductArgs p;
@@ -577,12 +593,11 @@ ssgd_status product(const Operands& o, int sms, cudaStream_t s) {
   p.tiles_k = (unsigned)((fp4_block_count(FORMAT, o.K) + 3) / 4);
   p.a_row_tiles = (unsigned)((o.M + 127) / 128);
   p.tiles_i = (unsigned)tiles_i;
-  p.dtype = o.dtype;
   switch (nt) {
-    case 16: return launch_product<FORMAT, 16>(a_map, b_map, p, tiles, splits, s);
-    case 32: return launch_product<FORMAT, 32>(a_map, b_map, p, tiles, splits, s);
-    case 64: return launch_product<FORMAT, 64>(a_map, b_map, p, tiles, splits, s);
-    default: return launch_product<FORMAT, 128>(a_map, b_map, p, tiles, splits, s);
+    case 16: return launch_product_typed<FORMAT, 16>(a_map, b_map, p, o.dtype, tiles, splits, s);
+    case 32: return launch_product_typed<FORMAT, 32>(a_map, b_map, p, o.dtype, tiles, splits, s);
+    case 64: return launch_product_typed<FORMAT, 64>(a_map, b_map, p, o.dtype, tiles, splits, s);
+    default: return launch_product_typed<FORMAT, 128>(a_map, b_map, p, o.dtype, tiles, splits, s);
   }
 }
 
@@ -609,7 +624,7 @@ ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
   const unsigned pairs = (unsigned)(tiles < (size_t)(sms / 2) ? tiles : (size_t)(sms / 2));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * pairs);
-  cfg.blockDim = dim3(kPairThreads);
+  cfg.blockDim = dim3(kMmaThreads);
   cfg.dynamicSmemBytes = S::smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -638,15 +653,31 @@ ssgd_status pair_product(const Operands& o, bool wide, int sms, cudaStream_t s) 
   }
 }
 
+// Nanoseconds of a product by pairs with tiles of 256 x nt, fitted on B200: a start, a stage, and for each further tile of a
+// pair its stages or its writing out, whichever is longer (2048 x 1024 x 4096, nt = 64 / 128 / 256: 9.3 / 7.7 / 11.1 us, fitted
+// 8.1 / 7.0 / 10.4; 2048 x 4096 x 1024: - / 9.9 / 9.6, fitted 9.9 / 9.1 / 8.9; 777 x 1111 x 1500: 5.8 / 6.4 / -, fitted 4.6 / 5.4).
+inline unsigned long long pair_cost(unsigned long long tiles_p, size_t Q, unsigned nt, unsigned long long stages_k, unsigned pairs) {
+  const unsigned long long tiles = tiles_p * ((Q + nt - 1) / nt), rounds = (tiles + pairs - 1) / pairs;
+  const unsigned start = nt == 64 ? 3900 : nt == 128 ? 4400 : 5600, stage = nt == 64 ? 123 : nt == 128 ? 160 : 300,
+                 write = nt == 64 ? 1000 : nt == 128 ? 1350 : 2100;
+  const unsigned long long work = stages_k * stage;
+  return start + work + (rounds - 1) * (work + 250 > write ? work + 250 : write);
+}
+
 template <int FORMAT>
 ssgd_status any_product(const Operands& o, int sms, cudaStream_t s) {
+  // Up to 128 rows of A: the weight's rows are the lanes and stream through once.  More rows, but few tiles and a long k: the
+  // same kernel, because it splits k (150 x 300 x 16384: 8.5 us against 13.8 by pairs; x 4096 7.3 against 6.7).
+  const size_t stages_k = (ssgd_fp4_row_bytes(o.K) + 127) / 128;
+  if (o.M <= 128 || (stages_k >= 24 && ((o.M + 127) / 128) * ((o.N + kTileJ - 1) / kTileJ) * 8 <= (size_t)sms)) return product<FORMAT>(o, sms, s);
   const size_t e = dtype_bytes((unsigned)o.dtype);
   const bool wide = reinterpret_cast<uintptr_t>(o.out) % 32 == 0 && o.ldo * e % 32 == 0;
-  if (o.M <= 128) return product<FORMAT>(o, sms, s);
-  const size_t P = wide ? o.M : o.N, Q = wide ? o.N : o.M, tiles_p = (P + 255) / 256, pairs = (size_t)(sms / 2);
-  if (tiles_p * ((Q + 255) / 256) >= pairs) return pair_product<FORMAT, 256>(o, wide, sms, s);
-  if (tiles_p * ((Q + 127) / 128) >= pairs) return pair_product<FORMAT, 128>(o, wide, sms, s);
-  return pair_product<FORMAT, 64>(o, wide, sms, s);
+  const size_t P = wide ? o.M : o.N, Q = wide ? o.N : o.M, tiles_p = (P + 255) / 256;
+  const unsigned pairs = (unsigned)(sms / 2);
+  const unsigned long long c64 = pair_cost(tiles_p, Q, 64, stages_k, pairs), c128 = pair_cost(tiles_p, Q, 128, stages_k, pairs),
+                           c256 = pair_cost(tiles_p, Q, 256, stages_k, pairs);
+  if (c256 <= c128 && c256 <= c64) return pair_product<FORMAT, 256>(o, wide, sms, s);
+  return c128 <= c64 ? pair_product<FORMAT, 128>(o, wide, sms, s) : pair_product<FORMAT, 64>(o, wide, sms, s);
 }
 
 }  // namespace
