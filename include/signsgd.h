@@ -385,8 +385,9 @@ ssgd_status ssgd_table_size(const ssgd_tensor* tensors, size_t T, size_t groups,
 ssgd_status ssgd_table_build(const ssgd_tensor* tensors, size_t T, size_t groups, void* table_host, size_t table_bytes);
 
 /* Norm of each group: SSGD_NORM_TWO sqrt(sum g^2), summed in fp64; SSGD_NORM_MAX max |g|.  NaN and infinity carry
- * through; an empty group has norm 0.  No atomics: equal inputs give equal bits.
- *   table  DEVICE copy of the table; ws DEVICE, ws_bytes, 16-byte aligned;  norms out DEVICE float [groups]         */
+ * through; an empty group has norm 0.  Sums go in a fixed order: equal inputs give equal bits.
+ *   table  DEVICE copy of the table;  norms out DEVICE float [groups]
+ *   ws     DEVICE, ws_bytes, 16-byte aligned; calls that may run at the same time need one each                       */
 #define SSGD_NORM_TWO 0
 #define SSGD_NORM_MAX 1
 ssgd_status ssgd_tensors_norm(const void* table, size_t tiles, size_t groups, int kind, void* ws, float* norms,

@@ -61,6 +61,32 @@ __device__ __forceinline__ void store4(T* p, float4 v) {
   __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack2(T(), v.x, v.y), pack2(T(), v.z, v.w)));
 }
 
+// Eight consecutive elements; the address is a multiple of eight elements (for fp32 loads, of four).
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+  const uint4 q = *reinterpret_cast<const uint4*>(p);
+  v[0] = low_to_float(T(), q.x); v[1] = high_to_float(T(), q.x); v[2] = low_to_float(T(), q.y); v[3] = high_to_float(T(), q.y);
+  v[4] = low_to_float(T(), q.z); v[5] = high_to_float(T(), q.z); v[6] = low_to_float(T(), q.w); v[7] = high_to_float(T(), q.w);
+}
+// 32 bytes in one store; the address is a multiple of 32.
+__device__ __forceinline__ void store32(void* at, const unsigned* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  store4(p, make_float4(v[0], v[1], v[2], v[3]));
+  store4(p + 4, make_float4(v[4], v[5], v[6], v[7]));
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack2(T(), v[0], v[1]), pack2(T(), v[2], v[3]), pack2(T(), v[4], v[5]), pack2(T(), v[6], v[7])));
+}
+
 }  // namespace
 
 #endif  // SSGD_DTYPES_CUH_

@@ -303,12 +303,6 @@ __device__ __forceinline__ TilePlace tile_place(unsigned tile, const PairArgs& a
   return {(band * kBand + in % high) * 256, in / high * NT};
 }
 
-__device__ __forceinline__ void store32(void* at, const unsigned* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-
 template <int FORMAT, int NT, typename T, bool WIDE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
 fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_constant__ CUtensorMap q_map,
@@ -529,7 +523,8 @@ template <int FORMAT, int NT, typename T>
 ssgd_status launch_product(const CUtensorMap& a_map, const CUtensorMap& b_map, const ProductArgs& p, unsigned tiles, unsigned splits, cudaStream_t s) {
   using S = Shape<FORMAT, NT>;
   auto kernel = fp4_matmul_kernel<FORMAT, NT, T>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem) != cudaSuccess) return SSGD_ERR_CUDA;
+  static unsigned long long seen = 0;
+  if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(tiles * splits);
   cfg.blockDim = dim3(kMmaThreads);
@@ -619,7 +614,8 @@ ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
   p.tiles_p = (unsigned)tiles_p;
   p.tiles_q = (unsigned)tiles_q;
   auto kernel = fp4_matmul_pair_kernel<FORMAT, NT, T, WIDE>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem) != cudaSuccess) return SSGD_ERR_CUDA;
+  static unsigned long long seen = 0;
+  if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
   const size_t tiles = tiles_p * tiles_q;
   const unsigned pairs = (unsigned)(tiles < (size_t)(sms / 2) ? tiles : (size_t)(sms / 2));
   cudaLaunchConfig_t cfg = {};

@@ -397,8 +397,8 @@ ssgd_status launch_quantise(const T* x, size_t rows, size_t cols, size_t ldx, co
   const bool vec = rows_aligned(x, ldx);
   const unsigned smem = tile_smem<T>(COLS || !vec, COLS);
   auto kernel = fp4_quantise_kernel<FORMAT, ROWS, COLS, T>;
-  if (smem > 32768 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tile_smem<T>(true, COLS)) != cudaSuccess)
-    return SSGD_ERR_CUDA;
+  static unsigned long long seen = 0;
+  if (smem > 32768 && !allow_smem(reinterpret_cast<const void*>(kernel), tile_smem<T>(true, COLS), &seen)) return SSGD_ERR_CUDA;
   launch_kernel(kernel, dim3((unsigned)tiles), dim3(kThreads), smem, s, true, x, (unsigned)rows, (unsigned)cols, ldx, vec, amax, tensor_scale,
                 codes, scales, codes_t, scales_t, (unsigned)tiles_c);
   return launch_status();

@@ -63,6 +63,18 @@ inline bool beta_ok(float beta) { return beta >= 0.0f && beta < 1.0f; }  // fals
 
 ssgd_status launch_status() { return cudaGetLastError() == cudaSuccess ? SSGD_OK : SSGD_ERR_CUDA; }
 
+// Lets a kernel have `bytes` of dynamic shared memory, asked of the runtime once per kernel and device: `seen` is a
+// static of the caller's, one for each kernel, a bit for each device.
+bool allow_smem(const void* kernel, size_t bytes, unsigned long long* seen) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (__atomic_load_n(seen, __ATOMIC_RELAXED) & bit) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+  __atomic_fetch_or(seen, bit, __ATOMIC_RELAXED);
+  return true;
+}
+
 // Kernel launch with the programmatic-serialization attribute (see pdl_wait in device_common.cuh), for
 // kernels that begin with pdl_wait(); pdl = false gives an ordinary launch.
 template <typename... KArgs, typename... Args>

@@ -1,15 +1,17 @@
 // Norm and clipping of gradients that come as many tensors, into the flat rows that the step takes.
 // See include/signsgd.h for the contract of each call.
 //
-// The host cuts every tensor into tiles of at most kTile elements and writes them into a table (caller-owned
-// memory, copied to the device once); a CTA takes one tile, so tensors of any number and size are one launch
-// and no CTA gets more than its share.  Tiles of a group (a worker) are consecutive:
-//   pass 1  tensors_norm_kernel    partial[tile] = sum of squares (or largest magnitude) of the tile
-//   pass 2  norms_finish_kernel    norm of each group from its partials, in a fixed order
-//   pass 3  tensors_scale_kernel   dst = c * src with c = max_norm / norm where norm > max_norm, else 1
-// No atomics: the same inputs give the same bits.  Squares are summed in fp64, where the product of two fp32 numbers is
-// exact and can neither overflow nor vanish.
+// The host cuts every tensor into tiles of at most kTile elements and writes them into a table (caller-owned memory,
+// copied to the device once); a CTA takes one tile, so tensors of any number and size are one launch and no CTA gets
+// more than its share.  Tiles of a group (a worker) are consecutive.
+//   pass 1  tensors_norm_kernel   a sum of squares (or largest magnitude) for each tile
+//   pass 2  norms_finish_kernel   norm of each group from its tiles', in a fixed order
+//   pass 3  tensors_scale_kernel  dst = c * src with c = max_norm / norm where norm > max_norm, else 1; from the last tile
+//                                 to the first, since the last ones read are still in L2
+// Small groups: tensors_clip_small_kernel, all of it in one launch, one cluster of eight CTAs for a group.
+// Sums go in a fixed order: equal inputs give equal bits.
 
+#include <cooperative_groups.h>
 #include <string.h>
 
 #include "host_common.h"
@@ -34,91 +36,112 @@ inline size_t table_head_bytes(size_t groups) { return ((groups + 1) * sizeof(ui
 
 constexpr int kNormTwo = 0, kNormMax = 1;
 
-template <int KIND>
-__device__ __forceinline__ void norm_fold(double& acc, float v) {
-  if constexpr (KIND == kNormTwo) {
-    const double t = (double)v;
-    acc = fma(t, t, acc);
-  }
-}
-
 // |v| as ordered bits: NaN sorts above infinity, so one maximum carries it through.
 __device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-template <int KIND, typename T>
-__device__ __forceinline__ void tile_norm(const T* __restrict__ src, unsigned n, double& acc, unsigned& top) {
-  const bool aligned = (reinterpret_cast<uintptr_t>(src) & (4 * sizeof(T) - 1)) == 0;
-  const unsigned body = aligned ? n & ~3u : 0u;
-#pragma unroll 8
-  for (unsigned i = threadIdx.x * 4; i < body; i += kThreads * 4) {
-    const float4 q = load4(src + i);
-    if constexpr (KIND == kNormTwo) {
-      norm_fold<KIND>(acc, q.x); norm_fold<KIND>(acc, q.y); norm_fold<KIND>(acc, q.z); norm_fold<KIND>(acc, q.w);
+// Squares go to fp64, where the product of two fp32 numbers is exact and neither overflows nor vanishes.  16-bit
+// elements have squares of 16 or 22 bits: eight of them are added in fp32 first (one conversion for eight elements:
+// conversions to fp64 would cost more than the loads), unless bf16's range calls for fp64.
+template <typename T>
+__device__ __forceinline__ void fold8(const float (&v)[8], double& acc) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc = fma((double)v[i], (double)v[i], acc);
+  } else {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = __fmaf_rn(v[i], v[i], s);
+    if (s > 1e-25f && s < 1e38f) {
+      acc += (double)s;
     } else {
-      top = max(max(top, max(magnitude_bits(q.x), magnitude_bits(q.y))), max(magnitude_bits(q.z), magnitude_bits(q.w)));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc = fma((double)v[i], (double)v[i], acc);
     }
   }
-#pragma unroll 8
-  for (unsigned i = body + threadIdx.x; i < n; i += kThreads) {
-    const float v = to_float(src[i]);
-    if constexpr (KIND == kNormTwo) norm_fold<KIND>(acc, v);
+}
+
+// One tile's contribution of this thread: a double for the two-norm, the largest magnitude's bits for the maximum.
+template <int KIND, typename T>
+__device__ __forceinline__ void tile_norm(const T* __restrict__ src, unsigned n, double& acc, unsigned& top) {
+  const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(src) / sizeof(T)) & 7u;
+  const unsigned head = min(n, off ? 8u - off : 0u), groups = (n - head) / 8;
+  const T* body = src + head;
+#pragma unroll 4
+  for (unsigned g = threadIdx.x; g < groups; g += kThreads) {
+    float v[8];
+    load8(body + 8 * g, v);
+    if constexpr (KIND == kNormTwo) {
+      fold8<T>(v, acc);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[i]));
+    }
+  }
+  // what lies before the first and behind the last group of eight: at most 14 elements
+  const unsigned rest = head + 8 * groups, loose = n - 8 * groups;
+  if (threadIdx.x < loose) {
+    const float v = to_float(src[threadIdx.x < head ? threadIdx.x : rest + threadIdx.x - head]);
+    if constexpr (KIND == kNormTwo) acc = fma((double)v, (double)v, acc);
     else top = max(top, magnitude_bits(v));
   }
 }
 
 template <int KIND>
-__global__ void __launch_bounds__(kThreads)
-tensors_norm_kernel(const Tile* __restrict__ tiles, double* __restrict__ partial) {
-  pdl_launch_dependents();
-  pdl_wait();
-  const Tile t = tiles[blockIdx.x];
-  double acc = 0.0;
-  unsigned top = 0;
+__device__ __forceinline__ void any_tile_norm(const Tile& t, double& acc, unsigned& top) {
   switch (t.types & 15u) {
     case SSGD_F32: tile_norm<KIND>(static_cast<const float*>(t.src), t.n, acc, top); break;
     case SSGD_BF16: tile_norm<KIND>(static_cast<const __nv_bfloat16*>(t.src), t.n, acc, top); break;
     default: tile_norm<KIND>(static_cast<const __half*>(t.src), t.n, acc, top); break;
   }
-  __shared__ double part[kThreads / 32];
-  const unsigned lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  if constexpr (KIND == kNormTwo) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, o);
-  } else {
-    acc = (double)__reduce_max_sync(0xFFFFFFFFu, top);
-  }
-  if (lane == 0) part[warp] = acc;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double s = part[0];
-#pragma unroll
-    for (int w = 1; w < kThreads / 32; ++w) s = KIND == kNormTwo ? s + part[w] : fmax(s, part[w]);
-    partial[blockIdx.x] = s;
-  }
 }
 
 template <int KIND>
+__device__ __forceinline__ double combine(double a, double b) { return KIND == kNormTwo ? a + b : fmax(a, b); }
+
+// Over the CTA, in thread 0 (every thread must call).
+template <int KIND, int THREADS>
+__device__ __forceinline__ double cta_combine(double s, double* part) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s = combine<KIND>(s, __shfl_xor_sync(0xFFFFFFFFu, s, o));
+  if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = s;
+  __syncthreads();
+  double r = part[0];
+#pragma unroll
+  for (int w = 1; w < THREADS / 32; ++w) r = combine<KIND>(r, part[w]);
+  return r;
+}
+
+template <int KIND>
+__device__ __forceinline__ float finish_norm(double r) { return KIND == kNormTwo ? (float)sqrt(r) : __uint_as_float((unsigned)r); }
+
+template <int KIND>
 __global__ void __launch_bounds__(kThreads)
+tensors_norm_kernel(const Tile* __restrict__ tiles, double* __restrict__ partial) {
+  __shared__ double part[kThreads / 32];
+  pdl_launch_dependents();
+  pdl_wait();
+  const Tile t = tiles[blockIdx.x];
+  double acc = 0.0;
+  unsigned top = 0;
+  any_tile_norm<KIND>(t, acc, top);
+  const double s = cta_combine<KIND, kThreads>(KIND == kNormTwo ? acc : (double)top, part);
+  if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+constexpr int kFinishThreads = 1024;
+
+template <int KIND>
+__global__ void __launch_bounds__(kFinishThreads)
 norms_finish_kernel(const uint64_t* __restrict__ first_tile, const double* __restrict__ partial, float* __restrict__ norms) {
+  __shared__ double part[kFinishThreads / 32];
   pdl_launch_dependents();
   pdl_wait();
   const uint64_t a = first_tile[blockIdx.x], b = first_tile[blockIdx.x + 1];
   double s = 0.0;
-  for (uint64_t i = a + threadIdx.x; i < b; i += kThreads) s = KIND == kNormTwo ? s + partial[i] : fmax(s, partial[i]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const double other = __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    s = KIND == kNormTwo ? s + other : fmax(s, other);
-  }
-  __shared__ double part[kThreads / 32];
-  if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double r = part[0];
-#pragma unroll
-    for (int w = 1; w < kThreads / 32; ++w) r = KIND == kNormTwo ? r + part[w] : fmax(r, part[w]);
-    norms[blockIdx.x] = KIND == kNormTwo ? (float)sqrt(r) : __uint_as_float((unsigned)r);
-  }
+#pragma unroll 4
+  for (uint64_t i = a + threadIdx.x; i < b; i += kFinishThreads) s = combine<KIND>(s, partial[i]);
+  s = cta_combine<KIND, kFinishThreads>(s, part);
+  if (threadIdx.x == 0) norms[blockIdx.x] = finish_norm<KIND>(s);
 }
 
 // c of one group, and whether its rows are zeroed instead (norm not finite, when the caller asked for that).
@@ -127,48 +150,102 @@ __device__ __forceinline__ float clip_factor(float norm, float max_norm, int zer
   return norm > max_norm ? __fdiv_rn(max_norm, norm) : (norm == norm ? 1.0f : norm);
 }
 
-template <typename S, typename D>
-__device__ __forceinline__ void tile_scale(const S* __restrict__ src, D* __restrict__ dst, unsigned n, float c, bool zero) {
+// Four elements of a lane at a time where source and destination both allow it, BATCH of them in flight, else element by
+// element, LOOSE in flight: lanes lie side by side either way.  In place every element is read before it is written, by
+// the thread that writes it.
+template <int BATCH, int LOOSE, typename S, typename D>
+__device__ __forceinline__ void tile_scale(const S* src, D* dst, unsigned n, float c, bool zero) {
   const bool aligned = ((reinterpret_cast<uintptr_t>(src) & (4 * sizeof(S) - 1)) | (reinterpret_cast<uintptr_t>(dst) & (4 * sizeof(D) - 1))) == 0;
-  const unsigned body = aligned ? n & ~3u : 0u;
-#pragma unroll 4
-  for (unsigned i = threadIdx.x * 4; i < body; i += kThreads * 4) {
-    float4 q = load4(src + i);
-    q = make_float4(__fmul_rn(q.x, c), __fmul_rn(q.y, c), __fmul_rn(q.z, c), __fmul_rn(q.w, c));
-    if (zero) q = make_float4(0.f, 0.f, 0.f, 0.f);
-    store4(dst + i, q);
+  const unsigned groups = aligned ? n / 4 : 0u;
+  for (unsigned g0 = threadIdx.x; g0 < groups; g0 += BATCH * kThreads) {
+    float4 v[BATCH];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u)
+      if (g0 + u * kThreads < groups) v[u] = load4(src + 4 * (g0 + u * kThreads));
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u)
+      if (g0 + u * kThreads < groups) {
+        const float4 q = zero ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(__fmul_rn(v[u].x, c), __fmul_rn(v[u].y, c), __fmul_rn(v[u].z, c), __fmul_rn(v[u].w, c));
+        store4(dst + 4 * (g0 + u * kThreads), q);
+      }
   }
-#pragma unroll 4
-  for (unsigned i = body + threadIdx.x; i < n; i += kThreads) {
-    const float v = __fmul_rn(to_float(src[i]), c);
-    dst[i] = from_float<D>(zero ? 0.0f : v);
+  for (unsigned i0 = 4 * groups + threadIdx.x; i0 < n; i0 += LOOSE * kThreads) {
+    S v[LOOSE];
+#pragma unroll
+    for (int u = 0; u < LOOSE; ++u)
+      if (i0 + u * kThreads < n) v[u] = src[i0 + u * kThreads];
+#pragma unroll
+    for (int u = 0; u < LOOSE; ++u)
+      if (i0 + u * kThreads < n) dst[i0 + u * kThreads] = from_float<D>(zero ? 0.0f : __fmul_rn(to_float(v[u]), c));
   }
 }
 
-template <typename S>
+template <int BATCH, int LOOSE, typename S>
 __device__ __forceinline__ void tile_scale_from(const Tile& t, float c, bool zero) {
   const S* src = static_cast<const S*>(t.src);
   switch (t.types >> 4) {
-    case SSGD_F32: tile_scale(src, static_cast<float*>(t.dst), t.n, c, zero); break;
-    case SSGD_BF16: tile_scale(src, static_cast<__nv_bfloat16*>(t.dst), t.n, c, zero); break;
-    default: tile_scale(src, static_cast<__half*>(t.dst), t.n, c, zero); break;
+    case SSGD_F32: tile_scale<BATCH, LOOSE>(src, static_cast<float*>(t.dst), t.n, c, zero); break;
+    case SSGD_BF16: tile_scale<BATCH, LOOSE>(src, static_cast<__nv_bfloat16*>(t.dst), t.n, c, zero); break;
+    default: tile_scale<BATCH, LOOSE>(src, static_cast<__half*>(t.dst), t.n, c, zero); break;
   }
 }
 
-__global__ void __launch_bounds__(kThreads)
+template <int BATCH, int LOOSE>
+__device__ __forceinline__ void any_tile_scale(const Tile& t, float norm, float max_norm, int zero_nonfinite) {
+  if (t.dst == nullptr) return;
+  bool zero;
+  const float c = clip_factor(norm, max_norm, zero_nonfinite, &zero);
+  if (t.src == t.dst && c == 1.0f && !zero) return;   // in place and nothing to change
+  switch (t.types & 15u) {
+    case SSGD_F32: tile_scale_from<BATCH, LOOSE, float>(t, c, zero); break;
+    case SSGD_BF16: tile_scale_from<BATCH, LOOSE, __nv_bfloat16>(t, c, zero); break;
+    default: tile_scale_from<BATCH, LOOSE, __half>(t, c, zero); break;
+  }
+}
+
+// Bound by memory: 335 M elements in 320 tensors on B200, whole call, fp32 to fp32 584 us = 6.90 TB/s of its three passes, bf16 to
+// fp32 415 us = 6.47 TB/s; Resnet-50's 161 tensors x 7 workers in fp32 316 us = 6.80 TB/s.  Measured and worse: batches of 2
+// (bf16 442, at 8 CTAs per SM 420), 8 elements a lane (429), half and quarter tiles per CTA (457 - 580), two to four tiles in a
+// row per CTA (670 and more), tiles in order instead of from the end (+ 3).
+constexpr int kBatch = 4, kLoose = 8;
+__global__ void __launch_bounds__(kThreads, 6)
 tensors_scale_kernel(const Tile* __restrict__ tiles, const float* __restrict__ norms, float max_norm, int zero_nonfinite) {
   pdl_launch_dependents();
   pdl_wait();
-  const Tile t = tiles[blockIdx.x];
-  if (t.dst == nullptr) return;
-  bool zero;
-  const float c = clip_factor(norms[t.group], max_norm, zero_nonfinite, &zero);
-  if (t.src == t.dst && c == 1.0f && !zero) return;   // in place and nothing to change
-  switch (t.types & 15u) {
-    case SSGD_F32: tile_scale_from<float>(t, c, zero); break;
-    case SSGD_BF16: tile_scale_from<__nv_bfloat16>(t, c, zero); break;
-    default: tile_scale_from<__half>(t, c, zero); break;
-  }
+  const Tile t = tiles[gridDim.x - 1 - blockIdx.x];
+  any_tile_scale<kBatch, kLoose>(t, norms[t.group], max_norm, zero_nonfinite);
+}
+
+// Both passes for groups of few tiles: the cluster's CTAs take the group's tiles in turn, exchange their sums through
+// shared memory and scale the same tiles.  SCALE = false: the norms only.
+constexpr unsigned kCluster = 8;
+
+template <int KIND, bool SCALE>
+__global__ void __launch_bounds__(kThreads)
+tensors_clip_small_kernel(const uint64_t* __restrict__ first_tile, const Tile* __restrict__ tiles, float* __restrict__ norms, float max_norm,
+                          int zero_nonfinite) {
+  __shared__ double part[kThreads / 32];
+  __shared__ double mine;
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  const unsigned group = blockIdx.x / kCluster, rank = cluster.block_rank();
+  pdl_launch_dependents();
+  pdl_wait();
+  const uint64_t a = first_tile[group], b = first_tile[group + 1];
+  double acc = 0.0;
+  unsigned top = 0;
+  for (uint64_t i = a + rank; i < b; i += kCluster) any_tile_norm<KIND>(tiles[i], acc, top);
+  const double s = cta_combine<KIND, kThreads>(KIND == kNormTwo ? acc : (double)top, part);
+  if (threadIdx.x == 0) mine = s;
+  cluster.sync();
+  double all = 0.0;
+#pragma unroll
+  for (unsigned r = 0; r < kCluster; ++r) all = combine<KIND>(all, *cluster.map_shared_rank(&mine, r));
+  const float norm = finish_norm<KIND>(all);
+  if (rank == 0 && threadIdx.x == 0) norms[group] = norm;
+  if (SCALE)
+    for (uint64_t i = a + rank; i < b; i += kCluster) any_tile_scale<2, 4>(tiles[i], norm, max_norm, zero_nonfinite);
+  cluster.sync();                                     // nobody leaves while its sum is still read
 }
 
 ssgd_status check_tensors(const ssgd_tensor* t, size_t T, size_t groups, size_t* tiles) {
@@ -203,12 +280,40 @@ inline const Tile* table_tiles(const void* table, size_t groups) {
   return reinterpret_cast<const Tile*>(static_cast<const char*>(table) + table_head_bytes(groups));
 }
 
+// Workspace: a double for each tile.
+inline size_t ws_size(size_t tiles) { return (tiles + 2) / 2 * 2 * sizeof(double); }
+
+// The one-launch form: up to kSmallTiles tiles a group on average, and no more clusters than are there at one time.
+constexpr size_t kSmallTiles = 32, kSmallGroups = 16;
+
 template <int KIND>
-void launch_norm(const void* table, size_t tiles, size_t groups, double* ws, float* norms, cudaStream_t s) {
-  if (tiles > 0)
-    launch_kernel(tensors_norm_kernel<KIND>, dim3((unsigned)tiles), dim3(kThreads), 0, s, true, table_tiles(table, groups), ws);
-  launch_kernel(norms_finish_kernel<KIND>, dim3((unsigned)groups), dim3(kThreads), 0, s, true,
-                static_cast<const uint64_t*>(table), static_cast<const double*>(ws), norms);
+ssgd_status launch_clip(const void* table, size_t tiles, size_t groups, bool scale, float max_norm, int zero_nonfinite, void* ws, float* norms,
+                        cudaStream_t s) {
+  const uint64_t* first = static_cast<const uint64_t*>(table);
+  const Tile* list = table_tiles(table, groups);
+  if (groups <= kSmallGroups && tiles <= kSmallTiles) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)groups * kCluster);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    auto kernel = scale ? tensors_clip_small_kernel<KIND, true> : tensors_clip_small_kernel<KIND, false>;
+    (void)cudaLaunchKernelEx(&cfg, kernel, first, list, norms, max_norm, zero_nonfinite);
+    return launch_status();
+  }
+  double* partial = static_cast<double*>(ws);
+  if (tiles > 0) launch_kernel(tensors_norm_kernel<KIND>, dim3((unsigned)tiles), dim3(kThreads), 0, s, true, list, partial);
+  launch_kernel(norms_finish_kernel<KIND>, dim3((unsigned)groups), dim3(kFinishThreads), 0, s, true, first, static_cast<const double*>(partial), norms);
+  if (scale && tiles > 0)
+    launch_kernel(tensors_scale_kernel, dim3((unsigned)tiles), dim3(kThreads), 0, s, true, list, static_cast<const float*>(norms), max_norm, zero_nonfinite);
+  return launch_status();
 }
 
 }  // namespace
@@ -221,7 +326,7 @@ ssgd_status ssgd_table_size(const ssgd_tensor* tensors, size_t T, size_t groups,
   const ssgd_status st = check_tensors(tensors, T, groups, tiles);
   if (st != SSGD_OK) return st;
   *table_bytes = table_head_bytes(groups) + *tiles * sizeof(Tile);
-  *ws_bytes = (*tiles + 2) / 2 * 2 * sizeof(double);
+  *ws_bytes = ws_size(*tiles);
   return SSGD_OK;
 }
 
@@ -259,19 +364,18 @@ ssgd_status ssgd_tensors_norm(const void* table, size_t tiles, size_t groups, in
   if (st != SSGD_OK) return st;
   if (kind != SSGD_NORM_TWO && kind != SSGD_NORM_MAX) return SSGD_ERR_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (kind == SSGD_NORM_TWO) launch_norm<kNormTwo>(table, tiles, groups, static_cast<double*>(ws), norms, s);
-  else launch_norm<kNormMax>(table, tiles, groups, static_cast<double*>(ws), norms, s);
-  return launch_status();
+  return kind == SSGD_NORM_TWO ? launch_clip<kNormTwo>(table, tiles, groups, false, 0.0f, 0, ws, norms, s)
+                               : launch_clip<kNormMax>(table, tiles, groups, false, 0.0f, 0, ws, norms, s);
 }
 
 ssgd_status ssgd_tensors_clip(const void* table, size_t tiles, size_t groups, int kind, float max_norm, int zero_nonfinite,
                               void* ws, float* norms, void* stream) {
-  if (!(max_norm >= 0.0f)) return SSGD_ERR_ARG;
-  const ssgd_status st = ssgd_tensors_norm(table, tiles, groups, kind, ws, norms, stream);
-  if (st != SSGD_OK || tiles == 0) return st;
-  launch_kernel(tensors_scale_kernel, dim3((unsigned)tiles), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), true,
-                table_tiles(table, groups), static_cast<const float*>(norms), max_norm, zero_nonfinite);
-  return launch_status();
+  const ssgd_status st = check_table(table, tiles, groups, ws, norms);
+  if (st != SSGD_OK) return st;
+  if ((kind != SSGD_NORM_TWO && kind != SSGD_NORM_MAX) || !(max_norm >= 0.0f)) return SSGD_ERR_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return kind == SSGD_NORM_TWO ? launch_clip<kNormTwo>(table, tiles, groups, true, max_norm, zero_nonfinite, ws, norms, s)
+                               : launch_clip<kNormMax>(table, tiles, groups, true, max_norm, zero_nonfinite, ws, norms, s);
 }
 
 }  // extern "C"

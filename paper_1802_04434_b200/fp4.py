@@ -34,18 +34,19 @@ class Packed:
         if fmt not in _BLOCK:
             raise ValueError("fmt must be 'mx' or 'nv'")
         need = _sizes(rows, cols, fmt)
-        for name, t, n in (("codes", codes, need[0]), ("scales", scales, need[1])):
-            B._ptr(t, torch.uint8, name)
-            B._need(t, n, name)
+        ts = None if tensor_scale is None else B._ptr(tensor_scale, torch.float32, "tensor_scale")
+        self.pointers = (B._ptr(codes, torch.uint8, "codes"), B._ptr(scales, torch.uint8, "scales"), ts)
+        if codes.numel() < need[0] or scales.numel() < need[1]:
+            raise ValueError("codes hold %d bytes, scales %d; %d x %d %s needs %d and %d" % (codes.numel(), scales.numel(), rows, cols, fmt, *need))
         self.rows, self.cols, self.fmt, self.device = rows, cols, fmt, codes.device
-        self.pointers = (codes.data_ptr(), scales.data_ptr(), B._ptr(tensor_scale, torch.float32, "tensor_scale"))
         self._parts, self._buffer = (codes, scales, tensor_scale), None
 
     @classmethod
-    def _in(cls, buffer: torch.Tensor, base: int, at: Tuple[int, int, Optional[int]], rows: int, cols: int, fmt: str) -> "Packed":
+    def _in(cls, buffer: torch.Tensor, base: int, at: Tuple[int, int, Optional[int]], rows: int, cols: int, fmt: str,
+            device: torch.device) -> "Packed":
         """Parts at the given byte offsets of one buffer whose address is `base`."""
         p = cls.__new__(cls)
-        p.rows, p.cols, p.fmt, p.device = rows, cols, fmt, buffer.device
+        p.rows, p.cols, p.fmt, p.device = rows, cols, fmt, device
         p.pointers = (base + at[0], base + at[1], None if at[2] is None else base + at[2])
         p._parts, p._buffer = None, (buffer, at)
         return p
@@ -89,45 +90,47 @@ def check(device="cuda") -> None:
         raise RuntimeError("a 4-bit product did not receive its operands in time; its output is not valid")
 
 
-def _matrix(x: torch.Tensor) -> torch.Tensor:
-    if x.dim() != 2:
-        raise ValueError("a matrix is wanted, got %d dimensions" % x.dim())
-    if not x.is_cuda:
-        raise ValueError("the matrix must live in device memory")
-    if x.dtype not in B.DTYPE_CODE:
-        raise TypeError("the matrix must be of dtype float32, bfloat16 or float16")
-    # rows at any stride; a single column, or a single row, has no stride of its own to look at
-    if x.is_contiguous() or ((x.stride(1) == 1 or x.shape[1] <= 1) and x.stride(0) >= x.shape[1]):
-        return x
-    return x.contiguous()
-
-
 def _quantise(x, fmt, amax, by_rows, by_columns):
-    if fmt not in _BLOCK:
+    block = _BLOCK.get(fmt)
+    if block is None:
         raise ValueError("fmt must be 'mx' or 'nv'")
-    x = _matrix(x)
-    rows, cols = x.shape
+    dtype = B.DTYPE_CODE.get(x.dtype)
+    if dtype is None:
+        raise TypeError("the matrix must be of dtype float32, bfloat16 or float16")
+    shape = x.shape
+    if len(shape) != 2:
+        raise ValueError("a matrix is wanted, got %d dimensions" % len(shape))
+    rows, cols = shape
+    index = x.get_device()
+    if index < 0:
+        raise ValueError("the matrix must live in device memory")
+    ldx, step = x.stride()
+    # rows at any stride; a single column, or a single row, has no stride of its own to look at
+    if (step != 1 and cols > 1) or (ldx < cols and rows > 1):
+        x = x.contiguous()
+        ldx = cols
     n = m = nt = mt = 0
     if by_rows:
         n, m = _sizes(rows, cols, fmt)
     if by_columns:
         nt, mt = _sizes(cols, rows, fmt)
-    nv = fmt == "nv"
+    nv = block == 16
     ts = n + m + nt + mt                      # all parts are multiples of 16 bytes
-    buffer = torch.empty(ts + 16, dtype=torch.uint8, device=x.device)
+    device = x.device
+    buffer = torch.empty(ts + 16, dtype=torch.uint8, device=device)
     base = buffer.data_ptr()
     if rows and cols:
         status = B.lib().ssgd_fp4_quantise(
-            x.data_ptr(), B.DTYPE_CODE[x.dtype], rows, cols, max(x.stride(0), cols), B.FP4_FORMAT[fmt], B._ptr(amax, torch.float32, "amax"),
-            base + ts if nv else None, base if by_rows else None, base + n, base + n + m if by_columns else None, base + n + m + nt,
-            B._stream_of(x.device))
+            x.data_ptr(), dtype, rows, cols, ldx if ldx > cols else cols, 1 if nv else 0,
+            None if amax is None else B._ptr(amax, torch.float32, "amax"), base + ts if nv else None, base if by_rows else None, base + n,
+            base + n + m if by_columns else None, base + n + m + nt, B._stream_of(index))
         if status:
             B._check(status, "ssgd_fp4_quantise")
     elif nv:
         buffer[ts:ts + 8].view(torch.float32).fill_(1.0)
     at = ts if nv else None
-    return (Packed._in(buffer, base, (0, n, at), rows, cols, fmt) if by_rows else None,
-            Packed._in(buffer, base, (n + m, n + m + nt, at), cols, rows, fmt) if by_columns else None)
+    return (Packed._in(buffer, base, (0, n, at), rows, cols, fmt, device) if by_rows else None,
+            Packed._in(buffer, base, (n + m, n + m + nt, at), cols, rows, fmt, device) if by_columns else None)
 
 
 def quantise(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor] = None) -> Packed:
@@ -152,7 +155,7 @@ def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     if p.rows and p.cols:
         codes, scales, ts = p.pointers
         status = B.lib().ssgd_fp4_dequantise(codes, scales, ts, B.FP4_FORMAT[p.fmt], p.rows, p.cols, out.data_ptr(), B.DTYPE_CODE[dtype],
-                                             p.cols, B._stream_of(p.device))
+                                             p.cols, B._stream_of(p.device.index))
         if status:
             B._check(status, "ssgd_fp4_dequantise")
     return out
@@ -174,7 +177,7 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optio
         return out.zero_()
     if rows and cols:
         status = B.lib().ssgd_fp4_matmul(*a.pointers, *b.pointers, rows, cols, a.cols, B.FP4_FORMAT[a.fmt], out.data_ptr(),
-                                         B.DTYPE_CODE[out.dtype], ldo, _status_of(a.device)[1], B._stream_of(a.device))
+                                         B.DTYPE_CODE[out.dtype], ldo, _status_of(a.device)[1], B._stream_of(a.device.index))
         if status:
             B._check(status, "ssgd_fp4_matmul")
     return out
