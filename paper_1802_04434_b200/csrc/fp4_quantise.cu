@@ -12,6 +12,40 @@ namespace {
 
 __device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
+// Larger magnitude of two words of elements (one fp32 or two 16-bit), a NaN carried through; the sign is not defined.
+__device__ __forceinline__ unsigned larger(float, unsigned a, unsigned b) {
+  unsigned r;
+  asm("{\n\t.reg .f32 x, y;\n\tmov.b32 x, %1;\n\tmov.b32 y, %2;\n\tmax.NaN.xorsign.abs.f32 x, x, y;\n\tmov.b32 %0, x;\n\t}" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned larger(__nv_bfloat16, unsigned a, unsigned b) {
+  unsigned r;
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ unsigned larger(__half, unsigned a, unsigned b) {
+  unsigned r;
+  asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // Largest magnitude of a matrix, as ordered bits (NaN above infinity); `out` starts at 0.  A maximum does not depend on
 // the order, so the atomic gives the same bits every time.
 template <typename T>
@@ -79,86 +113,100 @@ __device__ __forceinline__ unsigned small_amax(const T* __restrict__ x, unsigned
   return top;
 }
 
-// x / s rounded to nearest, from the correctly rounded reciprocal r of s: one Newton correction of the product
-// (Markstein, "Computation of elementary functions on the IBM RISC System/6000", 1990).  In this order of signs a
-// quotient of -0 stays -0.
-__device__ __forceinline__ float quotient(float x, float s, float r) {
-  const float q = __fmul_rn(x, r);
-  return __fmaf_rn(__fmaf_rn(q, s, -x), -r, q);
-}
-
-// Eight values to the four bytes of their codes: nearest, ties to even, saturating.
-__device__ __forceinline__ unsigned fp4_pack8(const float* v) {
+// Eight values (four pairs) to the four bytes of their codes: nearest, ties to even, saturating.
+__device__ __forceinline__ unsigned fp4_pack8(const uint64_t (&v)[4]) {
   unsigned out;
-  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t.reg .f32 l0, l1, l2, l3, h0, h1, h2, h3;\n\t"
+      "mov.b64 {l0, h0}, %1;\n\tmov.b64 {l1, h1}, %2;\n\tmov.b64 {l2, h2}, %3;\n\tmov.b64 {l3, h3}, %4;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, h0, l0;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b1, h1, l1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, h2, l2;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b3, h3, l3;\n\t"
       "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
       : "=r"(out)
-      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+      : "l"(v[0]), "l"(v[1]), "l"(v[2]), "l"(v[3]));
   return out;
 }
 
-// Scale byte of a block from its largest magnitude, and what its values are divided by.
+// How a block is divided by its scale S: mx multiplies by 1 / S, a power of two.  nv multiplies by a reciprocal in two parts,
+// high <= 1 / S and low >= 0, as fma(x, high, x * low): off by 2^-43 before the one rounding, so the quotient is the correctly
+// rounded one except within that of halfway, and a tie between two codes stays a tie (a single fp32 reciprocal would send 1 %
+// of a bf16 tensor's values to the wrong side).  Two multiplications instead of a division's ten instructions.
 struct BlockScale {
   unsigned byte;
-  float S;        // nv: block scale times tensor scale
-  float inverse;  // nv: 1 / S to within the power of two correctly rounded; mx: 1 / S exactly
+  float high, low;
+  bool finite;
 };
 template <int FORMAT>
-__device__ __forceinline__ BlockScale block_scale(unsigned top_bits, float tensor_scale, float tensor_inverse) {
+__device__ __forceinline__ BlockScale block_scale(unsigned top_bits, float tensor_inverse) {
   BlockScale b;
-  b.S = 1.0f;
+  b.finite = top_bits < 0x7F800000u;
+  b.low = 0.0f;
   if constexpr (FORMAT == SSGD_MXFP4) {
     // exponent of max|x| minus 2, kept at -127 or above (a block of zeros or subnormals)
-    b.byte = top_bits >= 0x7F800000u ? 255u : (unsigned)max((int)(top_bits >> 23) - 2, 0);
-    b.inverse = b.byte == 255u ? 1.0f : __uint_as_float((254u - b.byte) << 23);
+    b.byte = b.finite ? (unsigned)max((int)(top_bits >> 23) - 2, 0) : 255u;
+    b.high = __uint_as_float((254u - b.byte) << 23);                    // not used where byte is 255
   } else {
-    const float s = __fdiv_rn(__fmul_rn(__uint_as_float(top_bits), tensor_inverse), 6.0f);
-    const __nv_fp8_storage_t q = __nv_cvt_float_to_fp8(fminf(s, 448.0f), __NV_SATFINITE, __NV_E4M3);
-    b.byte = top_bits >= 0x7F800000u ? 0x7Fu : max((unsigned)q, 1u);   // 1 = 2^-9, the least positive
-    const float scale = b.byte == 0x7Fu ? 1.0f : e4m3_value(b.byte);
-    b.S = scale * tensor_scale;
-    b.inverse = __frcp_rn(scale) * tensor_inverse;
+    // max|x| / t / 6 with 1 / 6 in two parts, then to the nearest E4M3 number, at most 448
+    const float v = __fmul_rn(__uint_as_float(top_bits), tensor_inverse);
+    const float s = __fmaf_rn(v, 0x1.555554p-3f, __fmul_rn(v, 0x1.555556p-27f));
+    unsigned short q;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q) : "f"(0.0f), "f"(s));
+    const unsigned byte = max((unsigned)q, 1u);                         // 1 = 2^-9, the least positive
+    unsigned half2;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half2) : "h"((unsigned short)byte));
+    const float scale = __low2float(*reinterpret_cast<const __half2*>(&half2));
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(scale));
+    r = __fmul_rn(r, 1.0f - 0x1p-22f);                                  // below 1 / scale for certain
+    b.high = r * tensor_inverse;
+    b.low = __fmul_rn(__fmaf_rn(-scale, r, 1.0f), b.high);
+    b.byte = b.finite ? byte : 0x7Fu;
   }
   return b;
 }
 
-// The codes of one block (B / 8 words) and its scale byte.
+// The codes of one block of B values, given as pairs, and its scale byte.
 template <int FORMAT, int B>
-__device__ __forceinline__ unsigned quantise_block(float (&v)[B], float tensor_scale, float tensor_inverse, unsigned (&word)[B / 8]) {
-  unsigned top = 0;
+__device__ __forceinline__ unsigned quantise_block(uint64_t (&v)[B / 2], unsigned top_bits, float tensor_inverse, unsigned (&word)[B / 8]) {
+  const BlockScale b = block_scale<FORMAT>(top_bits, tensor_inverse);
+  if (FORMAT == SSGD_NVFP4 && __uint_as_float(top_bits) * tensor_inverse > 1e30f) {   // a tensor scale far too small: saturate
+    const float limit = 1e30f / tensor_inverse;
 #pragma unroll
-  for (int i = 0; i < B; ++i) top = max(top, magnitude_bits(v[i]));
-  const BlockScale b = block_scale<FORMAT>(top, tensor_scale, tensor_inverse);
-  if (FORMAT == SSGD_NVFP4 && __uint_as_float(top) * tensor_inverse > 1e30f) {   // a tensor scale far too small: saturate
-    const float limit = 1e30f * tensor_scale;
-#pragma unroll
-    for (int i = 0; i < B; ++i) v[i] = fmaxf(-limit, fminf(limit, v[i]));
+    for (int i = 0; i < B / 2; ++i) {
+      const float lo = __uint_as_float((unsigned)v[i]), hi = __uint_as_float((unsigned)(v[i] >> 32));
+      v[i] = pair_of(fmaxf(-limit, fminf(limit, lo)), fmaxf(-limit, fminf(limit, hi)));
+    }
   }
+  const uint64_t high = pair_of(b.high, b.high), low = pair_of(b.low, b.low);
 #pragma unroll
-  for (int i = 0; i < B; ++i) v[i] = FORMAT == SSGD_MXFP4 ? __fmul_rn(v[i], b.inverse) : quotient(v[i], b.S, b.inverse);
+  for (int i = 0; i < B / 2; ++i) v[i] = FORMAT == SSGD_MXFP4 ? mul_pair(v[i], high) : fma_pair(v[i], high, mul_pair(v[i], low));
 #pragma unroll
-  for (int w = 0; w < B / 8; ++w) word[w] = top < 0x7F800000u ? fp4_pack8(v + 8 * w) : 0u;
+  for (int w = 0; w < B / 8; ++w) {
+    const uint64_t four[4] = {v[4 * w], v[4 * w + 1], v[4 * w + 2], v[4 * w + 3]};
+    word[w] = b.finite ? fp4_pack8(four) : 0u;
+  }
   return b.byte;
 }
 
-// Elements of B * sizeof(T) bytes in 16-byte pieces as floats.
-template <typename T, int B>
-__device__ __forceinline__ void to_floats(const uint4 (&raw)[B * sizeof(T) / 16], float (&v)[B]) {
-  const unsigned* w = reinterpret_cast<const unsigned*>(raw);
-  if constexpr (sizeof(T) == 4) {
+// Largest magnitude of an fp32 or of both 16-bit elements of a word, as the bits of a float.
+template <typename T> __device__ __forceinline__ unsigned top_of_word(unsigned w) {
+  const unsigned lo = magnitude_bits(low_to_float(T(), w));
+  return sizeof(T) == 4 ? lo : max(lo, magnitude_bits(high_to_float(T(), w)));
+}
+
+// A block that lies along words of elements.
+template <int FORMAT, int B, typename T>
+__device__ __forceinline__ unsigned quantise_words(const unsigned* w, float tensor_inverse, unsigned (&word)[B / 8]) {
+  constexpr int W = B * (int)sizeof(T) / 4;
+  unsigned top = w[0];
 #pragma unroll
-    for (int i = 0; i < B; ++i) v[i] = __uint_as_float(w[i]);
-  } else {
+  for (int i = 1; i < W; ++i) top = larger(T(), top, w[i]);
+  uint64_t v[B / 2];
 #pragma unroll
-    for (int i = 0; i < B / 2; ++i) {
-      v[2 * i] = low_to_float(T(), w[i]);
-      v[2 * i + 1] = high_to_float(T(), w[i]);
-    }
-  }
+  for (int i = 0; i < B / 2; ++i)
+    v[i] = sizeof(T) == 4 ? pair_of(__uint_as_float(w[(2 * i) % W]), __uint_as_float(w[(2 * i + 1) % W])) : pair_of(low_to_float(T(), w[i]), high_to_float(T(), w[i]));
+  return quantise_block<FORMAT, B>(v, top_of_word<T>(top), tensor_inverse, word);
 }
 
 // A CTA takes a tile of 128 x 128: whole scale tiles and 64 bytes of codes of every row, in both directions.
@@ -257,10 +305,8 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
 #pragma unroll
     for (unsigned u = 0; u < ITEMS; ++u) {
       const unsigned i = u * kThreads + threadIdx.x, r = i / NB, blk = i % NB, row = r0 + r, c = c0 + blk * B;
-      float v[B];
       unsigned word[B / 8];
-      to_floats<T, B>(raw[u], v);
-      const unsigned byte = quantise_block<FORMAT, B>(v, ts, ti, word);
+      const unsigned byte = quantise_words<FORMAT, B, T>(reinterpret_cast<const unsigned*>(raw[u]), ti, word);
       row_scales[blk / 4 * 512 + (r & 31u) * 16 + (r >> 5) * 4 + (blk & 3u)] = row < rows && c < cols ? (uint8_t)byte : 0;
       if (row < rows && c < row_bytes * 2) {
         uint8_t* out = codes + (size_t)row * row_bytes + c / 2;
@@ -279,14 +325,19 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
       unsigned element[B];
 #pragma unroll
       for (unsigned q = 0; q < B; ++q) element[q] = *reinterpret_cast<const unsigned*>(tile + (blk * B + q) * PITCH + w * 4);
+      unsigned top = element[0];
+#pragma unroll
+      for (unsigned q = 1; q < B; ++q) top = larger(T(), top, element[q]);
 #pragma unroll
       for (unsigned h = 0; h < PAIR; ++h) {
-        float v[B];
+        uint64_t v[B / 2];
         unsigned word[B / 8];
 #pragma unroll
-        for (unsigned q = 0; q < B; ++q)
-          v[q] = PAIR == 1 ? __uint_as_float(element[q]) : h == 0 ? low_to_float(T(), element[q]) : high_to_float(T(), element[q]);
-        const unsigned byte = quantise_block<FORMAT, B>(v, ts, ti, word), c = w * PAIR + h;
+        for (unsigned q = 0; q < B / 2; ++q)
+          v[q] = h == 0 ? pair_of(low_to_float(T(), element[2 * q]), low_to_float(T(), element[2 * q + 1]))
+                        : pair_of(high_to_float(T(), element[2 * q]), high_to_float(T(), element[2 * q + 1]));
+        const unsigned c = w * PAIR + h;
+        const unsigned byte = quantise_block<FORMAT, B>(v, magnitude_bits(h == 0 ? low_to_float(T(), top) : high_to_float(T(), top)), ti, word);
         col_scales[blk / 4 * 512 + (c & 31u) * 16 + (c >> 5) * 4 + (blk & 3u)] = c0 + c < cols && r0 + blk * B < rows ? (uint8_t)byte : 0;
         unsigned* out = reinterpret_cast<unsigned*>(out_codes + c * kCodePitch + blk * (B / 2));
         if constexpr (B == 16) *reinterpret_cast<uint2*>(out) = make_uint2(word[0], word[1]);
@@ -313,56 +364,56 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
   }
 }
 
-// Eight values per thread and group, at places where the stores are 16-byte aligned: row by row the first group starts up
-// to seven columns before the row, and a group's codes are cut out of two words.  A CTA takes kGroups x 256 groups from
-// its place in the sequence of all rows' groups; the one 64-bit division is the CTA's.
-constexpr unsigned kGroups = 4;
+// A thread takes groups of eight values, kRows rows of its place; `wide` threads of a CTA lie along a row, the others in
+// rows below, so that no index needs a division.
+//   ALIGNED    rows of out start at multiples of 16 bytes: a group is one word of codes and lies in one block
+//   otherwise  a row's groups start up to seven columns before it, where its stores are aligned; their codes are cut out of
+//              two words and may lie in two blocks
+constexpr unsigned kRows = 4;
 
-template <int FORMAT, typename T>
+template <int FORMAT, bool ALIGNED, typename T>
 __global__ void __launch_bounds__(kThreads)
 fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ tensor_scale,
-                      unsigned rows, unsigned cols, T* __restrict__ out, size_t ldo, unsigned groups) {
+                      unsigned rows, unsigned cols, T* __restrict__ out, size_t ldo, unsigned groups, unsigned wide, unsigned strips) {
   constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, V = 16 / sizeof(T);
-  __shared__ unsigned start[2];
-  if (threadIdx.x == 0) {
-    const size_t first = (size_t)blockIdx.x * (kThreads * kGroups);
-    start[0] = (unsigned)(first / groups);
-    start[1] = (unsigned)(first % groups);
-  }
-  __syncthreads();
   pdl_launch_dependents();
   pdl_wait();
   const float ts = FORMAT == SSGD_NVFP4 && tensor_scale ? __ldg(tensor_scale) : 1.0f;
-  const unsigned row_words = (cols + 31) / 32 * 4;
-  const size_t tiles_k = ((cols + B - 1) / B + 3) / 4;
-  T* line[kGroups];
-  int column[kGroups];
-  unsigned lo[kGroups], hi[kGroups], byte0[kGroups], byte1[kGroups];
+  const unsigned strip = blockIdx.x % strips, high = kThreads / wide;                 // strips of wide groups; rows at a time
+  const unsigned g = strip * wide + (threadIdx.x & (wide - 1)), row0 = blockIdx.x / strips * (high * kRows) + threadIdx.x / wide;
+  if (g >= groups) return;
+  const unsigned row_words = (cols + 31) / 32 * 4, tiles_k = ((cols + B - 1) / B + 3) / 4;
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(codes);
+  unsigned lo[kRows], hi[kRows], byte0[kRows], byte1[kRows];
+  int column[kRows];
 #pragma unroll
-  for (unsigned u = 0; u < kGroups; ++u) {
-    const unsigned from = start[1] + u * kThreads + threadIdx.x, row = start[0] + from / groups;
-    line[u] = out + (size_t)row * ldo;
-    const unsigned back = (unsigned)(reinterpret_cast<uintptr_t>(line[u]) / sizeof(T)) & (V - 1);   // columns before the row that complete 16 bytes
-    const int c = (int)(from % groups * 8) - (int)back;                                              // first column of the group
-    column[u] = row < rows ? c : (int)cols;
+  for (unsigned u = 0; u < kRows; ++u) {
+    const unsigned row = row0 + u * high;
     lo[u] = hi[u] = byte0[u] = byte1[u] = 0;
-    if (row < rows && c < (int)cols) {
-      const uint32_t* words = reinterpret_cast<const uint32_t*>(codes) + (size_t)row * row_words;
-      const int w = c >> 3;                                                                          // rounds down
-      if (w >= 0) lo[u] = words[w];
-      if (((unsigned)c & 7u) && (unsigned)(w + 1) < row_words) hi[u] = words[w + 1];
-      const unsigned b0 = (unsigned)max(c, 0) / B, b1 = min((unsigned)(c + 7), cols - 1) / B;
-      byte0[u] = scales[fp4_scale_index(row, b0, tiles_k)];
+    column[u] = (int)(g * 8);
+    if (!ALIGNED) column[u] -= (int)((unsigned)(reinterpret_cast<uintptr_t>(out + (size_t)row * ldo) / sizeof(T)) & (V - 1));
+    if (row >= rows || column[u] >= (int)cols) {
+      column[u] = (int)cols;
+      continue;
+    }
+    const int c = column[u], w = c >> 3;                                              // rounds down
+    const uint32_t* at = words + (size_t)row * row_words;
+    if (ALIGNED || w >= 0) lo[u] = at[w];
+    const unsigned b0 = (unsigned)max(c, 0) / B;
+    byte0[u] = scales[fp4_scale_index(row, b0, tiles_k)];
+    if (!ALIGNED) {
+      if (((unsigned)c & 7u) && (unsigned)(w + 1) < row_words) hi[u] = at[w + 1];
+      const unsigned b1 = min((unsigned)(c + 7), cols - 1) / B;
       byte1[u] = b1 == b0 ? byte0[u] : scales[fp4_scale_index(row, b1, tiles_k)];
     }
   }
 #pragma unroll
-  for (unsigned u = 0; u < kGroups; ++u) {
+  for (unsigned u = 0; u < kRows; ++u) {
     const int c = column[u];
     if (c >= (int)cols) continue;
-    const unsigned eight = __funnelshift_r(lo[u], hi[u], ((unsigned)c & 7u) * 4);
-    const float s0 = __fmul_rn(fp4_scale_value<FORMAT>(byte0[u]), ts), s1 = __fmul_rn(fp4_scale_value<FORMAT>(byte1[u]), ts);
-    const int change = (max(c, 0) / (int)B + 1) * (int)B - c;           // the group's place from which the second scale holds
+    const unsigned eight = ALIGNED ? lo[u] : __funnelshift_r(lo[u], hi[u], ((unsigned)c & 7u) * 4);
+    const float s0 = __fmul_rn(fp4_scale_value<FORMAT>(byte0[u]), ts), s1 = ALIGNED ? s0 : __fmul_rn(fp4_scale_value<FORMAT>(byte1[u]), ts);
+    const int change = ALIGNED ? 8 : (max(c, 0) / (int)B + 1) * (int)B - c;           // the group's place from which the second scale holds
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
@@ -370,7 +421,7 @@ fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
       v[j] = __fmul_rn(two.x, j < change ? s0 : s1);
       v[j + 1] = __fmul_rn(two.y, j + 1 < change ? s0 : s1);
     }
-    T* o = line[u] + c;
+    T* o = out + (size_t)(row0 + u * high) * ldo + c;
     if (c >= 0 && c + 8 <= (int)cols) {
       if constexpr (sizeof(T) == 4) {
         store4(o, make_float4(v[0], v[1], v[2], v[3]));
@@ -429,10 +480,15 @@ ssgd_status quantise_format(const T* x, size_t rows, size_t cols, size_t ldx, in
 
 template <int FORMAT, typename T>
 ssgd_status launch_dequantise(const uint8_t* codes, const uint8_t* scales, const float* ts, size_t rows, size_t cols, T* out, size_t ldo, cudaStream_t s) {
-  const size_t groups = (cols + 7) / 8 + (rows_aligned(out, rows > 1 ? ldo : 16 / sizeof(T)) ? 0 : 1), ctas = (rows * groups + kThreads * kGroups - 1) / (kThreads * kGroups);
+  const bool aligned = rows_aligned(out, rows > 1 ? ldo : 16 / sizeof(T));
+  const size_t groups = (cols + 7) / 8 + (aligned ? 0 : 1);
+  unsigned wide = 32;
+  while (wide < (unsigned)kThreads && wide < groups) wide *= 2;
+  const size_t strips = (groups + wide - 1) / wide, high = kThreads / wide * kRows, ctas = (rows + high - 1) / high * strips;
   if (ctas > kMaxGrid) return SSGD_ERR_SIZE;
-  launch_kernel(fp4_dequantise_kernel<FORMAT, T>, dim3((unsigned)ctas), dim3(kThreads), 0, s, true, codes, scales, ts, (unsigned)rows, (unsigned)cols,
-                out, ldo, (unsigned)groups);
+  auto kernel = aligned ? fp4_dequantise_kernel<FORMAT, true, T> : fp4_dequantise_kernel<FORMAT, false, T>;
+  launch_kernel(kernel, dim3((unsigned)ctas), dim3(kThreads), 0, s, true, codes, scales, ts, (unsigned)rows, (unsigned)cols, out, ldo, (unsigned)groups,
+                wide, (unsigned)strips);
   return launch_status();
 }
 
