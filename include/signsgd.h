@@ -417,6 +417,8 @@ ssgd_status ssgd_tensors_clip(const void* table, size_t tiles, size_t groups, in
  *   both 16-byte aligned.  Sides go up to SSGD_FP4_MAX_SIDE.                                                        */
 typedef enum { SSGD_MXFP4 = 0, SSGD_NVFP4 = 1 } ssgd_fp4_format;
 #define SSGD_FP4_MAX_SIDE ((size_t)1 << 30)
+#define SSGD_FP4_SMALL 32768        /* elements; see ssgd_fp4_quantise */
+#define SSGD_FP4_SCALE_FLOATS 1026
 
 size_t ssgd_fp4_row_bytes(size_t cols);
 size_t ssgd_fp4_scale_bytes(int format, size_t rows, size_t cols); /* 0 for a bad format or side */
@@ -430,7 +432,9 @@ size_t ssgd_fp4_scale_bytes(int format, size_t rows, size_t cols); /* 0 for a ba
  *   code = the value nearest to x / S (fp32 quotient), ties to the even code, magnitudes above 6 to 6.  A block with
  *   an infinity or a NaN has the NaN scale and reads back as NaN.
  *   amax          in   DEVICE float, nv only: max |x| of the operand, or NULL: the call finds it
- *   tensor_scale  out  DEVICE float[2], nv only (may be NULL for mx): [0] = t; [1] = the amax found when amax is NULL  */
+ *   tensor_scale  out  DEVICE, nv only (may be NULL for mx): [0] = t; [1] = the amax found when amax is NULL.  float[2];
+ *                      float[SSGD_FP4_SCALE_FLOATS], the rest being workspace, when amax is NULL and the matrix has more
+ *                      than SSGD_FP4_SMALL elements                                                                 */
 ssgd_status ssgd_fp4_quantise(const void* x, int dtype, size_t rows, size_t cols, size_t ldx, int format,
                               const float* amax, float* tensor_scale, uint8_t* codes, uint8_t* scales,
                               uint8_t* codes_t, uint8_t* scales_t, void* stream);

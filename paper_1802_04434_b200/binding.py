@@ -469,6 +469,7 @@ def tensors_clip(table: TensorTable, max_norm: float, norms: torch.Tensor, kind:
 
 
 FP4_FORMAT = {"mx": 0, "nv": 1}
+FP4_SMALL, FP4_SCALE_FLOATS = 32768, 1026
 
 
 def fp4_row_bytes(cols: int) -> int:
@@ -490,7 +491,7 @@ def fp4_quantise(x: torch.Tensor, rows: int, cols: int, ldx: int, fmt: str, amax
         if c is not None:
             _need(c, r * ((k + 31) // 32 * 16), name); _need(s, fp4_scale_bytes(fmt, r, k), "scales of " + name)
     if fmt == "nv":
-        _need(tensor_scale, 2, "tensor_scale")
+        _need(tensor_scale, FP4_SCALE_FLOATS if amax is None and rows * cols > FP4_SMALL else 2, "tensor_scale")
     u8, f32 = torch.uint8, torch.float32
     _check(lib().ssgd_fp4_quantise(
         _typed_ptr(x, "x"), DTYPE_CODE[x.dtype], rows, cols, ldx, FP4_FORMAT[fmt], _ptr(amax, f32, "amax"),

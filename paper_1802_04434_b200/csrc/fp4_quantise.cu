@@ -29,6 +29,12 @@ __device__ __forceinline__ unsigned larger(__half, unsigned a, unsigned b) {
   return r;
 }
 
+// Largest magnitude of an fp32 or of both 16-bit elements of a word, as the bits of a float.
+template <typename T> __device__ __forceinline__ unsigned top_of_word(unsigned w) {
+  const unsigned lo = magnitude_bits(low_to_float(T(), w));
+  return sizeof(T) == 4 ? lo : max(lo, magnitude_bits(high_to_float(T(), w)));
+}
+
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
   uint64_t r;
@@ -66,47 +72,62 @@ __device__ __forceinline__ unsigned piece_amax(const T* __restrict__ at, unsigne
   return top;
 }
 
-// A CTA takes a rectangle of kAmaxRows rows by 256 pieces of 16 bytes, eight pieces of a thread in flight; rows that are
-// not 16-byte aligned are read element by element, lanes side by side.
+// Largest magnitude of what each CTA sees, as bits, to a place of its own: no memory has to start at zero, and every CTA
+// of the quantisation that follows takes the largest of them.  A CTA takes rectangles of kAmaxRows rows by 256 pieces of
+// 16 bytes, eight pieces of a thread in flight; rows that are not 16-byte aligned are read element by element, lanes side
+// by side.
 constexpr unsigned kAmaxRows = 8;
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, unsigned tiles_c, unsigned* __restrict__ out) {
+fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, unsigned tiles_c, unsigned long long units,
+                unsigned* __restrict__ out) {
   constexpr unsigned V = 16 / sizeof(T), WIDE = kThreads * V;
-  const unsigned r0 = blockIdx.x / tiles_c * kAmaxRows, c0 = blockIdx.x % tiles_c * WIDE;
+  pdl_launch_dependents();
+  pdl_wait();
   unsigned top = 0;
-  if (vec) {
+  for (unsigned long long i = blockIdx.x; i < units; i += gridDim.x) {
+    const unsigned r0 = (unsigned)(i / tiles_c) * kAmaxRows, c0 = (unsigned)(i % tiles_c) * WIDE;
     const unsigned c = c0 + threadIdx.x * V;
+    if (vec && r0 + kAmaxRows <= rows && c + V <= cols) {
+      uint4 q[kAmaxRows];
 #pragma unroll
-    for (unsigned r = 0; r < kAmaxRows; ++r)
-      if (r0 + r < rows && c < cols) top = max(top, piece_amax(x + (size_t)(r0 + r) * ldx + c, cols - c, true));
-  } else {
-#pragma unroll 2
-    for (unsigned r = 0; r < kAmaxRows; ++r)
+      for (unsigned r = 0; r < kAmaxRows; ++r) q[r] = *reinterpret_cast<const uint4*>(x + (size_t)(r0 + r) * ldx + c);
+      unsigned w = 0;
 #pragma unroll
-      for (unsigned q = 0; q < V; ++q) {
-        const unsigned c = c0 + q * kThreads + threadIdx.x;
-        if (r0 + r < rows && c < cols) top = max(top, magnitude_bits(to_float(x[(size_t)(r0 + r) * ldx + c])));
-      }
+      for (unsigned r = 0; r < kAmaxRows; ++r) w = larger(T(), larger(T(), w, larger(T(), q[r].x, q[r].y)), larger(T(), q[r].z, q[r].w));
+      top = max(top, top_of_word<T>(w));
+    } else if (vec) {
+      for (unsigned r = 0; r < kAmaxRows; ++r)
+        if (r0 + r < rows && c < cols) top = max(top, piece_amax(x + (size_t)(r0 + r) * ldx + c, cols - c, true));
+    } else {
+#pragma unroll 4
+      for (unsigned r = 0; r < kAmaxRows; ++r)
+#pragma unroll
+        for (unsigned q = 0; q < V; ++q) {
+          const unsigned c = c0 + q * kThreads + threadIdx.x;
+          if (r0 + r < rows && c < cols) top = max(top, magnitude_bits(to_float(x[(size_t)(r0 + r) * ldx + c])));
+        }
+    }
   }
   top = __reduce_max_sync(0xFFFFFFFFu, top);
   __shared__ unsigned part[kThreads / 32];
   if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = top;
   __syncthreads();
-  if (threadIdx.x < 32) {
-    const unsigned all = __reduce_max_sync(0xFFFFFFFFu, threadIdx.x < kThreads / 32 ? part[threadIdx.x] : 0u);
-    if (threadIdx.x == 0) atomicMax(out, all);
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < kThreads / 32; ++w) top = max(top, part[w]);
+    out[blockIdx.x] = top;
   }
 }
 
 // Largest magnitude of a small matrix, by one CTA.
-template <typename T>
+template <unsigned THREADS, typename T>
 __device__ __forceinline__ unsigned small_amax(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec) {
   constexpr unsigned V = 16 / sizeof(T);
   const unsigned pieces = (cols + V - 1) / V, total = rows * pieces;
   unsigned top = 0;
 #pragma unroll 4
-  for (unsigned i = threadIdx.x; i < total; i += kThreads) {
+  for (unsigned i = threadIdx.x; i < total; i += THREADS) {
     const unsigned r = i / pieces, c = i % pieces * V;
     top = max(top, piece_amax(x + (size_t)r * ldx + c, cols - c, vec));
   }
@@ -189,12 +210,6 @@ __device__ __forceinline__ unsigned quantise_block(uint64_t (&v)[B / 2], unsigne
   return b.byte;
 }
 
-// Largest magnitude of an fp32 or of both 16-bit elements of a word, as the bits of a float.
-template <typename T> __device__ __forceinline__ unsigned top_of_word(unsigned w) {
-  const unsigned lo = magnitude_bits(low_to_float(T(), w));
-  return sizeof(T) == 4 ? lo : max(lo, magnitude_bits(high_to_float(T(), w)));
-}
-
 // A block that lies along words of elements.
 template <int FORMAT, int B, typename T>
 __device__ __forceinline__ unsigned quantise_words(const unsigned* w, float tensor_inverse, unsigned (&word)[B / 8]) {
@@ -209,54 +224,86 @@ __device__ __forceinline__ unsigned quantise_words(const unsigned* w, float tens
   return quantise_block<FORMAT, B>(v, top_of_word<T>(top), tensor_inverse, word);
 }
 
-// A CTA takes a tile of 128 x 128: whole scale tiles and 64 bytes of codes of every row, in both directions.
-//   rows     a thread takes a block of a row: its 16-byte loads are the tile's load, coalesced over the blocks of a row
-//   columns  the tile goes through shared memory; lanes run along the columns (two 16-bit columns in a word), the codes
-//            go back through shared memory so that 64 contiguous bytes of a column's row leave together
-// Rows that are not 16-byte aligned are loaded element by element, coalesced, into the same shared tile.
+// A CTA takes a tile of 128 x 128: whole scale tiles and 64 bytes of codes of every row, in both directions.  The tile goes
+// to shared memory by asynchronous copies, lanes side by side, in pieces of 16 bytes where the rows allow it, else of 4,
+// else element by element through registers; what lies outside the matrix becomes 0.
+//   rows     lanes run down the rows (a row is 16 bytes longer than its elements: no bank conflicts), a thread takes a
+//            block of a row
+//   columns  lanes run along the columns (two 16-bit columns in a word), a thread takes a block of a column, or of two
+// Either way the codes go back through shared memory, so that 64 contiguous bytes of a row of codes leave together.
 constexpr unsigned kSide = 128;
-constexpr unsigned kCodePitch = 80;                       // bytes of a column's 64 bytes of codes in shared memory
-
+constexpr unsigned kCodePitch = 80;                       // of the 64 bytes of codes of a row in shared memory
 template <typename T> constexpr unsigned kTilePitch = kSide * sizeof(T) + 16;
-template <typename T> unsigned tile_smem(bool tile, bool columns) {
-  return (tile ? kSide * kTilePitch<T> : 0) + (columns ? kSide * kCodePitch : 0);
-}
-constexpr size_t kFusedAmax = 32768;                      // elements up to which every CTA finds the tensor's maximum itself
+template <typename T> constexpr unsigned kTileSmem = kSide * kTilePitch<T> + kSide * kCodePitch;
+// fp32 tiles leave room for two CTAs of an SM, 16-bit ones for four
+template <typename T> constexpr unsigned kTileThreads = sizeof(T) == 4 ? 512 : 256;
+constexpr size_t kFusedAmax = SSGD_FP4_SMALL;             // elements up to which every CTA finds the tensor's maximum itself
 
+template <unsigned BYTES>
+__device__ __forceinline__ void copy_async(unsigned dst, const void* src, unsigned valid) {   // `valid` bytes, the rest 0
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(valid) : "memory");
+}
+
+template <unsigned BYTES, unsigned THREADS, typename T>
+__device__ __forceinline__ void load_tile(unsigned tile, const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, unsigned r0, unsigned c0) {
+  constexpr unsigned V = BYTES / sizeof(T), PER_ROW = kSide / V;
+#pragma unroll 8
+  for (unsigned i = threadIdx.x; i < kSide * PER_ROW; i += THREADS) {
+    const unsigned r = i / PER_ROW, c = i % PER_ROW * V;
+    const bool in = r0 + r < rows && c0 + c < cols;
+    const unsigned valid = in ? min(V, cols - (c0 + c)) * (unsigned)sizeof(T) : 0u;
+    copy_async<BYTES>(tile + r * kTilePitch<T> + c * (unsigned)sizeof(T), in ? x + (size_t)(r0 + r) * ldx + c0 + c : x, valid);
+  }
+}
+
+// 64 bytes of codes of each of the tile's rows, and its scale tiles, from shared memory.
+template <unsigned NB, unsigned THREADS>
+__device__ __forceinline__ void write_out(const unsigned char* staged, const uint8_t* staged_scales, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                          unsigned rows, unsigned cols, unsigned r0, unsigned c0) {
+  const size_t row_bytes = (size_t)((cols + 31) / 32) * 16, tiles_k = ((cols + kSide / NB - 1) / (kSide / NB) + 3) / 4, first = c0 / (kSide / NB) / 4;
+#pragma unroll
+  for (unsigned i = threadIdx.x; i < kSide * 4; i += THREADS) {
+    const unsigned r = i / 4, at = i % 4 * 16;
+    if (r0 + r < rows && c0 / 2 + at < row_bytes)
+      *reinterpret_cast<uint4*>(codes + (size_t)(r0 + r) * row_bytes + c0 / 2 + at) = *reinterpret_cast<const uint4*>(staged + r * kCodePitch + at);
+  }
+  if (threadIdx.x < NB / 4 * 32 && first + threadIdx.x / 32 < tiles_k)
+    reinterpret_cast<uint4*>(scales + (r0 / kSide * tiles_k + first) * 512)[threadIdx.x] = reinterpret_cast<const uint4*>(staged_scales)[threadIdx.x];
+}
+
+template <int B>
+__device__ __forceinline__ void stage_codes(unsigned char* to, const unsigned (&word)[B / 8]) {
+  if constexpr (B == 16) *reinterpret_cast<uint2*>(to) = make_uint2(word[0], word[1]);
+  else *reinterpret_cast<uint4*>(to) = make_uint4(word[0], word[1], word[2], word[3]);
+}
+
+// piece: bytes that a copy of x's elements may have (16, 4, or 0: none, its rows start at odd 16-bit elements)
 template <int FORMAT, bool ROWS, bool COLS, typename T>
-__global__ void __launch_bounds__(kThreads)
-fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, const float* __restrict__ amax,
-                    float* __restrict__ tensor_scale, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+__global__ void __launch_bounds__(kTileThreads<T>)
+fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, unsigned piece, const float* __restrict__ amax,
+                    unsigned maxima, float* tensor_scale, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                     uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, unsigned tiles_c) {
-  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, NB = kSide / B, ITEMS = kSide * NB / kThreads;
+  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, NB = kSide / B, THREADS = kTileThreads<T>;
   constexpr unsigned PIECES = B * sizeof(T) / 16, PITCH = kTilePitch<T>;
   extern __shared__ __align__(16) unsigned char tile[];
-  __shared__ __align__(16) uint8_t row_scales[NB * kSide], col_scales[COLS ? NB * kSide : 16];
-  __shared__ unsigned part[kThreads / 32];
+  __shared__ __align__(16) uint8_t staged_scales[NB * kSide];
+  __shared__ unsigned part[THREADS / 32];
+  unsigned char* staged = tile + kSide * PITCH;
   pdl_launch_dependents();
   pdl_wait();
   const unsigned at = gridDim.x - 1 - blockIdx.x;         // from the end: what the maximum's pass read last is still in L2
   const unsigned r0 = at / tiles_c * kSide, c0 = at % tiles_c * kSide;
 
-  uint4 raw[ITEMS][PIECES];
-  if (vec) {
-#pragma unroll
-    for (unsigned u = 0; u < ITEMS; ++u) {
-      const unsigned i = u * kThreads + threadIdx.x, row = r0 + i / NB, c = c0 + i % NB * B;
-      const T* src = x + (size_t)row * ldx + c;
-#pragma unroll
-      for (unsigned q = 0; q < PIECES; ++q) {
-        constexpr unsigned V = 16 / sizeof(T);
-        raw[u][q] = make_uint4(0, 0, 0, 0);
-        if (row < rows && c + (q + 1) * V <= cols) {
-          raw[u][q] = *reinterpret_cast<const uint4*>(src + q * V);
-        } else if (row < rows && c + q * V < cols) {      // the row ends inside this piece
-          T e[V];
-#pragma unroll
-          for (unsigned j = 0; j < V; ++j) e[j] = c + q * V + j < cols ? src[q * V + j] : from_float<T>(0.0f);
-          raw[u][q] = *reinterpret_cast<const uint4*>(e);
-        }
-      }
+  if (piece == 16) {
+    load_tile<16, THREADS>((unsigned)__cvta_generic_to_shared(tile), x, rows, cols, ldx, r0, c0);
+  } else if (piece == 4) {
+    load_tile<4, THREADS>((unsigned)__cvta_generic_to_shared(tile), x, rows, cols, ldx, r0, c0);
+  } else {
+#pragma unroll 32
+    for (unsigned i = threadIdx.x; i < kSide * kSide; i += THREADS) {
+      const unsigned r = i / kSide, c = i % kSide;
+      const bool in = r0 + r < rows && c0 + c < cols;
+      *reinterpret_cast<T*>(tile + r * PITCH + c * sizeof(T)) = in ? x[(size_t)(r0 + r) * ldx + c0 + c] : from_float<T>(0.0f);
     }
   }
   float ts = 1.0f;
@@ -264,13 +311,16 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
     float top;
     if (amax) {
       top = __ldg(amax);
-    } else {
-      const unsigned t = __reduce_max_sync(0xFFFFFFFFu, small_amax(x, rows, cols, ldx, vec));
+    } else {                                              // from the maxima of the pass before, or from the matrix itself
+      unsigned t = 0;
+      for (unsigned i = threadIdx.x; i < maxima; i += THREADS) t = max(t, __float_as_uint(__ldcg(tensor_scale + 2 + i)));
+      if (maxima == 0) t = small_amax<THREADS>(x, rows, cols, ldx, piece == 16);
+      t = __reduce_max_sync(0xFFFFFFFFu, t);
       if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = t;
       __syncthreads();
       unsigned all = 0;
 #pragma unroll
-      for (int w = 0; w < kThreads / 32; ++w) all = max(all, part[w]);
+      for (unsigned w = 0; w < THREADS / 32; ++w) all = max(all, part[w]);
       top = __uint_as_float(all);
       if (blockIdx.x == 0 && threadIdx.x == 0) tensor_scale[1] = top;
     }
@@ -278,50 +328,30 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
     if (blockIdx.x == 0 && threadIdx.x == 0) tensor_scale[0] = ts;
   }
   const float ti = __fdiv_rn(1.0f, ts);
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
 
-  if (!vec) {
-#pragma unroll 16
-    for (unsigned i = threadIdx.x; i < kSide * kSide; i += kThreads) {
-      const unsigned r = i / kSide, c = i % kSide;
-      const bool in = r0 + r < rows && c0 + c < cols;
-      *reinterpret_cast<T*>(tile + r * PITCH + c * sizeof(T)) = in ? x[(size_t)(r0 + r) * ldx + c0 + c] : from_float<T>(0.0f);
+  if constexpr (ROWS) {
+#pragma unroll
+    for (unsigned u = 0; u < kSide * NB / THREADS; ++u) {
+      const unsigned i = u * THREADS + threadIdx.x, r = i % kSide, blk = i / kSide;
+      uint4 raw[PIECES];
+#pragma unroll
+      for (unsigned q = 0; q < PIECES; ++q) raw[q] = *reinterpret_cast<const uint4*>(tile + r * PITCH + blk * B * sizeof(T) + q * 16);
+      unsigned word[B / 8];
+      const unsigned byte = quantise_words<FORMAT, B, T>(reinterpret_cast<const unsigned*>(raw), ti, word);
+      staged_scales[blk / 4 * 512 + (r & 31u) * 16 + (r >> 5) * 4 + (blk & 3u)] = r0 + r < rows && c0 + blk * B < cols ? (uint8_t)byte : 0;
+      stage_codes<B>(staged + r * kCodePitch + blk * (B / 2), word);
     }
     __syncthreads();
+    write_out<NB, THREADS>(staged, staged_scales, codes, scales, rows, cols, r0, c0);
+    if (COLS) __syncthreads();
   }
-  if (COLS || !vec) {
-#pragma unroll
-    for (unsigned u = 0; u < ITEMS; ++u) {
-      const unsigned i = u * kThreads + threadIdx.x;
-      uint4* slot = reinterpret_cast<uint4*>(tile + i / NB * PITCH + i % NB * B * sizeof(T));
-#pragma unroll
-      for (unsigned q = 0; q < PIECES; ++q) {
-        if (vec) slot[q] = raw[u][q];
-        else if (ROWS) raw[u][q] = slot[q];
-      }
-    }
-  }
-  if constexpr (ROWS) {
-    const size_t row_bytes = (size_t)((cols + 31) / 32) * 16;
-#pragma unroll
-    for (unsigned u = 0; u < ITEMS; ++u) {
-      const unsigned i = u * kThreads + threadIdx.x, r = i / NB, blk = i % NB, row = r0 + r, c = c0 + blk * B;
-      unsigned word[B / 8];
-      const unsigned byte = quantise_words<FORMAT, B, T>(reinterpret_cast<const unsigned*>(raw[u]), ti, word);
-      row_scales[blk / 4 * 512 + (r & 31u) * 16 + (r >> 5) * 4 + (blk & 3u)] = row < rows && c < cols ? (uint8_t)byte : 0;
-      if (row < rows && c < row_bytes * 2) {
-        uint8_t* out = codes + (size_t)row * row_bytes + c / 2;
-        if constexpr (B == 16) *reinterpret_cast<uint2*>(out) = make_uint2(word[0], word[1]);
-        else *reinterpret_cast<uint4*>(out) = make_uint4(word[0], word[1], word[2], word[3]);
-      }
-    }
-  }
-  if (COLS) __syncthreads();
   if constexpr (COLS) {
     constexpr unsigned PAIR = sizeof(T) == 4 ? 1 : 2, WORDS = kSide / PAIR;     // columns of a word, words of a row
-    unsigned char* out_codes = tile + kSide * PITCH;
 #pragma unroll
-    for (unsigned u = 0; u < WORDS * NB / kThreads; ++u) {
-      const unsigned i = u * kThreads + threadIdx.x, w = i % WORDS, blk = i / WORDS;
+    for (unsigned u = 0; u < (WORDS * NB + THREADS - 1) / THREADS; ++u) {
+      const unsigned i = u * THREADS + threadIdx.x, w = i % WORDS, blk = i / WORDS;
       unsigned element[B];
 #pragma unroll
       for (unsigned q = 0; q < B; ++q) element[q] = *reinterpret_cast<const unsigned*>(tile + (blk * B + q) * PITCH + w * 4);
@@ -338,36 +368,19 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
                         : pair_of(high_to_float(T(), element[2 * q]), high_to_float(T(), element[2 * q + 1]));
         const unsigned c = w * PAIR + h;
         const unsigned byte = quantise_block<FORMAT, B>(v, magnitude_bits(h == 0 ? low_to_float(T(), top) : high_to_float(T(), top)), ti, word);
-        col_scales[blk / 4 * 512 + (c & 31u) * 16 + (c >> 5) * 4 + (blk & 3u)] = c0 + c < cols && r0 + blk * B < rows ? (uint8_t)byte : 0;
-        unsigned* out = reinterpret_cast<unsigned*>(out_codes + c * kCodePitch + blk * (B / 2));
-        if constexpr (B == 16) *reinterpret_cast<uint2*>(out) = make_uint2(word[0], word[1]);
-        else *reinterpret_cast<uint4*>(out) = make_uint4(word[0], word[1], word[2], word[3]);
+        staged_scales[blk / 4 * 512 + (c & 31u) * 16 + (c >> 5) * 4 + (blk & 3u)] = c0 + c < cols && r0 + blk * B < rows ? (uint8_t)byte : 0;
+        stage_codes<B>(staged + c * kCodePitch + blk * (B / 2), word);
       }
     }
-  }
-  __syncthreads();
-  if constexpr (ROWS) {
-    const size_t tiles_k = ((cols + B - 1) / B + 3) / 4, first = c0 / B / 4;
-    if (threadIdx.x < NB / 4 * 32 && first + threadIdx.x / 32 < tiles_k)
-      reinterpret_cast<uint4*>(scales + (r0 / kSide * tiles_k + first) * 512)[threadIdx.x] = reinterpret_cast<const uint4*>(row_scales)[threadIdx.x];
-  }
-  if constexpr (COLS) {
-    const size_t row_bytes = (size_t)((rows + 31) / 32) * 16, tiles_k = ((rows + B - 1) / B + 3) / 4, first = r0 / B / 4;
-    if (threadIdx.x < NB / 4 * 32 && first + threadIdx.x / 32 < tiles_k)
-      reinterpret_cast<uint4*>(scales_t + (c0 / kSide * tiles_k + first) * 512)[threadIdx.x] = reinterpret_cast<const uint4*>(col_scales)[threadIdx.x];
-#pragma unroll
-    for (unsigned i = threadIdx.x; i < kSide * 4; i += kThreads) {
-      const unsigned c = i / 4, b = i % 4 * 16;
-      if (c0 + c < cols && r0 / 2 + b < row_bytes)
-        *reinterpret_cast<uint4*>(codes_t + (size_t)(c0 + c) * row_bytes + r0 / 2 + b) = *reinterpret_cast<const uint4*>(tile + kSide * PITCH + c * kCodePitch + b);
-    }
+    __syncthreads();
+    write_out<NB, THREADS>(staged, staged_scales, codes_t, scales_t, cols, rows, c0, r0);
   }
 }
 
-// A thread takes groups of eight values, kRows rows of its place; `wide` threads of a CTA lie along a row, the others in
+// A thread takes groups of G values, kRows rows of its place; `wide` threads of a CTA lie along a row, the others in
 // rows below, so that no index needs a division.
-//   ALIGNED    rows of out start at multiples of 16 bytes: a group is one word of codes and lies in one block
-//   otherwise  a row's groups start up to seven columns before it, where its stores are aligned; their codes are cut out of
+//   ALIGNED    rows of out start at multiples of 16 bytes: a group is 16 bytes, lies in one block, and its codes in one word
+//   otherwise  a row's groups of eight start up to V - 1 columns before it, where its stores are aligned; their codes are cut out of
 //              two words and may lie in two blocks
 constexpr unsigned kRows = 4;
 
@@ -375,7 +388,7 @@ template <int FORMAT, bool ALIGNED, typename T>
 __global__ void __launch_bounds__(kThreads)
 fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ tensor_scale,
                       unsigned rows, unsigned cols, T* __restrict__ out, size_t ldo, unsigned groups, unsigned wide, unsigned strips) {
-  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, V = 16 / sizeof(T);
+  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, V = 16 / sizeof(T), G = ALIGNED ? V : 8;
   pdl_launch_dependents();
   pdl_wait();
   const float ts = FORMAT == SSGD_NVFP4 && tensor_scale ? __ldg(tensor_scale) : 1.0f;
@@ -390,7 +403,7 @@ fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
   for (unsigned u = 0; u < kRows; ++u) {
     const unsigned row = row0 + u * high;
     lo[u] = hi[u] = byte0[u] = byte1[u] = 0;
-    column[u] = (int)(g * 8);
+    column[u] = (int)(g * G);
     if (!ALIGNED) column[u] -= (int)((unsigned)(reinterpret_cast<uintptr_t>(out + (size_t)row * ldo) / sizeof(T)) & (V - 1));
     if (row >= rows || column[u] >= (int)cols) {
       column[u] = (int)cols;
@@ -402,8 +415,8 @@ fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
     const unsigned b0 = (unsigned)max(c, 0) / B;
     byte0[u] = scales[fp4_scale_index(row, b0, tiles_k)];
     if (!ALIGNED) {
-      if (((unsigned)c & 7u) && (unsigned)(w + 1) < row_words) hi[u] = at[w + 1];
-      const unsigned b1 = min((unsigned)(c + 7), cols - 1) / B;
+      if (((unsigned)c & 7u) + G > 8 && (unsigned)(w + 1) < row_words) hi[u] = at[w + 1];
+      const unsigned b1 = min((unsigned)(c + (int)G - 1), cols - 1) / B;
       byte1[u] = b1 == b0 ? byte0[u] : scales[fp4_scale_index(row, b1, tiles_k)];
     }
   }
@@ -411,27 +424,27 @@ fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
   for (unsigned u = 0; u < kRows; ++u) {
     const int c = column[u];
     if (c >= (int)cols) continue;
-    const unsigned eight = ALIGNED ? lo[u] : __funnelshift_r(lo[u], hi[u], ((unsigned)c & 7u) * 4);
+    const unsigned four = ((unsigned)c & 7u) * 4, bits = ALIGNED ? lo[u] >> four : __funnelshift_r(lo[u], hi[u], four);
     const float s0 = __fmul_rn(fp4_scale_value<FORMAT>(byte0[u]), ts), s1 = ALIGNED ? s0 : __fmul_rn(fp4_scale_value<FORMAT>(byte1[u]), ts);
-    const int change = ALIGNED ? 8 : (max(c, 0) / (int)B + 1) * (int)B - c;           // the group's place from which the second scale holds
-    float v[8];
+    const int change = ALIGNED ? (int)G : (max(c, 0) / (int)B + 1) * (int)B - c;           // the group's place from which the second scale holds
+    float v[G];
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-      const float2 two = fp4_pair_value(eight >> (4 * j));
+    for (int j = 0; j < (int)G; j += 2) {
+      const float2 two = fp4_pair_value(bits >> (4 * j));
       v[j] = __fmul_rn(two.x, j < change ? s0 : s1);
       v[j + 1] = __fmul_rn(two.y, j + 1 < change ? s0 : s1);
     }
     T* o = out + (size_t)(row0 + u * high) * ldo + c;
-    if (c >= 0 && c + 8 <= (int)cols) {
+    if (c >= 0 && c + (int)G <= (int)cols) {
       if constexpr (sizeof(T) == 4) {
-        store4(o, make_float4(v[0], v[1], v[2], v[3]));
-        store4(o + 4, make_float4(v[4], v[5], v[6], v[7]));
+#pragma unroll
+        for (int j = 0; j < (int)G; j += 4) store4(o + j, make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]));
       } else {
         __stcs(reinterpret_cast<uint4*>(o), make_uint4(pack2(T(), v[0], v[1]), pack2(T(), v[2], v[3]), pack2(T(), v[4], v[5]), pack2(T(), v[6], v[7])));
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < (int)G; ++j)
         if (c + j >= 0 && c + j < (int)cols) o[j] = from_float<T>(v[j]);
     }
   }
@@ -441,34 +454,37 @@ template <typename T>
 bool rows_aligned(const T* x, size_t ldx) { return aligned16(x) && ldx * sizeof(T) % 16 == 0; }
 
 template <int FORMAT, bool ROWS, bool COLS, typename T>
-ssgd_status launch_quantise(const T* x, size_t rows, size_t cols, size_t ldx, const float* amax, float* tensor_scale, uint8_t* codes,
-                            uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, cudaStream_t s) {
+ssgd_status launch_quantise(const T* x, size_t rows, size_t cols, size_t ldx, const float* amax, unsigned maxima, float* tensor_scale,
+                            uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, cudaStream_t s) {
   const size_t tiles_c = (cols + kSide - 1) / kSide, tiles = (rows + kSide - 1) / kSide * tiles_c;
   if (tiles > kMaxGrid) return SSGD_ERR_SIZE;
-  const bool vec = rows_aligned(x, ldx);
-  const unsigned smem = tile_smem<T>(COLS || !vec, COLS);
+  const bool words = (reinterpret_cast<uintptr_t>(x) | ldx * sizeof(T)) % 4 == 0;
+  const unsigned piece = rows_aligned(x, ldx) ? 16 : words ? 4 : 0;
   auto kernel = fp4_quantise_kernel<FORMAT, ROWS, COLS, T>;
   static unsigned long long seen = 0;
-  if (smem > 32768 && !allow_smem(reinterpret_cast<const void*>(kernel), tile_smem<T>(true, COLS), &seen)) return SSGD_ERR_CUDA;
-  launch_kernel(kernel, dim3((unsigned)tiles), dim3(kThreads), smem, s, true, x, (unsigned)rows, (unsigned)cols, ldx, vec, amax, tensor_scale,
-                codes, scales, codes_t, scales_t, (unsigned)tiles_c);
+  if (!allow_smem(reinterpret_cast<const void*>(kernel), kTileSmem<T>, &seen)) return SSGD_ERR_CUDA;
+  launch_kernel(kernel, dim3((unsigned)tiles), dim3(kTileThreads<T>), kTileSmem<T>, s, true, x, (unsigned)rows, (unsigned)cols, ldx, piece, amax,
+                maxima, tensor_scale, codes, scales, codes_t, scales_t, (unsigned)tiles_c);
   return launch_status();
 }
 
 template <int FORMAT, typename T>
 ssgd_status quantise_typed(const T* x, size_t rows, size_t cols, size_t ldx, const float* amax, float* tensor_scale, uint8_t* codes,
                            uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, cudaStream_t s) {
+  unsigned maxima = 0;
   if (FORMAT == SSGD_NVFP4 && !amax && rows * cols > kFusedAmax) {
-    if (cudaMemsetAsync(tensor_scale + 1, 0, sizeof(float), s) != cudaSuccess) return SSGD_ERR_CUDA;
-    const size_t wide = kThreads * 16 / sizeof(T), tiles_c = (cols + wide - 1) / wide, ctas = (rows + kAmaxRows - 1) / kAmaxRows * tiles_c;
-    if (ctas > kMaxGrid) return SSGD_ERR_SIZE;
-    fp4_amax_kernel<<<(unsigned)ctas, kThreads, 0, s>>>(x, (unsigned)rows, (unsigned)cols, ldx, rows_aligned(x, ldx), (unsigned)tiles_c,
-                                                        reinterpret_cast<unsigned*>(tensor_scale + 1));
-    amax = tensor_scale + 1;
+    DeviceInfo info;
+    if (!device_info(&info)) return SSGD_ERR_CUDA;
+    const size_t wide = kThreads * 16 / sizeof(T), tiles_c = (cols + wide - 1) / wide, units = (rows + kAmaxRows - 1) / kAmaxRows * tiles_c;
+    const size_t most = (size_t)info.sms * 6 < SSGD_FP4_SCALE_FLOATS - 2 ? (size_t)info.sms * 6 : SSGD_FP4_SCALE_FLOATS - 2;
+    maxima = (unsigned)(units < most ? units : most);
+    launch_kernel(fp4_amax_kernel<T>, dim3(maxima), dim3(kThreads), 0, s, true, x, (unsigned)rows, (unsigned)cols, ldx, rows_aligned(x, ldx),
+                  (unsigned)tiles_c, (unsigned long long)units, reinterpret_cast<unsigned*>(tensor_scale + 2));
   }
-  if (codes && codes_t) return launch_quantise<FORMAT, true, true>(x, rows, cols, ldx, amax, tensor_scale, codes, scales, codes_t, scales_t, s);
-  if (codes) return launch_quantise<FORMAT, true, false>(x, rows, cols, ldx, amax, tensor_scale, codes, scales, codes_t, scales_t, s);
-  return launch_quantise<FORMAT, false, true>(x, rows, cols, ldx, amax, tensor_scale, codes, scales, codes_t, scales_t, s);
+  if (codes && codes_t)
+    return launch_quantise<FORMAT, true, true>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
+  if (codes) return launch_quantise<FORMAT, true, false>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
+  return launch_quantise<FORMAT, false, true>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
 }
 
 template <typename T>
@@ -481,7 +497,7 @@ ssgd_status quantise_format(const T* x, size_t rows, size_t cols, size_t ldx, in
 template <int FORMAT, typename T>
 ssgd_status launch_dequantise(const uint8_t* codes, const uint8_t* scales, const float* ts, size_t rows, size_t cols, T* out, size_t ldo, cudaStream_t s) {
   const bool aligned = rows_aligned(out, rows > 1 ? ldo : 16 / sizeof(T));
-  const size_t groups = (cols + 7) / 8 + (aligned ? 0 : 1);
+  const size_t G = aligned ? 16 / sizeof(T) : 8, groups = (cols + G - 1) / G + (aligned ? 0 : 1);
   unsigned wide = 32;
   while (wide < (unsigned)kThreads && wide < groups) wide *= 2;
   const size_t strips = (groups + wide - 1) / wide, high = kThreads / wide * kRows, ctas = (rows + high - 1) / high * strips;

@@ -117,7 +117,8 @@ def _quantise(x, fmt, amax, by_rows, by_columns):
     nv = block == 16
     ts = n + m + nt + mt                      # all parts are multiples of 16 bytes
     device = x.device
-    buffer = torch.empty(ts + 16, dtype=torch.uint8, device=device)
+    tail = 0 if not nv else 4 * B.FP4_SCALE_FLOATS if amax is None and rows * cols > B.FP4_SMALL else 8
+    buffer = torch.empty(ts + tail, dtype=torch.uint8, device=device)
     base = buffer.data_ptr()
     if rows and cols:
         status = B.lib().ssgd_fp4_quantise(
