@@ -73,11 +73,10 @@ __device__ __forceinline__ unsigned piece_amax(const T* __restrict__ at, unsigne
 }
 
 // Largest magnitude of what each CTA sees, as bits, to a place of its own: no memory has to start at zero, and every CTA
-// of the quantisation that follows takes the largest of them.  A CTA takes rectangles of kAmaxRows rows by 256 pieces of
-// 16 bytes, eight pieces of a thread in flight; rows that are not 16-byte aligned are read element by element, lanes side
+// of the quantisation that follows takes the largest of them.  A CTA takes rectangles of ROWS rows by 256 pieces of
+// 16 bytes, all pieces of a thread in flight: eight rows, or two where eight would leave SMs without work; rows that are not 16-byte aligned are read element by element, lanes side
 // by side.
-constexpr unsigned kAmaxRows = 8;
-template <typename T>
+template <unsigned ROWS, typename T>
 __global__ void __launch_bounds__(kThreads)
 fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, unsigned tiles_c, unsigned long long units,
                 unsigned* __restrict__ out) {
@@ -86,22 +85,22 @@ fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ld
   pdl_wait();
   unsigned top = 0;
   for (unsigned long long i = blockIdx.x; i < units; i += gridDim.x) {
-    const unsigned r0 = (unsigned)(i / tiles_c) * kAmaxRows, c0 = (unsigned)(i % tiles_c) * WIDE;
+    const unsigned r0 = (unsigned)(i / tiles_c) * ROWS, c0 = (unsigned)(i % tiles_c) * WIDE;
     const unsigned c = c0 + threadIdx.x * V;
-    if (vec && r0 + kAmaxRows <= rows && c + V <= cols) {
-      uint4 q[kAmaxRows];
+    if (vec && r0 + ROWS <= rows && c + V <= cols) {
+      uint4 q[ROWS];
 #pragma unroll
-      for (unsigned r = 0; r < kAmaxRows; ++r) q[r] = *reinterpret_cast<const uint4*>(x + (size_t)(r0 + r) * ldx + c);
+      for (unsigned r = 0; r < ROWS; ++r) q[r] = *reinterpret_cast<const uint4*>(x + (size_t)(r0 + r) * ldx + c);
       unsigned w = 0;
 #pragma unroll
-      for (unsigned r = 0; r < kAmaxRows; ++r) w = larger(T(), larger(T(), w, larger(T(), q[r].x, q[r].y)), larger(T(), q[r].z, q[r].w));
+      for (unsigned r = 0; r < ROWS; ++r) w = larger(T(), larger(T(), w, larger(T(), q[r].x, q[r].y)), larger(T(), q[r].z, q[r].w));
       top = max(top, top_of_word<T>(w));
     } else if (vec) {
-      for (unsigned r = 0; r < kAmaxRows; ++r)
+      for (unsigned r = 0; r < ROWS; ++r)
         if (r0 + r < rows && c < cols) top = max(top, piece_amax(x + (size_t)(r0 + r) * ldx + c, cols - c, true));
     } else {
-#pragma unroll 4
-      for (unsigned r = 0; r < kAmaxRows; ++r)
+#pragma unroll (ROWS < 4 ? ROWS : 4)
+      for (unsigned r = 0; r < ROWS; ++r)
 #pragma unroll
         for (unsigned q = 0; q < V; ++q) {
           const unsigned c = c0 + q * kThreads + threadIdx.x;
@@ -235,8 +234,6 @@ constexpr unsigned kSide = 128;
 constexpr unsigned kCodePitch = 80;                       // of the 64 bytes of codes of a row in shared memory
 template <typename T> constexpr unsigned kTilePitch = kSide * sizeof(T) + 16;
 template <typename T> constexpr unsigned kTileSmem = kSide * kTilePitch<T> + kSide * kCodePitch;
-// fp32 tiles leave room for two CTAs of an SM, 16-bit ones for four
-template <typename T> constexpr unsigned kTileThreads = sizeof(T) == 4 ? 512 : 256;
 constexpr size_t kFusedAmax = SSGD_FP4_SMALL;             // elements up to which every CTA finds the tensor's maximum itself
 
 template <unsigned BYTES>
@@ -278,12 +275,12 @@ __device__ __forceinline__ void stage_codes(unsigned char* to, const unsigned (&
 }
 
 // piece: bytes that a copy of x's elements may have (16, 4, or 0: none, its rows start at odd 16-bit elements)
-template <int FORMAT, bool ROWS, bool COLS, typename T>
-__global__ void __launch_bounds__(kTileThreads<T>)
+template <int FORMAT, bool ROWS, bool COLS, unsigned THREADS, typename T>
+__global__ void __launch_bounds__(THREADS)
 fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, unsigned piece, const float* __restrict__ amax,
                     unsigned maxima, float* tensor_scale, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                     uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, unsigned tiles_c) {
-  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, NB = kSide / B, THREADS = kTileThreads<T>;
+  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, NB = kSide / B;
   constexpr unsigned PIECES = B * sizeof(T) / 16, PITCH = kTilePitch<T>;
   extern __shared__ __align__(16) unsigned char tile[];
   __shared__ __align__(16) uint8_t staged_scales[NB * kSide];
@@ -296,10 +293,10 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
 
   if (piece == 16) {
     load_tile<16, THREADS>((unsigned)__cvta_generic_to_shared(tile), x, rows, cols, ldx, r0, c0);
-  } else if (piece == 4) {
+  } else if (sizeof(T) == 4 || piece == 4) {
     load_tile<4, THREADS>((unsigned)__cvta_generic_to_shared(tile), x, rows, cols, ldx, r0, c0);
   } else {
-#pragma unroll 32
+#pragma unroll 16
     for (unsigned i = threadIdx.x; i < kSide * kSide; i += THREADS) {
       const unsigned r = i / kSide, c = i % kSide;
       const bool in = r0 + r < rows && c0 + c < cols;
@@ -333,7 +330,7 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
 
   if constexpr (ROWS) {
 #pragma unroll
-    for (unsigned u = 0; u < kSide * NB / THREADS; ++u) {
+    for (unsigned u = 0; u < (kSide * NB + THREADS - 1) / THREADS; ++u) {
       const unsigned i = u * THREADS + threadIdx.x, r = i % kSide, blk = i / kSide;
       uint4 raw[PIECES];
 #pragma unroll
@@ -352,6 +349,7 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
 #pragma unroll
     for (unsigned u = 0; u < (WORDS * NB + THREADS - 1) / THREADS; ++u) {
       const unsigned i = u * THREADS + threadIdx.x, w = i % WORDS, blk = i / WORDS;
+      if (WORDS * NB % THREADS != 0 && i >= WORDS * NB) continue;
       unsigned element[B];
 #pragma unroll
       for (unsigned q = 0; q < B; ++q) element[q] = *reinterpret_cast<const unsigned*>(tile + (blk * B + q) * PITCH + w * 4);
@@ -453,19 +451,32 @@ fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restri
 template <typename T>
 bool rows_aligned(const T* x, size_t ldx) { return aligned16(x) && ldx * sizeof(T) % 16 == 0; }
 
-template <int FORMAT, bool ROWS, bool COLS, typename T>
-ssgd_status launch_quantise(const T* x, size_t rows, size_t cols, size_t ldx, const float* amax, unsigned maxima, float* tensor_scale,
+template <int FORMAT, bool ROWS, bool COLS, unsigned THREADS, typename T>
+ssgd_status launch_tiles(const T* x, size_t rows, size_t cols, size_t ldx, const float* amax, unsigned maxima, float* tensor_scale,
                             uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, cudaStream_t s) {
   const size_t tiles_c = (cols + kSide - 1) / kSide, tiles = (rows + kSide - 1) / kSide * tiles_c;
   if (tiles > kMaxGrid) return SSGD_ERR_SIZE;
   const bool words = (reinterpret_cast<uintptr_t>(x) | ldx * sizeof(T)) % 4 == 0;
   const unsigned piece = rows_aligned(x, ldx) ? 16 : words ? 4 : 0;
-  auto kernel = fp4_quantise_kernel<FORMAT, ROWS, COLS, T>;
+  auto kernel = fp4_quantise_kernel<FORMAT, ROWS, COLS, THREADS, T>;
   static unsigned long long seen = 0;
   if (!allow_smem(reinterpret_cast<const void*>(kernel), kTileSmem<T>, &seen)) return SSGD_ERR_CUDA;
-  launch_kernel(kernel, dim3((unsigned)tiles), dim3(kTileThreads<T>), kTileSmem<T>, s, true, x, (unsigned)rows, (unsigned)cols, ldx, piece, amax,
+  launch_kernel(kernel, dim3((unsigned)tiles), dim3(THREADS), kTileSmem<T>, s, true, x, (unsigned)rows, (unsigned)cols, ldx, piece, amax,
                 maxima, tensor_scale, codes, scales, codes_t, scales_t, (unsigned)tiles_c);
   return launch_status();
+}
+
+// 512 threads for fp32, whose tiles leave room for two CTAs of an SM, and for few 16-bit tiles, where a CTA's own time counts;
+// else 256, of which four fit (B200, bf16 both ways: 2048 x 1024 mx 3.2 us with 512, 4.0 with 256; 1999 x 4103 nv 15.1 and 13.8;
+// 8192 x 8192 mx 83 and 41).
+template <int FORMAT, bool ROWS, bool COLS, typename T>
+ssgd_status launch_quantise(const T* x, size_t rows, size_t cols, size_t ldx, const float* amax, unsigned maxima, float* tensor_scale,
+                            uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, cudaStream_t s) {
+  DeviceInfo info;
+  if (!device_info(&info)) return SSGD_ERR_CUDA;
+  if (sizeof(T) == 4 || (rows + kSide - 1) / kSide * ((cols + kSide - 1) / kSide) <= (size_t)info.sms * 2)
+    return launch_tiles<FORMAT, ROWS, COLS, 512>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
+  return launch_tiles<FORMAT, ROWS, COLS, sizeof(T) == 4 ? 512 : 256>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
 }
 
 template <int FORMAT, typename T>
@@ -475,11 +486,13 @@ ssgd_status quantise_typed(const T* x, size_t rows, size_t cols, size_t ldx, con
   if (FORMAT == SSGD_NVFP4 && !amax && rows * cols > kFusedAmax) {
     DeviceInfo info;
     if (!device_info(&info)) return SSGD_ERR_CUDA;
-    const size_t wide = kThreads * 16 / sizeof(T), tiles_c = (cols + wide - 1) / wide, units = (rows + kAmaxRows - 1) / kAmaxRows * tiles_c;
+    const size_t wide = kThreads * 16 / sizeof(T), tiles_c = (cols + wide - 1) / wide;
+    const unsigned high = (rows + 7) / 8 * tiles_c < (size_t)info.sms * 2 ? 2 : 8;
+    const size_t units = (rows + high - 1) / high * tiles_c;
     const size_t most = (size_t)info.sms * 6 < SSGD_FP4_SCALE_FLOATS - 2 ? (size_t)info.sms * 6 : SSGD_FP4_SCALE_FLOATS - 2;
     maxima = (unsigned)(units < most ? units : most);
-    launch_kernel(fp4_amax_kernel<T>, dim3(maxima), dim3(kThreads), 0, s, true, x, (unsigned)rows, (unsigned)cols, ldx, rows_aligned(x, ldx),
-                  (unsigned)tiles_c, (unsigned long long)units, reinterpret_cast<unsigned*>(tensor_scale + 2));
+    launch_kernel(high == 2 ? fp4_amax_kernel<2, T> : fp4_amax_kernel<8, T>, dim3(maxima), dim3(kThreads), 0, s, true, x, (unsigned)rows, (unsigned)cols,
+                  ldx, rows_aligned(x, ldx), (unsigned)tiles_c, (unsigned long long)units, reinterpret_cast<unsigned*>(tensor_scale + 2));
   }
   if (codes && codes_t)
     return launch_quantise<FORMAT, true, true>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
