@@ -73,9 +73,13 @@ _status = {}
 
 
 def _status_of(device: torch.device) -> Tuple[torch.Tensor, int]:
+    """The word of a device in which a product reports a wait that ran out."""
     s = _status.get(device)
     if s is None:
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("the first 4-bit product on a device must come before any stream capture")
         t = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.synchronize(device)      # zero before a product on any stream may use it
         s = _status[device] = (t, t.data_ptr())
     return s
 

@@ -468,3 +468,102 @@ def test_linear_gradient_against_differences(fp4, fmt):
             out = fp4.linear_forward(moved if t is x else x, moved if t is w else w, fmt)[0]
             change = ((out - y).double() * dy.double()).sum().item()
             assert change == (moved[i2, j] - t[i2, j]).item() * grad[i2, j].item()
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# together
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_training_example(fmt):
+    """Products in 4 bits, clipping into the workers' rows and the vote, as the example runs them: the loss falls."""
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import train_fp4_signum as example
+    losses, norms, net, task = example.train(steps=150, workers=3, fmt=fmt)
+    assert all(math.isfinite(v) for v in losses + norms) and all(n > 0 for n in norms)
+    assert sum(losses[-10:]) < 0.5 * sum(losses[:10])
+    assert math.isfinite(example.serve(net, task))
+
+
+def test_clipped_rows_feed_the_step(B):
+    """bf16 tensors through tensors_clip and signsgd_step against the step on rows clipped in 64 bits."""
+    sizes, M = [100, 33, 4096, 7], 5
+    d = sum(-(-n // 32) * 32 for n in sizes)
+    src = [randn(n, seed=100 * w + n, dtype=BF16, scale=3.0 ** w) for w in range(M) for n in sizes]
+    rows = torch.zeros(M, d, device="cuda")
+    dst = [p[:n] for row in rows for p, n in zip(row.split([-(-n // 32) * 32 for n in sizes]), sizes)]
+    norms = torch.zeros(M, device="cuda")
+    B.tensors_clip(B.TensorTable(src, dst, [w for w in range(M) for _ in sizes]), 10.0, norms)
+    for w in range(M):
+        flat = torch.cat([t.double() for t in src[w * len(sizes):(w + 1) * len(sizes)]])
+        c = min(1.0, 10.0 / float(flat.norm()))
+        got = torch.cat([t for t in dst[w * len(sizes):(w + 1) * len(sizes)]])
+        assert torch.equal(got > 0, flat > 0) and float((got.double() - flat * c).abs().max()) <= 4 * 2.0 ** -24 * float((flat * c).abs().max())
+    words = -(-d // 128) * 4
+    x, m = torch.zeros(d, device="cuda"), torch.zeros(M, d, device="cuda")
+    bits, vote = torch.zeros(M, words, dtype=torch.int32, device="cuda"), torch.zeros(-(-d // 32), dtype=torch.int32, device="cuda")
+    B.signsgd_step(x, rows, m, M, d, d, 0.9, 1.0, bits, words, vote)
+    votes = torch.where(rows < 0, -1, 1).sum(0)
+    assert torch.equal(x, torch.where(votes >= 0, -1.0, 1.0))
+
+
+def test_product_in_a_graph(fp4):
+    x, w = randn(150, 700, seed=61, dtype=BF16), fp4.quantise(randn(300, 700, seed=62), "nv")
+    out = torch.zeros(150, 300, device="cuda")
+    fp4.matmul(fp4.quantise(x, "nv"), w, out=out)             # first call: attributes, the status word
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        fp4.matmul(fp4.quantise(x, "nv"), w, out=out)
+    for seed in (63, 64):
+        x.copy_(randn(150, 700, seed=seed, dtype=BF16))
+        g.replay()
+        torch.cuda.synchronize()
+        check_product(fp4.quantise(x, "nv"), w, out, F32)
+
+
+def test_linear_layers_share_nothing_over_streams(fp4):
+    """Products on two streams at the same time."""
+    a = [fp4.quantise(randn(m, 1000, seed=m), "mx") for m in (1, 40, 200, 600)]
+    w = fp4.quantise(randn(500, 1000, seed=9), "mx")
+    want = [fp4.matmul(p, w, F32) for p in a]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for k in range(40):
+        with torch.cuda.stream(streams[k % 2]):
+            got.append(fp4.matmul(a[k % 4], w, F32))
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[k], want[k % 4]) for k in range(40))
+    fp4.check()
+
+
+def test_refusals_of_the_torch_layer(fp4, B):
+    x = randn(4, 64)
+    with pytest.raises(ValueError):
+        fp4.quantise(x, "e4")
+    with pytest.raises(ValueError):
+        fp4.quantise(x[0], "mx")
+    with pytest.raises(ValueError):
+        fp4.quantise(x.cpu(), "mx")
+    with pytest.raises(TypeError):
+        fp4.quantise(x.double(), "mx")
+    a = fp4.quantise(x, "mx")
+    with pytest.raises(ValueError):
+        fp4.matmul(a, fp4.quantise(x, "nv"))
+    with pytest.raises(ValueError):
+        fp4.matmul(a, fp4.quantise(randn(4, 32), "mx"))
+    with pytest.raises(ValueError):
+        fp4.matmul(a, a, out=torch.empty(4, 5, device="cuda"))
+    with pytest.raises(ValueError):
+        fp4.Packed(a.codes[:2].contiguous(), a.scales, None, 4, 64, "mx")
+    with pytest.raises(ValueError):
+        B.TensorTable([x], [x[:2].contiguous()])
+    with pytest.raises(ValueError):
+        B.TensorTable([x[:, ::2]])
+    with pytest.raises(TypeError):
+        B.TensorTable([x.to(torch.int32)])
+    with pytest.raises(B.SignSGDError):
+        B.tensors_clip(B.TensorTable([x]), -1.0, torch.zeros(1, device="cuda"))
+    with pytest.raises(ValueError):
+        B.tensors_norm(B.TensorTable([x, x], None, [0, 1]), torch.zeros(1, device="cuda"))
