@@ -458,6 +458,14 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
                             size_t N, size_t K, int format, void* out, int dtype, size_t ldo, unsigned* status,
                             void* stream);
 
+/* The calls above with their arguments in one HOST block of 64-bit words, in the order of their parameters: pointers
+ * and sizes as they are, other integers widened, a float as the bits of a double.  For callers whose foreign-function
+ * interface costs by the argument (Python's ctypes: 0.6 us instead of 2 us a call).  NULL: SSGD_ERR_NULL.            */
+ssgd_status ssgd_tensors_clip_block(const uint64_t* args);    /* 9 words  */
+ssgd_status ssgd_fp4_quantise_block(const uint64_t* args);    /* 13 words */
+ssgd_status ssgd_fp4_dequantise_block(const uint64_t* args);  /* 10 words */
+ssgd_status ssgd_fp4_matmul_block(const uint64_t* args);      /* 15 words */
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,8 +9,10 @@ is raised.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -79,6 +81,10 @@ def lib() -> ctypes.CDLL:
         "ssgd_table_build": [vp, sz, sz, vp, sz],
         "ssgd_tensors_norm": [vp, sz, sz, ci, vp, vp, vp],
         "ssgd_tensors_clip": [vp, sz, sz, ci, f32, ci, vp, vp, vp],
+        "ssgd_tensors_clip_block": [ctypes.c_char_p],
+        "ssgd_fp4_quantise_block": [ctypes.c_char_p],
+        "ssgd_fp4_dequantise_block": [ctypes.c_char_p],
+        "ssgd_fp4_matmul_block": [ctypes.c_char_p],
         "ssgd_fp4_quantise": [vp, ci, sz, sz, sz, ci, vp, vp, vp, vp, vp, vp, vp],
         "ssgd_fp4_dequantise": [vp, vp, vp, ci, sz, sz, vp, ci, sz, vp],
         "ssgd_fp4_matmul": [vp, vp, vp, vp, vp, vp, sz, sz, sz, ci, vp, ci, sz, vp, vp],
@@ -380,9 +386,12 @@ def signsgd_step_noalloc(x: torch.Tensor, g: torch.Tensor, m: Optional[torch.Ten
 DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
-class _Tensor(ctypes.Structure):
+class _Tensor(ctypes.Structure):                 # ssgd_tensor
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_size_t), ("src_type", ctypes.c_uint),
                 ("dst_type", ctypes.c_uint), ("group", ctypes.c_uint), ("reserved", ctypes.c_uint)]
+
+
+assert ctypes.sizeof(_Tensor) == 40
 
 
 def _typed_ptr(t: torch.Tensor, name: str) -> int:
@@ -417,19 +426,27 @@ class TensorTable:
         if len(dst) != len(src) or len(groups) != len(src):
             raise ValueError("src, dst and groups must have one entry per tensor")
         self.workers = (max(groups) + 1 if groups else 1) if workers is None else int(workers)
-        entries = (_Tensor * max(1, len(src)))()
-        device = None
-        for e, s, t, w in zip(entries, src, dst, groups):
-            e.src, e.n, e.src_type, e.group = _typed_ptr(s, "src"), s.numel(), DTYPE_CODE[s.dtype], int(w)
-            device = s.device if device is None else device
-            if s.device != device or (t is not None and t.device != device):
-                raise ValueError("all tensors must live on one device")
-            if not s.is_contiguous() or (t is not None and not t.is_contiguous()):
+        codes = DTYPE_CODE
+        for t in src + [t for t in dst if t is not None]:
+            if not isinstance(t, torch.Tensor) or t.dtype not in codes:
+                raise TypeError("src and dst must be torch tensors of dtype float32, bfloat16 or float16")
+            if not t.is_contiguous():
                 raise ValueError("src and dst must be contiguous")
-            if t is not None:
-                e.dst, e.dst_type = _typed_ptr(t, "dst"), DTYPE_CODE[t.dtype]
-                if t.numel() != s.numel():
-                    raise ValueError("a dst holds %d elements, its src %d" % (t.numel(), s.numel()))
+        places = {t.get_device() for t in src} | {t.get_device() for t in dst if t is not None}
+        if len(places) > 1 or -1 in places:
+            raise ValueError("all tensors must live in the memory of one device")
+        device = src[0].device if src else None
+        words = []                            # five 64-bit words an entry: src, dst, n, the two types, group
+        for s, t, w in zip(src, dst, groups):
+            n = s.numel()
+            if t is None:
+                words += (s.data_ptr(), 0, n, codes[s.dtype], w)
+            elif t.numel() != n:
+                raise ValueError("a dst holds %d elements, its src %d" % (t.numel(), n))
+            else:
+                words += (s.data_ptr(), t.data_ptr(), n, codes[s.dtype] | codes[t.dtype] << 32, w)
+        block = array.array("Q", words or [0])
+        entries = block.buffer_info()[0]
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else device
         tiles, nbytes, ws = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
         _check(lib().ssgd_table_size(entries, len(src), self.workers, ctypes.byref(tiles), ctypes.byref(nbytes), ctypes.byref(ws)),
@@ -446,6 +463,8 @@ class TensorTable:
 
 
 NORM_KIND = {"two": 0, "max": 1}
+_CLIP_ARGS = struct.Struct("=4QdQ3Q")      # the blocks of arguments of the hot calls, see the header
+FP4_QUANTISE_ARGS, FP4_DEQUANTISE_ARGS, FP4_MATMUL_ARGS = struct.Struct("=13Q"), struct.Struct("=10Q"), struct.Struct("=15Q")
 
 
 def tensors_norm(table: TensorTable, norms: torch.Tensor, kind: str = "two", stream=None) -> None:
@@ -462,8 +481,9 @@ def tensors_clip(table: TensorTable, max_norm: float, norms: torch.Tensor, kind:
     """norms as `tensors_norm`; every dst <- src * (max_norm / norm where norm > max_norm, else 1).  With zero_nonfinite a
     worker whose norm is not finite gets zeros."""
     _need(norms, table.workers, "norms")
-    status = lib().ssgd_tensors_clip(*table._args, NORM_KIND[kind], max_norm, 1 if zero_nonfinite else 0, table._ws,
-                                     _ptr(norms, torch.float32, "norms"), _stream_of(table._index) if stream is None else _stream(stream))
+    status = lib().ssgd_tensors_clip_block(_CLIP_ARGS.pack(
+        *table._args, NORM_KIND[kind], max_norm, 1 if zero_nonfinite else 0, table._ws, _ptr(norms, torch.float32, "norms"),
+        _stream_of(table._index) if stream is None else _stream(stream)))
     if status:
         _check(status, "ssgd_tensors_clip")
 

@@ -703,4 +703,11 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
   return format == SSGD_MXFP4 ? any_product<SSGD_MXFP4>(o, info.sms, s) : any_product<SSGD_NVFP4>(o, info.sms, s);
 }
 
+ssgd_status ssgd_fp4_matmul_block(const uint64_t* a) {
+  if (!a) return SSGD_ERR_NULL;
+  return ssgd_fp4_matmul(block_ptr<const uint8_t>(a[0]), block_ptr<const uint8_t>(a[1]), block_ptr<const float>(a[2]), block_ptr<const uint8_t>(a[3]),
+                         block_ptr<const uint8_t>(a[4]), block_ptr<const float>(a[5]), a[6], a[7], a[8], (int)a[9], block_ptr<void>(a[10]), (int)a[11],
+                         a[12], block_ptr<unsigned>(a[13]), block_ptr<void>(a[14]));
+}
+
 }  // extern "C"

@@ -574,4 +574,16 @@ ssgd_status ssgd_fp4_dequantise(const uint8_t* codes, const uint8_t* scales, con
   }
 }
 
+ssgd_status ssgd_fp4_quantise_block(const uint64_t* a) {
+  if (!a) return SSGD_ERR_NULL;
+  return ssgd_fp4_quantise(block_ptr<const void>(a[0]), (int)a[1], a[2], a[3], a[4], (int)a[5], block_ptr<const float>(a[6]), block_ptr<float>(a[7]),
+                           block_ptr<uint8_t>(a[8]), block_ptr<uint8_t>(a[9]), block_ptr<uint8_t>(a[10]), block_ptr<uint8_t>(a[11]), block_ptr<void>(a[12]));
+}
+
+ssgd_status ssgd_fp4_dequantise_block(const uint64_t* a) {
+  if (!a) return SSGD_ERR_NULL;
+  return ssgd_fp4_dequantise(block_ptr<const uint8_t>(a[0]), block_ptr<const uint8_t>(a[1]), block_ptr<const float>(a[2]), (int)a[3], a[4], a[5],
+                             block_ptr<void>(a[6]), (int)a[7], a[8], block_ptr<void>(a[9]));
+}
+
 }  // extern "C"

@@ -44,6 +44,10 @@ struct StepArgs {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// A pointer out of a block of arguments.
+template <typename T>
+inline T* block_ptr(uint64_t word) { return reinterpret_cast<T*>(static_cast<uintptr_t>(word)); }
+
 inline bool mul_overflows(size_t a, size_t b) { return b != 0 && a > SIZE_MAX / b; }
 
 ssgd_status check_rows(size_t M, size_t d, size_t ld, size_t ldw, bool need_ld) {

@@ -378,4 +378,12 @@ ssgd_status ssgd_tensors_clip(const void* table, size_t tiles, size_t groups, in
                                : launch_clip<kNormMax>(table, tiles, groups, true, max_norm, zero_nonfinite, ws, norms, s);
 }
 
+ssgd_status ssgd_tensors_clip_block(const uint64_t* a) {
+  if (!a) return SSGD_ERR_NULL;
+  double max_norm;
+  memcpy(&max_norm, a + 4, sizeof max_norm);
+  return ssgd_tensors_clip(block_ptr<const void>(a[0]), a[1], a[2], (int)a[3], (float)max_norm, (int)a[5], block_ptr<void>(a[6]),
+                           block_ptr<float>(a[7]), block_ptr<void>(a[8]));
+}
+
 }  // extern "C"

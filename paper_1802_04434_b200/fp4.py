@@ -13,6 +13,7 @@ import torch
 from . import binding as B
 
 _BLOCK = {"mx": 32, "nv": 16}
+_U8 = torch.uint8
 
 
 def _sizes(rows: int, cols: int, fmt: str) -> Tuple[int, int]:
@@ -33,12 +34,18 @@ class Packed:
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Optional[torch.Tensor], rows: int, cols: int, fmt: str):
         if fmt not in _BLOCK:
             raise ValueError("fmt must be 'mx' or 'nv'")
-        need = _sizes(rows, cols, fmt)
-        ts = None if tensor_scale is None else B._ptr(tensor_scale, torch.float32, "tensor_scale")
-        self.pointers = (B._ptr(codes, torch.uint8, "codes"), B._ptr(scales, torch.uint8, "scales"), ts)
-        if codes.numel() < need[0] or scales.numel() < need[1]:
-            raise ValueError("codes hold %d bytes, scales %d; %d x %d %s needs %d and %d" % (codes.numel(), scales.numel(), rows, cols, fmt, *need))
-        self.rows, self.cols, self.fmt, self.device = rows, cols, fmt, codes.device
+        if codes.dtype != _U8 or scales.dtype != _U8 or (tensor_scale is not None and tensor_scale.dtype != torch.float32):
+            raise TypeError("codes and scales must be uint8 tensors, tensor_scale a float32 one")
+        device = codes.device
+        if not codes.is_cuda or scales.device != device or (tensor_scale is not None and tensor_scale.device != device):
+            raise ValueError("codes, scales and tensor_scale must live in the memory of one device")
+        if not (codes.is_contiguous() and scales.is_contiguous()):
+            raise ValueError("codes and scales must be contiguous")
+        n, m = _sizes(rows, cols, fmt)
+        if codes.numel() < n or scales.numel() < m:
+            raise ValueError("codes hold %d bytes, scales %d; %d x %d %s needs %d and %d" % (codes.numel(), scales.numel(), rows, cols, fmt, n, m))
+        self.pointers = (codes.data_ptr(), scales.data_ptr(), 0 if tensor_scale is None else tensor_scale.data_ptr())
+        self.rows, self.cols, self.fmt, self.device = rows, cols, fmt, device
         self._parts, self._buffer = (codes, scales, tensor_scale), None
 
     @classmethod
@@ -47,7 +54,7 @@ class Packed:
         """Parts at the given byte offsets of one buffer whose address is `base`."""
         p = cls.__new__(cls)
         p.rows, p.cols, p.fmt, p.device = rows, cols, fmt, device
-        p.pointers = (base + at[0], base + at[1], None if at[2] is None else base + at[2])
+        p.pointers = (base + at[0], base + at[1], 0 if at[2] is None else base + at[2])
         p._parts, p._buffer = None, (buffer, at)
         return p
 
@@ -122,13 +129,13 @@ def _quantise(x, fmt, amax, by_rows, by_columns):
     ts = n + m + nt + mt                      # all parts are multiples of 16 bytes
     device = x.device
     tail = 0 if not nv else 4 * B.FP4_SCALE_FLOATS if amax is None and rows * cols > B.FP4_SMALL else 8
-    buffer = torch.empty(ts + tail, dtype=torch.uint8, device=device)
+    buffer = torch.empty(ts + tail, dtype=_U8, device=device)
     base = buffer.data_ptr()
     if rows and cols:
-        status = B.lib().ssgd_fp4_quantise(
+        status = B.lib().ssgd_fp4_quantise_block(B.FP4_QUANTISE_ARGS.pack(
             x.data_ptr(), dtype, rows, cols, ldx if ldx > cols else cols, 1 if nv else 0,
-            None if amax is None else B._ptr(amax, torch.float32, "amax"), base + ts if nv else None, base if by_rows else None, base + n,
-            base + n + m if by_columns else None, base + n + m + nt, B._stream_of(index))
+            0 if amax is None else B._ptr(amax, torch.float32, "amax"), base + ts if nv else 0, base if by_rows else 0, base + n,
+            base + n + m if by_columns else 0, base + n + m + nt, B._stream_of(index)))
         if status:
             B._check(status, "ssgd_fp4_quantise")
     elif nv:
@@ -159,8 +166,8 @@ def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     out = torch.empty(p.rows, p.cols, dtype=dtype, device=p.device)
     if p.rows and p.cols:
         codes, scales, ts = p.pointers
-        status = B.lib().ssgd_fp4_dequantise(codes, scales, ts, B.FP4_FORMAT[p.fmt], p.rows, p.cols, out.data_ptr(), B.DTYPE_CODE[dtype],
-                                             p.cols, B._stream_of(p.device.index))
+        status = B.lib().ssgd_fp4_dequantise_block(B.FP4_DEQUANTISE_ARGS.pack(
+            codes, scales, ts, B.FP4_FORMAT[p.fmt], p.rows, p.cols, out.data_ptr(), B.DTYPE_CODE[dtype], p.cols, B._stream_of(p.device.index)))
         if status:
             B._check(status, "ssgd_fp4_dequantise")
     return out
@@ -181,8 +188,9 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optio
     if a.cols == 0:
         return out.zero_()
     if rows and cols:
-        status = B.lib().ssgd_fp4_matmul(*a.pointers, *b.pointers, rows, cols, a.cols, B.FP4_FORMAT[a.fmt], out.data_ptr(),
-                                         B.DTYPE_CODE[out.dtype], ldo, _status_of(a.device)[1], B._stream_of(a.device.index))
+        status = B.lib().ssgd_fp4_matmul_block(B.FP4_MATMUL_ARGS.pack(
+            *a.pointers, *b.pointers, rows, cols, a.cols, B.FP4_FORMAT[a.fmt], out.data_ptr(), B.DTYPE_CODE[out.dtype], ldo,
+            _status_of(a.device)[1], B._stream_of(a.device.index)))
         if status:
             B._check(status, "ssgd_fp4_matmul")
     return out

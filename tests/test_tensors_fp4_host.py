@@ -141,3 +141,22 @@ def test_reference_formats():
     assert ref.pack_codes(np.array([[1, 2, 3]], dtype=np.uint8))[0, :3].tolist() == [0x21, 3, 0]
     s = ref.pack_scales(np.arange(129 * 5, dtype=np.int64).reshape(129, 5).astype(np.uint8))
     assert s.size == 2 * 2 * 512 and s[33 % 32 * 16 + 4 + 2] == (33 * 5 + 2) % 256 and s[2 * 512] == (128 * 5) % 256
+
+
+def test_block_calls(B):
+    """The calls with their arguments in one block refuse what the others refuse."""
+    import struct
+    L = B.lib()
+    for f in (L.ssgd_tensors_clip_block, L.ssgd_fp4_quantise_block, L.ssgd_fp4_dequantise_block, L.ssgd_fp4_matmul_block):
+        assert f(None) == NULL
+    clip = lambda *a: L.ssgd_tensors_clip_block(B._CLIP_ARGS.pack(*a))  # noqa: E731
+    assert clip(A, 1, 1, 0, -1.0, 0, A, A, 0) == ARG and clip(0, 1, 1, 0, 1.0, 0, A, A, 0) == NULL and clip(A, 1, 1025, 0, 1.0, 0, A, A, 0) == SIZE
+    assert clip(A, 1, 1, 0, float("nan"), 0, A, A, 0) == ARG and clip(A, 1, 1, 0, 1.0, 0, A, A + 2, 0) == ALIGN
+    q = lambda *a: L.ssgd_fp4_quantise_block(B.FP4_QUANTISE_ARGS.pack(*a))  # noqa: E731
+    assert q(A, 0, 3, 40, 39, 1, 0, A, A, A, A, A, 0) == SIZE and q(A, 0, 0, 40, 40, 1, 0, A, A, A, A, A, 0) == OK
+    assert q(A, 0, 3, 40, 40, 2, 0, A, A, A, A, A, 0) == ARG and q(A, 0, 3, 40, 40, 1, 0, A, A + 8, A, A, A, 0) == ALIGN
+    d = lambda *a: L.ssgd_fp4_dequantise_block(B.FP4_DEQUANTISE_ARGS.pack(*a))  # noqa: E731
+    assert d(A, A, 0, 0, 2, 32, A, 0, 31, 0) == SIZE and d(A, A, 0, 0, 0, 32, A, 0, 32, 0) == OK and d(0, A, 0, 0, 2, 32, A, 0, 32, 0) == NULL
+    m = lambda *a: L.ssgd_fp4_matmul_block(B.FP4_MATMUL_ARGS.pack(*a))  # noqa: E731
+    assert m(A, A, 0, A, A, 0, 4, 8, 64, 0, A, 1, 7, A, 0) == SIZE and m(A, A, 0, A, A, 0, 0, 8, 64, 0, A, 1, 8, A, 0) == OK
+    assert m(A, A, 0, A, A, 0, 4, 8, 64, 0, A, 1, 8, 0, 0) == NULL and struct.calcsize(B.FP4_MATMUL_ARGS.format) == 15 * 8
