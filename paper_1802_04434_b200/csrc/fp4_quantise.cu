@@ -35,6 +35,11 @@ template <typename T> __device__ __forceinline__ unsigned top_of_word(unsigned w
   return sizeof(T) == 4 ? lo : max(lo, magnitude_bits(high_to_float(T(), w)));
 }
 
+// One element as a word of elements.
+__device__ __forceinline__ unsigned word_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ unsigned word_of(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
+__device__ __forceinline__ unsigned word_of(__half v) { return __half_as_ushort(v); }
+
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
   uint64_t r;
@@ -73,49 +78,45 @@ __device__ __forceinline__ unsigned piece_amax(const T* __restrict__ at, unsigne
 }
 
 // Largest magnitude of what each CTA sees, as bits, to a place of its own: no memory has to start at zero, and every CTA
-// of the quantisation that follows takes the largest of them.  A CTA takes rectangles of ROWS rows by 256 pieces of
-// 16 bytes, all pieces of a thread in flight: eight rows, or two where eight would leave SMs without work; rows that are not 16-byte aligned are read element by element, lanes side
-// by side.
+// of the quantisation that follows takes the largest of them.  A CTA takes rectangles: `wide` threads (a power of two) lie
+// along a row, a piece of 16 bytes each, the others in rows below, every thread ROWS rows, all in flight.  Rows that are not
+// 16-byte aligned are read element by element, lanes side by side.
+constexpr unsigned kAmaxThreads = 512, kAmaxCtas = 2;     // CTAs of an SM
 template <unsigned ROWS, typename T>
-__global__ void __launch_bounds__(kThreads)
-fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, unsigned tiles_c, unsigned long long units,
+__global__ void __launch_bounds__(kAmaxThreads)
+fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, unsigned wide, unsigned strips, unsigned long long units,
                 unsigned* __restrict__ out) {
-  constexpr unsigned V = 16 / sizeof(T), WIDE = kThreads * V;
+  constexpr unsigned V = 16 / sizeof(T);
   pdl_launch_dependents();
   pdl_wait();
-  unsigned top = 0;
+  const unsigned lane = threadIdx.x & (wide - 1), below = threadIdx.x / wide, high = kAmaxThreads / wide;
+  unsigned w = 0;
   for (unsigned long long i = blockIdx.x; i < units; i += gridDim.x) {
-    const unsigned r0 = (unsigned)(i / tiles_c) * ROWS, c0 = (unsigned)(i % tiles_c) * WIDE;
-    const unsigned c = c0 + threadIdx.x * V;
-    if (vec && r0 + ROWS <= rows && c + V <= cols) {
+    const unsigned r0 = (unsigned)(i / strips) * (high * ROWS) + below, c0 = (unsigned)(i % strips) * (wide * V);
+    const unsigned c = c0 + lane * V;
+    if (vec && r0 + (ROWS - 1) * high < rows && c + V <= cols) {
       uint4 q[ROWS];
 #pragma unroll
-      for (unsigned r = 0; r < ROWS; ++r) q[r] = *reinterpret_cast<const uint4*>(x + (size_t)(r0 + r) * ldx + c);
-      unsigned w = 0;
+      for (unsigned r = 0; r < ROWS; ++r) q[r] = *reinterpret_cast<const uint4*>(x + (size_t)(r0 + r * high) * ldx + c);
 #pragma unroll
       for (unsigned r = 0; r < ROWS; ++r) w = larger(T(), larger(T(), w, larger(T(), q[r].x, q[r].y)), larger(T(), q[r].z, q[r].w));
-      top = max(top, top_of_word<T>(w));
-    } else if (vec) {
-      for (unsigned r = 0; r < ROWS; ++r)
-        if (r0 + r < rows && c < cols) top = max(top, piece_amax(x + (size_t)(r0 + r) * ldx + c, cols - c, true));
     } else {
 #pragma unroll (ROWS < 4 ? ROWS : 4)
       for (unsigned r = 0; r < ROWS; ++r)
 #pragma unroll
         for (unsigned q = 0; q < V; ++q) {
-          const unsigned c = c0 + q * kThreads + threadIdx.x;
-          if (r0 + r < rows && c < cols) top = max(top, magnitude_bits(to_float(x[(size_t)(r0 + r) * ldx + c])));
+          const unsigned e = c0 + q * wide + lane;
+          if (r0 + r * high < rows && e < cols) w = larger(T(), w, word_of(x[(size_t)(r0 + r * high) * ldx + e]));
         }
     }
   }
-  top = __reduce_max_sync(0xFFFFFFFFu, top);
-  __shared__ unsigned part[kThreads / 32];
+  const unsigned top = __reduce_max_sync(0xFFFFFFFFu, top_of_word<T>(w));
+  __shared__ unsigned part[kAmaxThreads / 32];
   if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = top;
   __syncthreads();
-  if (threadIdx.x == 0) {
-#pragma unroll
-    for (int w = 1; w < kThreads / 32; ++w) top = max(top, part[w]);
-    out[blockIdx.x] = top;
+  if (threadIdx.x < 32) {
+    const unsigned all = __reduce_max_sync(0xFFFFFFFFu, threadIdx.x < kAmaxThreads / 32 ? part[threadIdx.x] : 0u);
+    if (threadIdx.x == 0) out[blockIdx.x] = all;
   }
 }
 
@@ -151,7 +152,8 @@ __device__ __forceinline__ unsigned fp4_pack8(const uint64_t (&v)[4]) {
 // How a block is divided by its scale S: mx multiplies by 1 / S, a power of two.  nv multiplies by a reciprocal in two parts,
 // high <= 1 / S and low >= 0, as fma(x, high, x * low): off by 2^-43 before the one rounding, so the quotient is the correctly
 // rounded one except within that of halfway, and a tie between two codes stays a tie (a single fp32 reciprocal would send 1 %
-// of a bf16 tensor's values to the wrong side).  Two multiplications instead of a division's ten instructions.
+// of a bf16 tensor's values to the wrong side).  Two multiplications instead of a division's ten instructions.  A quotient
+// beyond fp32 (a tensor scale far too small) becomes an infinity of x's sign, and that saturates.
 struct BlockScale {
   unsigned byte;
   float high, low;
@@ -177,7 +179,7 @@ __device__ __forceinline__ BlockScale block_scale(unsigned top_bits, float tenso
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half2) : "h"((unsigned short)byte));
     const float scale = __low2float(*reinterpret_cast<const __half2*>(&half2));
     float r;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(scale));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(scale));
     r = __fmul_rn(r, 1.0f - 0x1p-22f);                                  // below 1 / scale for certain
     b.high = r * tensor_inverse;
     b.low = __fmul_rn(__fmaf_rn(-scale, r, 1.0f), b.high);
@@ -190,14 +192,6 @@ __device__ __forceinline__ BlockScale block_scale(unsigned top_bits, float tenso
 template <int FORMAT, int B>
 __device__ __forceinline__ unsigned quantise_block(uint64_t (&v)[B / 2], unsigned top_bits, float tensor_inverse, unsigned (&word)[B / 8]) {
   const BlockScale b = block_scale<FORMAT>(top_bits, tensor_inverse);
-  if (FORMAT == SSGD_NVFP4 && __uint_as_float(top_bits) * tensor_inverse > 1e30f) {   // a tensor scale far too small: saturate
-    const float limit = 1e30f / tensor_inverse;
-#pragma unroll
-    for (int i = 0; i < B / 2; ++i) {
-      const float lo = __uint_as_float((unsigned)v[i]), hi = __uint_as_float((unsigned)(v[i] >> 32));
-      v[i] = pair_of(fmaxf(-limit, fminf(limit, lo)), fmaxf(-limit, fminf(limit, hi)));
-    }
-  }
   const uint64_t high = pair_of(b.high, b.high), low = pair_of(b.low, b.low);
 #pragma unroll
   for (int i = 0; i < B / 2; ++i) v[i] = FORMAT == SSGD_MXFP4 ? mul_pair(v[i], high) : fma_pair(v[i], high, mul_pair(v[i], low));
@@ -231,7 +225,7 @@ __device__ __forceinline__ unsigned quantise_words(const unsigned* w, float tens
 //   columns  lanes run along the columns (two 16-bit columns in a word), a thread takes a block of a column, or of two
 // Either way the codes go back through shared memory, so that 64 contiguous bytes of a row of codes leave together.
 constexpr unsigned kSide = 128;
-constexpr unsigned kCodePitch = 80;                       // of the 64 bytes of codes of a row in shared memory
+constexpr unsigned kCodePitch = 72;                       // of the 64 bytes of codes of a row in shared memory
 template <typename T> constexpr unsigned kTilePitch = kSide * sizeof(T) + 16;
 template <typename T> constexpr unsigned kTileSmem = kSide * kTilePitch<T> + kSide * kCodePitch;
 constexpr size_t kFusedAmax = SSGD_FP4_SMALL;             // elements up to which every CTA finds the tensor's maximum itself
@@ -261,8 +255,10 @@ __device__ __forceinline__ void write_out(const unsigned char* staged, const uin
 #pragma unroll
   for (unsigned i = threadIdx.x; i < kSide * 4; i += THREADS) {
     const unsigned r = i / 4, at = i % 4 * 16;
-    if (r0 + r < rows && c0 / 2 + at < row_bytes)
-      *reinterpret_cast<uint4*>(codes + (size_t)(r0 + r) * row_bytes + c0 / 2 + at) = *reinterpret_cast<const uint4*>(staged + r * kCodePitch + at);
+    if (r0 + r < rows && c0 / 2 + at < row_bytes) {
+      const uint2 lo = *reinterpret_cast<const uint2*>(staged + r * kCodePitch + at), hi = *reinterpret_cast<const uint2*>(staged + r * kCodePitch + at + 8);
+      *reinterpret_cast<uint4*>(codes + (size_t)(r0 + r) * row_bytes + c0 / 2 + at) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
   }
   if (threadIdx.x < NB / 4 * 32 && first + threadIdx.x / 32 < tiles_k)
     reinterpret_cast<uint4*>(scales + (r0 / kSide * tiles_k + first) * 512)[threadIdx.x] = reinterpret_cast<const uint4*>(staged_scales)[threadIdx.x];
@@ -270,8 +266,8 @@ __device__ __forceinline__ void write_out(const unsigned char* staged, const uin
 
 template <int B>
 __device__ __forceinline__ void stage_codes(unsigned char* to, const unsigned (&word)[B / 8]) {
-  if constexpr (B == 16) *reinterpret_cast<uint2*>(to) = make_uint2(word[0], word[1]);
-  else *reinterpret_cast<uint4*>(to) = make_uint4(word[0], word[1], word[2], word[3]);
+#pragma unroll
+  for (int i = 0; i < B / 16; ++i) *reinterpret_cast<uint2*>(to + 8 * i) = make_uint2(word[2 * i], word[2 * i + 1]);
 }
 
 // piece: bytes that a copy of x's elements may have (16, 4, or 0: none, its rows start at odd 16-bit elements)
@@ -308,19 +304,20 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
     float top;
     if (amax) {
       top = __ldg(amax);
-    } else {                                              // from the maxima of the pass before, or from the matrix itself
+    } else if (maxima > 0) {                              // the largest of the pass before, by every warp for itself
       unsigned t = 0;
-      for (unsigned i = threadIdx.x; i < maxima; i += THREADS) t = max(t, __float_as_uint(__ldcg(tensor_scale + 2 + i)));
-      if (maxima == 0) t = small_amax<THREADS>(x, rows, cols, ldx, piece == 16);
-      t = __reduce_max_sync(0xFFFFFFFFu, t);
+      for (unsigned i = threadIdx.x & 31u; i < maxima; i += 32) t = max(t, __float_as_uint(tensor_scale[2 + i]));
+      top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, t));
+    } else {
+      const unsigned t = __reduce_max_sync(0xFFFFFFFFu, small_amax<THREADS>(x, rows, cols, ldx, piece == 16));
       if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = t;
       __syncthreads();
       unsigned all = 0;
 #pragma unroll
       for (unsigned w = 0; w < THREADS / 32; ++w) all = max(all, part[w]);
       top = __uint_as_float(all);
-      if (blockIdx.x == 0 && threadIdx.x == 0) tensor_scale[1] = top;
     }
+    if (!amax && blockIdx.x == 0 && threadIdx.x == 0) tensor_scale[1] = top;
     ts = fp4_tensor_scale(top);
     if (blockIdx.x == 0 && threadIdx.x == 0) tensor_scale[0] = ts;
   }
@@ -375,76 +372,78 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
   }
 }
 
-// A thread takes groups of G values, kRows rows of its place; `wide` threads of a CTA lie along a row, the others in
-// rows below, so that no index needs a division.
-//   ALIGNED    rows of out start at multiples of 16 bytes: a group is 16 bytes, lies in one block, and its codes in one word
-//   otherwise  a row's groups of eight start up to V - 1 columns before it, where its stores are aligned; their codes are cut out of
-//              two words and may lie in two blocks
+// Rows of out that start at multiples of 16 bytes.  A thread takes groups of 16 bytes (their codes lie in one word, the
+// values in one block), kRows rows of its place; `wide` threads of a CTA lie along a row, the others in rows below, so that
+// no index needs a division.
 constexpr unsigned kRows = 4;
 
-template <int FORMAT, bool ALIGNED, typename T>
+template <int FORMAT, typename T>
 __global__ void __launch_bounds__(kThreads)
 fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ tensor_scale,
                       unsigned rows, unsigned cols, T* __restrict__ out, size_t ldo, unsigned groups, unsigned wide, unsigned strips) {
-  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, V = 16 / sizeof(T), G = ALIGNED ? V : 8;
+  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, G = 16 / sizeof(T);
   pdl_launch_dependents();
   pdl_wait();
   const float ts = FORMAT == SSGD_NVFP4 && tensor_scale ? __ldg(tensor_scale) : 1.0f;
   const unsigned strip = blockIdx.x % strips, high = kThreads / wide;                 // strips of wide groups; rows at a time
   const unsigned g = strip * wide + (threadIdx.x & (wide - 1)), row0 = blockIdx.x / strips * (high * kRows) + threadIdx.x / wide;
   if (g >= groups) return;
-  const unsigned row_words = (cols + 31) / 32 * 4, tiles_k = ((cols + B - 1) / B + 3) / 4;
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(codes);
-  unsigned lo[kRows], hi[kRows], byte0[kRows], byte1[kRows];
-  int column[kRows];
+  const unsigned c = g * G, row_words = (cols + 31) / 32 * 4, tiles_k = ((cols + B - 1) / B + 3) / 4;
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(codes) + c / 8;
+  unsigned word[kRows], byte[kRows];
 #pragma unroll
   for (unsigned u = 0; u < kRows; ++u) {
     const unsigned row = row0 + u * high;
-    lo[u] = hi[u] = byte0[u] = byte1[u] = 0;
-    column[u] = (int)(g * G);
-    if (!ALIGNED) column[u] -= (int)((unsigned)(reinterpret_cast<uintptr_t>(out + (size_t)row * ldo) / sizeof(T)) & (V - 1));
-    if (row >= rows || column[u] >= (int)cols) {
-      column[u] = (int)cols;
-      continue;
-    }
-    const int c = column[u], w = c >> 3;                                              // rounds down
-    const uint32_t* at = words + (size_t)row * row_words;
-    if (ALIGNED || w >= 0) lo[u] = at[w];
-    const unsigned b0 = (unsigned)max(c, 0) / B;
-    byte0[u] = scales[fp4_scale_index(row, b0, tiles_k)];
-    if (!ALIGNED) {
-      if (((unsigned)c & 7u) + G > 8 && (unsigned)(w + 1) < row_words) hi[u] = at[w + 1];
-      const unsigned b1 = min((unsigned)(c + (int)G - 1), cols - 1) / B;
-      byte1[u] = b1 == b0 ? byte0[u] : scales[fp4_scale_index(row, b1, tiles_k)];
-    }
+    word[u] = row < rows ? words[(size_t)row * row_words] : 0u;
+    byte[u] = row < rows ? scales[fp4_scale_index(row, c / B, tiles_k)] : 0u;
   }
 #pragma unroll
   for (unsigned u = 0; u < kRows; ++u) {
-    const int c = column[u];
-    if (c >= (int)cols) continue;
-    const unsigned four = ((unsigned)c & 7u) * 4, bits = ALIGNED ? lo[u] >> four : __funnelshift_r(lo[u], hi[u], four);
-    const float s0 = __fmul_rn(fp4_scale_value<FORMAT>(byte0[u]), ts), s1 = ALIGNED ? s0 : __fmul_rn(fp4_scale_value<FORMAT>(byte1[u]), ts);
-    const int change = ALIGNED ? (int)G : (max(c, 0) / (int)B + 1) * (int)B - c;           // the group's place from which the second scale holds
+    if (row0 + u * high >= rows) break;
+    const unsigned bits = word[u] >> (c % 8 * 4);
+    const float scale = __fmul_rn(fp4_scale_value<FORMAT>(byte[u]), ts);
     float v[G];
 #pragma unroll
-    for (int j = 0; j < (int)G; j += 2) {
+    for (unsigned j = 0; j < G; j += 2) {
       const float2 two = fp4_pair_value(bits >> (4 * j));
-      v[j] = __fmul_rn(two.x, j < change ? s0 : s1);
-      v[j + 1] = __fmul_rn(two.y, j + 1 < change ? s0 : s1);
+      v[j] = __fmul_rn(two.x, scale);
+      v[j + 1] = __fmul_rn(two.y, scale);
     }
     T* o = out + (size_t)(row0 + u * high) * ldo + c;
-    if (c >= 0 && c + (int)G <= (int)cols) {
-      if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int j = 0; j < (int)G; j += 4) store4(o + j, make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]));
-      } else {
-        __stcs(reinterpret_cast<uint4*>(o), make_uint4(pack2(T(), v[0], v[1]), pack2(T(), v[2], v[3]), pack2(T(), v[4], v[5]), pack2(T(), v[6], v[7])));
-      }
+    if (c + G <= cols) {
+      if constexpr (sizeof(T) == 4) store4(o, make_float4(v[0], v[1], v[2], v[3]));
+      else __stcs(reinterpret_cast<uint4*>(o), make_uint4(pack2(T(), v[0], v[1]), pack2(T(), v[2], v[3]), pack2(T(), v[4], v[5]), pack2(T(), v[6], v[7])));
     } else {
 #pragma unroll
-      for (int j = 0; j < (int)G; ++j)
-        if (c + j >= 0 && c + j < (int)cols) o[j] = from_float<T>(v[j]);
+      for (unsigned j = 0; j < G; ++j)
+        if (c + j < cols) o[j] = from_float<T>(v[j]);
     }
+  }
+}
+
+// Rows of out that start anywhere.  A warp takes 256 columns of a row: a word of codes to a lane, the block scales to the first
+// lanes, then 32 neighbouring values at a time, one to a lane, codes and scale from the lanes that hold them.
+template <int FORMAT, typename T>
+__global__ void __launch_bounds__(kThreads)
+fp4_dequantise_rows_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ tensor_scale,
+                           unsigned rows, unsigned cols, T* __restrict__ out, size_t ldo, unsigned strips) {
+  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, NB = 256 / B;
+  pdl_launch_dependents();
+  pdl_wait();
+  const float ts = FORMAT == SSGD_NVFP4 && tensor_scale ? __ldg(tensor_scale) : 1.0f;
+  const unsigned lane = threadIdx.x & 31u, row = blockIdx.x / strips * (kThreads / 32) + (threadIdx.x >> 5), c0 = blockIdx.x % strips * 256;
+  if (row >= rows) return;
+  const unsigned row_words = (cols + 31) / 32 * 4, blocks = (cols + B - 1) / B, tiles_k = (blocks + 3) / 4;
+  const unsigned at = c0 / 8 + lane, block = c0 / B + lane;
+  const unsigned word = at < row_words ? reinterpret_cast<const uint32_t*>(codes)[(size_t)row * row_words + at] : 0u;
+  const unsigned byte = lane < NB && block < blocks ? scales[fp4_scale_index(row, block, tiles_k)] : 0u;
+  const float scale = __fmul_rn(fp4_scale_value<FORMAT>(byte), ts);
+  T* o = out + (size_t)row * ldo + c0 + lane;
+#pragma unroll
+  for (unsigned i = 0; i < 8; ++i) {
+    const unsigned code = __shfl_sync(0xFFFFFFFFu, word, 4 * i + lane / 8) >> (lane % 8 * 4);
+    const float s = __shfl_sync(0xFFFFFFFFu, scale, (32 * i + lane) / B);
+    if (c0 + 32 * i + lane < cols) o[32 * i] = from_float<T>(__fmul_rn(fp4_pair_value(code & 15u).x, s));
   }
 }
 
@@ -486,13 +485,16 @@ ssgd_status quantise_typed(const T* x, size_t rows, size_t cols, size_t ldx, con
   if (FORMAT == SSGD_NVFP4 && !amax && rows * cols > kFusedAmax) {
     DeviceInfo info;
     if (!device_info(&info)) return SSGD_ERR_CUDA;
-    const size_t wide = kThreads * 16 / sizeof(T), tiles_c = (cols + wide - 1) / wide;
-    const unsigned high = (rows + 7) / 8 * tiles_c < (size_t)info.sms * 2 ? 2 : 8;
-    const size_t units = (rows + high - 1) / high * tiles_c;
-    const size_t most = (size_t)info.sms * 6 < SSGD_FP4_SCALE_FLOATS - 2 ? (size_t)info.sms * 6 : SSGD_FP4_SCALE_FLOATS - 2;
-    maxima = (unsigned)(units < most ? units : most);
-    launch_kernel(high == 2 ? fp4_amax_kernel<2, T> : fp4_amax_kernel<8, T>, dim3(maxima), dim3(kThreads), 0, s, true, x, (unsigned)rows, (unsigned)cols,
-                  ldx, rows_aligned(x, ldx), (unsigned)tiles_c, (unsigned long long)units, reinterpret_cast<unsigned*>(tensor_scale + 2));
+    const size_t V = 16 / sizeof(T);
+    unsigned wide = 32;
+    while (wide < kAmaxThreads && wide * V < cols) wide *= 2;
+    const size_t strips = (cols + wide * V - 1) / (wide * V), high = kAmaxThreads / wide, most = (size_t)info.sms * kAmaxCtas;
+    const unsigned deep = (rows + high * 8 - 1) / (high * 8) * strips < most ? 2 : 8;      // rows of a thread: two where eight leave SMs without work
+    const size_t units = (rows + high * deep - 1) / (high * deep) * strips, slots = SSGD_FP4_SCALE_FLOATS - 2;
+    const size_t ctas = units < most ? units : most;
+    maxima = (unsigned)(ctas < slots ? ctas : slots);
+    launch_kernel(deep == 2 ? fp4_amax_kernel<2, T> : fp4_amax_kernel<8, T>, dim3(maxima), dim3(kAmaxThreads), 0, s, true, x, (unsigned)rows,
+                  (unsigned)cols, ldx, rows_aligned(x, ldx), wide, (unsigned)strips, (unsigned long long)units, reinterpret_cast<unsigned*>(tensor_scale + 2));
   }
   if (codes && codes_t)
     return launch_quantise<FORMAT, true, true>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
@@ -509,15 +511,20 @@ ssgd_status quantise_format(const T* x, size_t rows, size_t cols, size_t ldx, in
 
 template <int FORMAT, typename T>
 ssgd_status launch_dequantise(const uint8_t* codes, const uint8_t* scales, const float* ts, size_t rows, size_t cols, T* out, size_t ldo, cudaStream_t s) {
-  const bool aligned = rows_aligned(out, rows > 1 ? ldo : 16 / sizeof(T));
-  const size_t G = aligned ? 16 / sizeof(T) : 8, groups = (cols + G - 1) / G + (aligned ? 0 : 1);
+  if (!rows_aligned(out, rows > 1 ? ldo : 16 / sizeof(T))) {
+    const size_t strips = (cols + 255) / 256, high = kThreads / 32, ctas = (rows + high - 1) / high * strips;
+    if (ctas > kMaxGrid) return SSGD_ERR_SIZE;
+    launch_kernel(fp4_dequantise_rows_kernel<FORMAT, T>, dim3((unsigned)ctas), dim3(kThreads), 0, s, true, codes, scales, ts, (unsigned)rows,
+                  (unsigned)cols, out, ldo, (unsigned)strips);
+    return launch_status();
+  }
+  const size_t G = 16 / sizeof(T), groups = (cols + G - 1) / G;
   unsigned wide = 32;
   while (wide < (unsigned)kThreads && wide < groups) wide *= 2;
   const size_t strips = (groups + wide - 1) / wide, high = kThreads / wide * kRows, ctas = (rows + high - 1) / high * strips;
   if (ctas > kMaxGrid) return SSGD_ERR_SIZE;
-  auto kernel = aligned ? fp4_dequantise_kernel<FORMAT, true, T> : fp4_dequantise_kernel<FORMAT, false, T>;
-  launch_kernel(kernel, dim3((unsigned)ctas), dim3(kThreads), 0, s, true, codes, scales, ts, (unsigned)rows, (unsigned)cols, out, ldo, (unsigned)groups,
-                wide, (unsigned)strips);
+  launch_kernel(fp4_dequantise_kernel<FORMAT, T>, dim3((unsigned)ctas), dim3(kThreads), 0, s, true, codes, scales, ts, (unsigned)rows, (unsigned)cols, out,
+                ldo, (unsigned)groups, wide, (unsigned)strips);
   return launch_status();
 }
 
