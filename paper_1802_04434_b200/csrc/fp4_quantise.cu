@@ -247,11 +247,20 @@ __device__ __forceinline__ void load_tile(unsigned tile, const T* __restrict__ x
   }
 }
 
+// The scale tiles of a tile of rows, from shared memory.
+template <unsigned NB>
+__device__ __forceinline__ void write_scales(const uint8_t* staged_scales, uint8_t* __restrict__ scales, unsigned cols, unsigned r0, unsigned c0) {
+  constexpr unsigned B = kSide / NB;
+  const size_t tiles_k = ((cols + B - 1) / B + 3) / 4, first = c0 / B / 4;
+  if (threadIdx.x < NB / 4 * 32 && first + threadIdx.x / 32 < tiles_k)
+    reinterpret_cast<uint4*>(scales + (r0 / kSide * tiles_k + first) * 512)[threadIdx.x] = reinterpret_cast<const uint4*>(staged_scales)[threadIdx.x];
+}
+
 // 64 bytes of codes of each of the tile's rows, and its scale tiles, from shared memory.
 template <unsigned NB, unsigned THREADS>
 __device__ __forceinline__ void write_out(const unsigned char* staged, const uint8_t* staged_scales, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                           unsigned rows, unsigned cols, unsigned r0, unsigned c0) {
-  const size_t row_bytes = (size_t)((cols + 31) / 32) * 16, tiles_k = ((cols + kSide / NB - 1) / (kSide / NB) + 3) / 4, first = c0 / (kSide / NB) / 4;
+  const size_t row_bytes = (size_t)((cols + 31) / 32) * 16;
 #pragma unroll
   for (unsigned i = threadIdx.x; i < kSide * 4; i += THREADS) {
     const unsigned r = i / 4, at = i % 4 * 16;
@@ -260,14 +269,43 @@ __device__ __forceinline__ void write_out(const unsigned char* staged, const uin
       *reinterpret_cast<uint4*>(codes + (size_t)(r0 + r) * row_bytes + c0 / 2 + at) = make_uint4(lo.x, lo.y, hi.x, hi.y);
     }
   }
-  if (threadIdx.x < NB / 4 * 32 && first + threadIdx.x / 32 < tiles_k)
-    reinterpret_cast<uint4*>(scales + (r0 / kSide * tiles_k + first) * 512)[threadIdx.x] = reinterpret_cast<const uint4*>(staged_scales)[threadIdx.x];
+  write_scales<NB>(staged_scales, scales, cols, r0, c0);
 }
 
 template <int B>
 __device__ __forceinline__ void stage_codes(unsigned char* to, const unsigned (&word)[B / 8]) {
 #pragma unroll
   for (int i = 0; i < B / 16; ++i) *reinterpret_cast<uint2*>(to + 8 * i) = make_uint2(word[2 * i], word[2 * i + 1]);
+}
+
+// The tensor scale (1 for mx), from the caller's maximum, from the maxima of the pass before, or from a small matrix itself;
+// the first CTA writes down what was found.  Every thread of the CTA must call.
+template <int FORMAT, unsigned THREADS, typename T>
+__device__ __forceinline__ float tensor_scale_of(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, const float* __restrict__ amax,
+                                                 unsigned maxima, float* tensor_scale, unsigned* part) {
+  if constexpr (FORMAT == SSGD_MXFP4) return 1.0f;
+  float top;
+  if (amax) {
+    top = __ldg(amax);
+  } else if (maxima > 0) {                                // every warp for itself
+    unsigned t = 0;
+    for (unsigned i = threadIdx.x & 31u; i < maxima; i += 32) t = max(t, __float_as_uint(tensor_scale[2 + i]));
+    top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, t));
+  } else {
+    const unsigned t = __reduce_max_sync(0xFFFFFFFFu, small_amax<THREADS>(x, rows, cols, ldx, vec));
+    if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = t;
+    __syncthreads();
+    unsigned all = 0;
+#pragma unroll
+    for (unsigned w = 0; w < THREADS / 32; ++w) all = max(all, part[w]);
+    top = __uint_as_float(all);
+  }
+  const float ts = fp4_tensor_scale(top);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    tensor_scale[0] = ts;
+    if (!amax) tensor_scale[1] = top;
+  }
+  return ts;
 }
 
 // piece: bytes that a copy of x's elements may have (16, 4, or 0: none, its rows start at odd 16-bit elements)
@@ -299,29 +337,7 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
       *reinterpret_cast<T*>(tile + r * PITCH + c * sizeof(T)) = in ? x[(size_t)(r0 + r) * ldx + c0 + c] : from_float<T>(0.0f);
     }
   }
-  float ts = 1.0f;
-  if constexpr (FORMAT == SSGD_NVFP4) {
-    float top;
-    if (amax) {
-      top = __ldg(amax);
-    } else if (maxima > 0) {                              // the largest of the pass before, by every warp for itself
-      unsigned t = 0;
-      for (unsigned i = threadIdx.x & 31u; i < maxima; i += 32) t = max(t, __float_as_uint(tensor_scale[2 + i]));
-      top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, t));
-    } else {
-      const unsigned t = __reduce_max_sync(0xFFFFFFFFu, small_amax<THREADS>(x, rows, cols, ldx, piece == 16));
-      if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = t;
-      __syncthreads();
-      unsigned all = 0;
-#pragma unroll
-      for (unsigned w = 0; w < THREADS / 32; ++w) all = max(all, part[w]);
-      top = __uint_as_float(all);
-    }
-    if (!amax && blockIdx.x == 0 && threadIdx.x == 0) tensor_scale[1] = top;
-    ts = fp4_tensor_scale(top);
-    if (blockIdx.x == 0 && threadIdx.x == 0) tensor_scale[0] = ts;
-  }
-  const float ti = __fdiv_rn(1.0f, ts);
+  const float ti = __fdiv_rn(1.0f, tensor_scale_of<FORMAT, THREADS>(x, rows, cols, ldx, piece == 16, amax, maxima, tensor_scale, part));
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
 
@@ -370,6 +386,55 @@ fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_
     __syncthreads();
     write_out<NB, THREADS>(staged, staged_scales, codes_t, scales_t, cols, rows, c0, r0);
   }
+}
+
+// By rows only, 16-bit elements, rows at multiples of 16 bytes: the same tiles without the way through shared memory.  A thread
+// loads its block (lanes over the blocks of a row, 16-byte pieces), and its codes leave with its neighbours', 64 bytes of a
+// row (B200, 8192 x 8192 bf16, mx / nv: 27 / 29 us; through shared memory 35 / 39; fp32, mx: 65 instead of 52, so not for it).
+template <int FORMAT, typename T>
+__global__ void __launch_bounds__(kThreads)
+fp4_quantise_rows_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, const float* __restrict__ amax, unsigned maxima,
+                         float* tensor_scale, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, unsigned tiles_c) {
+  constexpr unsigned B = FORMAT == SSGD_MXFP4 ? 32 : 16, NB = kSide / B, ITEMS = kSide * NB / kThreads, PIECES = B * sizeof(T) / 16, V = 16 / sizeof(T);
+  __shared__ __align__(16) uint8_t staged_scales[NB * kSide];
+  __shared__ unsigned part[kThreads / 32];
+  pdl_launch_dependents();
+  pdl_wait();
+  const unsigned at = gridDim.x - 1 - blockIdx.x, r0 = at / tiles_c * kSide, c0 = at % tiles_c * kSide;
+  uint4 raw[ITEMS][PIECES];
+#pragma unroll
+  for (unsigned u = 0; u < ITEMS; ++u) {
+    const unsigned i = u * kThreads + threadIdx.x, row = r0 + i / NB, c = c0 + i % NB * B;
+    const T* src = x + (size_t)row * ldx + c;
+#pragma unroll
+    for (unsigned q = 0; q < PIECES; ++q) {
+      raw[u][q] = make_uint4(0, 0, 0, 0);
+      if (row < rows && c + (q + 1) * V <= cols) {
+        raw[u][q] = *reinterpret_cast<const uint4*>(src + q * V);
+      } else if (row < rows && c + q * V < cols) {        // the row ends inside this piece
+        T e[V];
+#pragma unroll
+        for (unsigned j = 0; j < V; ++j) e[j] = c + q * V + j < cols ? src[q * V + j] : from_float<T>(0.0f);
+        raw[u][q] = *reinterpret_cast<const uint4*>(e);
+      }
+    }
+  }
+  const float ti = __fdiv_rn(1.0f, tensor_scale_of<FORMAT, kThreads>(x, rows, cols, ldx, true, amax, maxima, tensor_scale, part));
+  const size_t row_bytes = (size_t)((cols + 31) / 32) * 16;
+#pragma unroll
+  for (unsigned u = 0; u < ITEMS; ++u) {
+    const unsigned i = u * kThreads + threadIdx.x, r = i / NB, blk = i % NB, row = r0 + r, c = c0 + blk * B;
+    unsigned word[B / 8];
+    const unsigned byte = quantise_words<FORMAT, B, T>(reinterpret_cast<const unsigned*>(raw[u]), ti, word);
+    staged_scales[blk / 4 * 512 + (r & 31u) * 16 + (r >> 5) * 4 + (blk & 3u)] = row < rows && c < cols ? (uint8_t)byte : 0;
+    if (row < rows && c < row_bytes * 2) {
+      uint8_t* out = codes + (size_t)row * row_bytes + c / 2;
+      if constexpr (B == 16) *reinterpret_cast<uint2*>(out) = make_uint2(word[0], word[1]);
+      else *reinterpret_cast<uint4*>(out) = make_uint4(word[0], word[1], word[2], word[3]);
+    }
+  }
+  __syncthreads();
+  write_scales<NB>(staged_scales, scales, cols, r0, c0);
 }
 
 // Rows of out that start at multiples of 16 bytes.  A thread takes groups of 16 bytes (their codes lie in one word, the
@@ -473,6 +538,15 @@ ssgd_status launch_quantise(const T* x, size_t rows, size_t cols, size_t ldx, co
                             uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, cudaStream_t s) {
   DeviceInfo info;
   if (!device_info(&info)) return SSGD_ERR_CUDA;
+  if constexpr (ROWS && !COLS && sizeof(T) == 2) {
+    const size_t tiles_c = (cols + kSide - 1) / kSide, tiles = (rows + kSide - 1) / kSide * tiles_c;
+    if (rows_aligned(x, ldx)) {
+      if (tiles > kMaxGrid) return SSGD_ERR_SIZE;
+      launch_kernel(fp4_quantise_rows_kernel<FORMAT, T>, dim3((unsigned)tiles), dim3(kThreads), 0, s, true, x, (unsigned)rows, (unsigned)cols, ldx, amax,
+                    maxima, tensor_scale, codes, scales, (unsigned)tiles_c);
+      return launch_status();
+    }
+  }
   if (sizeof(T) == 4 || (rows + kSide - 1) / kSide * ((cols + kSide - 1) / kSide) <= (size_t)info.sms * 2)
     return launch_tiles<FORMAT, ROWS, COLS, 512>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
   return launch_tiles<FORMAT, ROWS, COLS, sizeof(T) == 4 ? 512 : 256>(x, rows, cols, ldx, amax, maxima, tensor_scale, codes, scales, codes_t, scales_t, s);
