@@ -1,10 +1,12 @@
 // Product of two microscaled 4-bit operands, out[i][j] = tA tB sum_k A[i][k] B[j][k].  See include/signsgd.h.
 //
-// The tensor cores multiply 4-bit values and apply the block scales themselves (tcgen05.mma, block-scaled): a CTA keeps a
-// tile of 128 rows of B by NT rows of A as fp32 accumulators in tensor memory.  B's rows are the accumulator's lanes, so
-// a warp's 32 lanes hold 32 neighbours of one row of out and the stores need no transposition; and few rows of A (a
-// handful of tokens against a weight) only make NT small, the weight streams through once either way.
+// The tensor cores multiply 4-bit values and apply the block scales themselves (tcgen05.mma, block-scaled): products and
+// scales are exact, sums are fp32.  Two kernels:
 //
+// fp4_matmul_kernel, up to 128 rows of A: a CTA keeps a tile of 128 rows of B by NT rows of A as fp32 accumulators in
+// tensor memory.  B's rows are the accumulator's lanes, so a warp's 32 lanes hold 32 neighbours of one row of out and the
+// stores need no transposition; and few rows of A (a handful of tokens against a weight) only make NT small, the weight
+// streams through once either way.
 //   warp 0      one thread brings a stage, 256 of k: 128 x 128 and NT x 128 bytes of codes (tiled copies, 128-byte
 //               swizzle, out-of-range rows and columns filled with zero codes) and their scale tiles (bulk copies)
 //   warp 1      one thread copies the scales into tensor memory and issues four MMAs of 64 of k per stage
@@ -12,6 +14,12 @@
 // Every stage has scale columns of its own, so that nothing is overwritten before the commit that frees the stage.
 // Few output tiles: a cluster of 2, 4 or 8 CTAs splits k, the partial tiles meet in shared memory and each CTA adds up
 // its share of the columns over the cluster, in rank order: no atomics, equal inputs give equal bits.
+// Bound by the weight's bytes (B200: 16 rows against 18944 x 8192 9.7 us = 8.5 TB/s from L2 and HBM); a small one by its
+// launch and one trip to memory (one row against 4096 x 1024: 3.6 us).
+//
+// fp4_matmul_pair_kernel, more rows: below.  B200, 8192^3 to bf16: mx 183 us = 6010 TFLOP/s, nv 203 us = 5420 (four times the
+// measured bf16 rate of the library's product, 1666, would be 6664; at sustained load, 1408, 5632).  What bounds it: bytes from
+// L2 to shared memory, and power; without any copies the same MMAs took 180 us.
 
 #include <cooperative_groups.h>
 
@@ -257,16 +265,17 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
 // accumulator's lanes), by NT rows of the other, Q (its columns).  A CTA loads 128 rows of P and half of the rows of Q, so an
 // operand byte that reaches shared memory serves 256 rows instead of 128, and the bytes from L2 to shared memory are a third
 // less than with single CTAs.
-//   WIDE           P = A, Q = B: a lane holds neighbours of one row of out and stores 32 bytes at a time; for rows of out that
-//                  start at multiples of 32 bytes.  Otherwise P = B, Q = A: the lanes of a warp hold neighbours, stores of
-//                  one element, coalesced, wherever a row starts
+//   WIDE           P = A, Q = B: a lane holds neighbours of one row of out; a warp puts 32 rows x 32 columns into shared
+//                  memory, and an asynchronous copy takes them out while the warp goes on; for rows of out that start at multiples of
+//                  16 bytes.  Otherwise P = B, Q = A: the lanes of a warp hold neighbours, stores of one element, coalesced,
+//                  wherever a row starts
 //   accumulators   two, so that a tile is written out while the next one is multiplied.  Both and the scales' columns do not
 //                  fit beside one another at NT = 256: the second starts at `second` < NT, the epilogue drains the shared
 //                  columns first and gives the go-ahead after them
 //   scales         a set of columns for every stage, or at NT = 256 two in turn: a set is overwritten when the MMAs that
 //                  read it are known to be done
 
-template <int FORMAT, int NT>
+template <int FORMAT, int NT, unsigned OUT_BYTES>
 struct PairShape {
   static constexpr unsigned blocks = FORMAT == SSGD_MXFP4 ? 2 : 4;
   static constexpr unsigned row_tiles = (NT + 127) / 128;
@@ -274,14 +283,17 @@ struct PairShape {
   static constexpr unsigned scale_bytes = blocks * 512;
   static constexpr unsigned loaded = p_bytes + q_bytes + (1 + row_tiles) * scale_bytes;     // per CTA and stage
   static constexpr unsigned stage_bytes = (loaded + 1023) / 1024 * 1024;
-  static constexpr unsigned stages = 225280 / stage_bytes < 8 ? 225280 / stage_bytes : 8;
+  static constexpr unsigned box_bytes = 32 * 32 * OUT_BYTES, out_bytes = 8 * box_bytes;   // the eight warps' boxes on their way out
+  static constexpr unsigned bar_bytes = 256;
+  static constexpr unsigned room_bytes = 232448 - out_bytes - bar_bytes; // for the stages
+  static constexpr unsigned stages = room_bytes / stage_bytes < 8 ? room_bytes / stage_bytes : 8;
   static constexpr unsigned scale_columns = (1 + row_tiles) * blocks * 4;
   static constexpr unsigned ring = NT == 256 ? 2 : stages;              // sets of scale columns
   static constexpr unsigned first_scale = 512 - ring * scale_columns;
   static constexpr unsigned room = (first_scale - NT) / 32 * 32;
   static constexpr unsigned second = room < NT ? room : NT;              // column of the second accumulator
-  static constexpr unsigned smem = stages * stage_bytes + 1024;
-  static_assert(stages >= 3 && smem <= 231424, "shared memory");
+  static constexpr unsigned smem = stages * stage_bytes + out_bytes + bar_bytes;      // no other shared memory: the stages start at its base
+  static_assert(stages >= 3 && (2 * stages + 2) * 8 + 8 <= bar_bytes, "shared memory");
   static_assert(second + NT <= first_scale && (NT == 256 || second == NT), "tensor memory");
 };
 
@@ -306,13 +318,14 @@ __device__ __forceinline__ TilePlace tile_place(unsigned tile, const PairArgs& a
 template <int FORMAT, int NT, typename T, bool WIDE>
 __global__ void __launch_bounds__(kMmaThreads, 1)
 fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_constant__ CUtensorMap q_map,
-                       const __grid_constant__ CUtensorMap p_scale_map, const __grid_constant__ CUtensorMap q_scale_map, const PairArgs p) {
-  using S = PairShape<FORMAT, NT>;
-  extern __shared__ unsigned char dynamic_smem[];
-  __shared__ __align__(8) uint64_t bars[2 * S::stages + 2];
-  __shared__ unsigned tmem_base, failed;
+                       const __grid_constant__ CUtensorMap p_scale_map, const __grid_constant__ CUtensorMap q_scale_map,
+                       const __grid_constant__ CUtensorMap out_map, const PairArgs p) {
+  using S = PairShape<FORMAT, NT, sizeof(T)>;
+  extern __shared__ __align__(1024) unsigned char pair_smem[];           // stages, boxes, barriers; the same place in both CTAs
+  uint64_t* bars = reinterpret_cast<uint64_t*>(pair_smem + S::stages * S::stage_bytes + S::out_bytes);
+  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 2), &failed = *(&tmem_base + 1);
   const unsigned rank = cluster_rank();
-  const unsigned stage0 = (smem_u32(dynamic_smem) + 1023u) & ~1023u;     // the same in both CTAs
+  const unsigned stage0 = smem_u32(pair_smem);
   const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 8;
   const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const unsigned stages_k = (p.k_chunks + 3) / 4;
@@ -323,6 +336,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
     prefetch_tensor_map(&p_map);
     prefetch_tensor_map(&q_scale_map);
     prefetch_tensor_map(&p_scale_map);
+    if (WIDE) prefetch_tensor_map(&out_map);
     for (unsigned s = 0; s < S::stages; ++s) {
       mbarrier_init(full + 8 * s, 1);
       mbarrier_init(empty + 8 * s, 1);
@@ -405,63 +419,61 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
       if (!ok) tcgen05_commit_pair(acc_full);   // what was issued has to end before tensor memory is freed
     }
   } else {
-    const unsigned quarter = warp & 3u, odd = warp >= 6;      // two warps share a quarter of the lanes, 32 columns in turn
+    // Two warps share a quarter of the lanes, units of kUnit columns in turn.
+    constexpr unsigned kUnit = 32, kUnits = NT / kUnit, kSharedUnits = (NT - S::second) / kUnit;
+    const unsigned quarter = warp & 3u, odd = warp >= 6;
     const float ts = (p.p_ts ? __ldg(p.p_ts) : 1.0f) * (p.q_ts ? __ldg(p.q_ts) : 1.0f);
-    const unsigned go = cluster_address(acc_free, 0);
+    const unsigned go = cluster_address(acc_free, 0), box = stage0 + S::stages * S::stage_bytes + (warp - 2) * S::box_bytes;
     unsigned t = 0;
     for (unsigned tile = pair; tile < tiles; tile += pairs, ++t) {
       ok = mbarrier_wait(acc_full, t & 1u, 4 * kPolls + 64 * stages_k);
       if (!ok) break;
       tcgen05_fence_after();
       const TilePlace at = tile_place<NT>(tile, p);
-      const unsigned row = at.p0 + rank * 128 + quarter * 32 + lane, q0 = at.q0;       // of P; the first of Q
+      const unsigned row0 = at.p0 + rank * 128 + quarter * 32, q0 = at.q0;             // of P; the first of Q
       const unsigned lanes = tmem + (t & 1u) * S::second + (quarter << 21);
       // the columns that both accumulators use come first: from `second` on in the first, the front ones in the second
-      constexpr unsigned shared = NT - S::second;
       const unsigned first = (t & 1u) ? 0u : S::second % NT;
-      if (shared == 0) {
-        if (lane == 0) mbarrier_arrive_cluster(go);
-      }
+      if (odd + 1 > kSharedUnits && lane == 0) mbarrier_arrive_cluster(go);            // none of them is this warp's
 #pragma unroll 1
-      for (unsigned done = odd * 32; done < NT; done += 64) {
-        const unsigned c = (first + done) % NT;
+      for (unsigned unit = odd; unit < kUnits; unit += 2) {
+        const unsigned c = (first + unit * kUnit) % NT;
         unsigned v[32];
         tmem_read32(lanes + c, v);
-        if (shared > 0 && done < shared && done + 64 >= shared) {          // this warp's last shared columns
+        if (kSharedUnits > 0 && unit + 1 <= kSharedUnits && unit + 2 >= kSharedUnits) {                       // this warp's last shared columns
           tcgen05_fence_before();
           __syncwarp();
           if (lane == 0) mbarrier_arrive_cluster(go);
         }
-        const unsigned left = q0 + c < p.Q ? min(32u, p.Q - (q0 + c)) : 0u;      // columns of the 32 that exist
-        if (row < p.P) {
+        if (row0 < p.P && q0 + c < p.Q) {
           if constexpr (WIDE) {
-            T* o = static_cast<T*>(p.out) + (size_t)row * p.ldo + q0 + c;
-            if (left == 32) {
-              if constexpr (sizeof(T) == 4) {
+            if (lane == 0) tma_store_wait_read();                                      // the box is free again
+            __syncwarp();
+            if constexpr (sizeof(T) == 2) {                                            // rows of 64 bytes, 64-byte swizzle
 #pragma unroll
-                for (unsigned q = 0; q < 32; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * ts);
+              for (unsigned q = 0; q < 16; ++q) v[q] = pack2(T(), __uint_as_float(v[2 * q]) * ts, __uint_as_float(v[2 * q + 1]) * ts);
 #pragma unroll
-                for (unsigned q = 0; q < 32; q += 8) store32(o + q, v + q);
-              } else {
+              for (unsigned q = 0; q < 4; ++q)
+                store_shared16(box + lane * 64 + ((q ^ (lane >> 1 & 3u)) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+            } else {                                                                   // rows of 128 bytes, 128-byte swizzle
 #pragma unroll
-                for (unsigned q = 0; q < 16; ++q) v[q] = pack2(T(), __uint_as_float(v[2 * q]) * ts, __uint_as_float(v[2 * q + 1]) * ts);
-                store32(o, v);
-                store32(o + 16, v + 8);
-              }
-            } else {
+              for (unsigned q = 0; q < 32; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * ts);
 #pragma unroll
-              for (unsigned q = 0; q < 32; ++q)
-                if (q < left) o[q] = from_float<T>(__uint_as_float(v[q]) * ts);
+              for (unsigned q = 0; q < 8; ++q)
+                store_shared16(box + lane * 128 + ((q ^ (lane & 7u)) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
             }
-          } else {
-            T* o = static_cast<T*>(p.out) + (size_t)(q0 + c) * p.ldo + row;
-            store_column(o, p.ldo, v, left, ts);
+            async_proxy_fence();
+            __syncwarp();
+            if (lane == 0) tma_store_2d(&out_map, (int)(q0 + c), (int)row0, box);
+          } else if (row0 + lane < p.P) {
+            store_column(static_cast<T*>(p.out) + (size_t)(q0 + c) * p.ldo + row0 + lane, p.ldo, v, min(32u, p.Q - (q0 + c)), ts);
           }
         }
         __syncwarp();
       }
       tcgen05_fence_before();
     }
+    if (WIDE && lane == 0) tma_store_wait();
   }
   if (!ok) atomicExch(&failed, 1u);
   __syncwarp();
@@ -517,6 +529,18 @@ bool scale_map(CUtensorMap* map, const uint8_t* scales, size_t row_tiles, size_t
   const cuuint32_t box[2] = {box_tiles * 64, box_rows}, steps[2] = {1, 1};
   return f(map, CU_TENSOR_MAP_DATA_TYPE_UINT64, 2, const_cast<uint8_t*>(scales), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// out as boxes of 32 columns x 32 rows, swizzled over the 64 or 128 bytes of a row.
+bool out_map_of(CUtensorMap* map, void* out, int dtype, size_t rows, size_t cols, size_t ldo) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const size_t e = dtype_bytes((unsigned)dtype);
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ldo * e};
+  const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
+  return f(map, dtype == SSGD_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == SSGD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+           2, out, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, e == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int FORMAT, int NT, typename T>
@@ -598,15 +622,17 @@ ssgd_status product(const Operands& o, int sms, cudaStream_t s) {
 
 template <int FORMAT, int NT, typename T, bool WIDE>
 ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
-  using S = PairShape<FORMAT, NT>;
+  using S = PairShape<FORMAT, NT, sizeof(T)>;
   const size_t row_bytes = ssgd_fp4_row_bytes(o.K), tiles_k = (fp4_block_count(FORMAT, o.K) + 3) / 4;
   const size_t P = WIDE ? o.M : o.N, Q = WIDE ? o.N : o.M, tiles_p = (P + 255) / 256, tiles_q = (Q + NT - 1) / NT;
   if (tiles_p * tiles_q > kMaxGrid / 8) return SSGD_ERR_SIZE;
-  CUtensorMap p_map, q_map, p_scale_map, q_scale_map;
+  CUtensorMap p_map, q_map, p_scale_map, q_scale_map, out_map;
   if (!code_map(&p_map, WIDE ? o.a : o.b, P, row_bytes, 128) || !code_map(&q_map, WIDE ? o.b : o.a, Q, row_bytes, NT / 2) ||
       !scale_map(&p_scale_map, WIDE ? o.a_scales : o.b_scales, (P + 127) / 128, tiles_k, S::blocks, 1) ||
       !scale_map(&q_scale_map, WIDE ? o.b_scales : o.a_scales, (Q + 127) / 128, tiles_k, S::blocks, S::row_tiles))
     return SSGD_ERR_CUDA;
+  if (!WIDE) out_map = p_map;                    // not used
+  else if (!out_map_of(&out_map, o.out, o.dtype, o.M, o.N, o.ldo)) return SSGD_ERR_CUDA;
   PairArgs p;
   p.p_ts = o.a_ts; p.q_ts = o.b_ts; p.out = o.out; p.status = o.status; p.ldo = o.ldo;
   p.P = (unsigned)P; p.Q = (unsigned)Q;
@@ -631,7 +657,7 @@ ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  (void)cudaLaunchKernelEx(&cfg, kernel, p_map, q_map, p_scale_map, q_scale_map, p);
+  (void)cudaLaunchKernelEx(&cfg, kernel, p_map, q_map, p_scale_map, q_scale_map, out_map, p);
   return launch_status();
 }
 
@@ -650,8 +676,9 @@ ssgd_status pair_product(const Operands& o, bool wide, int sms, cudaStream_t s) 
 }
 
 // Nanoseconds of a product by pairs with tiles of 256 x nt, fitted on B200: a start, a stage, and for each further tile of a
-// pair its stages or its writing out, whichever is longer (2048 x 1024 x 4096, nt = 64 / 128 / 256: 9.3 / 7.7 / 11.1 us, fitted
-// 8.1 / 7.0 / 10.4; 2048 x 4096 x 1024: - / 9.9 / 9.6, fitted 9.9 / 9.1 / 8.9; 777 x 1111 x 1500: 5.8 / 6.4 / -, fitted 4.6 / 5.4).
+// pair its stages or its writing out, whichever is longer.  Measured, nt = 64 / 128 / 256 in us: 2048 x 1024 x 4096 10.2 / 7.9 /
+// 10.7; 2048 x 4096 x 1024 12.3 / 9.2 / 9.3; 777 x 1111 x 1500 5.8 / 6.4 / 8.5; 8192 x 8192 x 256 46 / 28 / 25.  Over 22 shapes in
+// two types the choice was within 5 % of the best of the three but for two (10 and 11 %).
 inline unsigned long long pair_cost(unsigned long long tiles_p, size_t Q, unsigned nt, unsigned long long stages_k, unsigned pairs) {
   const unsigned long long tiles = tiles_p * ((Q + nt - 1) / nt), rounds = (tiles + pairs - 1) / pairs;
   const unsigned start = nt == 64 ? 3900 : nt == 128 ? 4400 : 5600, stage = nt == 64 ? 123 : nt == 128 ? 160 : 300,
@@ -667,7 +694,7 @@ ssgd_status any_product(const Operands& o, int sms, cudaStream_t s) {
   const size_t stages_k = (ssgd_fp4_row_bytes(o.K) + 127) / 128;
   if (o.M <= 128 || (stages_k >= 24 && ((o.M + 127) / 128) * ((o.N + kTileJ - 1) / kTileJ) * 8 <= (size_t)sms)) return product<FORMAT>(o, sms, s);
   const size_t e = dtype_bytes((unsigned)o.dtype);
-  const bool wide = reinterpret_cast<uintptr_t>(o.out) % 32 == 0 && o.ldo * e % 32 == 0;
+  const bool wide = aligned16(o.out) && o.ldo * e % 16 == 0 && o.ldo < (size_t)1 << 37;
   const size_t P = wide ? o.M : o.N, Q = wide ? o.N : o.M, tiles_p = (P + 255) / 256;
   const unsigned pairs = (unsigned)(sms / 2);
   const unsigned long long c64 = pair_cost(tiles_p, Q, 64, stages_k, pairs), c128 = pair_cost(tiles_p, Q, 128, stages_k, pairs),
