@@ -17,9 +17,9 @@
 // Bound by the weight's bytes (B200: 16 rows against 18944 x 8192 9.7 us = 8.5 TB/s from L2 and HBM); a small one by its
 // launch and one trip to memory (one row against 4096 x 1024: 3.6 us).
 //
-// fp4_matmul_pair_kernel, more rows: below.  B200, 8192^3 to bf16: mx 183 us = 6010 TFLOP/s, nv 203 us = 5420 (four times the
-// measured bf16 rate of the library's product, 1666, would be 6664; at sustained load, 1408, 5632).  What bounds it: bytes from
-// L2 to shared memory, and power; without any copies the same MMAs took 180 us.
+// fp4_matmul_pair_kernel, more rows: below.  B200, 8192^3 to bf16, a few in a row: mx 184 us = 5980 TFLOP/s, nv 203 us = 5420 (four
+// times the library's measured bf16 rate, 1666, is 6664).  The same MMAs on operands that are not loaded again take 150 / 162
+// us: the rest is bytes from L2 to shared memory.  Run for longer it is bound by power: 234 us nv at 1.37 GHz and 945 W.
 
 #include <cooperative_groups.h>
 

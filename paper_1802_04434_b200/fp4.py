@@ -29,7 +29,7 @@ class Packed:
     tensor_scale   float32, its first element (None: 1)
 
     Its three parts may lie in one buffer, as `quantise` makes them; they are cut out of it when they are asked for."""
-    __slots__ = ("rows", "cols", "fmt", "device", "pointers", "_parts", "_buffer")
+    __slots__ = ("rows", "cols", "fmt", "device", "pointers", "_parts", "_buffer")      # _buffer: (buffer, byte offsets of the parts)
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Optional[torch.Tensor], rows: int, cols: int, fmt: str):
         if fmt not in _BLOCK:
@@ -47,16 +47,6 @@ class Packed:
         self.pointers = (codes.data_ptr(), scales.data_ptr(), 0 if tensor_scale is None else tensor_scale.data_ptr())
         self.rows, self.cols, self.fmt, self.device = rows, cols, fmt, device
         self._parts, self._buffer = (codes, scales, tensor_scale), None
-
-    @classmethod
-    def _in(cls, buffer: torch.Tensor, base: int, at: Tuple[int, int, Optional[int]], rows: int, cols: int, fmt: str,
-            device: torch.device) -> "Packed":
-        """Parts at the given byte offsets of one buffer whose address is `base`."""
-        p = cls.__new__(cls)
-        p.rows, p.cols, p.fmt, p.device = rows, cols, fmt, device
-        p.pointers = (base + at[0], base + at[1], 0 if at[2] is None else base + at[2])
-        p._parts, p._buffer = None, (buffer, at)
-        return p
 
     def _cut(self):
         if self._parts is None:
@@ -101,59 +91,85 @@ def check(device="cuda") -> None:
         raise RuntimeError("a 4-bit product did not receive its operands in time; its output is not valid")
 
 
+# These calls are a few microseconds of Python each, next to kernels of a few microseconds: what is below avoids calls,
+# temporary objects and look-ups on the way to the library.
+_new = object.__new__
+_stream_of = B._stream_of
+_pack_quantise, _pack_dequantise, _pack_matmul = B.FP4_QUANTISE_ARGS.pack, B.FP4_DEQUANTISE_ARGS.pack, B.FP4_MATMUL_ARGS.pack
+_DTYPES, _FORMATS = B.DTYPE_CODE, B.FP4_FORMAT
+
+
+def _packed_in(buffer, base, codes, scales, ts, rows, cols, fmt, device):
+    """A packed matrix whose parts lie at the given byte offsets of one buffer, whose address is `base`."""
+    p = _new(Packed)
+    p.rows = rows
+    p.cols = cols
+    p.fmt = fmt
+    p.device = device
+    p.pointers = (base + codes, base + scales, 0 if ts is None else base + ts)
+    p._parts = None
+    p._buffer = (buffer, (codes, scales, ts))
+    return p
+
+
 def _quantise(x, fmt, amax, by_rows, by_columns):
     block = _BLOCK.get(fmt)
     if block is None:
         raise ValueError("fmt must be 'mx' or 'nv'")
-    dtype = B.DTYPE_CODE.get(x.dtype)
+    dtype = _DTYPES.get(x.dtype)
     if dtype is None:
         raise TypeError("the matrix must be of dtype float32, bfloat16 or float16")
-    shape = x.shape
-    if len(shape) != 2:
-        raise ValueError("a matrix is wanted, got %d dimensions" % len(shape))
-    rows, cols = shape
-    index = x.get_device()
-    if index < 0:
+    strides = x.stride()
+    if len(strides) != 2:
+        raise ValueError("a matrix is wanted, got %d dimensions" % len(strides))
+    device = x.device
+    index = device.index
+    if index is None or not x.is_cuda:
         raise ValueError("the matrix must live in device memory")
-    ldx, step = x.stride()
+    rows, cols = x.shape
+    ldx, step = strides
     # rows at any stride; a single column, or a single row, has no stride of its own to look at
     if (step != 1 and cols > 1) or (ldx < cols and rows > 1):
         x = x.contiguous()
         ldx = cols
-    n = m = nt = mt = 0
+    at = 0                                    # the parts one after another: all are multiples of 16 bytes
     if by_rows:
-        n, m = _sizes(rows, cols, fmt)
+        s = rows * ((cols + 31) // 32 * 16)
+        at = s + (rows + 127) // 128 * ((cols + 4 * block - 1) // (4 * block)) * 512
     if by_columns:
-        nt, mt = _sizes(cols, rows, fmt)
-    nv = block == 16
-    ts = n + m + nt + mt                      # all parts are multiples of 16 bytes
-    device = x.device
-    tail = 0 if not nv else 4 * B.FP4_SCALE_FLOATS if amax is None and rows * cols > B.FP4_SMALL else 8
-    buffer = torch.empty(ts + tail, dtype=_U8, device=device)
+        ct = at
+        st = ct + cols * ((rows + 31) // 32 * 16)
+        at = st + (cols + 127) // 128 * ((rows + 4 * block - 1) // (4 * block)) * 512
+    if block == 32:
+        ts, size = None, at
+    else:
+        ts, size = at, at + (4 * B.FP4_SCALE_FLOATS if amax is None and rows * cols > B.FP4_SMALL else 8)
+    buffer = torch.empty(size, dtype=_U8, device=device)
     base = buffer.data_ptr()
     if rows and cols:
-        status = B.lib().ssgd_fp4_quantise_block(B.FP4_QUANTISE_ARGS.pack(
-            x.data_ptr(), dtype, rows, cols, ldx if ldx > cols else cols, 1 if nv else 0,
-            0 if amax is None else B._ptr(amax, torch.float32, "amax"), base + ts if nv else 0, base if by_rows else 0, base + n,
-            base + n + m if by_columns else 0, base + n + m + nt, B._stream_of(index)))
+        status = B.lib().ssgd_fp4_quantise_block(_pack_quantise(
+            x.data_ptr(), dtype, rows, cols, ldx if ldx > cols else cols, 0 if ts is None else 1,
+            0 if amax is None else B._ptr(amax, torch.float32, "amax"), 0 if ts is None else base + ts, base if by_rows else 0,
+            base + s if by_rows else 0, base + ct if by_columns else 0, base + st if by_columns else 0, _stream_of(index)))
         if status:
             B._check(status, "ssgd_fp4_quantise")
-    elif nv:
+    elif ts is not None:
         buffer[ts:ts + 8].view(torch.float32).fill_(1.0)
-    at = ts if nv else None
-    return (Packed._in(buffer, base, (0, n, at), rows, cols, fmt, device) if by_rows else None,
-            Packed._in(buffer, base, (n + m, n + m + nt, at), cols, rows, fmt, device) if by_columns else None)
+    if not by_columns:
+        return _packed_in(buffer, base, 0, s, ts, rows, cols, fmt, device)
+    transposed = _packed_in(buffer, base, ct, st, ts, cols, rows, fmt, device)
+    return (_packed_in(buffer, base, 0, s, ts, rows, cols, fmt, device), transposed) if by_rows else transposed
 
 
 def quantise(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor] = None) -> Packed:
     """x (float32, bfloat16 or float16, rows at any stride) packed with blocks along its columns.  `amax`: a device
     float32 with max |x|, "nv" only, where the caller has it already (`binding.tensors_norm(kind="max")`)."""
-    return _quantise(x, fmt, amax, True, False)[0]
+    return _quantise(x, fmt, amax, True, False)
 
 
 def quantise_columns(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor] = None) -> Packed:
     """The transpose of x packed: blocks along x's rows."""
-    return _quantise(x, fmt, amax, False, True)[1]
+    return _quantise(x, fmt, amax, False, True)
 
 
 def quantise_both(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor] = None) -> Tuple[Packed, Packed]:
@@ -163,11 +179,11 @@ def quantise_both(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor]
 
 def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """The values of a packed matrix."""
-    out = torch.empty(p.rows, p.cols, dtype=dtype, device=p.device)
-    if p.rows and p.cols:
-        codes, scales, ts = p.pointers
-        status = B.lib().ssgd_fp4_dequantise_block(B.FP4_DEQUANTISE_ARGS.pack(
-            codes, scales, ts, B.FP4_FORMAT[p.fmt], p.rows, p.cols, out.data_ptr(), B.DTYPE_CODE[dtype], p.cols, B._stream_of(p.device.index)))
+    rows, cols, device = p.rows, p.cols, p.device
+    out = torch.empty(rows, cols, dtype=dtype, device=device)
+    if rows and cols:
+        status = B.lib().ssgd_fp4_dequantise_block(_pack_dequantise(
+            *p.pointers, _FORMATS[p.fmt], rows, cols, out.data_ptr(), _DTYPES[dtype], cols, _stream_of(device.index)))
         if status:
             B._check(status, "ssgd_fp4_dequantise")
     return out
@@ -175,24 +191,26 @@ def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
 
 def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """a b^T of two packed matrices of one format, fp32 accumulation; into `out` (rows at any stride) where given."""
-    if a.fmt != b.fmt or a.cols != b.cols or a.device != b.device:
-        raise ValueError("a product needs operands of one format, one length and one device: got %s x %d and %s x %d" % (a.fmt, a.cols, b.fmt, b.cols))
+    fmt, k, device = a.fmt, a.cols, a.device
+    if fmt != b.fmt or k != b.cols or device != b.device:
+        raise ValueError("a product needs operands of one format, one length and one device: got %s x %d and %s x %d" % (fmt, k, b.fmt, b.cols))
     rows, cols = a.rows, b.rows
-    ldo = max(1, cols)
+    ldo = cols or 1
     if out is None:
-        out = torch.empty(rows, cols, dtype=dtype, device=a.device)
+        out = torch.empty(rows, cols, dtype=dtype, device=device)
     else:
-        if out.shape != (rows, cols) or out.device != a.device or (cols > 1 and out.stride(1) != 1) or (rows > 1 and out.stride(0) < cols):
+        dtype = out.dtype
+        if out.shape != (rows, cols) or out.device != device or (cols > 1 and out.stride(1) != 1) or (rows > 1 and out.stride(0) < cols):
             raise ValueError("out must be %d x %d with unit column stride, on the operands' device" % (rows, cols))
         ldo = out.stride(0) if rows > 1 else ldo
-    if a.cols == 0:
+    if k == 0:
         return out.zero_()
     if rows and cols:
-        status = B.lib().ssgd_fp4_matmul_block(B.FP4_MATMUL_ARGS.pack(
-            *a.pointers, *b.pointers, rows, cols, a.cols, B.FP4_FORMAT[a.fmt], out.data_ptr(), B.DTYPE_CODE[out.dtype], ldo,
-            _status_of(a.device)[1], B._stream_of(a.device.index)))
-        if status:
-            B._check(status, "ssgd_fp4_matmul")
+        status = _status.get(device) or _status_of(device)
+        failed = B.lib().ssgd_fp4_matmul_block(_pack_matmul(
+            *a.pointers, *b.pointers, rows, cols, k, _FORMATS[fmt], out.data_ptr(), _DTYPES[dtype], ldo, status[1], _stream_of(device.index)))
+        if failed:
+            B._check(failed, "ssgd_fp4_matmul")
     return out
 
 
