@@ -83,7 +83,7 @@ __device__ __forceinline__ unsigned piece_amax(const T* __restrict__ at, unsigne
 // 16-byte aligned are read element by element, lanes side by side.
 constexpr unsigned kAmaxThreads = 512, kAmaxCtas = 2;     // CTAs of an SM
 template <unsigned ROWS, typename T>
-__global__ void __launch_bounds__(kAmaxThreads)
+__global__ void __launch_bounds__(kAmaxThreads, kAmaxCtas)
 fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, bool vec, unsigned wide, unsigned strips, unsigned long long units,
                 unsigned* __restrict__ out) {
   constexpr unsigned V = 16 / sizeof(T);
@@ -310,7 +310,7 @@ __device__ __forceinline__ float tensor_scale_of(const T* __restrict__ x, unsign
 
 // piece: bytes that a copy of x's elements may have (16, 4, or 0: none, its rows start at odd 16-bit elements)
 template <int FORMAT, bool ROWS, bool COLS, unsigned THREADS, typename T>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 0)
 fp4_quantise_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ldx, unsigned piece, const float* __restrict__ amax,
                     unsigned maxima, float* tensor_scale, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                     uint8_t* __restrict__ codes_t, uint8_t* __restrict__ scales_t, unsigned tiles_c) {
@@ -532,7 +532,7 @@ ssgd_status launch_tiles(const T* x, size_t rows, size_t cols, size_t ldx, const
 
 // 512 threads for fp32, whose tiles leave room for two CTAs of an SM, and for few 16-bit tiles, where a CTA's own time counts;
 // else 256, of which four fit (B200, bf16 both ways: 2048 x 1024 mx 3.2 us with 512, 4.0 with 256; 1999 x 4103 nv 15.1 and 13.8;
-// 8192 x 8192 mx 83 and 41).
+// 8192 x 8192 mx 83 and 41).  Registers as the compiler likes them: held to four or five CTAs, 256 threads take 44 and 55 us there.
 template <int FORMAT, bool ROWS, bool COLS, typename T>
 ssgd_status launch_quantise(const T* x, size_t rows, size_t cols, size_t ldx, const float* amax, unsigned maxima, float* tensor_scale,
                             uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, cudaStream_t s) {

@@ -138,8 +138,14 @@ norms_finish_kernel(const uint64_t* __restrict__ first_tile, const double* __res
   pdl_wait();
   const uint64_t a = first_tile[blockIdx.x], b = first_tile[blockIdx.x + 1];
   double s = 0.0;
-#pragma unroll 4
-  for (uint64_t i = a + threadIdx.x; i < b; i += kFinishThreads) s = combine<KIND>(s, partial[i]);
+  // sixteen loads in flight: one CTA has to bring a double for every tile of the group
+  for (uint64_t i = a + threadIdx.x; i < b; i += 16 * kFinishThreads) {
+    double v[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) v[u] = i + u * kFinishThreads < b ? partial[i + u * kFinishThreads] : 0.0;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) s = combine<KIND>(s, v[u]);
+  }
   s = cta_combine<KIND, kFinishThreads>(s, part);
   if (threadIdx.x == 0) norms[blockIdx.x] = finish_norm<KIND>(s);
 }
