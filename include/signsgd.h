@@ -458,6 +458,13 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
                             size_t N, size_t K, int format, void* out, int dtype, size_t ldo, unsigned* status,
                             void* stream);
 
+/* Self-test of the bounded waits of ssgd_fp4_matmul: the same launch with every stage armed for more bytes than its copies
+ * deliver (all copies still complete).  The kernel must return within its limits (a few seconds) with bit 0 of *status
+ * set and `out` untouched; the context stays usable.  M, N <= 256, K <= 512.                                            */
+ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
+                                          const uint8_t* b_scales, size_t M, size_t N, size_t K, int format, void* out,
+                                          int dtype, size_t ldo, unsigned* status, void* stream);
+
 /* The calls above with their arguments in one HOST block of 64-bit words, in the order of their parameters: pointers
  * and sizes as they are, other integers widened, a float as the bits of a double.  For callers whose foreign-function
  * interface costs by the argument (Python's ctypes: 0.6 us instead of 2 us a call).  NULL: SSGD_ERR_NULL.            */

@@ -81,6 +81,7 @@ def lib() -> ctypes.CDLL:
         "ssgd_table_build": [vp, sz, sz, vp, sz],
         "ssgd_tensors_norm": [vp, sz, sz, ci, vp, vp, vp],
         "ssgd_tensors_clip": [vp, sz, sz, ci, f32, ci, vp, vp, vp],
+        "ssgd_fp4_matmul_wait_selftest": [vp, vp, vp, vp, sz, sz, sz, ci, vp, ci, sz, vp, vp],
         "ssgd_tensors_clip_block": [ctypes.c_char_p],
         "ssgd_fp4_quantise_block": [ctypes.c_char_p],
         "ssgd_fp4_dequantise_block": [ctypes.c_char_p],

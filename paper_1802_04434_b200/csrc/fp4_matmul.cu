@@ -95,6 +95,7 @@ struct ProductArgs {
   unsigned tiles_k;       // scale tiles along k of one row of tiles
   unsigned a_row_tiles;   // scale row tiles of A
   unsigned tiles_i;
+  unsigned starve;        // bytes that a stage waits for in vain: 0 but in the self-test of the waits
 };
 
 // 32 accumulators of one lane to a column of out (rows of stride ldo), `left` of them wanted.
@@ -162,7 +163,7 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
         const unsigned kt = k * S::blocks, blocks = min(S::blocks, p.tiles_k - kt);
         const unsigned row_tiles = min(S::row_tiles, p.a_row_tiles - it);
         issued = n + 1;
-        mbarrier_expect(bar, S::b_bytes + S::a_bytes + (1 + row_tiles) * blocks * 512);
+        mbarrier_expect(bar, S::b_bytes + S::a_bytes + (1 + row_tiles) * blocks * 512 + p.starve);
         tma_load_2d(base, &b_map, (int)(k * 128), (int)j0, bar);
         tma_load_2d(base + S::b_bytes, &a_map, (int)(k * 128), (int)i0, bar);
         const unsigned sc = base + S::b_bytes + S::a_bytes;
@@ -293,7 +294,7 @@ struct PairShape {
   static constexpr unsigned room = (first_scale - NT) / 32 * 32;
   static constexpr unsigned second = room < NT ? room : NT;              // column of the second accumulator
   static constexpr unsigned smem = stages * stage_bytes + out_bytes + bar_bytes;      // no other shared memory: the stages start at its base
-  static_assert(stages >= 3 && (2 * stages + 2) * 8 + 8 <= bar_bytes, "shared memory");
+  static_assert(stages >= 3 && (2 * stages + 3) * 8 + 8 <= bar_bytes, "shared memory");
   static_assert(second + NT <= first_scale && (NT == 256 || second == NT), "tensor memory");
 };
 
@@ -304,6 +305,7 @@ struct PairArgs {
   unsigned* status;
   size_t ldo;
   unsigned P, Q, k_chunks, tiles_p, tiles_q;    // rows and tiles of either side
+  unsigned starve;                              // bytes that a stage waits for in vain: 0 but in the self-test of the waits
 };
 
 // Tiles go through bands of eight of P's tiles, so that those in flight share rows of both operands.
@@ -323,10 +325,10 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
   using S = PairShape<FORMAT, NT, sizeof(T)>;
   extern __shared__ __align__(1024) unsigned char pair_smem[];           // stages, boxes, barriers; the same place in both CTAs
   uint64_t* bars = reinterpret_cast<uint64_t*>(pair_smem + S::stages * S::stage_bytes + S::out_bytes);
-  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 2), &failed = *(&tmem_base + 1);
+  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 3), &failed = *(&tmem_base + 1);
   const unsigned rank = cluster_rank();
   const unsigned stage0 = smem_u32(pair_smem);
-  const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 8;
+  const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 8, ended = acc_free + 8;
   const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const unsigned stages_k = (p.k_chunks + 3) / 4;
   const unsigned pair = blockIdx.x / 2, pairs = gridDim.x / 2, tiles = p.tiles_p * p.tiles_q;
@@ -342,6 +344,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
       mbarrier_init(empty + 8 * s, 1);
     }
     mbarrier_init(acc_full, 1);
+    mbarrier_init(ended, 1);
     mbarrier_init(acc_free, 16);                // one arrival from each of the two CTAs' eight epilogue warps
     mbarrier_init_fence();
     failed = 0;
@@ -367,7 +370,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
           if (n >= S::stages) ok = mbarrier_wait(empty + 8 * s, (n / S::stages - 1) & 1u, kPolls);
           if (!ok) break;
           const unsigned base = stage0 + s * S::stage_bytes, bar = cluster_address(full + 8 * s, 0);
-          if (rank == 0) mbarrier_expect(full + 8 * s, 2 * S::loaded);
+          if (rank == 0) mbarrier_expect(full + 8 * s, 2 * S::loaded + p.starve);
           tma_load_2d_pair(base, &p_map, (int)(k * 128), (int)p0, bar);
           tma_load_2d_pair(base + S::p_bytes, &q_map, (int)(k * 128), (int)(q0 + rank * (NT / 2)), bar);
           const unsigned sc = base + S::p_bytes + S::q_bytes;
@@ -416,7 +419,10 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
         }
         if (ok) tcgen05_commit_pair(acc_full);
       }
-      if (!ok) tcgen05_commit_pair(acc_full);   // what was issued has to end before tensor memory is freed
+      if (!ok) {                                // what was issued has to end before tensor memory is freed; nobody writes it out
+        tcgen05_commit_pair(ended);
+        (void)mbarrier_wait(ended, 0, kPolls);
+      }
     }
   } else {
     // Two warps share a quarter of the lanes, units of kUnit columns in turn.
@@ -574,6 +580,7 @@ struct Operands {
   int dtype;
   size_t ldo;
   unsigned* status;
+  unsigned starve;
 };
 
 template <int FORMAT, int NT>
@@ -612,6 +619,7 @@ ssgd_status product(const Operands& o, int sms, cudaStream_t s) {
   p.tiles_k = (unsigned)((fp4_block_count(FORMAT, o.K) + 3) / 4);
   p.a_row_tiles = (unsigned)((o.M + 127) / 128);
   p.tiles_i = (unsigned)tiles_i;
+  p.starve = o.starve;
   switch (nt) {
     case 16: return launch_product_typed<FORMAT, 16>(a_map, b_map, p, o.dtype, tiles, splits, s);
     case 32: return launch_product_typed<FORMAT, 32>(a_map, b_map, p, o.dtype, tiles, splits, s);
@@ -639,6 +647,7 @@ ssgd_status launch_pair(const Operands& o, int sms, cudaStream_t s) {
   p.k_chunks = (unsigned)((row_bytes + 31) / 32);
   p.tiles_p = (unsigned)tiles_p;
   p.tiles_q = (unsigned)tiles_q;
+  p.starve = o.starve;
   auto kernel = fp4_matmul_pair_kernel<FORMAT, NT, T, WIDE>;
   static unsigned long long seen = 0;
   if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
@@ -703,13 +712,9 @@ ssgd_status any_product(const Operands& o, int sms, cudaStream_t s) {
   return c128 <= c64 ? pair_product<FORMAT, 128>(o, wide, sms, s) : pair_product<FORMAT, 64>(o, wide, sms, s);
 }
 
-}  // namespace
-
-extern "C" {
-
-ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_tensor_scale, const uint8_t* b_codes,
-                            const uint8_t* b_scales, const float* b_tensor_scale, size_t M, size_t N, size_t K, int format, void* out,
-                            int dtype, size_t ldo, unsigned* status, void* stream) {
+ssgd_status checked_product(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_tensor_scale, const uint8_t* b_codes, const uint8_t* b_scales,
+                            const float* b_tensor_scale, size_t M, size_t N, size_t K, int format, void* out, int dtype, size_t ldo, unsigned* status,
+                            unsigned starve, void* stream) {
   if (!fp4_format_ok(format) || dtype_bytes((unsigned)dtype) == 0) return SSGD_ERR_ARG;
   if (!a_codes || !a_scales || !b_codes || !b_scales || !out || !status) return SSGD_ERR_NULL;
   if (M > SSGD_FP4_MAX_SIDE || N > SSGD_FP4_MAX_SIDE || K > SSGD_FP4_MAX_SIDE || ldo < N || mul_overflows(M, ldo) || mul_overflows(M * ldo, 4))
@@ -726,8 +731,24 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
   }
   DeviceInfo info;
   if (!device_info(&info)) return SSGD_ERR_CUDA;
-  const Operands o = {a_codes, a_scales, b_codes, b_scales, a_tensor_scale, b_tensor_scale, M, N, K, out, dtype, ldo, status};
+  const Operands o = {a_codes, a_scales, b_codes, b_scales, a_tensor_scale, b_tensor_scale, M, N, K, out, dtype, ldo, status, starve};
   return format == SSGD_MXFP4 ? any_product<SSGD_MXFP4>(o, info.sms, s) : any_product<SSGD_NVFP4>(o, info.sms, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_tensor_scale, const uint8_t* b_codes,
+                            const uint8_t* b_scales, const float* b_tensor_scale, size_t M, size_t N, size_t K, int format, void* out,
+                            int dtype, size_t ldo, unsigned* status, void* stream) {
+  return checked_product(a_codes, a_scales, a_tensor_scale, b_codes, b_scales, b_tensor_scale, M, N, K, format, out, dtype, ldo, status, 0, stream);
+}
+
+ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, size_t M,
+                                          size_t N, size_t K, int format, void* out, int dtype, size_t ldo, unsigned* status, void* stream) {
+  if (M > 256 || N > 256 || K > 512) return SSGD_ERR_SIZE;      // one tile, two stages: the waits run out once
+  return checked_product(a_codes, a_scales, nullptr, b_codes, b_scales, nullptr, M, N, K, format, out, dtype, ldo, status, 16, stream);
 }
 
 ssgd_status ssgd_fp4_matmul_block(const uint64_t* a) {

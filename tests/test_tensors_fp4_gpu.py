@@ -567,3 +567,18 @@ def test_refusals_of_the_torch_layer(fp4, B):
         B.tensors_clip(B.TensorTable([x]), -1.0, torch.zeros(1, device="cuda"))
     with pytest.raises(ValueError):
         B.tensors_norm(B.TensorTable([x, x], None, [0, 1]), torch.zeros(1, device="cuda"))
+
+
+@pytest.mark.parametrize("M,N", [(5, 100), (128, 128), (200, 250), (250, 256)])
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_waits_of_the_product_run_out(fp4, B, M, N, fmt):
+    """Stages that wait for bytes nobody sends: the kernel gives up, says so, writes nothing, and the next product is right."""
+    a, b = fp4.quantise(randn(M, 500, seed=71), fmt), fp4.quantise(randn(N, 500, seed=72), fmt)
+    out, status = torch.full((M, N), 7.0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    st = B.lib().ssgd_fp4_matmul_wait_selftest(a.pointers[0], a.pointers[1], b.pointers[0], b.pointers[1], M, N, 500, B.FP4_FORMAT[fmt],
+                                               out.data_ptr(), 0, N, status.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    torch.cuda.synchronize()
+    assert status.item() == 1 and bool((out == 7.0).all())
+    check_product(a, b, fp4.matmul(a, b, F32), F32)
+    fp4.check()
