@@ -10,7 +10,7 @@ ROOT = os.path.dirname(_HERE)
 SOURCES = [os.path.join(_HERE, "csrc", n) for n in ("signsgd.cu", "variants.cu", "stats.cu", "exchange.cu", "vote_staged.cu",
                                                      "tensors.cu", "fp4_quantise.cu", "fp4_matmul.cu")]
 HEADERS = [os.path.join(ROOT, "include", "signsgd.h")] + [
-    os.path.join(_HERE, "csrc", n) for n in ("device_common.cuh", "host_common.h", "vote_launch.h", "step_rows.cuh", "dtypes.cuh", "fp4.cuh", "sm100.cuh")]
+    os.path.join(_HERE, "csrc", n) for n in ("device_common.cuh", "host_common.h", "vote_launch.h", "step_rows.cuh", "host_calls.h", "dtypes.cuh", "fp4.cuh", "sm100.cuh")]
 LIB = os.path.join(_HERE, "libsignsgd_b200.so")
 
 NVCC_FLAGS = [

@@ -23,7 +23,7 @@
 
 #include <cooperative_groups.h>
 
-#include "host_common.h"
+#include "host_calls.h"
 #include "dtypes.cuh"
 #include "fp4.cuh"
 #include "sm100.cuh"

@@ -4,7 +4,7 @@
 //   code = nearest 4-bit value to x / S, ties to the even code, magnitudes above 6 to 6
 // A block that holds an infinity or a NaN gets the NaN scale: it reads back as NaN, and so do products with it.
 
-#include "host_common.h"
+#include "host_calls.h"
 #include "dtypes.cuh"
 #include "fp4.cuh"
 

@@ -44,10 +44,6 @@ struct StepArgs {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// A pointer out of a block of arguments.
-template <typename T>
-inline T* block_ptr(uint64_t word) { return reinterpret_cast<T*>(static_cast<uintptr_t>(word)); }
-
 inline bool mul_overflows(size_t a, size_t b) { return b != 0 && a > SIZE_MAX / b; }
 
 ssgd_status check_rows(size_t M, size_t d, size_t ld, size_t ldw, bool need_ld) {
@@ -66,18 +62,6 @@ ssgd_status check_rows(size_t M, size_t d, size_t ld, size_t ldw, bool need_ld) 
 inline bool beta_ok(float beta) { return beta >= 0.0f && beta < 1.0f; }  // false for NaN
 
 ssgd_status launch_status() { return cudaGetLastError() == cudaSuccess ? SSGD_OK : SSGD_ERR_CUDA; }
-
-// Lets a kernel have `bytes` of dynamic shared memory, asked of the runtime once per kernel and device: `seen` is a
-// static of the caller's, one for each kernel, a bit for each device.
-bool allow_smem(const void* kernel, size_t bytes, unsigned long long* seen) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
-  if (__atomic_load_n(seen, __ATOMIC_RELAXED) & bit) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
-  __atomic_fetch_or(seen, bit, __ATOMIC_RELAXED);
-  return true;
-}
 
 // Kernel launch with the programmatic-serialization attribute (see pdl_wait in device_common.cuh), for
 // kernels that begin with pdl_wait(); pdl = false gives an ordinary launch.

@@ -14,7 +14,7 @@
 #include <cooperative_groups.h>
 #include <string.h>
 
-#include "host_common.h"
+#include "host_calls.h"
 #include "dtypes.cuh"
 
 namespace {
