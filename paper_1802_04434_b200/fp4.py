@@ -239,16 +239,32 @@ def linear_backward(kept: Kept, dy: torch.Tensor, dw: Optional[torch.Tensor] = N
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, fmt):
-        y, ctx.kept = linear_forward(x.detach(), w.detach(), fmt)
-        ctx.w_dtype = w.dtype
-        return y
+        rows = x.reshape(-1, x.shape[-1])
+        need_x, need_w = ctx.needs_input_grad[:2]
+        # only what the backward products will want is packed by columns
+        xr, xc = quantise_both(rows, fmt) if need_w else (quantise(rows, fmt), None)
+        wr, wc = quantise_both(w, fmt) if need_x else (quantise(w, fmt), None)
+        ctx.kept, ctx.w_dtype, ctx.x_shape = Kept(xc, wc, x.dtype), w.dtype, x.shape
+        return matmul(xr, wr, x.dtype).view(*x.shape[:-1], w.shape[0])
 
     @staticmethod
     def backward(ctx, dy):
-        dx, dw = linear_backward(ctx.kept, dy, dw_dtype=ctx.w_dtype)
+        kept = ctx.kept
+        fmt = (kept.x_columns or kept.w_columns).fmt
+        rows = dy.reshape(-1, dy.shape[-1])
+        if kept.x_columns is None:
+            dr, dc = quantise(rows, fmt), None
+        elif kept.w_columns is None:
+            dr, dc = None, quantise_columns(rows, fmt)
+        else:
+            dr, dc = quantise_both(rows, fmt)
+        dx = matmul(dr, kept.w_columns, kept.dtype).view(ctx.x_shape) if dr is not None else None
+        dw = matmul(dc, kept.x_columns, ctx.w_dtype) if dc is not None else None
         return dx, dw, None
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, fmt: str = "mx") -> torch.Tensor:
-    """x w^T with all three products in 4 bits, for torch's autograd."""
+    """x w^T with all three products in 4 bits, for torch's autograd; x [..., in], w [out][in]."""
+    if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
+        raise ValueError("x's last side must be w's second: got %s and %s" % (tuple(x.shape), tuple(w.shape)))
     return _Linear.apply(x, w, fmt)

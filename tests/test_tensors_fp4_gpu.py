@@ -582,3 +582,61 @@ def test_waits_of_the_product_run_out(fp4, B, M, N, fmt):
     assert status.item() == 1 and bool((out == 7.0).all())
     check_product(a, b, fp4.matmul(a, b, F32), F32)
     fp4.check()
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_linear_in_autograd(fp4, fmt):
+    """Leading sides, a broadcast gradient, inputs that want no gradient."""
+    x, w = randn(3, 5, 96, seed=81, dtype=BF16), randn(40, 96, seed=82, scale=0.1)
+    xa, wa = x.clone().requires_grad_(), w.clone().requires_grad_()
+    y = fp4.linear(xa, wa, fmt)
+    assert y.shape == (3, 5, 40)
+    y.sum().backward()                                        # dy is one number, expanded
+    flat, kept = fp4.linear_forward(x.view(15, 96), w, fmt)
+    dx, dw = fp4.linear_backward(kept, torch.ones(15, 40, dtype=BF16, device="cuda"))
+    assert torch.equal(y.view(15, 40), flat) and torch.equal(xa.grad.view(15, 96), dx) and torch.equal(wa.grad, dw)
+    xb, wb = x.clone().requires_grad_(), w.clone().requires_grad_()
+    fp4.linear(xb, w, fmt).sum().backward()
+    fp4.linear(x, wb, fmt).sum().backward()
+    assert torch.equal(xb.grad, xa.grad) and torch.equal(wb.grad, wa.grad)
+    with torch.no_grad():
+        assert torch.equal(fp4.linear(x, w, fmt), y)
+    z = fp4.linear(torch.zeros(0, 96, device="cuda", requires_grad=True), w.requires_grad_(), fmt)
+    z.sum().backward()
+    assert z.shape == (0, 40) and bool((w.grad == 0).all())
+    with pytest.raises(ValueError):
+        fp4.linear(x, w.t(), fmt)
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_rows_beyond_32_bits(fp4, B, fmt):
+    """Rows so far apart that their places pass 2^32 elements and bytes."""
+    stride = (1 << 31) + 64
+    base = torch.empty(2 * stride + 1024, dtype=BF16, device="cuda")
+    x = base.as_strided((3, 200), (stride, 1), 8)
+    x.copy_(randn(3, 200, seed=91))
+    p, pt = fp4.quantise_both(x, fmt)
+    check_packed(p, f64(x), fmt)
+    check_packed(pt, f64(x).T, fmt)
+    B.fp4_dequantise(p.codes, p.scales, p.tensor_scale, fmt, 3, 200, x, stride)
+    assert torch.equal(x, fp4.dequantise(p, BF16))
+    del base, x
+    a, b = fp4.quantise(randn(150, 320, seed=92), fmt), fp4.quantise(randn(60, 320, seed=93), fmt)
+    for rows, ldo in ((150, 1 << 25), (150, (1 << 25) + 1), (100, (1 << 25) + (1 << 24))):
+        q = fp4.quantise(randn(rows, 320, seed=92), fmt)
+        out = torch.empty(rows * ldo, device="cuda").as_strided((rows, 60), (ldo, 1))
+        fp4.matmul(q, b, out=out)
+        assert torch.equal(out, fp4.matmul(q, b, F32))
+        del out
+    fp4.check()
+
+
+def test_norm_of_more_than_32_bits_of_elements(B):
+    n = (1 << 32) + 5
+    x = torch.empty(n, dtype=BF16, device="cuda").fill_(0.5)
+    norms = torch.zeros(1, device="cuda")
+    B.tensors_clip(B.TensorTable([x], [x]), 1.0, norms)
+    want = 0.5 * math.sqrt(n)
+    assert abs(norms.item() - want) <= want * 2.0 ** -23
+    c = torch.tensor(0.5, device="cuda") * (torch.tensor(1.0, device="cuda") / norms[0])
+    assert bool((x[-9:] == c.to(BF16)).all()) and bool((x[(1 << 31) - 4:(1 << 31) + 4] == c.to(BF16)).all()) and x[0] == c.to(BF16)
