@@ -80,7 +80,8 @@ __device__ __forceinline__ unsigned piece_amax(const T* __restrict__ at, unsigne
 // Largest magnitude of what each CTA sees, as bits, to a place of its own: no memory has to start at zero, and every CTA
 // of the quantisation that follows takes the largest of them.  A CTA takes rectangles: `wide` threads (a power of two) lie
 // along a row, a piece of 16 bytes each, the others in rows below, every thread ROWS rows, all in flight.  Rows that are not
-// 16-byte aligned are read element by element, lanes side by side.
+// 16-byte aligned are read element by element, lanes side by side: which of the two is the matrix's, not a thread's, choice,
+// because the lanes' elements lie elsewhere than their pieces.
 constexpr unsigned kAmaxThreads = 512, kAmaxCtas = 2;     // CTAs of an SM
 template <unsigned ROWS, typename T>
 __global__ void __launch_bounds__(kAmaxThreads, kAmaxCtas)
@@ -94,12 +95,21 @@ fp4_amax_kernel(const T* __restrict__ x, unsigned rows, unsigned cols, size_t ld
   for (unsigned long long i = blockIdx.x; i < units; i += gridDim.x) {
     const unsigned r0 = (unsigned)(i / strips) * (high * ROWS) + below, c0 = (unsigned)(i % strips) * (wide * V);
     const unsigned c = c0 + lane * V;
-    if (vec && r0 + (ROWS - 1) * high < rows && c + V <= cols) {
-      uint4 q[ROWS];
+    if (vec) {
+      if (r0 + (ROWS - 1) * high < rows && c + V <= cols) {
+        uint4 q[ROWS];
 #pragma unroll
-      for (unsigned r = 0; r < ROWS; ++r) q[r] = *reinterpret_cast<const uint4*>(x + (size_t)(r0 + r * high) * ldx + c);
+        for (unsigned r = 0; r < ROWS; ++r) q[r] = *reinterpret_cast<const uint4*>(x + (size_t)(r0 + r * high) * ldx + c);
 #pragma unroll
-      for (unsigned r = 0; r < ROWS; ++r) w = larger(T(), larger(T(), w, larger(T(), q[r].x, q[r].y)), larger(T(), q[r].z, q[r].w));
+        for (unsigned r = 0; r < ROWS; ++r) w = larger(T(), larger(T(), w, larger(T(), q[r].x, q[r].y)), larger(T(), q[r].z, q[r].w));
+      } else if (c < cols) {                              // the matrix ends within the thread's rows or its piece
+        const unsigned left = min(V, cols - c);
+#pragma unroll (ROWS < 4 ? ROWS : 4)
+        for (unsigned r = 0; r < ROWS; ++r)
+#pragma unroll
+          for (unsigned e = 0; e < V; ++e)
+            if (r0 + r * high < rows && e < left) w = larger(T(), w, word_of(x[(size_t)(r0 + r * high) * ldx + c + e]));
+      }
     } else {
 #pragma unroll (ROWS < 4 ? ROWS : 4)
       for (unsigned r = 0; r < ROWS; ++r)

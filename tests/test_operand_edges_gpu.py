@@ -1,0 +1,60 @@
+"""Operands, products and clipping where they went wrong once: slices, extreme scales, sums of 16-bit squares; on a B200
+against plain forms in 64 bits."""
+import math
+import os
+import sys
+
+import numpy as np
+import pytest
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import fp4_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1802_04434_b200 import binding
+    binding.lib()
+    return binding
+
+
+@pytest.fixture(scope="module")
+def fp4(B):
+    from paper_1802_04434_b200 import fp4
+    return fp4
+
+
+def randn(*shape, seed=0, dtype=F32, scale=1.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# the tensor scale of a slice
+
+
+@pytest.mark.parametrize("rows,cols,width,dtype", [
+    (64, 1111, 1112, BF16), (512, 100, 104, F16), (512, 101, 104, F32), (300, 129, 136, BF16), (33, 2049, 2056, F16), (40, 1000, 1008, BF16),
+    (16, 4103, 4104, F32), (9, 8205, 8208, BF16), (2100, 1501, 1504, BF16), (1999, 515, 516, F32), (3000, 33, 40, F16)])
+def test_largest_value_in_the_last_columns_of_a_slice(fp4, rows, cols, width, dtype):
+    """Rows at multiples of 16 bytes whose last 16-byte piece is not whole: each of its columns holds the largest value once."""
+    piece = 128 // torch.finfo(dtype).bits
+    base = randn(rows, width, seed=rows + cols, dtype=dtype)
+    base[:, cols:] = math.inf                                  # not part of the matrix
+    x = base[:, :cols]
+    for back in range(1, cols % piece + 1):
+        y = x.clone()
+        x[(back * 37) % rows, cols - back] = 1000.0
+        want = ref.quantise(x.float().cpu().numpy(), "nv")
+        for p, t in ((fp4.quantise(x, "nv"), False), (fp4.quantise_columns(x, "nv"), True), (fp4.quantise_both(x, "nv")[0], False)):
+            assert p.tensor_scale.tolist() == [want[2], 1000.0]
+            if not t:
+                assert np.array_equal(p.codes.cpu().numpy(), ref.pack_codes(want[0]))
+                assert np.array_equal(p.scales.cpu().numpy(), ref.pack_scales(want[1]))
+        x.copy_(y)
