@@ -403,6 +403,12 @@ def _typed_ptr(t: torch.Tensor, name: str) -> int:
     return t.data_ptr()
 
 
+def _need_first(t: Optional[torch.Tensor], name: str) -> None:
+    """A tensor of one value that may be left out must hold it where it is given: an empty one has address 0, as one that is left out."""
+    if t is not None:
+        _need(t, 1, name)
+
+
 def _need_rows(t: torch.Tensor, rows: int, cols: int, ld: int, name: str) -> None:
     """t's memory, from its first element on, must hold `rows` rows of `cols` elements at a stride of ld."""
     n = (rows - 1) * ld + cols if rows and cols else 0
@@ -508,6 +514,7 @@ def fp4_quantise(x: torch.Tensor, rows: int, cols: int, ldx: int, fmt: str, amax
                  codes_t: Optional[torch.Tensor], scales_t: Optional[torch.Tensor], stream=None) -> None:
     """Packs x (its first element at x, rows of stride ldx) by rows, by columns, or both, into uint8 buffers."""
     _need_rows(x, rows, cols, ldx, "x")
+    _need_first(amax, "amax")
     for name, c, s, r, k in (("codes", codes, scales, rows, cols), ("codes_t", codes_t, scales_t, cols, rows)):
         if c is not None:
             _need(c, r * ((k + 31) // 32 * 16), name); _need(s, fp4_scale_bytes(fmt, r, k), "scales of " + name)
@@ -524,6 +531,7 @@ def fp4_dequantise(codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Opti
                    cols: int, out: torch.Tensor, ldo: int, stream=None) -> None:
     """out <- the values of a packed operand (rows of stride ldo)."""
     _need(codes, rows * ((cols + 31) // 32 * 16), "codes"); _need(scales, fp4_scale_bytes(fmt, rows, cols), "scales")
+    _need_first(tensor_scale, "tensor_scale")
     _need_rows(out, rows, cols, ldo, "out")
     _check(lib().ssgd_fp4_dequantise(
         _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), _ptr(tensor_scale, torch.float32, "tensor_scale"),
@@ -538,6 +546,7 @@ def fp4_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, a_tensor_scale: Op
     row = (K + 31) // 32 * 16
     _need(a_codes, M * row, "a_codes"); _need(b_codes, N * row, "b_codes"); _need(status, 1, "status")
     _need(a_scales, fp4_scale_bytes(fmt, M, K), "a_scales"); _need(b_scales, fp4_scale_bytes(fmt, N, K), "b_scales")
+    _need_first(a_tensor_scale, "a_tensor_scale"); _need_first(b_tensor_scale, "b_tensor_scale")
     _need_rows(out, M, N, ldo, "out")
     u8, f32 = torch.uint8, torch.float32
     _check(lib().ssgd_fp4_matmul(

@@ -39,6 +39,7 @@ class Packed:
         device = codes.device
         if not codes.is_cuda or scales.device != device or (tensor_scale is not None and tensor_scale.device != device):
             raise ValueError("codes, scales and tensor_scale must live in the memory of one device")
+        B._need_first(tensor_scale, "tensor_scale")
         if not (codes.is_contiguous() and scales.is_contiguous()):
             raise ValueError("codes and scales must be contiguous")
         n, m = _sizes(rows, cols, fmt)
@@ -126,6 +127,8 @@ def _quantise(x, fmt, amax, by_rows, by_columns):
     index = device.index
     if index is None or not x.is_cuda:
         raise ValueError("the matrix must live in device memory")
+    if amax is not None:
+        B._need_first(amax, "amax")
     rows, cols = x.shape
     ldx, step = strides
     # rows at any stride; a single column, or a single row, has no stride of its own to look at
