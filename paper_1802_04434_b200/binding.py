@@ -10,6 +10,7 @@ is raised.
 from __future__ import annotations
 
 import array
+import contextlib
 import ctypes
 import os
 import struct
@@ -134,6 +135,21 @@ def _stream_of(index: int) -> int:
     """The current stream of a device.  (torch.cuda.current_stream() makes a stream object; this only asks for its handle,
     2 us less a call.)"""
     return torch._C._cuda_getCurrentRawStream(index)
+
+
+# torch.cuda.current_device() without its check that CUDA is up, which it is where a device tensor is at hand
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _on(index: int):
+    """Makes a device current, where it is not: a launch goes to the current device, whatever stream and pointers it is given."""
+    return contextlib.nullcontext() if index == _current_device() else torch.cuda.device(index)
+
+
+def _need_device(index: int, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != index:
+            raise ValueError("%s must live in the memory of device %d, as the call's other tensors" % (name, index))
 
 
 def _check(status: int, where: str) -> None:
@@ -475,8 +491,12 @@ FP4_QUANTISE_ARGS, FP4_DEQUANTISE_ARGS, FP4_MATMUL_ARGS = struct.Struct("=13Q"),
 
 
 def tensors_norm(table: TensorTable, norms: torch.Tensor, kind: str = "two", stream=None) -> None:
-    """norms[w] <- norm of worker w's gradient over all its tensors ("two": sqrt of the sum of squares, "max")."""
-    _need(norms, table.workers, "norms")
+    """norms[w] <- norm of worker w's gradient over all its tensors ("two": sqrt of the sum of squares, "max").  Runs on the
+    table's device, whichever is current, by default on its current stream."""
+    _need(norms, table.workers, "norms"); _need_device(table._index, norms=norms)
+    if table._index != _current_device():
+        with _on(table._index):
+            return tensors_norm(table, norms, kind, stream)
     status = lib().ssgd_tensors_norm(*table._args, NORM_KIND[kind], table._ws, _ptr(norms, torch.float32, "norms"),
                                      _stream_of(table._index) if stream is None else _stream(stream))
     if status:
@@ -487,7 +507,11 @@ def tensors_clip(table: TensorTable, max_norm: float, norms: torch.Tensor, kind:
                  stream=None) -> None:
     """norms as `tensors_norm`; every dst <- src * (max_norm / norm where norm > max_norm, else 1).  With zero_nonfinite a
     worker whose norm is not finite gets zeros."""
-    _need(norms, table.workers, "norms")
+    if norms.numel() < table.workers or norms.get_device() != table._index:       # one of the two raises
+        _need(norms, table.workers, "norms"); _need_device(table._index, norms=norms)
+    if table._index != _current_device():
+        with _on(table._index):
+            return tensors_clip(table, max_norm, norms, kind, zero_nonfinite, stream)
     status = lib().ssgd_tensors_clip_block(_CLIP_ARGS.pack(
         *table._args, NORM_KIND[kind], max_norm, 1 if zero_nonfinite else 0, table._ws, _ptr(norms, torch.float32, "norms"),
         _stream_of(table._index) if stream is None else _stream(stream)))
@@ -520,11 +544,13 @@ def fp4_quantise(x: torch.Tensor, rows: int, cols: int, ldx: int, fmt: str, amax
             _need(c, r * ((k + 31) // 32 * 16), name); _need(s, fp4_scale_bytes(fmt, r, k), "scales of " + name)
     if fmt == "nv":
         _need(tensor_scale, FP4_SCALE_FLOATS if amax is None and rows * cols > FP4_SMALL else 2, "tensor_scale")
-    u8, f32 = torch.uint8, torch.float32
-    _check(lib().ssgd_fp4_quantise(
-        _typed_ptr(x, "x"), DTYPE_CODE[x.dtype], rows, cols, ldx, FP4_FORMAT[fmt], _ptr(amax, f32, "amax"),
-        _ptr(tensor_scale, f32, "tensor_scale"), _ptr(codes, u8, "codes"), _ptr(scales, u8, "scales"),
-        _ptr(codes_t, u8, "codes_t"), _ptr(scales_t, u8, "scales_t"), _stream(stream)), "ssgd_fp4_quantise")
+    at, index, u8, f32 = _typed_ptr(x, "x"), x.get_device(), torch.uint8, torch.float32
+    _need_device(index, amax=amax, tensor_scale=tensor_scale, codes=codes, scales=scales, codes_t=codes_t, scales_t=scales_t)
+    with _on(index):
+        _check(lib().ssgd_fp4_quantise(
+            at, DTYPE_CODE[x.dtype], rows, cols, ldx, FP4_FORMAT[fmt], _ptr(amax, f32, "amax"),
+            _ptr(tensor_scale, f32, "tensor_scale"), _ptr(codes, u8, "codes"), _ptr(scales, u8, "scales"),
+            _ptr(codes_t, u8, "codes_t"), _ptr(scales_t, u8, "scales_t"), _stream(stream)), "ssgd_fp4_quantise")
 
 
 def fp4_dequantise(codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Optional[torch.Tensor], fmt: str, rows: int,
@@ -533,9 +559,12 @@ def fp4_dequantise(codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Opti
     _need(codes, rows * ((cols + 31) // 32 * 16), "codes"); _need(scales, fp4_scale_bytes(fmt, rows, cols), "scales")
     _need_first(tensor_scale, "tensor_scale")
     _need_rows(out, rows, cols, ldo, "out")
-    _check(lib().ssgd_fp4_dequantise(
-        _ptr(codes, torch.uint8, "codes"), _ptr(scales, torch.uint8, "scales"), _ptr(tensor_scale, torch.float32, "tensor_scale"),
-        FP4_FORMAT[fmt], rows, cols, _typed_ptr(out, "out"), DTYPE_CODE[out.dtype], ldo, _stream(stream)), "ssgd_fp4_dequantise")
+    at, index, u8 = _typed_ptr(out, "out"), out.get_device(), torch.uint8
+    _need_device(index, codes=codes, scales=scales, tensor_scale=tensor_scale)
+    with _on(index):
+        _check(lib().ssgd_fp4_dequantise(
+            _ptr(codes, u8, "codes"), _ptr(scales, u8, "scales"), _ptr(tensor_scale, torch.float32, "tensor_scale"),
+            FP4_FORMAT[fmt], rows, cols, at, DTYPE_CODE[out.dtype], ldo, _stream(stream)), "ssgd_fp4_dequantise")
 
 
 def fp4_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, a_tensor_scale: Optional[torch.Tensor], b_codes: torch.Tensor,
@@ -548,9 +577,11 @@ def fp4_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, a_tensor_scale: Op
     _need(a_scales, fp4_scale_bytes(fmt, M, K), "a_scales"); _need(b_scales, fp4_scale_bytes(fmt, N, K), "b_scales")
     _need_first(a_tensor_scale, "a_tensor_scale"); _need_first(b_tensor_scale, "b_tensor_scale")
     _need_rows(out, M, N, ldo, "out")
-    u8, f32 = torch.uint8, torch.float32
-    _check(lib().ssgd_fp4_matmul(
-        _ptr(a_codes, u8, "a_codes"), _ptr(a_scales, u8, "a_scales"), _ptr(a_tensor_scale, f32, "a_tensor_scale"),
-        _ptr(b_codes, u8, "b_codes"), _ptr(b_scales, u8, "b_scales"), _ptr(b_tensor_scale, f32, "b_tensor_scale"), M, N, K,
-        FP4_FORMAT[fmt], _typed_ptr(out, "out"), DTYPE_CODE[out.dtype], ldo, _ptr(status, torch.int32, "status"),
-        _stream(stream)), "ssgd_fp4_matmul")
+    at, index, u8, f32 = _typed_ptr(out, "out"), out.get_device(), torch.uint8, torch.float32
+    _need_device(index, a_codes=a_codes, a_scales=a_scales, a_tensor_scale=a_tensor_scale, b_codes=b_codes, b_scales=b_scales,
+                 b_tensor_scale=b_tensor_scale, status=status)
+    with _on(index):
+        _check(lib().ssgd_fp4_matmul(
+            _ptr(a_codes, u8, "a_codes"), _ptr(a_scales, u8, "a_scales"), _ptr(a_tensor_scale, f32, "a_tensor_scale"),
+            _ptr(b_codes, u8, "b_codes"), _ptr(b_scales, u8, "b_scales"), _ptr(b_tensor_scale, f32, "b_tensor_scale"), M, N, K,
+            FP4_FORMAT[fmt], at, DTYPE_CODE[out.dtype], ldo, _ptr(status, torch.int32, "status"), _stream(stream)), "ssgd_fp4_matmul")

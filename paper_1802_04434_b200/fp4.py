@@ -2,7 +2,7 @@
 
 A thin layer over ``binding.fp4_*`` that allocates the outputs; the formats ("mx": blocks of 32 with a power of two,
 "nv": blocks of 16 with an E4M3 number and a tensor scale) and the arithmetic are those of ``include/signsgd.h``.  All
-work is enqueued on the current stream of the operands' device.
+work is enqueued on the current stream of the operands' device, whichever device is current.
 """
 from __future__ import annotations
 
@@ -95,7 +95,7 @@ def check(device="cuda") -> None:
 # These calls are a few microseconds of Python each, next to kernels of a few microseconds: what is below avoids calls,
 # temporary objects and look-ups on the way to the library.
 _new = object.__new__
-_stream_of = B._stream_of
+_stream_of, _current_device = B._stream_of, B._current_device
 _pack_quantise, _pack_dequantise, _pack_matmul = B.FP4_QUANTISE_ARGS.pack, B.FP4_DEQUANTISE_ARGS.pack, B.FP4_MATMUL_ARGS.pack
 _DTYPES, _FORMATS = B.DTYPE_CODE, B.FP4_FORMAT
 
@@ -129,6 +129,10 @@ def _quantise(x, fmt, amax, by_rows, by_columns):
         raise ValueError("the matrix must live in device memory")
     if amax is not None:
         B._need_first(amax, "amax")
+        B._need_device(index, amax=amax)
+    if index != _current_device():
+        with B._on(index):
+            return _quantise(x, fmt, amax, by_rows, by_columns)
     rows, cols = x.shape
     ldx, step = strides
     # rows at any stride; a single column, or a single row, has no stride of its own to look at
@@ -183,6 +187,9 @@ def quantise_both(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor]
 def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """The values of a packed matrix."""
     rows, cols, device = p.rows, p.cols, p.device
+    if device.index != _current_device():
+        with B._on(device.index):
+            return dequantise(p, dtype)
     out = torch.empty(rows, cols, dtype=dtype, device=device)
     if rows and cols:
         status = B.lib().ssgd_fp4_dequantise_block(_pack_dequantise(
@@ -197,6 +204,9 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optio
     fmt, k, device = a.fmt, a.cols, a.device
     if fmt != b.fmt or k != b.cols or device != b.device:
         raise ValueError("a product needs operands of one format, one length and one device: got %s x %d and %s x %d" % (fmt, k, b.fmt, b.cols))
+    if device.index != _current_device():
+        with B._on(device.index):
+            return matmul(a, b, dtype, out)
     rows, cols = a.rows, b.rows
     ldo = cols or 1
     if out is None:

@@ -75,3 +75,92 @@ def test_an_empty_maximum_or_tensor_scale_is_refused(fp4, B, monkeypatch):
     for a, b, name in ((none, None, "a_tensor_scale"), (ts, none, "b_tensor_scale")):
         with pytest.raises(ValueError, match=name + " holds 0"):
             B.fp4_matmul(codes, scales, a, codes, scales, b, 4, 4, 64, "nv", Standin(4, 4), 4, Standin(1, dtype=torch.int32), 0)
+
+
+class Devices:
+    """Stands in for the runtime: the current device, a device's stream, and what the library was called with on which device."""
+
+    def __init__(self, fp4, B, monkeypatch):
+        self.current, self.calls = 0, []
+        outer = self
+
+        class Switch:
+            def __init__(self, index):
+                self.index = index
+
+            def __enter__(self):
+                self.before, outer.current = outer.current, self.index
+
+            def __exit__(self, *exc):
+                outer.current = self.before
+
+        class Library:
+            def __getattr__(self, name):
+                def call(*args):
+                    if name == "ssgd_fp4_scale_bytes":
+                        return 512
+                    words = args
+                    if name.endswith("_block"):
+                        pack = {"ssgd_fp4_quantise_block": B.FP4_QUANTISE_ARGS, "ssgd_fp4_dequantise_block": B.FP4_DEQUANTISE_ARGS,
+                                "ssgd_fp4_matmul_block": B.FP4_MATMUL_ARGS, "ssgd_tensors_clip_block": B._CLIP_ARGS}[name]
+                        words = pack.unpack(args[0])
+                    outer.calls.append((name, outer.current, words[-1]))
+                    return 0
+                return call
+
+        monkeypatch.setattr(torch.cuda, "device", Switch)
+        monkeypatch.setattr(B, "_current_device", lambda: outer.current, raising=False)
+        monkeypatch.setattr(fp4, "_current_device", lambda: outer.current, raising=False)
+        monkeypatch.setattr(B, "lib", lambda: Library())
+        monkeypatch.setattr(B, "_ptr", lambda t, *a: None if t is None else t.data_ptr())
+        monkeypatch.setattr(B, "_typed_ptr", lambda t, *a: t.data_ptr())
+        monkeypatch.setattr(B, "_stream_of", lambda index: 1000 + index)
+        monkeypatch.setattr(fp4, "_stream_of", lambda index: 1000 + index)
+        monkeypatch.setattr(B, "_stream", lambda stream: 1000 + outer.current if stream is None else stream)
+        monkeypatch.setattr(torch, "empty", lambda *s, dtype=F32, device=None: Standin(*s, dtype=dtype, index=device.index))
+        for i in (0, 1):
+            monkeypatch.setitem(fp4._status, torch.device("cuda", i), (None, 0x7000))
+
+
+def test_calls_run_on_their_operands_device(fp4, B, monkeypatch):
+    """With device 0 current, operands on device 1: that device is current when the library is called, with its stream, and 0 again
+    afterwards."""
+    d = Devices(fp4, B, monkeypatch)
+    for index in (1, 0):
+        at = {"index": index}
+        x = Standin(64, 96, **at)
+        p = fp4.quantise(x, "nv", Standin(1, **at))
+        fp4.quantise_columns(x)
+        fp4.quantise_both(x, "nv")
+        fp4.dequantise(p)
+        fp4.matmul(p, p)
+        u8 = Standin(1 << 16, dtype=U8, **at)
+        B.fp4_quantise(x, 64, 96, 96, "mx", None, None, u8, u8, None, None)
+        B.fp4_dequantise(u8, u8, None, "mx", 64, 96, x, 96)
+        B.fp4_matmul(u8, u8, None, u8, u8, None, 64, 64, 96, "mx", Standin(64, 64, **at), 64, Standin(1, **at))
+        table = object.__new__(B.TensorTable)
+        table.workers, table.device, table._index, table._args, table._ws = 1, torch.device("cuda", index), index, (0x1000, 1, 1), 0x2000
+        B.tensors_norm(table, Standin(1, **at))
+        B.tensors_clip(table, 1.0, Standin(1, **at))
+        names = {c[0] for c in d.calls}
+        assert len(d.calls) == 10 and len(names) == 8 and d.current == 0
+        assert all(c[1:] == (index, 1000 + index) for c in d.calls), d.calls
+        d.calls.clear()
+
+
+def test_operands_of_two_devices_are_refused(fp4, B, monkeypatch):
+    d = Devices(fp4, B, monkeypatch)
+    x, other, u8, elsewhere = Standin(64, 96), Standin(4, index=1), Standin(1 << 16, dtype=U8), Standin(1 << 16, dtype=U8, index=1)
+    table = object.__new__(B.TensorTable)
+    table.workers, table.device, table._index, table._args, table._ws = 1, torch.device("cuda", 0), 0, (0x1000, 1, 1), 0x2000
+    for call in (lambda: fp4.quantise(x, "nv", other), lambda: B.tensors_norm(table, other), lambda: B.tensors_clip(table, 1.0, other),
+                 lambda: B.fp4_quantise(x, 64, 96, 96, "nv", other, Standin(4), u8, u8, None, None),
+                 lambda: B.fp4_quantise(x, 64, 96, 96, "mx", None, None, u8, elsewhere, None, None),
+                 lambda: B.fp4_quantise(x, 64, 96, 96, "mx", None, None, None, None, elsewhere, u8),
+                 lambda: B.fp4_dequantise(u8, u8, other, "nv", 64, 96, x, 96),
+                 lambda: B.fp4_dequantise(elsewhere, elsewhere, None, "mx", 64, 96, x, 96),
+                 lambda: B.fp4_matmul(u8, u8, None, elsewhere, u8, None, 64, 64, 96, "mx", Standin(64, 64), 64, Standin(1)),
+                 lambda: B.fp4_matmul(u8, u8, None, u8, u8, None, 64, 64, 96, "mx", Standin(64, 64), 64, other)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    assert d.calls == []
