@@ -98,6 +98,25 @@ struct ProductArgs {
   unsigned starve;        // bytes that a stage waits for in vain: 0 but in the self-test of the waits
 };
 
+// The tensor scales of both operands.  Powers of two up to 2^120 either way, so their product may leave fp32's range where the
+// result does not, or is an exact zero: then they multiply one after the other.  Both are large, or both small, in that
+// case, so that the first multiplication does not leave the range unless the result does; where their product is in range
+// that would not be so (2^117 and 2^-100).  The second multiplication of all results would cost 8 % of a product that writes
+// much (8192 x 8192 x 256 to bf16 25.3 -> 27.5 us), so the first is a branch that is hardly ever taken (25.5, nv 25.8 us).
+struct TensorScales { float first, last; };
+__device__ __forceinline__ TensorScales tensor_scales(const float* a, const float* b) {
+  const float ta = a ? __ldg(a) : 1.0f, tb = b ? __ldg(b) : 1.0f, both = ta * tb;
+  const bool in_range = fabsf(both) >= 1.175494351e-38f && fabsf(both) <= 3.402823466e38f;
+  return in_range ? TensorScales{1.0f, both} : TensorScales{ta, tb};
+}
+// 32 accumulators times the first of them.
+__device__ __forceinline__ void scale_first(unsigned (&v)[32], const TensorScales& t) {
+  if (__builtin_expect(t.first != 1.0f, 0)) {
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * t.first);
+  }
+}
+
 // 32 accumulators of one lane to a column of out (rows of stride ldo), `left` of them wanted.
 template <typename T>
 __device__ __forceinline__ void store_column(T* o, size_t ldo, const unsigned (&v)[32], unsigned left, float ts) {
@@ -197,7 +216,7 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
     tcgen05_fence_after();
     const unsigned quarter = warp & 3u, j = j0 + quarter * 32 + lane;
     const unsigned lanes = tmem + (quarter << 21);
-    const float ts = (p.a_ts ? __ldg(p.a_ts) : 1.0f) * (p.b_ts ? __ldg(p.b_ts) : 1.0f);
+    const TensorScales ts = tensor_scales(p.a_ts, p.b_ts);
     float* partial = reinterpret_cast<float*>(stage_mem);       // [NT][128]; the stages are used up by now
     if (ok) {
 #pragma unroll 1
@@ -207,7 +226,8 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
         tmem_read32(lanes + c, v);                              // at NT = 16 the columns from 16 on are other data, not wanted
         const unsigned left = min((unsigned)NT - c, p.M - (i0 + c));
         if (splits == 1) {
-          if (j < p.N) store_column(static_cast<T*>(p.out) + (size_t)(i0 + c) * p.ldo + j, p.ldo, v, left, ts);
+          scale_first(v, ts);
+          if (j < p.N) store_column(static_cast<T*>(p.out) + (size_t)(i0 + c) * p.ldo + j, p.ldo, v, left, ts.last);
         } else {
 #pragma unroll
           for (unsigned q = 0; q < 32; ++q)
@@ -233,7 +253,7 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
     __syncwarp();
     cluster.sync();
     // this CTA's columns are split, split + splits, ...: four rows of one column to a thread, all ranks' loads in flight
-    const float ts = (p.a_ts ? __ldg(p.a_ts) : 1.0f) * (p.b_ts ? __ldg(p.b_ts) : 1.0f);
+    const TensorScales ts = tensor_scales(p.a_ts, p.b_ts);
     const unsigned columns = min((unsigned)NT, p.M - i0);
     for (unsigned i = threadIdx.x; split + i / 32 * splits < columns; i += kMmaThreads) {
       const unsigned c = split + i / 32 * splits, row = i % 32 * 4, j = j0 + row;
@@ -247,10 +267,10 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
         if (r < splits) sum = make_float4(sum.x + v[r].x, sum.y + v[r].y, sum.z + v[r].z, sum.w + v[r].w);
       const size_t at = (size_t)(i0 + c) * p.ldo + j;
       T* o = static_cast<T*>(p.out) + at;
-      if (j < p.N) o[0] = from_float<T>(sum.x * ts);
-      if (j + 1 < p.N) o[1] = from_float<T>(sum.y * ts);
-      if (j + 2 < p.N) o[2] = from_float<T>(sum.z * ts);
-      if (j + 3 < p.N) o[3] = from_float<T>(sum.w * ts);
+      if (j < p.N) o[0] = from_float<T>(sum.x * ts.first * ts.last);
+      if (j + 1 < p.N) o[1] = from_float<T>(sum.y * ts.first * ts.last);
+      if (j + 2 < p.N) o[2] = from_float<T>(sum.z * ts.first * ts.last);
+      if (j + 3 < p.N) o[3] = from_float<T>(sum.w * ts.first * ts.last);
     }
     __syncwarp();
     cluster.sync();                             // nobody leaves while its shared memory is still read
@@ -428,7 +448,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
     // Two warps share a quarter of the lanes, units of kUnit columns in turn.
     constexpr unsigned kUnit = 32, kUnits = NT / kUnit, kSharedUnits = (NT - S::second) / kUnit;
     const unsigned quarter = warp & 3u, odd = warp >= 6;
-    const float ts = (p.p_ts ? __ldg(p.p_ts) : 1.0f) * (p.q_ts ? __ldg(p.q_ts) : 1.0f);
+    const TensorScales ts = tensor_scales(p.p_ts, p.q_ts);
     const unsigned go = cluster_address(acc_free, 0), box = stage0 + S::stages * S::stage_bytes + (warp - 2) * S::box_bytes;
     unsigned t = 0;
     for (unsigned tile = pair; tile < tiles; tile += pairs, ++t) {
@@ -452,18 +472,19 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
           if (lane == 0) mbarrier_arrive_cluster(go);
         }
         if (row0 < p.P && q0 + c < p.Q) {
+          scale_first(v, ts);
           if constexpr (WIDE) {
             if (lane == 0) tma_store_wait_read();                                      // the box is free again
             __syncwarp();
             if constexpr (sizeof(T) == 2) {                                            // rows of 64 bytes, 64-byte swizzle
 #pragma unroll
-              for (unsigned q = 0; q < 16; ++q) v[q] = pack2(T(), __uint_as_float(v[2 * q]) * ts, __uint_as_float(v[2 * q + 1]) * ts);
+              for (unsigned q = 0; q < 16; ++q) v[q] = pack2(T(), __uint_as_float(v[2 * q]) * ts.last, __uint_as_float(v[2 * q + 1]) * ts.last);
 #pragma unroll
               for (unsigned q = 0; q < 4; ++q)
                 store_shared16(box + lane * 64 + ((q ^ (lane >> 1 & 3u)) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
             } else {                                                                   // rows of 128 bytes, 128-byte swizzle
 #pragma unroll
-              for (unsigned q = 0; q < 32; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * ts);
+              for (unsigned q = 0; q < 32; ++q) v[q] = __float_as_uint(__uint_as_float(v[q]) * ts.last);
 #pragma unroll
               for (unsigned q = 0; q < 8; ++q)
                 store_shared16(box + lane * 128 + ((q ^ (lane & 7u)) << 4), v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
@@ -472,7 +493,7 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
             __syncwarp();
             if (lane == 0) tma_store_2d(&out_map, (int)(q0 + c), (int)row0, box);
           } else if (row0 + lane < p.P) {
-            store_column(static_cast<T*>(p.out) + (size_t)(q0 + c) * p.ldo + row0 + lane, p.ldo, v, min(32u, p.Q - (q0 + c)), ts);
+            store_column(static_cast<T*>(p.out) + (size_t)(q0 + c) * p.ldo + row0 + lane, p.ldo, v, min(32u, p.Q - (q0 + c)), ts.last);
           }
         }
         __syncwarp();

@@ -58,3 +58,38 @@ def test_largest_value_in_the_last_columns_of_a_slice(fp4, rows, cols, width, dt
                 assert np.array_equal(p.codes.cpu().numpy(), ref.pack_codes(want[0]))
                 assert np.array_equal(p.scales.cpu().numpy(), ref.pack_scales(want[1]))
         x.copy_(y)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# tensor scales at the ends of their range
+
+
+def constant(fp4, rows, K, code, byte, scale, zero_row=None):
+    """An nv operand of one code and one scale byte, one row of it zeros."""
+    c = np.full((rows, K), code, dtype=np.uint8)
+    if zero_row is not None:
+        c[zero_row] = 0
+    b = np.full((rows, K // 16), byte, dtype=np.uint8)
+    return fp4.Packed(torch.from_numpy(ref.pack_codes(c)).cuda(), torch.from_numpy(ref.pack_scales(b)).cuda(),
+                      torch.tensor([scale], device="cuda"), rows, K, "nv")
+
+
+@pytest.mark.parametrize("M,N,K,ldo", [(3, 40, 512, 40), (3, 40, 4096, 40), (200, 300, 512, 301), (200, 300, 512, 304), (150, 300, 8192, 300)])
+@pytest.mark.parametrize("ta,tb", [(100, 60), (60, 117), (-80, -70), (-100, -60), (117, -100), (-100, 117), (-90, 117), (64, 64), (-63, -64)])
+@pytest.mark.parametrize("code", [2, 7])
+def test_product_of_extreme_tensor_scales(fp4, M, N, K, ldo, ta, tb, code):
+    """Sums that are exact in fp32, so the result is the formula's, rounded once: infinity or a subnormal where it has to be, and
+    zeros stay zeros."""
+    for byte in (0x38, 0x7E):                                  # 1 and 448
+        a, b = constant(fp4, M, K, code, byte, 2.0 ** ta, zero_row=1), constant(fp4, N, K, code, byte, 2.0 ** tb)
+        value = ref.LEVELS[code] * ref.E4M3[byte]
+        exact = value * value * K                              # an integer of at most 24 bits times a power of two
+        with np.errstate(over="ignore"):
+            want = np.float32(exact * 2.0 ** (ta + tb))        # exact in 64 bits before
+        for dtype in (F32, BF16):
+            out = torch.empty(M, ldo, dtype=dtype, device="cuda")[:, :N]
+            fp4.matmul(a, b, out=out)
+            expected = torch.full((M, N), float(want), device="cuda").to(dtype)
+            expected[1] = 0
+            assert torch.equal(out, expected), (byte, dtype, out[0, 0].item(), float(want))
+    fp4.check()
