@@ -432,7 +432,7 @@ size_t ssgd_fp4_scale_bytes(int format, size_t rows, size_t cols); /* 0 for a ba
  *   code = the value nearest to x / S (fp32 quotient), ties to the even code, magnitudes above 6 to 6.  A block with
  *   an infinity or a NaN has the NaN scale and reads back as NaN.
  *   amax          in   DEVICE float, nv only: max |x| of the operand, or NULL: the call finds it
- *   tensor_scale  out  DEVICE, nv only (may be NULL for mx): [0] = t; [1] = the amax found when amax is NULL.  float[2];
+ *   tensor_scale  out  DEVICE, nv only (not written for mx): [0] = t; [1] = the amax found when amax is NULL.  float[2];
  *                      float[SSGD_FP4_SCALE_FLOATS], the rest being workspace, when amax is NULL and the matrix has more
  *                      than SSGD_FP4_SMALL elements                                                                 */
 ssgd_status ssgd_fp4_quantise(const void* x, int dtype, size_t rows, size_t cols, size_t ldx, int format,
@@ -440,7 +440,8 @@ ssgd_status ssgd_fp4_quantise(const void* x, int dtype, size_t rows, size_t cols
                               uint8_t* codes_t, uint8_t* scales_t, void* stream);
 
 /* The values of a packed operand: out[r][c] = code * S, rounded once to dtype.
- *   tensor_scale in DEVICE float or NULL (1);  out DEVICE [rows][ldo], ldo >= cols, aligned to its element           */
+ *   tensor_scale in DEVICE float or NULL (1); nv only, not read for mx
+ *   out          out DEVICE [rows][ldo], ldo >= cols, aligned to its element                                          */
 ssgd_status ssgd_fp4_dequantise(const uint8_t* codes, const uint8_t* scales, const float* tensor_scale, int format,
                                 size_t rows, size_t cols, void* out, int dtype, size_t ldo, void* stream);
 
@@ -448,7 +449,7 @@ ssgd_status ssgd_fp4_dequantise(const uint8_t* codes, const uint8_t* scales, con
  *   out[i][j] = tA tB sum_k A[i][k] B[j][k]      (fp32 accumulation, rounded once to dtype; K = 0 gives 0)
  * A layer's forward product is y = x w^T (A = x, B = w by rows); its backward products take the packed transposes:
  * dx = dy w (A = dy by rows, B = w by columns), dw = dy^T x (A = dy by columns, B = x by columns).
- *   a_tensor_scale, b_tensor_scale  in DEVICE float or NULL (1)
+ *   a_tensor_scale, b_tensor_scale  in DEVICE float or NULL (1); nv only: NULL for mx (SSGD_ERR_ARG)
  *   out     out DEVICE [M][ldo] of dtype, ldo >= N, aligned to its element
  *   status  in/out DEVICE unsigned, 0 before the first call: every wait in the kernel has an iteration limit, and a
  *           block whose operands do not arrive within it sets bit 0 here and gives up its part of out; it stays 0 in

@@ -744,6 +744,7 @@ ssgd_status checked_product(const uint8_t* a_codes, const uint8_t* a_scales, con
       reinterpret_cast<uintptr_t>(out) % dtype_bytes((unsigned)dtype) != 0 ||
       ((reinterpret_cast<uintptr_t>(a_tensor_scale) | reinterpret_cast<uintptr_t>(b_tensor_scale) | reinterpret_cast<uintptr_t>(status)) & 3u))
     return SSGD_ERR_ALIGN;
+  if (format == SSGD_MXFP4 && (a_tensor_scale || b_tensor_scale)) return SSGD_ERR_ARG;
   if (M == 0 || N == 0) return SSGD_OK;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (K == 0) {

@@ -26,7 +26,7 @@ class Packed:
 
     codes          uint8 [rows][row bytes], contiguous
     scales         uint8, tiles of 128 rows x 4 blocks, contiguous
-    tensor_scale   float32, its first element (None: 1)
+    tensor_scale   float32, its first element (None: 1); "nv" only
 
     Its three parts may lie in one buffer, as `quantise` makes them; they are cut out of it when they are asked for."""
     __slots__ = ("rows", "cols", "fmt", "device", "pointers", "_parts", "_buffer")      # _buffer: (buffer, byte offsets of the parts)
@@ -34,6 +34,8 @@ class Packed:
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Optional[torch.Tensor], rows: int, cols: int, fmt: str):
         if fmt not in _BLOCK:
             raise ValueError("fmt must be 'mx' or 'nv'")
+        if fmt == "mx" and tensor_scale is not None:
+            raise ValueError("the mx format has no tensor scale")
         if codes.dtype != _U8 or scales.dtype != _U8 or (tensor_scale is not None and tensor_scale.dtype != torch.float32):
             raise TypeError("codes and scales must be uint8 tensors, tensor_scale a float32 one")
         device = codes.device

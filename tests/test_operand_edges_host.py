@@ -164,3 +164,18 @@ def test_operands_of_two_devices_are_refused(fp4, B, monkeypatch):
         with pytest.raises(ValueError, match="device"):
             call()
     assert d.calls == []
+
+
+def test_mx_has_no_tensor_scale(fp4, B):
+    """Values of the mx format have a block scale alone: a product used to multiply by a tensor scale that reading back left out."""
+    codes, scales, ts = Standin(64, dtype=U8), Standin(512, dtype=U8), Standin(1)
+    with pytest.raises(ValueError, match="mx"):
+        fp4.Packed(codes, scales, ts, 4, 32, "mx")
+    assert fp4.Packed(codes, scales, None, 4, 32, "mx").tensor_scale is None
+    assert fp4.Packed(codes, scales, ts, 4, 32, "nv").tensor_scale is ts
+    A, OK, ARG = 0x10000, 0, 4
+    f = B.lib().ssgd_fp4_matmul
+    for a, b in ((A, None), (None, A), (A, A)):
+        assert f(A, A, a, A, A, b, 4, 8, 64, 0, A, 1, 8, A, None) == ARG
+        assert f(A, A, a, A, A, b, 0, 8, 64, 0, A, 1, 8, A, None) == ARG
+    assert f(A, A, A, A, A, A, 0, 8, 64, 1, A, 1, 8, A, None) == OK and f(A, A, None, A, A, None, 0, 8, 64, 0, A, 1, 8, A, None) == OK
