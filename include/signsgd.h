@@ -452,8 +452,8 @@ ssgd_status ssgd_fp4_dequantise(const uint8_t* codes, const uint8_t* scales, con
  *   a_tensor_scale, b_tensor_scale  in DEVICE float or NULL (1); nv only: NULL for mx (SSGD_ERR_ARG)
  *   out     out DEVICE [M][ldo] of dtype, ldo >= N, aligned to its element
  *   status  in/out DEVICE unsigned, 0 before the first call: every wait in the kernel has an iteration limit, and a
- *           block whose operands do not arrive within it sets bit 0 here and gives up its part of out; it stays 0 in
- *           normal operation                                                                                         */
+ *           block whose operands do not arrive within it sets bit 0 here and gives up its part of out, and so do the
+ *           blocks that share its tile; it stays 0 in normal operation                                                */
 ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_tensor_scale,
                             const uint8_t* b_codes, const uint8_t* b_scales, const float* b_tensor_scale, size_t M,
                             size_t N, size_t K, int format, void* out, int dtype, size_t ldo, unsigned* status,
@@ -461,7 +461,8 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
 
 /* Self-test of the bounded waits of ssgd_fp4_matmul: the same launch with every stage armed for more bytes than its copies
  * deliver (all copies still complete).  The kernel must return within its limits (a few seconds) with bit 0 of *status
- * set and `out` untouched; the context stays usable.  M, N <= 256, K <= 512.                                            */
+ * set and `out` untouched; the context stays usable.  M, N <= 256; K <= 4096 where M <= 128 (a long k is split over a
+ * cluster), else 512.                                                                                                   */
 ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes,
                                           const uint8_t* b_scales, size_t M, size_t N, size_t K, int format, void* out,
                                           int dtype, size_t ldo, unsigned* status, void* stream);

@@ -33,6 +33,9 @@ namespace {
 constexpr int kMmaThreads = 320;            // copies, MMAs, eight warps that write out
 constexpr unsigned kTileJ = 128;            // rows of B in a tile: lanes of the accumulator
 constexpr unsigned kPolls = 200000;         // bound of a wait, about 0.2 s
+// Bits of a partial sum that a CTA could not finish: a NaN that no arithmetic makes, looked for where the cluster's sum is NaN.
+// (A flag of each CTA, asked for through the cluster's shared memory, costs 0.2 us of a split product's 4 us, this 0.05.)
+constexpr unsigned kGivenUp = 0x7FC0DEADu;
 
 // One stage's tensor-core work: its scales to tensor memory (4 columns for each tile of 128 rows x 4 blocks: the lanes'
 // operand first, then for each four blocks the columns' operand's row tiles side by side), then up to four MMAs of 64 of k.
@@ -241,13 +244,15 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
   __syncwarp();
   __syncthreads();
   if (failed) {
-    // copies that were asked for have to land before the CTA gives its memory up
     if (threadIdx.x == 0) atomicOr(p.status, 1u);
+    // copies that were asked for have to land before the CTA gives its memory up
     if (issued > 0) {
       for (unsigned n = issued > S::stages ? issued - S::stages : 0; n < issued; ++n)
         (void)mbarrier_wait(full + 8 * (n % S::stages), (n / S::stages) & 1u, kPolls);
     }
     __syncthreads();
+    // a tile that one CTA gives up is given up by its cluster: the others' sums would not be sums of all of k
+    for (unsigned i = threadIdx.x; splits > 1 && i < NT * kTileJ; i += kMmaThreads) reinterpret_cast<unsigned*>(stage_mem)[i] = kGivenUp;
   }
   if (splits > 1) {
     __syncwarp();
@@ -265,6 +270,12 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
 #pragma unroll
       for (unsigned r = 1; r < 8; ++r)
         if (r < splits) sum = make_float4(sum.x + v[r].x, sum.y + v[r].y, sum.z + v[r].z, sum.w + v[r].w);
+      if (__builtin_expect(sum.x != sum.x, 0)) {
+        bool given_up = false;
+        for (unsigned r = 0; r < splits; ++r)
+          given_up |= *cluster.map_shared_rank(reinterpret_cast<unsigned*>(stage_mem) + c * kTileJ + row, r) == kGivenUp;
+        if (given_up) continue;
+      }
       const size_t at = (size_t)(i0 + c) * p.ldo + j;
       T* o = static_cast<T*>(p.out) + at;
       if (j < p.N) o[0] = from_float<T>(sum.x * ts.first * ts.last);
@@ -769,7 +780,8 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
 
 ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, size_t M,
                                           size_t N, size_t K, int format, void* out, int dtype, size_t ldo, unsigned* status, void* stream) {
-  if (M > 256 || N > 256 || K > 512) return SSGD_ERR_SIZE;      // one tile, two stages: the waits run out once
+  // one tile of a pair, two stages, or a few tiles whose k may be split: the waits run out once
+  if (M > 256 || N > 256 || K > (M <= 128 ? 4096 : 512)) return SSGD_ERR_SIZE;
   return checked_product(a_codes, a_scales, nullptr, b_codes, b_scales, nullptr, M, N, K, format, out, dtype, ldo, status, 16, stream);
 }
 

@@ -93,3 +93,31 @@ def test_product_of_extreme_tensor_scales(fp4, M, N, K, ldo, ta, tb, code):
             expected[1] = 0
             assert torch.equal(out, expected), (byte, dtype, out[0, 0].item(), float(want))
     fp4.check()
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# waits that run out where k is split over a cluster
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,N", [(5, 100), (40, 250), (128, 256)])
+def test_waits_of_a_split_product_run_out(fp4, B, fmt, M, N):
+    """k is split over a cluster of eight: nobody adds up what its neighbours did not finish, `out` stays as it was."""
+    K = 4096
+    a, b = fp4.quantise(randn(M, K, seed=1), fmt), fp4.quantise(randn(N, K, seed=2), fmt)
+    want = fp4.matmul(a, b, F32)
+    out, status = torch.full((M, N), 7.0, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    st = B.lib().ssgd_fp4_matmul_wait_selftest(a.pointers[0], a.pointers[1], b.pointers[0], b.pointers[1], M, N, K, B.FP4_FORMAT[fmt],
+                                               out.data_ptr(), 0, N, status.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    torch.cuda.synchronize()
+    assert status.item() == 1 and bool((out == 7.0).all())
+    assert torch.equal(fp4.matmul(a, b, F32), want)
+    fp4.check()
+
+
+def test_waits_selftest_refuses_large_products(B):
+    A, SIZE = 0x10000, 3
+    f = B.lib().ssgd_fp4_matmul_wait_selftest
+    for M, N, K in ((257, 8, 64), (8, 257, 64), (8, 8, 4097), (129, 8, 513)):
+        assert f(A, A, A, A, M, N, K, 0, A, 0, N, A, None) == SIZE
