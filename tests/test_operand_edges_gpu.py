@@ -121,3 +121,21 @@ def test_waits_selftest_refuses_large_products(B):
     f = B.lib().ssgd_fp4_matmul_wait_selftest
     for M, N, K in ((257, 8, 64), (8, 257, 64), (8, 8, 4097), (129, 8, 513)):
         assert f(A, A, A, A, M, N, K, 0, A, 0, N, A, None) == SIZE
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# norms
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("repeats", [1, 1000, 200_000])
+@pytest.mark.parametrize("pattern", [[1.0] + [2.0 ** -12] * 7, [2.0 ** -12] * 7 + [1.0], [1.0, 2.0 ** -12, 2.0 ** -12, 2.0 ** -12] * 2,
+                                     [1.0, 0.0, 2.0 ** -12, 0.0, 2.0 ** -12, 0.0, 2.0 ** -12, 0.0], [0.0, 1.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0]])
+def test_norm_of_16_bit_squares_that_differ_in_size(B, dtype, repeats, pattern):
+    """Squares of 2^-24 next to squares of 1: an fp32 sum of many drops them, always to the same side."""
+    x = torch.tensor(pattern, dtype=dtype, device="cuda").repeat(repeats)
+    norms = torch.zeros(1, device="cuda")
+    B.tensors_norm(B.TensorTable([x]), norms)
+    want = math.sqrt(repeats * sum(v * v for v in pattern))
+    # 2^-24 for the fours in fp32 (two roundings of a sum of squares are half of that in its root), 2^-24 for the norm's own
+    assert abs(norms.item() - want) <= 2.0 ** -23 * want
