@@ -396,9 +396,9 @@ ssgd_status ssgd_tensors_norm(const void* table, size_t tiles, size_t groups, in
 
 /* ssgd_tensors_norm, then for every tensor with a dst
  *   dst <- c * src,  c = max_norm / norm where norm > max_norm, else 1     (one fp32 rounding, one to dst's type)
- * max_norm >= 0; infinity: no clipping, only the copy.  A norm that is not finite: with zero_nonfinite != 0 that
- * group's dst becomes 0, so that a broken gradient does not enter the momentum; else c is what the formula gives
- * (0 for infinity, NaN for NaN).                                                                                    */
+ * max_norm >= 0; infinity: no clipping, c = 1 whatever the norm.  A norm that is not finite: with zero_nonfinite != 0
+ * that group's dst becomes 0, so that a broken gradient does not enter the momentum; else c is 0 for infinity and NaN
+ * for NaN where max_norm is finite.                                                                                 */
 ssgd_status ssgd_tensors_clip(const void* table, size_t tiles, size_t groups, int kind, float max_norm,
                               int zero_nonfinite, void* ws, float* norms, void* stream);
 

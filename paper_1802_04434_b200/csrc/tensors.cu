@@ -168,10 +168,11 @@ norms_finish_kernel(const uint64_t* __restrict__ first_tile, const double* __res
   if (threadIdx.x == 0) norms[blockIdx.x] = finish_norm<KIND>(s);
 }
 
-// c of one group, and whether its rows are zeroed instead (norm not finite, when the caller asked for that).
+// c of one group, and whether its rows are zeroed instead (norm not finite, when the caller asked for that).  No clipping is a
+// copy, whatever the norm.
 __device__ __forceinline__ float clip_factor(float norm, float max_norm, int zero_nonfinite, bool* zero) {
   *zero = zero_nonfinite && !(norm <= 3.402823466e38f);
-  return norm > max_norm ? __fdiv_rn(max_norm, norm) : (norm == norm ? 1.0f : norm);
+  return norm > max_norm ? __fdiv_rn(max_norm, norm) : (norm == norm || isinf(max_norm) ? 1.0f : norm);
 }
 
 // Four elements of a lane at a time where source and destination both allow it, BATCH of them in flight, else element by

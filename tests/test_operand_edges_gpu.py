@@ -139,3 +139,19 @@ def test_norm_of_16_bit_squares_that_differ_in_size(B, dtype, repeats, pattern):
     want = math.sqrt(repeats * sum(v * v for v in pattern))
     # 2^-24 for the fours in fp32 (two roundings of a sum of squares are half of that in its root), 2^-24 for the norm's own
     assert abs(norms.item() - want) <= 2.0 ** -23 * want
+
+
+@pytest.mark.parametrize("n", [1000, 600_000])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("kind", ["two", "max"])
+def test_no_clipping_is_a_copy_whatever_the_norm(B, n, bad, kind):
+    x = randn(n, seed=7)
+    x[n // 3] = bad
+    out, same, norms = torch.zeros_like(x), x.clone(), torch.zeros(1, device="cuda")
+    B.tensors_clip(B.TensorTable([x], [out]), math.inf, norms, kind)
+    # 1 * NaN is a NaN, of which payload is not said
+    assert torch.equal(out.isnan(), x.isnan()) and torch.equal(out.nan_to_num(0.0), x.nan_to_num(0.0)) and not math.isfinite(norms.item())
+    B.tensors_clip(B.TensorTable([same], [same]), math.inf, norms, kind)
+    assert torch.equal(same.view(torch.int32), x.view(torch.int32))
+    B.tensors_clip(B.TensorTable([x], [out]), math.inf, norms, kind, zero_nonfinite=True)
+    assert bool((out == 0).all())
