@@ -440,7 +440,8 @@ class TensorTable:
             altogether: norm only); a tensor of `src` itself: in place.  Slices of a worker's flat row are the usual ones
     groups  the worker of each tensor, not descending; None: all belong to worker 0
 
-    The table keeps the tensors alive and holds for as long as they stay where they are."""
+    The table keeps the tensors alive and holds for as long as they stay where they are.  Its calls share one workspace: they go
+    to one stream, or wait for one another; for calls that may run at the same time build a table each."""
 
     def __init__(self, src, dst=None, groups=None, workers: Optional[int] = None):
         src = list(src)
@@ -478,7 +479,7 @@ class TensorTable:
         _check(lib().ssgd_table_build(entries, len(src), self.workers, host.data_ptr(), nbytes.value), "ssgd_table_build")
         self.tiles = tiles.value
         self.table = host.to(self.device)
-        self.ws = torch.zeros(ws.value, dtype=torch.uint8, device=self.device)
+        self.ws = torch.empty(ws.value, dtype=torch.uint8, device=self.device)      # not filled: nothing is pending when this returns
         self._keep = (src, dst)
         self._index = self.device.index
         self._args = (self.table.data_ptr(), self.tiles, self.workers)

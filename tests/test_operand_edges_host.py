@@ -179,3 +179,34 @@ def test_mx_has_no_tensor_scale(fp4, B):
         assert f(A, A, a, A, A, b, 4, 8, 64, 0, A, 1, 8, A, None) == ARG
         assert f(A, A, a, A, A, b, 0, 8, 64, 0, A, 1, 8, A, None) == ARG
     assert f(A, A, A, A, A, A, 0, 8, 64, 1, A, 1, 8, A, None) == OK and f(A, A, None, A, A, None, 0, 8, 64, 0, A, 1, 8, A, None) == OK
+
+
+class OnDevice(torch.Tensor):
+    """A host tensor that says it lives on device 0."""
+    device = property(lambda self: torch.device("cuda", 0))
+
+    def get_device(self):
+        return 0
+
+
+def on_device(*shape):
+    return torch.zeros(*shape).as_subclass(OnDevice)
+
+
+def test_a_table_leaves_no_work_pending_on_its_stream(B, monkeypatch):
+    """The workspace is not filled: the fill would be pending on the stream that builds the table, and could clear the partial sums of
+    a call on another."""
+    made = []
+
+    def make(name, real):
+        def f(*shape, device=None, **k):
+            if device is not None and torch.device(device).type == "cuda":
+                made.append(name)
+            return real(*shape, **k)
+        return f
+
+    for name in ("zeros", "ones", "full", "empty"):
+        monkeypatch.setattr(torch, name, make(name, getattr(torch, name)))
+    monkeypatch.setattr(torch.Tensor, "to", lambda self, *a, **k: self)
+    table = B.TensorTable([on_device(5), on_device(9000)], [on_device(5), None], [0, 1])
+    assert made == ["empty"] and table.ws.numel() == 32 and table.tiles == 3
