@@ -251,6 +251,19 @@ def linear_backward(kept: Kept, dy: torch.Tensor, dw: Optional[torch.Tensor] = N
     return matmul(dr, kept.w_columns, kept.dtype), matmul(dc, kept.x_columns, dw_dtype, dw)
 
 
+class _Once(torch.autograd.Function):
+    """Passes a gradient on; an error where somebody differentiates it.  (torch's once_differentiable does so only where the gradient
+    that comes in can be differentiated, but dx depends on w, and dw on x, whatever comes in.)"""
+
+    @staticmethod
+    def forward(ctx, gradient, dy):
+        return gradient.view_as(gradient)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("fp4.linear can be differentiated once only: its products' gradients have none of their own")
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, fmt):
@@ -264,6 +277,14 @@ class _Linear(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
+        with torch.no_grad():
+            dx, dw = _Linear._gradients(ctx, dy)
+        if torch.is_grad_enabled():            # create_graph=True
+            dx, dw = [None if g is None else _Once.apply(g.requires_grad_(), dy) for g in (dx, dw)]
+        return dx, dw, None
+
+    @staticmethod
+    def _gradients(ctx, dy):
         kept = ctx.kept
         fmt = (kept.x_columns or kept.w_columns).fmt
         rows = dy.reshape(-1, dy.shape[-1])
@@ -274,12 +295,11 @@ class _Linear(torch.autograd.Function):
         else:
             dr, dc = quantise_both(rows, fmt)
         dx = matmul(dr, kept.w_columns, kept.dtype).view(ctx.x_shape) if dr is not None else None
-        dw = matmul(dc, kept.x_columns, ctx.w_dtype) if dc is not None else None
-        return dx, dw, None
+        return dx, matmul(dc, kept.x_columns, ctx.w_dtype) if dc is not None else None
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, fmt: str = "mx") -> torch.Tensor:
-    """x w^T with all three products in 4 bits, for torch's autograd; x [..., in], w [out][in]."""
+    """x w^T with all three products in 4 bits, for torch's autograd; x [..., in], w [out][in].  First derivatives only."""
     if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
         raise ValueError("x's last side must be w's second: got %s and %s" % (tuple(x.shape), tuple(w.shape)))
     return _Linear.apply(x, w, fmt)

@@ -210,3 +210,58 @@ def test_a_table_leaves_no_work_pending_on_its_stream(B, monkeypatch):
     monkeypatch.setattr(torch.Tensor, "to", lambda self, *a, **k: self)
     table = B.TensorTable([on_device(5), on_device(9000)], [on_device(5), None], [0, 1])
     assert made == ["empty"] and table.ws.numel() == 32 and table.tiles == 3
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# the linear layer with quantisation and product replaced by exact ones on the host
+
+
+@pytest.fixture
+def exact(fp4, monkeypatch):
+    """Packed matrices whose buffer holds the float32 values themselves; what was packed, in order."""
+    packed = []
+
+    def quantise(x, fmt, amax, by_rows, by_columns):
+        assert x.dim() == 2
+        packed.append((tuple(x.shape), by_rows, by_columns))
+        rows, cols = x.shape
+        values = x.detach().float().contiguous()
+        buffer = torch.cat([values.reshape(-1), values.t().reshape(-1)]).view(U8)
+        r = fp4._packed_in(buffer, buffer.data_ptr(), 0, 0, None, rows, cols, fmt, x.device)
+        c = fp4._packed_in(buffer, buffer.data_ptr(), 4 * rows * cols, 0, None, cols, rows, fmt, x.device)
+        return (r, c) if by_rows and by_columns else r if by_rows else c
+
+    def values(p):
+        buffer, (at, _, _) = p._buffer
+        assert p.pointers[0] == buffer.data_ptr() + at
+        return buffer[at:at + 4 * p.rows * p.cols].view(F32).view(p.rows, p.cols)
+
+    def matmul(a, b, dtype=BF16, out=None):
+        assert a.fmt == b.fmt and a.cols == b.cols
+        y = (values(a) @ values(b).t()).to(dtype)
+        return y if out is None else out.copy_(y)
+
+    monkeypatch.setattr(fp4, "_quantise", quantise)
+    monkeypatch.setattr(fp4, "matmul", matmul)
+    return packed
+
+
+def leaf(*shape, seed=0):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return torch.randn(*shape, generator=g).requires_grad_()
+
+
+def test_second_derivatives_of_the_layer_are_an_error(fp4, exact):
+    """They would have been left out in silence: a gradient penalty added to a loss changed nothing."""
+    for loss_of in (lambda y: y.sum(), lambda y: y.square().sum()):            # a gradient of y that depends on nothing, and one that does
+        x, w = leaf(5, 8, seed=1), leaf(3, 8, seed=2)
+        y = fp4.linear(x, w)
+        for wanted in ((x,), (w,), (x, w)):
+            first = torch.autograd.grad(loss_of(y), wanted, create_graph=True)
+            plain = torch.autograd.grad(loss_of(torch.nn.functional.linear(x, w)), wanted)
+            assert all(torch.allclose(a, b, rtol=1e-5, atol=1e-6) for a, b in zip(first, plain))
+            with pytest.raises(RuntimeError, match="once"):
+                (loss_of(y) + sum(g.square().sum() for g in first)).backward(retain_graph=True)
+        loss_of(fp4.linear(x, w)).backward(create_graph=True)                  # first derivatives alone go on as before
+        assert x.grad.shape == x.shape and w.grad.shape == w.shape
