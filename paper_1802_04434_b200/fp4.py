@@ -266,9 +266,10 @@ class _Once(torch.autograd.Function):
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, fmt):
+    def forward(ctx, x, w, fmt, grad):
         rows = x.reshape(-1, x.shape[-1])
-        need_x, need_w = ctx.needs_input_grad[:2]
+        # needs_input_grad says what the inputs want, in whatever mode the call is made
+        need_x, need_w = [grad and need for need in ctx.needs_input_grad[:2]]
         # only what the backward products will want is packed by columns
         xr, xc = quantise_both(rows, fmt) if need_w else (quantise(rows, fmt), None)
         wr, wc = quantise_both(w, fmt) if need_x else (quantise(w, fmt), None)
@@ -281,7 +282,7 @@ class _Linear(torch.autograd.Function):
             dx, dw = _Linear._gradients(ctx, dy)
         if torch.is_grad_enabled():            # create_graph=True
             dx, dw = [None if g is None else _Once.apply(g.requires_grad_(), dy) for g in (dx, dw)]
-        return dx, dw, None
+        return dx, dw, None, None
 
     @staticmethod
     def _gradients(ctx, dy):
@@ -302,4 +303,4 @@ def linear(x: torch.Tensor, w: torch.Tensor, fmt: str = "mx") -> torch.Tensor:
     """x w^T with all three products in 4 bits, for torch's autograd; x [..., in], w [out][in].  First derivatives only."""
     if w.dim() != 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
         raise ValueError("x's last side must be w's second: got %s and %s" % (tuple(x.shape), tuple(w.shape)))
-    return _Linear.apply(x, w, fmt)
+    return _Linear.apply(x, w, fmt, torch.is_grad_enabled())

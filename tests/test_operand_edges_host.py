@@ -265,3 +265,19 @@ def test_second_derivatives_of_the_layer_are_an_error(fp4, exact):
                 (loss_of(y) + sum(g.square().sum() for g in first)).backward(retain_graph=True)
         loss_of(fp4.linear(x, w)).backward(create_graph=True)                  # first derivatives alone go on as before
         assert x.grad.shape == x.shape and w.grad.shape == w.shape
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_without_gradients_only_rows_are_packed(fp4, exact, mode):
+    """Parameters that want gradients, and a call that can have none: nothing is packed for a backward pass."""
+    x, w = leaf(2, 5, 8, seed=1), leaf(3, 8, seed=2)
+    with mode():
+        y = fp4.linear(x, w)
+        assert torch.allclose(y, torch.nn.functional.linear(x, w), rtol=1e-5, atol=1e-6) and not y.requires_grad
+    assert exact == [((10, 8), True, False), ((3, 8), True, False)]
+    del exact[:]
+    fp4.linear(x, w)
+    fp4.linear(x, w.detach())
+    fp4.linear(x.detach(), w)
+    fp4.linear(x.detach(), w.detach())
+    assert [p[2] for p in exact] == [True, True, False, True, True, False, False, False]
