@@ -6,6 +6,7 @@ work is enqueued on the current stream of the operands' device, whichever device
 """
 from __future__ import annotations
 
+import math
 from typing import NamedTuple, Optional, Tuple
 
 import torch
@@ -251,6 +252,11 @@ def linear_backward(kept: Kept, dy: torch.Tensor, dw: Optional[torch.Tensor] = N
     return matmul(dr, kept.w_columns, kept.dtype), matmul(dc, kept.x_columns, dw_dtype, dw)
 
 
+def _rows_of(x: torch.Tensor) -> torch.Tensor:
+    """x [..., n] as a matrix; its sides may be 0, where reshape(-1, n) would not know how many rows there are."""
+    return x.reshape(math.prod(x.shape[:-1]), x.shape[-1])
+
+
 class _Once(torch.autograd.Function):
     """Passes a gradient on; an error where somebody differentiates it.  (torch's once_differentiable does so only where the gradient
     that comes in can be differentiated, but dx depends on w, and dw on x, whatever comes in.)"""
@@ -267,7 +273,7 @@ class _Once(torch.autograd.Function):
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, fmt, grad):
-        rows = x.reshape(-1, x.shape[-1])
+        rows = _rows_of(x)
         # needs_input_grad says what the inputs want, in whatever mode the call is made
         need_x, need_w = [grad and need for need in ctx.needs_input_grad[:2]]
         # only what the backward products will want is packed by columns
@@ -288,7 +294,7 @@ class _Linear(torch.autograd.Function):
     def _gradients(ctx, dy):
         kept = ctx.kept
         fmt = (kept.x_columns or kept.w_columns).fmt
-        rows = dy.reshape(-1, dy.shape[-1])
+        rows = _rows_of(dy)
         if kept.x_columns is None:
             dr, dc = quantise(rows, fmt), None
         elif kept.w_columns is None:

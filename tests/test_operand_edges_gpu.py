@@ -155,3 +155,20 @@ def test_no_clipping_is_a_copy_whatever_the_norm(B, n, bad, kind):
     assert torch.equal(same.view(torch.int32), x.view(torch.int32))
     B.tensors_clip(B.TensorTable([x], [out]), math.inf, norms, kind, zero_nonfinite=True)
     assert bool((out == 0).all())
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# linear layer
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("lead,n_in,n_out", [((2, 5), 0, 3), ((2, 5), 8, 0), ((5,), 0, 0), ((0, 4), 0, 3), ((2, 0), 8, 0)])
+def test_layers_without_inputs_outputs_or_tokens(fp4, fmt, lead, n_in, n_out):
+    x, w = randn(*lead, n_in, dtype=BF16).requires_grad_(), randn(n_out, n_in).requires_grad_()
+    y = fp4.linear(x, w, fmt)
+    assert y.shape == (*lead, n_out) and bool((y == 0).all())
+    y.sum().backward()
+    assert x.grad.shape == x.shape and w.grad.shape == w.shape and bool((x.grad == 0).all()) and bool((w.grad == 0).all())
+    with torch.no_grad():
+        assert torch.equal(fp4.linear(x, w, fmt), y)
+    fp4.check()

@@ -281,3 +281,16 @@ def test_without_gradients_only_rows_are_packed(fp4, exact, mode):
     fp4.linear(x.detach(), w)
     fp4.linear(x.detach(), w.detach())
     assert [p[2] for p in exact] == [True, True, False, True, True, False, False, False]
+
+
+@pytest.mark.parametrize("lead,n_in,n_out", [((5,), 0, 3), ((2, 5), 0, 3), ((5,), 8, 0), ((2, 5), 8, 0), ((5,), 0, 0), ((0,), 8, 3), ((0, 4), 0, 3), ((2, 0), 8, 0),
+                                             ((), 8, 3), ((), 0, 3)])
+def test_layers_without_inputs_outputs_or_tokens(fp4, exact, lead, n_in, n_out):
+    x, w = leaf(*lead, n_in, seed=1), leaf(n_out, n_in, seed=2)
+    y = fp4.linear(x, w)
+    want = torch.nn.functional.linear(x, w)
+    assert y.shape == want.shape == (*lead, n_out) and torch.allclose(y, want, rtol=1e-5, atol=1e-6)
+    y.sum().backward()
+    got, x.grad, w.grad = (x.grad, w.grad), None, None
+    want.sum().backward()
+    assert all(a.shape == b.shape and torch.allclose(a, b, rtol=1e-5, atol=1e-6) for a, b in zip(got, (x.grad, w.grad)))
