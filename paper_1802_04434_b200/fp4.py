@@ -279,7 +279,9 @@ class _Linear(torch.autograd.Function):
         # only what the backward products will want is packed by columns
         xr, xc = quantise_both(rows, fmt) if need_w else (quantise(rows, fmt), None)
         wr, wc = quantise_both(w, fmt) if need_x else (quantise(w, fmt), None)
-        ctx.kept, ctx.w_dtype, ctx.x_shape = Kept(xc, wc, x.dtype), w.dtype, x.shape
+        ctx.save_for_backward(*[None if p is None else p._buffer[0] for p in (xc, wc)])
+        ctx.places = [None if p is None else (*p._buffer[1], p.rows, p.cols) for p in (xc, wc)]      # in their buffers, and sides
+        ctx.fmt, ctx.x_dtype, ctx.w_dtype, ctx.x_shape = fmt, x.dtype, w.dtype, x.shape
         return matmul(xr, wr, x.dtype).view(*x.shape[:-1], w.shape[0])
 
     @staticmethod
@@ -292,17 +294,17 @@ class _Linear(torch.autograd.Function):
 
     @staticmethod
     def _gradients(ctx, dy):
-        kept = ctx.kept
-        fmt = (kept.x_columns or kept.w_columns).fmt
+        fmt = ctx.fmt
+        xc, wc = [None if b is None else _packed_in(b, b.data_ptr(), *at, fmt, b.device) for b, at in zip(ctx.saved_tensors, ctx.places)]
         rows = _rows_of(dy)
-        if kept.x_columns is None:
+        if xc is None:
             dr, dc = quantise(rows, fmt), None
-        elif kept.w_columns is None:
+        elif wc is None:
             dr, dc = None, quantise_columns(rows, fmt)
         else:
             dr, dc = quantise_both(rows, fmt)
-        dx = matmul(dr, kept.w_columns, kept.dtype).view(ctx.x_shape) if dr is not None else None
-        return dx, matmul(dc, kept.x_columns, ctx.w_dtype) if dc is not None else None
+        dx = matmul(dr, wc, ctx.x_dtype).view(ctx.x_shape) if dr is not None else None
+        return dx, matmul(dc, xc, ctx.w_dtype) if dc is not None else None
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, fmt: str = "mx") -> torch.Tensor:

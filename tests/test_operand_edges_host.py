@@ -7,6 +7,7 @@ import pytest
 
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 torch = pytest.importorskip("torch")
+import torch.utils.checkpoint  # noqa: E402
 
 F32, BF16, U8 = torch.float32, torch.bfloat16, torch.uint8
 
@@ -294,3 +295,31 @@ def test_layers_without_inputs_outputs_or_tokens(fp4, exact, lead, n_in, n_out):
     got, x.grad, w.grad = (x.grad, w.grad), None, None
     want.sum().backward()
     assert all(a.shape == b.shape and torch.allclose(a, b, rtol=1e-5, atol=1e-6) for a, b in zip(got, (x.grad, w.grad)))
+
+
+def test_what_the_layer_keeps_is_saved_the_way_of_autograd(fp4, exact):
+    """Hooks on saved tensors (offloading, checkpointing) see the packed operands, and a backward pass frees them."""
+    x, w = leaf(5, 8, seed=1), leaf(3, 8, seed=2)
+    seen = []
+
+    def pack(t):
+        seen.append(t)
+        return t.clone()
+
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t.clone()):
+        y = fp4.linear(x, w)
+    assert [t.dtype for t in seen] == [U8, U8]
+    got = torch.autograd.grad(y.sum(), (x, w), retain_graph=True)
+    want = torch.autograd.grad(torch.nn.functional.linear(x, w).sum(), (x, w))
+    assert all(torch.allclose(a, b, rtol=1e-5, atol=1e-6) for a, b in zip(got, want))
+    torch.autograd.grad(y.sum(), (x, w))                       # the graph goes, and what it kept with it
+    with pytest.raises(RuntimeError, match="retain_graph"):
+        torch.autograd.grad(y.sum(), (x, w))
+    for a, b in ((x, w.detach()), (x.detach(), w)):
+        y = fp4.linear(a, b)
+        got, = torch.autograd.grad(y.sum(), [t for t in (a, b) if t.requires_grad])
+        assert torch.allclose(got, want[0] if a is x else want[1], rtol=1e-5, atol=1e-6)
+    y = torch.utils.checkpoint.checkpoint(lambda a, b: fp4.linear(a, b).square(), x, w, use_reentrant=False)
+    got = torch.autograd.grad(y.sum(), (x, w))
+    want = torch.autograd.grad(torch.nn.functional.linear(x, w).square().sum(), (x, w))
+    assert all(torch.allclose(a, b, rtol=1e-4, atol=1e-5) for a, b in zip(got, want))
