@@ -121,6 +121,8 @@ def _ptr(t: Optional[torch.Tensor], dtype, name: str, cuda: bool = True) -> Opti
 
 
 def _need(t: torch.Tensor, n: int, name: str) -> None:
+    if t is None:
+        raise ValueError("%s must be given" % name)
     if t.numel() < n:
         raise ValueError("%s holds %d elements, the call needs %d" % (name, t.numel(), n))
 
@@ -400,7 +402,18 @@ def signsgd_step_noalloc(x: torch.Tensor, g: torch.Tensor, m: Optional[torch.Ten
 # --------------------------------------------------------------------------
 # gradients that come as many tensors; 4-bit operands
 
-DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+class _Codes(dict):
+    """The header's codes of some names; looking up anything else raises what the caller should see."""
+
+    def __init__(self, codes, error, message):
+        super().__init__(codes)
+        self.error, self.message = error, message
+
+    def __missing__(self, name):
+        raise self.error("%s, got %r" % (self.message, name))
+
+
+DTYPE_CODE = _Codes({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}, TypeError, "the dtype must be float32, bfloat16 or float16")
 
 
 class _Tensor(ctypes.Structure):                 # ssgd_tensor
@@ -486,7 +499,7 @@ class TensorTable:
         self._ws = self.ws.data_ptr()
 
 
-NORM_KIND = {"two": 0, "max": 1}
+NORM_KIND = _Codes({"two": 0, "max": 1}, ValueError, "kind must be 'two' or 'max'")
 _CLIP_ARGS = struct.Struct("=4QdQ3Q")      # the blocks of arguments of the hot calls, see the header
 FP4_QUANTISE_ARGS, FP4_DEQUANTISE_ARGS, FP4_MATMUL_ARGS = struct.Struct("=13Q"), struct.Struct("=10Q"), struct.Struct("=15Q")
 
@@ -520,7 +533,7 @@ def tensors_clip(table: TensorTable, max_norm: float, norms: torch.Tensor, kind:
         _check(status, "ssgd_tensors_clip")
 
 
-FP4_FORMAT = {"mx": 0, "nv": 1}
+FP4_FORMAT = _Codes({"mx": 0, "nv": 1}, ValueError, "fmt must be 'mx' or 'nv'")
 FP4_SMALL, FP4_SCALE_FLOATS = 32768, 1026
 
 

@@ -189,6 +189,7 @@ def quantise_both(x: torch.Tensor, fmt: str = "mx", amax: Optional[torch.Tensor]
 
 def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """The values of a packed matrix."""
+    code = _DTYPES[dtype]
     rows, cols, device = p.rows, p.cols, p.device
     if device.index != _current_device():
         with B._on(device.index):
@@ -196,7 +197,7 @@ def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     out = torch.empty(rows, cols, dtype=dtype, device=device)
     if rows and cols:
         status = B.lib().ssgd_fp4_dequantise_block(_pack_dequantise(
-            *p.pointers, _FORMATS[p.fmt], rows, cols, out.data_ptr(), _DTYPES[dtype], cols, _stream_of(device.index)))
+            *p.pointers, _FORMATS[p.fmt], rows, cols, out.data_ptr(), code, cols, _stream_of(device.index)))
         if status:
             B._check(status, "ssgd_fp4_dequantise")
     return out
@@ -212,10 +213,10 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optio
             return matmul(a, b, dtype, out)
     rows, cols = a.rows, b.rows
     ldo = cols or 1
+    code = _DTYPES[dtype if out is None else out.dtype]
     if out is None:
         out = torch.empty(rows, cols, dtype=dtype, device=device)
     else:
-        dtype = out.dtype
         if out.shape != (rows, cols) or out.device != device or (cols > 1 and out.stride(1) != 1) or (rows > 1 and out.stride(0) < cols):
             raise ValueError("out must be %d x %d with unit column stride, on the operands' device" % (rows, cols))
         ldo = out.stride(0) if rows > 1 else ldo
@@ -224,7 +225,7 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optio
     if rows and cols:
         status = _status.get(device) or _status_of(device)
         failed = B.lib().ssgd_fp4_matmul_block(_pack_matmul(
-            *a.pointers, *b.pointers, rows, cols, k, _FORMATS[fmt], out.data_ptr(), _DTYPES[dtype], ldo, status[1], _stream_of(device.index)))
+            *a.pointers, *b.pointers, rows, cols, k, _FORMATS[fmt], out.data_ptr(), code, ldo, status[1], _stream_of(device.index)))
         if failed:
             B._check(failed, "ssgd_fp4_matmul")
     return out

@@ -323,3 +323,34 @@ def test_what_the_layer_keeps_is_saved_the_way_of_autograd(fp4, exact):
     got = torch.autograd.grad(y.sum(), (x, w))
     want = torch.autograd.grad(torch.nn.functional.linear(x, w).square().sum(), (x, w))
     assert all(torch.allclose(a, b, rtol=1e-4, atol=1e-5) for a, b in zip(got, want))
+
+
+def test_unknown_types_formats_and_kinds_are_refused_by_name(fp4, B, monkeypatch):
+    """As quantise refuses them, and before anything is allocated."""
+    d = Devices(fp4, B, monkeypatch)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: pytest.fail("allocated"))
+    u8 = Standin(1 << 16, dtype=U8)
+    p = fp4.Packed(u8, u8, None, 64, 96, "mx")
+    for dtype in (torch.float64, torch.int32, None):
+        with pytest.raises(TypeError, match="float32, bfloat16 or float16"):
+            fp4.dequantise(p, dtype)
+        with pytest.raises(TypeError, match="float32, bfloat16 or float16"):
+            fp4.matmul(p, p, dtype)
+    with pytest.raises(TypeError, match="float32, bfloat16 or float16"):
+        fp4.matmul(p, p, out=Standin(64, 64, dtype=torch.float64))
+    x, out, status = Standin(64, 96), Standin(64, 96), Standin(1, dtype=torch.int32)
+    for call in (lambda f: B.fp4_scale_bytes(f, 64, 96), lambda f: B.fp4_quantise(x, 64, 96, 96, f, None, None, u8, u8, None, None),
+                 lambda f: B.fp4_dequantise(u8, u8, None, f, 64, 96, out, 96),
+                 lambda f: B.fp4_matmul(u8, u8, None, u8, u8, None, 64, 64, 96, f, out, 64, status)):
+        with pytest.raises(ValueError, match="fmt must be 'mx' or 'nv'"):
+            call("e4")
+    table = object.__new__(B.TensorTable)
+    table.workers, table.device, table._index, table._args, table._ws = 1, torch.device("cuda", 0), 0, (0x1000, 1, 1), 0x2000
+    for call in (lambda: B.tensors_norm(table, Standin(1), "l2"), lambda: B.tensors_clip(table, 1.0, Standin(1), "l2")):
+        with pytest.raises(ValueError, match="kind must be 'two' or 'max'"):
+            call()
+    with pytest.raises(ValueError, match="tensor_scale"):
+        B.fp4_quantise(x, 64, 96, 96, "nv", None, None, u8, u8, None, None)
+    with pytest.raises(ValueError, match="scales of codes_t"):
+        B.fp4_quantise(x, 64, 96, 96, "mx", None, None, None, None, u8, None)
+    assert d.calls == []
