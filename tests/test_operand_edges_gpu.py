@@ -172,3 +172,22 @@ def test_layers_without_inputs_outputs_or_tokens(fp4, fmt, lead, n_in, n_out):
     with torch.no_grad():
         assert torch.equal(fp4.linear(x, w, fmt), y)
     fp4.check()
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# products into slices
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("M,N,K", [(200, 1, 64), (200, 3, 300), (257, 5, 64), (300, 9, 100), (129, 33, 64), (300, 257, 300), (500, 509, 64), (2050, 2057, 300),
+                                   (4100, 4101, 300), (20000, 129, 64)])
+def test_product_into_a_slice_of_odd_width(fp4, M, N, K, dtype):
+    """Rows of out at multiples of 16 bytes, but not its last columns: what lies behind them belongs to somebody else."""
+    a, b = fp4.quantise(randn(M, K, seed=1)), fp4.quantise(randn(N, K, seed=2))
+    apart = torch.empty(M, N + 1 - N % 2, dtype=dtype, device="cuda")[:, :N]    # rows that start anywhere: stores of one element
+    fp4.matmul(a, b, out=apart)
+    base = torch.full((M + 1, -(-N // 8) * 8 + 8), 7.0, dtype=dtype, device="cuda")
+    fp4.matmul(a, b, out=base[:M, :N])
+    assert torch.equal(base[:M, :N], apart)
+    assert bool((base[:M, N:] == 7.0).all()) and bool((base[M] == 7.0).all())
+    fp4.check()
