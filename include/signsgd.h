@@ -460,6 +460,12 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
                             size_t N, size_t K, int format, void* out, int dtype, size_t ldo, unsigned* status,
                             void* stream);
 
+/* The form that ssgd_fp4_matmul takes on a device of `sms` SMs for an out that starts at a multiple of 16 bytes: form[5] =
+ * CTAs of a tile (1, or 2 as a pair), rows of the narrower side of a tile (A's for single CTAs), CTAs that split k, whether
+ * tiles leave by asynchronous copies (rows of out in whole 16-byte pieces), tiles that a pair takes one after the other at
+ * most (1 for single CTAs).  Pure host arithmetic; for tests and for looking into timings.                              */
+ssgd_status ssgd_fp4_matmul_form(size_t M, size_t N, size_t K, int dtype, size_t ldo, int sms, unsigned* form);
+
 /* Self-test of the bounded waits of ssgd_fp4_matmul: the same launch with every stage armed for more bytes than its copies
  * deliver (all copies still complete).  The kernel must return within its limits (a few seconds) with bit 0 of *status
  * set and `out` untouched; the context stays usable.  M, N <= 256; K <= 4096 where M <= 128 (a long k is split over a

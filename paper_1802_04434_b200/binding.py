@@ -14,7 +14,7 @@ import contextlib
 import ctypes
 import os
 import struct
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -82,6 +82,7 @@ def lib() -> ctypes.CDLL:
         "ssgd_table_build": [vp, sz, sz, vp, sz],
         "ssgd_tensors_norm": [vp, sz, sz, ci, vp, vp, vp],
         "ssgd_tensors_clip": [vp, sz, sz, ci, f32, ci, vp, vp, vp],
+        "ssgd_fp4_matmul_form": [sz, sz, sz, ci, sz, ci, vp],
         "ssgd_fp4_matmul_wait_selftest": [vp, vp, vp, vp, sz, sz, sz, ci, vp, ci, sz, vp, vp],
         "ssgd_tensors_clip_block": [ctypes.c_char_p],
         "ssgd_fp4_quantise_block": [ctypes.c_char_p],
@@ -545,6 +546,22 @@ def fp4_row_bytes(cols: int) -> int:
 def fp4_scale_bytes(fmt: str, rows: int, cols: int) -> int:
     """Bytes of the scales of a packed operand."""
     return int(lib().ssgd_fp4_scale_bytes(FP4_FORMAT[fmt], rows, cols))
+
+
+class ProductForm(NamedTuple):
+    """How a product is computed, see ssgd_fp4_matmul_form."""
+    ctas: int
+    rows: int
+    splits: int
+    wide: bool
+    rounds: int
+
+
+def fp4_matmul_form(M: int, N: int, K: int, dtype: torch.dtype = torch.bfloat16, ldo: Optional[int] = None, sms: int = 148) -> ProductForm:
+    """The form of a product M x N x K into rows of stride ldo (None: N)."""
+    form = (ctypes.c_uint * 5)()
+    _check(lib().ssgd_fp4_matmul_form(M, N, K, DTYPE_CODE[dtype], N if ldo is None else ldo, sms, form), "ssgd_fp4_matmul_form")
+    return ProductForm(form[0], form[1], form[2], bool(form[3]), form[4])
 
 
 def fp4_quantise(x: torch.Tensor, rows: int, cols: int, ldx: int, fmt: str, amax: Optional[torch.Tensor],

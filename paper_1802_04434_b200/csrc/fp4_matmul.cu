@@ -637,13 +637,22 @@ inline unsigned k_splits(unsigned tiles, unsigned stages_k, int sms) {
   return 1;
 }
 
+// The form of a product: by single CTAs, tiles of 128 rows of B by nt rows of A, k split over `splits` of them; or by pairs, tiles of
+// 256 x nt, WIDE where rows of out allow it.
+struct Form {
+  bool pairs, wide;
+  unsigned nt, splits;
+  size_t tiles;
+};
+Form choose_form(size_t M, size_t N, size_t K, bool rows_of_16_bytes, int sms);
+
 template <int FORMAT>
-ssgd_status product(const Operands& o, int sms, cudaStream_t s) {
+ssgd_status product(const Operands& o, const Form& form, cudaStream_t s) {
   const size_t row_bytes = ssgd_fp4_row_bytes(o.K);
-  const unsigned nt = o.M <= 16 ? 16 : o.M <= 32 ? 32 : o.M <= 64 ? 64 : 128;
-  const size_t tiles_i = (o.M + nt - 1) / nt, all = (o.N + kTileJ - 1) / kTileJ * tiles_i;
-  if (all > (size_t)1 << 27) return SSGD_ERR_SIZE;
-  const unsigned tiles = (unsigned)all, stages_k = (unsigned)((row_bytes + 127) / 128), splits = k_splits(tiles, stages_k, sms);
+  const unsigned nt = form.nt, splits = form.splits;
+  const size_t tiles_i = (o.M + nt - 1) / nt;
+  if (form.tiles > (size_t)1 << 27) return SSGD_ERR_SIZE;
+  const unsigned tiles = (unsigned)form.tiles;
   CUtensorMap a_map, b_map;
   if (!code_map(&a_map, o.a, o.M, row_bytes, nt) || !code_map(&b_map, o.b, o.N, row_bytes, kTileJ)) return SSGD_ERR_CUDA;
   ProductArgs p;
@@ -730,20 +739,37 @@ inline unsigned long long pair_cost(unsigned long long tiles_p, size_t Q, unsign
   return start + work + (rounds - 1) * (work + 250 > write ? work + 250 : write);
 }
 
-template <int FORMAT>
-ssgd_status any_product(const Operands& o, int sms, cudaStream_t s) {
+Form choose_form(size_t M, size_t N, size_t K, bool rows_of_16_bytes, int sms) {
   // Up to 128 rows of A: the weight's rows are the lanes and stream through once.  More rows, but few tiles and a long k: the
   // same kernel, because it splits k (150 x 300 x 16384: 8.5 us against 13.8 by pairs; x 4096 7.3 against 6.7).
-  const size_t stages_k = (ssgd_fp4_row_bytes(o.K) + 127) / 128;
-  if (o.M <= 128 || (stages_k >= 24 && ((o.M + 127) / 128) * ((o.N + kTileJ - 1) / kTileJ) * 8 <= (size_t)sms)) return product<FORMAT>(o, sms, s);
-  const size_t e = dtype_bytes((unsigned)o.dtype);
-  const bool wide = aligned16(o.out) && o.ldo * e % 16 == 0 && o.N * e % 16 == 0 && o.ldo < (size_t)1 << 37;
-  const size_t P = wide ? o.M : o.N, Q = wide ? o.N : o.M, tiles_p = (P + 255) / 256;
+  const size_t stages_k = (ssgd_fp4_row_bytes(K) + 127) / 128, tiles_j = (N + kTileJ - 1) / kTileJ;
+  if (M <= 128 || (stages_k >= 24 && ((M + 127) / 128) * tiles_j * 8 <= (size_t)sms)) {
+    const unsigned nt = M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    const size_t tiles = tiles_j * ((M + nt - 1) / nt);
+    return {false, false, nt, k_splits((unsigned)tiles, (unsigned)stages_k, sms), tiles};
+  }
+  const bool wide = rows_of_16_bytes;
+  const size_t P = wide ? M : N, Q = wide ? N : M, tiles_p = (P + 255) / 256;
   const unsigned pairs = (unsigned)(sms / 2);
   const unsigned long long c64 = pair_cost(tiles_p, Q, 64, stages_k, pairs), c128 = pair_cost(tiles_p, Q, 128, stages_k, pairs),
                            c256 = pair_cost(tiles_p, Q, 256, stages_k, pairs);
-  if (c256 <= c128 && c256 <= c64) return pair_product<FORMAT, 256>(o, wide, sms, s);
-  return c128 <= c64 ? pair_product<FORMAT, 128>(o, wide, sms, s) : pair_product<FORMAT, 64>(o, wide, sms, s);
+  const unsigned nt = c256 <= c128 && c256 <= c64 ? 256 : c128 <= c64 ? 128 : 64;
+  return {true, wide, nt, 1, tiles_p * ((Q + nt - 1) / nt)};
+}
+
+// Rows of out in whole 16-byte pieces, at a stride that a tensor map holds.
+inline bool rows_of_16_bytes(const void* out, size_t N, size_t ldo, int dtype) {
+  const size_t e = dtype_bytes((unsigned)dtype);
+  return aligned16(out) && ldo * e % 16 == 0 && N * e % 16 == 0 && ldo < (size_t)1 << 37;
+}
+
+template <int FORMAT>
+ssgd_status any_product(const Operands& o, int sms, cudaStream_t s) {
+  const Form form = choose_form(o.M, o.N, o.K, rows_of_16_bytes(o.out, o.N, o.ldo, o.dtype), sms);
+  if (!form.pairs) return product<FORMAT>(o, form, s);
+  return form.nt == 256   ? pair_product<FORMAT, 256>(o, form.wide, sms, s)
+         : form.nt == 128 ? pair_product<FORMAT, 128>(o, form.wide, sms, s)
+                          : pair_product<FORMAT, 64>(o, form.wide, sms, s);
 }
 
 ssgd_status checked_product(const uint8_t* a_codes, const uint8_t* a_scales, const float* a_tensor_scale, const uint8_t* b_codes, const uint8_t* b_scales,
@@ -778,6 +804,20 @@ ssgd_status ssgd_fp4_matmul(const uint8_t* a_codes, const uint8_t* a_scales, con
                             const uint8_t* b_scales, const float* b_tensor_scale, size_t M, size_t N, size_t K, int format, void* out,
                             int dtype, size_t ldo, unsigned* status, void* stream) {
   return checked_product(a_codes, a_scales, a_tensor_scale, b_codes, b_scales, b_tensor_scale, M, N, K, format, out, dtype, ldo, status, 0, stream);
+}
+
+ssgd_status ssgd_fp4_matmul_form(size_t M, size_t N, size_t K, int dtype, size_t ldo, int sms, unsigned* form) {
+  if (!form) return SSGD_ERR_NULL;
+  if (dtype_bytes((unsigned)dtype) == 0 || sms < 2) return SSGD_ERR_ARG;
+  if (M < 1 || N < 1 || K < 1 || M > SSGD_FP4_MAX_SIDE || N > SSGD_FP4_MAX_SIDE || K > SSGD_FP4_MAX_SIDE || ldo < N) return SSGD_ERR_SIZE;
+  const Form f = choose_form(M, N, K, rows_of_16_bytes(nullptr, N, ldo, dtype), sms);
+  const size_t most = f.pairs ? (size_t)(sms / 2) : f.tiles;
+  form[0] = f.pairs ? 2 : 1;
+  form[1] = f.nt;
+  form[2] = f.splits;
+  form[3] = f.wide;
+  form[4] = (unsigned)((f.tiles + most - 1) / most);
+  return SSGD_OK;
 }
 
 ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, size_t M,

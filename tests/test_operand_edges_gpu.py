@@ -190,4 +190,59 @@ def test_product_into_a_slice_of_odd_width(fp4, M, N, K, dtype):
     fp4.matmul(a, b, out=base[:M, :N])
     assert torch.equal(base[:M, :N], apart)
     assert bool((base[:M, N:] == 7.0).all()) and bool((base[M] == 7.0).all())
+
+
+# every form of the product: tile widths, several tiles of a pair one after the other, splits of k
+
+
+def values_of(p):
+    """float64 values of a packed operand on its device, from its bytes."""
+    code = p.codes.view(p.rows, -1)
+    code = torch.stack((code & 15, code >> 4), 2).reshape(p.rows, -1)[:, :p.cols].long()
+    value = torch.from_numpy(np.concatenate([ref.LEVELS, -ref.LEVELS])).cuda()[code]
+    block = ref.BLOCK[p.fmt]
+    nb = -(-p.cols // block)
+    tk = -(-nb // 4)
+    r, k = torch.arange(p.rows, device="cuda")[:, None], torch.arange(nb, device="cuda")[None]
+    byte = p.scales[((r // 128) * tk + k // 4) * 512 + (r % 32) * 16 + (r % 128) // 32 * 4 + k % 4].long()
+    table = 2.0 ** (np.arange(256.0) - 127) if p.fmt == "mx" else np.concatenate([ref.E4M3, np.full(129, np.nan)])
+    scale = torch.from_numpy(table).cuda()[byte]
+    if p.fmt == "nv":
+        scale = scale * p.tensor_scale[0].double()
+    return value * scale.repeat_interleave(block, 1)[:, :p.cols]
+
+
+# M, N, K, row stride of out; CTAs of a tile, rows, splits, by asynchronous copies, rounds (at least)
+FORMS = [(2048, 2056, 700, 2056, 2, 128, 1, True, 2), (2050, 2064, 700, 2072, 2, 128, 1, True, 3), (2050, 2057, 700, 2064, 2, 128, 1, False, 3), (2050, 2057, 700, 2057, 2, 128, 1, False, 3),
+         (129, 15000, 2600, 15000, 2, 128, 1, True, 2), (20000, 40, 2600, 41, 2, 128, 1, False, 3),
+         (4100, 4104, 300, 4104, 2, 256, 1, True, 4), (4100, 4104, 300, 4112, 2, 256, 1, True, 4), (4100, 4101, 300, 4104, 2, 256, 1, False, 4), (4100, 4101, 300, 4101, 2, 256, 1, False, 4),
+         (4096, 4096, 520, 4096, 2, 256, 1, True, 4), (129, 30000, 5000, 30000, 2, 256, 1, True, 2), (193, 30000, 5000, 30001, 2, 256, 1, False, 2),
+         (20000, 136, 64, 144, 2, 64, 1, True, 4), (20000, 40, 2600, 40, 2, 64, 1, True, 2), (129, 20000, 2600, 20001, 2, 64, 1, False, 4),
+         (16, 5003, 4096, 5003, 1, 16, 2, False, 1), (16, 2000, 3200, 2000, 1, 16, 4, False, 1), (3, 1000, 4096, 1000, 1, 16, 8, False, 1),
+         (30, 5003, 4096, 5003, 1, 32, 2, False, 1), (60, 2000, 3200, 2003, 1, 64, 4, False, 1), (120, 1400, 5000, 1400, 1, 128, 8, False, 1),
+         (128, 3000, 3300, 3000, 1, 128, 4, False, 1), (150, 300, 8192, 300, 1, 128, 8, False, 1), (300, 600, 8192, 601, 1, 128, 4, False, 1),
+         (64, 5003, 700, 5003, 1, 64, 1, False, 1)]
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+@pytest.mark.parametrize("M,N,K,ldo,ctas,rows,splits,wide,rounds", FORMS)
+def test_product_of_every_form(fp4, B, M, N, K, ldo, ctas, rows, splits, wide, rounds, fmt):
+    a = fp4.quantise(randn(M, K, seed=M + K) * torch.exp(randn(M, 1, seed=1)), fmt)
+    b = fp4.quantise(randn(N, K, seed=N * 3 + K, scale=0.02, dtype=BF16), fmt)
+    va, vb = values_of(a), values_of(b)
+    want, total = va @ vb.t(), va.abs() @ vb.abs().t()
+    for dtype in (F32, BF16, F16):
+        form = B.fp4_matmul_form(M, N, K, dtype, ldo, torch.cuda.get_device_properties(0).multi_processor_count)
+        # 4-byte elements keep rows of 16 bytes at strides where 2-byte ones do not: the sizes are chosen for both alike
+        assert form[:4] == (ctas, rows, splits, wide) and form.rounds >= rounds, form
+        base = torch.full((M, ldo), 7.0, dtype=dtype, device="cuda")
+        out = base[:, :N]
+        fp4.matmul(a, b, out=out)
+        # any order of K additions with one ulp (2^-23) of a partial sum lost in each, then the type's rounding
+        tol = K * 2.0 ** -23 * total + torch.finfo(dtype).eps / 2 * want.abs() + (2.0 ** -25 if dtype == F16 else 0.0)
+        assert bool(((out.double() - want).abs() <= tol).all())
+        assert bool((base[:, N:] == 7.0).all())
+        again = torch.empty_like(base)[:, :N]
+        fp4.matmul(a, b, out=again)
+        assert torch.equal(out, again)
     fp4.check()

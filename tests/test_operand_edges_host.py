@@ -354,3 +354,17 @@ def test_unknown_types_formats_and_kinds_are_refused_by_name(fp4, B, monkeypatch
     with pytest.raises(ValueError, match="scales of codes_t"):
         B.fp4_quantise(x, 64, 96, 96, "mx", None, None, None, None, u8, None)
     assert d.calls == []
+
+
+def test_forms_of_the_product(B):
+    f = B.fp4_matmul_form
+    assert f(8192, 8192, 8192) == (2, 256, 1, True, 14) and f(777, 1111, 1500) == (2, 64, 1, False, 1) and f(777, 1104, 1500, ldo=1112).wide
+    assert f(1, 4096, 1024) == (1, 16, 1, False, 1) and f(128, 3000, 3300) == (1, 128, 4, False, 1) and f(129, 3000, 3300).ctas == 2
+    assert not f(777, 1104, 1500, ldo=1110).wide and not f(777, 1111, 1500, ldo=1112).wide
+    assert f(777, 1108, 1500, torch.float32, 1112).wide and not f(777, 1108, 1500, torch.float32, 1110).wide and not f(777, 1108, 1500, ldo=1112).wide
+    import ctypes
+    out = (ctypes.c_uint * 5)()
+    g = B.lib().ssgd_fp4_matmul_form
+    assert g(1, 1, 1, 0, 1, 148, None) == 1 and g(1, 1, 1, 3, 1, 148, out) == 4 and g(1, 1, 1, 0, 1, 1, out) == 4
+    for M, N, K, ldo in ((0, 1, 1, 1), (1, 0, 1, 1), (1, 1, 0, 1), (1 << 31, 1, 1, 1), (1, 1 << 31, 1, 1 << 31), (1, 1, 1 << 31, 1), (1, 2, 1, 1)):
+        assert g(M, N, K, 0, ldo, 148, out) == 3
