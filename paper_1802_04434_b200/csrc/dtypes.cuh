@@ -72,20 +72,6 @@ __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
   v[0] = low_to_float(T(), q.x); v[1] = high_to_float(T(), q.x); v[2] = low_to_float(T(), q.y); v[3] = high_to_float(T(), q.y);
   v[4] = low_to_float(T(), q.z); v[5] = high_to_float(T(), q.z); v[6] = low_to_float(T(), q.w); v[7] = high_to_float(T(), q.w);
 }
-// 32 bytes in one store; the address is a multiple of 32.
-__device__ __forceinline__ void store32(void* at, const unsigned* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  store4(p, make_float4(v[0], v[1], v[2], v[3]));
-  store4(p + 4, make_float4(v[4], v[5], v[6], v[7]));
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
-  __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack2(T(), v[0], v[1]), pack2(T(), v[2], v[3]), pack2(T(), v[4], v[5]), pack2(T(), v[6], v[7])));
-}
 
 }  // namespace
 

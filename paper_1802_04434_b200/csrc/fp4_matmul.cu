@@ -71,12 +71,12 @@ __device__ __forceinline__ void issue_stage(unsigned d, uint64_t p_desc, uint64_
 template <int FORMAT, int NT>
 struct Shape {
   static constexpr unsigned blocks = FORMAT == SSGD_MXFP4 ? 2 : 4;          // scale tiles (of four blocks) of a stage and 128 rows
-  static constexpr unsigned row_tiles = (NT + 127) / 128;                  // of A
+  static_assert(NT <= 128, "one scale tile holds A's rows");
   static constexpr unsigned b_bytes = kTileJ * 128, a_bytes = NT * 128;
   static constexpr unsigned scale_bytes = blocks * 512;
-  static constexpr unsigned stage_bytes = b_bytes + a_bytes + ((1 + row_tiles) * scale_bytes + 1023) / 1024 * 1024;
+  static constexpr unsigned stage_bytes = b_bytes + a_bytes + (2 * scale_bytes + 1023) / 1024 * 1024;
   static constexpr unsigned stages = 221184 / stage_bytes < 8 ? 221184 / stage_bytes : 8;
-  static constexpr unsigned scale_columns = (1 + row_tiles) * blocks * 4;  // of a stage, in tensor memory
+  static constexpr unsigned scale_columns = 2 * blocks * 4;               // of a stage, in tensor memory
   static constexpr unsigned columns_used = NT + stages * scale_columns;
   static constexpr unsigned columns = columns_used <= 64 ? 64 : columns_used <= 128 ? 128 : columns_used <= 256 ? 256 : 512;
   static_assert(columns_used <= 512, "tensor memory");
@@ -96,7 +96,6 @@ struct ProductArgs {
   unsigned M, N;
   unsigned k_chunks;      // 64-column pieces of k
   unsigned tiles_k;       // scale tiles along k of one row of tiles
-  unsigned a_row_tiles;   // scale row tiles of A
   unsigned tiles_i;
   unsigned starve;        // bytes that a stage waits for in vain: 0 but in the self-test of the waits
 };
@@ -183,15 +182,13 @@ fp4_matmul_kernel(const __grid_constant__ CUtensorMap a_map, const __grid_consta
         if (!ok) break;
         const unsigned base = stage0 + s * S::stage_bytes, bar = full + 8 * s;
         const unsigned kt = k * S::blocks, blocks = min(S::blocks, p.tiles_k - kt);
-        const unsigned row_tiles = min(S::row_tiles, p.a_row_tiles - it);
         issued = n + 1;
-        mbarrier_expect(bar, S::b_bytes + S::a_bytes + (1 + row_tiles) * blocks * 512 + p.starve);
+        mbarrier_expect(bar, S::b_bytes + S::a_bytes + 2 * blocks * 512 + p.starve);
         tma_load_2d(base, &b_map, (int)(k * 128), (int)j0, bar);
         tma_load_2d(base + S::b_bytes, &a_map, (int)(k * 128), (int)i0, bar);
         const unsigned sc = base + S::b_bytes + S::a_bytes;
         bulk_copy(sc, p.b_scales + ((size_t)jt * p.tiles_k + kt) * 512, blocks * 512, bar);
-        for (unsigned t = 0; t < row_tiles; ++t)
-          bulk_copy(sc + (1 + t) * S::scale_bytes, p.a_scales + ((size_t)(it + t) * p.tiles_k + kt) * 512, blocks * 512, bar);
+        bulk_copy(sc + S::scale_bytes, p.a_scales + ((size_t)it * p.tiles_k + kt) * 512, blocks * 512, bar);
       }
     }
   } else if (warp == 1) {
@@ -660,7 +657,6 @@ ssgd_status product(const Operands& o, const Form& form, cudaStream_t s) {
   p.M = (unsigned)o.M; p.N = (unsigned)o.N;
   p.k_chunks = (unsigned)((row_bytes + 31) / 32);
   p.tiles_k = (unsigned)((fp4_block_count(FORMAT, o.K) + 3) / 4);
-  p.a_row_tiles = (unsigned)((o.M + 127) / 128);
   p.tiles_i = (unsigned)tiles_i;
   p.starve = o.starve;
   switch (nt) {
