@@ -384,8 +384,7 @@ ssgd_status ssgd_table_size(const ssgd_tensor* tensors, size_t T, size_t groups,
 /* Writes the table into HOST memory; copy its table_bytes to the device (16-byte aligned) before use.               */
 ssgd_status ssgd_table_build(const ssgd_tensor* tensors, size_t T, size_t groups, void* table_host, size_t table_bytes);
 
-/* Norm of each group: SSGD_NORM_TWO sqrt(sum g^2), summed in fp64 (squares of 16-bit elements by fours in fp32 first, which
- * changes the norm by 2^-24 of itself at most; then one rounding to fp32); SSGD_NORM_MAX max |g|.  NaN and infinity carry
+/* Norm of each group: SSGD_NORM_TWO sqrt(sum g^2), summed in fp64; SSGD_NORM_MAX max |g|.  NaN and infinity carry
  * through; an empty group has norm 0.  Sums go in a fixed order: equal inputs give equal bits.
  *   table  DEVICE copy of the table;  norms out DEVICE float [groups]
  *   ws     DEVICE, ws_bytes, 16-byte aligned; calls that may run at the same time need one each                       */

@@ -39,24 +39,10 @@ constexpr int kNormTwo = 0, kNormMax = 1;
 // |v| as ordered bits: NaN sorts above infinity, so one maximum carries it through.
 __device__ __forceinline__ unsigned magnitude_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-// Squares go to fp64, where the product of two fp32 numbers is exact and neither overflows nor vanishes.  16-bit
-// elements have squares of 16 or 22 bits: four of them are added in fp32 first, in two pairs, unless bf16's range calls for
-// fp64.  Two roundings lie on the way of a square there, so the norm is off by 2^-24 of itself at most before its own rounding
-// (eight in a row made that 7 * 2^-25).  Two fours are then added without loss: their sum goes to fp64, and what its rounding
-// took away is kept beside it in fp32, since conversions to fp64 cost more than the loads (335 M elements 138 us with one
-// conversion for eight elements, 165 with two).
-__device__ __forceinline__ float squares4(const float* v) {
-  return __fadd_rn(__fmaf_rn(v[1], v[1], __fmul_rn(v[0], v[0])), __fmaf_rn(v[3], v[3], __fmul_rn(v[2], v[2])));
-}
-__device__ __forceinline__ void fold8(const float (&v)[8], double& acc, float& rest) {
-  const float a = squares4(v), b = squares4(v + 4), big = fmaxf(a, b), small = fminf(a, b), s = __fadd_rn(a, b);   // s carries a NaN on
-  if (small > 1e-25f && s < 1e38f) {
-    acc += (double)s;
-    rest += __fsub_rn(small, __fsub_rn(s, big));
-  } else {
+// Squares go to fp64, where the product of two fp32 numbers is exact and neither overflows nor vanishes.
+__device__ __forceinline__ void fold8(const float (&v)[8], double& acc) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc = fma((double)v[i], (double)v[i], acc);
-  }
+  for (int i = 0; i < 8; ++i) acc = fma((double)v[i], (double)v[i], acc);
 }
 
 // One tile's contribution of this thread: a double for the two-norm, the largest magnitude's bits for the maximum.
@@ -66,32 +52,32 @@ __device__ __forceinline__ void tile_norm(const T* __restrict__ src, unsigned n,
   const unsigned head = min(n, off ? 8u - off : 0u), groups = (n - head) / 8;
   const T* body = src + head;
   if constexpr (KIND == kNormTwo && sizeof(T) == 2) {
-    // two loads in flight by hand: left to the unrolling, the folds' temporaries leave room for fewer in 32 registers (171 us
-    // where this takes 137); four take 40 registers and an SM's eighth CTA (fp32, in the same kernel, 195 -> 217 us)
-    float rest = 0.0f;
-    for (unsigned g0 = threadIdx.x; g0 < groups; g0 += 2 * kThreads) {
-      uint4 q[2];
+    // Four loads in flight by hand, within the 32 registers of eight CTAs an SM: left to the unrolling there are fewer.  335 M
+    // bf16 elements 109 us = 6.2 TB/s; two by hand 137, and that with fours of squares added in fp32 first, which saves
+    // three quarters of the conversions to fp64 and was no faster than this even with four (114).
+    for (unsigned g0 = threadIdx.x; g0 < groups; g0 += 4 * kThreads) {
+      uint4 q[4];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 4; ++u)
         q[u] = g0 + u * kThreads < groups ? *reinterpret_cast<const uint4*>(body + 8 * (g0 + u * kThreads)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < 4; ++u) {
         if (g0 + u * kThreads >= groups) break;
         const float v[8] = {low_to_float(T(), q[u].x), high_to_float(T(), q[u].x), low_to_float(T(), q[u].y), high_to_float(T(), q[u].y),
                             low_to_float(T(), q[u].z), high_to_float(T(), q[u].z), low_to_float(T(), q[u].w), high_to_float(T(), q[u].w)};
-        fold8(v, acc, rest);
+        fold8(v, acc);
       }
     }
-    acc += (double)rest;
   } else {
 #pragma unroll 4
     for (unsigned g = threadIdx.x; g < groups; g += kThreads) {
       float v[8];
       load8(body + 8 * g, v);
+      if constexpr (KIND == kNormTwo) {
+        fold8(v, acc);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (KIND == kNormTwo) acc = fma((double)v[i], (double)v[i], acc);
-        else top = max(top, magnitude_bits(v[i]));
+        for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[i]));
       }
     }
   }

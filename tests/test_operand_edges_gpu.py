@@ -137,7 +137,7 @@ def test_norm_of_16_bit_squares_that_differ_in_size(B, dtype, repeats, pattern):
     norms = torch.zeros(1, device="cuda")
     B.tensors_norm(B.TensorTable([x]), norms)
     want = math.sqrt(repeats * sum(v * v for v in pattern))
-    # 2^-24 for the fours in fp32 (two roundings of a sum of squares are half of that in its root), 2^-24 for the norm's own
+    # sums in fp64, one rounding to fp32
     assert abs(norms.item() - want) <= 2.0 ** -23 * want
 
 
