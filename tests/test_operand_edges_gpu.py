@@ -157,6 +157,21 @@ def test_no_clipping_is_a_copy_whatever_the_norm(B, n, bad, kind):
     assert bool((out == 0).all())
 
 
+@pytest.mark.parametrize("groups", [1, 2, 15, 16])
+@pytest.mark.parametrize("elements", [8192, 8 * 8192, 8 * 8192 + 1, 16 * 8192])
+@pytest.mark.parametrize("even", [True, False])
+def test_norms_around_the_one_launch_form(B, groups, elements, even):
+    """Groups of 1, 8, 9 and 16 tiles, each of them or only the last."""
+    src = [randn(elements if even or g == groups - 1 else 1, seed=g, dtype=BF16) for g in range(groups)]
+    dst, norms = [torch.zeros(t.numel(), device="cuda") for t in src], torch.zeros(groups, device="cuda")
+    B.tensors_clip(B.TensorTable(src, dst, list(range(groups))), 0.5, norms)
+    for t, d, n in zip(src, dst, norms.tolist()):
+        want = float(t.double().norm())
+        assert abs(n - want) <= 2.0 ** -23 * want
+        c = 0.5 / want if want > 0.5 else 1.0
+        assert bool(((d.double() - t.double() * c).abs() <= 4 * 2.0 ** -24 * (t.double() * c).abs()).all())
+
+
 # ---------------------------------------------------------------------------------------------------------------------
 # linear layer
 
