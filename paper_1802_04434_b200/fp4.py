@@ -191,13 +191,14 @@ def dequantise(p: Packed, dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """The values of a packed matrix."""
     code = _DTYPES[dtype]
     rows, cols, device = p.rows, p.cols, p.device
-    if device.index != _current_device():
-        with B._on(device.index):
+    index = device.index
+    if index != _current_device():
+        with B._on(index):
             return dequantise(p, dtype)
     out = torch.empty(rows, cols, dtype=dtype, device=device)
     if rows and cols:
         status = B.lib().ssgd_fp4_dequantise_block(_pack_dequantise(
-            *p.pointers, _FORMATS[p.fmt], rows, cols, out.data_ptr(), code, cols, _stream_of(device.index)))
+            *p.pointers, _FORMATS[p.fmt], rows, cols, out.data_ptr(), code, cols, _stream_of(index)))
         if status:
             B._check(status, "ssgd_fp4_dequantise")
     return out
@@ -208,8 +209,9 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optio
     fmt, k, device = a.fmt, a.cols, a.device
     if fmt != b.fmt or k != b.cols or device != b.device:
         raise ValueError("a product needs operands of one format, one length and one device: got %s x %d and %s x %d" % (fmt, k, b.fmt, b.cols))
-    if device.index != _current_device():
-        with B._on(device.index):
+    index = device.index
+    if index != _current_device():
+        with B._on(index):
             return matmul(a, b, dtype, out)
     rows, cols = a.rows, b.rows
     ldo = cols or 1
@@ -225,7 +227,7 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optio
     if rows and cols:
         status = _status.get(device) or _status_of(device)
         failed = B.lib().ssgd_fp4_matmul_block(_pack_matmul(
-            *a.pointers, *b.pointers, rows, cols, k, _FORMATS[fmt], out.data_ptr(), code, ldo, status[1], _stream_of(device.index)))
+            *a.pointers, *b.pointers, rows, cols, k, _FORMATS[fmt], out.data_ptr(), code, ldo, status[1], _stream_of(index)))
         if failed:
             B._check(failed, "ssgd_fp4_matmul")
     return out
