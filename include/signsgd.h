@@ -473,6 +473,85 @@ ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t*
                                           const uint8_t* b_scales, size_t M, size_t N, size_t K, int format, void* out,
                                           int dtype, size_t ldo, unsigned* status, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Cross entropy of a linear head over a large vocabulary, and its gradients: the loss that the step's gradients begin at.
+ *
+ *   z = h w^T       h [T][D] a row a token, w [V][D] a row a word of the vocabulary
+ *   losses[t] = log sum_v exp z[t][v] - z[t][targets[t]]
+ *   dz[t][v]  = g[t] (exp(z[t][v] - lse[t]) - [v = targets[t]]),   dh = dz w,   dw = dz^T h
+ * The logits are never in memory: a tile at a time, forward and once more backward.  A token whose target is `ignore` has
+ * loss 0 and no part in any gradient (its row of dh is 0), whatever its row of h and its g hold, NaN included.  Any
+ * other target outside 0 .. V-1 gives NaN, the loss and the gradients that it reaches.  Logits, statistics, losses and sums are
+ * fp32; dz is rounded to the type of h and w (fp16: times a power of two that brings the largest |g| to 2^14 .. 2^15)
+ * before the products of the gradients.  Sums go in a fixed order: equal inputs give equal bits.
+ *   h, w      DEVICE, SSGD_BF16 or SSGD_F16, both the same; 16-byte aligned, rows of stride ldh, ldw >= D, multiples of 8
+ *   targets   DEVICE int64 [T], 8-byte aligned
+ *   ws        DEVICE, bytes as ssgd_xent_sizes says (for the current device), 16-byte aligned; calls that may run at the same time need one each
+ *   status    in/out DEVICE unsigned, as for ssgd_fp4_matmul
+ * D, V >= 1 and sides up to 2^30; T * V and T * D up to 2^44.                                                       */
+ssgd_status ssgd_xent_sizes(size_t T, size_t V, size_t D, size_t* forward_bytes, size_t* backward_bytes);
+
+/*   losses, lse  out DEVICE float [T];  lse: log sum exp, for the backward pass
+ *   kinds        out DEVICE uint8 [T], for the backward pass: 0, or 1 for an ignored token, 2 where its row of h is not finite */
+ssgd_status ssgd_xent_forward(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V,
+                              size_t D, const int64_t* targets, int64_t ignore, float* losses, float* lse,
+                              uint8_t* kinds, void* ws, unsigned* status, void* stream);
+
+/*   g        in  DEVICE float, the gradient of losses[t] at g[t * g_stride] (stride 0: one for all)
+ *   dh       out DEVICE [T][lddh] of h's type, or NULL: not wanted
+ *   dw       out DEVICE [V][lddw] of dw_type, or NULL: not wanted.  Both aligned to their elements.
+ * h, w, targets, lse, kinds as the forward pass had and left them.                                                  */
+ssgd_status ssgd_xent_backward(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V,
+                               size_t D, const int64_t* targets, const float* lse, const uint8_t* kinds,
+                               const float* g, size_t g_stride, void* dh, size_t lddh, void* dw, int dw_type,
+                               size_t lddw, void* ws, unsigned* status, void* stream);
+
+/* Self-test of the bounded waits, as for ssgd_fp4_matmul: bit 0 of *status set; what the call writes is not valid, the context
+ * stays usable.  T, V <= 256, D <= 128.                                                                             */
+ssgd_status ssgd_xent_wait_selftest(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V,
+                                    size_t D, const int64_t* targets, int64_t ignore, float* losses, float* lse,
+                                    uint8_t* kinds, void* ws, unsigned* status, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Orthogonalised updates: a matrix with its singular values brought near one.  Where the step above moves each parameter by
+ * the sign of its momentum, this moves a weight matrix by the sign of its momentum's singular values, so to say, as the
+ * Muon optimiser does.
+ *
+ *   X = U / |U|_F (0 for U = 0);  `steps` times  X <- a X + (b A + c A^2) X  with A = X X^T
+ * for n matrices of rows x cols at a time.  A matrix that holds a NaN or an infinity becomes NaN.  The coefficients should keep the
+ * singular values below 4, and |b t + c t^2| below 8 for their squares t: beyond that the result is not finite or not right.
+ *   products   3: products of operands in two fp16 parts, 22 bits: as exact as products in fp32
+ *              1: operands of 11 bits, sums in fp32: the result is off by about 10^-3 of its norm (less than bf16's rounding of it
+ *                 for a side of 256 and more; up to 4 * 10^-3 for small matrices of low rank)
+ *   coefficients  HOST float[3]: a, b, c, finite;  steps 1 .. 100
+ *   a batch       first element, rows at a stride of ld >= cols, matrices at a stride (any where n = 1); in elements, aligned to one
+ *   ws            DEVICE, ssgd_orthogonal_ws_bytes(n, rows, cols), 16-byte aligned; calls that may run at the same time
+ *                 need one each
+ *   status        in/out DEVICE unsigned, as for ssgd_fp4_matmul
+ * Sides 1 .. SSGD_ORTHOGONAL_MAX_SIDE, n up to 65535 (0: nothing is done).  Sums go in a fixed order.                 */
+#define SSGD_ORTHOGONAL_MAX_SIDE ((size_t)32768)
+size_t ssgd_orthogonal_ws_bytes(size_t n, size_t rows, size_t cols); /* 0 for sizes out of range */
+
+/*   u    in  DEVICE batch of u_type;  out  DEVICE batch of out_type, each element rounded once.  out may be u where the types and
+ *        strides are equal                                                                                             */
+ssgd_status ssgd_orthogonalise(const void* u, int u_type, size_t n, size_t rows, size_t cols, size_t ldu,
+                               size_t stride_u, const float* coefficients, unsigned steps, int products, void* out,
+                               int out_type, size_t ldo, size_t stride_o, void* ws, unsigned* status, void* stream);
+
+/* A whole step, its momentum that of Algorithm 2:
+ *   m <- fma(beta, m, fl((1 - beta) g));   u = m, or, nesterov != 0, fma(beta, m, fl((1 - beta) g)) with the new m
+ *   x <- x - delta orthogonalise(u)
+ *   x, m   in/out DEVICE batches of float;  g  in DEVICE batch of g_type;  beta in [0,1), delta finite                */
+ssgd_status ssgd_orthogonal_step(float* x, size_t ldx, size_t stride_x, const void* g, int g_type, size_t ldg,
+                                 size_t stride_g, float* m, size_t ldm, size_t stride_m, size_t n, size_t rows,
+                                 size_t cols, float beta, float delta, int nesterov, const float* coefficients,
+                                 unsigned steps, int products, void* ws, unsigned* status, void* stream);
+
+/* Self-test of the bounded waits, one step of one contiguous matrix: bit 0 of *status set, the context stays usable.  Sides
+ * up to 256.                                                                                                           */
+ssgd_status ssgd_orthogonal_wait_selftest(const void* u, int u_type, size_t rows, size_t cols, const float* coefficients,
+                                          int products, void* out, int out_type, void* ws, unsigned* status, void* stream);
+
 /* The calls above with their arguments in one HOST block of 64-bit words, in the order of their parameters: pointers
  * and sizes as they are, other integers widened, a float as the bits of a double.  For callers whose foreign-function
  * interface costs by the argument (Python's ctypes: 0.6 us instead of 2 us a call).  NULL: SSGD_ERR_NULL.            */
@@ -480,6 +559,10 @@ ssgd_status ssgd_tensors_clip_block(const uint64_t* args);    /* 9 words  */
 ssgd_status ssgd_fp4_quantise_block(const uint64_t* args);    /* 13 words */
 ssgd_status ssgd_fp4_dequantise_block(const uint64_t* args);  /* 10 words */
 ssgd_status ssgd_fp4_matmul_block(const uint64_t* args);      /* 15 words */
+ssgd_status ssgd_xent_forward_block(const uint64_t* args);    /* 16 words */
+ssgd_status ssgd_xent_backward_block(const uint64_t* args);   /* 21 words */
+ssgd_status ssgd_orthogonalise_block(const uint64_t* args);   /* 19 words: the coefficients as three floats */
+ssgd_status ssgd_orthogonal_step_block(const uint64_t* args); /* 24 words, the same */
 
 #ifdef __cplusplus
 }

@@ -42,6 +42,7 @@ def lib() -> ctypes.CDLL:
             "(needs nvcc); there is no CPU fallback" % LIB_PATH)
     L = ctypes.CDLL(LIB_PATH)
     sz, f32, vp, ci = ctypes.c_size_t, ctypes.c_float, ctypes.c_void_p, ctypes.c_int
+    i64, u32 = ctypes.c_int64, ctypes.c_uint
     L.ssgd_words.restype = sz
     L.ssgd_words.argtypes = [sz]
     L.ssgd_density_from_sums.restype = ctypes.c_double
@@ -58,6 +59,8 @@ def lib() -> ctypes.CDLL:
     L.ssgd_fp4_scale_bytes.argtypes = [ci, sz, sz]
     L.ssgd_status_str.restype = ctypes.c_char_p
     L.ssgd_status_str.argtypes = [ci]
+    L.ssgd_orthogonal_ws_bytes.restype = sz
+    L.ssgd_orthogonal_ws_bytes.argtypes = [sz, sz, sz]
     sigs = {
         "ssgd_sign_pack": [vp, sz, sz, sz, vp, sz, vp],
         "ssgd_signum_momentum_pack": [vp, vp, sz, sz, sz, f32, vp, sz, vp],
@@ -91,6 +94,17 @@ def lib() -> ctypes.CDLL:
         "ssgd_fp4_quantise": [vp, ci, sz, sz, sz, ci, vp, vp, vp, vp, vp, vp, vp],
         "ssgd_fp4_dequantise": [vp, vp, vp, ci, sz, sz, vp, ci, sz, vp],
         "ssgd_fp4_matmul": [vp, vp, vp, vp, vp, vp, sz, sz, sz, ci, vp, ci, sz, vp, vp],
+        "ssgd_xent_sizes": [sz, sz, sz, vp, vp],
+        "ssgd_xent_forward": [vp, sz, vp, sz, ci, sz, sz, sz, vp, i64, vp, vp, vp, vp, vp, vp],
+        "ssgd_xent_wait_selftest": [vp, sz, vp, sz, ci, sz, sz, sz, vp, i64, vp, vp, vp, vp, vp, vp],
+        "ssgd_xent_backward": [vp, sz, vp, sz, ci, sz, sz, sz, vp, vp, vp, vp, sz, vp, sz, vp, ci, sz, vp, vp, vp],
+        "ssgd_orthogonalise": [vp, ci, sz, sz, sz, sz, sz, vp, u32, ci, vp, ci, sz, sz, vp, vp, vp],
+        "ssgd_orthogonal_wait_selftest": [vp, ci, sz, sz, vp, ci, vp, ci, vp, vp, vp],
+        "ssgd_orthogonal_step": [vp, sz, sz, vp, ci, sz, sz, vp, sz, sz, sz, sz, sz, f32, f32, ci, vp, u32, ci, vp, vp, vp],
+        "ssgd_xent_forward_block": [ctypes.c_char_p],
+        "ssgd_xent_backward_block": [ctypes.c_char_p],
+        "ssgd_orthogonalise_block": [ctypes.c_char_p],
+        "ssgd_orthogonal_step_block": [ctypes.c_char_p],
     }
     for name, args in sigs.items():
         fn = getattr(L, name)
@@ -618,3 +632,25 @@ def fp4_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, a_tensor_scale: Op
             _ptr(a_codes, u8, "a_codes"), _ptr(a_scales, u8, "a_scales"), _ptr(a_tensor_scale, f32, "a_tensor_scale"),
             _ptr(b_codes, u8, "b_codes"), _ptr(b_scales, u8, "b_scales"), _ptr(b_tensor_scale, f32, "b_tensor_scale"), M, N, K,
             FP4_FORMAT[fmt], at, DTYPE_CODE[out.dtype], ldo, _ptr(status, torch.int32, "status"), _stream(stream)), "ssgd_fp4_matmul")
+
+
+# --------------------------------------------------------------------------
+# the loss over a large vocabulary; orthogonalised updates (``loss`` and ``orthogonal`` call these with torch tensors)
+
+XENT_FORWARD_ARGS, XENT_BACKWARD_ARGS = struct.Struct("=9Qq6Q"), struct.Struct("=21Q")
+ORTHOGONALISE_ARGS, ORTHOGONAL_STEP_ARGS = struct.Struct("=7Q3d9Q"), struct.Struct("=13Q2dQ3d5Q")
+
+
+def xent_sizes(tokens: int, vocab: int, width: int):
+    """Workspace bytes of ssgd_xent_forward and ssgd_xent_backward on the current device."""
+    forward, backward = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib().ssgd_xent_sizes(tokens, vocab, width, ctypes.byref(forward), ctypes.byref(backward)), "ssgd_xent_sizes")
+    return forward.value, backward.value
+
+
+def orthogonal_ws_bytes(n: int, rows: int, cols: int) -> int:
+    """Workspace bytes of ssgd_orthogonalise and ssgd_orthogonal_step."""
+    size = lib().ssgd_orthogonal_ws_bytes(n, rows, cols)
+    if not size:
+        raise ValueError("%d matrices of %d x %d: at most 65535, sides up to 32768" % (n, rows, cols))
+    return int(size)

@@ -1,0 +1,578 @@
+// Cross entropy of a linear head over a large vocabulary, z = h w^T, without the logits: they live in tensor memory only, as
+// tiles.  See include/signsgd.h for the contract.
+//
+//   forward   a product of h and w whose epilogue keeps, for each token and each half tile of the vocabulary, the largest logit and
+//             the sum of exponentials below it, and the target's logit; a second kernel joins them (fixed order) to
+//             log sum exp and the loss
+//   backward  by pieces of the vocabulary: the logits' tiles once more, this time to dz = g (exp(z - lse) - [v = y]), rounded
+//             to the operands' type, which is what the two products take that follow: dh += dz w, dw = dz^T h (no operand
+//             is transposed in memory, the products read them either way)
+// Statistics, losses and all sums are fp32; dz is the one rounding to 16 bits, as large as that of the gradients
+// themselves.  An fp16 dz is scaled by a power of two, so that the largest |g| lies just below 2^15: a gradient of
+// 1/tokens times a probability would be below fp16's range.
+
+#include "half_product.cuh"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kInf = __builtin_inff();
+
+__device__ __forceinline__ float exp2_fast(float x) {   // 2 ulp; exp2(-inf) = 0
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// A maximum that may be subtracted: -inf - -inf would be NaN where all is -inf so far.
+__device__ __forceinline__ float base_of(float top) { return top == -kInf ? 0.0f : top; }
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Forward.
+
+// Each thread has one token and half of the tile's columns: a running maximum and sum, nothing to exchange.
+struct StatsEpilogue {
+  struct Args {
+    const int64_t* targets;
+    float2* partial;            // [2 * tiles_q][tokens]: maximum, sum
+    float* picked;              // [tokens]: the target's logit
+    unsigned tokens;
+  };
+  float top, sum;
+  int64_t target;
+  unsigned row, part;
+  __device__ StatsEpilogue(const Args&, unsigned char*) {}
+  __device__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned odd) {
+    row = row0 + lane;
+    part = 2 * at.tile_q + odd;
+    top = -kInf;
+    sum = 0.0f;
+    target = row < a.tokens ? a.targets[row] : -1;
+  }
+  __device__ void unit(const Args& a, unsigned column, unsigned left, const unsigned (&v)[32]) {
+    float z[32];
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) z[q] = __uint_as_float(v[q]);
+    if (left < 32) {
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q)
+        if (q >= left) z[q] = -kInf;
+    }
+    float m = top;
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) m = fmaxf(m, z[q]);
+    const float b = base_of(m);
+    float s0 = sum * exp2_fast((top - b) * kLog2e), s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+    for (unsigned q = 0; q < 32; q += 4) {
+      s0 += exp2_fast((z[q] - b) * kLog2e);
+      s1 += exp2_fast((z[q + 1] - b) * kLog2e);
+      s2 += exp2_fast((z[q + 2] - b) * kLog2e);
+      s3 += exp2_fast((z[q + 3] - b) * kLog2e);
+    }
+    sum = (s0 + s1) + (s2 + s3);
+    top = m;
+    const int64_t at = target - (int64_t)column;
+    if (at >= 0 && at < (int64_t)left) {
+      float picked = 0.0f;
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q)
+        if ((unsigned)at == q) picked = z[q];
+      a.picked[row] = picked;
+    }
+  }
+  __device__ void end(const Args& a, const HalfPlace&, unsigned) {
+    if (row < a.tokens) a.partial[(size_t)part * a.tokens + row] = make_float2(top, sum);
+  }
+  __device__ void finish() {}
+};
+
+// What the backward pass has to know of a token.
+constexpr uint8_t kCounts = 0, kIgnored = 1, kIgnoredNotFinite = 2;
+
+// Joins the parts of TOKENS tokens a CTA, its other threads side by side along the parts; then the losses, and a look at the
+// ignored tokens' rows of h: one that is not finite must not reach dw through 0 * inf.
+template <unsigned TOKENS, typename T>
+__global__ void __launch_bounds__(256)
+xent_join_kernel(const float2* __restrict__ partial, const float* __restrict__ picked, const int64_t* __restrict__ targets, int64_t ignore, unsigned tokens,
+                 unsigned parts, unsigned vocab, const T* __restrict__ h, size_t ldh, unsigned width, float* __restrict__ losses, float* __restrict__ lse,
+                 uint8_t* __restrict__ kinds) {
+  constexpr unsigned kSlices = 256 / TOKENS;
+  __shared__ float2 part[kSlices][TOKENS];
+  pdl_launch_dependents();
+  pdl_wait();
+  const unsigned i = threadIdx.x % TOKENS, slice = threadIdx.x / TOKENS, t0 = blockIdx.x * TOKENS, t = t0 + i;
+  float top = -kInf, sum = 0.0f;
+  if (t < tokens) {
+    for (unsigned p0 = slice; p0 < parts; p0 += 8 * kSlices) {
+      float2 v[8];
+#pragma unroll
+      for (unsigned u = 0; u < 8; ++u) v[u] = p0 + u * kSlices < parts ? partial[(size_t)(p0 + u * kSlices) * tokens + t] : make_float2(-kInf, 0.0f);
+      float m = top;
+#pragma unroll
+      for (unsigned u = 0; u < 8; ++u) m = fmaxf(m, v[u].x);
+      const float b = base_of(m);
+      sum *= exp2_fast((top - b) * kLog2e);
+#pragma unroll
+      for (unsigned u = 0; u < 8; ++u) sum += v[u].y * exp2_fast((v[u].x - b) * kLog2e);
+      top = m;
+    }
+  }
+  part[slice][i] = make_float2(top, sum);
+  __syncthreads();
+  if (threadIdx.x < TOKENS && t < tokens) {
+    float m = -kInf, s = 0.0f;
+    for (unsigned k = 0; k < kSlices; ++k) m = fmaxf(m, part[k][i].x);
+    const float b = base_of(m);
+    for (unsigned k = 0; k < kSlices; ++k) s += part[k][i].y * exp2_fast((part[k][i].x - b) * kLog2e);
+    const int64_t y = targets[t];
+    const bool ignored = y == ignore, inside = y >= 0 && y < (int64_t)vocab;
+    // a target that is neither ignored nor in the vocabulary: NaN, here and in the gradients
+    const float l = inside || ignored ? m + logf(s) : __uint_as_float(0x7FC00000u);
+    losses[t] = ignored ? 0.0f : inside ? (m - picked[t]) + logf(s) : l;
+    lse[t] = l;
+    if (!ignored) kinds[t] = kCounts;
+  }
+  // a warp for each ignored token
+  for (unsigned k = threadIdx.x / 32; k < TOKENS; k += 8) {
+    const unsigned row = t0 + k;
+    if (row >= tokens || targets[row] != ignore) continue;
+    bool finite = true;
+    for (unsigned c = threadIdx.x % 32; c < width; c += 32) finite &= isfinite(to_float(h[(size_t)row * ldh + c])) != 0;
+    finite = __all_sync(0xFFFFFFFFu, finite);
+    if (threadIdx.x % 32 == 0) kinds[row] = finite ? kIgnored : kIgnoredNotFinite;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Backward.
+
+// Before the products: the scale of an fp16 dz, and, only where an ignored token's row of h is not finite, a copy of h with the
+// ignored rows zero, which dw's product then takes for h.
+struct Prepared {
+  unsigned copied;              // h's copy is to be taken
+  float scale, unscale;         // of dz: powers of two, 1 for bf16
+  unsigned unused;
+};
+template <typename T, bool SCALED>
+__global__ void __launch_bounds__(256)
+xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__ g, size_t g_stride, unsigned tokens, const T* __restrict__ h, size_t ldh,
+                    unsigned width, T* __restrict__ copy, size_t ldc, Prepared* __restrict__ out) {
+  __shared__ unsigned part[8];
+  pdl_launch_dependents();
+  pdl_wait();
+  unsigned bad = 0;
+  for (unsigned t = threadIdx.x; t < tokens; t += 256) bad |= kinds[t] == kIgnoredNotFinite;
+  bad = __syncthreads_or((int)bad) != 0;
+  if (blockIdx.x == 0) {
+    unsigned top = 0;                                       // |g|'s bits are ordered as |g| is
+    if (SCALED) {
+      for (unsigned t = threadIdx.x; t < tokens; t += 256)
+        if (kinds[t] == kCounts) top = max(top, __float_as_uint(g[t * g_stride]) & 0x7FFFFFFFu);
+      top = __reduce_max_sync(0xFFFFFFFFu, top);
+      if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = top;
+      __syncthreads();
+      for (unsigned k = 0; k < 8; ++k) top = max(top, part[k]);
+    }
+    if (threadIdx.x == 0) {
+      // top = m 2^e, 1 <= m < 2: times 2^(14 - e) it lies in [2^14, 2^15); exponents kept where both powers are fp32 numbers
+      int e = SCALED && top >= 0x00800000u && top < 0x7F800000u ? 14 - ((int)(top >> 23) - 127) : 0;
+      if (SCALED && top > 0 && top < 0x00800000u) e = 126;
+      e = max(-126, min(126, e));
+      out->copied = bad;
+      out->scale = __uint_as_float((unsigned)(127 + e) << 23);
+      out->unscale = __uint_as_float((unsigned)(127 - e) << 23);
+      out->unused = 0;
+    }
+  }
+  if (!bad) return;
+  for (unsigned t = blockIdx.x; t < tokens; t += gridDim.x) {
+    const bool keep = kinds[t] == kCounts;
+    for (unsigned c = threadIdx.x; c < width; c += 256) copy[(size_t)t * ldc + c] = keep ? h[(size_t)t * ldh + c] : from_float<T>(0.0f);
+  }
+}
+
+template <typename T>
+struct GradEpilogue {
+  struct Args {
+    const int64_t* targets;
+    const float* lse;
+    const float* g;
+    const uint8_t* kinds;
+    const Prepared* prepared;
+    T* dz;                      // [tokens][lddz], columns of this piece
+    size_t g_stride, lddz;
+    unsigned tokens, first;     // first: column of the vocabulary at which the piece begins
+  };
+  float lse, g;
+  int64_t target;
+  T* out;
+  bool counts;
+  __device__ GradEpilogue(const Args&, unsigned char*) {}
+  __device__ void begin(const Args& a, const HalfPlace&, unsigned row0, unsigned lane, unsigned) {
+    const unsigned row = row0 + lane;
+    counts = false;
+    out = nullptr;
+    if (row >= a.tokens) return;
+    out = a.dz + (size_t)row * a.lddz;
+    counts = a.kinds[row] == kCounts;
+    lse = a.lse[row];
+    g = a.g[row * a.g_stride] * a.prepared->scale;
+    target = a.targets[row] - (int64_t)a.first;
+  }
+  __device__ void unit(const Args&, unsigned column, unsigned left, const unsigned (&v)[32]) {
+    if (!out) return;
+    float d[32];
+    if (counts) {
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) d[q] = exp2_fast((__uint_as_float(v[q]) - lse) * kLog2e);
+      const int64_t at = target - (int64_t)column;
+      if (at >= 0 && at < 32) {
+#pragma unroll
+        for (unsigned q = 0; q < 32; ++q)
+          if ((unsigned)at == q) d[q] -= 1.0f;
+      }
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) d[q] *= g;
+    } else {
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) d[q] = 0.0f;
+    }
+    store_row32(out + column, d, 32);               // a row of dz is padded to whole tiles
+  }
+  __device__ void end(const Args&, const HalfPlace&, unsigned) {}
+  __device__ void finish() {}
+};
+
+// dh: rows of tokens, those that are ignored zero.  Where the vocabulary is in several pieces the sums so far are in fp32; where k
+// is split, each split has a plane of its own.
+template <typename T>
+struct TokensEpilogue {
+  struct Args {
+    const uint8_t* kinds;
+    const Prepared* prepared;
+    float* sums;                // [splits][tokens][width], or null
+    T* out;                     // null while pieces are to come, and where splits are joined later
+    size_t ldo;
+    unsigned tokens, width, add;
+  };
+  float unscale;
+  T* out;
+  float* sums;
+  __device__ TokensEpilogue(const Args&, unsigned char*) {}
+  __device__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
+    const unsigned row = row0 + lane;
+    out = nullptr;
+    sums = nullptr;
+    if (row >= a.tokens) return;
+    unscale = a.kinds[row] == kCounts ? a.prepared->unscale : 0.0f;
+    if (a.out) out = a.out + (size_t)row * a.ldo;
+    if (a.sums) sums = a.sums + ((size_t)at.split * a.tokens + row) * a.width;
+  }
+  __device__ void unit(const Args& a, unsigned column, unsigned left, const unsigned (&v)[32]) {
+    if (!out && !sums) return;
+    float d[32];
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) d[q] = unscale == 0.0f ? 0.0f : __uint_as_float(v[q]);
+    if (a.add) {
+      float w[32];
+      load_row32(sums + column, w, left);
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) d[q] += w[q];
+    }
+    if (out) {
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) d[q] *= unscale;
+      store_row32(out + column, d, left);
+    } else {
+      store_row32(sums + column, d, left);
+    }
+  }
+  __device__ void end(const Args&, const HalfPlace&, unsigned) {}
+  __device__ void finish() {}
+};
+
+template <typename T>
+__global__ void __launch_bounds__(256)
+xent_planes_kernel(const float* __restrict__ sums, unsigned planes, size_t plane, const Prepared* __restrict__ prepared, unsigned width, T* __restrict__ out,
+                   size_t ldo) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= plane) return;
+  float s = 0.0f;
+  for (unsigned p0 = 0; p0 < planes; p0 += 8) {
+    float v[8];
+#pragma unroll
+    for (unsigned u = 0; u < 8; ++u) v[u] = p0 + u < planes ? sums[(p0 + u) * plane + i] : 0.0f;
+#pragma unroll
+    for (unsigned u = 0; u < 8; ++u) s += v[u];
+  }
+  out[i / width * ldo + i % width] = from_float<T>(s * prepared->unscale);
+}
+
+// dw: rows of the vocabulary.
+template <typename T>
+struct WeightEpilogue {
+  struct Args {
+    const Prepared* prepared;
+    T* out;
+    size_t ldo;
+    unsigned rows;
+  };
+  float unscale;
+  T* out;
+  __device__ WeightEpilogue(const Args& a, unsigned char*) { unscale = a.prepared->unscale; }
+  __device__ void begin(const Args& a, const HalfPlace&, unsigned row0, unsigned lane, unsigned) {
+    out = row0 + lane < a.rows ? a.out + (size_t)(row0 + lane) * a.ldo : nullptr;
+  }
+  __device__ void unit(const Args&, unsigned column, unsigned left, const unsigned (&v)[32]) {
+    if (!out) return;
+    float d[32];
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) d[q] = __uint_as_float(v[q]) * unscale;
+    store_row32(out + column, d, left);
+  }
+  __device__ void end(const Args&, const HalfPlace&, unsigned) {}
+  __device__ void finish() {}
+};
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Host side.
+
+constexpr size_t kSide = (size_t)1 << 30;
+inline size_t up(size_t n, size_t k) { return (n + k - 1) / k * k; }
+
+struct HeadSizes {
+  size_t parts;                             // most partial statistics of a token: two for each 64 columns
+  size_t forward_bytes;
+  size_t piece, pieces;                     // columns of the vocabulary at a time
+  unsigned splits;                          // of dh's k, the vocabulary
+  size_t prepared, copy, copy_ld, dz, dz_ld, sums, backward_bytes;       // offsets and row lengths
+};
+
+// Pieces: dz of a piece is at most 2^27 numbers (256 MB), in whole 256 columns.
+constexpr size_t kPieceElements = (size_t)1 << 27;
+inline bool head_sizes(size_t T, size_t V, size_t D, int sms, HeadSizes* s) {
+  if (T < 1 || V < 1 || D < 1 || T > kSide || V > kSide || D > kSide || T > ((size_t)1 << 44) / V || T > ((size_t)1 << 44) / D) return false;
+  s->parts = 2 * ((V + 63) / 64);
+  s->forward_bytes = up(T * 4, 16) + s->parts * T * sizeof(float2);
+  const size_t columns = up(V, 256);
+  s->piece = up(kPieceElements / T < 256 ? 256 : kPieceElements / T / 256 * 256, 256);
+  if (s->piece > columns) s->piece = columns;
+  s->pieces = (V + s->piece - 1) / s->piece;
+  // few tiles of dh and a long k: split it, four stages or more each
+  const size_t tiles = (T + 127) / 128 * ((D + 63) / 64), stages = (V + 63) / 64;
+  size_t splits = s->pieces > 1 || tiles * 2 > (size_t)sms ? 1 : (size_t)sms / tiles;
+  if (splits > stages / 4) splits = stages / 4 < 1 ? 1 : stages / 4;
+  s->splits = (unsigned)splits;
+  size_t at = 0;
+  s->prepared = at; at += 64;
+  s->copy = at; s->copy_ld = up(D, 8); at += up(T * s->copy_ld * 2, 128);
+  s->dz = at; s->dz_ld = s->piece; at += up(T * s->dz_ld * 2, 128);
+  s->sums = at;
+  if (s->pieces > 1 || s->splits > 1) at += up(s->splits * T * D * 4, 128);
+  s->backward_bytes = at;
+  return true;
+}
+
+ssgd_status check_head(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V, size_t D, const int64_t* targets, const void* ws,
+                       const unsigned* status) {
+  if (dtype != SSGD_BF16 && dtype != SSGD_F16) return SSGD_ERR_ARG;
+  if (V < 1 || D < 1 || T > kSide || V > kSide || D > kSide || ldh < D || ldw < D || ldh >= (size_t)1 << 38 || ldw >= (size_t)1 << 38) return SSGD_ERR_SIZE;
+  if (T == 0) return SSGD_OK;
+  if (!h || !w || !targets || !ws || !status) return SSGD_ERR_NULL;
+  if (!aligned16(h) || !aligned16(w) || ldh % 8 != 0 || ldw % 8 != 0 || !aligned16(ws) || (reinterpret_cast<uintptr_t>(targets) & 7u) ||
+      (reinterpret_cast<uintptr_t>(status) & 3u))
+    return SSGD_ERR_ALIGN;
+  return SSGD_OK;
+}
+
+template <typename T>
+ssgd_status head_forward(const T* h, size_t ldh, const T* w, size_t ldw, size_t tokens, size_t vocab, size_t width, const int64_t* targets, int64_t ignore,
+                         float* losses, float* lse, uint8_t* kinds, void* ws, unsigned* status, unsigned starve, int sms, cudaStream_t s) {
+  HalfProduct p = {};
+  p.p = {h, nullptr, ldh, 0, false};
+  p.q = {w, nullptr, ldw, 0, false};
+  p.P = tokens; p.Q = vocab; p.K = width; p.batch = 1;
+  p.bf16 = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value;
+  p.status = status;
+  p.starve = starve;
+  const HalfForm form = half_form(p, 1, 1, sms);
+  float* picked = static_cast<float*>(ws);
+  float2* partial = reinterpret_cast<float2*>(static_cast<char*>(ws) + up(tokens * 4, 16));
+  const StatsEpilogue::Args args = {targets, partial, picked, (unsigned)tokens};
+  const ssgd_status st = launch_half<StatsEpilogue, 1>(p, args, form, 1, sms, s);
+  if (st != SSGD_OK) return st;
+  const unsigned parts = 2 * (unsigned)((vocab + form.nt - 1) / form.nt);
+  if (tokens <= 256)
+    launch_kernel(xent_join_kernel<4, T>, dim3((unsigned)(tokens + 3) / 4), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
+                  (unsigned)vocab, h, ldh, (unsigned)width, losses, lse, kinds);
+  else
+    launch_kernel(xent_join_kernel<32, T>, dim3((unsigned)(tokens + 31) / 32), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
+                  (unsigned)vocab, h, ldh, (unsigned)width, losses, lse, kinds);
+  return launch_status();
+}
+
+struct HeadBackward {
+  const void *h, *w;
+  size_t ldh, ldw, T, V, D;
+  const int64_t* targets;
+  const float* lse;
+  const uint8_t* kinds;
+  const float* g;
+  size_t g_stride;
+  void* dh;
+  size_t lddh;
+  void* dw;
+  int dw_type;
+  size_t lddw;
+  char* ws;
+  unsigned* status;
+};
+
+template <typename O>
+ssgd_status weight_product(const HalfProduct& p, const HeadBackward& b, const Prepared* prepared, size_t first, size_t rows, int sms, cudaStream_t s) {
+  const typename WeightEpilogue<O>::Args args = {prepared, static_cast<O*>(b.dw) + first * b.lddw, b.lddw, (unsigned)rows};
+  return launch_half<WeightEpilogue<O>, 1>(p, args, half_form(p, 1, 1, sms), 1, sms, s);
+}
+
+template <typename T>
+ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  HeadSizes z;
+  if (!head_sizes(b.T, b.V, b.D, sms, &z)) return SSGD_ERR_SIZE;
+  const T *h = static_cast<const T*>(b.h), *w = static_cast<const T*>(b.w);
+  Prepared* prepared = reinterpret_cast<Prepared*>(b.ws + z.prepared);
+  T *copy = reinterpret_cast<T*>(b.ws + z.copy), *dz = reinterpret_cast<T*>(b.ws + z.dz);
+  float* sums = reinterpret_cast<float*>(b.ws + z.sums);
+  const unsigned tokens = (unsigned)b.T, width = (unsigned)b.D;
+  launch_kernel(xent_prepare_kernel<T, !kBf16>, dim3(tokens < (unsigned)sms * 4 ? tokens : (unsigned)sms * 4), dim3(256), 0, s, true, b.kinds, b.g, b.g_stride,
+                tokens, h, b.ldh, width, copy, z.copy_ld, prepared);
+  ssgd_status st = launch_status();
+  for (size_t first = 0; st == SSGD_OK && first < b.V; first += z.piece) {
+    const size_t columns = b.V - first < z.piece ? b.V - first : z.piece;
+    const T* w_piece = w + first * b.ldw;
+    const bool last = first + columns == b.V;
+    HalfProduct p = {};
+    p.batch = 1;
+    p.bf16 = kBf16;
+    p.status = b.status;
+    p.p = {h, nullptr, b.ldh, 0, false};
+    p.q = {w_piece, nullptr, b.ldw, 0, false};
+    p.P = b.T; p.Q = columns; p.K = b.D;
+    const typename GradEpilogue<T>::Args grad = {b.targets, b.lse, b.g, b.kinds, prepared, dz, b.g_stride, z.dz_ld, tokens, (unsigned)first};
+    st = launch_half<GradEpilogue<T>, 1>(p, grad, half_form(p, 1, 1, sms), 1, sms, s);
+    if (st != SSGD_OK) break;
+    if (b.dh) {
+      p.p = {dz, nullptr, z.dz_ld, 0, false};
+      p.q = {w_piece, nullptr, b.ldw, 0, true};
+      p.P = b.T; p.Q = b.D; p.K = columns;
+      T* out = last && z.splits == 1 ? static_cast<T*>(b.dh) : nullptr;
+      const typename TokensEpilogue<T>::Args args = {b.kinds, prepared, z.pieces > 1 || z.splits > 1 ? sums : nullptr, out, b.lddh, tokens, width, first > 0};
+      st = launch_half<TokensEpilogue<T>, 1>(p, args, half_form(p, 1, z.splits, sms), z.splits, sms, s);
+      if (st == SSGD_OK && z.splits > 1) {
+        const size_t plane = b.T * b.D;
+        launch_kernel(xent_planes_kernel<T>, dim3(grid_for((plane + 255) / 256)), dim3(256), 0, s, true, sums, z.splits, plane, prepared, width,
+                      static_cast<T*>(b.dh), b.lddh);
+        st = launch_status();
+      }
+    }
+    if (st == SSGD_OK && b.dw) {
+      p.p = {dz, nullptr, z.dz_ld, 0, true};
+      p.q = {h, nullptr, b.ldh, 0, true};
+      p.P = columns; p.Q = b.D; p.K = b.T;
+      HalfProduct other = p;
+      other.q_other = copy;
+      other.q_choice = &prepared->copied;
+      other.q_other_ld = z.copy_ld;
+      st = b.dw_type == SSGD_F32    ? weight_product<float>(other, b, prepared, first, columns, sms, s)
+           : b.dw_type == SSGD_BF16 ? weight_product<__nv_bfloat16>(other, b, prepared, first, columns, sms, s)
+                                    : weight_product<__half>(other, b, prepared, first, columns, sms, s);
+    }
+  }
+  return st;
+}
+
+ssgd_status checked_forward(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V, size_t D, const int64_t* targets,
+                            int64_t ignore, float* losses, float* lse, uint8_t* kinds, void* ws, unsigned* status, unsigned starve, void* stream) {
+  const ssgd_status st = check_head(h, ldh, w, ldw, dtype, T, V, D, targets, ws, status);
+  if (st != SSGD_OK || T == 0) return st;
+  if (!losses || !lse || !kinds) return SSGD_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(losses) | reinterpret_cast<uintptr_t>(lse)) & 3u) return SSGD_ERR_ALIGN;
+  DeviceInfo info;
+  if (!device_info(&info)) return SSGD_ERR_CUDA;
+  HeadSizes z;
+  if (!head_sizes(T, V, D, info.sms, &z)) return SSGD_ERR_SIZE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return dtype == SSGD_BF16 ? head_forward(static_cast<const __nv_bfloat16*>(h), ldh, static_cast<const __nv_bfloat16*>(w), ldw, T, V, D, targets, ignore,
+                                           losses, lse, kinds, ws, status, starve, info.sms, s)
+                            : head_forward(static_cast<const __half*>(h), ldh, static_cast<const __half*>(w), ldw, T, V, D, targets, ignore, losses, lse,
+                                           kinds, ws, status, starve, info.sms, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+ssgd_status ssgd_xent_sizes(size_t T, size_t V, size_t D, size_t* forward_bytes, size_t* backward_bytes) {
+  if (!forward_bytes || !backward_bytes) return SSGD_ERR_NULL;
+  *forward_bytes = *backward_bytes = 16;
+  if (T == 0 && V >= 1 && D >= 1) return SSGD_OK;
+  DeviceInfo info;
+  if (!device_info(&info)) return SSGD_ERR_CUDA;
+  HeadSizes z;
+  if (!head_sizes(T, V, D, info.sms, &z)) return SSGD_ERR_SIZE;
+  *forward_bytes = z.forward_bytes;
+  *backward_bytes = z.backward_bytes;
+  return SSGD_OK;
+}
+
+ssgd_status ssgd_xent_forward(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V, size_t D, const int64_t* targets,
+                              int64_t ignore, float* losses, float* lse, uint8_t* kinds, void* ws, unsigned* status, void* stream) {
+  return checked_forward(h, ldh, w, ldw, dtype, T, V, D, targets, ignore, losses, lse, kinds, ws, status, 0, stream);
+}
+
+ssgd_status ssgd_xent_wait_selftest(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V, size_t D, const int64_t* targets,
+                                    int64_t ignore, float* losses, float* lse, uint8_t* kinds, void* ws, unsigned* status, void* stream) {
+  if (T > 256 || V > 256 || D > 128) return SSGD_ERR_SIZE;      // one round of tiles, two stages: the waits run out once
+  return checked_forward(h, ldh, w, ldw, dtype, T, V, D, targets, ignore, losses, lse, kinds, ws, status, 16, stream);
+}
+
+ssgd_status ssgd_xent_backward(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V, size_t D, const int64_t* targets,
+                               const float* lse, const uint8_t* kinds, const float* g, size_t g_stride, void* dh, size_t lddh, void* dw, int dw_type,
+                               size_t lddw, void* ws, unsigned* status, void* stream) {
+  const ssgd_status st = check_head(h, ldh, w, ldw, dtype, T, V, D, targets, ws, status);
+  if (st != SSGD_OK) return st;
+  if (dw && dtype_bytes((unsigned)dw_type) == 0) return SSGD_ERR_ARG;
+  if ((dh && lddh < D) || (dw && (lddw < D || mul_overflows(V, lddw) || mul_overflows(V * lddw, 4)))) return SSGD_ERR_SIZE;
+  if ((dh && (reinterpret_cast<uintptr_t>(dh) & 1u)) || (dw && reinterpret_cast<uintptr_t>(dw) % dtype_bytes((unsigned)dw_type) != 0)) return SSGD_ERR_ALIGN;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (T == 0) {
+    if (!dw) return SSGD_OK;
+    const size_t e = dtype_bytes((unsigned)dw_type);
+    return cudaMemset2DAsync(dw, lddw * e, 0, D * e, V, s) == cudaSuccess ? SSGD_OK : SSGD_ERR_CUDA;
+  }
+  if (!lse || !kinds || !g) return SSGD_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(g)) & 3u) return SSGD_ERR_ALIGN;
+  if (!dh && !dw) return SSGD_OK;
+  DeviceInfo info;
+  if (!device_info(&info)) return SSGD_ERR_CUDA;
+  const HeadBackward b = {h, w, ldh, ldw, T, V, D, targets, lse, kinds, g, g_stride, dh, lddh, dw, dw_type, lddw, static_cast<char*>(ws), status};
+  return dtype == SSGD_BF16 ? head_backward<__nv_bfloat16>(b, info.sms, s) : head_backward<__half>(b, info.sms, s);
+}
+
+ssgd_status ssgd_xent_forward_block(const uint64_t* a) {
+  if (!a) return SSGD_ERR_NULL;
+  return ssgd_xent_forward(block_ptr<const void>(a[0]), a[1], block_ptr<const void>(a[2]), a[3], (int)a[4], a[5], a[6], a[7], block_ptr<const int64_t>(a[8]),
+                           (int64_t)a[9], block_ptr<float>(a[10]), block_ptr<float>(a[11]), block_ptr<uint8_t>(a[12]), block_ptr<void>(a[13]),
+                           block_ptr<unsigned>(a[14]), block_ptr<void>(a[15]));
+}
+
+ssgd_status ssgd_xent_backward_block(const uint64_t* a) {
+  if (!a) return SSGD_ERR_NULL;
+  return ssgd_xent_backward(block_ptr<const void>(a[0]), a[1], block_ptr<const void>(a[2]), a[3], (int)a[4], a[5], a[6], a[7], block_ptr<const int64_t>(a[8]),
+                            block_ptr<const float>(a[9]), block_ptr<const uint8_t>(a[10]), block_ptr<const float>(a[11]), a[12], block_ptr<void>(a[13]), a[14],
+                            block_ptr<void>(a[15]), (int)a[16], a[17], block_ptr<void>(a[18]), block_ptr<unsigned>(a[19]), block_ptr<void>(a[20]));
+}
+
+}  // extern "C"

@@ -27,6 +27,7 @@
 #include "dtypes.cuh"
 #include "fp4.cuh"
 #include "sm100.cuh"
+#include "tensor_map.h"
 
 namespace {
 
@@ -528,24 +529,6 @@ fp4_matmul_pair_kernel(const __grid_constant__ CUtensorMap p_map, const __grid_c
     tcgen05_fence_after();
     tmem_free_pair(tmem, 512);
   }
-}
-
-// cuTensorMapEncodeTiled, found through the runtime so that the library needs no link to the driver.
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled encode_tiled() {
-  static EncodeTiled cached = nullptr;          // any thread stores the same value
-  EncodeTiled f = __atomic_load_n(&cached, __ATOMIC_RELAXED);
-  if (f) return f;
-  void* p = nullptr;
-  cudaDriverEntryPointQueryResult found;
-  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-      found != cudaDriverEntryPointSuccess)
-    return nullptr;
-  f = reinterpret_cast<EncodeTiled>(p);
-  __atomic_store_n(&cached, f, __ATOMIC_RELAXED);
-  return f;
 }
 
 // Codes as a byte matrix, in boxes of 128 bytes x `box_rows`, 128-byte swizzle, zero beyond the edges.

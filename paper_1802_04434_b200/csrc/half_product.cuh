@@ -1,0 +1,429 @@
+// Products of 16-bit operands on the tensor cores, out[i][j] = sum_k P[i][k] Q[j][k] in fp32, with what becomes of the sums left to
+// the caller: a class that takes 32 neighbouring columns of one row at a time (an epilogue).
+//
+// A persistent CTA, or pair of CTAs (cta_group::2), takes tiles of 128 (256) rows of P by NT rows of Q in turn.  P's rows are the
+// accumulator's lanes, so a thread of the epilogue has neighbours of one row, and what is summed along a row (a softmax)
+// needs no exchange between threads.
+//   warp 0      one thread brings stages of 64 of k (tiled copies, 128-byte swizzle, zeros beyond the edges)
+//   warp 1      one thread issues the MMAs, four of 16 of k a stage
+//   warps 2..9  read the accumulators, two warps to a quarter of the lanes, 32 columns in turn; two accumulators, so that a tile
+//               is written out while the next is multiplied
+// An operand may lie in memory with its k side by side, or with its rows side by side (a matrix that another product
+// takes the other way round): the copies and the tensor cores take both, nothing is transposed.
+// TERMS = 3: each operand is a sum of two fp16 matrices, high and low part (22 bits together); high * high, high * low and low * high
+// go into the same sum, low * low is below the last bit that counts.
+// Every wait has an iteration limit and reports through a status word, as in the 4-bit product.
+#ifndef SSGD_HALF_PRODUCT_CUH_
+#define SSGD_HALF_PRODUCT_CUH_
+
+#include <type_traits>
+
+#include "host_calls.h"
+#include "dtypes.cuh"
+#include "sm100.cuh"
+#include "tensor_map.h"
+
+namespace {
+
+constexpr int kHalfThreads = 320;
+constexpr unsigned kHalfPolls = 200000;           // bound of a wait, about 0.2 s
+
+struct HalfMaps {
+  CUtensorMap p[2], q[2];                         // high and low part (TERMS = 3); TERMS = 1: q[1] may be another choice for q
+};
+
+struct HalfPlan {
+  unsigned P, Q;                                  // rows of the operands of one matrix
+  unsigned k_stages, k_chunks;                    // k in pieces of 64 and of 16
+  unsigned tiles_p, tiles_q, per_matrix, tiles;   // tiles: per matrix, and of all matrices and splits
+  unsigned splits;                                // pieces of k that are summed apart
+  unsigned p_by_rows, q_by_rows;                  // the operand lies with its rows side by side
+  unsigned p_box;                                 // rows of P that a CTA loads: fewer than 128 where P has fewer
+  unsigned idesc;
+  unsigned symmetric;                             // only tiles that reach the diagonal or lie above it
+  unsigned starve;                                // bytes that a stage waits for in vain: 0 but in the self-test of the waits
+  const unsigned* q_choice;                       // not null: where it points to non-zero, q[1] is taken for q[0]
+  unsigned* status;
+};
+
+struct HalfPlace { unsigned matrix, split, p0, q0, tile, tile_q, rows; };      // rows: of P in a tile
+
+template <bool PAIR, int NT, int TERMS>
+struct HalfShape {
+  static constexpr unsigned rows = PAIR ? 256 : 128;                       // of P in a tile
+  static constexpr unsigned q_rows = PAIR ? NT / 2 : NT;                   // of Q that a CTA loads
+  static constexpr unsigned parts = TERMS == 3 ? 2 : 1;
+  static constexpr unsigned p_bytes = 128 * 128, q_bytes = q_rows * 128;
+  static constexpr unsigned stage_bytes = parts * (p_bytes + q_bytes);
+  static constexpr unsigned box_bytes = 4096, out_bytes = 8 * box_bytes;   // the eight warps' room on the way out
+  static constexpr unsigned bar_bytes = 256;
+  static constexpr unsigned room = 232448 - out_bytes - bar_bytes;
+  static constexpr unsigned stages = room / stage_bytes < 8 ? room / stage_bytes : 8;
+  static constexpr unsigned columns = 2 * NT;                              // two accumulators
+  // more than half of an SM's shared memory always: CTAs that hold and wait for tensor memory on one SM would never end
+  static constexpr unsigned needed = stages * stage_bytes + out_bytes + bar_bytes;
+  static constexpr unsigned smem = needed < 118784 ? 118784 : needed;
+  static_assert(stages >= 3 && (2 * stages + 5) * 8 + 8 <= bar_bytes && columns <= 512 && q_rows % 64 == 0, "shape");
+};
+
+// Tiles go through bands of eight of P's tiles, so that those in flight share rows of both operands.
+template <bool PAIR, int NT>
+__device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p) {
+  constexpr unsigned rows = PAIR ? 256 : 128, kBand = 8;
+  const unsigned z = tile / p.per_matrix, in_matrix = tile - z * p.per_matrix;
+  HalfPlace at;
+  at.matrix = z / p.splits;
+  at.split = z - at.matrix * p.splits;
+  at.tile = in_matrix;
+  if (p.symmetric) {
+    unsigned i = 0, left = in_matrix;
+    while (left >= p.tiles_q - i * (rows / NT)) left -= p.tiles_q - i++ * (rows / NT);
+    at.p0 = i * rows;
+    at.q0 = (i * (rows / NT) + left) * NT;
+  } else {
+    const unsigned band = in_matrix / (kBand * p.tiles_q), in = in_matrix - band * kBand * p.tiles_q, high = min(kBand, p.tiles_p - band * kBand);
+    at.p0 = (band * kBand + in % high) * rows;
+    at.q0 = in / high * NT;
+  }
+  at.tile_q = at.q0 / NT;
+  at.rows = rows;
+  return at;
+}
+
+// What an epilogue offers, besides its Args:
+//   begin(args, place, row, tile of this CTA's rows)   before the first columns of a tile; row: this thread's
+//   unit(args, column, left, v)                        32 accumulators of columns column .., `left` of them inside
+//   end(args, place, warp)                             behind the last; every thread of the warp calls it
+template <class Epilogue, bool PAIR, int NT, int TERMS>
+__global__ void __launch_bounds__(kHalfThreads, 1)
+half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, const typename Epilogue::Args args) {
+  using S = HalfShape<PAIR, NT, TERMS>;
+  extern __shared__ __align__(1024) unsigned char half_smem[];           // stages, boxes, barriers; the same place in both CTAs
+  uint64_t* bars = reinterpret_cast<uint64_t*>(half_smem + S::stages * S::stage_bytes + S::out_bytes);
+  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 5), &failed = *(&tmem_base + 1);
+  const unsigned rank = PAIR ? cluster_rank() : 0;
+  const unsigned stage0 = smem_u32(half_smem);
+  const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 16, ended = acc_free + 16;
+  const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const unsigned worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
+
+  if (threadIdx.x == 0) {
+    prefetch_tensor_map(&maps.p[0]);
+    prefetch_tensor_map(&maps.q[0]);
+    for (unsigned s = 0; s < S::stages; ++s) {
+      mbarrier_init(full + 8 * s, 1);
+      mbarrier_init(empty + 8 * s, 1);
+    }
+    for (unsigned b = 0; b < 2; ++b) {
+      mbarrier_init(acc_full + 8 * b, 1);
+      mbarrier_init(acc_free + 8 * b, PAIR ? 16 : 8);     // one arrival from each of the CTAs' eight epilogue warps
+    }
+    mbarrier_init(ended, 1);
+    mbarrier_init_fence();
+    failed = 0;
+  }
+  pdl_launch_dependents();
+  pdl_wait();                                   // before tensor memory is taken: its last holder has finished
+  if (warp == 1) {
+    if (PAIR) tmem_alloc_pair(smem_u32(&tmem_base), S::columns);
+    else tmem_alloc(smem_u32(&tmem_base), S::columns);
+  }
+  tcgen05_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync();                     // the other CTA's barriers are ready too
+  tcgen05_fence_after();
+  const unsigned tmem = tmem_base;
+  bool ok = true;
+  unsigned n = 0;                               // stages so far, over all tiles
+
+  if (warp == 0) {
+    if (elect_one()) {
+      const CUtensorMap* q_high = p.q_choice && *p.q_choice ? &maps.q[1] : &maps.q[0];
+      const unsigned p_loaded = p.p_by_rows ? S::p_bytes : p.p_box * 128;
+      const unsigned expected = (PAIR ? 2 : 1) * S::parts * (p_loaded + S::q_bytes) + p.starve;
+      for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
+        const HalfPlace at = half_place<PAIR, NT>(tile, p);
+        const int p0 = (int)(at.p0 + rank * 128), q0 = (int)(at.q0 + rank * S::q_rows), z = (int)at.matrix;
+        const unsigned first = (unsigned)((uint64_t)p.k_stages * at.split / p.splits), last = (unsigned)((uint64_t)p.k_stages * (at.split + 1) / p.splits);
+        for (unsigned k = first; k < last; ++k, ++n) {
+          const unsigned s = n % S::stages;
+          if (n >= S::stages) ok = mbarrier_wait(empty + 8 * s, (n / S::stages - 1) & 1u, kHalfPolls);
+          if (!ok) break;
+          const unsigned base = stage0 + s * S::stage_bytes;
+          const unsigned bar = PAIR ? cluster_address(full + 8 * s, 0) : full + 8 * s;
+          if (rank == 0) mbarrier_expect(full + 8 * s, expected);
+          const int k0 = (int)(k * 64);
+          auto load = [&](unsigned dst, const CUtensorMap* map, int x, int y) {
+            if (PAIR) tma_load_3d_pair(dst, map, x, y, z, bar);
+            else tma_load_3d(dst, map, x, y, z, bar);
+          };
+#pragma unroll
+          for (unsigned h = 0; h < S::parts; ++h) {
+            const unsigned pd = base + h * (S::p_bytes + S::q_bytes), qd = pd + S::p_bytes;
+            const CUtensorMap* qm = h == 0 ? q_high : &maps.q[1];
+            if (p.p_by_rows) {
+#pragma unroll
+              for (unsigned j = 0; j < 2; ++j) load(pd + j * 8192, &maps.p[h], p0 + (int)(64 * j), k0);
+            } else {
+              load(pd, &maps.p[h], k0, p0);
+            }
+            if (p.q_by_rows) {
+#pragma unroll
+              for (unsigned j = 0; j < S::q_rows / 64; ++j) load(qd + j * 8192, qm, q0 + (int)(64 * j), k0);
+            } else {
+              load(qd, qm, k0, q0);
+            }
+          }
+        }
+      }
+      // the last stages' commits have to arrive before this CTA may go
+      for (unsigned m = n > S::stages ? n - S::stages : 0; m < n && ok; ++m)
+        ok = mbarrier_wait(empty + 8 * (m % S::stages), (m / S::stages) & 1u, kHalfPolls);
+    }
+  } else if (warp == 1) {
+    if (rank == 0 && elect_one()) {
+      const uint64_t p_desc = half_descriptor(stage0, p.p_by_rows), q_desc = half_descriptor(stage0 + S::p_bytes, p.q_by_rows);
+      const unsigned p_step = p.p_by_rows ? 2048 >> 4 : 32 >> 4, q_step = p.q_by_rows ? 2048 >> 4 : 32 >> 4;    // 16 of k
+      constexpr unsigned low = (S::p_bytes + S::q_bytes) >> 4;
+      unsigned s = 0, parity = 0;
+      bool ready = false;                       // the next stage's operands are known to be there
+      unsigned t = 0;                           // tiles so far
+      for (unsigned tile = worker; tile < p.tiles && ok; tile += workers, ++t) {
+        if (t > 1) ok = PAIR ? mbarrier_wait_cluster(acc_free + 8 * (t & 1u), (t / 2 - 1) & 1u, kHalfPolls)
+                             : mbarrier_wait(acc_free + 8 * (t & 1u), (t / 2 - 1) & 1u, kHalfPolls);
+        if (!ok) break;
+        tcgen05_fence_after();
+        const unsigned d = tmem + (t & 1u) * NT;
+        const unsigned split = tile / p.per_matrix % p.splits;
+        const unsigned first = (unsigned)((uint64_t)p.k_stages * split / p.splits), last = (unsigned)((uint64_t)p.k_stages * (split + 1) / p.splits);
+        for (unsigned k = first; k < last; ++k, ++n) {
+          ok = ready || mbarrier_wait(full + 8 * s, parity, kHalfPolls);
+          if (!ok) break;
+          tcgen05_fence_after();
+          const unsigned next = s + 1 == S::stages ? 0 : s + 1, next_parity = parity ^ (next == 0);
+          ready = mbarrier_test(full + 8 * next, next_parity);    // its answer comes while this stage is issued
+          const uint64_t pd = p_desc + s * (S::stage_bytes >> 4), qd = q_desc + s * (S::stage_bytes >> 4);
+          const unsigned chunks = p.k_chunks - k * 4;
+#pragma unroll
+          for (unsigned c = 0; c < 4; ++c) {
+            if (c == 0 || c < chunks) {
+              const uint64_t pc = pd + c * p_step, qc = qd + c * q_step;
+              mma_half<PAIR>(d, pc, qc, p.idesc, k > first || c > 0);
+              if constexpr (TERMS == 3) {
+                mma_half<PAIR>(d, pc, qc + low, p.idesc, true);
+                mma_half<PAIR>(d, pc + low, qc, p.idesc, true);
+              }
+            }
+          }
+          if (PAIR) tcgen05_commit_pair(empty + 8 * s);
+          else tcgen05_commit(empty + 8 * s);
+          s = next;
+          parity = next_parity;
+        }
+        if (ok) {
+          if (PAIR) tcgen05_commit_pair(acc_full + 8 * (t & 1u));
+          else tcgen05_commit(acc_full + 8 * (t & 1u));
+        }
+      }
+      if (!ok) {                                // what was issued has to end before tensor memory is freed; nobody writes it out
+        if (PAIR) tcgen05_commit_pair(ended);
+        else tcgen05_commit(ended);
+        (void)mbarrier_wait(ended, 0, kHalfPolls);
+      }
+    }
+  } else {
+    constexpr unsigned kUnits = NT / 32;
+    const unsigned quarter = warp & 3u, odd = warp >= 6;
+    const unsigned go = PAIR ? cluster_address(acc_free, 0) : acc_free;
+    Epilogue epilogue(args, half_smem + S::stages * S::stage_bytes + (warp - 2) * S::box_bytes);
+    unsigned t = 0;
+    for (unsigned tile = worker; tile < p.tiles; tile += workers, ++t) {
+      const HalfPlace at = half_place<PAIR, NT>(tile, p);
+      const unsigned row0 = at.p0 + rank * 128 + quarter * 32;
+      epilogue.begin(args, at, row0, lane, odd);
+      ok = mbarrier_wait(acc_full + 8 * (t & 1u), (t / 2) & 1u, 4 * kHalfPolls + 64 * p.k_stages);
+      if (!ok) break;
+      tcgen05_fence_after();
+      const unsigned lanes = tmem + (t & 1u) * NT + (quarter << 21);
+#pragma unroll 1
+      for (unsigned unit = odd; unit < kUnits; unit += 2) {
+        unsigned v[32];
+        tmem_read32(lanes + unit * 32, v);
+        if (unit + 2 >= kUnits) {               // this warp's last columns
+          tcgen05_fence_before();
+          __syncwarp();
+          if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t & 1u));
+        }
+        const unsigned column = at.q0 + unit * 32;
+        if (row0 < p.P && column < p.Q) epilogue.unit(args, column, min(32u, p.Q - column), v);
+        __syncwarp();
+      }
+      epilogue.end(args, at, rank * 8 + warp - 2);
+      __syncwarp();
+    }
+    epilogue.finish();
+  }
+  if (!ok) atomicExch(&failed, 1u);
+  __syncwarp();
+  __syncthreads();
+  if (failed) {
+    // copies that were asked for, here and by the other CTA, have to land before the memory is given up
+    if (threadIdx.x == 0) atomicOr(p.status, 1u);
+    if (rank == 0 && warp == 0)
+      for (unsigned m = n > S::stages ? n - S::stages : 0; m < n; ++m)
+        (void)mbarrier_wait(full + 8 * (m % S::stages), (m / S::stages) & 1u, kHalfPolls);
+  }
+  __syncthreads();
+  if (PAIR) cluster_sync();
+  if (warp == 1) {
+    tcgen05_fence_after();
+    if (PAIR) tmem_free_pair(tmem, S::columns);
+    else tmem_free(tmem, S::columns);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// What epilogues share: 32 neighbours of a row between a thread and memory.
+
+// Any place, `left` of them.
+template <typename T>
+__device__ __forceinline__ void store_row32(T* o, const float (&v)[32], unsigned left) {
+  if (left >= 32 && (reinterpret_cast<uintptr_t>(o) & 15u) == 0) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (unsigned q = 0; q < 8; ++q) reinterpret_cast<float4*>(o)[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+    } else {
+#pragma unroll
+      for (unsigned q = 0; q < 4; ++q)
+        reinterpret_cast<uint4*>(o)[q] = make_uint4(pack2(T(), v[8 * q], v[8 * q + 1]), pack2(T(), v[8 * q + 2], v[8 * q + 3]),
+                                                    pack2(T(), v[8 * q + 4], v[8 * q + 5]), pack2(T(), v[8 * q + 6], v[8 * q + 7]));
+    }
+  } else {
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q)
+      if (q < left) o[q] = from_float<T>(v[q]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void load_row32(const T* o, float (&v)[32], unsigned left) {
+  if (left >= 32 && (reinterpret_cast<uintptr_t>(o) & 15u) == 0) {
+#pragma unroll
+    for (unsigned q = 0; q < 4; ++q) {
+      float w[8];
+      load8(o + 8 * q, w);
+#pragma unroll
+      for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = w[i];
+    }
+  } else {
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) v[q] = q < left ? to_float(o[q]) : 0.0f;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Host side.
+
+// Operand `rows` x k of a batch, as its copies see it: stored [rows][ld] (k side by side) or, by_rows, [k][ld].
+struct HalfOperand {
+  const void* high;
+  const void* low;          // TERMS = 3
+  size_t ld, batch_stride;  // elements; multiples of eight
+  bool by_rows;
+};
+
+inline bool half_map(CUtensorMap* map, const void* base, bool bf16, const HalfOperand& o, size_t rows, size_t k, size_t batch, unsigned box_rows) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const cuuint64_t dims[3] = {o.by_rows ? rows : k, o.by_rows ? k : rows, batch};
+  const cuuint64_t strides[2] = {o.ld * 2, (batch > 1 ? o.batch_stride : o.ld) * 2};
+  const cuuint32_t box[3] = {64, o.by_rows ? 64u : box_rows, 1}, steps[3] = {1, 1, 1};
+  return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, steps,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct HalfProduct {
+  HalfOperand p, q;
+  const void* q_other;            // another q, rows of stride q_other_ld, taken where *q_choice is not zero
+  size_t q_other_ld;
+  const unsigned* q_choice;
+  size_t P, Q, K, batch;
+  bool bf16, symmetric;
+  unsigned* status;
+  unsigned starve;
+};
+
+// Clocks of a product by tiles of a form: rounds of tiles, each its stages, beside a start.
+struct HalfForm { bool pairs; unsigned nt; };
+inline unsigned long long half_tiles(const HalfProduct& h, unsigned rows, unsigned nt) {
+  const unsigned long long tp = (h.P + rows - 1) / rows, tq = (h.Q + nt - 1) / nt;
+  if (!h.symmetric) return tp * tq;
+  unsigned long long n = 0;
+  for (unsigned long long i = 0; i < tp; ++i) n += tq > i * (rows / nt) ? tq - i * (rows / nt) : 0;
+  return n;
+}
+inline HalfForm half_form(const HalfProduct& h, int terms, unsigned splits, int sms) {
+  const unsigned long long stages = (h.K + 63) / 64 / splits + 1, batch = h.batch * splits, pairs = (unsigned)sms / 2;
+  const unsigned long long r256 = (half_tiles(h, 256, 256) * batch + pairs - 1) / pairs, r128 = (half_tiles(h, 256, 128) * batch + pairs - 1) / pairs,
+                           r64 = (half_tiles(h, 128, 64) * batch + sms - 1) / (unsigned)sms;
+  const unsigned long long c256 = r256 * (stages * 530 * terms + 1500) + 2500, c128 = r128 * (stages * 290 * terms + 1200) + 1800,
+                           c64 = r64 * (stages * 170 * terms + 1000) + 1200;
+  if (c256 <= c128 && c256 <= c64) return {true, 256};
+  return c128 <= c64 ? HalfForm{true, 128} : HalfForm{false, 64};
+}
+
+template <class Epilogue, bool PAIR, int NT, int TERMS>
+ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args& args, unsigned splits, int sms, cudaStream_t s) {
+  using S = HalfShape<PAIR, NT, TERMS>;
+  HalfPlan p = {};
+  const unsigned long long per = half_tiles(h, S::rows, NT), tiles = per * h.batch * splits;
+  if (h.P >= (1ull << 31) || h.Q >= (1ull << 31) || h.K >= (1ull << 31) || tiles >= (1ull << 30)) return SSGD_ERR_SIZE;
+  p.P = (unsigned)h.P; p.Q = (unsigned)h.Q;
+  p.k_stages = (unsigned)((h.K + 63) / 64); p.k_chunks = (unsigned)((h.K + 15) / 16);
+  p.tiles_p = (unsigned)((h.P + S::rows - 1) / S::rows); p.tiles_q = (unsigned)((h.Q + NT - 1) / NT);
+  p.per_matrix = (unsigned)per; p.tiles = (unsigned)tiles;
+  p.splits = splits;
+  p.p_by_rows = h.p.by_rows; p.q_by_rows = h.q.by_rows;
+  p.p_box = h.P < 128 ? (unsigned)(h.P + 7) / 8 * 8 : 128;
+  p.idesc = mma_half_descriptor(S::rows, NT, h.bf16, h.p.by_rows, h.q.by_rows);
+  p.symmetric = h.symmetric;
+  p.starve = h.starve;
+  p.q_choice = h.q_choice;
+  p.status = h.status;
+  HalfMaps maps;
+  HalfOperand q1 = h.q;
+  if (h.q_other) q1.high = h.q_other, q1.ld = h.q_other_ld;
+  if (!half_map(&maps.p[0], h.p.high, h.bf16, h.p, h.P, h.K, h.batch, p.p_box) || !half_map(&maps.q[0], h.q.high, h.bf16, h.q, h.Q, h.K, h.batch, S::q_rows) ||
+      !half_map(&maps.p[1], TERMS == 3 ? h.p.low : h.p.high, h.bf16, h.p, h.P, h.K, h.batch, p.p_box) ||
+      !half_map(&maps.q[1], TERMS == 3 ? q1.low : q1.high, h.bf16, q1, h.Q, h.K, h.batch, S::q_rows))
+    return SSGD_ERR_CUDA;
+  auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS>;
+  static unsigned long long seen = 0;
+  if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
+  const unsigned long long most = PAIR ? (unsigned)sms / 2 : (unsigned)sms, workers = tiles < most ? tiles : most;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(PAIR ? 2 * workers : workers));
+  cfg.blockDim = dim3(kHalfThreads);
+  cfg.dynamicSmemBytes = S::smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = PAIR ? 2 : 1;
+  (void)cudaLaunchKernelEx(&cfg, kernel, maps, p, args);
+  return launch_status();
+}
+
+template <class Epilogue, int TERMS>
+ssgd_status launch_half(const HalfProduct& h, const typename Epilogue::Args& args, const HalfForm& form, unsigned splits, int sms, cudaStream_t s) {
+  if (!form.pairs) return launch_half_form<Epilogue, false, 64, TERMS>(h, args, splits, sms, s);
+  return form.nt == 128 ? launch_half_form<Epilogue, true, 128, TERMS>(h, args, splits, sms, s)
+                        : launch_half_form<Epilogue, true, 256, TERMS>(h, args, splits, sms, s);
+}
+
+}  // namespace
+
+#endif  // SSGD_HALF_PRODUCT_CUH_

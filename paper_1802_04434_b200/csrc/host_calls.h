@@ -2,6 +2,8 @@
 #ifndef SSGD_HOST_CALLS_H_
 #define SSGD_HOST_CALLS_H_
 
+#include <string.h>
+
 #include "host_common.h"
 
 namespace {
@@ -9,6 +11,13 @@ namespace {
 // A pointer out of a block of arguments.
 template <typename T>
 inline T* block_ptr(uint64_t word) { return reinterpret_cast<T*>(static_cast<uintptr_t>(word)); }
+
+// A float out of a block: the bits of a double.
+inline float block_float(uint64_t word) {
+  double v;
+  memcpy(&v, &word, sizeof v);
+  return (float)v;
+}
 
 // Lets a kernel have `bytes` of dynamic shared memory, asked of the runtime once per kernel and device: `seen` is a
 // static of the caller's, one for each kernel, a bit for each device.

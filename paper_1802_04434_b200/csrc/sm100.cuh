@@ -1,5 +1,5 @@
-// The sm_100a instructions that the 4-bit product is written in: mbarriers, bulk and tiled asynchronous copies, tensor
-// memory, block-scaled tcgen05.mma.  One wrapper per instruction, no policy except that every wait is bounded.
+// The sm_100a instructions that the products are written in: mbarriers, bulk and tiled asynchronous copies, tensor
+// memory, tcgen05.mma of 16-bit and of block-scaled 4-bit operands.  One wrapper per instruction, no policy except that every wait is bounded.
 #ifndef SSGD_SM100_CUH_
 #define SSGD_SM100_CUH_
 
@@ -149,6 +149,40 @@ __device__ __forceinline__ unsigned mma_fp4_descriptor(unsigned m, unsigned n, b
   return scale_id << 4 | 1u << 7 | 1u << 10 | (n >> 3) << 17 | (e8m0 ? 1u << 23 : 0u) | (m >> 4) << 24 | scale_id << 29;
 }
 
+// D[m x n] (+)= A[m x 16] B[n x 16]^T of 16-bit operands, by one CTA (m = 128) or a pair (m = 256, see below).
+template <bool PAIR>
+__device__ __forceinline__ void mma_half(unsigned d, uint64_t a, uint64_t b, unsigned idesc, bool add) {
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((unsigned)add)
+        : "memory");
+}
+// Instruction descriptor: fp32 accumulators; both operands bf16 or both fp16; whether each lies with its rows (m, n) side by side
+// instead of its k.
+__host__ __device__ constexpr unsigned mma_half_descriptor(unsigned m, unsigned n, bool bf16, bool a_by_rows, bool b_by_rows) {
+  return 1u << 4 | (bf16 ? 1u << 7 | 1u << 10 : 0u) | (a_by_rows ? 1u << 15 : 0u) | (b_by_rows ? 1u << 16 : 0u) | (n >> 3) << 17 | (m >> 4) << 24;
+}
+// Descriptor of a 16-bit operand in shared memory as tiled copies of 128-byte rows leave it (128-byte swizzle).  A row holds 64
+// of k (groups of eight rows 1024 bytes apart); or, the operand lying by rows, 64 of its rows for one k: eight k 1024 bytes
+// apart, the next 64 rows 8192.
+__device__ __forceinline__ uint64_t half_descriptor(unsigned addr, bool by_rows) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(by_rows ? 8192 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Box of a three-dimensional tensor to shared memory; x is a multiple of 16 bytes.
+__device__ __forceinline__ void tma_load_3d(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
+
 // ---------------------------------------------------------------------------------------------------------------------
 // Two CTAs of a cluster as one unit (cta_group::2): one thread of the first CTA issues for both; an MMA has 256 rows, 128
 // from each CTA, and takes half of its n rows from each; each CTA holds its half of D, and the scales it needs.
@@ -190,6 +224,11 @@ __device__ __forceinline__ bool mbarrier_wait_cluster(unsigned bar, unsigned par
 __device__ __forceinline__ void tma_load_2d_pair(unsigned dst, const CUtensorMap* map, int x, int y, unsigned cluster_bar) {
   asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar)
+               : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned cluster_bar) {
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(cluster_bar)
                : "memory");
 }
 __device__ __forceinline__ void tmem_alloc_pair(unsigned where, unsigned columns) {
