@@ -40,22 +40,20 @@ struct StatsEpilogue {
   float top, sum;
   int64_t target;
   unsigned row, part;
-  __device__ StatsEpilogue(const Args&, unsigned char*) {}
-  __device__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned odd) {
+  __device__ __forceinline__ StatsEpilogue(const Args&, unsigned char*) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned odd) {
     row = row0 + lane;
     part = 2 * at.tile_q + odd;
     top = -kInf;
     sum = 0.0f;
     target = row < a.tokens ? a.targets[row] : -1;
   }
-  __device__ void unit(const Args& a, unsigned column, unsigned left, const unsigned (&v)[32]) {
-    float z[32];
-#pragma unroll
-    for (unsigned q = 0; q < 32; ++q) z[q] = __uint_as_float(v[q]);
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
+    float(&z)[32] = v;
     if (left < 32) {
 #pragma unroll
       for (unsigned q = 0; q < 32; ++q)
-        if (q >= left) z[q] = -kInf;
+        z[q] = q >= left ? -kInf : z[q];
     }
     float m = top;
 #pragma unroll
@@ -74,16 +72,19 @@ struct StatsEpilogue {
     const int64_t at = target - (int64_t)column;
     if (at >= 0 && at < (int64_t)left) {
       float picked = 0.0f;
+      unsigned which = (unsigned)at;
 #pragma unroll
-      for (unsigned q = 0; q < 32; ++q)
-        if ((unsigned)at == q) picked = z[q];
+      for (unsigned q = 0; q < 32; ++q) {
+        asm volatile("" : "+r"(which));           // or the compiler makes an index of it, and puts the sums into local memory
+        picked = which == q ? z[q] : picked;
+      }
       a.picked[row] = picked;
     }
   }
-  __device__ void end(const Args& a, const HalfPlace&, unsigned) {
+  __device__ __forceinline__ void end(const Args& a, const HalfPlace&, unsigned) {
     if (row < a.tokens) a.partial[(size_t)part * a.tokens + row] = make_float2(top, sum);
   }
-  __device__ void finish() {}
+  __device__ __forceinline__ void finish() {}
 };
 
 // What the backward pass has to know of a token.
@@ -207,8 +208,8 @@ struct GradEpilogue {
   int64_t target;
   T* out;
   bool counts;
-  __device__ GradEpilogue(const Args&, unsigned char*) {}
-  __device__ void begin(const Args& a, const HalfPlace&, unsigned row0, unsigned lane, unsigned) {
+  __device__ __forceinline__ GradEpilogue(const Args&, unsigned char*) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace&, unsigned row0, unsigned lane, unsigned) {
     const unsigned row = row0 + lane;
     counts = false;
     out = nullptr;
@@ -219,17 +220,17 @@ struct GradEpilogue {
     g = a.g[row * a.g_stride] * a.prepared->scale;
     target = a.targets[row] - (int64_t)a.first;
   }
-  __device__ void unit(const Args&, unsigned column, unsigned left, const unsigned (&v)[32]) {
+  __device__ __forceinline__ void unit(const Args&, unsigned column, unsigned left, float (&v)[32]) {
     if (!out) return;
     float d[32];
     if (counts) {
 #pragma unroll
-      for (unsigned q = 0; q < 32; ++q) d[q] = exp2_fast((__uint_as_float(v[q]) - lse) * kLog2e);
+      for (unsigned q = 0; q < 32; ++q) d[q] = exp2_fast((v[q] - lse) * kLog2e);
       const int64_t at = target - (int64_t)column;
       if (at >= 0 && at < 32) {
 #pragma unroll
         for (unsigned q = 0; q < 32; ++q)
-          if ((unsigned)at == q) d[q] -= 1.0f;
+          d[q] = (unsigned)at == q ? d[q] - 1.0f : d[q];
       }
 #pragma unroll
       for (unsigned q = 0; q < 32; ++q) d[q] *= g;
@@ -239,8 +240,8 @@ struct GradEpilogue {
     }
     store_row32(out + column, d, 32);               // a row of dz is padded to whole tiles
   }
-  __device__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ void finish() {}
+  __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
+  __device__ __forceinline__ void finish() {}
 };
 
 // dh: rows of tokens, those that are ignored zero.  Where the vocabulary is in several pieces the sums so far are in fp32; where k
@@ -258,8 +259,8 @@ struct TokensEpilogue {
   float unscale;
   T* out;
   float* sums;
-  __device__ TokensEpilogue(const Args&, unsigned char*) {}
-  __device__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
+  __device__ __forceinline__ TokensEpilogue(const Args&, unsigned char*) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
     const unsigned row = row0 + lane;
     out = nullptr;
     sums = nullptr;
@@ -268,11 +269,11 @@ struct TokensEpilogue {
     if (a.out) out = a.out + (size_t)row * a.ldo;
     if (a.sums) sums = a.sums + ((size_t)at.split * a.tokens + row) * a.width;
   }
-  __device__ void unit(const Args& a, unsigned column, unsigned left, const unsigned (&v)[32]) {
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
     if (!out && !sums) return;
     float d[32];
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) d[q] = unscale == 0.0f ? 0.0f : __uint_as_float(v[q]);
+    for (unsigned q = 0; q < 32; ++q) d[q] = unscale == 0.0f ? 0.0f : v[q];
     if (a.add) {
       float w[32];
       load_row32(sums + column, w, left);
@@ -287,8 +288,8 @@ struct TokensEpilogue {
       store_row32(sums + column, d, left);
     }
   }
-  __device__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ void finish() {}
+  __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
+  __device__ __forceinline__ void finish() {}
 };
 
 template <typename T>
@@ -321,19 +322,19 @@ struct WeightEpilogue {
   };
   float unscale;
   T* out;
-  __device__ WeightEpilogue(const Args& a, unsigned char*) { unscale = a.prepared->unscale; }
-  __device__ void begin(const Args& a, const HalfPlace&, unsigned row0, unsigned lane, unsigned) {
+  __device__ __forceinline__ WeightEpilogue(const Args& a, unsigned char*) { unscale = a.prepared->unscale; }
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace&, unsigned row0, unsigned lane, unsigned) {
     out = row0 + lane < a.rows ? a.out + (size_t)(row0 + lane) * a.ldo : nullptr;
   }
-  __device__ void unit(const Args&, unsigned column, unsigned left, const unsigned (&v)[32]) {
+  __device__ __forceinline__ void unit(const Args&, unsigned column, unsigned left, float (&v)[32]) {
     if (!out) return;
     float d[32];
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) d[q] = __uint_as_float(v[q]) * unscale;
+    for (unsigned q = 0; q < 32; ++q) d[q] = v[q] * unscale;
     store_row32(out + column, d, left);
   }
-  __device__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ void finish() {}
+  __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
+  __device__ __forceinline__ void finish() {}
 };
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -401,7 +402,7 @@ ssgd_status head_forward(const T* h, size_t ldh, const T* w, size_t ldw, size_t 
   float* picked = static_cast<float*>(ws);
   float2* partial = reinterpret_cast<float2*>(static_cast<char*>(ws) + up(tokens * 4, 16));
   const StatsEpilogue::Args args = {targets, partial, picked, (unsigned)tokens};
-  const ssgd_status st = launch_half<StatsEpilogue, 1>(p, args, form, 1, sms, s);
+  const ssgd_status st = launch_half<StatsEpilogue, 1, 4>(p, args, form, 1, sms, s);
   if (st != SSGD_OK) return st;
   const unsigned parts = 2 * (unsigned)((vocab + form.nt - 1) / form.nt);
   if (tokens <= 256)
@@ -433,7 +434,7 @@ struct HeadBackward {
 template <typename O>
 ssgd_status weight_product(const HalfProduct& p, const HeadBackward& b, const Prepared* prepared, size_t first, size_t rows, int sms, cudaStream_t s) {
   const typename WeightEpilogue<O>::Args args = {prepared, static_cast<O*>(b.dw) + first * b.lddw, b.lddw, (unsigned)rows};
-  return launch_half<WeightEpilogue<O>, 1>(p, args, half_form(p, 1, 1, sms), 1, sms, s);
+  return launch_half<WeightEpilogue<O>, 1, 0>(p, args, half_form(p, 1, 1, sms), 1, sms, s);
 }
 
 template <typename T>
@@ -461,7 +462,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
     p.q = {w_piece, nullptr, b.ldw, 0, false};
     p.P = b.T; p.Q = columns; p.K = b.D;
     const typename GradEpilogue<T>::Args grad = {b.targets, b.lse, b.g, b.kinds, prepared, dz, b.g_stride, z.dz_ld, tokens, (unsigned)first};
-    st = launch_half<GradEpilogue<T>, 1>(p, grad, half_form(p, 1, 1, sms), 1, sms, s);
+    st = launch_half<GradEpilogue<T>, 1, 0>(p, grad, half_form(p, 1, 1, sms), 1, sms, s);
     if (st != SSGD_OK) break;
     if (b.dh) {
       p.p = {dz, nullptr, z.dz_ld, 0, false};
@@ -469,7 +470,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
       p.P = b.T; p.Q = b.D; p.K = columns;
       T* out = last && z.splits == 1 ? static_cast<T*>(b.dh) : nullptr;
       const typename TokensEpilogue<T>::Args args = {b.kinds, prepared, z.pieces > 1 || z.splits > 1 ? sums : nullptr, out, b.lddh, tokens, width, first > 0};
-      st = launch_half<TokensEpilogue<T>, 1>(p, args, half_form(p, 1, z.splits, sms), z.splits, sms, s);
+      st = launch_half<TokensEpilogue<T>, 1, 0>(p, args, half_form(p, 1, z.splits, sms), z.splits, sms, s);
       if (st == SSGD_OK && z.splits > 1) {
         const size_t plane = b.T * b.D;
         launch_kernel(xent_planes_kernel<T>, dim3(grid_for((plane + 255) / 256)), dim3(256), 0, s, true, sums, z.splits, plane, prepared, width,

@@ -6,12 +6,15 @@
 // needs no exchange between threads.
 //   warp 0      one thread brings stages of 64 of k (tiled copies, 128-byte swizzle, zeros beyond the edges)
 //   warp 1      one thread issues the MMAs, four of 16 of k a stage
-//   warps 2..9  read the accumulators, two warps to a quarter of the lanes, 32 columns in turn; two accumulators, so that a tile
+//   warps 4..11 read the accumulators, two warps to a quarter of the lanes, 32 columns in turn; two accumulators, so that a tile
 //               is written out while the next is multiplied
 // An operand may lie in memory with its k side by side, or with its rows side by side (a matrix that another product
 // takes the other way round): the copies and the tensor cores take both, nothing is transposed.
-// TERMS = 3: each operand is a sum of two fp16 matrices, high and low part (22 bits together); high * high, high * low and low * high
-// go into the same sum, low * low is below the last bit that counts.
+// TERMS = 3: each operand is a sum of two fp16 matrices, high and low part (22 bits together); high * low, low * high and high * high
+// go into the same sum, the small ones first; low * low is below the last bit that counts.
+// CHUNK > 0: the tensor cores add with fp32 accumulators, but cut off what does not fit instead of rounding it, so that a sum is off
+// by up to 2^-24 of itself for each 16 of k, always to the same side (measured: 10^-8 of the sum for each of k).  Where that
+// counts the sum is taken every CHUNK stages, and the parts are added by the epilogue's threads, rounded to nearest.
 // Every wait has an iteration limit and reports through a status word, as in the 4-bit product.
 #ifndef SSGD_HALF_PRODUCT_CUH_
 #define SSGD_HALF_PRODUCT_CUH_
@@ -25,7 +28,7 @@
 
 namespace {
 
-constexpr int kHalfThreads = 320;
+constexpr int kHalfThreads = 384;                 // a warpgroup for copies and MMAs, two that write out
 constexpr unsigned kHalfPolls = 200000;           // bound of a wait, about 0.2 s
 
 struct HalfMaps {
@@ -91,10 +94,14 @@ __device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p
 }
 
 // What an epilogue offers, besides its Args:
-//   begin(args, place, row, tile of this CTA's rows)   before the first columns of a tile; row: this thread's
-//   unit(args, column, left, v)                        32 accumulators of columns column .., `left` of them inside
-//   end(args, place, warp)                             behind the last; every thread of the warp calls it
-template <class Epilogue, bool PAIR, int NT, int TERMS>
+//   begin(args, place, row0, lane, odd)   before a tile's first columns; this thread's row is row0 + lane, odd: which half of the columns
+//   unit(args, column, left, v)           32 sums of columns column .., `left` of them inside; it may change them
+//   end(args, place, warp)                behind the last; every thread of the warp calls it
+//   finish()                              behind the last tile
+constexpr unsigned kShiftRegisters = 168;
+__host__ __device__ constexpr bool half_shifts(int nt, int chunk) { return nt == 256 && chunk > 0; }
+
+template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK>
 __global__ void __launch_bounds__(kHalfThreads, 1)
 half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, const typename Epilogue::Args args) {
   using S = HalfShape<PAIR, NT, TERMS>;
@@ -136,6 +143,12 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
   bool ok = true;
   unsigned n = 0;                               // stages so far, over all tiles
 
+  // Tiles of 256 columns summed by chunks: 128 sums a thread.  The epilogue's warps take the registers that the first warpgroup
+  // does without: 128 * 40 + 256 * 232 = 384 * 168, which is what the block is launched with (the host has made sure).
+  constexpr bool kShift = half_shifts(NT, CHUNK);
+
+  if (warp < 4) {
+  if constexpr (kShift) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
   if (warp == 0) {
     if (elect_one()) {
       const CUtensorMap* q_high = p.q_choice && *p.q_choice ? &maps.q[1] : &maps.q[0];
@@ -187,42 +200,47 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       constexpr unsigned low = (S::p_bytes + S::q_bytes) >> 4;
       unsigned s = 0, parity = 0;
       bool ready = false;                       // the next stage's operands are known to be there
-      unsigned t = 0;                           // tiles so far
-      for (unsigned tile = worker; tile < p.tiles && ok; tile += workers, ++t) {
-        if (t > 1) ok = PAIR ? mbarrier_wait_cluster(acc_free + 8 * (t & 1u), (t / 2 - 1) & 1u, kHalfPolls)
-                             : mbarrier_wait(acc_free + 8 * (t & 1u), (t / 2 - 1) & 1u, kHalfPolls);
-        if (!ok) break;
-        tcgen05_fence_after();
-        const unsigned d = tmem + (t & 1u) * NT;
+      unsigned t = 0;                           // sums taken so far: of tiles, or of their chunks
+      for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
         const unsigned split = tile / p.per_matrix % p.splits;
         const unsigned first = (unsigned)((uint64_t)p.k_stages * split / p.splits), last = (unsigned)((uint64_t)p.k_stages * (split + 1) / p.splits);
-        for (unsigned k = first; k < last; ++k, ++n) {
-          ok = ready || mbarrier_wait(full + 8 * s, parity, kHalfPolls);
+        for (unsigned from = first; from < last && ok; ++t) {
+          const unsigned to = CHUNK > 0 ? min(last, from + CHUNK) : last;
+          if (t > 1) ok = PAIR ? mbarrier_wait_cluster(acc_free + 8 * (t & 1u), (t / 2 - 1) & 1u, kHalfPolls)
+                               : mbarrier_wait(acc_free + 8 * (t & 1u), (t / 2 - 1) & 1u, kHalfPolls);
           if (!ok) break;
           tcgen05_fence_after();
-          const unsigned next = s + 1 == S::stages ? 0 : s + 1, next_parity = parity ^ (next == 0);
-          ready = mbarrier_test(full + 8 * next, next_parity);    // its answer comes while this stage is issued
-          const uint64_t pd = p_desc + s * (S::stage_bytes >> 4), qd = q_desc + s * (S::stage_bytes >> 4);
-          const unsigned chunks = p.k_chunks - k * 4;
+          const unsigned d = tmem + (t & 1u) * NT;
+          for (unsigned k = from; k < to; ++k, ++n) {
+            ok = ready || mbarrier_wait(full + 8 * s, parity, kHalfPolls);
+            if (!ok) break;
+            tcgen05_fence_after();
+            const unsigned next = s + 1 == S::stages ? 0 : s + 1, next_parity = parity ^ (next == 0);
+            ready = mbarrier_test(full + 8 * next, next_parity);    // its answer comes while this stage is issued
+            const uint64_t pd = p_desc + s * (S::stage_bytes >> 4), qd = q_desc + s * (S::stage_bytes >> 4);
+            const unsigned chunks = p.k_chunks - k * 4;
+            if constexpr (TERMS == 3) {
 #pragma unroll
-          for (unsigned c = 0; c < 4; ++c) {
-            if (c == 0 || c < chunks) {
-              const uint64_t pc = pd + c * p_step, qc = qd + c * q_step;
-              mma_half<PAIR>(d, pc, qc, p.idesc, k > first || c > 0);
-              if constexpr (TERMS == 3) {
-                mma_half<PAIR>(d, pc, qc + low, p.idesc, true);
-                mma_half<PAIR>(d, pc + low, qc, p.idesc, true);
+              for (unsigned c = 0; c < 4; ++c) {
+                if (c == 0 || c < chunks) {
+                  mma_half<PAIR>(d, pd + c * p_step, qd + c * q_step + low, p.idesc, k > from || c > 0);
+                  mma_half<PAIR>(d, pd + c * p_step + low, qd + c * q_step, p.idesc, true);
+                }
               }
             }
+#pragma unroll
+            for (unsigned c = 0; c < 4; ++c)
+              if (c == 0 || c < chunks) mma_half<PAIR>(d, pd + c * p_step, qd + c * q_step, p.idesc, TERMS == 3 || k > from || c > 0);
+            if (PAIR) tcgen05_commit_pair(empty + 8 * s);
+            else tcgen05_commit(empty + 8 * s);
+            s = next;
+            parity = next_parity;
           }
-          if (PAIR) tcgen05_commit_pair(empty + 8 * s);
-          else tcgen05_commit(empty + 8 * s);
-          s = next;
-          parity = next_parity;
-        }
-        if (ok) {
-          if (PAIR) tcgen05_commit_pair(acc_full + 8 * (t & 1u));
-          else tcgen05_commit(acc_full + 8 * (t & 1u));
+          if (ok) {
+            if (PAIR) tcgen05_commit_pair(acc_full + 8 * (t & 1u));
+            else tcgen05_commit(acc_full + 8 * (t & 1u));
+          }
+          from = to;
         }
       }
       if (!ok) {                                // what was issued has to end before tensor memory is freed; nobody writes it out
@@ -231,34 +249,70 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
         (void)mbarrier_wait(ended, 0, kHalfPolls);
       }
     }
+  }
   } else {
-    constexpr unsigned kUnits = NT / 32;
-    const unsigned quarter = warp & 3u, odd = warp >= 6;
+    if constexpr (kShift) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+    constexpr unsigned kUnits = NT / 64;        // of 32 columns, of this warp
+    const unsigned quarter = warp & 3u, odd = warp >= 8;
     const unsigned go = PAIR ? cluster_address(acc_free, 0) : acc_free;
-    Epilogue epilogue(args, half_smem + S::stages * S::stage_bytes + (warp - 2) * S::box_bytes);
+    Epilogue epilogue(args, half_smem + S::stages * S::stage_bytes + (warp - 4) * S::box_bytes);
     unsigned t = 0;
-    for (unsigned tile = worker; tile < p.tiles; tile += workers, ++t) {
+    for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
       const HalfPlace at = half_place<PAIR, NT>(tile, p);
       const unsigned row0 = at.p0 + rank * 128 + quarter * 32;
       epilogue.begin(args, at, row0, lane, odd);
-      ok = mbarrier_wait(acc_full + 8 * (t & 1u), (t / 2) & 1u, 4 * kHalfPolls + 64 * p.k_stages);
-      if (!ok) break;
-      tcgen05_fence_after();
-      const unsigned lanes = tmem + (t & 1u) * NT + (quarter << 21);
-#pragma unroll 1
-      for (unsigned unit = odd; unit < kUnits; unit += 2) {
-        unsigned v[32];
-        tmem_read32(lanes + unit * 32, v);
-        if (unit + 2 >= kUnits) {               // this warp's last columns
-          tcgen05_fence_before();
-          __syncwarp();
-          if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t & 1u));
+      if constexpr (CHUNK > 0) {
+        const unsigned first = (unsigned)((uint64_t)p.k_stages * at.split / p.splits), last = (unsigned)((uint64_t)p.k_stages * (at.split + 1) / p.splits);
+        float sum[kUnits][32];
+        for (unsigned from = first; from < last; from += CHUNK, ++t) {
+          ok = mbarrier_wait(acc_full + 8 * (t & 1u), (t / 2) & 1u, 4 * kHalfPolls);
+          if (!ok) break;
+          tcgen05_fence_after();
+          const unsigned lanes = tmem + (t & 1u) * NT + (quarter << 21);
+#pragma unroll
+          for (unsigned j = 0; j < kUnits; ++j) {
+            unsigned v[32];
+            tmem_read32(lanes + (odd + 2 * j) * 32, v);
+            if (j + 1 == kUnits) {
+              tcgen05_fence_before();
+              __syncwarp();
+              if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t & 1u));
+            }
+#pragma unroll
+            for (unsigned q = 0; q < 32; ++q) sum[j][q] = from == first ? __uint_as_float(v[q]) : sum[j][q] + __uint_as_float(v[q]);
+          }
         }
-        const unsigned column = at.q0 + unit * 32;
-        if (row0 < p.P && column < p.Q) epilogue.unit(args, column, min(32u, p.Q - column), v);
-        __syncwarp();
+        if (!ok) break;
+#pragma unroll
+        for (unsigned j = 0; j < kUnits; ++j) {
+          const unsigned column = at.q0 + (odd + 2 * j) * 32;
+          if (row0 < p.P && column < p.Q) epilogue.unit(args, column, min(32u, p.Q - column), sum[j]);
+          __syncwarp();
+        }
+      } else {
+        ok = mbarrier_wait(acc_full + 8 * (t & 1u), (t / 2) & 1u, 4 * kHalfPolls + 64 * p.k_stages);
+        if (!ok) break;
+        tcgen05_fence_after();
+        const unsigned lanes = tmem + (t & 1u) * NT + (quarter << 21);
+#pragma unroll 1
+        for (unsigned j = 0; j < kUnits; ++j) {
+          unsigned v[32];
+          tmem_read32(lanes + (odd + 2 * j) * 32, v);
+          if (j + 1 == kUnits) {                // this warp's last columns
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t & 1u));
+          }
+          float f[32];
+#pragma unroll
+          for (unsigned q = 0; q < 32; ++q) f[q] = __uint_as_float(v[q]);
+          const unsigned column = at.q0 + (odd + 2 * j) * 32;
+          if (row0 < p.P && column < p.Q) epilogue.unit(args, column, min(32u, p.Q - column), f);
+          __syncwarp();
+        }
+        ++t;
       }
-      epilogue.end(args, at, rank * 8 + warp - 2);
+      epilogue.end(args, at, rank * 8 + warp - 4);
       __syncwarp();
     }
     epilogue.finish();
@@ -320,6 +374,19 @@ __device__ __forceinline__ void load_row32(const T* o, float (&v)[32], unsigned 
   }
 }
 
+// Eight neighbours at a time, for epilogues that hold a tile's sums in registers and have few left; 16-byte aligned.
+__device__ __forceinline__ void store8(__half* o, const float* v) {
+  *reinterpret_cast<uint4*>(o) = make_uint4(pack2(__half(), v[0], v[1]), pack2(__half(), v[2], v[3]), pack2(__half(), v[4], v[5]), pack2(__half(), v[6], v[7]));
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* o, const float* v) {
+  *reinterpret_cast<uint4*>(o) = make_uint4(pack2(__nv_bfloat16(), v[0], v[1]), pack2(__nv_bfloat16(), v[2], v[3]), pack2(__nv_bfloat16(), v[4], v[5]),
+                                            pack2(__nv_bfloat16(), v[6], v[7]));
+}
+__device__ __forceinline__ void store8(float* o, const float* v) {
+  reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
 // ---------------------------------------------------------------------------------------------------------------------
 // Host side.
 
@@ -371,7 +438,7 @@ inline HalfForm half_form(const HalfProduct& h, int terms, unsigned splits, int 
   return c128 <= c64 ? HalfForm{true, 128} : HalfForm{false, 64};
 }
 
-template <class Epilogue, bool PAIR, int NT, int TERMS>
+template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK>
 ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args& args, unsigned splits, int sms, cudaStream_t s) {
   using S = HalfShape<PAIR, NT, TERMS>;
   HalfPlan p = {};
@@ -396,9 +463,18 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
       !half_map(&maps.p[1], TERMS == 3 ? h.p.low : h.p.high, h.bf16, h.p, h.P, h.K, h.batch, p.p_box) ||
       !half_map(&maps.q[1], TERMS == 3 ? q1.low : q1.high, h.bf16, q1, h.Q, h.K, h.batch, S::q_rows))
     return SSGD_ERR_CUDA;
-  auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS>;
+  auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS, CHUNK>;
   static unsigned long long seen = 0;
   if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
+  if constexpr (half_shifts(NT, CHUNK)) {         // registers as the kernel's own shares add up to
+    static int registers = 0;
+    if (__atomic_load_n(&registers, __ATOMIC_RELAXED) == 0) {
+      cudaFuncAttributes a;
+      if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) return SSGD_ERR_CUDA;
+      __atomic_store_n(&registers, a.numRegs, __ATOMIC_RELAXED);
+    }
+    if (registers != (int)kShiftRegisters) return SSGD_ERR_CUDA;
+  }
   const unsigned long long most = PAIR ? (unsigned)sms / 2 : (unsigned)sms, workers = tiles < most ? tiles : most;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(PAIR ? 2 * workers : workers));
@@ -417,11 +493,11 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
   return launch_status();
 }
 
-template <class Epilogue, int TERMS>
+template <class Epilogue, int TERMS, int CHUNK>
 ssgd_status launch_half(const HalfProduct& h, const typename Epilogue::Args& args, const HalfForm& form, unsigned splits, int sms, cudaStream_t s) {
-  if (!form.pairs) return launch_half_form<Epilogue, false, 64, TERMS>(h, args, splits, sms, s);
-  return form.nt == 128 ? launch_half_form<Epilogue, true, 128, TERMS>(h, args, splits, sms, s)
-                        : launch_half_form<Epilogue, true, 256, TERMS>(h, args, splits, sms, s);
+  if (!form.pairs) return launch_half_form<Epilogue, false, 64, TERMS, CHUNK>(h, args, splits, sms, s);
+  return form.nt == 128 ? launch_half_form<Epilogue, true, 128, TERMS, CHUNK>(h, args, splits, sms, s)
+                        : launch_half_form<Epilogue, true, 256, TERMS, CHUNK>(h, args, splits, sms, s);
 }
 
 }  // namespace

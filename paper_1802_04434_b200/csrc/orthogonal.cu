@@ -32,27 +32,28 @@ __device__ __forceinline__ void split_half(float v, __half* high, __half* low) {
   *low = __float2half_rn(v - __half2float(*high));
 }
 
-// 32 neighbours of a row to high and low part.  The matrices' rows are padded to whole 64 columns, so `left` need not be asked.
+// Eight neighbours of a row as high and low part.  The matrices' rows are padded to whole 64 columns, so that nobody has to ask
+// where they end.
 template <bool LOW>
-__device__ __forceinline__ void store_split32(__half* high, __half* low, size_t at, const float (&v)[32]) {
-  float h[32];
+__device__ __forceinline__ void store_split8(__half* high, __half* low, size_t at, const float* v) {
+  float h[8];
 #pragma unroll
-  for (unsigned q = 0; q < 32; ++q) h[q] = __half2float(__float2half_rn(v[q]));
-  store_row32(high + at, h, 32);
+  for (unsigned q = 0; q < 8; ++q) h[q] = __half2float(__float2half_rn(v[q]));
+  store8(high + at, h);
   if constexpr (LOW) {
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) h[q] = v[q] - h[q];
-    store_row32(low + at, h, 32);
+    for (unsigned q = 0; q < 8; ++q) h[q] = v[q] - h[q];
+    store8(low + at, h);
   }
 }
 template <bool LOW>
-__device__ __forceinline__ void load_split32(const __half* high, const __half* low, size_t at, float (&v)[32]) {
-  load_row32(high + at, v, 32);
+__device__ __forceinline__ void load_split8(const __half* high, const __half* low, size_t at, float (&v)[8]) {
+  load8(high + at, v);
   if constexpr (LOW) {
-    float w[32];
-    load_row32(low + at, w, 32);
+    float w[8];
+    load8(low + at, w);
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) v[q] += w[q];
+    for (unsigned q = 0; q < 8; ++q) v[q] += w[q];
   }
 }
 
@@ -66,7 +67,8 @@ struct Square {                   // a batch of symmetric matrices, high and low
 // side).  Tiles on the diagonal hold both halves themselves.
 template <bool LOW>
 __device__ __forceinline__ void store_symmetric(const Square& s, size_t matrix, unsigned row, unsigned column, unsigned left, bool mirrored, const float (&v)[32]) {
-  store_split32<LOW>(s.high, s.low, matrix + (size_t)row * s.ld + column, v);
+#pragma unroll
+  for (unsigned c = 0; c < 32; c += 8) store_split8<LOW>(s.high, s.low, matrix + (size_t)row * s.ld + column + c, v + c);
   if (mirrored) {
 #pragma unroll
     for (unsigned q = 0; q < 32; ++q) {
@@ -94,8 +96,8 @@ struct GramEpilogue {
   unsigned row, seen;
   size_t matrix;
   bool mirrored, inside;
-  __device__ GramEpilogue(const Args&, unsigned char*) { seen = ~0u; }
-  __device__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
+  __device__ __forceinline__ GramEpilogue(const Args&, unsigned char*) { seen = ~0u; }
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
     row = row0 + lane;
     inside = row < a.e.side;
     mirrored = at.q0 >= at.p0 + at.rows;
@@ -113,20 +115,19 @@ struct GramEpilogue {
     }
     if (at.tile == 0 && row == 0) a.d[at.matrix] = d;      // two warps: the same value
   }
-  __device__ void unit(const Args& a, unsigned column, unsigned left, const unsigned (&u)[32]) {
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
     if (!inside) return;
-    float v[32];
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) v[q] = __uint_as_float(u[q]) * kUnscale;
+    for (unsigned q = 0; q < 32; ++q) v[q] *= kUnscale;
     if (row - column < 32u) {
 #pragma unroll
       for (unsigned q = 0; q < 32; ++q)
-        if (column + q == row) v[q] -= d * kScale;
+        v[q] = row - column == q ? v[q] - d * kScale : v[q];
     }
     store_symmetric<LOW>(a.e, matrix, row, column, left, mirrored, v);
   }
-  __device__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ void finish() {}
+  __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
+  __device__ __forceinline__ void finish() {}
 };
 
 // M = p E + c E^2.
@@ -141,24 +142,27 @@ struct PolynomialEpilogue {
   unsigned row;
   size_t matrix;
   bool mirrored, inside;
-  __device__ PolynomialEpilogue(const Args&, unsigned char*) {}
-  __device__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
+  __device__ __forceinline__ PolynomialEpilogue(const Args&, unsigned char*) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
     row = row0 + lane;
     inside = row < a.e.side;
     mirrored = at.q0 >= at.p0 + at.rows;
     matrix = at.matrix * a.e.stride;
     s = step_of(a.f, a.d[at.matrix]);
   }
-  __device__ void unit(const Args& a, unsigned column, unsigned left, const unsigned (&u)[32]) {
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
     if (!inside) return;
-    float e[32];
-    load_split32<LOW>(a.e.high, a.e.low, matrix + (size_t)row * a.e.ld + column, e);
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) e[q] = fmaf(s.c, __uint_as_float(u[q]) * kUnscale, s.p * e[q]);
-    store_symmetric<LOW>(a.m, matrix, row, column, left, mirrored, e);
+    for (unsigned c = 0; c < 32; c += 8) {
+      float e[8];
+      load_split8<LOW>(a.e.high, a.e.low, matrix + (size_t)row * a.e.ld + column + c, e);
+#pragma unroll
+      for (unsigned q = 0; q < 8; ++q) v[c + q] = fmaf(s.c, v[c + q] * kUnscale, s.p * e[q]);
+    }
+    store_symmetric<LOW>(a.m, matrix, row, column, left, mirrored, v);
   }
-  __device__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ void finish() {}
+  __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
+  __device__ __forceinline__ void finish() {}
 };
 
 struct Whole {                    // a batch of matrices X, high and low part
@@ -185,8 +189,8 @@ struct UpdateEpilogue {
   bool inside;
   size_t at_x;
   T* out;
-  __device__ UpdateEpilogue(const Args&, unsigned char*) {}
-  __device__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
+  __device__ __forceinline__ UpdateEpilogue(const Args&, unsigned char*) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
     row = row0 + lane;
     inside = row < a.rows;
     at_x = at.matrix * a.x.stride + (size_t)row * a.x.ld;
@@ -194,38 +198,52 @@ struct UpdateEpilogue {
     q = step_of(a.f, a.d[at.matrix]).q;
     sum = 0.0f;
   }
-  __device__ void unit(const Args& a, unsigned column, unsigned left, const unsigned (&u)[32]) {
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
     if (!inside) return;
-    float v[32];
-    load_split32<true>(a.x.high, a.x.low, at_x + column, v);
+    const bool wide = TO != kNextStep && left >= 32 && (reinterpret_cast<uintptr_t>(out + column) & 15u) == 0;
 #pragma unroll
-    for (unsigned i = 0; i < 32; ++i) v[i] = fmaf(q, v[i], __uint_as_float(u[i]) * kUnscale);
-    if constexpr (TO == kNextStep) {
+    for (unsigned c = 0; c < 32; c += 8) {
+      float x[8];
+      load_split8<true>(a.x.high, a.x.low, at_x + column + c, x);
 #pragma unroll
-      for (unsigned i = 0; i < 32; ++i)
-        if (i < left) sum = fmaf(v[i], v[i], sum);
-      store_split32<true>(a.next.high, a.next.low, at_x + column, v);
-    } else if constexpr (TO == kOut) {
+      for (unsigned i = 0; i < 8; ++i) v[c + i] = fmaf(q, x[i], v[c + i] * kUnscale);
+      if constexpr (TO == kNextStep) {
 #pragma unroll
-      for (unsigned i = 0; i < 32; ++i) v[i] *= kUnscale;
-      store_row32(out + column, v, left);
-    } else {
-      float x[32];
-      load_row32(out + column, x, left);
-      const float step = a.delta * kUnscale;
+        for (unsigned i = 0; i < 8; ++i) sum = c + i < left ? fmaf(v[c + i], v[c + i], sum) : sum;
+        store_split8<true>(a.next.high, a.next.low, at_x + column + c, v + c);
+      } else if constexpr (TO == kOut) {
 #pragma unroll
-      for (unsigned i = 0; i < 32; ++i) x[i] = fmaf(-step, v[i], x[i]);
-      store_row32(out + column, x, left);
+        for (unsigned i = 0; i < 8; ++i) v[c + i] *= kUnscale;
+        if (wide) {
+          store8(out + column + c, v + c);
+        } else {
+#pragma unroll
+          for (unsigned i = 0; i < 8; ++i)
+            if (c + i < left) out[column + c + i] = from_float<T>(v[c + i]);
+        }
+      } else {
+        const float step = a.delta * kUnscale;
+        if (wide) {
+          load8(out + column + c, x);
+#pragma unroll
+          for (unsigned i = 0; i < 8; ++i) x[i] = fmaf(-step, v[c + i], x[i]);
+          store8(out + column + c, x);
+        } else {
+#pragma unroll
+          for (unsigned i = 0; i < 8; ++i)
+            if (c + i < left) out[column + c + i] = fmaf(-step, v[c + i], out[column + c + i]);
+        }
+      }
     }
   }
-  __device__ void end(const Args& a, const HalfPlace& at, unsigned warp) {
+  __device__ __forceinline__ void end(const Args& a, const HalfPlace& at, unsigned warp) {
     if constexpr (TO == kNextStep) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       if ((threadIdx.x & 31u) == 0) a.squares[(size_t)at.matrix * a.count + at.tile * a.slots + warp] = sum * (kUnscale * kUnscale);
     }
   }
-  __device__ void finish() {}
+  __device__ __forceinline__ void finish() {}
 };
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -416,6 +434,9 @@ ssgd_status launch_source_typed(const Problem& p, const Layout& l, const Whole& 
   }
 }
 
+// Stages between two times that a sum of three terms is taken.
+constexpr int kChunk = 2;
+
 struct Buffers {
   Whole x[2];
   Square e, m;
@@ -445,7 +466,7 @@ ssgd_status launch_update(const Problem& p, const Buffers& b, int now, unsigned*
   a.x = x; a.next = b.x[1 - now]; a.d = b.d; a.squares = b.squares;
   a.out = static_cast<T*>(p.out); a.ldo = p.ldo; a.out_stride = p.out_stride;
   a.f = p.f; a.delta = p.delta; a.rows = (unsigned)p.rows; a.count = *count; a.slots = slots;
-  return launch_half<UpdateEpilogue<TO, T>, TERMS>(h, a, form, 1, sms, s);
+  return launch_half<UpdateEpilogue<TO, T>, TERMS, TERMS == 3 ? kChunk : 0>(h, a, form, 1, sms, s);
 }
 
 template <int TERMS>
@@ -464,13 +485,13 @@ ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, i
     h.status = p.status;
     h.starve = p.starve;
     const typename GramEpilogue<TERMS == 3>::Args gram = {b.e, k ? b.squares : nullptr, b.d, count};
-    ssgd_status st = launch_half<GramEpilogue<TERMS == 3>, TERMS>(h, gram, half_form(h, TERMS, 1, sms), 1, sms, s);
+    ssgd_status st = launch_half<GramEpilogue<TERMS == 3>, TERMS, TERMS == 3 ? kChunk : 0>(h, gram, half_form(h, TERMS, 1, sms), 1, sms, s);
     if (st != SSGD_OK) return st;
     h.p = {b.e.high, b.e.low, b.e.ld, b.e.stride, false};
     h.q = h.p;
     h.K = l.side;
     const typename PolynomialEpilogue<TERMS == 3>::Args polynomial = {b.e, b.m, b.d, p.f};
-    st = launch_half<PolynomialEpilogue<TERMS == 3>, TERMS>(h, polynomial, half_form(h, TERMS, 1, sms), 1, sms, s);
+    st = launch_half<PolynomialEpilogue<TERMS == 3>, TERMS, TERMS == 3 ? kChunk : 0>(h, polynomial, half_form(h, TERMS, 1, sms), 1, sms, s);
     if (st != SSGD_OK) return st;
     if (k + 1 < p.steps) st = launch_update<kNextStep, float, TERMS>(p, b, now, &count, sms, s);
     else if (p.momentum) st = launch_update<kParameters, float, TERMS>(p, b, now, &count, sms, s);
