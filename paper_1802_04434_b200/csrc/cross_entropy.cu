@@ -37,12 +37,15 @@ struct StatsEpilogue {
     float* picked;              // [tokens]: the target's logit
     unsigned tokens;
   };
+  static constexpr unsigned kBox = 0;
+  Box box;
   float top, sum;
   int64_t target;
   unsigned row, part;
-  __device__ __forceinline__ StatsEpilogue(const Args&, unsigned char*) {}
-  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned odd) {
-    row = row0 + lane;
+  __device__ __forceinline__ StatsEpilogue(const Args&, const Box& b) : box(b) {}
+  __device__ __forceinline__ void ahead(const Args&, unsigned) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned odd) {
+    row = row0 + box.lane;
     part = 2 * at.tile_q + odd;
     top = -kInf;
     sum = 0.0f;
@@ -84,7 +87,7 @@ struct StatsEpilogue {
   __device__ __forceinline__ void end(const Args& a, const HalfPlace&, unsigned) {
     if (row < a.tokens) a.partial[(size_t)part * a.tokens + row] = make_float2(top, sum);
   }
-  __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ void finish(const Args&) {}
 };
 
 // What the backward pass has to know of a token.
@@ -195,53 +198,56 @@ xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__
 template <typename T>
 struct GradEpilogue {
   struct Args {
+    CUtensorMap dz;             // [tokens][columns of this piece]
     const int64_t* targets;
     const float* lse;
     const float* g;
     const uint8_t* kinds;
     const Prepared* prepared;
-    T* dz;                      // [tokens][lddz], columns of this piece
-    size_t g_stride, lddz;
+    size_t g_stride;
     unsigned tokens, first;     // first: column of the vocabulary at which the piece begins
   };
+  static constexpr unsigned kBox = 4096;      // two boxes in turn
+  Box box;
   float lse, g;
   int64_t target;
-  T* out;
+  unsigned row0, half;
   bool counts;
-  __device__ __forceinline__ GradEpilogue(const Args&, unsigned char*) {}
-  __device__ __forceinline__ void begin(const Args& a, const HalfPlace&, unsigned row0, unsigned lane, unsigned) {
-    const unsigned row = row0 + lane;
+  __device__ __forceinline__ GradEpilogue(const Args&, const Box& b) : box(b), half(0) {}
+  __device__ __forceinline__ void ahead(const Args&, unsigned) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace&, unsigned first_row, unsigned) {
+    row0 = first_row;
+    const unsigned row = row0 + box.lane;
     counts = false;
-    out = nullptr;
     if (row >= a.tokens) return;
-    out = a.dz + (size_t)row * a.lddz;
     counts = a.kinds[row] == kCounts;
     lse = a.lse[row];
     g = a.g[row * a.g_stride] * a.prepared->scale;
     target = a.targets[row] - (int64_t)a.first;
   }
-  __device__ __forceinline__ void unit(const Args&, unsigned column, unsigned left, float (&v)[32]) {
-    if (!out) return;
-    float d[32];
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned, float (&v)[32]) {
     if (counts) {
 #pragma unroll
-      for (unsigned q = 0; q < 32; ++q) d[q] = exp2_fast((v[q] - lse) * kLog2e);
+      for (unsigned q = 0; q < 32; ++q) v[q] = exp2_fast((v[q] - lse) * kLog2e);
       const int64_t at = target - (int64_t)column;
       if (at >= 0 && at < 32) {
 #pragma unroll
-        for (unsigned q = 0; q < 32; ++q)
-          d[q] = (unsigned)at == q ? d[q] - 1.0f : d[q];
+        for (unsigned q = 0; q < 32; ++q) v[q] = (unsigned)at == q ? v[q] - 1.0f : v[q];
       }
 #pragma unroll
-      for (unsigned q = 0; q < 32; ++q) d[q] *= g;
+      for (unsigned q = 0; q < 32; ++q) v[q] *= g;
     } else {
 #pragma unroll
-      for (unsigned q = 0; q < 32; ++q) d[q] = 0.0f;
+      for (unsigned q = 0; q < 32; ++q) v[q] = 0.0f;
     }
-    store_row32(out + column, d, 32);               // a row of dz is padded to whole tiles
+    half ^= 2048;
+    box.sent_but_last();
+    box.template put16<T>(half, v);
+    box.fence();
+    box.send(a.dz, half, column, row0, 0);
   }
   __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ void finish(const Args&) { box.finish(); }
 };
 
 // dh: rows of tokens, those that are ignored zero.  Where the vocabulary is in several pieces the sums so far are in fp32; where k
@@ -256,40 +262,37 @@ struct TokensEpilogue {
     size_t ldo;
     unsigned tokens, width, add;
   };
+  static constexpr unsigned kBox = 4096;
+  Box box;
   float unscale;
-  T* out;
-  float* sums;
-  __device__ __forceinline__ TokensEpilogue(const Args&, unsigned char*) {}
-  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
-    const unsigned row = row0 + lane;
-    out = nullptr;
-    sums = nullptr;
-    if (row >= a.tokens) return;
-    unscale = a.kinds[row] == kCounts ? a.prepared->unscale : 0.0f;
-    if (a.out) out = a.out + (size_t)row * a.ldo;
-    if (a.sums) sums = a.sums + ((size_t)at.split * a.tokens + row) * a.width;
+  unsigned row0, split;
+  bool counts;
+  __device__ __forceinline__ TokensEpilogue(const Args& a, const Box& b) : box(b) { unscale = a.prepared->unscale; }
+  __device__ __forceinline__ void ahead(const Args&, unsigned) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
+    row0 = first_row;
+    split = at.split;
+    counts = row0 + box.lane < a.tokens && a.kinds[row0 + box.lane] == kCounts;
   }
   __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
-    if (!out && !sums) return;
-    float d[32];
+    const float by = a.out ? unscale : 1.0f;
+    if (!a.add) {
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) d[q] = unscale == 0.0f ? 0.0f : v[q];
-    if (a.add) {
-      float w[32];
-      load_row32(sums + column, w, left);
-#pragma unroll
-      for (unsigned q = 0; q < 32; ++q) d[q] += w[q];
-    }
-    if (out) {
-#pragma unroll
-      for (unsigned q = 0; q < 32; ++q) d[q] *= unscale;
-      store_row32(out + column, d, left);
+      for (unsigned q = 0; q < 32; ++q) v[q] = counts ? v[q] * by : 0.0f;
     } else {
-      store_row32(sums + column, d, left);
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) v[q] = counts ? v[q] : 0.0f;
     }
+    const unsigned rows = min(32u, a.tokens - row0);
+    float* sums = a.sums + ((size_t)split * a.tokens + row0) * a.width + column;
+    T* out = a.out + (size_t)row0 * a.ldo + column;
+    if (a.add && a.out) box.rows_join(sums, a.width, out, a.ldo, rows, left, v, [by](float old, float now) { return (old + now) * by; });
+    else if (a.add) box.rows_join(sums, a.width, sums, a.width, rows, left, v, [](float old, float now) { return old + now; });
+    else if (a.out) box.rows_out(out, a.ldo, rows, left, v);
+    else box.rows_out(sums, a.width, rows, left, v);
   }
   __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ void finish(const Args&) {}
 };
 
 template <typename T>
@@ -320,21 +323,20 @@ struct WeightEpilogue {
     size_t ldo;
     unsigned rows;
   };
+  static constexpr unsigned kBox = 4096;
+  Box box;
   float unscale;
-  T* out;
-  __device__ __forceinline__ WeightEpilogue(const Args& a, unsigned char*) { unscale = a.prepared->unscale; }
-  __device__ __forceinline__ void begin(const Args& a, const HalfPlace&, unsigned row0, unsigned lane, unsigned) {
-    out = row0 + lane < a.rows ? a.out + (size_t)(row0 + lane) * a.ldo : nullptr;
-  }
-  __device__ __forceinline__ void unit(const Args&, unsigned column, unsigned left, float (&v)[32]) {
-    if (!out) return;
-    float d[32];
+  unsigned row0;
+  __device__ __forceinline__ WeightEpilogue(const Args& a, const Box& b) : box(b) { unscale = a.prepared->unscale; }
+  __device__ __forceinline__ void ahead(const Args&, unsigned) {}
+  __device__ __forceinline__ void begin(const Args&, const HalfPlace&, unsigned first_row, unsigned) { row0 = first_row; }
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) d[q] = v[q] * unscale;
-    store_row32(out + column, d, left);
+    for (unsigned q = 0; q < 32; ++q) v[q] *= unscale;
+    box.rows_out(a.out + (size_t)row0 * a.ldo + column, a.ldo, min(32u, a.rows - row0), left, v);
   }
   __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ void finish(const Args&) {}
 };
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -461,7 +463,8 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
     p.p = {h, nullptr, b.ldh, 0, false};
     p.q = {w_piece, nullptr, b.ldw, 0, false};
     p.P = b.T; p.Q = columns; p.K = b.D;
-    const typename GradEpilogue<T>::Args grad = {b.targets, b.lse, b.g, b.kinds, prepared, dz, b.g_stride, z.dz_ld, tokens, (unsigned)first};
+    typename GradEpilogue<T>::Args grad = {{}, b.targets, b.lse, b.g, b.kinds, prepared, b.g_stride, tokens, (unsigned)first};
+    if (!box_map(&grad.dz, dz, kBf16, b.T, columns, z.dz_ld, 1, 0)) return SSGD_ERR_CUDA;
     st = launch_half<GradEpilogue<T>, 1, 0>(p, grad, half_form(p, 1, 1, sms), 1, sms, s);
     if (st != SSGD_OK) break;
     if (b.dh) {

@@ -31,6 +31,144 @@ namespace {
 constexpr int kHalfThreads = 384;                 // a warpgroup for copies and MMAs, two that write out
 constexpr unsigned kHalfPolls = 200000;           // bound of a wait, about 0.2 s
 
+// ---------------------------------------------------------------------------------------------------------------------
+// What epilogues share.  A thread has 32 neighbours of a row, memory wants neighbours from the lanes of a warp: 32 x 32 elements
+// change hands in a warp's box.  (Threads that went to memory by themselves, 16 bytes of their rows at a time, made 32 lookups of every
+// access: 480 us for 24 matrices of 1024 x 4096 where their product takes 150.)
+
+struct Box {
+  unsigned at, full, lane;      // shared memory; two barriers; this thread
+  bool fine = true;             // no wait has run out
+  unsigned pending = 0, phase = 0;      // bits of the two barriers: asked for and not yet there; parity
+  __device__ __forceinline__ Box(unsigned at_, unsigned full_, unsigned lane_) : at(at_), full(full_), lane(lane_) {}
+
+  // 16-bit elements, a row 64 bytes, as copies with 64-byte swizzle have them.
+  __device__ __forceinline__ unsigned place16(unsigned offset, unsigned row, unsigned piece) const {
+    return at + offset + row * 64 + ((piece ^ (row >> 1 & 3u)) << 4);
+  }
+  template <typename T>
+  __device__ __forceinline__ void put16(unsigned offset, const float* v) const {
+#pragma unroll
+    for (unsigned q = 0; q < 4; ++q)
+      store_shared16(place16(offset, lane, q), pack2(T(), v[8 * q], v[8 * q + 1]), pack2(T(), v[8 * q + 2], v[8 * q + 3]), pack2(T(), v[8 * q + 4], v[8 * q + 5]),
+                     pack2(T(), v[8 * q + 6], v[8 * q + 7]));
+  }
+  // What is left of v beside its fp16 part, in fp16.
+  __device__ __forceinline__ void put_low(unsigned offset, const float* v) const {
+#pragma unroll
+    for (unsigned q = 0; q < 4; ++q) {
+      float w[8];
+#pragma unroll
+      for (unsigned i = 0; i < 8; ++i) w[i] = v[8 * q + i] - __half2float(__float2half_rn(v[8 * q + i]));
+      store_shared16(place16(offset, lane, q), pack2(__half(), w[0], w[1]), pack2(__half(), w[2], w[3]), pack2(__half(), w[4], w[5]), pack2(__half(), w[6], w[7]));
+    }
+  }
+  // Transposed: this thread's row is a column of the box.
+  template <bool LOW>
+  __device__ __forceinline__ void put_across(unsigned offset, const float* v) const {
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) {
+      __half h = __float2half_rn(v[q]);
+      if (LOW) h = __float2half_rn(v[q] - __half2float(h));
+      asm volatile("st.shared.b16 [%0], %1;" ::"r"(place16(offset, q, lane >> 3) + (lane & 7u) * 2), "h"(__half_as_ushort(h)) : "memory");
+    }
+  }
+  __device__ __forceinline__ void get8(unsigned offset, unsigned piece, float (&v)[8]) const {
+    unsigned a, b, c, d;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(a), "=r"(b), "=r"(c), "=r"(d) : "r"(place16(offset, lane, piece)) : "memory");
+    v[0] = low_to_float(__half(), a); v[1] = high_to_float(__half(), a); v[2] = low_to_float(__half(), b); v[3] = high_to_float(__half(), b);
+    v[4] = low_to_float(__half(), c); v[5] = high_to_float(__half(), c); v[6] = low_to_float(__half(), d); v[7] = high_to_float(__half(), d);
+  }
+  // Shared memory as the threads have written it goes out; several may follow one another behind one fence.
+  __device__ __forceinline__ void fence() const {
+    async_proxy_fence();
+    __syncwarp();
+  }
+  __device__ __forceinline__ void send(const CUtensorMap& map, unsigned offset, unsigned x, unsigned y, unsigned z) const {
+    if (lane == 0) tma_store_3d(&map, (int)x, (int)y, (int)z, at + offset);
+  }
+  // What went out may be overwritten.
+  __device__ __forceinline__ void sent() const {
+    if (lane == 0) tma_store_wait_read();
+    __syncwarp();
+  }
+  __device__ __forceinline__ void sent_but_last() const {
+    if (lane == 0) tma_store_wait_read_but_last();
+    __syncwarp();
+  }
+  // 32 x 32 elements of 16 bits of one or two matrices to `offset` (and 2048 behind), counted on barrier b; and the wait for them.
+  __device__ __forceinline__ void ask(unsigned b, unsigned offset, const CUtensorMap& first, const CUtensorMap* second, unsigned x, unsigned y, unsigned z) {
+    if (lane == 0) {
+      mbarrier_expect(full + 8 * b, second ? 4096 : 2048);
+      tma_load_3d(at + offset, &first, (int)x, (int)y, (int)z, full + 8 * b);
+      if (second) tma_load_3d(at + offset + 2048, second, (int)x, (int)y, (int)z, full + 8 * b);
+    }
+    pending |= 1u << b;
+  }
+  __device__ __forceinline__ void take(unsigned b) {
+    fine = __all_sync(0xFFFFFFFFu, mbarrier_wait(full + 8 * b, phase >> b & 1u, kHalfPolls)) && fine;
+    phase ^= 1u << b;
+    pending &= ~(1u << b);
+  }
+  __device__ __forceinline__ void finish() {
+    if (lane == 0) tma_store_wait();
+    for (unsigned b = 0; b < 2; ++b)
+      if (pending >> b & 1u) take(b);           // asked for, and given up before it was used
+  }
+
+  // fp32 elements, a row 128 bytes, its eight pieces of 16 in an order of its own, so that rows and columns are read without conflicts.
+  __device__ __forceinline__ unsigned place32(unsigned row, unsigned column) const { return at + row * 128 + (((column >> 2) ^ (row & 7u)) << 4) + (column & 3u) * 4; }
+  __device__ __forceinline__ void put32(const float* v) const {
+    __syncwarp();
+#pragma unroll
+    for (unsigned q = 0; q < 8; ++q)
+      store_shared16(place32(lane, 4 * q), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+    __syncwarp();
+  }
+  __device__ __forceinline__ float get32(unsigned row, unsigned column) const {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(place32(row, column)) : "memory");
+    return v;
+  }
+  // The box's first `rows` rows and `left` columns to memory at any place and stride, lanes side by side: one element each, or, 16 bits
+  // that start at multiples of four bytes, two elements of two rows at a time.
+  template <typename T>
+  __device__ __forceinline__ void rows_out(T* o, size_t ld, unsigned rows, unsigned left, const float* v) const {
+    put32(v);
+    if (sizeof(T) == 2 && ((reinterpret_cast<uintptr_t>(o) & 3u) | (ld & 1u)) == 0) {
+      const unsigned c = (lane & 15u) * 2;
+      T* p = o + (lane >> 4) * ld + c;
+#pragma unroll 8
+      for (unsigned r = lane >> 4; r < rows; r += 2, p += 2 * ld) {
+        float a, b;
+        asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(a), "=f"(b) : "r"(place32(r, c)) : "memory");
+        if constexpr (sizeof(T) == 2) {
+          if (c + 1 < left) *reinterpret_cast<unsigned*>(p) = pack2(T(), a, b);
+          else if (c < left) *p = from_float<T>(a);
+        }
+      }
+    } else if (lane < left) {
+      T* p = o + lane;
+#pragma unroll 8
+      for (unsigned r = 0; r < rows; ++r, p += ld) *p = from_float<T>(get32(r, lane));
+    }
+  }
+  // out = f(what is in memory, the box's value), row by row, eight loads in flight.
+  template <typename T, typename F>
+  __device__ __forceinline__ void rows_join(const float* in, size_t ld_in, T* o, size_t ld, unsigned rows, unsigned left, const float* v, F f) const {
+    put32(v);
+    if (lane >= left) return;
+    for (unsigned r0 = 0; r0 < rows; r0 += 8) {
+      float old[8];
+#pragma unroll
+      for (unsigned u = 0; u < 8; ++u) old[u] = r0 + u < rows ? in[(r0 + u) * ld_in + lane] : 0.0f;
+#pragma unroll
+      for (unsigned u = 0; u < 8; ++u)
+        if (r0 + u < rows) o[(r0 + u) * ld + lane] = from_float<T>(f(old[u], get32(r0 + u, lane)));
+    }
+  }
+};
+
 struct HalfMaps {
   CUtensorMap p[2], q[2];                         // high and low part (TERMS = 3); TERMS = 1: q[1] may be another choice for q
 };
@@ -51,22 +189,22 @@ struct HalfPlan {
 
 struct HalfPlace { unsigned matrix, split, p0, q0, tile, tile_q, rows; };      // rows: of P in a tile
 
-template <bool PAIR, int NT, int TERMS>
+template <bool PAIR, int NT, int TERMS, unsigned BOX>
 struct HalfShape {
   static constexpr unsigned rows = PAIR ? 256 : 128;                       // of P in a tile
   static constexpr unsigned q_rows = PAIR ? NT / 2 : NT;                   // of Q that a CTA loads
   static constexpr unsigned parts = TERMS == 3 ? 2 : 1;
   static constexpr unsigned p_bytes = 128 * 128, q_bytes = q_rows * 128;
   static constexpr unsigned stage_bytes = parts * (p_bytes + q_bytes);
-  static constexpr unsigned box_bytes = 4096, out_bytes = 8 * box_bytes;   // the eight warps' room on the way out
-  static constexpr unsigned bar_bytes = 256;
+  static constexpr unsigned box_bytes = BOX, out_bytes = 8 * box_bytes;    // the eight warps' room on the way out
+  static constexpr unsigned bar_bytes = 384;
   static constexpr unsigned room = 232448 - out_bytes - bar_bytes;
   static constexpr unsigned stages = room / stage_bytes < 8 ? room / stage_bytes : 8;
   static constexpr unsigned columns = 2 * NT;                              // two accumulators
   // more than half of an SM's shared memory always: CTAs that hold and wait for tensor memory on one SM would never end
   static constexpr unsigned needed = stages * stage_bytes + out_bytes + bar_bytes;
   static constexpr unsigned smem = needed < 118784 ? 118784 : needed;
-  static_assert(stages >= 3 && (2 * stages + 5) * 8 + 8 <= bar_bytes && columns <= 512 && q_rows % 64 == 0, "shape");
+  static_assert(stages >= 3 && (2 * stages + 5 + 16) * 8 + 8 <= bar_bytes && columns <= 512 && q_rows % 64 == 0, "shape");
 };
 
 // Tiles go through bands of eight of P's tiles, so that those in flight share rows of both operands.
@@ -94,23 +232,26 @@ __device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p
 }
 
 // What an epilogue offers, besides its Args:
-//   begin(args, place, row0, lane, odd)   before a tile's first columns; this thread's row is row0 + lane, odd: which half of the columns
-//   unit(args, column, left, v)           32 sums of columns column .., `left` of them inside; it may change them
-//   end(args, place, warp)                behind the last; every thread of the warp calls it
-//   finish()                              behind the last tile
+//   kBox                            bytes of shared memory of a warp
+//   begin(args, place, row0, odd)   before a tile's first columns; a thread's row is row0 + lane, odd: which half of the columns
+//   ahead(args, column)             before the sums of those columns are there: what it needs of memory may be asked for
+//   unit(args, column, left, v)     32 sums of columns column .., `left` of them inside; it may change them
+//   end(args, place, warp)          behind the last
+//   finish(args)                    behind the last tile
+// All threads of a warp call each of them.
 constexpr unsigned kShiftRegisters = 168;
 __host__ __device__ constexpr bool half_shifts(int nt, int chunk) { return nt == 256 && chunk > 0; }
 
 template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK>
 __global__ void __launch_bounds__(kHalfThreads, 1)
-half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, const typename Epilogue::Args args) {
-  using S = HalfShape<PAIR, NT, TERMS>;
+half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, const __grid_constant__ typename Epilogue::Args args) {
+  using S = HalfShape<PAIR, NT, TERMS, Epilogue::kBox>;
   extern __shared__ __align__(1024) unsigned char half_smem[];           // stages, boxes, barriers; the same place in both CTAs
   uint64_t* bars = reinterpret_cast<uint64_t*>(half_smem + S::stages * S::stage_bytes + S::out_bytes);
-  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 5), &failed = *(&tmem_base + 1);
+  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 5 + 16), &failed = *(&tmem_base + 1);
   const unsigned rank = PAIR ? cluster_rank() : 0;
   const unsigned stage0 = smem_u32(half_smem);
-  const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 16, ended = acc_free + 16;
+  const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 16, ended = acc_free + 16, box_full = ended + 8;
   const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const unsigned worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
 
@@ -126,6 +267,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       mbarrier_init(acc_free + 8 * b, PAIR ? 16 : 8);     // one arrival from each of the CTAs' eight epilogue warps
     }
     mbarrier_init(ended, 1);
+    for (unsigned b = 0; b < 16; ++b) mbarrier_init(box_full + 8 * b, 1);      // two for each epilogue warp
     mbarrier_init_fence();
     failed = 0;
   }
@@ -255,12 +397,13 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
     constexpr unsigned kUnits = NT / 64;        // of 32 columns, of this warp
     const unsigned quarter = warp & 3u, odd = warp >= 8;
     const unsigned go = PAIR ? cluster_address(acc_free, 0) : acc_free;
-    Epilogue epilogue(args, half_smem + S::stages * S::stage_bytes + (warp - 4) * S::box_bytes);
+    Epilogue epilogue(args, Box{stage0 + S::stages * S::stage_bytes + (warp - 4) * S::box_bytes, box_full + 16 * (warp - 4), lane});
     unsigned t = 0;
     for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
       const HalfPlace at = half_place<PAIR, NT>(tile, p);
       const unsigned row0 = at.p0 + rank * 128 + quarter * 32;
-      epilogue.begin(args, at, row0, lane, odd);
+      epilogue.begin(args, at, row0, odd);
+      if (row0 < p.P && at.q0 + odd * 32 < p.Q) epilogue.ahead(args, at.q0 + odd * 32);
       if constexpr (CHUNK > 0) {
         const unsigned first = (unsigned)((uint64_t)p.k_stages * at.split / p.splits), last = (unsigned)((uint64_t)p.k_stages * (at.split + 1) / p.splits);
         float sum[kUnits][32];
@@ -286,6 +429,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
 #pragma unroll
         for (unsigned j = 0; j < kUnits; ++j) {
           const unsigned column = at.q0 + (odd + 2 * j) * 32;
+          if (j + 1 < kUnits && row0 < p.P && column + 64 < p.Q) epilogue.ahead(args, column + 64);
           if (row0 < p.P && column < p.Q) epilogue.unit(args, column, min(32u, p.Q - column), sum[j]);
           __syncwarp();
         }
@@ -307,6 +451,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
 #pragma unroll
           for (unsigned q = 0; q < 32; ++q) f[q] = __uint_as_float(v[q]);
           const unsigned column = at.q0 + (odd + 2 * j) * 32;
+          if (j + 1 < kUnits && row0 < p.P && column + 64 < p.Q) epilogue.ahead(args, column + 64);
           if (row0 < p.P && column < p.Q) epilogue.unit(args, column, min(32u, p.Q - column), f);
           __syncwarp();
         }
@@ -314,8 +459,9 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       }
       epilogue.end(args, at, rank * 8 + warp - 4);
       __syncwarp();
+      ok = epilogue.box.fine;
     }
-    epilogue.finish();
+    epilogue.finish(args);
   }
   if (!ok) atomicExch(&failed, 1u);
   __syncwarp();
@@ -334,57 +480,6 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
     if (PAIR) tmem_free_pair(tmem, S::columns);
     else tmem_free(tmem, S::columns);
   }
-}
-
-// ---------------------------------------------------------------------------------------------------------------------
-// What epilogues share: 32 neighbours of a row between a thread and memory.
-
-// Any place, `left` of them.
-template <typename T>
-__device__ __forceinline__ void store_row32(T* o, const float (&v)[32], unsigned left) {
-  if (left >= 32 && (reinterpret_cast<uintptr_t>(o) & 15u) == 0) {
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (unsigned q = 0; q < 8; ++q) reinterpret_cast<float4*>(o)[q] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-    } else {
-#pragma unroll
-      for (unsigned q = 0; q < 4; ++q)
-        reinterpret_cast<uint4*>(o)[q] = make_uint4(pack2(T(), v[8 * q], v[8 * q + 1]), pack2(T(), v[8 * q + 2], v[8 * q + 3]),
-                                                    pack2(T(), v[8 * q + 4], v[8 * q + 5]), pack2(T(), v[8 * q + 6], v[8 * q + 7]));
-    }
-  } else {
-#pragma unroll
-    for (unsigned q = 0; q < 32; ++q)
-      if (q < left) o[q] = from_float<T>(v[q]);
-  }
-}
-template <typename T>
-__device__ __forceinline__ void load_row32(const T* o, float (&v)[32], unsigned left) {
-  if (left >= 32 && (reinterpret_cast<uintptr_t>(o) & 15u) == 0) {
-#pragma unroll
-    for (unsigned q = 0; q < 4; ++q) {
-      float w[8];
-      load8(o + 8 * q, w);
-#pragma unroll
-      for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = w[i];
-    }
-  } else {
-#pragma unroll
-    for (unsigned q = 0; q < 32; ++q) v[q] = q < left ? to_float(o[q]) : 0.0f;
-  }
-}
-
-// Eight neighbours at a time, for epilogues that hold a tile's sums in registers and have few left; 16-byte aligned.
-__device__ __forceinline__ void store8(__half* o, const float* v) {
-  *reinterpret_cast<uint4*>(o) = make_uint4(pack2(__half(), v[0], v[1]), pack2(__half(), v[2], v[3]), pack2(__half(), v[4], v[5]), pack2(__half(), v[6], v[7]));
-}
-__device__ __forceinline__ void store8(__nv_bfloat16* o, const float* v) {
-  *reinterpret_cast<uint4*>(o) = make_uint4(pack2(__nv_bfloat16(), v[0], v[1]), pack2(__nv_bfloat16(), v[2], v[3]), pack2(__nv_bfloat16(), v[4], v[5]),
-                                            pack2(__nv_bfloat16(), v[6], v[7]));
-}
-__device__ __forceinline__ void store8(float* o, const float* v) {
-  reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -419,6 +514,17 @@ struct HalfProduct {
   unsigned starve;
 };
 
+// A batch of 16-bit matrices as an epilogue's boxes see it: 32 x 32 elements, 64-byte swizzle.
+inline bool box_map(CUtensorMap* map, const void* base, bool bf16, size_t rows, size_t cols, size_t ld, size_t batch, size_t batch_stride) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const cuuint64_t dims[3] = {cols, rows, batch};
+  const cuuint64_t strides[2] = {ld * 2, (batch > 1 ? batch_stride : ld) * 2};
+  const cuuint32_t box[3] = {32, 32, 1}, steps[3] = {1, 1, 1};
+  return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box, steps,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Clocks of a product by tiles of a form: rounds of tiles, each its stages, beside a start.
 struct HalfForm { bool pairs; unsigned nt; };
 inline unsigned long long half_tiles(const HalfProduct& h, unsigned rows, unsigned nt) {
@@ -440,7 +546,7 @@ inline HalfForm half_form(const HalfProduct& h, int terms, unsigned splits, int 
 
 template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK>
 ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args& args, unsigned splits, int sms, cudaStream_t s) {
-  using S = HalfShape<PAIR, NT, TERMS>;
+  using S = HalfShape<PAIR, NT, TERMS, Epilogue::kBox>;
   HalfPlan p = {};
   const unsigned long long per = half_tiles(h, S::rows, NT), tiles = per * h.batch * splits;
   if (h.P >= (1ull << 31) || h.Q >= (1ull << 31) || h.K >= (1ull << 31) || tiles >= (1ull << 30)) return SSGD_ERR_SIZE;

@@ -5,13 +5,12 @@
 //
 // Three products a step, on the tensor cores, A and A^2 by the tiles on and above their diagonals alone.  An fp16 operand has
 // eleven bits, and what a step loses, the next ones multiply by up to a (a direction whose singular value is still small grows
-// by that), so the arithmetic is arranged to lose little:
-//   - with d = |X|_F^2 / s (s the shorter side), A = d I + E, and the step is  X <- (a + b d + c d^2) X + ((b + 2 c d) E + c E^2) X:  the
-//     part along X is done in fp32, and what goes through fp16 shrinks as X approaches its goal (A near I, E small).  For 16-bit
-//     results: error of X relative 4e-4 .. 1e-3, without this 2e-3 .. 3e-3; the rounding to bf16 alone is 1.7e-3
-//   - X is kept as the sum of two fp16 matrices, so that (a + ..) X loses nothing
-//   - TERMS = 3: products take both parts of each operand (22 bits; error 2e-7 .. 4e-6, an fp32 product's 1e-6 .. 1e-5); TERMS = 1:
-//     the high parts alone
+// by that).  Two ways:
+//   TERMS = 3  every matrix is the sum of two fp16 matrices (22 bits), a product three: error 2e-7 .. 1e-6 of the result, products in fp32
+//              1e-6 .. 5e-6.  b A + c A^2 is had from the square of A + (b / 2 c) I, so that nothing is read beside the operands
+//   TERMS = 1  products of the high parts alone, X still kept in two.  With d = |X|_F^2 / s (s the shorter side) and A = d I + E the step
+//              is  X <- (a + b d + c d^2) X + ((b + 2 c d) E + c E^2) X:  the part along X is done in fp32, and what goes through fp16 shrinks as X
+//              approaches its goal (A near I, E small).  Error 4e-4 .. 1e-3, without this 2e-3 .. 3e-3; rounding to bf16 alone is 1.7e-3
 // All matrices are stored times 2^13: elements are at most 1.2 in size, and the smallest that count stay normal numbers of fp16.
 
 #include "half_product.cuh"
@@ -21,161 +20,164 @@ namespace {
 constexpr float kScale = 8192.0f, kUnscale = 1.0f / 8192.0f;      // of X, E and M as they are stored
 
 struct Polynomial { float a, b, c; };
-struct Step { float q, p, c; };                                    // X' = q X + (p E + c E^2) X
-__device__ __forceinline__ Step step_of(const Polynomial& f, float d) {
-  return {f.a + d * (f.b + d * f.c), f.b + 2.0f * f.c * d, f.c};
-}
 
-// What a value is stored as.
-__device__ __forceinline__ void split_half(float v, __half* high, __half* low) {
-  *high = __float2half_rn(v);
-  *low = __float2half_rn(v - __half2float(*high));
-}
+// The 16-bit matrices that the products leave to one another, as boxes: high and low part.
+struct Parts { CUtensorMap high, low; };
 
-// Eight neighbours of a row as high and low part.  The matrices' rows are padded to whole 64 columns, so that nobody has to ask
-// where they end.
+// 32 x 32 elements of a symmetric matrix: there, and, from tiles wholly above the diagonal, mirrored.  Tiles on the diagonal hold
+// both halves themselves.
 template <bool LOW>
-__device__ __forceinline__ void store_split8(__half* high, __half* low, size_t at, const float* v) {
-  float h[8];
-#pragma unroll
-  for (unsigned q = 0; q < 8; ++q) h[q] = __half2float(__float2half_rn(v[q]));
-  store8(high + at, h);
-  if constexpr (LOW) {
-#pragma unroll
-    for (unsigned q = 0; q < 8; ++q) h[q] = v[q] - h[q];
-    store8(low + at, h);
+__device__ __forceinline__ void send_symmetric(const Box& box, unsigned offset, const Parts& to, unsigned row0, unsigned column, unsigned matrix, bool mirrored,
+                                               const float* v) {
+  box.sent();
+  box.put16<__half>(offset, v);
+  if (LOW) box.put_low(offset + 2048, v);
+  else if (mirrored) box.put_across<false>(offset + 2048, v);
+  box.fence();
+  box.send(to.high, offset, column, row0, matrix);
+  if (LOW) box.send(to.low, offset + 2048, column, row0, matrix);
+  if (!mirrored) return;
+  if (LOW) {
+    box.sent();
+    box.put_across<false>(offset, v);
+    box.put_across<true>(offset + 2048, v);
+    box.fence();
+    box.send(to.low, offset + 2048, row0, column, matrix);
   }
-}
-template <bool LOW>
-__device__ __forceinline__ void load_split8(const __half* high, const __half* low, size_t at, float (&v)[8]) {
-  load8(high + at, v);
-  if constexpr (LOW) {
-    float w[8];
-    load8(low + at, w);
-#pragma unroll
-    for (unsigned q = 0; q < 8; ++q) v[q] += w[q];
-  }
+  box.send(to.high, LOW ? offset : offset + 2048, row0, column, matrix);
 }
 
-struct Square {                   // a batch of symmetric matrices, high and low part
-  __half *high, *low;
-  size_t ld, stride;
-  unsigned side;
-};
-
-// A thread's 32 columns of a row of a symmetric matrix: there, and, from tiles wholly above the diagonal, mirrored (lanes side by
-// side).  Tiles on the diagonal hold both halves themselves.
-template <bool LOW>
-__device__ __forceinline__ void store_symmetric(const Square& s, size_t matrix, unsigned row, unsigned column, unsigned left, bool mirrored, const float (&v)[32]) {
-#pragma unroll
-  for (unsigned c = 0; c < 32; c += 8) store_split8<LOW>(s.high, s.low, matrix + (size_t)row * s.ld + column + c, v + c);
-  if (mirrored) {
-#pragma unroll
-    for (unsigned q = 0; q < 32; ++q) {
-      if (q < left) {
-        __half high, low;
-        split_half(v[q], &high, &low);
-        s.high[matrix + (size_t)(column + q) * s.ld + row] = high;
-        if (LOW) s.low[matrix + (size_t)(column + q) * s.ld + row] = low;
-      }
-    }
-  }
-}
-
-// E = X X^T - d I.  d comes from the sums of squares that the last step left, added in a fixed order by each warp; the first tile
-// of each matrix leaves it for the other two products.
+// The product X X^T.  High parts alone: E = A - d I, where d comes from the sums of squares that the last step left, added in a fixed
+// order by each warp; the first tile of each matrix leaves it for the other two products.  Both parts: A + (b / 2 c) I, see below.
 template <bool LOW>
 struct GramEpilogue {
   struct Args {
-    Square e;
+    Parts e;
     const float* squares;       // [matrix][count], or null: |X| is 1
     float* d;                   // [matrix]
-    unsigned count;
+    unsigned count, side;
+    float shift;
   };
-  float d;
-  unsigned row, seen;
-  size_t matrix;
-  bool mirrored, inside;
-  __device__ __forceinline__ GramEpilogue(const Args&, unsigned char*) { seen = ~0u; }
-  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
-    row = row0 + lane;
-    inside = row < a.e.side;
+  static constexpr unsigned kBox = 4096;
+  Box box;
+  float diagonal;               // what is added there
+  unsigned row0, seen, matrix;
+  bool mirrored;
+  __device__ __forceinline__ GramEpilogue(const Args& a, const Box& b) : box(b), diagonal(a.shift * kScale), seen(~0u) {}
+  __device__ __forceinline__ void ahead(const Args&, unsigned) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
+    row0 = first_row;
+    matrix = at.matrix;
     mirrored = at.q0 >= at.p0 + at.rows;
-    matrix = at.matrix * a.e.stride;
-    if (at.matrix != seen) {
-      seen = at.matrix;
-      float sum = 1.0f;
-      if (a.squares) {
-        sum = 0.0f;
-        for (unsigned i = lane; i < a.count; i += 32) sum += a.squares[(size_t)at.matrix * a.count + i];
+    if (!LOW) {
+      if (matrix != seen) {
+        seen = matrix;
+        float sum = 1.0f;
+        if (a.squares) {
+          sum = 0.0f;
+          for (unsigned i = box.lane; i < a.count; i += 32) sum += a.squares[(size_t)matrix * a.count + i];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+          for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+        }
+        diagonal = -(sum / (float)a.side) * kScale;
       }
-      d = sum / (float)a.e.side;
+      if (at.tile == 0 && row0 + box.lane == 0) a.d[matrix] = diagonal * -kUnscale;      // two warps: the same value
     }
-    if (at.tile == 0 && row == 0) a.d[at.matrix] = d;      // two warps: the same value
   }
-  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
-    if (!inside) return;
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned, float (&v)[32]) {
+    const unsigned on = row0 + box.lane - column;
 #pragma unroll
     for (unsigned q = 0; q < 32; ++q) v[q] *= kUnscale;
-    if (row - column < 32u) {
+    if (on < 32u) {
 #pragma unroll
-      for (unsigned q = 0; q < 32; ++q)
-        v[q] = row - column == q ? v[q] - d * kScale : v[q];
+      for (unsigned q = 0; q < 32; ++q) v[q] = on == q ? v[q] + diagonal : v[q];
     }
-    store_symmetric<LOW>(a.e, matrix, row, column, left, mirrored, v);
+    send_symmetric<LOW>(box, 0, a.e, row0, column, matrix, mirrored, v);
   }
   __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ void finish(const Args&) { box.finish(); }
 };
 
-// M = p E + c E^2.
+// The polynomial from the square of what the first product left.
+//   high parts alone   M = p E + c E^2 with p = b + 2 c d;  X' = (a + b d + c d^2) X + M X
+//   both parts         M = a I + b A + c A^2 = (a - b^2 / 4 c) I + c (A + (b / 2 c) I)^2, nothing to be read again;  X' = M X.  Where c is too
+//                      small for that, shift = 0 and A is read
 template <bool LOW>
 struct PolynomialEpilogue {
   struct Args {
-    Square e, m;
+    Parts e, m;
     const float* d;
     Polynomial f;
+    float diagonal;             // LOW: what is added there
+    unsigned shifted;
   };
-  Step s;
-  unsigned row;
-  size_t matrix;
-  bool mirrored, inside;
-  __device__ __forceinline__ PolynomialEpilogue(const Args&, unsigned char*) {}
-  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
-    row = row0 + lane;
-    inside = row < a.e.side;
+  static constexpr unsigned kBox = LOW ? 4096 : 8192;     // high parts: two boxes for E, two on their way out
+  Box box;
+  float p;
+  unsigned row0, matrix, asks, takes;
+  bool mirrored;
+  __device__ __forceinline__ PolynomialEpilogue(const Args&, const Box& b) : box(b), asks(0), takes(0) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
+    row0 = first_row;
+    matrix = at.matrix;
     mirrored = at.q0 >= at.p0 + at.rows;
-    matrix = at.matrix * a.e.stride;
-    s = step_of(a.f, a.d[at.matrix]);
+    if (!LOW) p = a.f.b + 2.0f * a.f.c * a.d[matrix];
   }
-  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
-    if (!inside) return;
-#pragma unroll
-    for (unsigned c = 0; c < 32; c += 8) {
-      float e[8];
-      load_split8<LOW>(a.e.high, a.e.low, matrix + (size_t)row * a.e.ld + column + c, e);
-#pragma unroll
-      for (unsigned q = 0; q < 8; ++q) v[c + q] = fmaf(s.c, v[c + q] * kUnscale, s.p * e[q]);
+  __device__ __forceinline__ void ahead(const Args& a, unsigned column) {
+    if (!LOW) {
+      box.ask(asks & 1u, (asks & 1u) * 2048, a.e.high, nullptr, column, row0, matrix);
+      ++asks;
     }
-    store_symmetric<LOW>(a.m, matrix, row, column, left, mirrored, v);
+  }
+  __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned, float (&v)[32]) {
+    const float c = a.f.c * kUnscale;
+    if (!LOW) {
+      const unsigned b = takes++ & 1u;
+      box.take(b);
+#pragma unroll
+      for (unsigned q = 0; q < 4; ++q) {
+        float e[8];
+        box.get8(b * 2048, q, e);
+#pragma unroll
+        for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = fmaf(c, v[8 * q + i], p * e[i]);
+      }
+    } else if (a.shifted) {
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) v[q] *= c;
+    } else {
+      box.sent();
+      box.ask(0, 0, a.e.high, &a.e.low, column, row0, matrix);
+      box.take(0);
+#pragma unroll
+      for (unsigned q = 0; q < 4; ++q) {
+        float high[8], low[8];
+        box.get8(0, q, high);
+        box.get8(2048, q, low);
+#pragma unroll
+        for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = fmaf(c, v[8 * q + i], a.f.b * (high[i] + low[i]));
+      }
+      __syncwarp();
+    }
+    if (LOW) {
+      const unsigned on = row0 + box.lane - column;
+      if (on < 32u) {
+#pragma unroll
+        for (unsigned q = 0; q < 32; ++q) v[q] = on == q ? v[q] + a.diagonal : v[q];
+      }
+    }
+    send_symmetric<LOW>(box, LOW ? 0 : 4096, a.m, row0, column, matrix, mirrored, v);
   }
   __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
-  __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ void finish(const Args&) { box.finish(); }
 };
 
-struct Whole {                    // a batch of matrices X, high and low part
-  __half *high, *low;
-  size_t ld, stride;
-};
-
-// X' = q X + M X: kept for the next step, with its sum of squares; or, behind the last, written out as T; or x <- x - delta X'.
+// X' = M X, or of the high parts (a + b d + c d^2) X + M X: kept for the next step, with its sum of squares; or, behind the last, written
+// out as T; or x <- x - delta X'.
 enum UpdateTo { kNextStep, kOut, kParameters };
-template <int TO, typename T>
+template <int TO, typename T, bool LOW>
 struct UpdateEpilogue {
   struct Args {
-    Whole x, next;
+    Parts x, next;
     const float* d;
     float* squares;             // [matrix][count]
     T* out;
@@ -184,71 +186,87 @@ struct UpdateEpilogue {
     float delta;
     unsigned rows, count, slots;        // sums of squares of a matrix, and of a tile
   };
+  // two boxes of X's parts, in which X' goes out again, and one of fp32
+  static constexpr unsigned kLoads = LOW ? 0 : 8192, kBox = kLoads + (LOW || TO != kNextStep ? 4096 : 0);
+  Box box;
   float q, sum;
-  unsigned row;
-  bool inside;
-  size_t at_x;
-  T* out;
-  __device__ __forceinline__ UpdateEpilogue(const Args&, unsigned char*) {}
-  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned lane, unsigned) {
-    row = row0 + lane;
-    inside = row < a.rows;
-    at_x = at.matrix * a.x.stride + (size_t)row * a.x.ld;
-    if (TO != kNextStep && inside) out = a.out + at.matrix * a.out_stride + (size_t)row * a.ldo;
-    q = step_of(a.f, a.d[at.matrix]).q;
-    sum = 0.0f;
+  unsigned row0, matrix, asks, takes;
+  __device__ __forceinline__ UpdateEpilogue(const Args&, const Box& b) : box(b), asks(0), takes(0) {}
+  __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
+    row0 = first_row;
+    matrix = at.matrix;
+    if (!LOW) {
+      const float d = a.d[matrix];
+      q = a.f.a + d * (a.f.b + d * a.f.c);
+      sum = 0.0f;
+    }
+  }
+  __device__ __forceinline__ void ahead(const Args& a, unsigned column) {
+    if (!LOW) {
+      if (TO == kNextStep) box.sent();
+      box.ask(asks & 1u, (asks & 1u) * 4096, a.x.high, &a.x.low, column, row0, matrix);
+      ++asks;
+    }
   }
   __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
-    if (!inside) return;
-    const bool wide = TO != kNextStep && left >= 32 && (reinterpret_cast<uintptr_t>(out + column) & 15u) == 0;
+    unsigned from = 0;
+    if (LOW) {
 #pragma unroll
-    for (unsigned c = 0; c < 32; c += 8) {
-      float x[8];
-      load_split8<true>(a.x.high, a.x.low, at_x + column + c, x);
+      for (unsigned i = 0; i < 32; ++i) v[i] *= kUnscale;
+      if (TO == kNextStep) box.sent();
+    } else {
+      const unsigned b = takes++ & 1u;
+      from = b * 4096;
+      box.take(b);
 #pragma unroll
-      for (unsigned i = 0; i < 8; ++i) v[c + i] = fmaf(q, x[i], v[c + i] * kUnscale);
-      if constexpr (TO == kNextStep) {
+      for (unsigned p = 0; p < 4; ++p) {
+        float high[8], low[8];
+        box.get8(from, p, high);
+        box.get8(from + 2048, p, low);
 #pragma unroll
-        for (unsigned i = 0; i < 8; ++i) sum = c + i < left ? fmaf(v[c + i], v[c + i], sum) : sum;
-        store_split8<true>(a.next.high, a.next.low, at_x + column + c, v + c);
-      } else if constexpr (TO == kOut) {
-#pragma unroll
-        for (unsigned i = 0; i < 8; ++i) v[c + i] *= kUnscale;
-        if (wide) {
-          store8(out + column + c, v + c);
-        } else {
-#pragma unroll
-          for (unsigned i = 0; i < 8; ++i)
-            if (c + i < left) out[column + c + i] = from_float<T>(v[c + i]);
-        }
-      } else {
-        const float step = a.delta * kUnscale;
-        if (wide) {
-          load8(out + column + c, x);
-#pragma unroll
-          for (unsigned i = 0; i < 8; ++i) x[i] = fmaf(-step, v[c + i], x[i]);
-          store8(out + column + c, x);
-        } else {
-#pragma unroll
-          for (unsigned i = 0; i < 8; ++i)
-            if (c + i < left) out[column + c + i] = fmaf(-step, v[c + i], out[column + c + i]);
-        }
+        for (unsigned i = 0; i < 8; ++i) v[8 * p + i] = fmaf(q, high[i] + low[i], v[8 * p + i] * kUnscale);
       }
+      __syncwarp();
+    }
+    if constexpr (TO == kNextStep) {
+      if (!LOW && row0 + box.lane < a.rows) {   // behind the last column there are zeros
+#pragma unroll
+        for (unsigned i = 0; i < 32; ++i) sum = fmaf(v[i], v[i], sum);
+      }
+      box.template put16<__half>(from, v);
+      box.put_low(from + 2048, v);
+      box.fence();
+      box.send(a.next.high, from, column, row0, matrix);
+      box.send(a.next.low, from + 2048, column, row0, matrix);
+    } else {
+      const float by = TO == kOut ? kUnscale : -a.delta * kUnscale;
+#pragma unroll
+      for (unsigned i = 0; i < 32; ++i) v[i] *= by;
+      Box whole(box.at + kLoads, box.full, box.lane);
+      T* o = a.out + matrix * a.out_stride + (size_t)row0 * a.ldo + column;
+      const unsigned rows = min(32u, a.rows - row0);
+      if constexpr (TO == kOut) whole.rows_out(o, a.ldo, rows, left, v);
+      else whole.rows_join(o, a.ldo, o, a.ldo, rows, left, v, [](float x, float step) { return x + step; });
     }
   }
   __device__ __forceinline__ void end(const Args& a, const HalfPlace& at, unsigned warp) {
-    if constexpr (TO == kNextStep) {
+    if constexpr (TO == kNextStep && !LOW) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-      if ((threadIdx.x & 31u) == 0) a.squares[(size_t)at.matrix * a.count + at.tile * a.slots + warp] = sum * (kUnscale * kUnscale);
+      if (box.lane == 0) a.squares[(size_t)matrix * a.count + at.tile * a.slots + warp] = sum * (kUnscale * kUnscale);
     }
   }
-  __device__ __forceinline__ void finish() {}
+  __device__ __forceinline__ void finish(const Args&) { box.finish(); }
 };
 
 // ---------------------------------------------------------------------------------------------------------------------
 // Before the products: the norm, then X's two parts.  A momentum step makes its U on the way, in both passes the same:
 //   m <- fma(beta, m, fl((1 - beta) g)),  u = m, or looking ahead fma(beta, m, fl((1 - beta) g))
+
+struct Whole {                    // a batch of matrices, high and low part
+  __half *high, *low;
+  size_t ld, stride;
+};
 
 struct Source {
   const void* u;                // the matrix itself; with a momentum the gradient
@@ -435,20 +453,20 @@ ssgd_status launch_source_typed(const Problem& p, const Layout& l, const Whole& 
 }
 
 // Stages between two times that a sum of three terms is taken.
-constexpr int kChunk = 2;
+constexpr int kChunk = 1;
 
 struct Buffers {
-  Whole x[2];
-  Square e, m;
+  Whole x[2], e, m;
+  Parts x_parts[2], e_parts, m_parts;
   float *d, *squares;
 };
 
 template <int TO, typename T, int TERMS>
-ssgd_status launch_update(const Problem& p, const Buffers& b, int now, unsigned* count, int sms, cudaStream_t s) {
+ssgd_status launch_update(const Problem& p, const Layout& l, const Buffers& b, int now, unsigned* count, int sms, cudaStream_t s) {
   const Whole& x = b.x[now];
   const HalfOperand whole = {x.high, x.low, x.ld, x.stride, false}, square = {b.m.high, b.m.low, b.m.ld, b.m.stride, false};
   HalfProduct h = {};
-  h.P = p.rows; h.Q = p.cols; h.K = b.m.side; h.batch = p.n;
+  h.P = p.rows; h.Q = p.cols; h.K = l.side; h.batch = p.n;
   h.status = p.status;
   h.starve = p.starve;
   if (p.rows <= p.cols) {                       // M X: X's columns are Q's rows
@@ -462,17 +480,22 @@ ssgd_status launch_update(const Problem& p, const Buffers& b, int now, unsigned*
   const HalfForm form = half_form(h, TERMS, 1, sms);
   const unsigned slots = form.pairs ? 16 : 8;                  // epilogue warps of a tile
   *count = slots * (unsigned)half_tiles(h, form.pairs ? 256 : 128, form.nt);
-  typename UpdateEpilogue<TO, T>::Args a = {};
-  a.x = x; a.next = b.x[1 - now]; a.d = b.d; a.squares = b.squares;
+  typename UpdateEpilogue<TO, T, TERMS == 3>::Args a = {};
+  a.x = b.x_parts[now]; a.next = b.x_parts[1 - now]; a.d = b.d; a.squares = b.squares;
   a.out = static_cast<T*>(p.out); a.ldo = p.ldo; a.out_stride = p.out_stride;
   a.f = p.f; a.delta = p.delta; a.rows = (unsigned)p.rows; a.count = *count; a.slots = slots;
-  return launch_half<UpdateEpilogue<TO, T>, TERMS, TERMS == 3 ? kChunk : 0>(h, a, form, 1, sms, s);
+  return launch_half<UpdateEpilogue<TO, T, TERMS == 3>, TERMS, TERMS == 3 ? kChunk : 0>(h, a, form, 1, sms, s);
 }
+
+// The largest |b / 2 c| that is added to A's diagonal: A + that, times 2^13, is an fp16 number, and little of A is lost beside it.
+constexpr float kMostShift = 4.0f;
 
 template <int TERMS>
 ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, int sms, cudaStream_t s) {
   unsigned count = 0;
   int now = 0;
+  const float shift = p.f.b / (2.0f * p.f.c);
+  const bool shifted = TERMS == 3 && p.f.c != 0.0f && fabsf(shift) <= kMostShift;
   for (unsigned k = 0; k < p.steps; ++k) {
     const Whole& x = b.x[now];
     HalfProduct h = {};
@@ -484,24 +507,29 @@ ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, i
     h.symmetric = true;
     h.status = p.status;
     h.starve = p.starve;
-    const typename GramEpilogue<TERMS == 3>::Args gram = {b.e, k ? b.squares : nullptr, b.d, count};
+    const typename GramEpilogue<TERMS == 3>::Args gram = {b.e_parts, k ? b.squares : nullptr, b.d, count, (unsigned)l.side, shifted ? shift : 0.0f};
     ssgd_status st = launch_half<GramEpilogue<TERMS == 3>, TERMS, TERMS == 3 ? kChunk : 0>(h, gram, half_form(h, TERMS, 1, sms), 1, sms, s);
     if (st != SSGD_OK) return st;
     h.p = {b.e.high, b.e.low, b.e.ld, b.e.stride, false};
     h.q = h.p;
     h.K = l.side;
-    const typename PolynomialEpilogue<TERMS == 3>::Args polynomial = {b.e, b.m, b.d, p.f};
+    const typename PolynomialEpilogue<TERMS == 3>::Args polynomial = {
+        b.e_parts, b.m_parts, b.d, p.f, kScale * (shifted ? p.f.a - p.f.b * shift * 0.5f : p.f.a), shifted};
     st = launch_half<PolynomialEpilogue<TERMS == 3>, TERMS, TERMS == 3 ? kChunk : 0>(h, polynomial, half_form(h, TERMS, 1, sms), 1, sms, s);
     if (st != SSGD_OK) return st;
-    if (k + 1 < p.steps) st = launch_update<kNextStep, float, TERMS>(p, b, now, &count, sms, s);
-    else if (p.momentum) st = launch_update<kParameters, float, TERMS>(p, b, now, &count, sms, s);
-    else if (p.out_type == SSGD_F32) st = launch_update<kOut, float, TERMS>(p, b, now, &count, sms, s);
-    else if (p.out_type == SSGD_BF16) st = launch_update<kOut, __nv_bfloat16, TERMS>(p, b, now, &count, sms, s);
-    else st = launch_update<kOut, __half, TERMS>(p, b, now, &count, sms, s);
+    if (k + 1 < p.steps) st = launch_update<kNextStep, float, TERMS>(p, l, b, now, &count, sms, s);
+    else if (p.momentum) st = launch_update<kParameters, float, TERMS>(p, l, b, now, &count, sms, s);
+    else if (p.out_type == SSGD_F32) st = launch_update<kOut, float, TERMS>(p, l, b, now, &count, sms, s);
+    else if (p.out_type == SSGD_BF16) st = launch_update<kOut, __nv_bfloat16, TERMS>(p, l, b, now, &count, sms, s);
+    else st = launch_update<kOut, __half, TERMS>(p, l, b, now, &count, sms, s);
     if (st != SSGD_OK) return st;
     now = 1 - now;
   }
   return SSGD_OK;
+}
+
+inline bool parts_of(Parts* parts, const Whole& w, size_t rows, size_t cols, size_t n) {
+  return box_map(&parts->high, w.high, false, rows, cols, w.ld, n, w.stride) && box_map(&parts->low, w.low, false, rows, cols, w.ld, n, w.stride);
 }
 
 inline bool fours_of(const void* p, size_t element, size_t ld, size_t stride, size_t n) {
@@ -542,8 +570,11 @@ ssgd_status solve(Problem p, const float* coefficients, cudaStream_t s) {
   auto half_at = [](char* at) { return reinterpret_cast<__half*>(at); };
   for (int i = 0; i < 2; ++i) b.x[i] = {half_at(x + (2 * i) * whole), half_at(x + (2 * i + 1) * whole), l.ldx, l.x_elements};
   char* e = p.ws + l.e;
-  b.e = {half_at(e), half_at(e + square), l.lds, l.e_elements, (unsigned)l.side};
-  b.m = {half_at(e + 2 * square), half_at(e + 3 * square), l.lds, l.e_elements, (unsigned)l.side};
+  b.e = {half_at(e), half_at(e + square), l.lds, l.e_elements};
+  b.m = {half_at(e + 2 * square), half_at(e + 3 * square), l.lds, l.e_elements};
+  if (!parts_of(&b.x_parts[0], b.x[0], p.rows, p.cols, p.n) || !parts_of(&b.x_parts[1], b.x[1], p.rows, p.cols, p.n) ||
+      !parts_of(&b.e_parts, b.e, l.side, l.side, p.n) || !parts_of(&b.m_parts, b.m, l.side, l.side, p.n))
+    return SSGD_ERR_CUDA;
   b.d = reinterpret_cast<float*>(p.ws + l.d);
   b.squares = reinterpret_cast<float*>(p.ws + l.squares);
   const ssgd_status st = p.momentum ? launch_source_typed<kMomentum>(p, l, b.x[0], s) : launch_source_typed<kPlainSource>(p, l, b.x[0], s);
