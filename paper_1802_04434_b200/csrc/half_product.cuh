@@ -36,6 +36,15 @@ constexpr unsigned kHalfPolls = 200000;           // bound of a wait, about 0.2 
 // change hands in a warp's box.  (Threads that went to memory by themselves, 16 bytes of their rows at a time, made 32 lookups of every
 // access: 480 us for 24 matrices of 1024 x 4096 where their product takes 150.)
 
+// Two numbers as the sum of two fp16 numbers each, 22 bits together.
+__device__ __forceinline__ void split_pair(float a, float b, unsigned& high, unsigned& low) {
+  high = pack2(__half(), a, b);
+  low = pack2(__half(), a - low_to_float(__half(), high), b - high_to_float(__half(), high));
+}
+__device__ __forceinline__ void store_shared2(unsigned at, unsigned v) {
+  asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((unsigned short)v) : "memory");
+}
+
 struct Box {
   unsigned at, full, lane;      // shared memory; two barriers; this thread
   bool fine = true;             // no wait has run out
@@ -53,24 +62,31 @@ struct Box {
       store_shared16(place16(offset, lane, q), pack2(T(), v[8 * q], v[8 * q + 1]), pack2(T(), v[8 * q + 2], v[8 * q + 3]), pack2(T(), v[8 * q + 4], v[8 * q + 5]),
                      pack2(T(), v[8 * q + 6], v[8 * q + 7]));
   }
-  // What is left of v beside its fp16 part, in fp16.
-  __device__ __forceinline__ void put_low(unsigned offset, const float* v) const {
+  // High and low part, the latter 2048 bytes behind.
+  __device__ __forceinline__ void put_parts(unsigned offset, const float* v) const {
 #pragma unroll
     for (unsigned q = 0; q < 4; ++q) {
-      float w[8];
+      unsigned h[4], l[4];
 #pragma unroll
-      for (unsigned i = 0; i < 8; ++i) w[i] = v[8 * q + i] - __half2float(__float2half_rn(v[8 * q + i]));
-      store_shared16(place16(offset, lane, q), pack2(__half(), w[0], w[1]), pack2(__half(), w[2], w[3]), pack2(__half(), w[4], w[5]), pack2(__half(), w[6], w[7]));
+      for (unsigned i = 0; i < 4; ++i) split_pair(v[8 * q + 2 * i], v[8 * q + 2 * i + 1], h[i], l[i]);
+      store_shared16(place16(offset, lane, q), h[0], h[1], h[2], h[3]);
+      store_shared16(place16(offset + 2048, lane, q), l[0], l[1], l[2], l[3]);
     }
   }
   // Transposed: this thread's row is a column of the box.
-  template <bool LOW>
+  template <bool PARTS>
   __device__ __forceinline__ void put_across(unsigned offset, const float* v) const {
 #pragma unroll
-    for (unsigned q = 0; q < 32; ++q) {
-      __half h = __float2half_rn(v[q]);
-      if (LOW) h = __float2half_rn(v[q] - __half2float(h));
-      asm volatile("st.shared.b16 [%0], %1;" ::"r"(place16(offset, q, lane >> 3) + (lane & 7u) * 2), "h"(__half_as_ushort(h)) : "memory");
+    for (unsigned q = 0; q < 32; q += 2) {
+      unsigned h, l;
+      split_pair(v[q], v[q + 1], h, l);
+      const unsigned at0 = place16(offset, q, lane >> 3) + (lane & 7u) * 2, at1 = place16(offset, q + 1, lane >> 3) + (lane & 7u) * 2;
+      store_shared2(at0, h);
+      store_shared2(at1, h >> 16);
+      if (PARTS) {
+        store_shared2(at0 + 2048, l);
+        store_shared2(at1 + 2048, l >> 16);
+      }
     }
   }
   __device__ __forceinline__ void get8(unsigned offset, unsigned piece, float (&v)[8]) const {

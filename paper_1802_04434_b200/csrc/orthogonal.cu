@@ -30,17 +30,16 @@ template <bool LOW>
 __device__ __forceinline__ void send_symmetric(const Box& box, unsigned offset, const Parts& to, unsigned row0, unsigned column, unsigned matrix, bool mirrored,
                                                const float* v) {
   box.sent();
-  box.put16<__half>(offset, v);
-  if (LOW) box.put_low(offset + 2048, v);
-  else if (mirrored) box.put_across<false>(offset + 2048, v);
+  if (LOW) box.put_parts(offset, v);
+  else box.put16<__half>(offset, v);
+  if (!LOW && mirrored) box.put_across<false>(offset + 2048, v);
   box.fence();
   box.send(to.high, offset, column, row0, matrix);
   if (LOW) box.send(to.low, offset + 2048, column, row0, matrix);
   if (!mirrored) return;
   if (LOW) {
     box.sent();
-    box.put_across<false>(offset, v);
-    box.put_across<true>(offset + 2048, v);
+    box.put_across<true>(offset, v);
     box.fence();
     box.send(to.low, offset + 2048, row0, column, matrix);
   }
@@ -233,8 +232,7 @@ struct UpdateEpilogue {
 #pragma unroll
         for (unsigned i = 0; i < 32; ++i) sum = fmaf(v[i], v[i], sum);
       }
-      box.template put16<__half>(from, v);
-      box.put_low(from + 2048, v);
+      box.put_parts(from, v);
       box.fence();
       box.send(a.next.high, from, column, row0, matrix);
       box.send(a.next.low, from + 2048, column, row0, matrix);
@@ -347,6 +345,16 @@ orthogonal_norm_kernel(const Source s, double* __restrict__ partial) {
   }
 }
 
+// scale / norm in two factors, a power of two that brings the norm to [1, 2) where that is an fp32 number, and the rest: the first
+// multiplication is exact, and neither leaves fp32's range.  A zero matrix stays zero, one that is not finite becomes NaN.
+struct Inverse { float first, rest; };
+__device__ __forceinline__ Inverse inverse_of(double norm, float scale) {
+  const bool finite = isfinite(norm);
+  const int e = norm > 0.0 && finite ? max(-126, min(126, -ilogb(norm))) : 0;
+  const float first = __uint_as_float((unsigned)(127 + e) << 23);
+  return {first, norm > 0.0 ? (finite ? (float)((double)scale / (norm * (double)first)) : __uint_as_float(0x7FC00000u)) : finite ? 0.0f : __uint_as_float(0x7FC00000u)};
+}
+
 template <int KIND, typename T>
 __global__ void __launch_bounds__(kNormThreads)
 orthogonal_split_kernel(const Source s, const double* __restrict__ partial, unsigned parts, const Whole x) {
@@ -361,12 +369,7 @@ orthogonal_split_kernel(const Source s, const double* __restrict__ partial, unsi
     if (threadIdx.x == 0) norm2 = sum;
   }
   __syncthreads();
-  // 1 / |U| in two factors, a power of two that brings |U| to [1, 2) where that is an fp32 number, and the rest: the first
-  // multiplication is exact, and neither leaves fp32's range.  A zero matrix stays zero, one that is not finite becomes NaN.
-  const double norm = sqrt(norm2);
-  const int e = norm > 0.0 && isfinite(norm) ? max(-126, min(126, -ilogb(norm))) : 0;
-  const float first = __uint_as_float((unsigned)(127 + e) << 23);
-  const float rest = norm > 0.0 ? (isfinite(norm) ? (float)((double)kScale / (norm * (double)first)) : __uint_as_float(0x7FC00000u)) : 0.0f;
+  const Inverse inverse = inverse_of(sqrt(norm2), kScale);
   const unsigned fours = (s.cols + 3) / 4, total = fours * s.rows;
   for (unsigned i = blockIdx.x * kNormThreads + threadIdx.x; i < total; i += gridDim.x * kNormThreads) {
     const unsigned row = i / fours, column = i % fours * 4;
@@ -375,13 +378,298 @@ orthogonal_split_kernel(const Source s, const double* __restrict__ partial, unsi
     float h[4], l[4];
 #pragma unroll
     for (unsigned k = 0; k < 4; ++k) {
-      const float v = u[k] * first * rest;
+      const float v = u[k] * inverse.first * inverse.rest;
       h[k] = __half2float(__float2half_rn(v));
       l[k] = v - h[k];
     }
     const size_t at = blockIdx.y * x.stride + (size_t)row * x.ld + column;
     *reinterpret_cast<uint2*>(x.high + at) = make_uint2(pack2(__half(), h[0], h[1]), pack2(__half(), h[2], h[3]));
     *reinterpret_cast<uint2*>(x.low + at) = make_uint2(pack2(__half(), l[0], l[1]), pack2(__half(), l[2], l[3]));
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Matrices of up to 128 x 128: a CTA does all of it, one launch instead of two and three a step (64 x 64, five steps: 80 -> 2x us).
+//
+// X and E = X X^T - d I stay in registers in fp32, a thread a row and 32 columns, which is how the tensor cores give their sums back; their
+// fp16 parts lie in shared memory as the tensor cores take operands, 64 columns to a block of 128 rows x 128 bytes.  The same
+// bytes serve as an operand with its k side by side and as one with its rows side by side: X X^T and M X, and for tall matrices X^T X
+// and X M, need no transpose.  M takes E's place.
+
+constexpr unsigned kSmallSide = 128, kSmallThreads = 512;
+constexpr unsigned kSmallPart = 32768;                                      // one 128 x 128 fp16 matrix
+constexpr unsigned kStageLd = kSmallSide + 1;                               // fp32 rows on their way in and out
+constexpr unsigned kSmallSmem = 4 * kSmallPart + kSmallSide * kStageLd * 4 + 1024;
+
+struct SmallArgs {
+  Source source;
+  int source_type, out_type, momentum;
+  void* out;                    // of out_type, or the parameters
+  size_t ldo, out_stride;
+  Polynomial f;
+  float delta;
+  unsigned steps, starve;
+  unsigned* status;
+};
+
+__device__ __forceinline__ float load_any(const void* p, int type, size_t at) {
+  switch (type) {
+    case SSGD_F32: return static_cast<const float*>(p)[at];
+    case SSGD_BF16: return to_float(static_cast<const __nv_bfloat16*>(p)[at]);
+    default: return to_float(static_cast<const __half*>(p)[at]);
+  }
+}
+__device__ __forceinline__ void store_any(void* p, int type, size_t at, float v) {
+  switch (type) {
+    case SSGD_F32: static_cast<float*>(p)[at] = v; break;
+    case SSGD_BF16: static_cast<__nv_bfloat16*>(p)[at] = from_float<__nv_bfloat16>(v); break;
+    default: static_cast<__half*>(p)[at] = from_float<__half>(v); break;
+  }
+}
+
+// A thread's 32 values of a row as the two parts of an operand; group: which 32 columns.
+__device__ __forceinline__ void put_operand(unsigned high, unsigned row, unsigned group, const float (&v)[32]) {
+  const unsigned block = high + group / 2 * (kSmallPart / 2) + row * 128;
+#pragma unroll
+  for (unsigned q = 0; q < 4; ++q) {
+    unsigned h[4], l[4];
+#pragma unroll
+    for (unsigned i = 0; i < 4; ++i) split_pair(v[8 * q + 2 * i], v[8 * q + 2 * i + 1], h[i], l[i]);
+    const unsigned at = block + ((((group & 1u) * 4 + q) ^ (row & 7u)) << 4);
+    store_shared16(at, h[0], h[1], h[2], h[3]);
+    store_shared16(at + kSmallPart, l[0], l[1], l[2], l[3]);
+  }
+}
+
+// D = P Q^T of operands in shared memory, k in pieces of 16; by one thread.  Unrolled, with descriptors that differ by constants: what the
+// thread computes between two of them is what the tensor cores wait for.
+template <bool P_BY_ROWS, bool Q_BY_ROWS>
+__device__ __forceinline__ void small_product(unsigned d, unsigned p, unsigned q, unsigned columns, unsigned k, unsigned done) {
+  const unsigned idesc = mma_half_descriptor(128, (columns + 15) / 16 * 16, false, P_BY_ROWS, Q_BY_ROWS);
+  const uint64_t pd = half_descriptor(p, P_BY_ROWS, kSmallPart / 2), qd = half_descriptor(q, Q_BY_ROWS, kSmallPart / 2);
+  constexpr unsigned low = kSmallPart >> 4;
+  // rows side by side: 16 of k are 16 rows; else 32 bytes, four of them a block
+  auto at = [](bool by_rows, unsigned c) { return by_rows ? c * (2048 >> 4) : c / 4 * (kSmallPart / 2 >> 4) + c % 4 * (32 >> 4); };
+#pragma unroll
+  for (unsigned c = 0; c < kSmallSide / 16; ++c) {
+    if (c == 0 || c * 16 < k) {
+      mma_half<false>(d, pd + at(P_BY_ROWS, c), qd + at(Q_BY_ROWS, c) + low, idesc, c > 0);
+      mma_half<false>(d, pd + at(P_BY_ROWS, c) + low, qd + at(Q_BY_ROWS, c), idesc, true);
+    }
+  }
+#pragma unroll
+  for (unsigned c = 0; c < kSmallSide / 16; ++c)
+    if (c == 0 || c * 16 < k) mma_half<false>(d, pd + at(P_BY_ROWS, c), qd + at(Q_BY_ROWS, c), idesc, true);
+  tcgen05_commit(done);
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 1)
+orthogonal_small_kernel(const SmallArgs a) {
+  extern __shared__ unsigned char small_smem[];
+  __shared__ __align__(8) uint64_t done_bar;
+  __shared__ unsigned tmem_base;
+  __shared__ double norms[kSmallThreads / 32];
+  __shared__ float squares[kSmallThreads / 32];
+  __shared__ Inverse inverse;
+  const unsigned pad = (1024u - (smem_u32(small_smem) & 1023u)) & 1023u;
+  const unsigned x_at = smem_u32(small_smem) + pad, e_at = x_at + 2 * kSmallPart;
+  float* stage = reinterpret_cast<float*>(small_smem + pad + 4 * kSmallPart);
+  const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, row = (warp & 3u) * 32 + lane, group = warp >> 2;
+  const unsigned rows = a.source.rows, cols = a.source.cols, side = min(rows, cols), matrix = blockIdx.x;
+  const unsigned done = smem_u32(&done_bar);
+  const bool tall = rows > cols;
+
+  if (threadIdx.x == 0) {
+    mbarrier_init(done, a.starve ? 2 : 1);
+    mbarrier_init_fence();
+  }
+  pdl_launch_dependents();
+  pdl_wait();                                   // before tensor memory is taken: its last holder has finished
+  if (warp == 1) tmem_alloc(smem_u32(&tmem_base), 128);
+  tcgen05_fence_before();
+
+  // U, a warp a row, lanes side by side, two rows in flight; a momentum is brought forward on the way.
+  const size_t u0 = matrix * a.source.u_stride, m0 = matrix * a.source.m_stride;
+  constexpr unsigned kWarps = kSmallThreads / 32;
+  for (unsigned r0 = warp; r0 < rows; r0 += 2 * kWarps) {
+    float u[8], m[8];
+#pragma unroll
+    for (unsigned k = 0; k < 8; ++k) {
+      const unsigned r = r0 + k / 4 * kWarps, c = lane + k % 4 * 32;
+      u[k] = m[k] = 0.0f;
+      if (r < rows && c < cols) {
+        u[k] = load_any(a.source.u, a.source_type, u0 + (size_t)r * a.source.ldu + c);
+        if (a.momentum) m[k] = a.source.m[m0 + (size_t)r * a.source.ldm + c];
+      }
+    }
+#pragma unroll
+    for (unsigned k = 0; k < 8; ++k) {
+      const unsigned r = r0 + k / 4 * kWarps, c = lane + k % 4 * 32;
+      if (r < rows && c < cols) {
+        if (a.momentum) {
+          const float g = __fmul_rn(1.0f - a.source.beta, u[k]), next = __fmaf_rn(a.source.beta, m[k], g);
+          a.source.m[m0 + (size_t)r * a.source.ldm + c] = next;
+          u[k] = a.source.ahead ? __fmaf_rn(a.source.beta, next, g) : next;
+        }
+        stage[r * kStageLd + c] = u[k];
+      }
+    }
+  }
+  __syncthreads();
+  tcgen05_fence_after();
+  const unsigned tmem = tmem_base, lanes = tmem + ((warp & 3u) << 21) + group * 32;
+
+  // Where a warp has something of X (of E, M): the others only keep step.  What lies beyond a matrix is zero, and stays so.
+  const unsigned row0 = (warp & 3u) * 32;
+  const bool has_x = row0 < rows && group * 32 < cols, has_e = row0 < side && group * 32 < side;
+  float x[32], e[32];                           // times 2^13, as their parts are stored
+  double sum = 0.0;
+#pragma unroll
+  for (unsigned q = 0; q < 32; ++q) x[q] = e[q] = 0.0f;
+  if (has_x) {
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) x[q] = row < rows && group * 32 + q < cols ? stage[row * kStageLd + group * 32 + q] : 0.0f;
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) sum = fma((double)x[q], (double)x[q], sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+  }
+  if (lane == 0) norms[warp] = sum;
+  __syncthreads();
+  if (warp == 0) {
+    sum = lane < kWarps ? norms[lane] : 0.0;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (lane == 0) inverse = inverse_of(sqrt(sum), kScale);
+  }
+  __syncthreads();
+  if (has_x) {
+    const Inverse by = inverse;
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) x[q] = x[q] * by.first * by.rest;
+  }
+  put_operand(x_at, row, group, x);
+  put_operand(e_at, row, group, e);
+  async_proxy_fence();
+  __syncthreads();
+
+  bool ok = true;
+  unsigned parity = 0;
+  float d = 1.0f / (float)side;
+  // The tensor cores' sums are there, for every thread or for none.  One warp asks; the others wait for it at the CTA's barrier.
+  auto wait = [&]() {
+    bool there = true;
+    if (warp == 0) {
+      there = false;
+      for (unsigned i = 0; i < 16 * kHalfPolls && !there; ++i) there = mbarrier_test(done, parity);
+    }
+    ok = __syncthreads_and(there) != 0;
+    parity ^= 1u;
+    tcgen05_fence_after();
+    return ok;
+  };
+  // Operands as the threads have written them are the tensor cores' to read, and the sums that the threads have read theirs to write.
+  auto publish = [&]() {
+    async_proxy_fence();
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+  };
+  // This warp's sums, times 2^13.  The product has had `columns`, rounded up to 16: behind them tensor memory holds anything.
+  auto sums = [&](unsigned columns, float (&v)[32]) {
+    unsigned u[32];
+    tmem_read32(lanes, u);
+    const bool second = group * 32 + 16 < columns;
+#pragma unroll
+    for (unsigned q = 0; q < 32; ++q) v[q] = q < 16 || second ? __uint_as_float(u[q]) * kUnscale : 0.0f;
+  };
+  for (unsigned k = 0; k < a.steps; ++k) {
+    if (warp == 0 && elect_one()) {
+      if (tall) small_product<true, true>(tmem, x_at, x_at, cols, rows, done);
+      else small_product<false, false>(tmem, x_at, x_at, rows, cols, done);
+    }
+    __syncwarp();
+    if (!wait()) break;
+    if (has_e) {
+      sums(side, e);
+      if (row0 == group * 32 && row < side) {
+#pragma unroll
+        for (unsigned q = 0; q < 32; ++q) e[q] = lane == q ? e[q] - d * kScale : e[q];
+      }
+      put_operand(e_at, row, group, e);
+    }
+    publish();
+    if (warp == 0 && elect_one()) small_product<false, false>(tmem, e_at, e_at, side, side, done);
+    __syncwarp();
+    if (!wait()) break;
+    const float p = a.f.b + 2.0f * a.f.c * d, own = a.f.a + d * (a.f.b + d * a.f.c);
+    if (has_e) {
+      float v[32];
+      sums(side, v);
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) e[q] = fmaf(a.f.c, v[q], p * e[q]);
+      put_operand(e_at, row, group, e);
+    }
+    publish();
+    if (warp == 0 && elect_one()) {
+      if (tall) small_product<false, false>(tmem, x_at, e_at, cols, cols, done);
+      else small_product<false, true>(tmem, e_at, x_at, cols, rows, done);
+    }
+    __syncwarp();
+    if (!wait()) break;
+    float square = 0.0f;
+    if (has_x) {
+      float v[32];
+      sums(cols, v);
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) {
+        x[q] = fmaf(own, x[q], v[q]);
+        square = fmaf(x[q], x[q], square);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) square += __shfl_xor_sync(0xFFFFFFFFu, square, o);
+    }
+    if (k + 1 == a.steps) break;
+    if (lane == 0) squares[warp] = square;
+    if (has_x) put_operand(x_at, row, group, x);
+    publish();
+    d = 0.0f;
+#pragma unroll
+    for (unsigned w = 0; w < kWarps; ++w) d += squares[w];
+    d *= kUnscale * kUnscale / (float)side;
+  }
+
+  if (ok) {
+    if (has_x) {
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) stage[row * kStageLd + group * 32 + q] = x[q] * kUnscale;
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    const size_t o0 = matrix * a.out_stride;
+    for (unsigned r0 = warp; r0 < rows; r0 += 2 * kWarps) {
+      float old[8];
+#pragma unroll
+      for (unsigned k = 0; k < 8; ++k) {
+        const unsigned r = r0 + k / 4 * kWarps, c = lane + k % 4 * 32;
+        old[k] = a.momentum && r < rows && c < cols ? static_cast<const float*>(a.out)[o0 + (size_t)r * a.ldo + c] : 0.0f;
+      }
+#pragma unroll
+      for (unsigned k = 0; k < 8; ++k) {
+        const unsigned r = r0 + k / 4 * kWarps, c = lane + k % 4 * 32;
+        if (r < rows && c < cols) {
+          const float v = stage[r * kStageLd + c];
+          store_any(a.out, a.out_type, o0 + (size_t)r * a.ldo + c, a.momentum ? fmaf(-a.delta, v, old[k]) : v);
+        }
+      }
+    }
+  } else {
+    if (threadIdx.x == 0) atomicOr(a.status, 1u);
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tcgen05_fence_after();
+    tmem_free(tmem, 128);
   }
 }
 
@@ -558,12 +846,21 @@ ssgd_status check_problem(size_t n, size_t rows, size_t cols, const float* coeff
   return SSGD_OK;
 }
 
+ssgd_status solve_small(const Problem& p, cudaStream_t s) {
+  static unsigned long long seen = 0;
+  if (!allow_smem(reinterpret_cast<const void*>(orthogonal_small_kernel), kSmallSmem, &seen)) return SSGD_ERR_CUDA;
+  const SmallArgs a = {p.source, p.source_type, p.out_type, p.momentum, p.out, p.ldo, p.out_stride, p.f, p.delta, p.steps, p.starve, p.status};
+  launch_kernel(orthogonal_small_kernel, dim3((unsigned)p.n), dim3(kSmallThreads), kSmallSmem, s, true, a);
+  return launch_status();
+}
+
 ssgd_status solve(Problem p, const float* coefficients, cudaStream_t s) {
+  p.f = {coefficients[0], coefficients[1], coefficients[2]};
+  if (p.rows <= kSmallSide && p.cols <= kSmallSide) return solve_small(p, s);
   DeviceInfo info;
   if (!device_info(&info)) return SSGD_ERR_CUDA;
   Layout l;
   if (!layout_of(p.n, p.rows, p.cols, &l)) return SSGD_ERR_SIZE;
-  p.f = {coefficients[0], coefficients[1], coefficients[2]};
   Buffers b;
   char* x = p.ws + l.x;
   const size_t whole = round_up(p.n * l.x_elements * 2, 128), square = round_up(p.n * l.e_elements * 2, 128);

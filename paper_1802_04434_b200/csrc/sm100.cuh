@@ -179,9 +179,9 @@ __host__ __device__ constexpr unsigned mma_half_descriptor(unsigned m, unsigned 
 }
 // Descriptor of a 16-bit operand in shared memory as tiled copies of 128-byte rows leave it (128-byte swizzle).  A row holds 64
 // of k (groups of eight rows 1024 bytes apart); or, the operand lying by rows, 64 of its rows for one k: eight k 1024 bytes
-// apart, the next 64 rows 8192.
-__device__ __forceinline__ uint64_t half_descriptor(unsigned addr, bool by_rows) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(by_rows ? 8192 >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+// apart, the next 64 rows `next_rows` bytes.
+__device__ __forceinline__ uint64_t half_descriptor(unsigned addr, bool by_rows, unsigned next_rows = 8192) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(by_rows ? next_rows >> 4 : 1) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 // Box of a three-dimensional tensor to shared memory; x is a multiple of 16 bytes.
 __device__ __forceinline__ void tma_load_3d(unsigned dst, const CUtensorMap* map, int x, int y, int z, unsigned bar) {
