@@ -43,6 +43,7 @@ struct StatsEpilogue {
   int64_t target;
   unsigned row, part;
   __device__ __forceinline__ StatsEpilogue(const Args&, const Box& b) : box(b) {}
+  static __device__ __forceinline__ void prefetch(const Args&) {}
   __device__ __forceinline__ void ahead(const Args&, unsigned) {}
   __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned row0, unsigned odd) {
     row = row0 + box.lane;
@@ -93,7 +94,13 @@ struct StatsEpilogue {
 // What the backward pass has to know of a token.
 constexpr uint8_t kCounts = 0, kIgnored = 1, kIgnoredNotFinite = 2;
 
-// Joins the parts of TOKENS tokens a CTA, its other threads side by side along the parts; then the losses, and a look at the
+// Two parts of a sum of exponentials, each beside its maximum.
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  const float m = fmaxf(a.x, b.x), base = base_of(m);
+  return make_float2(m, a.y * exp2_fast((a.x - base) * kLog2e) + b.y * exp2_fast((b.x - base) * kLog2e));
+}
+
+// Joins the parts of TOKENS tokens a CTA (1 or 32), its other threads side by side along the parts; then the losses, and a look at the
 // ignored tokens' rows of h: one that is not finite must not reach dw through 0 * inf.
 template <unsigned TOKENS, typename T>
 __global__ void __launch_bounds__(256)
@@ -101,38 +108,44 @@ xent_join_kernel(const float2* __restrict__ partial, const float* __restrict__ p
                  unsigned parts, unsigned vocab, const T* __restrict__ h, size_t ldh, unsigned width, float* __restrict__ losses, float* __restrict__ lse,
                  uint8_t* __restrict__ kinds) {
   constexpr unsigned kSlices = 256 / TOKENS;
-  __shared__ float2 part[kSlices][TOKENS];
+  __shared__ float2 part[8][TOKENS];
   pdl_launch_dependents();
   pdl_wait();
   const unsigned i = threadIdx.x % TOKENS, slice = threadIdx.x / TOKENS, t0 = blockIdx.x * TOKENS, t = t0 + i;
-  float top = -kInf, sum = 0.0f;
+  const bool mine = threadIdx.x < TOKENS && t < tokens;
+  const int64_t y = mine ? targets[t] : 0;
+  float2 sum = make_float2(-kInf, 0.0f);
   if (t < tokens) {
     for (unsigned p0 = slice; p0 < parts; p0 += 8 * kSlices) {
       float2 v[8];
 #pragma unroll
       for (unsigned u = 0; u < 8; ++u) v[u] = p0 + u * kSlices < parts ? partial[(size_t)(p0 + u * kSlices) * tokens + t] : make_float2(-kInf, 0.0f);
-      float m = top;
+      float m = sum.x;
 #pragma unroll
       for (unsigned u = 0; u < 8; ++u) m = fmaxf(m, v[u].x);
       const float b = base_of(m);
-      sum *= exp2_fast((top - b) * kLog2e);
+      sum.y *= exp2_fast((sum.x - b) * kLog2e);
 #pragma unroll
-      for (unsigned u = 0; u < 8; ++u) sum += v[u].y * exp2_fast((v[u].x - b) * kLog2e);
-      top = m;
+      for (unsigned u = 0; u < 8; ++u) sum.y += v[u].y * exp2_fast((v[u].x - b) * kLog2e);
+      sum.x = m;
     }
   }
-  part[slice][i] = make_float2(top, sum);
+  if (TOKENS == 1) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum = join(sum, make_float2(__shfl_xor_sync(0xFFFFFFFFu, sum.x, o), __shfl_xor_sync(0xFFFFFFFFu, sum.y, o)));
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32][0] = sum;
+  } else {
+    part[slice][i] = sum;
+  }
   __syncthreads();
-  if (threadIdx.x < TOKENS && t < tokens) {
-    float m = -kInf, s = 0.0f;
-    for (unsigned k = 0; k < kSlices; ++k) m = fmaxf(m, part[k][i].x);
-    const float b = base_of(m);
-    for (unsigned k = 0; k < kSlices; ++k) s += part[k][i].y * exp2_fast((part[k][i].x - b) * kLog2e);
-    const int64_t y = targets[t];
+  if (mine) {
+    sum = part[0][i];
+#pragma unroll
+    for (unsigned k = 1; k < 8; ++k) sum = join(sum, part[k][i]);
     const bool ignored = y == ignore, inside = y >= 0 && y < (int64_t)vocab;
     // a target that is neither ignored nor in the vocabulary: NaN, here and in the gradients
-    const float l = inside || ignored ? m + logf(s) : __uint_as_float(0x7FC00000u);
-    losses[t] = ignored ? 0.0f : inside ? (m - picked[t]) + logf(s) : l;
+    const float log_sum = logf(sum.y), l = inside || ignored ? sum.x + log_sum : __uint_as_float(0x7FC00000u);
+    losses[t] = ignored ? 0.0f : inside ? (sum.x - picked[t]) + log_sum : l;
     lse[t] = l;
     if (!ignored) kinds[t] = kCounts;
   }
@@ -141,6 +154,7 @@ xent_join_kernel(const float2* __restrict__ partial, const float* __restrict__ p
     const unsigned row = t0 + k;
     if (row >= tokens || targets[row] != ignore) continue;
     bool finite = true;
+#pragma unroll 8
     for (unsigned c = threadIdx.x % 32; c < width; c += 32) finite &= isfinite(to_float(h[(size_t)row * ldh + c])) != 0;
     finite = __all_sync(0xFFFFFFFFu, finite);
     if (threadIdx.x % 32 == 0) kinds[row] = finite ? kIgnored : kIgnoredNotFinite;
@@ -214,6 +228,7 @@ struct GradEpilogue {
   unsigned row0, half;
   bool counts;
   __device__ __forceinline__ GradEpilogue(const Args&, const Box& b) : box(b), half(0) {}
+  static __device__ __forceinline__ void prefetch(const Args& a) { prefetch_tensor_map(&a.dz); }
   __device__ __forceinline__ void ahead(const Args&, unsigned) {}
   __device__ __forceinline__ void begin(const Args& a, const HalfPlace&, unsigned first_row, unsigned) {
     row0 = first_row;
@@ -268,6 +283,7 @@ struct TokensEpilogue {
   unsigned row0, split;
   bool counts;
   __device__ __forceinline__ TokensEpilogue(const Args& a, const Box& b) : box(b) { unscale = a.prepared->unscale; }
+  static __device__ __forceinline__ void prefetch(const Args&) {}
   __device__ __forceinline__ void ahead(const Args&, unsigned) {}
   __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
     row0 = first_row;
@@ -328,6 +344,7 @@ struct WeightEpilogue {
   float unscale;
   unsigned row0;
   __device__ __forceinline__ WeightEpilogue(const Args& a, const Box& b) : box(b) { unscale = a.prepared->unscale; }
+  static __device__ __forceinline__ void prefetch(const Args&) {}
   __device__ __forceinline__ void ahead(const Args&, unsigned) {}
   __device__ __forceinline__ void begin(const Args&, const HalfPlace&, unsigned first_row, unsigned) { row0 = first_row; }
   __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
@@ -404,11 +421,11 @@ ssgd_status head_forward(const T* h, size_t ldh, const T* w, size_t ldw, size_t 
   float* picked = static_cast<float*>(ws);
   float2* partial = reinterpret_cast<float2*>(static_cast<char*>(ws) + up(tokens * 4, 16));
   const StatsEpilogue::Args args = {targets, partial, picked, (unsigned)tokens};
-  const ssgd_status st = launch_half<StatsEpilogue, 1, 4>(p, args, form, 1, sms, s);
+  const ssgd_status st = launch_half<StatsEpilogue, 1, 4, kBothByK>(p, args, form, 1, sms, s);
   if (st != SSGD_OK) return st;
   const unsigned parts = 2 * (unsigned)((vocab + form.nt - 1) / form.nt);
-  if (tokens <= 256)
-    launch_kernel(xent_join_kernel<4, T>, dim3((unsigned)(tokens + 3) / 4), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
+  if (tokens <= 512)
+    launch_kernel(xent_join_kernel<1, T>, dim3((unsigned)tokens), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
                   (unsigned)vocab, h, ldh, (unsigned)width, losses, lse, kinds);
   else
     launch_kernel(xent_join_kernel<32, T>, dim3((unsigned)(tokens + 31) / 32), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
@@ -436,7 +453,7 @@ struct HeadBackward {
 template <typename O>
 ssgd_status weight_product(const HalfProduct& p, const HeadBackward& b, const Prepared* prepared, size_t first, size_t rows, int sms, cudaStream_t s) {
   const typename WeightEpilogue<O>::Args args = {prepared, static_cast<O*>(b.dw) + first * b.lddw, b.lddw, (unsigned)rows};
-  return launch_half<WeightEpilogue<O>, 1, 0>(p, args, half_form(p, 1, 1, sms), 1, sms, s);
+  return launch_half<WeightEpilogue<O>, 1, 0, kBothByRows>(p, args, half_form(p, 1, 1, sms), 1, sms, s);
 }
 
 template <typename T>
@@ -465,7 +482,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
     p.P = b.T; p.Q = columns; p.K = b.D;
     typename GradEpilogue<T>::Args grad = {{}, b.targets, b.lse, b.g, b.kinds, prepared, b.g_stride, tokens, (unsigned)first};
     if (!box_map(&grad.dz, dz, kBf16, b.T, columns, z.dz_ld, 1, 0)) return SSGD_ERR_CUDA;
-    st = launch_half<GradEpilogue<T>, 1, 0>(p, grad, half_form(p, 1, 1, sms), 1, sms, s);
+    st = launch_half<GradEpilogue<T>, 1, 0, kBothByK>(p, grad, half_form(p, 1, 1, sms), 1, sms, s);
     if (st != SSGD_OK) break;
     if (b.dh) {
       p.p = {dz, nullptr, z.dz_ld, 0, false};
@@ -473,7 +490,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
       p.P = b.T; p.Q = b.D; p.K = columns;
       T* out = last && z.splits == 1 ? static_cast<T*>(b.dh) : nullptr;
       const typename TokensEpilogue<T>::Args args = {b.kinds, prepared, z.pieces > 1 || z.splits > 1 ? sums : nullptr, out, b.lddh, tokens, width, first > 0};
-      st = launch_half<TokensEpilogue<T>, 1, 0>(p, args, half_form(p, 1, z.splits, sms), z.splits, sms, s);
+      st = launch_half<TokensEpilogue<T>, 1, 0, kQByRows>(p, args, half_form(p, 1, z.splits, sms), z.splits, sms, s);
       if (st == SSGD_OK && z.splits > 1) {
         const size_t plane = b.T * b.D;
         launch_kernel(xent_planes_kernel<T>, dim3(grid_for((plane + 255) / 256)), dim3(256), 0, s, true, sums, z.splits, plane, prepared, width,

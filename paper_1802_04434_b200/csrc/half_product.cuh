@@ -194,7 +194,6 @@ struct HalfPlan {
   unsigned k_stages, k_chunks;                    // k in pieces of 64 and of 16
   unsigned tiles_p, tiles_q, per_matrix, tiles;   // tiles: per matrix, and of all matrices and splits
   unsigned splits;                                // pieces of k that are summed apart
-  unsigned p_by_rows, q_by_rows;                  // the operand lies with its rows side by side
   unsigned p_box;                                 // rows of P that a CTA loads: fewer than 128 where P has fewer
   unsigned idesc;
   unsigned symmetric;                             // only tiles that reach the diagonal or lie above it
@@ -205,7 +204,7 @@ struct HalfPlan {
 
 struct HalfPlace { unsigned matrix, split, p0, q0, tile, tile_q, rows; };      // rows: of P in a tile
 
-template <bool PAIR, int NT, int TERMS, unsigned BOX>
+template <bool PAIR, int NT, int TERMS, int CHUNK, unsigned BOX>
 struct HalfShape {
   static constexpr unsigned rows = PAIR ? 256 : 128;                       // of P in a tile
   static constexpr unsigned q_rows = PAIR ? NT / 2 : NT;                   // of Q that a CTA loads
@@ -213,14 +212,16 @@ struct HalfShape {
   static constexpr unsigned p_bytes = 128 * 128, q_bytes = q_rows * 128;
   static constexpr unsigned stage_bytes = parts * (p_bytes + q_bytes);
   static constexpr unsigned box_bytes = BOX, out_bytes = 8 * box_bytes;    // the eight warps' room on the way out
-  static constexpr unsigned bar_bytes = 384;
+  static constexpr unsigned bar_bytes = 512;
   static constexpr unsigned room = 232448 - out_bytes - bar_bytes;
   static constexpr unsigned stages = room / stage_bytes < 8 ? room / stage_bytes : 8;
-  static constexpr unsigned columns = 2 * NT;                              // two accumulators
+  // Accumulators.  Sums that are taken every few stages need several on their way between the tensor cores and the threads: a
+  // round takes about 1000 clocks, a stage of 64 columns 128 (TERMS = 1)
+  static constexpr unsigned accs = CHUNK > 0 ? 512 / NT : 2, columns = accs * NT;
   // more than half of an SM's shared memory always: CTAs that hold and wait for tensor memory on one SM would never end
   static constexpr unsigned needed = stages * stage_bytes + out_bytes + bar_bytes;
   static constexpr unsigned smem = needed < 118784 ? 118784 : needed;
-  static_assert(stages >= 3 && (2 * stages + 5 + 16) * 8 + 8 <= bar_bytes && columns <= 512 && q_rows % 64 == 0, "shape");
+  static_assert(stages >= 3 && (2 * stages + 1 + 16 + 2 * accs) * 8 + 8 <= bar_bytes && columns <= 512 && q_rows % 64 == 0, "shape");
 };
 
 // Tiles go through bands of eight of P's tiles, so that those in flight share rows of both operands.
@@ -229,7 +230,7 @@ __device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p
   constexpr unsigned rows = PAIR ? 256 : 128, kBand = 8;
   const unsigned z = tile / p.per_matrix, in_matrix = tile - z * p.per_matrix;
   HalfPlace at;
-  at.matrix = z / p.splits;
+  at.matrix = p.splits > 1 ? z / p.splits : z;
   at.split = z - at.matrix * p.splits;
   at.tile = in_matrix;
   if (p.symmetric) {
@@ -249,6 +250,7 @@ __device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p
 
 // What an epilogue offers, besides its Args:
 //   kBox                            bytes of shared memory of a warp
+//   prefetch(args)                  of its tensor maps, by one thread
 //   begin(args, place, row0, odd)   before a tile's first columns; a thread's row is row0 + lane, odd: which half of the columns
 //   ahead(args, column)             before the sums of those columns are there: what it needs of memory may be asked for
 //   unit(args, column, left, v)     32 sums of columns column .., `left` of them inside; it may change them
@@ -258,27 +260,72 @@ __device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p
 constexpr unsigned kShiftRegisters = 168;
 __host__ __device__ constexpr bool half_shifts(int nt, int chunk) { return nt == 256 && chunk > 0; }
 
-template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK>
+// How the operands lie in memory: which of them with their rows side by side.
+enum HalfLayout { kBothByK = 0, kQByRows = 1, kBothByRows = 3 };
+
+// One stage's MMAs.  Their descriptors differ by constants: with offsets that were only known at run time the issuing thread took 90
+// clocks an MMA, and one of 128 x 64 x 16 takes 32 to 48.
+template <bool PAIR, int TERMS, int LAYOUT, unsigned LOW>
+__device__ __forceinline__ void half_issue(unsigned d, uint64_t pd, uint64_t qd, unsigned idesc, unsigned chunks, bool add) {
+  constexpr unsigned ps = LAYOUT & 2 ? 2048 >> 4 : 32 >> 4, qs = LAYOUT & 1 ? 2048 >> 4 : 32 >> 4;      // 16 of k
+  if (chunks >= 4) {
+    if constexpr (TERMS == 3) {
+#pragma unroll
+      for (unsigned c = 0; c < 4; ++c) {
+        mma_half<PAIR>(d, pd + c * ps, qd + c * qs + LOW, idesc, c > 0 || add);
+        mma_half<PAIR>(d, pd + c * ps + LOW, qd + c * qs, idesc, true);
+      }
+    }
+#pragma unroll
+    for (unsigned c = 0; c < 4; ++c) mma_half<PAIR>(d, pd + c * ps, qd + c * qs, idesc, TERMS == 3 || c > 0 || add);
+  } else {
+    if constexpr (TERMS == 3) {
+#pragma unroll 1
+      for (unsigned c = 0; c < chunks; ++c) {
+        mma_half<PAIR>(d, pd + c * ps, qd + c * qs + LOW, idesc, c > 0 || add);
+        mma_half<PAIR>(d, pd + c * ps + LOW, qd + c * qs, idesc, true);
+      }
+    }
+#pragma unroll 1
+    for (unsigned c = 0; c < chunks; ++c) mma_half<PAIR>(d, pd + c * ps, qd + c * qs, idesc, TERMS == 3 || c > 0 || add);
+  }
+}
+
+// The stages of a split of k.
+__device__ __forceinline__ void half_range(const HalfPlan& p, unsigned split, unsigned& first, unsigned& last) {
+  first = 0;
+  last = p.k_stages;
+  if (p.splits > 1) {                           // a 64-bit division takes a third of a microsecond
+    first = (unsigned)((uint64_t)p.k_stages * split / p.splits);
+    last = (unsigned)((uint64_t)p.k_stages * (split + 1) / p.splits);
+  }
+}
+
+template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK, int LAYOUT>
 __global__ void __launch_bounds__(kHalfThreads, 1)
 half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, const __grid_constant__ typename Epilogue::Args args) {
-  using S = HalfShape<PAIR, NT, TERMS, Epilogue::kBox>;
+  using S = HalfShape<PAIR, NT, TERMS, CHUNK, Epilogue::kBox>;
   extern __shared__ __align__(1024) unsigned char half_smem[];           // stages, boxes, barriers; the same place in both CTAs
   uint64_t* bars = reinterpret_cast<uint64_t*>(half_smem + S::stages * S::stage_bytes + S::out_bytes);
-  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 5 + 16), &failed = *(&tmem_base + 1);
+  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 1 + 16 + 2 * S::accs), &failed = *(&tmem_base + 1);
   const unsigned rank = PAIR ? cluster_rank() : 0;
   const unsigned stage0 = smem_u32(half_smem);
-  const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 16, ended = acc_free + 16, box_full = ended + 8;
+  const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 8 * S::accs, ended = acc_free + 8 * S::accs, box_full = ended + 8;
   const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   const unsigned worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
 
   if (threadIdx.x == 0) {
+    // the first use of a map that is not at hand costs over a microsecond (200 x 200: a product 6.2 -> 5 us)
     prefetch_tensor_map(&maps.p[0]);
     prefetch_tensor_map(&maps.q[0]);
+    if (TERMS == 3) prefetch_tensor_map(&maps.p[1]);
+    if (TERMS == 3 || p.q_choice) prefetch_tensor_map(&maps.q[1]);
+    Epilogue::prefetch(args);
     for (unsigned s = 0; s < S::stages; ++s) {
       mbarrier_init(full + 8 * s, 1);
       mbarrier_init(empty + 8 * s, 1);
     }
-    for (unsigned b = 0; b < 2; ++b) {
+    for (unsigned b = 0; b < S::accs; ++b) {
       mbarrier_init(acc_full + 8 * b, 1);
       mbarrier_init(acc_free + 8 * b, PAIR ? 16 : 8);     // one arrival from each of the CTAs' eight epilogue warps
     }
@@ -310,12 +357,14 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
   if (warp == 0) {
     if (elect_one()) {
       const CUtensorMap* q_high = p.q_choice && *p.q_choice ? &maps.q[1] : &maps.q[0];
-      const unsigned p_loaded = p.p_by_rows ? S::p_bytes : p.p_box * 128;
+      constexpr bool kPRows = (LAYOUT & 2) != 0, kQRows = (LAYOUT & 1) != 0;
+      const unsigned p_loaded = kPRows ? S::p_bytes : p.p_box * 128;
       const unsigned expected = (PAIR ? 2 : 1) * S::parts * (p_loaded + S::q_bytes) + p.starve;
       for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
         const HalfPlace at = half_place<PAIR, NT>(tile, p);
         const int p0 = (int)(at.p0 + rank * 128), q0 = (int)(at.q0 + rank * S::q_rows), z = (int)at.matrix;
-        const unsigned first = (unsigned)((uint64_t)p.k_stages * at.split / p.splits), last = (unsigned)((uint64_t)p.k_stages * (at.split + 1) / p.splits);
+        unsigned first, last;
+        half_range(p, at.split, first, last);
         for (unsigned k = first; k < last; ++k, ++n) {
           const unsigned s = n % S::stages;
           if (n >= S::stages) ok = mbarrier_wait(empty + 8 * s, (n / S::stages - 1) & 1u, kHalfPolls);
@@ -332,13 +381,13 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
           for (unsigned h = 0; h < S::parts; ++h) {
             const unsigned pd = base + h * (S::p_bytes + S::q_bytes), qd = pd + S::p_bytes;
             const CUtensorMap* qm = h == 0 ? q_high : &maps.q[1];
-            if (p.p_by_rows) {
+            if (kPRows) {
 #pragma unroll
               for (unsigned j = 0; j < 2; ++j) load(pd + j * 8192, &maps.p[h], p0 + (int)(64 * j), k0);
             } else {
               load(pd, &maps.p[h], k0, p0);
             }
-            if (p.q_by_rows) {
+            if (kQRows) {
 #pragma unroll
               for (unsigned j = 0; j < S::q_rows / 64; ++j) load(qd + j * 8192, qm, q0 + (int)(64 * j), k0);
             } else {
@@ -353,22 +402,22 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
     }
   } else if (warp == 1) {
     if (rank == 0 && elect_one()) {
-      const uint64_t p_desc = half_descriptor(stage0, p.p_by_rows), q_desc = half_descriptor(stage0 + S::p_bytes, p.q_by_rows);
-      const unsigned p_step = p.p_by_rows ? 2048 >> 4 : 32 >> 4, q_step = p.q_by_rows ? 2048 >> 4 : 32 >> 4;    // 16 of k
+      const uint64_t p_desc = half_descriptor(stage0, (LAYOUT & 2) != 0), q_desc = half_descriptor(stage0 + S::p_bytes, (LAYOUT & 1) != 0);
       constexpr unsigned low = (S::p_bytes + S::q_bytes) >> 4;
       unsigned s = 0, parity = 0;
       bool ready = false;                       // the next stage's operands are known to be there
       unsigned t = 0;                           // sums taken so far: of tiles, or of their chunks
       for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
-        const unsigned split = tile / p.per_matrix % p.splits;
-        const unsigned first = (unsigned)((uint64_t)p.k_stages * split / p.splits), last = (unsigned)((uint64_t)p.k_stages * (split + 1) / p.splits);
+        unsigned first, last;
+        half_range(p, p.splits > 1 ? tile / p.per_matrix % p.splits : 0, first, last);
         for (unsigned from = first; from < last && ok; ++t) {
           const unsigned to = CHUNK > 0 ? min(last, from + CHUNK) : last;
-          if (t > 1) ok = PAIR ? mbarrier_wait_cluster(acc_free + 8 * (t & 1u), (t / 2 - 1) & 1u, kHalfPolls)
-                               : mbarrier_wait(acc_free + 8 * (t & 1u), (t / 2 - 1) & 1u, kHalfPolls);
+          const unsigned acc = t % S::accs;
+          if (t >= S::accs) ok = PAIR ? mbarrier_wait_cluster(acc_free + 8 * acc, (t / S::accs - 1) & 1u, kHalfPolls)
+                                      : mbarrier_wait(acc_free + 8 * acc, (t / S::accs - 1) & 1u, kHalfPolls);
           if (!ok) break;
           tcgen05_fence_after();
-          const unsigned d = tmem + (t & 1u) * NT;
+          const unsigned d = tmem + acc * NT;
           for (unsigned k = from; k < to; ++k, ++n) {
             ok = ready || mbarrier_wait(full + 8 * s, parity, kHalfPolls);
             if (!ok) break;
@@ -376,27 +425,15 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
             const unsigned next = s + 1 == S::stages ? 0 : s + 1, next_parity = parity ^ (next == 0);
             ready = mbarrier_test(full + 8 * next, next_parity);    // its answer comes while this stage is issued
             const uint64_t pd = p_desc + s * (S::stage_bytes >> 4), qd = q_desc + s * (S::stage_bytes >> 4);
-            const unsigned chunks = p.k_chunks - k * 4;
-            if constexpr (TERMS == 3) {
-#pragma unroll
-              for (unsigned c = 0; c < 4; ++c) {
-                if (c == 0 || c < chunks) {
-                  mma_half<PAIR>(d, pd + c * p_step, qd + c * q_step + low, p.idesc, k > from || c > 0);
-                  mma_half<PAIR>(d, pd + c * p_step + low, qd + c * q_step, p.idesc, true);
-                }
-              }
-            }
-#pragma unroll
-            for (unsigned c = 0; c < 4; ++c)
-              if (c == 0 || c < chunks) mma_half<PAIR>(d, pd + c * p_step, qd + c * q_step, p.idesc, TERMS == 3 || k > from || c > 0);
+            half_issue<PAIR, TERMS, LAYOUT, low>(d, pd, qd, p.idesc, p.k_chunks - k * 4, k > from);
             if (PAIR) tcgen05_commit_pair(empty + 8 * s);
             else tcgen05_commit(empty + 8 * s);
             s = next;
             parity = next_parity;
           }
           if (ok) {
-            if (PAIR) tcgen05_commit_pair(acc_full + 8 * (t & 1u));
-            else tcgen05_commit(acc_full + 8 * (t & 1u));
+            if (PAIR) tcgen05_commit_pair(acc_full + 8 * acc);
+            else tcgen05_commit(acc_full + 8 * acc);
           }
           from = to;
         }
@@ -421,13 +458,14 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       epilogue.begin(args, at, row0, odd);
       if (row0 < p.P && at.q0 + odd * 32 < p.Q) epilogue.ahead(args, at.q0 + odd * 32);
       if constexpr (CHUNK > 0) {
-        const unsigned first = (unsigned)((uint64_t)p.k_stages * at.split / p.splits), last = (unsigned)((uint64_t)p.k_stages * (at.split + 1) / p.splits);
+        unsigned first, last;
+        half_range(p, at.split, first, last);
         float sum[kUnits][32];
         for (unsigned from = first; from < last; from += CHUNK, ++t) {
-          ok = mbarrier_wait(acc_full + 8 * (t & 1u), (t / 2) & 1u, 4 * kHalfPolls);
+          ok = mbarrier_wait(acc_full + 8 * (t % S::accs), (t / S::accs) & 1u, 4 * kHalfPolls);
           if (!ok) break;
           tcgen05_fence_after();
-          const unsigned lanes = tmem + (t & 1u) * NT + (quarter << 21);
+          const unsigned lanes = tmem + t % S::accs * NT + (quarter << 21);
 #pragma unroll
           for (unsigned j = 0; j < kUnits; ++j) {
             unsigned v[32];
@@ -435,7 +473,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
             if (j + 1 == kUnits) {
               tcgen05_fence_before();
               __syncwarp();
-              if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t & 1u));
+              if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t % S::accs));
             }
 #pragma unroll
             for (unsigned q = 0; q < 32; ++q) sum[j][q] = from == first ? __uint_as_float(v[q]) : sum[j][q] + __uint_as_float(v[q]);
@@ -450,10 +488,10 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
           __syncwarp();
         }
       } else {
-        ok = mbarrier_wait(acc_full + 8 * (t & 1u), (t / 2) & 1u, 4 * kHalfPolls + 64 * p.k_stages);
+        ok = mbarrier_wait(acc_full + 8 * (t % S::accs), (t / S::accs) & 1u, 4 * kHalfPolls + 64 * p.k_stages);
         if (!ok) break;
         tcgen05_fence_after();
-        const unsigned lanes = tmem + (t & 1u) * NT + (quarter << 21);
+        const unsigned lanes = tmem + t % S::accs * NT + (quarter << 21);
 #pragma unroll 1
         for (unsigned j = 0; j < kUnits; ++j) {
           unsigned v[32];
@@ -461,7 +499,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
           if (j + 1 == kUnits) {                // this warp's last columns
             tcgen05_fence_before();
             __syncwarp();
-            if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t & 1u));
+            if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t % S::accs));
           }
           float f[32];
 #pragma unroll
@@ -541,7 +579,10 @@ inline bool box_map(CUtensorMap* map, const void* base, bool bf16, size_t rows, 
            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Clocks of a product by tiles of a form: rounds of tiles, each its stages, beside a start.
+// Clocks of a product by tiles of a form: rounds of tiles, each its stages, beside a start.  What a stage takes is the tensor cores'
+// time (512 clocks for 256 x 256, 64 of k and one term) or shared memory's, 128 bytes a clock, for what the copies write and the
+// tensor cores read: 32 + 32, 24 + 24 and 24 + 24 KB for tiles of 256, 128 and 64 columns and one term, 64 + 96, 48 + 72 and 48 + 72 for
+// three (measured: 1000 clocks for the last).
 struct HalfForm { bool pairs; unsigned nt; };
 inline unsigned long long half_tiles(const HalfProduct& h, unsigned rows, unsigned nt) {
   const unsigned long long tp = (h.P + rows - 1) / rows, tq = (h.Q + nt - 1) / nt;
@@ -554,15 +595,15 @@ inline HalfForm half_form(const HalfProduct& h, int terms, unsigned splits, int 
   const unsigned long long stages = (h.K + 63) / 64 / splits + 1, batch = h.batch * splits, pairs = (unsigned)sms / 2;
   const unsigned long long r256 = (half_tiles(h, 256, 256) * batch + pairs - 1) / pairs, r128 = (half_tiles(h, 256, 128) * batch + pairs - 1) / pairs,
                            r64 = (half_tiles(h, 128, 64) * batch + sms - 1) / (unsigned)sms;
-  const unsigned long long c256 = r256 * (stages * 530 * terms + 1500) + 2500, c128 = r128 * (stages * 290 * terms + 1200) + 1800,
-                           c64 = r64 * (stages * 170 * terms + 1000) + 1200;
+  const unsigned s256 = terms == 3 ? 1560 : 530, s128 = terms == 3 ? 980 : 400, s64 = terms == 3 ? 1000 : 390;
+  const unsigned long long c256 = r256 * (stages * s256 + 1500) + 6500, c128 = r128 * (stages * s128 + 1200) + 5500, c64 = r64 * (stages * s64 + 1000) + 5000;
   if (c256 <= c128 && c256 <= c64) return {true, 256};
   return c128 <= c64 ? HalfForm{true, 128} : HalfForm{false, 64};
 }
 
-template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK>
+template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK, int LAYOUT>
 ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args& args, unsigned splits, int sms, cudaStream_t s) {
-  using S = HalfShape<PAIR, NT, TERMS, Epilogue::kBox>;
+  using S = HalfShape<PAIR, NT, TERMS, CHUNK, Epilogue::kBox>;
   HalfPlan p = {};
   const unsigned long long per = half_tiles(h, S::rows, NT), tiles = per * h.batch * splits;
   if (h.P >= (1ull << 31) || h.Q >= (1ull << 31) || h.K >= (1ull << 31) || tiles >= (1ull << 30)) return SSGD_ERR_SIZE;
@@ -571,7 +612,6 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
   p.tiles_p = (unsigned)((h.P + S::rows - 1) / S::rows); p.tiles_q = (unsigned)((h.Q + NT - 1) / NT);
   p.per_matrix = (unsigned)per; p.tiles = (unsigned)tiles;
   p.splits = splits;
-  p.p_by_rows = h.p.by_rows; p.q_by_rows = h.q.by_rows;
   p.p_box = h.P < 128 ? (unsigned)(h.P + 7) / 8 * 8 : 128;
   p.idesc = mma_half_descriptor(S::rows, NT, h.bf16, h.p.by_rows, h.q.by_rows);
   p.symmetric = h.symmetric;
@@ -585,7 +625,7 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
       !half_map(&maps.p[1], TERMS == 3 ? h.p.low : h.p.high, h.bf16, h.p, h.P, h.K, h.batch, p.p_box) ||
       !half_map(&maps.q[1], TERMS == 3 ? q1.low : q1.high, h.bf16, q1, h.Q, h.K, h.batch, S::q_rows))
     return SSGD_ERR_CUDA;
-  auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS, CHUNK>;
+  auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS, CHUNK, LAYOUT>;
   static unsigned long long seen = 0;
   if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
   if constexpr (half_shifts(NT, CHUNK)) {         // registers as the kernel's own shares add up to
@@ -615,11 +655,12 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
   return launch_status();
 }
 
-template <class Epilogue, int TERMS, int CHUNK>
+// LAYOUT says what h.p.by_rows and h.q.by_rows say.
+template <class Epilogue, int TERMS, int CHUNK, int LAYOUT>
 ssgd_status launch_half(const HalfProduct& h, const typename Epilogue::Args& args, const HalfForm& form, unsigned splits, int sms, cudaStream_t s) {
-  if (!form.pairs) return launch_half_form<Epilogue, false, 64, TERMS, CHUNK>(h, args, splits, sms, s);
-  return form.nt == 128 ? launch_half_form<Epilogue, true, 128, TERMS, CHUNK>(h, args, splits, sms, s)
-                        : launch_half_form<Epilogue, true, 256, TERMS, CHUNK>(h, args, splits, sms, s);
+  if (!form.pairs) return launch_half_form<Epilogue, false, 64, TERMS, CHUNK, LAYOUT>(h, args, splits, sms, s);
+  return form.nt == 128 ? launch_half_form<Epilogue, true, 128, TERMS, CHUNK, LAYOUT>(h, args, splits, sms, s)
+                        : launch_half_form<Epilogue, true, 256, TERMS, CHUNK, LAYOUT>(h, args, splits, sms, s);
 }
 
 }  // namespace

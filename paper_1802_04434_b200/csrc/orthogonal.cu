@@ -23,6 +23,10 @@ struct Polynomial { float a, b, c; };
 
 // The 16-bit matrices that the products leave to one another, as boxes: high and low part.
 struct Parts { CUtensorMap high, low; };
+__device__ __forceinline__ void prefetch_parts(const Parts& p) {
+  prefetch_tensor_map(&p.high);
+  prefetch_tensor_map(&p.low);
+}
 
 // 32 x 32 elements of a symmetric matrix: there, and, from tiles wholly above the diagonal, mirrored.  Tiles on the diagonal hold
 // both halves themselves.
@@ -58,6 +62,7 @@ struct GramEpilogue {
     float shift;
   };
   static constexpr unsigned kBox = 4096;
+  static __device__ __forceinline__ void prefetch(const Args& a) { prefetch_parts(a.e); }
   Box box;
   float diagonal;               // what is added there
   unsigned row0, seen, matrix;
@@ -111,6 +116,10 @@ struct PolynomialEpilogue {
     unsigned shifted;
   };
   static constexpr unsigned kBox = LOW ? 4096 : 8192;     // high parts: two boxes for E, two on their way out
+  static __device__ __forceinline__ void prefetch(const Args& a) {
+    prefetch_parts(a.m);
+    if (!LOW || !a.shifted) prefetch_parts(a.e);
+  }
   Box box;
   float p;
   unsigned row0, matrix, asks, takes;
@@ -187,6 +196,10 @@ struct UpdateEpilogue {
   };
   // two boxes of X's parts, in which X' goes out again, and one of fp32
   static constexpr unsigned kLoads = LOW ? 0 : 8192, kBox = kLoads + (LOW || TO != kNextStep ? 4096 : 0);
+  static __device__ __forceinline__ void prefetch(const Args& a) {
+    if (TO == kNextStep) prefetch_parts(a.next);
+    if (!LOW) prefetch_parts(a.x);
+  }
   Box box;
   float q, sum;
   unsigned row0, matrix, asks, takes;
@@ -772,7 +785,9 @@ ssgd_status launch_update(const Problem& p, const Layout& l, const Buffers& b, i
   a.x = b.x_parts[now]; a.next = b.x_parts[1 - now]; a.d = b.d; a.squares = b.squares;
   a.out = static_cast<T*>(p.out); a.ldo = p.ldo; a.out_stride = p.out_stride;
   a.f = p.f; a.delta = p.delta; a.rows = (unsigned)p.rows; a.count = *count; a.slots = slots;
-  return launch_half<UpdateEpilogue<TO, T, TERMS == 3>, TERMS, TERMS == 3 ? kChunk : 0>(h, a, form, 1, sms, s);
+  using Epilogue = UpdateEpilogue<TO, T, TERMS == 3>;
+  constexpr int chunk = TERMS == 3 ? kChunk : 0;
+  return h.q.by_rows ? launch_half<Epilogue, TERMS, chunk, kQByRows>(h, a, form, 1, sms, s) : launch_half<Epilogue, TERMS, chunk, kBothByK>(h, a, form, 1, sms, s);
 }
 
 // The largest |b / 2 c| that is added to A's diagonal: A + that, times 2^13, is an fp16 number, and little of A is lost beside it.
@@ -796,14 +811,17 @@ ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, i
     h.status = p.status;
     h.starve = p.starve;
     const typename GramEpilogue<TERMS == 3>::Args gram = {b.e_parts, k ? b.squares : nullptr, b.d, count, (unsigned)l.side, shifted ? shift : 0.0f};
-    ssgd_status st = launch_half<GramEpilogue<TERMS == 3>, TERMS, TERMS == 3 ? kChunk : 0>(h, gram, half_form(h, TERMS, 1, sms), 1, sms, s);
+    constexpr int chunk = TERMS == 3 ? kChunk : 0;
+    const HalfForm form = half_form(h, TERMS, 1, sms);
+    ssgd_status st = h.p.by_rows ? launch_half<GramEpilogue<TERMS == 3>, TERMS, chunk, kBothByRows>(h, gram, form, 1, sms, s)
+                                 : launch_half<GramEpilogue<TERMS == 3>, TERMS, chunk, kBothByK>(h, gram, form, 1, sms, s);
     if (st != SSGD_OK) return st;
     h.p = {b.e.high, b.e.low, b.e.ld, b.e.stride, false};
     h.q = h.p;
     h.K = l.side;
     const typename PolynomialEpilogue<TERMS == 3>::Args polynomial = {
         b.e_parts, b.m_parts, b.d, p.f, kScale * (shifted ? p.f.a - p.f.b * shift * 0.5f : p.f.a), shifted};
-    st = launch_half<PolynomialEpilogue<TERMS == 3>, TERMS, TERMS == 3 ? kChunk : 0>(h, polynomial, half_form(h, TERMS, 1, sms), 1, sms, s);
+    st = launch_half<PolynomialEpilogue<TERMS == 3>, TERMS, chunk, kBothByK>(h, polynomial, half_form(h, TERMS, 1, sms), 1, sms, s);
     if (st != SSGD_OK) return st;
     if (k + 1 < p.steps) st = launch_update<kNextStep, float, TERMS>(p, l, b, now, &count, sms, s);
     else if (p.momentum) st = launch_update<kParameters, float, TERMS>(p, l, b, now, &count, sms, s);
