@@ -225,13 +225,13 @@ struct HalfShape {
 };
 
 // Tiles go through bands of eight of P's tiles, so that those in flight share rows of both operands.
-template <bool PAIR, int NT>
+template <bool PAIR, int NT, bool SPLIT>
 __device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p) {
   constexpr unsigned rows = PAIR ? 256 : 128, kBand = 8;
   const unsigned z = tile / p.per_matrix, in_matrix = tile - z * p.per_matrix;
   HalfPlace at;
-  at.matrix = p.splits > 1 ? z / p.splits : z;
-  at.split = z - at.matrix * p.splits;
+  at.matrix = !SPLIT && p.splits > 1 ? z / p.splits : z;
+  at.split = SPLIT ? 0 : z - at.matrix * p.splits;
   at.tile = in_matrix;
   if (p.symmetric) {
     unsigned i = 0, left = in_matrix;
@@ -301,7 +301,9 @@ __device__ __forceinline__ void half_range(const HalfPlan& p, unsigned split, un
   }
 }
 
-template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK, int LAYOUT>
+// SPLIT: few tiles and a long k.  A cluster of CTAs takes one tile, each a part of k; the sums meet in shared memory and are added in
+// rank order, each of the eight warps' parts by one of the CTAs.
+template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK, int LAYOUT, bool SPLIT>
 __global__ void __launch_bounds__(kHalfThreads, 1)
 half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, const __grid_constant__ typename Epilogue::Args args) {
   using S = HalfShape<PAIR, NT, TERMS, CHUNK, Epilogue::kBox>;
@@ -312,7 +314,9 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
   const unsigned stage0 = smem_u32(half_smem);
   const unsigned full = smem_u32(bars), empty = full + 8 * S::stages, acc_full = empty + 8 * S::stages, acc_free = acc_full + 8 * S::accs, ended = acc_free + 8 * S::accs, box_full = ended + 8;
   const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-  const unsigned worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
+  static_assert(!SPLIT || (!PAIR && NT == 64), "a split tile is one of 128 x 64");
+  const unsigned cluster = SPLIT ? p.splits : PAIR ? 2 : 1;
+  const unsigned worker = blockIdx.x / cluster, workers = gridDim.x / cluster, part = SPLIT ? cluster_rank() : 0;
 
   if (threadIdx.x == 0) {
     // the first use of a map that is not at hand costs over a microsecond (200 x 200: a product 6.2 -> 5 us)
@@ -361,10 +365,10 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       const unsigned p_loaded = kPRows ? S::p_bytes : p.p_box * 128;
       const unsigned expected = (PAIR ? 2 : 1) * S::parts * (p_loaded + S::q_bytes) + p.starve;
       for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
-        const HalfPlace at = half_place<PAIR, NT>(tile, p);
+        const HalfPlace at = half_place<PAIR, NT, SPLIT>(tile, p);
         const int p0 = (int)(at.p0 + rank * 128), q0 = (int)(at.q0 + rank * S::q_rows), z = (int)at.matrix;
         unsigned first, last;
-        half_range(p, at.split, first, last);
+        half_range(p, SPLIT ? part : at.split, first, last);
         for (unsigned k = first; k < last; ++k, ++n) {
           const unsigned s = n % S::stages;
           if (n >= S::stages) ok = mbarrier_wait(empty + 8 * s, (n / S::stages - 1) & 1u, kHalfPolls);
@@ -409,7 +413,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       unsigned t = 0;                           // sums taken so far: of tiles, or of their chunks
       for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
         unsigned first, last;
-        half_range(p, p.splits > 1 ? tile / p.per_matrix % p.splits : 0, first, last);
+        half_range(p, SPLIT ? part : p.splits > 1 ? tile / p.per_matrix % p.splits : 0, first, last);
         for (unsigned from = first; from < last && ok; ++t) {
           const unsigned to = CHUNK > 0 ? min(last, from + CHUNK) : last;
           const unsigned acc = t % S::accs;
@@ -453,16 +457,19 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
     Epilogue epilogue(args, Box{stage0 + S::stages * S::stage_bytes + (warp - 4) * S::box_bytes, box_full + 16 * (warp - 4), lane});
     unsigned t = 0;
     for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
-      const HalfPlace at = half_place<PAIR, NT>(tile, p);
+      const HalfPlace at = half_place<PAIR, NT, SPLIT>(tile, p);
       const unsigned row0 = at.p0 + rank * 128 + quarter * 32;
-      epilogue.begin(args, at, row0, odd);
-      if (row0 < p.P && at.q0 + odd * 32 < p.Q) epilogue.ahead(args, at.q0 + odd * 32);
-      if constexpr (CHUNK > 0) {
+      if (!SPLIT || part == (warp - 4) % cluster) {
+        epilogue.begin(args, at, row0, odd);
+        if (row0 < p.P && at.q0 + odd * 32 < p.Q) epilogue.ahead(args, at.q0 + odd * 32);
+      }
+      if constexpr (CHUNK > 0 || SPLIT) {
+        constexpr unsigned kTake = CHUNK > 0 ? CHUNK : 1u << 30;
         unsigned first, last;
-        half_range(p, at.split, first, last);
+        half_range(p, SPLIT ? part : at.split, first, last);
         float sum[kUnits][32];
-        for (unsigned from = first; from < last; from += CHUNK, ++t) {
-          ok = mbarrier_wait(acc_full + 8 * (t % S::accs), (t / S::accs) & 1u, 4 * kHalfPolls);
+        for (unsigned from = first; from < last; from += min(kTake, last - from), ++t) {
+          ok = __all_sync(0xFFFFFFFFu, mbarrier_wait(acc_full + 8 * (t % S::accs), (t / S::accs) & 1u, 4 * kHalfPolls + 64 * p.k_stages));
           if (!ok) break;
           tcgen05_fence_after();
           const unsigned lanes = tmem + t % S::accs * NT + (quarter << 21);
@@ -479,6 +486,14 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
             for (unsigned q = 0; q < 32; ++q) sum[j][q] = from == first ? __uint_as_float(v[q]) : sum[j][q] + __uint_as_float(v[q]);
           }
         }
+        if (SPLIT) {
+          // all of this CTA's MMAs are done, and with them what its stages held
+          if (ok)
+#pragma unroll
+            for (unsigned q = 0; q < 32; ++q) store_shared4(stage0 + (warp - 4) * 4096 + q * 128 + lane * 4, __float_as_uint(sum[0][q]));
+          if (!ok) atomicExch(&failed, 1u);
+          break;
+        }
         if (!ok) break;
 #pragma unroll
         for (unsigned j = 0; j < kUnits; ++j) {
@@ -488,7 +503,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
           __syncwarp();
         }
       } else {
-        ok = mbarrier_wait(acc_full + 8 * (t % S::accs), (t / S::accs) & 1u, 4 * kHalfPolls + 64 * p.k_stages);
+        ok = __all_sync(0xFFFFFFFFu, mbarrier_wait(acc_full + 8 * (t % S::accs), (t / S::accs) & 1u, 4 * kHalfPolls + 64 * p.k_stages));
         if (!ok) break;
         tcgen05_fence_after();
         const unsigned lanes = tmem + t % S::accs * NT + (quarter << 21);
@@ -515,7 +530,39 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       __syncwarp();
       ok = epilogue.box.fine;
     }
+    if constexpr (SPLIT) {
+      cluster_sync();
+      const HalfPlace at = half_place<PAIR, NT, SPLIT>(worker, p);
+      const unsigned row0 = at.p0 + quarter * 32, column = at.q0 + odd * 32, mine = stage0 + (warp - 4) * 4096 + lane * 4;
+      const bool given_up = __any_sync(0xFFFFFFFFu, lane < cluster && load_cluster(cluster_address(smem_u32(&failed), lane)) != 0);
+      if (part == (warp - 4) % cluster && !given_up) {
+        float sum[32];
+#pragma unroll
+        for (unsigned q = 0; q < 32; ++q) sum[q] = 0.0f;
+        for (unsigned r = 0; r < cluster; ++r) {
+          const unsigned from = cluster_address(mine, r);
+          float v[32];
+#pragma unroll
+          for (unsigned q = 0; q < 32; ++q) v[q] = __uint_as_float(load_cluster(from + q * 128));
+#pragma unroll
+          for (unsigned q = 0; q < 32; ++q) sum[q] = r == 0 ? v[q] : sum[q] + v[q];
+        }
+        if (row0 < p.P && column < p.Q) epilogue.unit(args, column, min(32u, p.Q - column), sum);
+        __syncwarp();
+        epilogue.end(args, at, warp - 4);
+        __syncwarp();
+        ok = ok && epilogue.box.fine;
+      }
+    }
     epilogue.finish(args);
+  }
+  if constexpr (SPLIT) {
+    if (warp < 4) {
+      __syncwarp();
+      if (!ok) atomicExch(&failed, 1u);
+      __syncwarp();
+      cluster_sync();
+    }
   }
   if (!ok) atomicExch(&failed, 1u);
   __syncwarp();
@@ -528,7 +575,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
         (void)mbarrier_wait(full + 8 * (m % S::stages), (m / S::stages) & 1u, kHalfPolls);
   }
   __syncthreads();
-  if (PAIR) cluster_sync();
+  if (PAIR || SPLIT) cluster_sync();             // nobody leaves while its shared memory is still read
   if (warp == 1) {
     tcgen05_fence_after();
     if (PAIR) tmem_free_pair(tmem, S::columns);
@@ -583,7 +630,7 @@ inline bool box_map(CUtensorMap* map, const void* base, bool bf16, size_t rows, 
 // time (512 clocks for 256 x 256, 64 of k and one term) or shared memory's, 128 bytes a clock, for what the copies write and the
 // tensor cores read: 32 + 32, 24 + 24 and 24 + 24 KB for tiles of 256, 128 and 64 columns and one term, 64 + 96, 48 + 72 and 48 + 72 for
 // three (measured: 1000 clocks for the last).
-struct HalfForm { bool pairs; unsigned nt; };
+struct HalfForm { bool pairs; unsigned nt, split; };      // split: CTAs that share a tile's k, of 128 x 64
 inline unsigned long long half_tiles(const HalfProduct& h, unsigned rows, unsigned nt) {
   const unsigned long long tp = (h.P + rows - 1) / rows, tq = (h.Q + nt - 1) / nt;
   if (!h.symmetric) return tp * tq;
@@ -597,15 +644,28 @@ inline HalfForm half_form(const HalfProduct& h, int terms, unsigned splits, int 
                            r64 = (half_tiles(h, 128, 64) * batch + sms - 1) / (unsigned)sms;
   const unsigned s256 = terms == 3 ? 1560 : 530, s128 = terms == 3 ? 980 : 400, s64 = terms == 3 ? 1000 : 390;
   const unsigned long long c256 = r256 * (stages * s256 + 1500) + 6500, c128 = r128 * (stages * s128 + 1200) + 5500, c64 = r64 * (stages * s64 + 1000) + 5000;
-  if (c256 <= c128 && c256 <= c64) return {true, 256};
-  return c128 <= c64 ? HalfForm{true, 128} : HalfForm{false, 64};
+  HalfForm best = c256 <= c128 && c256 <= c64 ? HalfForm{true, 256, 1} : c128 <= c64 ? HalfForm{true, 128, 1} : HalfForm{false, 64, 1};
+  unsigned long long least = c256 < c128 ? c256 : c128;
+  if (c64 < least) least = c64;
+  // k shared by a cluster, where all clusters find their place at one time (on 148 SMs two CTAs 72 times, four 32 times, eight 12 times)
+  const unsigned long long tiles = half_tiles(h, 128, 64) * batch;
+  for (unsigned split = 2; split <= 8 && splits == 1; split *= 2) {
+    const unsigned fit = (unsigned)sms * (split == 2 ? 72 : split == 4 ? 32 : 12) / 148;
+    if (tiles > fit || stages < 2 * split) break;
+    const unsigned long long c = ((h.K + 63) / 64 / split + 1) * s64 + 1000 + 5000 + 2500;
+    if (c < least) {
+      least = c;
+      best = {false, 64, split};
+    }
+  }
+  return best;
 }
 
-template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK, int LAYOUT>
+template <class Epilogue, bool PAIR, int NT, int TERMS, int CHUNK, int LAYOUT, bool SPLIT>
 ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args& args, unsigned splits, int sms, cudaStream_t s) {
   using S = HalfShape<PAIR, NT, TERMS, CHUNK, Epilogue::kBox>;
   HalfPlan p = {};
-  const unsigned long long per = half_tiles(h, S::rows, NT), tiles = per * h.batch * splits;
+  const unsigned long long per = half_tiles(h, S::rows, NT), tiles = per * h.batch * (SPLIT ? 1 : splits);
   if (h.P >= (1ull << 31) || h.Q >= (1ull << 31) || h.K >= (1ull << 31) || tiles >= (1ull << 30)) return SSGD_ERR_SIZE;
   p.P = (unsigned)h.P; p.Q = (unsigned)h.Q;
   p.k_stages = (unsigned)((h.K + 63) / 64); p.k_chunks = (unsigned)((h.K + 15) / 16);
@@ -625,7 +685,7 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
       !half_map(&maps.p[1], TERMS == 3 ? h.p.low : h.p.high, h.bf16, h.p, h.P, h.K, h.batch, p.p_box) ||
       !half_map(&maps.q[1], TERMS == 3 ? q1.low : q1.high, h.bf16, q1, h.Q, h.K, h.batch, S::q_rows))
     return SSGD_ERR_CUDA;
-  auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS, CHUNK, LAYOUT>;
+  auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS, CHUNK, LAYOUT, SPLIT>;
   static unsigned long long seen = 0;
   if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
   if constexpr (half_shifts(NT, CHUNK)) {         // registers as the kernel's own shares add up to
@@ -639,7 +699,7 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
   }
   const unsigned long long most = PAIR ? (unsigned)sms / 2 : (unsigned)sms, workers = tiles < most ? tiles : most;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(PAIR ? 2 * workers : workers));
+  cfg.gridDim = dim3((unsigned)(SPLIT ? splits * tiles : PAIR ? 2 * workers : workers));
   cfg.blockDim = dim3(kHalfThreads);
   cfg.dynamicSmemBytes = S::smem;
   cfg.stream = s;
@@ -647,10 +707,10 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.x = SPLIT ? splits : 2;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = PAIR ? 2 : 1;
+  cfg.numAttrs = PAIR || SPLIT ? 2 : 1;
   (void)cudaLaunchKernelEx(&cfg, kernel, maps, p, args);
   return launch_status();
 }
@@ -658,9 +718,10 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
 // LAYOUT says what h.p.by_rows and h.q.by_rows say.
 template <class Epilogue, int TERMS, int CHUNK, int LAYOUT>
 ssgd_status launch_half(const HalfProduct& h, const typename Epilogue::Args& args, const HalfForm& form, unsigned splits, int sms, cudaStream_t s) {
-  if (!form.pairs) return launch_half_form<Epilogue, false, 64, TERMS, CHUNK, LAYOUT>(h, args, splits, sms, s);
-  return form.nt == 128 ? launch_half_form<Epilogue, true, 128, TERMS, CHUNK, LAYOUT>(h, args, splits, sms, s)
-                        : launch_half_form<Epilogue, true, 256, TERMS, CHUNK, LAYOUT>(h, args, splits, sms, s);
+  if (form.split > 1) return launch_half_form<Epilogue, false, 64, TERMS, CHUNK, LAYOUT, true>(h, args, form.split, sms, s);
+  if (!form.pairs) return launch_half_form<Epilogue, false, 64, TERMS, CHUNK, LAYOUT, false>(h, args, splits, sms, s);
+  return form.nt == 128 ? launch_half_form<Epilogue, true, 128, TERMS, CHUNK, LAYOUT, false>(h, args, splits, sms, s)
+                        : launch_half_form<Epilogue, true, 256, TERMS, CHUNK, LAYOUT, false>(h, args, splits, sms, s);
 }
 
 }  // namespace

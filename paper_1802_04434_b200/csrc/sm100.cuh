@@ -129,6 +129,8 @@ __device__ __forceinline__ void tcgen05_copy_scales(unsigned tmem, uint64_t desc
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
+__device__ __forceinline__ void store_shared4(unsigned at, unsigned v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+
 // Shared-memory matrix descriptor: start address, stride between groups of eight rows, layout (0: none, 2: 128-byte swizzle).
 __device__ __forceinline__ uint64_t smem_descriptor(unsigned addr, unsigned group_stride, unsigned layout) {
   return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(group_stride >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)layout << 61;
@@ -206,6 +208,11 @@ __device__ __forceinline__ unsigned cluster_address(unsigned addr, unsigned rank
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ unsigned load_cluster(unsigned cluster_addr) {          // from another CTA's shared memory
+  unsigned v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_addr) : "memory");
+  return v;
 }
 // An arrival at a barrier of another CTA that orders tensor memory only (between the two tcgen05 fences): relaxed, since a
 // release would first wait for all of this thread's stores to global memory (a third of the time of a short product).
