@@ -257,9 +257,6 @@ __device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p
 //   end(args, place, warp)          behind the last
 //   finish(args)                    behind the last tile
 // All threads of a warp call each of them.
-constexpr unsigned kShiftRegisters = 168;
-__host__ __device__ constexpr bool half_shifts(int nt, int chunk) { return nt == 256 && chunk > 0; }
-
 // How the operands lie in memory: which of them with their rows side by side.
 enum HalfLayout { kBothByK = 0, kQByRows = 1, kBothByRows = 3 };
 
@@ -338,6 +335,11 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
     mbarrier_init_fence();
     failed = 0;
   }
+  // What can be done while the kernel before this one ends: the other CTA's barriers, and the first tile's place (its code is cold).
+  HalfPlace start = half_place<PAIR, NT, SPLIT>(worker, p);
+  asm volatile("" : "+r"(start.p0), "+r"(start.q0), "+r"(start.matrix), "+r"(start.split), "+r"(start.tile));
+  __syncwarp();                                 // the barrier wants whole warps
+  if (PAIR) cluster_sync();
   pdl_launch_dependents();
   pdl_wait();                                   // before tensor memory is taken: its last holder has finished
   if (warp == 1) {
@@ -345,19 +347,12 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
     else tmem_alloc(smem_u32(&tmem_base), S::columns);
   }
   tcgen05_fence_before();
-  __syncthreads();
-  if (PAIR) cluster_sync();                     // the other CTA's barriers are ready too
+  __syncthreads();                              // a pair's products begin when both CTAs' operands are there, and so both have come here
   tcgen05_fence_after();
   const unsigned tmem = tmem_base;
   bool ok = true;
   unsigned n = 0;                               // stages so far, over all tiles
 
-  // Tiles of 256 columns summed by chunks: 128 sums a thread.  The epilogue's warps take the registers that the first warpgroup
-  // does without: 128 * 40 + 256 * 232 = 384 * 168, which is what the block is launched with (the host has made sure).
-  constexpr bool kShift = half_shifts(NT, CHUNK);
-
-  if (warp < 4) {
-  if constexpr (kShift) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
   if (warp == 0) {
     if (elect_one()) {
       const CUtensorMap* q_high = p.q_choice && *p.q_choice ? &maps.q[1] : &maps.q[0];
@@ -365,7 +360,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       const unsigned p_loaded = kPRows ? S::p_bytes : p.p_box * 128;
       const unsigned expected = (PAIR ? 2 : 1) * S::parts * (p_loaded + S::q_bytes) + p.starve;
       for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
-        const HalfPlace at = half_place<PAIR, NT, SPLIT>(tile, p);
+        const HalfPlace at = tile == worker ? start : half_place<PAIR, NT, SPLIT>(tile, p);
         const int p0 = (int)(at.p0 + rank * 128), q0 = (int)(at.q0 + rank * S::q_rows), z = (int)at.matrix;
         unsigned first, last;
         half_range(p, SPLIT ? part : at.split, first, last);
@@ -448,16 +443,14 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
         (void)mbarrier_wait(ended, 0, kHalfPolls);
       }
     }
-  }
-  } else {
-    if constexpr (kShift) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+  } else if (warp >= 4) {
     constexpr unsigned kUnits = NT / 64;        // of 32 columns, of this warp
     const unsigned quarter = warp & 3u, odd = warp >= 8;
     const unsigned go = PAIR ? cluster_address(acc_free, 0) : acc_free;
     Epilogue epilogue(args, Box{stage0 + S::stages * S::stage_bytes + (warp - 4) * S::box_bytes, box_full + 16 * (warp - 4), lane});
     unsigned t = 0;
     for (unsigned tile = worker; tile < p.tiles && ok; tile += workers) {
-      const HalfPlace at = half_place<PAIR, NT, SPLIT>(tile, p);
+      const HalfPlace at = tile == worker ? start : half_place<PAIR, NT, SPLIT>(tile, p);
       const unsigned row0 = at.p0 + rank * 128 + quarter * 32;
       if (!SPLIT || part == (warp - 4) % cluster) {
         epilogue.begin(args, at, row0, odd);
@@ -468,22 +461,28 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
         unsigned first, last;
         half_range(p, SPLIT ? part : at.split, first, last);
         float sum[kUnits][32];
+#pragma unroll
+        for (unsigned j = 0; j < kUnits; ++j)
+#pragma unroll
+          for (unsigned q = 0; q < 32; ++q) sum[j][q] = 0.0f;
+#pragma unroll 1
         for (unsigned from = first; from < last; from += min(kTake, last - from), ++t) {
           ok = __all_sync(0xFFFFFFFFu, mbarrier_wait(acc_full + 8 * (t % S::accs), (t / S::accs) & 1u, 4 * kHalfPolls + 64 * p.k_stages));
           if (!ok) break;
           tcgen05_fence_after();
           const unsigned lanes = tmem + t % S::accs * NT + (quarter << 21);
+          // 16 columns at a time: beside the 128 sums of 256 columns a thread has 40 registers
 #pragma unroll
-          for (unsigned j = 0; j < kUnits; ++j) {
-            unsigned v[32];
-            tmem_read32(lanes + (odd + 2 * j) * 32, v);
-            if (j + 1 == kUnits) {
+          for (unsigned j = 0; j < 2 * kUnits; ++j) {
+            unsigned v[16];
+            tmem_read16(lanes + (odd + j / 2 * 2) * 32 + j % 2 * 16, v);
+            if (j + 1 == 2 * kUnits) {
               tcgen05_fence_before();
               __syncwarp();
               if (lane == 0) mbarrier_arrive_cluster(go + 8 * (t % S::accs));
             }
 #pragma unroll
-            for (unsigned q = 0; q < 32; ++q) sum[j][q] = from == first ? __uint_as_float(v[q]) : sum[j][q] + __uint_as_float(v[q]);
+            for (unsigned q = 0; q < 16; ++q) sum[j / 2][j % 2 * 16 + q] += __uint_as_float(v[q]);
           }
         }
         if (SPLIT) {
@@ -531,8 +530,9 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
       ok = epilogue.box.fine;
     }
     if constexpr (SPLIT) {
+      __syncwarp();
       cluster_sync();
-      const HalfPlace at = half_place<PAIR, NT, SPLIT>(worker, p);
+      const HalfPlace at = start;
       const unsigned row0 = at.p0 + quarter * 32, column = at.q0 + odd * 32, mine = stage0 + (warp - 4) * 4096 + lane * 4;
       const bool given_up = __any_sync(0xFFFFFFFFu, lane < cluster && load_cluster(cluster_address(smem_u32(&failed), lane)) != 0);
       if (part == (warp - 4) % cluster && !given_up) {
@@ -575,6 +575,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
         (void)mbarrier_wait(full + 8 * (m % S::stages), (m / S::stages) & 1u, kHalfPolls);
   }
   __syncthreads();
+  __syncwarp();
   if (PAIR || SPLIT) cluster_sync();             // nobody leaves while its shared memory is still read
   if (warp == 1) {
     tcgen05_fence_after();
@@ -688,15 +689,6 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
   auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS, CHUNK, LAYOUT, SPLIT>;
   static unsigned long long seen = 0;
   if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
-  if constexpr (half_shifts(NT, CHUNK)) {         // registers as the kernel's own shares add up to
-    static int registers = 0;
-    if (__atomic_load_n(&registers, __ATOMIC_RELAXED) == 0) {
-      cudaFuncAttributes a;
-      if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess) return SSGD_ERR_CUDA;
-      __atomic_store_n(&registers, a.numRegs, __ATOMIC_RELAXED);
-    }
-    if (registers != (int)kShiftRegisters) return SSGD_ERR_CUDA;
-  }
   const unsigned long long most = PAIR ? (unsigned)sms / 2 : (unsigned)sms, workers = tiles < most ? tiles : most;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(SPLIT ? splits * tiles : PAIR ? 2 * workers : workers));

@@ -124,6 +124,16 @@ __device__ __forceinline__ void tmem_read32(unsigned tmem, unsigned (&v)[32]) {
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_read16(unsigned tmem, unsigned (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(tmem)
+      : "memory");
+}
+
 // 512 bytes, a tile of block scales, to four columns, the same in each 32 lanes.
 __device__ __forceinline__ void tcgen05_copy_scales(unsigned tmem, uint64_t desc) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
