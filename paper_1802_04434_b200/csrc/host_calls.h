@@ -31,6 +31,19 @@ inline bool allow_smem(const void* kernel, size_t bytes, unsigned long long* see
   return true;
 }
 
+// Whether a launch by clusters of more than eight CTAs has room on the current device, asked once per kernel and device.
+inline bool allow_wide_clusters(const void* kernel, const cudaLaunchConfig_t& cfg, unsigned long long* seen) {
+  int dev = 0, clusters = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 32) return false;
+  const unsigned long long known = __atomic_load_n(seen, __ATOMIC_RELAXED) >> (2 * dev) & 3u;      // 2: asked, 1: there is room
+  if (known & 2u) return known & 1u;
+  const bool room = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                    cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0;
+  if (!room) (void)cudaGetLastError();
+  __atomic_fetch_or(seen, (room ? 3ull : 2ull) << (2 * dev), __ATOMIC_RELAXED);
+  return room;
+}
+
 }  // namespace
 
 #endif  // SSGD_HOST_CALLS_H_

@@ -50,9 +50,9 @@ __device__ __forceinline__ void send_symmetric(const Box& box, unsigned offset, 
   box.send(to.high, LOW ? offset : offset + 2048, row0, column, matrix);
 }
 
-// The product X X^T.  High parts alone: E = A - d I, where d comes from the sums of squares that the last step left, added in a fixed
-// order by each warp; the first tile of each matrix leaves it for the other two products.  Both parts: A + (b / 2 c) I, see below.
-template <bool LOW>
+// The product X X^T.  DEFLATED: E = A - d I, where d comes from the sums of squares that the last step left, added in a fixed order by each
+// warp; the first tile of each matrix leaves it for the other two products.  Else A + (b / 2 c) I, see below.
+template <bool LOW, bool DEFLATED>
 struct GramEpilogue {
   struct Args {
     Parts e;
@@ -73,7 +73,7 @@ struct GramEpilogue {
     row0 = first_row;
     matrix = at.matrix;
     mirrored = at.q0 >= at.p0 + at.rows;
-    if (!LOW) {
+    if (DEFLATED) {
       if (matrix != seen) {
         seen = matrix;
         float sum = 1.0f;
@@ -103,22 +103,23 @@ struct GramEpilogue {
 };
 
 // The polynomial from the square of what the first product left.
-//   high parts alone   M = p E + c E^2 with p = b + 2 c d;  X' = (a + b d + c d^2) X + M X
-//   both parts         M = a I + b A + c A^2 = (a - b^2 / 4 c) I + c (A + (b / 2 c) I)^2, nothing to be read again;  X' = M X.  Where c is too
-//                      small for that, shift = 0 and A is read
-template <bool LOW>
+//   DEFLATED   M = p E + c E^2 with p = b + 2 c d;  X' = (a + b d + c d^2) X + M X
+//   else       M = a I + b A + c A^2 = (a - b^2 / 4 c) I + c (A + (b / 2 c) I)^2, nothing to be read again;  X' = M X.  Where c is too
+//              small for that, shift = 0 and A is read
+template <bool LOW, bool DEFLATED>
 struct PolynomialEpilogue {
   struct Args {
     Parts e, m;
     const float* d;
     Polynomial f;
-    float diagonal;             // LOW: what is added there
+    float diagonal;             // not deflated: what is added there
     unsigned shifted;
   };
-  static constexpr unsigned kBox = LOW ? 4096 : 8192;     // high parts: two boxes for E, two on their way out
+  // two boxes for E's parts, in which M's go out
+  static constexpr unsigned kBox = DEFLATED ? 8192 : 4096;
   static __device__ __forceinline__ void prefetch(const Args& a) {
     prefetch_parts(a.m);
-    if (!LOW || !a.shifted) prefetch_parts(a.e);
+    if (DEFLATED || !a.shifted) prefetch_parts(a.e);
   }
   Box box;
   float p;
@@ -129,60 +130,61 @@ struct PolynomialEpilogue {
     row0 = first_row;
     matrix = at.matrix;
     mirrored = at.q0 >= at.p0 + at.rows;
-    if (!LOW) p = a.f.b + 2.0f * a.f.c * a.d[matrix];
+    if (DEFLATED) p = a.f.b + 2.0f * a.f.c * a.d[matrix];
   }
   __device__ __forceinline__ void ahead(const Args& a, unsigned column) {
-    if (!LOW) {
-      box.ask(asks & 1u, (asks & 1u) * 2048, a.e.high, nullptr, column, row0, matrix);
+    if (DEFLATED) {
+      box.sent();
+      box.ask(asks & 1u, (asks & 1u) * 4096, a.e.high, LOW ? &a.e.low : nullptr, column, row0, matrix);
       ++asks;
     }
   }
   __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned, float (&v)[32]) {
-    const float c = a.f.c * kUnscale;
-    if (!LOW) {
-      const unsigned b = takes++ & 1u;
+    const float c = a.f.c * kUnscale, by = DEFLATED ? p : a.f.b;
+    unsigned from = 0;
+    if (DEFLATED || !a.shifted) {
+      const unsigned b = DEFLATED ? takes++ & 1u : 0;
+      from = b * 4096;
+      if (!DEFLATED) {
+        box.sent();
+        box.ask(0, 0, a.e.high, &a.e.low, column, row0, matrix);
+      }
       box.take(b);
 #pragma unroll
       for (unsigned q = 0; q < 4; ++q) {
         float e[8];
-        box.get8(b * 2048, q, e);
+        box.get8(from, q, e);
+        if (LOW) {
+          float low[8];
+          box.get8(from + 2048, q, low);
 #pragma unroll
-        for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = fmaf(c, v[8 * q + i], p * e[i]);
-      }
-    } else if (a.shifted) {
+          for (unsigned i = 0; i < 8; ++i) e[i] += low[i];
+        }
 #pragma unroll
-      for (unsigned q = 0; q < 32; ++q) v[q] *= c;
-    } else {
-      box.sent();
-      box.ask(0, 0, a.e.high, &a.e.low, column, row0, matrix);
-      box.take(0);
-#pragma unroll
-      for (unsigned q = 0; q < 4; ++q) {
-        float high[8], low[8];
-        box.get8(0, q, high);
-        box.get8(2048, q, low);
-#pragma unroll
-        for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = fmaf(c, v[8 * q + i], a.f.b * (high[i] + low[i]));
+        for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = fmaf(c, v[8 * q + i], by * e[i]);
       }
       __syncwarp();
+    } else {
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) v[q] *= c;
     }
-    if (LOW) {
+    if (!DEFLATED) {
       const unsigned on = row0 + box.lane - column;
       if (on < 32u) {
 #pragma unroll
         for (unsigned q = 0; q < 32; ++q) v[q] = on == q ? v[q] + a.diagonal : v[q];
       }
     }
-    send_symmetric<LOW>(box, LOW ? 0 : 4096, a.m, row0, column, matrix, mirrored, v);
+    send_symmetric<LOW>(box, from, a.m, row0, column, matrix, mirrored, v);
   }
   __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
   __device__ __forceinline__ void finish(const Args&) { box.finish(); }
 };
 
-// X' = M X, or of the high parts (a + b d + c d^2) X + M X: kept for the next step, with its sum of squares; or, behind the last, written
+// X' = M X, or deflated (a + b d + c d^2) X + M X: kept for the next step, with its sum of squares; or, behind the last, written
 // out as T; or x <- x - delta X'.
 enum UpdateTo { kNextStep, kOut, kParameters };
-template <int TO, typename T, bool LOW>
+template <int TO, typename T, bool LOW, bool DEFLATED>
 struct UpdateEpilogue {
   struct Args {
     Parts x, next;
@@ -194,11 +196,10 @@ struct UpdateEpilogue {
     float delta;
     unsigned rows, count, slots;        // sums of squares of a matrix, and of a tile
   };
-  // two boxes of X's parts, in which X' goes out again, and one of fp32
-  static constexpr unsigned kLoads = LOW ? 0 : 8192, kBox = kLoads + (LOW || TO != kNextStep ? 4096 : 0);
+  static constexpr unsigned kBox = DEFLATED ? 8192 : 4096;      // two boxes of X's parts, in which X' goes out again
   static __device__ __forceinline__ void prefetch(const Args& a) {
     if (TO == kNextStep) prefetch_parts(a.next);
-    if (!LOW) prefetch_parts(a.x);
+    if (DEFLATED) prefetch_parts(a.x);
   }
   Box box;
   float q, sum;
@@ -207,14 +208,14 @@ struct UpdateEpilogue {
   __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
     row0 = first_row;
     matrix = at.matrix;
-    if (!LOW) {
+    if (DEFLATED) {
       const float d = a.d[matrix];
       q = a.f.a + d * (a.f.b + d * a.f.c);
       sum = 0.0f;
     }
   }
   __device__ __forceinline__ void ahead(const Args& a, unsigned column) {
-    if (!LOW) {
+    if (DEFLATED) {
       if (TO == kNextStep) box.sent();
       box.ask(asks & 1u, (asks & 1u) * 4096, a.x.high, &a.x.low, column, row0, matrix);
       ++asks;
@@ -222,7 +223,7 @@ struct UpdateEpilogue {
   }
   __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
     unsigned from = 0;
-    if (LOW) {
+    if (!DEFLATED) {
 #pragma unroll
       for (unsigned i = 0; i < 32; ++i) v[i] *= kUnscale;
       if (TO == kNextStep) box.sent();
@@ -241,7 +242,7 @@ struct UpdateEpilogue {
       __syncwarp();
     }
     if constexpr (TO == kNextStep) {
-      if (!LOW && row0 + box.lane < a.rows) {   // behind the last column there are zeros
+      if (DEFLATED && row0 + box.lane < a.rows) {   // behind the last column there are zeros
 #pragma unroll
         for (unsigned i = 0; i < 32; ++i) sum = fmaf(v[i], v[i], sum);
       }
@@ -253,7 +254,7 @@ struct UpdateEpilogue {
       const float by = TO == kOut ? kUnscale : -a.delta * kUnscale;
 #pragma unroll
       for (unsigned i = 0; i < 32; ++i) v[i] *= by;
-      Box whole(box.at + kLoads, box.full, box.lane);
+      Box whole(box.at + from, box.full, box.lane);
       T* o = a.out + matrix * a.out_stride + (size_t)row0 * a.ldo + column;
       const unsigned rows = min(32u, a.rows - row0);
       if constexpr (TO == kOut) whole.rows_out(o, a.ldo, rows, left, v);
@@ -261,7 +262,7 @@ struct UpdateEpilogue {
     }
   }
   __device__ __forceinline__ void end(const Args& a, const HalfPlace& at, unsigned warp) {
-    if constexpr (TO == kNextStep && !LOW) {
+    if constexpr (TO == kNextStep && DEFLATED) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       if (box.lane == 0) a.squares[(size_t)matrix * a.count + at.tile * a.slots + warp] = sum * (kUnscale * kUnscale);
@@ -687,6 +688,220 @@ orthogonal_small_kernel(const SmallArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
+// Matrices of a few tiles: a cluster of CTAs does all steps of one matrix in one launch, a barrier of the cluster between two products.  (A
+// launch of its own costs a small product 4 of its 6 us: the gap, the start, code that is cold.)  Tiles of 128 x 64 and the same
+// stages, sums and epilogues as half_product_kernel's; what one product leaves for the next goes through L2.
+
+template <int TO, typename T>
+struct ClusterArgs {
+  CUtensorMap x[2][2], e[2], m[2];              // operands in boxes of 64 x 64, high and low part; the same boxes serve either way round
+  typename GramEpilogue<true, true>::Args gram[2];          // of the first step, and of the others
+  typename PolynomialEpilogue<true, true>::Args polynomial;
+  typename UpdateEpilogue<kNextStep, float, true, true>::Args next[2];
+  typename UpdateEpilogue<TO, T, true, true>::Args last;
+  unsigned rows, cols, steps, starve;
+  unsigned* status;
+};
+
+using ClusterShape = HalfShape<false, 64, 3, 1, 8192>;
+
+struct ClusterState {
+  unsigned stage0, full, empty, acc_full, acc_free, tmem, warp, lane, rank, size, matrix, starve;
+  unsigned n, t;                                // stages and sums so far, as this thread's role counts them
+  unsigned phase;                               // of this warp's box: the epilogues share it
+  bool ok;
+};
+
+// One product, tile after tile by the CTAs of the cluster in turn.
+template <int LAYOUT, bool SYMMETRIC, class Epilogue>
+__device__ __forceinline__ void cluster_product(ClusterState& st, const CUtensorMap* p_maps, const CUtensorMap* q_maps, unsigned P, unsigned Q, unsigned K,
+                                                Epilogue& epilogue, const typename Epilogue::Args& args) {
+  using S = ClusterShape;
+  constexpr unsigned low = (S::p_bytes + S::q_bytes) >> 4;
+  const unsigned tiles_p = (P + 127) / 128, tiles_q = (Q + 63) / 64, stages = (K + 63) / 64, chunks = (K + 15) / 16;
+  // f(first row, first column, whether it is the first tile) for this CTA's tiles, along the rows of tiles, in a symmetric product from the
+  // diagonal on
+  auto each_tile = [&](auto f) {
+    unsigned tile = st.rank;
+    for (unsigned i = 0; i < tiles_p && st.ok; ++i) {
+      const unsigned begin = SYMMETRIC ? 2 * i : 0, count = tiles_q > begin ? tiles_q - begin : 0;
+      for (; tile < count && st.ok; tile += st.size) f(i * 128, (begin + tile) * 64);
+      tile -= min(tile, count);
+    }
+  };
+  if (st.warp == 0) {
+    if (elect_one()) {
+      each_tile([&](unsigned p0, unsigned q0) {
+        for (unsigned k = 0; k < stages; ++k, ++st.n) {
+          const unsigned s = st.n % S::stages;
+          if (st.n >= S::stages) st.ok = mbarrier_wait(st.empty + 8 * s, (st.n / S::stages - 1) & 1u, kHalfPolls);
+          if (!st.ok) break;
+          const unsigned base = st.stage0 + s * S::stage_bytes, bar = st.full + 8 * s;
+          mbarrier_expect(bar, 2 * (S::p_bytes + S::q_bytes) + st.starve);
+#pragma unroll
+          for (unsigned h = 0; h < 2; ++h) {
+            const unsigned pd = base + h * (S::p_bytes + S::q_bytes), qd = pd + S::p_bytes;
+#pragma unroll
+            for (unsigned j = 0; j < 2; ++j) {
+              if (LAYOUT & 2) tma_load_3d(pd + j * 8192, &p_maps[h], (int)(p0 + 64 * j), (int)(k * 64), (int)st.matrix, bar);
+              else tma_load_3d(pd + j * 8192, &p_maps[h], (int)(k * 64), (int)(p0 + 64 * j), (int)st.matrix, bar);
+            }
+            if (LAYOUT & 1) tma_load_3d(qd, &q_maps[h], (int)q0, (int)(k * 64), (int)st.matrix, bar);
+            else tma_load_3d(qd, &q_maps[h], (int)(k * 64), (int)q0, (int)st.matrix, bar);
+          }
+        }
+      });
+    }
+    __syncwarp();
+  } else if (st.warp == 1) {
+    if (elect_one()) {
+      const uint64_t p_desc = half_descriptor(st.stage0, (LAYOUT & 2) != 0), q_desc = half_descriptor(st.stage0 + S::p_bytes, (LAYOUT & 1) != 0);
+      const unsigned idesc = mma_half_descriptor(128, 64, false, (LAYOUT & 2) != 0, (LAYOUT & 1) != 0);
+      each_tile([&](unsigned, unsigned) {
+        for (unsigned k = 0; k < stages; ++k, ++st.n, ++st.t) {
+          const unsigned s = st.n % S::stages, acc = st.t % S::accs;
+          if (st.t >= S::accs) st.ok = mbarrier_wait(st.acc_free + 8 * acc, (st.t / S::accs - 1) & 1u, kHalfPolls);
+          st.ok = st.ok && mbarrier_wait(st.full + 8 * s, (st.n / S::stages) & 1u, kHalfPolls);
+          if (!st.ok) break;
+          tcgen05_fence_after();
+          const unsigned at = s * (S::stage_bytes >> 4);
+          half_issue<false, 3, LAYOUT, low>(st.tmem + acc * 64, p_desc + at, q_desc + at, idesc, chunks - k * 4, false);
+          tcgen05_commit(st.empty + 8 * s);
+          tcgen05_commit(st.acc_full + 8 * acc);
+        }
+      });
+    }
+    __syncwarp();
+  } else if (st.warp >= 4) {
+    const unsigned quarter = st.warp & 3u, odd = st.warp >= 8;
+    epilogue.box.phase = st.phase;
+    each_tile([&](unsigned p0, unsigned q0) {
+      const unsigned row0 = p0 + quarter * 32, column = q0 + odd * 32;
+      const HalfPlace at = {st.matrix, 0, p0, q0, p0 / 128 * tiles_q + q0 / 64, 0, 128};
+      epilogue.begin(args, at, row0, odd);
+      const bool inside = row0 < P && column < Q;
+      if (inside) epilogue.ahead(args, column);
+      float sum[32];
+#pragma unroll
+      for (unsigned q = 0; q < 32; ++q) sum[q] = 0.0f;
+#pragma unroll 1
+      for (unsigned k = 0; k < stages; ++k, ++st.t) {
+        const unsigned acc = st.t % S::accs;
+        st.ok = __all_sync(0xFFFFFFFFu, mbarrier_wait(st.acc_full + 8 * acc, (st.t / S::accs) & 1u, 4 * kHalfPolls));
+        if (!st.ok) break;
+        tcgen05_fence_after();
+        unsigned v[32];
+        tmem_read32(st.tmem + acc * 64 + (quarter << 21) + odd * 32, v);
+        tcgen05_fence_before();
+        __syncwarp();
+        if (st.lane == 0) mbarrier_arrive_cluster(st.acc_free + 8 * acc);
+#pragma unroll
+        for (unsigned q = 0; q < 32; ++q) sum[q] += __uint_as_float(v[q]);
+      }
+      if (st.ok && inside) epilogue.unit(args, column, min(32u, Q - column), sum);
+      __syncwarp();
+      if (st.ok) epilogue.end(args, at, st.warp - 4);
+      __syncwarp();
+    });
+  }
+  if (st.warp >= 4) {
+    epilogue.box.finish();                      // what has been sent is there
+    st.ok = st.ok && epilogue.box.fine;
+    st.phase = epilogue.box.phase;
+  }
+}
+
+template <bool TALL, int TO, typename T>
+__global__ void __launch_bounds__(kHalfThreads, 1)
+orthogonal_cluster_kernel(const __grid_constant__ ClusterArgs<TO, T> a) {
+  using S = ClusterShape;
+  extern __shared__ __align__(1024) unsigned char cluster_smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(cluster_smem + S::stages * S::stage_bytes + S::out_bytes);
+  unsigned &tmem_base = *reinterpret_cast<unsigned*>(bars + 2 * S::stages + 1 + 16 + 2 * S::accs), &failed = *(&tmem_base + 1);
+  ClusterState st;
+  st.stage0 = smem_u32(cluster_smem);
+  st.full = smem_u32(bars);
+  st.empty = st.full + 8 * S::stages;
+  st.acc_full = st.empty + 8 * S::stages;
+  st.acc_free = st.acc_full + 8 * S::accs;
+  const unsigned box_full = st.acc_free + 8 * S::accs;
+  st.warp = threadIdx.x >> 5;
+  st.lane = threadIdx.x & 31u;
+  st.rank = cluster_rank();
+  st.size = cluster_size();
+  st.matrix = blockIdx.x / st.size;
+  st.starve = a.starve;
+  st.n = st.t = st.phase = 0;
+  st.ok = true;
+  if (threadIdx.x == 0) {
+    prefetch_tensor_map(&a.x[0][0]);
+    prefetch_tensor_map(&a.x[0][1]);
+    for (unsigned s = 0; s < S::stages; ++s) {
+      mbarrier_init(st.full + 8 * s, 1);
+      mbarrier_init(st.empty + 8 * s, 1);
+    }
+    for (unsigned b = 0; b < S::accs; ++b) {
+      mbarrier_init(st.acc_full + 8 * b, 1);
+      mbarrier_init(st.acc_free + 8 * b, 8);
+    }
+    for (unsigned b = 0; b < 16; ++b) mbarrier_init(box_full + 8 * b, 1);
+    mbarrier_init_fence();
+    failed = 0;
+  }
+  pdl_launch_dependents();
+  pdl_wait();                                   // before tensor memory is taken: its last holder has finished
+  if (st.warp == 1) tmem_alloc(smem_u32(&tmem_base), S::columns);
+  tcgen05_fence_before();
+  __syncthreads();
+  tcgen05_fence_after();
+  st.tmem = tmem_base;
+
+  const unsigned side = TALL ? a.cols : a.rows, other = TALL ? a.rows : a.cols, w = st.warp >= 4 ? st.warp - 4 : 0;
+  const Box box(st.stage0 + S::stages * S::stage_bytes + w * S::box_bytes, box_full + 16 * w, st.lane);
+  GramEpilogue<true, true> gram(a.gram[0], box);
+  PolynomialEpilogue<true, true> polynomial(a.polynomial, box);
+  UpdateEpilogue<kNextStep, float, true, true> next(a.next[0], box);
+  UpdateEpilogue<TO, T, true, true> last(a.last, box);
+  // All CTAs of the cluster have left a product behind.  A CTA that gave up keeps step and does nothing more.
+  auto between = [&]() {
+    if (!st.ok) atomicExch(&failed, 1u);
+    proxy_fence();
+    __syncwarp();
+    cluster_sync();
+    proxy_fence();
+    st.ok = *(volatile unsigned*)&failed == 0;
+  };
+  for (unsigned k = 0; k < a.steps; ++k) {
+    const CUtensorMap* x = a.x[k & 1u];
+    gram.seen = ~0u;                            // another step, another d
+    cluster_product<TALL ? kBothByRows : kBothByK, true>(st, x, x, side, side, other, gram, a.gram[k > 0]);
+    between();
+    cluster_product<kBothByK, true>(st, a.e, a.e, side, side, side, polynomial, a.polynomial);
+    between();
+    if (k + 1 < a.steps) {
+      if (TALL) cluster_product<kBothByK, false>(st, x, a.m, a.rows, a.cols, side, next, a.next[k & 1u]);
+      else cluster_product<kQByRows, false>(st, a.m, x, a.rows, a.cols, side, next, a.next[k & 1u]);
+    } else {
+      if (TALL) cluster_product<kBothByK, false>(st, x, a.m, a.rows, a.cols, side, last, a.last);
+      else cluster_product<kQByRows, false>(st, a.m, x, a.rows, a.cols, side, last, a.last);
+    }
+    between();
+  }
+  // the last stages' commits have to arrive, and where a wait ran out, the copies that were asked for
+  if (st.warp == 0 && st.n > 0)
+    for (unsigned m = st.n > S::stages ? st.n - S::stages : 0; m < st.n; ++m) {
+      const bool there = mbarrier_wait(st.empty + 8 * (m % S::stages), (m / S::stages) & 1u, st.ok ? kHalfPolls : 1000u);
+      if (!there) (void)mbarrier_wait(st.full + 8 * (m % S::stages), (m / S::stages) & 1u, st.ok ? kHalfPolls : 1000u);
+    }
+  __syncthreads();
+  if (threadIdx.x == 0 && failed) atomicOr(a.status, 1u);
+  if (st.warp == 1) {
+    tcgen05_fence_after();
+    tmem_free(st.tmem, S::columns);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
 // Host side.
 
 constexpr size_t kMostSide = SSGD_ORTHOGONAL_MAX_SIDE;
@@ -762,7 +977,14 @@ struct Buffers {
   float *d, *squares;
 };
 
-template <int TO, typename T, int TERMS>
+// Three terms, deflated: boxes and stages leave room for tiles of 128 columns.
+template <int TERMS, bool DEFLATED>
+constexpr unsigned kMostColumns = TERMS == 3 && DEFLATED ? 128 : 256;
+// Shorter side up to which three-term steps are deflated too: what the tensor cores cut off of the sums along X counts for more there
+// (130 x 130: 3.4e-6 of the result, deflated 6e-7, in fp32 1.5e-6; 512 x 512 1.7e-6, fp32 2.3e-6).
+constexpr size_t kDeflatedSide = 255;
+
+template <int TO, typename T, int TERMS, bool DEFLATED>
 ssgd_status launch_update(const Problem& p, const Layout& l, const Buffers& b, int now, unsigned* count, int sms, cudaStream_t s) {
   const Whole& x = b.x[now];
   const HalfOperand whole = {x.high, x.low, x.ld, x.stride, false}, square = {b.m.high, b.m.low, b.m.ld, b.m.stride, false};
@@ -778,14 +1000,14 @@ ssgd_status launch_update(const Problem& p, const Layout& l, const Buffers& b, i
     h.p = whole;
     h.q = square;
   }
-  const HalfForm form = half_form(h, TERMS, 1, sms);
+  const HalfForm form = half_form(h, TERMS, 1, sms, kMostColumns<TERMS, DEFLATED>);
   const unsigned slots = form.pairs ? 16 : 8;                  // epilogue warps of a tile
   *count = slots * (unsigned)half_tiles(h, form.pairs ? 256 : 128, form.nt);
-  typename UpdateEpilogue<TO, T, TERMS == 3>::Args a = {};
+  typename UpdateEpilogue<TO, T, TERMS == 3, DEFLATED>::Args a = {};
   a.x = b.x_parts[now]; a.next = b.x_parts[1 - now]; a.d = b.d; a.squares = b.squares;
   a.out = static_cast<T*>(p.out); a.ldo = p.ldo; a.out_stride = p.out_stride;
   a.f = p.f; a.delta = p.delta; a.rows = (unsigned)p.rows; a.count = *count; a.slots = slots;
-  using Epilogue = UpdateEpilogue<TO, T, TERMS == 3>;
+  using Epilogue = UpdateEpilogue<TO, T, TERMS == 3, DEFLATED>;
   constexpr int chunk = TERMS == 3 ? kChunk : 0;
   return h.q.by_rows ? launch_half<Epilogue, TERMS, chunk, kQByRows>(h, a, form, 1, sms, s) : launch_half<Epilogue, TERMS, chunk, kBothByK>(h, a, form, 1, sms, s);
 }
@@ -793,12 +1015,23 @@ ssgd_status launch_update(const Problem& p, const Layout& l, const Buffers& b, i
 // The largest |b / 2 c| that is added to A's diagonal: A + that, times 2^13, is an fp16 number, and little of A is lost beside it.
 constexpr float kMostShift = 4.0f;
 
-template <int TERMS>
+// b A + c A^2 + a I from the square of A + by I, or, where that is too far from A, of A.
+struct Shift { float by, diagonal; bool shifted; };
+inline Shift shift_of(const Polynomial& f) {
+  const float by = f.b / (2.0f * f.c);
+  if (f.c == 0.0f || !(fabsf(by) <= kMostShift)) return {0.0f, kScale * f.a, false};
+  return {by, kScale * (f.a - f.b * by * 0.5f), true};
+}
+
+template <int TERMS, bool DEFLATED>
 ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, int sms, cudaStream_t s) {
+  using Gram = GramEpilogue<TERMS == 3, DEFLATED>;
+  using Poly = PolynomialEpilogue<TERMS == 3, DEFLATED>;
+  constexpr int chunk = TERMS == 3 ? kChunk : 0;
+  constexpr unsigned most = kMostColumns<TERMS, DEFLATED>;
   unsigned count = 0;
   int now = 0;
-  const float shift = p.f.b / (2.0f * p.f.c);
-  const bool shifted = TERMS == 3 && p.f.c != 0.0f && fabsf(shift) <= kMostShift;
+  const Shift shift = shift_of(p.f);            // not deflated
   for (unsigned k = 0; k < p.steps; ++k) {
     const Whole& x = b.x[now];
     HalfProduct h = {};
@@ -810,24 +1043,22 @@ ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, i
     h.symmetric = true;
     h.status = p.status;
     h.starve = p.starve;
-    const typename GramEpilogue<TERMS == 3>::Args gram = {b.e_parts, k ? b.squares : nullptr, b.d, count, (unsigned)l.side, shifted ? shift : 0.0f};
-    constexpr int chunk = TERMS == 3 ? kChunk : 0;
-    const HalfForm form = half_form(h, TERMS, 1, sms);
-    ssgd_status st = h.p.by_rows ? launch_half<GramEpilogue<TERMS == 3>, TERMS, chunk, kBothByRows>(h, gram, form, 1, sms, s)
-                                 : launch_half<GramEpilogue<TERMS == 3>, TERMS, chunk, kBothByK>(h, gram, form, 1, sms, s);
+    const typename Gram::Args gram = {b.e_parts, k ? b.squares : nullptr, b.d, count, (unsigned)l.side, shift.by};
+    const HalfForm form = half_form(h, TERMS, 1, sms, most);
+    ssgd_status st = h.p.by_rows ? launch_half<Gram, TERMS, chunk, kBothByRows>(h, gram, form, 1, sms, s)
+                                 : launch_half<Gram, TERMS, chunk, kBothByK>(h, gram, form, 1, sms, s);
     if (st != SSGD_OK) return st;
     h.p = {b.e.high, b.e.low, b.e.ld, b.e.stride, false};
     h.q = h.p;
     h.K = l.side;
-    const typename PolynomialEpilogue<TERMS == 3>::Args polynomial = {
-        b.e_parts, b.m_parts, b.d, p.f, kScale * (shifted ? p.f.a - p.f.b * shift * 0.5f : p.f.a), shifted};
-    st = launch_half<PolynomialEpilogue<TERMS == 3>, TERMS, chunk, kBothByK>(h, polynomial, half_form(h, TERMS, 1, sms), 1, sms, s);
+    const typename Poly::Args polynomial = {b.e_parts, b.m_parts, b.d, p.f, shift.diagonal, shift.shifted};
+    st = launch_half<Poly, TERMS, chunk, kBothByK>(h, polynomial, half_form(h, TERMS, 1, sms, most), 1, sms, s);
     if (st != SSGD_OK) return st;
-    if (k + 1 < p.steps) st = launch_update<kNextStep, float, TERMS>(p, l, b, now, &count, sms, s);
-    else if (p.momentum) st = launch_update<kParameters, float, TERMS>(p, l, b, now, &count, sms, s);
-    else if (p.out_type == SSGD_F32) st = launch_update<kOut, float, TERMS>(p, l, b, now, &count, sms, s);
-    else if (p.out_type == SSGD_BF16) st = launch_update<kOut, __nv_bfloat16, TERMS>(p, l, b, now, &count, sms, s);
-    else st = launch_update<kOut, __half, TERMS>(p, l, b, now, &count, sms, s);
+    if (k + 1 < p.steps) st = launch_update<kNextStep, float, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
+    else if (p.momentum) st = launch_update<kParameters, float, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
+    else if (p.out_type == SSGD_F32) st = launch_update<kOut, float, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
+    else if (p.out_type == SSGD_BF16) st = launch_update<kOut, __nv_bfloat16, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
+    else st = launch_update<kOut, __half, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
     if (st != SSGD_OK) return st;
     now = 1 - now;
   }
@@ -836,6 +1067,95 @@ ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, i
 
 inline bool parts_of(Parts* parts, const Whole& w, size_t rows, size_t cols, size_t n) {
   return box_map(&parts->high, w.high, false, rows, cols, w.ld, n, w.stride) && box_map(&parts->low, w.low, false, rows, cols, w.ld, n, w.stride);
+}
+
+// A cluster for each matrix, where that is faster; the clocks of one step either way.  By launches: each product its own, and 5000 for the gap
+// between two.  By a cluster: tiles of 128 x 64 in rounds, 1000 a stage and 4500 beside (a trip through L2, the epilogue, the barrier); clusters
+// of 16 are there 6 times, of 8 12 times.  0: launches.
+inline unsigned cluster_ctas(const Problem& p, const Layout& l, int sms) {
+  const size_t s = l.side, other = p.rows > p.cols ? p.rows : p.cols;
+  HalfProduct h = {};
+  h.P = h.Q = s;
+  h.K = other;
+  h.batch = p.n;
+  h.symmetric = true;
+  const unsigned long long square_tiles = half_tiles(h, 128, 64);
+  unsigned long long launches = 3 * 5000ull, least = 0;
+  (void)half_form(h, p.terms, 1, sms, 256, &least);
+  launches += least;
+  h.K = s;
+  (void)half_form(h, p.terms, 1, sms, 256, &least);
+  launches += least;
+  h.P = p.rows; h.Q = p.cols; h.symmetric = false;
+  (void)half_form(h, p.terms, 1, sms, 256, &least);
+  launches += least;
+  const unsigned long long tiles = half_tiles(h, 128, 64), most = tiles > square_tiles ? tiles : square_tiles;
+  const unsigned ctas = most <= 2 ? 2 : most <= 4 ? 4 : most <= 8 ? 8 : 16, at_once = ctas == 16 ? 6 : 96 / ctas;
+  const unsigned long long square_rounds = (square_tiles + ctas - 1) / ctas, rounds = (tiles + ctas - 1) / ctas;
+  const unsigned long long stages = (other + 63) / 64, stages_s = (s + 63) / 64;
+  const unsigned long long cluster = (square_rounds * (stages + stages_s) + rounds * stages_s) * 1000 + 3 * 4500;
+  return cluster * ((p.n + at_once - 1) / at_once) < launches ? ctas : 0;
+}
+
+template <bool TALL, int TO, typename T>
+ssgd_status launch_cluster(const Problem& p, const Layout& l, const Buffers& b, unsigned ctas, cudaStream_t s) {
+  using S = ClusterShape;
+  ClusterArgs<TO, T> a = {};
+  auto operand = [&](CUtensorMap* maps, const Whole& w, size_t rows, size_t cols) {
+    const HalfOperand o = {w.high, w.low, w.ld, w.stride, false};
+    return half_map(&maps[0], w.high, false, o, rows, cols, p.n, 64) && half_map(&maps[1], w.low, false, o, rows, cols, p.n, 64);
+  };
+  if (!operand(a.x[0], b.x[0], p.rows, p.cols) || !operand(a.x[1], b.x[1], p.rows, p.cols) || !operand(a.e, b.e, l.side, l.side) ||
+      !operand(a.m, b.m, l.side, l.side))
+    return SSGD_ERR_CUDA;
+  const unsigned count = 8 * (unsigned)(((p.rows + 127) / 128) * ((p.cols + 63) / 64));
+  a.gram[0] = {b.e_parts, nullptr, b.d, count, (unsigned)l.side, 0.0f};
+  a.gram[1] = {b.e_parts, b.squares, b.d, count, (unsigned)l.side, 0.0f};
+  a.polynomial = {b.e_parts, b.m_parts, b.d, p.f, 0.0f, 0};
+  for (int i = 0; i < 2; ++i) {
+    a.next[i].x = b.x_parts[i];
+    a.next[i].next = b.x_parts[1 - i];
+    a.next[i].d = b.d; a.next[i].squares = b.squares; a.next[i].f = p.f;
+    a.next[i].rows = (unsigned)p.rows; a.next[i].count = count; a.next[i].slots = 8;
+  }
+  a.last.x = b.x_parts[(p.steps - 1) & 1u]; a.last.d = b.d; a.last.f = p.f;
+  a.last.out = static_cast<T*>(p.out); a.last.ldo = p.ldo; a.last.out_stride = p.out_stride;
+  a.last.delta = p.delta; a.last.rows = (unsigned)p.rows;
+  a.rows = (unsigned)p.rows; a.cols = (unsigned)p.cols; a.steps = p.steps; a.starve = p.starve; a.status = p.status;
+  auto kernel = orthogonal_cluster_kernel<TALL, TO, T>;
+  static unsigned long long seen = 0, seen_wide = 0;
+  if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kHalfThreads);
+  cfg.dynamicSmemBytes = S::smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ctas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cfg.gridDim = dim3((unsigned)p.n * ctas);
+  if (ctas > 8 && !allow_wide_clusters(reinterpret_cast<const void*>(kernel), cfg, &seen_wide)) {
+    attr[1].val.clusterDim.x = ctas = 8;
+    cfg.gridDim = dim3((unsigned)p.n * ctas);
+  }
+  (void)cudaLaunchKernelEx(&cfg, kernel, a);
+  return launch_status();
+}
+template <int TO, typename T>
+ssgd_status launch_cluster_any(const Problem& p, const Layout& l, const Buffers& b, unsigned ctas, cudaStream_t s) {
+  return p.rows > p.cols ? launch_cluster<true, TO, T>(p, l, b, ctas, s) : launch_cluster<false, TO, T>(p, l, b, ctas, s);
+}
+ssgd_status by_cluster(const Problem& p, const Layout& l, const Buffers& b, unsigned ctas, cudaStream_t s) {
+  if (p.momentum) return launch_cluster_any<kParameters, float>(p, l, b, ctas, s);
+  switch (p.out_type) {
+    case SSGD_F32: return launch_cluster_any<kOut, float>(p, l, b, ctas, s);
+    case SSGD_BF16: return launch_cluster_any<kOut, __nv_bfloat16>(p, l, b, ctas, s);
+    default: return launch_cluster_any<kOut, __half>(p, l, b, ctas, s);
+  }
 }
 
 inline bool fours_of(const void* p, size_t element, size_t ld, size_t stride, size_t n) {
@@ -894,7 +1214,9 @@ ssgd_status solve(Problem p, const float* coefficients, cudaStream_t s) {
   b.squares = reinterpret_cast<float*>(p.ws + l.squares);
   const ssgd_status st = p.momentum ? launch_source_typed<kMomentum>(p, l, b.x[0], s) : launch_source_typed<kPlainSource>(p, l, b.x[0], s);
   if (st != SSGD_OK) return st;
-  return p.terms == 3 ? newton_schulz<3>(p, l, b, info.sms, s) : newton_schulz<1>(p, l, b, info.sms, s);
+  if (const unsigned ctas = cluster_ctas(p, l, info.sms)) return by_cluster(p, l, b, ctas, s);
+  if (p.terms == 1) return newton_schulz<1, true>(p, l, b, info.sms, s);
+  return l.side <= kDeflatedSide ? newton_schulz<3, true>(p, l, b, info.sms, s) : newton_schulz<3, false>(p, l, b, info.sms, s);
 }
 
 ssgd_status checked_orthogonalise(const void* u, int u_type, size_t n, size_t rows, size_t cols, size_t ldu, size_t stride_u, const float* coefficients,
