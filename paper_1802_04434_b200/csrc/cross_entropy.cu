@@ -100,6 +100,101 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(m, a.y * exp2_fast((a.x - base) * kLog2e) + b.y * exp2_fast((b.x - base) * kLog2e));
 }
 
+// A few tokens: the weight's bytes are all that counts, and a warp takes four rows of it at a time against tokens that lie in shared memory,
+// in fp32.  (Whole forward passes over 30522 x 1024 on B200, this kernel / tiles of tensor-core products: one token 12.5 / 22.7 us, two 15.1 /
+// 22.7, four 20.9 / 22.7, so up to two; more registers and conversions per byte from there on.)
+constexpr unsigned kFewRows = 4, kFewWarps = 8;
+constexpr size_t kFewSmem = 98304;
+
+template <unsigned TOKENS, typename T>
+__global__ void __launch_bounds__(32 * kFewWarps, 2)
+xent_few_kernel(const T* __restrict__ h, size_t ldh, const T* __restrict__ w, size_t ldw, unsigned tokens, unsigned vocab, unsigned width,
+                const int64_t* __restrict__ targets, float2* __restrict__ partial, float* __restrict__ picked) {
+  // [token][half of eight][piece of 128][lane's four]: lanes read 16 bytes side by side
+  extern __shared__ float few_smem[];
+  __shared__ float2 parts[kFewWarps][kFewRows * TOKENS];
+  pdl_launch_dependents();
+  pdl_wait();
+  const unsigned warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, pieces = (width + 255) / 256;
+  for (unsigned i = threadIdx.x; i < TOKENS * pieces * 256; i += 32 * kFewWarps) {
+    const unsigned t = i / (pieces * 256), c = i % (pieces * 256);
+    few_smem[((t * 2 + (c >> 2 & 1u)) * pieces + (c >> 8)) * 128 + (c >> 3 & 31u) * 4 + (c & 3u)] = t < tokens && c < width ? to_float(h[(size_t)t * ldh + c]) : 0.0f;
+  }
+  __syncthreads();
+
+  // lane r * TOKENS + t keeps the running maximum and sum of the rows r of token t
+  const unsigned my_row = lane / TOKENS, my_token = lane % TOKENS;
+  const bool keeps = lane < kFewRows * TOKENS && my_token < tokens;
+  const int64_t target = keeps ? targets[my_token] : -1;
+  float top = -kInf, sum = 0.0f;
+  for (unsigned row0 = (blockIdx.x * kFewWarps + warp) * kFewRows; row0 < vocab; row0 += gridDim.x * kFewWarps * kFewRows) {
+    float z[kFewRows][TOKENS];
+#pragma unroll
+    for (unsigned r = 0; r < kFewRows; ++r)
+#pragma unroll
+      for (unsigned t = 0; t < TOKENS; ++t) z[r][t] = 0.0f;
+#pragma unroll 2
+    for (unsigned p = 0; p < pieces; ++p) {
+      const unsigned c = p * 256 + lane * 8;
+      uint4 q[kFewRows];
+#pragma unroll
+      for (unsigned r = 0; r < kFewRows; ++r)
+        q[r] = c < width && row0 + r < vocab ? __ldg(reinterpret_cast<const uint4*>(w + (size_t)(row0 + r) * ldw + c)) : make_uint4(0, 0, 0, 0);
+      if (c < width && c + 8 > width) {           // what lies behind the last column may be anything
+        const unsigned left = width - c;
+#pragma unroll
+        for (unsigned r = 0; r < kFewRows; ++r) {
+          unsigned* words = &q[r].x;
+#pragma unroll
+          for (unsigned k = 0; k < 4; ++k) words[k] = 2 * k + 1 < left ? words[k] : 2 * k < left ? words[k] & 0xFFFFu : 0u;
+        }
+      }
+#pragma unroll
+      for (unsigned t = 0; t < TOKENS; ++t) {
+        const float4 a = *reinterpret_cast<const float4*>(few_smem + ((t * 2) * pieces + p) * 128 + lane * 4);
+        const float4 b = *reinterpret_cast<const float4*>(few_smem + ((t * 2 + 1) * pieces + p) * 128 + lane * 4);
+#pragma unroll
+        for (unsigned r = 0; r < kFewRows; ++r) {
+          float s = z[r][t];
+          s = fmaf(low_to_float(T(), q[r].x), a.x, s);
+          s = fmaf(high_to_float(T(), q[r].x), a.y, s);
+          s = fmaf(low_to_float(T(), q[r].y), a.z, s);
+          s = fmaf(high_to_float(T(), q[r].y), a.w, s);
+          s = fmaf(low_to_float(T(), q[r].z), b.x, s);
+          s = fmaf(high_to_float(T(), q[r].z), b.y, s);
+          s = fmaf(low_to_float(T(), q[r].w), b.z, s);
+          z[r][t] = fmaf(high_to_float(T(), q[r].w), b.w, s);
+        }
+      }
+    }
+    float mine = 0.0f;
+#pragma unroll
+    for (unsigned r = 0; r < kFewRows; ++r)
+#pragma unroll
+      for (unsigned t = 0; t < TOKENS; ++t) {
+        float s = z[r][t];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        mine = lane == r * TOKENS + t ? s : mine;
+      }
+    if (keeps && row0 + my_row < vocab) {
+      if (target == (int64_t)(row0 + my_row)) picked[my_token] = mine;
+      const float2 both = join(make_float2(top, sum), make_float2(mine, 1.0f));
+      top = both.x;
+      sum = both.y;
+    }
+  }
+  if (lane < kFewRows * TOKENS) parts[warp][lane] = make_float2(top, sum);
+  __syncthreads();
+  if (threadIdx.x < TOKENS && threadIdx.x < tokens) {
+    float2 all = make_float2(-kInf, 0.0f);
+    for (unsigned k = 0; k < kFewWarps; ++k)
+#pragma unroll
+      for (unsigned r = 0; r < kFewRows; ++r) all = join(all, parts[k][r * TOKENS + threadIdx.x]);
+    partial[(size_t)blockIdx.x * tokens + threadIdx.x] = all;
+  }
+}
+
 // Joins the parts of TOKENS tokens a CTA (1 or 32), its other threads side by side along the parts; then the losses, and a look at the
 // ignored tokens' rows of h: one that is not finite must not reach dw through 0 * inf.
 template <unsigned TOKENS, typename T>
@@ -362,6 +457,8 @@ struct WeightEpilogue {
 constexpr size_t kSide = (size_t)1 << 30;
 inline size_t up(size_t n, size_t k) { return (n + k - 1) / k * k; }
 
+constexpr size_t kFewTokens = 2, kFewCtas = 2;      // see xent_few_kernel; CTAs of an SM
+
 struct HeadSizes {
   size_t parts;                             // most partial statistics of a token: two for each 64 columns
   size_t forward_bytes;
@@ -375,6 +472,7 @@ constexpr size_t kPieceElements = (size_t)1 << 27;
 inline bool head_sizes(size_t T, size_t V, size_t D, int sms, HeadSizes* s) {
   if (T < 1 || V < 1 || D < 1 || T > kSide || V > kSide || D > kSide || T > ((size_t)1 << 44) / V || T > ((size_t)1 << 44) / D) return false;
   s->parts = 2 * ((V + 63) / 64);
+  if (T <= kFewTokens && s->parts < kFewCtas * (size_t)sms) s->parts = kFewCtas * (size_t)sms;
   s->forward_bytes = up(T * 4, 16) + s->parts * T * sizeof(float2);
   const size_t columns = up(V, 256);
   s->piece = up(kPieceElements / T < 256 ? 256 : kPieceElements / T / 256 * 256, 256);
@@ -410,20 +508,34 @@ ssgd_status check_head(const void* h, size_t ldh, const void* w, size_t ldw, int
 template <typename T>
 ssgd_status head_forward(const T* h, size_t ldh, const T* w, size_t ldw, size_t tokens, size_t vocab, size_t width, const int64_t* targets, int64_t ignore,
                          float* losses, float* lse, uint8_t* kinds, void* ws, unsigned* status, unsigned starve, int sms, cudaStream_t s) {
-  HalfProduct p = {};
-  p.p = {h, nullptr, ldh, 0, false};
-  p.q = {w, nullptr, ldw, 0, false};
-  p.P = tokens; p.Q = vocab; p.K = width; p.batch = 1;
-  p.bf16 = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value;
-  p.status = status;
-  p.starve = starve;
-  const HalfForm form = half_form(p, 1, 1, sms);
   float* picked = static_cast<float*>(ws);
   float2* partial = reinterpret_cast<float2*>(static_cast<char*>(ws) + up(tokens * 4, 16));
-  const StatsEpilogue::Args args = {targets, partial, picked, (unsigned)tokens};
-  const ssgd_status st = launch_half<StatsEpilogue, 1, 4, kBothByK>(p, args, form, 1, sms, s);
-  if (st != SSGD_OK) return st;
-  const unsigned parts = 2 * (unsigned)((vocab + form.nt - 1) / form.nt);
+  unsigned parts;
+  const size_t few = tokens < kFewTokens ? 1 : kFewTokens, few_smem = few * ((width + 255) / 256) * 256 * 4;
+  if (tokens <= kFewTokens && few_smem <= kFewSmem && starve == 0) {
+    const size_t groups = (vocab + kFewWarps * kFewRows - 1) / (kFewWarps * kFewRows), most = kFewCtas * (size_t)sms;
+    parts = (unsigned)(groups < most ? groups : most);
+    auto kernel = few == 1 ? xent_few_kernel<1, T> : xent_few_kernel<2, T>;
+    static unsigned long long seen[2] = {0, 0};
+    if (!allow_smem(reinterpret_cast<const void*>(kernel), kFewSmem, &seen[few - 1])) return SSGD_ERR_CUDA;
+    launch_kernel(kernel, dim3(parts), dim3(32 * kFewWarps), few_smem, s, true, h, ldh, w, ldw, (unsigned)tokens, (unsigned)vocab, (unsigned)width, targets,
+                  partial, picked);
+    const ssgd_status st = launch_status();
+    if (st != SSGD_OK) return st;
+  } else {
+    HalfProduct p = {};
+    p.p = {h, nullptr, ldh, 0, false};
+    p.q = {w, nullptr, ldw, 0, false};
+    p.P = tokens; p.Q = vocab; p.K = width; p.batch = 1;
+    p.bf16 = std::is_same<T, __nv_bfloat16>::value;
+    p.status = status;
+    p.starve = starve;
+    const HalfForm form = half_form(p, 1, 1, sms);
+    const StatsEpilogue::Args args = {targets, partial, picked, (unsigned)tokens};
+    const ssgd_status st = launch_half<StatsEpilogue, 1, 4, kBothByK>(p, args, form, 1, sms, s);
+    if (st != SSGD_OK) return st;
+    parts = 2 * (unsigned)((vocab + form.nt - 1) / form.nt);
+  }
   if (tokens <= 512)
     launch_kernel(xent_join_kernel<1, T>, dim3((unsigned)tokens), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
                   (unsigned)vocab, h, ldh, (unsigned)width, losses, lse, kinds);

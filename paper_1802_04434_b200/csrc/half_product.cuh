@@ -684,10 +684,12 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
   HalfMaps maps;
   HalfOperand q1 = h.q;
   if (h.q_other) q1.high = h.q_other, q1.ld = h.q_other_ld;
-  if (!half_map(&maps.p[0], h.p.high, h.bf16, h.p, h.P, h.K, h.batch, p.p_box) || !half_map(&maps.q[0], h.q.high, h.bf16, h.q, h.Q, h.K, h.batch, S::q_rows) ||
-      !half_map(&maps.p[1], TERMS == 3 ? h.p.low : h.p.high, h.bf16, h.p, h.P, h.K, h.batch, p.p_box) ||
-      !half_map(&maps.q[1], TERMS == 3 ? q1.low : q1.high, h.bf16, q1, h.Q, h.K, h.batch, S::q_rows))
+  if (!half_map(&maps.p[0], h.p.high, h.bf16, h.p, h.P, h.K, h.batch, p.p_box) || !half_map(&maps.q[0], h.q.high, h.bf16, h.q, h.Q, h.K, h.batch, S::q_rows))
     return SSGD_ERR_CUDA;
+  maps.p[1] = maps.p[0];
+  maps.q[1] = maps.q[0];
+  if (TERMS == 3 && !half_map(&maps.p[1], h.p.low, h.bf16, h.p, h.P, h.K, h.batch, p.p_box)) return SSGD_ERR_CUDA;
+  if ((TERMS == 3 || h.q_other) && !half_map(&maps.q[1], TERMS == 3 ? q1.low : q1.high, h.bf16, q1, h.Q, h.K, h.batch, S::q_rows)) return SSGD_ERR_CUDA;
   auto kernel = half_product_kernel<Epilogue, PAIR, NT, TERMS, CHUNK, LAYOUT, SPLIT>;
   static unsigned long long seen = 0;
   if (!allow_smem(reinterpret_cast<const void*>(kernel), S::smem, &seen)) return SSGD_ERR_CUDA;

@@ -301,38 +301,69 @@ __device__ __forceinline__ void source_load(const T* p, unsigned left, bool four
   }
 }
 
-// U at four columns of a row; FIRST: m is brought forward and written.
+// U at four columns of a row, in two halves, so that several can be on their way; FIRST: m is brought forward and written.
+struct Fetched { float m[4], g[4]; };
 template <int KIND, bool FIRST, typename T>
-__device__ __forceinline__ void source_values(const Source& s, size_t matrix, unsigned row, unsigned column, float (&u)[4]) {
+__device__ __forceinline__ void source_fetch(const Source& s, size_t matrix, unsigned row, unsigned column, Fetched& f) {
   const unsigned left = s.cols - column;
+  if (KIND == kMomentum) source_load(s.m + matrix * s.m_stride + (size_t)row * s.ldm + column, left, s.fours, f.m);
+  if (KIND == kPlainSource || FIRST || s.ahead) source_load(static_cast<const T*>(s.u) + matrix * s.u_stride + (size_t)row * s.ldu + column, left, s.fours, f.g);
+}
+template <int KIND, bool FIRST>
+__device__ __forceinline__ void source_values(const Source& s, size_t matrix, unsigned row, unsigned column, Fetched& f, float (&u)[4]) {
   if constexpr (KIND == kPlainSource) {
-    source_load(static_cast<const T*>(s.u) + matrix * s.u_stride + (size_t)row * s.ldu + column, left, s.fours, u);
-  } else {
-    float* mp = s.m + matrix * s.m_stride + (size_t)row * s.ldm + column;
-    float m[4], g[4];
-    source_load(mp, left, s.fours, m);
-    if (FIRST || s.ahead) {
-      source_load(static_cast<const T*>(s.u) + matrix * s.u_stride + (size_t)row * s.ldu + column, left, s.fours, g);
 #pragma unroll
-      for (unsigned i = 0; i < 4; ++i) g[i] = __fmul_rn(1.0f - s.beta, g[i]);
+    for (unsigned i = 0; i < 4; ++i) u[i] = f.g[i];
+  } else {
+    if (FIRST || s.ahead) {
+#pragma unroll
+      for (unsigned i = 0; i < 4; ++i) f.g[i] = __fmul_rn(1.0f - s.beta, f.g[i]);
     }
     if (FIRST) {
+      float* mp = s.m + matrix * s.m_stride + (size_t)row * s.ldm + column;
+      const unsigned left = s.cols - column;
 #pragma unroll
-      for (unsigned i = 0; i < 4; ++i) m[i] = __fmaf_rn(s.beta, m[i], g[i]);
+      for (unsigned i = 0; i < 4; ++i) f.m[i] = __fmaf_rn(s.beta, f.m[i], f.g[i]);
       if (s.fours && left >= 4) {
-        *reinterpret_cast<float4*>(mp) = make_float4(m[0], m[1], m[2], m[3]);
+        *reinterpret_cast<float4*>(mp) = make_float4(f.m[0], f.m[1], f.m[2], f.m[3]);
       } else {
 #pragma unroll
         for (unsigned i = 0; i < 4; ++i)
-          if (i < left) mp[i] = m[i];
+          if (i < left) mp[i] = f.m[i];
       }
     }
 #pragma unroll
-    for (unsigned i = 0; i < 4; ++i) u[i] = s.ahead ? __fmaf_rn(s.beta, m[i], g[i]) : m[i];
+    for (unsigned i = 0; i < 4; ++i) u[i] = s.ahead ? __fmaf_rn(s.beta, f.m[i], f.g[i]) : f.m[i];
   }
 }
 
-constexpr unsigned kNormThreads = 256;
+constexpr unsigned kNormThreads = 256, kNormBatch = 4;
+
+// f(row, column, U's four values) for this CTA's share of a matrix, kNormBatch loads of each array in flight.  What lies behind a row's last
+// column is zero.
+template <int KIND, bool FIRST, typename T, typename F>
+__device__ __forceinline__ void each_four(const Source& s, size_t matrix, F f) {
+  const unsigned fours = (s.cols + 3) / 4, total = fours * s.rows, step = gridDim.x * kNormThreads;
+  for (unsigned i0 = blockIdx.x * kNormThreads + threadIdx.x; i0 < total; i0 += kNormBatch * step) {
+    Fetched v[kNormBatch];
+    unsigned row[kNormBatch];
+#pragma unroll
+    for (unsigned b = 0; b < kNormBatch; ++b) {
+      const unsigned i = i0 + b * step;
+      row[b] = i / fours;
+      if (i < total) source_fetch<KIND, FIRST, T>(s, matrix, row[b], (i - row[b] * fours) * 4, v[b]);
+    }
+#pragma unroll
+    for (unsigned b = 0; b < kNormBatch; ++b) {
+      const unsigned i = i0 + b * step;
+      if (i >= total) break;
+      const unsigned column = (i - row[b] * fours) * 4;
+      float u[4];
+      source_values<KIND, FIRST>(s, matrix, row[b], column, v[b], u);
+      f(row[b], column, u);
+    }
+  }
+}
 
 template <int KIND, typename T>
 __global__ void __launch_bounds__(kNormThreads)
@@ -340,15 +371,12 @@ orthogonal_norm_kernel(const Source s, double* __restrict__ partial) {
   __shared__ double part[kNormThreads / 32];
   pdl_launch_dependents();
   pdl_wait();
-  const unsigned fours = (s.cols + 3) / 4, total = fours * s.rows;
   double sum = 0.0;
-  for (unsigned i = blockIdx.x * kNormThreads + threadIdx.x; i < total; i += gridDim.x * kNormThreads) {
-    float u[4];
-    source_values<KIND, true, T>(s, blockIdx.y, i / fours, i % fours * 4, u);
+  each_four<KIND, true, T>(s, blockIdx.y, [&](unsigned, unsigned column, const float (&u)[4]) {
 #pragma unroll
     for (unsigned k = 0; k < 4; ++k)
-      if (i % fours * 4 + k < s.cols) sum = fma((double)u[k], (double)u[k], sum);
-  }
+      if (column + k < s.cols) sum = fma((double)u[k], (double)u[k], sum);
+  });
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
   if ((threadIdx.x & 31u) == 0) part[threadIdx.x >> 5] = sum;
@@ -384,22 +412,15 @@ orthogonal_split_kernel(const Source s, const double* __restrict__ partial, unsi
   }
   __syncthreads();
   const Inverse inverse = inverse_of(sqrt(norm2), kScale);
-  const unsigned fours = (s.cols + 3) / 4, total = fours * s.rows;
-  for (unsigned i = blockIdx.x * kNormThreads + threadIdx.x; i < total; i += gridDim.x * kNormThreads) {
-    const unsigned row = i / fours, column = i % fours * 4;
-    float u[4];
-    source_values<KIND, false, T>(s, blockIdx.y, row, column, u);
-    float h[4], l[4];
+  each_four<KIND, false, T>(s, blockIdx.y, [&](unsigned row, unsigned column, const float (&u)[4]) {
+    unsigned high[2], low[2];
 #pragma unroll
-    for (unsigned k = 0; k < 4; ++k) {
-      const float v = u[k] * inverse.first * inverse.rest;
-      h[k] = __half2float(__float2half_rn(v));
-      l[k] = v - h[k];
-    }
+    for (unsigned k = 0; k < 2; ++k)
+      split_pair(u[2 * k] * inverse.first * inverse.rest, u[2 * k + 1] * inverse.first * inverse.rest, high[k], low[k]);
     const size_t at = blockIdx.y * x.stride + (size_t)row * x.ld + column;
-    *reinterpret_cast<uint2*>(x.high + at) = make_uint2(pack2(__half(), h[0], h[1]), pack2(__half(), h[2], h[3]));
-    *reinterpret_cast<uint2*>(x.low + at) = make_uint2(pack2(__half(), l[0], l[1]), pack2(__half(), l[2], l[3]));
-  }
+    *reinterpret_cast<uint2*>(x.high + at) = make_uint2(high[0], high[1]);
+    *reinterpret_cast<uint2*>(x.low + at) = make_uint2(low[0], low[1]);
+  });
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -713,18 +734,17 @@ struct ClusterState {
 };
 
 // One product, tile after tile by the CTAs of the cluster in turn.
-template <int LAYOUT, bool SYMMETRIC, class Epilogue>
-__device__ __forceinline__ void cluster_product(ClusterState& st, const CUtensorMap* p_maps, const CUtensorMap* q_maps, unsigned P, unsigned Q, unsigned K,
+template <int LAYOUT, class Epilogue>
+__device__ __forceinline__ void cluster_product(ClusterState& st, bool symmetric, const CUtensorMap* p_maps, const CUtensorMap* q_maps, unsigned P, unsigned Q, unsigned K,
                                                 Epilogue& epilogue, const typename Epilogue::Args& args) {
   using S = ClusterShape;
   constexpr unsigned low = (S::p_bytes + S::q_bytes) >> 4;
   const unsigned tiles_p = (P + 127) / 128, tiles_q = (Q + 63) / 64, stages = (K + 63) / 64, chunks = (K + 15) / 16;
-  // f(first row, first column, whether it is the first tile) for this CTA's tiles, along the rows of tiles, in a symmetric product from the
-  // diagonal on
+  // f(first row, first column) for this CTA's tiles, along the rows of tiles, in a symmetric product from the diagonal on
   auto each_tile = [&](auto f) {
     unsigned tile = st.rank;
     for (unsigned i = 0; i < tiles_p && st.ok; ++i) {
-      const unsigned begin = SYMMETRIC ? 2 * i : 0, count = tiles_q > begin ? tiles_q - begin : 0;
+      const unsigned begin = symmetric ? 2 * i : 0, count = tiles_q > begin ? tiles_q - begin : 0;
       for (; tile < count && st.ok; tile += st.size) f(i * 128, (begin + tile) * 64);
       tile -= min(tile, count);
     }
@@ -777,7 +797,7 @@ __device__ __forceinline__ void cluster_product(ClusterState& st, const CUtensor
     epilogue.box.phase = st.phase;
     each_tile([&](unsigned p0, unsigned q0) {
       const unsigned row0 = p0 + quarter * 32, column = q0 + odd * 32;
-      const HalfPlace at = {st.matrix, 0, p0, q0, p0 / 128 * tiles_q + q0 / 64, 0, 128};
+      const HalfPlace at = {st.matrix, 0, p0, q0, p0 / 128 * tiles_q + q0 / 64, 0, symmetric ? 128u : 1u << 30};      // no tile lies wholly above the diagonal: nothing is mirrored
       epilogue.begin(args, at, row0, odd);
       const bool inside = row0 < P && column < Q;
       if (inside) epilogue.ahead(args, column);
@@ -857,6 +877,9 @@ orthogonal_cluster_kernel(const __grid_constant__ ClusterArgs<TO, T> a) {
   st.tmem = tmem_base;
 
   const unsigned side = TALL ? a.cols : a.rows, other = TALL ? a.rows : a.cols, w = st.warp >= 4 ? st.warp - 4 : 0;
+  // half of the tiles of a square, mirrored, where that saves a round
+  const unsigned squares = (side + 127) / 128 * ((side + 63) / 64);
+  const bool symmetric = squares > st.size;
   const Box box(st.stage0 + S::stages * S::stage_bytes + w * S::box_bytes, box_full + 16 * w, st.lane);
   GramEpilogue<true, true> gram(a.gram[0], box);
   PolynomialEpilogue<true, true> polynomial(a.polynomial, box);
@@ -874,16 +897,16 @@ orthogonal_cluster_kernel(const __grid_constant__ ClusterArgs<TO, T> a) {
   for (unsigned k = 0; k < a.steps; ++k) {
     const CUtensorMap* x = a.x[k & 1u];
     gram.seen = ~0u;                            // another step, another d
-    cluster_product<TALL ? kBothByRows : kBothByK, true>(st, x, x, side, side, other, gram, a.gram[k > 0]);
+    cluster_product<TALL ? kBothByRows : kBothByK>(st, symmetric, x, x, side, side, other, gram, a.gram[k > 0]);
     between();
-    cluster_product<kBothByK, true>(st, a.e, a.e, side, side, side, polynomial, a.polynomial);
+    cluster_product<kBothByK>(st, symmetric, a.e, a.e, side, side, side, polynomial, a.polynomial);
     between();
     if (k + 1 < a.steps) {
-      if (TALL) cluster_product<kBothByK, false>(st, x, a.m, a.rows, a.cols, side, next, a.next[k & 1u]);
-      else cluster_product<kQByRows, false>(st, a.m, x, a.rows, a.cols, side, next, a.next[k & 1u]);
+      if (TALL) cluster_product<kBothByK>(st, false, x, a.m, a.rows, a.cols, side, next, a.next[k & 1u]);
+      else cluster_product<kQByRows>(st, false, a.m, x, a.rows, a.cols, side, next, a.next[k & 1u]);
     } else {
-      if (TALL) cluster_product<kBothByK, false>(st, x, a.m, a.rows, a.cols, side, last, a.last);
-      else cluster_product<kQByRows, false>(st, a.m, x, a.rows, a.cols, side, last, a.last);
+      if (TALL) cluster_product<kBothByK>(st, false, x, a.m, a.rows, a.cols, side, last, a.last);
+      else cluster_product<kQByRows>(st, false, a.m, x, a.rows, a.cols, side, last, a.last);
     }
     between();
   }
