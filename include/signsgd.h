@@ -520,6 +520,7 @@ ssgd_status ssgd_xent_wait_selftest(const void* h, size_t ldh, const void* w, si
  *   X = U / |U|_F (0 for U = 0);  `steps` times  X <- a X + (b A + c A^2) X  with A = X X^T
  * for n matrices of rows x cols at a time.  A matrix that holds a NaN or an infinity becomes NaN.  The coefficients should keep the
  * singular values below 4, and |b t + c t^2| below 8 for their squares t: beyond that the result is not finite or not right.
+ * Elements of X are kept to 2^-38: singular values that coefficients take down to that size are lost.
  *   products   3: products of operands in two fp16 parts, 22 bits: as exact as products in fp32
  *              1: operands of 11 bits, sums in fp32: the result is off by about 10^-3 of its norm (less than bf16's rounding of it
  *                 for a side of 256 and more; up to 4 * 10^-3 for small matrices of low rank)

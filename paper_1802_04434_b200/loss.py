@@ -164,7 +164,9 @@ class _CrossEntropy(torch.autograd.Function):
 
 def cross_entropy(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100, reduction: str = "mean") -> torch.Tensor:
     """The losses of `cross_entropy_forward` for torch's autograd, h [..., width] and targets [...]: "none" as they are, "sum", or "mean"
-    over the tokens that are not ignored (0 where all are).  First derivatives only."""
+    over the tokens that are not ignored (0 where all are).  First derivatives only.  To capture gradients into a CUDA graph while an eager
+    graph of the same leaves lives, take leaves of the capture's own (`x.detach().requires_grad_()`): torch ties a leaf to the
+    stream of its living graph."""
     if reduction not in ("none", "sum", "mean"):
         raise ValueError("reduction must be 'none', 'sum' or 'mean', got %r" % (reduction,))
     if h.dim() < 1 or h.shape[:-1] != targets.shape:

@@ -55,8 +55,13 @@ def _batch(t: torch.Tensor, name: str, written: bool) -> Tuple[torch.Tensor, int
     return t, n, stride[-2] if rows > 1 else cols, stride[0] if n > 1 else rows * cols
 
 
-def _coefficients(c) -> Tuple[float, float, float]:
-    a, b, c = c
+def _options(steps, coefficients, products) -> Tuple[float, float, float]:
+    """The coefficients as floats; the options have been looked at."""
+    if not 1 <= steps <= 100:
+        raise ValueError("steps must be 1 to 100, got %r" % (steps,))
+    if products not in (1, 3):
+        raise ValueError("products must be 1 or 3, got %r" % (products,))
+    a, b, c = coefficients
     return float(a), float(b), float(c)
 
 
@@ -83,10 +88,11 @@ def orthogonalise(u: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS, dt
     rows, cols = us.shape[-2:]
     if products is None:
         products = 1 if out_code == 1 and min(rows, cols) >= ONE_PRODUCT_SIDE else 3
+    abc = _options(steps, coefficients, products)
     if n and rows and cols:
         work = torch.empty(_ws_bytes(n, rows, cols), dtype=torch.uint8, device=device)
         status = B.lib().ssgd_orthogonalise_block(_pack_orthogonalise(
-            us.data_ptr(), code, n, rows, cols, ldu, su, *_coefficients(coefficients), steps, products, os.data_ptr(), out_code, ldo, so,
+            us.data_ptr(), code, n, rows, cols, ldu, su, *abc, steps, products, os.data_ptr(), out_code, ldo, so,
             work.data_ptr(), status_of(device)[1], _stream_of(index)))
         if status:
             B._check(status, "ssgd_orthogonalise")
@@ -114,12 +120,13 @@ def momentum_step(x: torch.Tensor, g: torch.Tensor, m: torch.Tensor, beta: float
     ms, _, ldm, sm = _batch(m, "m", True)
     gs, _, ldg, sg = _batch(g, "g", False)
     rows, cols = xs.shape[-2:]
+    abc = _options(steps, coefficients, products)
     if n and rows and cols:
         if len({xs.data_ptr(), ms.data_ptr(), gs.data_ptr()}) < 3:
             raise ValueError("x, g and m must not share memory")
         work = torch.empty(_ws_bytes(n, rows, cols), dtype=torch.uint8, device=device)
         status = B.lib().ssgd_orthogonal_step_block(_pack_step(
             xs.data_ptr(), ldx, sx, gs.data_ptr(), code, ldg, sg, ms.data_ptr(), ldm, sm, n, rows, cols, beta, delta, 1 if nesterov else 0,
-            *_coefficients(coefficients), steps, products, work.data_ptr(), status_of(device)[1], _stream_of(index)))
+            *abc, steps, products, work.data_ptr(), status_of(device)[1], _stream_of(index)))
         if status:
             B._check(status, "ssgd_orthogonal_step")
