@@ -491,6 +491,11 @@ ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t*
  * D, V >= 1 and sides up to 2^30; T * V and T * D up to 2^44.                                                       */
 ssgd_status ssgd_xent_sizes(size_t T, size_t V, size_t D, size_t* forward_bytes, size_t* backward_bytes);
 
+/* Rows that start elsewhere: two matrices of 16-bit elements (either may have no rows), [rows][cols] at strides of ld and step elements, to
+ * rows of ldo elements (a multiple of 8, >= cols), zeros behind the last column.  to_a, to_b: DEVICE, 16-byte aligned.      */
+ssgd_status ssgd_xent_align(const void* a, size_t lda, size_t step_a, size_t rows_a, void* to_a, const void* b, size_t ldb,
+                            size_t step_b, size_t rows_b, void* to_b, size_t cols, size_t ldo, void* stream);
+
 /*   losses, lse  out DEVICE float [T];  lse: log sum exp, for the backward pass
  *   kinds        out DEVICE uint8 [T], for the backward pass: 0, or 1 for an ignored token, 2 where its row of h is not finite */
 ssgd_status ssgd_xent_forward(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V,
@@ -560,6 +565,7 @@ ssgd_status ssgd_tensors_clip_block(const uint64_t* args);    /* 9 words  */
 ssgd_status ssgd_fp4_quantise_block(const uint64_t* args);    /* 13 words */
 ssgd_status ssgd_fp4_dequantise_block(const uint64_t* args);  /* 10 words */
 ssgd_status ssgd_fp4_matmul_block(const uint64_t* args);      /* 15 words */
+ssgd_status ssgd_xent_align_block(const uint64_t* args);      /* 13 words */
 ssgd_status ssgd_xent_forward_block(const uint64_t* args);    /* 16 words */
 ssgd_status ssgd_xent_backward_block(const uint64_t* args);   /* 21 words */
 ssgd_status ssgd_orthogonalise_block(const uint64_t* args);   /* 19 words: the coefficients as three floats */

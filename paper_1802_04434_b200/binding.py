@@ -101,6 +101,8 @@ def lib() -> ctypes.CDLL:
         "ssgd_orthogonalise": [vp, ci, sz, sz, sz, sz, sz, vp, u32, ci, vp, ci, sz, sz, vp, vp, vp],
         "ssgd_orthogonal_wait_selftest": [vp, ci, sz, sz, vp, ci, vp, ci, vp, vp, vp],
         "ssgd_orthogonal_step": [vp, sz, sz, vp, ci, sz, sz, vp, sz, sz, sz, sz, sz, f32, f32, ci, vp, u32, ci, vp, vp, vp],
+        "ssgd_xent_align": [vp, sz, sz, sz, vp, vp, sz, sz, sz, vp, sz, sz, vp],
+        "ssgd_xent_align_block": [ctypes.c_char_p],
         "ssgd_xent_forward_block": [ctypes.c_char_p],
         "ssgd_xent_backward_block": [ctypes.c_char_p],
         "ssgd_orthogonalise_block": [ctypes.c_char_p],
@@ -637,6 +639,7 @@ def fp4_matmul(a_codes: torch.Tensor, a_scales: torch.Tensor, a_tensor_scale: Op
 # --------------------------------------------------------------------------
 # the loss over a large vocabulary; orthogonalised updates (``loss`` and ``orthogonal`` call these with torch tensors)
 
+XENT_ALIGN_ARGS = struct.Struct("=13Q")
 XENT_FORWARD_ARGS, XENT_BACKWARD_ARGS = struct.Struct("=9Qq6Q"), struct.Struct("=21Q")
 ORTHOGONALISE_ARGS, ORTHOGONAL_STEP_ARGS = struct.Struct("=7Q3d9Q"), struct.Struct("=13Q2dQ3d5Q")
 

@@ -451,6 +451,31 @@ struct WeightEpilogue {
   __device__ __forceinline__ void finish(const Args&) {}
 };
 
+// Rows of 16-bit elements at any place and strides to rows that asynchronous copies can read, of two matrices in one launch: eight elements
+// a thread, zeros behind the last column.
+struct Scattered {
+  const uint16_t* from;
+  uint16_t* to;
+  size_t ld, step, rows;
+};
+__global__ void __launch_bounds__(256)
+xent_align_kernel(const Scattered a, const Scattered b, unsigned cols, size_t ldo) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const unsigned pieces = (unsigned)(ldo / 8);
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, all = i / pieces;
+  const unsigned c = (unsigned)(i - all * pieces) * 8;
+  if (all >= a.rows + b.rows) return;
+  const bool second = all >= a.rows;
+  const Scattered& m = second ? b : a;
+  const size_t row = second ? all - a.rows : all;
+  const uint16_t* from = m.from + row * m.ld + c * m.step;
+  unsigned v[8];
+#pragma unroll
+  for (unsigned k = 0; k < 8; ++k) v[k] = c + k < cols ? from[k * m.step] : 0u;
+  *reinterpret_cast<uint4*>(m.to + row * ldo + c) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+}
+
 // ---------------------------------------------------------------------------------------------------------------------
 // Host side.
 
@@ -660,6 +685,20 @@ ssgd_status ssgd_xent_sizes(size_t T, size_t V, size_t D, size_t* forward_bytes,
   return SSGD_OK;
 }
 
+ssgd_status ssgd_xent_align(const void* a, size_t lda, size_t step_a, size_t rows_a, void* to_a, const void* b, size_t ldb, size_t step_b, size_t rows_b,
+                            void* to_b, size_t cols, size_t ldo, void* stream) {
+  if (cols < 1 || cols > kSide || ldo < cols || ldo > 2 * kSide || rows_a > kSide || rows_b > kSide) return SSGD_ERR_SIZE;
+  if ((rows_a && (!a || !to_a)) || (rows_b && (!b || !to_b))) return SSGD_ERR_NULL;
+  if (ldo % 8 != 0 || !aligned16(to_a) || !aligned16(to_b) || ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 1u)) return SSGD_ERR_ALIGN;
+  const size_t blocks = ((rows_a + rows_b) * (ldo / 8) + 255) / 256;
+  if (blocks > kMaxGrid) return SSGD_ERR_SIZE;
+  if (blocks == 0) return SSGD_OK;
+  const Scattered sa = {static_cast<const uint16_t*>(a), static_cast<uint16_t*>(to_a), lda, step_a, rows_a},
+                  sb = {static_cast<const uint16_t*>(b), static_cast<uint16_t*>(to_b), ldb, step_b, rows_b};
+  launch_kernel(xent_align_kernel, dim3((unsigned)blocks), dim3(256), 0, static_cast<cudaStream_t>(stream), true, sa, sb, (unsigned)cols, ldo);
+  return launch_status();
+}
+
 ssgd_status ssgd_xent_forward(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V, size_t D, const int64_t* targets,
                               int64_t ignore, float* losses, float* lse, uint8_t* kinds, void* ws, unsigned* status, void* stream) {
   return checked_forward(h, ldh, w, ldw, dtype, T, V, D, targets, ignore, losses, lse, kinds, ws, status, 0, stream);
@@ -706,6 +745,12 @@ ssgd_status ssgd_xent_backward_block(const uint64_t* a) {
   return ssgd_xent_backward(block_ptr<const void>(a[0]), a[1], block_ptr<const void>(a[2]), a[3], (int)a[4], a[5], a[6], a[7], block_ptr<const int64_t>(a[8]),
                             block_ptr<const float>(a[9]), block_ptr<const uint8_t>(a[10]), block_ptr<const float>(a[11]), a[12], block_ptr<void>(a[13]), a[14],
                             block_ptr<void>(a[15]), (int)a[16], a[17], block_ptr<void>(a[18]), block_ptr<unsigned>(a[19]), block_ptr<void>(a[20]));
+}
+
+ssgd_status ssgd_xent_align_block(const uint64_t* a) {
+  if (!a) return SSGD_ERR_NULL;
+  return ssgd_xent_align(block_ptr<const void>(a[0]), a[1], a[2], a[3], block_ptr<void>(a[4]), block_ptr<const void>(a[5]), a[6], a[7], a[8],
+                         block_ptr<void>(a[9]), a[10], a[11], block_ptr<void>(a[12]));
 }
 
 }  // extern "C"

@@ -62,31 +62,28 @@ struct Box {
       store_shared16(place16(offset, lane, q), pack2(T(), v[8 * q], v[8 * q + 1]), pack2(T(), v[8 * q + 2], v[8 * q + 3]), pack2(T(), v[8 * q + 4], v[8 * q + 5]),
                      pack2(T(), v[8 * q + 6], v[8 * q + 7]));
   }
-  // High and low part, the latter 2048 bytes behind.
-  __device__ __forceinline__ void put_parts(unsigned offset, const float* v) const {
+  // One of the two parts of what this thread has, high or low.
+  template <bool LOW_PART>
+  __device__ __forceinline__ void put_part(unsigned offset, const float* v) const {
 #pragma unroll
     for (unsigned q = 0; q < 4; ++q) {
       unsigned h[4], l[4];
 #pragma unroll
       for (unsigned i = 0; i < 4; ++i) split_pair(v[8 * q + 2 * i], v[8 * q + 2 * i + 1], h[i], l[i]);
-      store_shared16(place16(offset, lane, q), h[0], h[1], h[2], h[3]);
-      store_shared16(place16(offset + 2048, lane, q), l[0], l[1], l[2], l[3]);
+      if (LOW_PART) store_shared16(place16(offset, lane, q), l[0], l[1], l[2], l[3]);
+      else store_shared16(place16(offset, lane, q), h[0], h[1], h[2], h[3]);
     }
   }
   // Transposed: this thread's row is a column of the box.
-  template <bool PARTS>
-  __device__ __forceinline__ void put_across(unsigned offset, const float* v) const {
+  template <bool LOW_PART>
+  __device__ __forceinline__ void put_part_across(unsigned offset, const float* v) const {
 #pragma unroll
     for (unsigned q = 0; q < 32; q += 2) {
       unsigned h, l;
       split_pair(v[q], v[q + 1], h, l);
-      const unsigned at0 = place16(offset, q, lane >> 3) + (lane & 7u) * 2, at1 = place16(offset, q + 1, lane >> 3) + (lane & 7u) * 2;
-      store_shared2(at0, h);
-      store_shared2(at1, h >> 16);
-      if (PARTS) {
-        store_shared2(at0 + 2048, l);
-        store_shared2(at1 + 2048, l >> 16);
-      }
+      const unsigned w = LOW_PART ? l : h;
+      store_shared2(place16(offset, q, lane >> 3) + (lane & 7u) * 2, w);
+      store_shared2(place16(offset, q + 1, lane >> 3) + (lane & 7u) * 2, w >> 16);
     }
   }
   __device__ __forceinline__ void get8(unsigned offset, unsigned piece, float (&v)[8]) const {

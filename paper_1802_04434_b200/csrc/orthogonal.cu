@@ -28,26 +28,29 @@ __device__ __forceinline__ void prefetch_parts(const Parts& p) {
   prefetch_tensor_map(&p.low);
 }
 
-// 32 x 32 elements of a symmetric matrix: there, and, from tiles wholly above the diagonal, mirrored.  Tiles on the diagonal hold
-// both halves themselves.
+// 32 x 32 elements as high and, LOW, low part.  What goes out takes the halves of a box in turn: one is written while the other is read.
+template <bool LOW, bool ACROSS>
+__device__ __forceinline__ void send_parts(const Box& box, unsigned offset, const Parts& to, unsigned x, unsigned y, unsigned matrix, const float* v) {
+  box.sent_but_last();
+  if (ACROSS) box.put_part_across<false>(offset, v);
+  else box.put_part<false>(offset, v);
+  box.fence();
+  box.send(to.high, offset, x, y, matrix);
+  if (LOW) {
+    box.sent_but_last();
+    if (ACROSS) box.put_part_across<true>(offset + 2048, v);
+    else box.put_part<true>(offset + 2048, v);
+    box.fence();
+    box.send(to.low, offset + 2048, x, y, matrix);
+  }
+}
+// The same of a symmetric matrix: there, and, from tiles wholly above the diagonal, mirrored.  Tiles on the diagonal hold both halves
+// themselves.
 template <bool LOW>
 __device__ __forceinline__ void send_symmetric(const Box& box, unsigned offset, const Parts& to, unsigned row0, unsigned column, unsigned matrix, bool mirrored,
                                                const float* v) {
-  box.sent();
-  if (LOW) box.put_parts(offset, v);
-  else box.put16<__half>(offset, v);
-  if (!LOW && mirrored) box.put_across<false>(offset + 2048, v);
-  box.fence();
-  box.send(to.high, offset, column, row0, matrix);
-  if (LOW) box.send(to.low, offset + 2048, column, row0, matrix);
-  if (!mirrored) return;
-  if (LOW) {
-    box.sent();
-    box.put_across<true>(offset, v);
-    box.fence();
-    box.send(to.low, offset + 2048, row0, column, matrix);
-  }
-  box.send(to.high, LOW ? offset : offset + 2048, row0, column, matrix);
+  send_parts<LOW, false>(box, offset, to, column, row0, matrix, v);
+  if (mirrored) send_parts<LOW, true>(box, LOW ? offset : offset ^ 2048, to, row0, column, matrix, v);
 }
 
 // The product X X^T.  DEFLATED: E = A - d I, where d comes from the sums of squares that the last step left, added in a fixed order by each
@@ -65,9 +68,9 @@ struct GramEpilogue {
   static __device__ __forceinline__ void prefetch(const Args& a) { prefetch_parts(a.e); }
   Box box;
   float diagonal;               // what is added there
-  unsigned row0, seen, matrix;
+  unsigned row0, seen, matrix, half;
   bool mirrored;
-  __device__ __forceinline__ GramEpilogue(const Args& a, const Box& b) : box(b), diagonal(a.shift * kScale), seen(~0u) {}
+  __device__ __forceinline__ GramEpilogue(const Args& a, const Box& b) : box(b), diagonal(a.shift * kScale), seen(~0u), half(0) {}
   __device__ __forceinline__ void ahead(const Args&, unsigned) {}
   __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
     row0 = first_row;
@@ -96,7 +99,8 @@ struct GramEpilogue {
 #pragma unroll
       for (unsigned q = 0; q < 32; ++q) v[q] = on == q ? v[q] + diagonal : v[q];
     }
-    send_symmetric<LOW>(box, 0, a.e, row0, column, matrix, mirrored, v);
+    send_symmetric<LOW>(box, half, a.e, row0, column, matrix, mirrored, v);
+    if (!LOW && !mirrored) half ^= 2048;        // an odd number has gone out
   }
   __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
   __device__ __forceinline__ void finish(const Args&) { box.finish(); }
@@ -226,7 +230,6 @@ struct UpdateEpilogue {
     if (!DEFLATED) {
 #pragma unroll
       for (unsigned i = 0; i < 32; ++i) v[i] *= kUnscale;
-      if (TO == kNextStep) box.sent();
     } else {
       const unsigned b = takes++ & 1u;
       from = b * 4096;
@@ -246,10 +249,7 @@ struct UpdateEpilogue {
 #pragma unroll
         for (unsigned i = 0; i < 32; ++i) sum = fmaf(v[i], v[i], sum);
       }
-      box.put_parts(from, v);
-      box.fence();
-      box.send(a.next.high, from, column, row0, matrix);
-      box.send(a.next.low, from + 2048, column, row0, matrix);
+      send_parts<true, false>(box, from, a.next, column, row0, matrix, v);
     } else {
       const float by = TO == kOut ? kUnscale : -a.delta * kUnscale;
 #pragma unroll

@@ -17,7 +17,7 @@ from .waits import check, status_of  # noqa: F401  (check: part of this module)
 
 _DTYPES = B._Codes({torch.bfloat16: 1, torch.float16: 2}, TypeError, "h and w must be of dtype bfloat16 or float16")
 _stream_of, _current_device = B._stream_of, B._current_device
-_pack_forward, _pack_backward = B.XENT_FORWARD_ARGS.pack, B.XENT_BACKWARD_ARGS.pack
+_pack_align, _pack_forward, _pack_backward = B.XENT_ALIGN_ARGS.pack, B.XENT_FORWARD_ARGS.pack, B.XENT_BACKWARD_ARGS.pack
 
 
 @functools.lru_cache(maxsize=256)
@@ -26,20 +26,30 @@ def _sizes(index: int, tokens: int, vocab: int, width: int) -> Tuple[int, int]:
     return B.xent_sizes(tokens, vocab, width)
 
 
-def _aligned_rows(t: torch.Tensor) -> Tuple[torch.Tensor, int]:
-    """A matrix whose rows asynchronous copies can read, and its row stride: the tensor itself where its rows start at multiples of 16
-    bytes, else a copy."""
-    rows, cols = t.shape
+def _stride_as_it_is(t: torch.Tensor, width: int) -> int:
+    """The row stride of a matrix whose rows asynchronous copies can read as they lie, starting at multiples of 16 bytes; else 0."""
     ld, step = t.stride()
-    padded = (cols + 7) // 8 * 8
-    if (step == 1 or cols == 1) and t.data_ptr() % 16 == 0:
-        if rows == 1:
-            return t, padded
-        if ld % 8 == 0 and ld >= cols:
-            return t, ld
-    copy = torch.empty(rows, padded, dtype=t.dtype, device=t.device)
-    copy[:, :cols].copy_(t)
-    return copy, padded
+    if (step == 1 or width == 1) and t.data_ptr() % 16 == 0:
+        if t.shape[0] == 1:
+            return (width + 7) // 8 * 8
+        if ld % 8 == 0 and ld >= width:
+            return ld
+    return 0
+
+
+def _align(h: torch.Tensor, ldh: int, w: torch.Tensor, ldw: int, index: int):
+    """h and w, copied where their stride is given as 0, and their strides."""
+    tokens, width = h.shape
+    vocab = w.shape[0]
+    padded = (width + 7) // 8 * 8
+    rows = 0 if ldh else tokens
+    copy = torch.empty(rows + (0 if ldw else vocab), padded, dtype=h.dtype, device=h.device)
+    at = copy.data_ptr()
+    status = B.lib().ssgd_xent_align_block(_pack_align(
+        h.data_ptr(), *h.stride(), rows, at, w.data_ptr(), *w.stride(), 0 if ldw else vocab, at + 2 * rows * padded, width, padded, _stream_of(index)))
+    if status:
+        B._check(status, "ssgd_xent_align")
+    return h if ldh else copy[:tokens], ldh or padded, w if ldw else copy[rows:], ldw or padded
 
 
 class Kept(NamedTuple):
@@ -75,8 +85,9 @@ def cross_entropy_forward(h: torch.Tensor, w: torch.Tensor, targets: torch.Tenso
     if index != _current_device():
         with B._on(index):
             return cross_entropy_forward(h, w, targets, ignore_index)
-    hs, ldh = _aligned_rows(h)
-    ws, ldw = _aligned_rows(w)
+    ldh, ldw = _stride_as_it_is(h, width), _stride_as_it_is(w, width)
+    if tokens and not (ldh and ldw):
+        h, ldh, w, ldw = _align(h, ldh, w, ldw, index)
     if not targets.is_contiguous():
         targets = targets.contiguous()
     losses = torch.empty(tokens, dtype=torch.float32, device=device)
@@ -85,11 +96,11 @@ def cross_entropy_forward(h: torch.Tensor, w: torch.Tensor, targets: torch.Tenso
         work = torch.empty(_sizes(index, tokens, vocab, width)[0], dtype=torch.uint8, device=device)
         at = state.data_ptr()
         status = B.lib().ssgd_xent_forward_block(_pack_forward(
-            hs.data_ptr(), ldh, ws.data_ptr(), ldw, code, tokens, vocab, width, targets.data_ptr(), ignore_index, losses.data_ptr(), at,
+            h.data_ptr(), ldh, w.data_ptr(), ldw, code, tokens, vocab, width, targets.data_ptr(), ignore_index, losses.data_ptr(), at,
             at + 4 * tokens, work.data_ptr(), status_of(device)[1], _stream_of(index)))
         if status:
             B._check(status, "ssgd_xent_forward")
-    return losses, Kept(hs, ws, targets, state, (ldh, ldw), (tokens, vocab, width))
+    return losses, Kept(h, w, targets, state, (ldh, ldw), (tokens, vocab, width))
 
 
 def cross_entropy_backward(kept: Kept, g: torch.Tensor, dw: Optional[torch.Tensor] = None, dw_dtype: Optional[torch.dtype] = None,

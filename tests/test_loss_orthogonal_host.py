@@ -191,11 +191,19 @@ def test_batches_of_matrices():
 
 
 def test_rows_that_copies_can_read():
-    from paper_1802_04434_b200.loss import _aligned_rows
+    from paper_1802_04434_b200.loss import _stride_as_it_is
     whole = torch.arange(7 * 32, dtype=torch.float16).view(7, 32)
-    for t, same in ((whole, True), (whole[:, 8:20], True), (whole[::2], True), (whole[:, 1:9], False), (whole[:, :30][1:2], True), (whole.t(), False),
-                    (torch.zeros(7, 9, dtype=torch.float16), False), (torch.zeros(9, 1, dtype=torch.float16), False), (whole[:, ::2], False)):
-        r, ld = _aligned_rows(t)
-        assert ld % 8 == 0 and r.data_ptr() % 16 == 0 and (r.data_ptr() == t.data_ptr()) == same
-        rows, cols = t.shape
-        assert torch.equal(r.as_strided((rows, cols), (ld if rows > 1 else 0, 1)), t)
+    for t, ld in ((whole, 32), (whole[:, 8:20], 32), (whole[::2], 64), (whole[:, 1:9], 0), (whole[:, :30][1:2], 32), (whole.t(), 0), (whole[:1, :30].t(), 0),
+                  (torch.zeros(7, 9, dtype=torch.float16), 0), (torch.zeros(9, 1, dtype=torch.float16), 0), (whole[:, ::2], 0), (whole[:1, :9], 16),
+                  (whole[:1].expand(5, 32), 0)):
+        assert _stride_as_it_is(t, t.shape[1]) == ld
+
+
+def test_align_refusals(B):
+    def align(**change):
+        a = dict(a=A + 2, lda=5, step_a=1, rows_a=3, to_a=A, b=A, ldb=1, step_b=9, rows_b=4, to_b=A, cols=5, ldo=8, stream=None)
+        a.update(change)
+        return B.lib().ssgd_xent_align(*a.values())
+    for change, status in ((dict(a=None), NULL), (dict(to_b=None), NULL), (dict(a=A + 1), ALIGN), (dict(to_a=A + 8), ALIGN), (dict(ldo=12), ALIGN), (dict(ldo=0), SIZE),
+                           (dict(cols=0), SIZE), (dict(rows_b=(1 << 30) + 1), SIZE), (dict(rows_a=0, rows_b=0), OK), (dict(rows_a=0, rows_b=0, a=None, b=None), OK)):
+        assert align(**change) == status
