@@ -195,7 +195,7 @@ xent_few_kernel(const T* __restrict__ h, size_t ldh, const T* __restrict__ w, si
   }
 }
 
-// Joins the parts of TOKENS tokens a CTA (1 or 32), its other threads side by side along the parts; then the losses, and a look at the
+// Joins the parts of TOKENS tokens a CTA (1 or 8), its other threads side by side along the parts; then the losses, and a look at the
 // ignored tokens' rows of h: one that is not finite must not reach dw through 0 * inf.
 template <unsigned TOKENS, typename T>
 __global__ void __launch_bounds__(256)
@@ -203,7 +203,7 @@ xent_join_kernel(const float2* __restrict__ partial, const float* __restrict__ p
                  unsigned parts, unsigned vocab, const T* __restrict__ h, size_t ldh, unsigned width, float* __restrict__ losses, float* __restrict__ lse,
                  uint8_t* __restrict__ kinds) {
   constexpr unsigned kSlices = 256 / TOKENS;
-  __shared__ float2 part[8][TOKENS];
+  __shared__ float2 part[TOKENS == 1 ? 8 : kSlices][TOKENS];
   pdl_launch_dependents();
   pdl_wait();
   const unsigned i = threadIdx.x % TOKENS, slice = threadIdx.x / TOKENS, t0 = blockIdx.x * TOKENS, t = t0 + i;
@@ -236,7 +236,7 @@ xent_join_kernel(const float2* __restrict__ partial, const float* __restrict__ p
   if (mine) {
     sum = part[0][i];
 #pragma unroll
-    for (unsigned k = 1; k < 8; ++k) sum = join(sum, part[k][i]);
+    for (unsigned k = 1; k < (TOKENS == 1 ? 8 : kSlices); ++k) sum = join(sum, part[k][i]);
     const bool ignored = y == ignore, inside = y >= 0 && y < (int64_t)vocab;
     // a target that is neither ignored nor in the vocabulary: NaN, here and in the gradients
     const float log_sum = logf(sum.y), l = inside || ignored ? sum.x + log_sum : __uint_as_float(0x7FC00000u);
@@ -482,6 +482,8 @@ xent_align_kernel(const Scattered a, const Scattered b, unsigned cols, size_t ld
 constexpr size_t kSide = (size_t)1 << 30;
 inline size_t up(size_t n, size_t k) { return (n + k - 1) / k * k; }
 
+// Stages between two times that a logit's sum is taken (each takes the threads 1500 clocks of 256 columns; four: 102 us for 2048 x 30522 x 1024).
+constexpr int kSumStages = 8;
 constexpr size_t kFewTokens = 2, kFewCtas = 2;      // see xent_few_kernel; CTAs of an SM
 
 struct HeadSizes {
@@ -503,11 +505,22 @@ inline bool head_sizes(size_t T, size_t V, size_t D, int sms, HeadSizes* s) {
   s->piece = up(kPieceElements / T < 256 ? 256 : kPieceElements / T / 256 * 256, 256);
   if (s->piece > columns) s->piece = columns;
   s->pieces = (V + s->piece - 1) / s->piece;
-  // few tiles of dh and a long k: split it, four stages or more each
-  const size_t tiles = (T + 127) / 128 * ((D + 63) / 64), stages = (V + 63) / 64;
-  size_t splits = s->pieces > 1 || tiles * 2 > (size_t)sms ? 1 : (size_t)sms / tiles;
-  if (splits > stages / 4) splits = stages / 4 < 1 ? 1 : stages / 4;
-  s->splits = (unsigned)splits;
+  // dh has few tiles and a long k: split k, where that is faster, by what the products take and the planes of sums take to be added (22
+  // bytes of HBM a clock and SM, a launch)
+  HalfProduct dh = {};
+  dh.P = T; dh.Q = D; dh.K = V; dh.batch = 1;
+  s->splits = 1;
+  unsigned long long least = 0;
+  (void)half_form(dh, 1, 1, sms, 256, &least);
+  for (unsigned splits = 2; splits <= 16 && s->pieces == 1 && V >= 256 * (size_t)splits && splits * T * D <= kPieceElements; ++splits) {
+    unsigned long long clocks = 0;
+    (void)half_form(dh, 1, splits, sms, 256, &clocks);
+    clocks += 8000 + 2 * splits * T * D * 4 / (22 * (size_t)sms);
+    if (clocks < least) {
+      least = clocks;
+      s->splits = splits;
+    }
+  }
   size_t at = 0;
   s->prepared = at; at += 64;
   s->copy = at; s->copy_ld = up(D, 8); at += up(T * s->copy_ld * 2, 128);
@@ -557,7 +570,7 @@ ssgd_status head_forward(const T* h, size_t ldh, const T* w, size_t ldw, size_t 
     p.starve = starve;
     const HalfForm form = half_form(p, 1, 1, sms);
     const StatsEpilogue::Args args = {targets, partial, picked, (unsigned)tokens};
-    const ssgd_status st = launch_half<StatsEpilogue, 1, 4, kBothByK>(p, args, form, 1, sms, s);
+    const ssgd_status st = launch_half<StatsEpilogue, 1, kSumStages, kBothByK>(p, args, form, 1, sms, s);
     if (st != SSGD_OK) return st;
     parts = 2 * (unsigned)((vocab + form.nt - 1) / form.nt);
   }
@@ -565,7 +578,7 @@ ssgd_status head_forward(const T* h, size_t ldh, const T* w, size_t ldw, size_t 
     launch_kernel(xent_join_kernel<1, T>, dim3((unsigned)tokens), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
                   (unsigned)vocab, h, ldh, (unsigned)width, losses, lse, kinds);
   else
-    launch_kernel(xent_join_kernel<32, T>, dim3((unsigned)(tokens + 31) / 32), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
+    launch_kernel(xent_join_kernel<8, T>, dim3((unsigned)(tokens + 7) / 8), dim3(256), 0, s, true, partial, picked, targets, ignore, (unsigned)tokens, parts,
                   (unsigned)vocab, h, ldh, (unsigned)width, losses, lse, kinds);
   return launch_status();
 }

@@ -62,28 +62,16 @@ struct Box {
       store_shared16(place16(offset, lane, q), pack2(T(), v[8 * q], v[8 * q + 1]), pack2(T(), v[8 * q + 2], v[8 * q + 3]), pack2(T(), v[8 * q + 4], v[8 * q + 5]),
                      pack2(T(), v[8 * q + 6], v[8 * q + 7]));
   }
-  // One of the two parts of what this thread has, high or low.
-  template <bool LOW_PART>
-  __device__ __forceinline__ void put_part(unsigned offset, const float* v) const {
+  // 32 elements of 16 bits, in words: this thread's row, or, transposed, a column of the box.
+  __device__ __forceinline__ void put_words(unsigned offset, const unsigned (&w)[16]) const {
 #pragma unroll
-    for (unsigned q = 0; q < 4; ++q) {
-      unsigned h[4], l[4];
-#pragma unroll
-      for (unsigned i = 0; i < 4; ++i) split_pair(v[8 * q + 2 * i], v[8 * q + 2 * i + 1], h[i], l[i]);
-      if (LOW_PART) store_shared16(place16(offset, lane, q), l[0], l[1], l[2], l[3]);
-      else store_shared16(place16(offset, lane, q), h[0], h[1], h[2], h[3]);
-    }
+    for (unsigned q = 0; q < 4; ++q) store_shared16(place16(offset, lane, q), w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
   }
-  // Transposed: this thread's row is a column of the box.
-  template <bool LOW_PART>
-  __device__ __forceinline__ void put_part_across(unsigned offset, const float* v) const {
+  __device__ __forceinline__ void put_words_across(unsigned offset, const unsigned (&w)[16]) const {
 #pragma unroll
-    for (unsigned q = 0; q < 32; q += 2) {
-      unsigned h, l;
-      split_pair(v[q], v[q + 1], h, l);
-      const unsigned w = LOW_PART ? l : h;
-      store_shared2(place16(offset, q, lane >> 3) + (lane & 7u) * 2, w);
-      store_shared2(place16(offset, q + 1, lane >> 3) + (lane & 7u) * 2, w >> 16);
+    for (unsigned q = 0; q < 16; ++q) {
+      store_shared2(place16(offset, 2 * q, lane >> 3) + (lane & 7u) * 2, w[q]);
+      store_shared2(place16(offset, 2 * q + 1, lane >> 3) + (lane & 7u) * 2, w[q] >> 16);
     }
   }
   __device__ __forceinline__ void get8(unsigned offset, unsigned piece, float (&v)[8]) const {

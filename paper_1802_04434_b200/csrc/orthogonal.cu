@@ -28,18 +28,26 @@ __device__ __forceinline__ void prefetch_parts(const Parts& p) {
   prefetch_tensor_map(&p.low);
 }
 
+// 32 neighbours of a row as two fp16 parts, two elements a word.
+struct Words {
+  unsigned high[16], low[16];
+  __device__ __forceinline__ explicit Words(const float* v) {
+#pragma unroll
+    for (unsigned q = 0; q < 16; ++q) split_pair(v[2 * q], v[2 * q + 1], high[q], low[q]);
+  }
+};
 // 32 x 32 elements as high and, LOW, low part.  What goes out takes the halves of a box in turn: one is written while the other is read.
 template <bool LOW, bool ACROSS>
-__device__ __forceinline__ void send_parts(const Box& box, unsigned offset, const Parts& to, unsigned x, unsigned y, unsigned matrix, const float* v) {
+__device__ __forceinline__ void send_parts(const Box& box, unsigned offset, const Parts& to, unsigned x, unsigned y, unsigned matrix, const Words& w) {
   box.sent_but_last();
-  if (ACROSS) box.put_part_across<false>(offset, v);
-  else box.put_part<false>(offset, v);
+  if (ACROSS) box.put_words_across(offset, w.high);
+  else box.put_words(offset, w.high);
   box.fence();
   box.send(to.high, offset, x, y, matrix);
   if (LOW) {
     box.sent_but_last();
-    if (ACROSS) box.put_part_across<true>(offset + 2048, v);
-    else box.put_part<true>(offset + 2048, v);
+    if (ACROSS) box.put_words_across(offset + 2048, w.low);
+    else box.put_words(offset + 2048, w.low);
     box.fence();
     box.send(to.low, offset + 2048, x, y, matrix);
   }
@@ -49,8 +57,9 @@ __device__ __forceinline__ void send_parts(const Box& box, unsigned offset, cons
 template <bool LOW>
 __device__ __forceinline__ void send_symmetric(const Box& box, unsigned offset, const Parts& to, unsigned row0, unsigned column, unsigned matrix, bool mirrored,
                                                const float* v) {
-  send_parts<LOW, false>(box, offset, to, column, row0, matrix, v);
-  if (mirrored) send_parts<LOW, true>(box, LOW ? offset : offset ^ 2048, to, row0, column, matrix, v);
+  const Words w(v);
+  send_parts<LOW, false>(box, offset, to, column, row0, matrix, w);
+  if (mirrored) send_parts<LOW, true>(box, LOW ? offset : offset ^ 2048, to, row0, column, matrix, w);
 }
 
 // The product X X^T.  DEFLATED: E = A - d I, where d comes from the sums of squares that the last step left, added in a fixed order by each
@@ -249,7 +258,7 @@ struct UpdateEpilogue {
 #pragma unroll
         for (unsigned i = 0; i < 32; ++i) sum = fmaf(v[i], v[i], sum);
       }
-      send_parts<true, false>(box, from, a.next, column, row0, matrix, v);
+      send_parts<true, false>(box, from, a.next, column, row0, matrix, Words(v));
     } else {
       const float by = TO == kOut ? kUnscale : -a.delta * kUnscale;
 #pragma unroll
@@ -286,79 +295,81 @@ struct Source {
   size_t ldu, u_stride, ldm, m_stride;
   float beta;
   unsigned rows, cols;
-  bool ahead, fours;            // fours: every row of u and m starts at a multiple of four elements
+  bool ahead, eights;           // eights: every row of u and m can be read 16 bytes at a time, eight elements from its start on
 };
 enum { kPlainSource, kMomentum };
 
+// Eight elements of a row, `left` of them inside, zeros behind.
 template <typename T>
-__device__ __forceinline__ void source_load(const T* p, unsigned left, bool fours, float (&v)[4]) {
-  if (fours && left >= 4) {
-    const float4 q = load4(p);
-    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+__device__ __forceinline__ void source_load(const T* p, unsigned left, bool eights, float (&v)[8]) {
+  if (eights && left >= 8) {
+    load8(p, v);
   } else {
 #pragma unroll
-    for (unsigned i = 0; i < 4; ++i) v[i] = i < left ? to_float(p[i]) : 0.0f;
+    for (unsigned i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.0f;
   }
 }
 
-// U at four columns of a row, in two halves, so that several can be on their way; FIRST: m is brought forward and written.
-struct Fetched { float m[4], g[4]; };
+// U at eight columns of a row, in two halves, so that several can be on their way; FIRST: m is brought forward and written.
+struct Fetched { float m[8], g[8]; };
 template <int KIND, bool FIRST, typename T>
 __device__ __forceinline__ void source_fetch(const Source& s, size_t matrix, unsigned row, unsigned column, Fetched& f) {
   const unsigned left = s.cols - column;
-  if (KIND == kMomentum) source_load(s.m + matrix * s.m_stride + (size_t)row * s.ldm + column, left, s.fours, f.m);
-  if (KIND == kPlainSource || FIRST || s.ahead) source_load(static_cast<const T*>(s.u) + matrix * s.u_stride + (size_t)row * s.ldu + column, left, s.fours, f.g);
+  if (KIND == kMomentum) source_load(s.m + matrix * s.m_stride + (size_t)row * s.ldm + column, left, s.eights, f.m);
+  if (KIND == kPlainSource || FIRST || s.ahead) source_load(static_cast<const T*>(s.u) + matrix * s.u_stride + (size_t)row * s.ldu + column, left, s.eights, f.g);
 }
 template <int KIND, bool FIRST>
-__device__ __forceinline__ void source_values(const Source& s, size_t matrix, unsigned row, unsigned column, Fetched& f, float (&u)[4]) {
+__device__ __forceinline__ void source_values(const Source& s, size_t matrix, unsigned row, unsigned column, Fetched& f, float (&u)[8]) {
   if constexpr (KIND == kPlainSource) {
 #pragma unroll
-    for (unsigned i = 0; i < 4; ++i) u[i] = f.g[i];
+    for (unsigned i = 0; i < 8; ++i) u[i] = f.g[i];
   } else {
     if (FIRST || s.ahead) {
 #pragma unroll
-      for (unsigned i = 0; i < 4; ++i) f.g[i] = __fmul_rn(1.0f - s.beta, f.g[i]);
+      for (unsigned i = 0; i < 8; ++i) f.g[i] = __fmul_rn(1.0f - s.beta, f.g[i]);
     }
     if (FIRST) {
       float* mp = s.m + matrix * s.m_stride + (size_t)row * s.ldm + column;
       const unsigned left = s.cols - column;
 #pragma unroll
-      for (unsigned i = 0; i < 4; ++i) f.m[i] = __fmaf_rn(s.beta, f.m[i], f.g[i]);
-      if (s.fours && left >= 4) {
+      for (unsigned i = 0; i < 8; ++i) f.m[i] = __fmaf_rn(s.beta, f.m[i], f.g[i]);
+      if (s.eights && left >= 8) {
         *reinterpret_cast<float4*>(mp) = make_float4(f.m[0], f.m[1], f.m[2], f.m[3]);
+        *reinterpret_cast<float4*>(mp + 4) = make_float4(f.m[4], f.m[5], f.m[6], f.m[7]);
       } else {
 #pragma unroll
-        for (unsigned i = 0; i < 4; ++i)
+        for (unsigned i = 0; i < 8; ++i)
           if (i < left) mp[i] = f.m[i];
       }
     }
 #pragma unroll
-    for (unsigned i = 0; i < 4; ++i) u[i] = s.ahead ? __fmaf_rn(s.beta, f.m[i], f.g[i]) : f.m[i];
+    for (unsigned i = 0; i < 8; ++i) u[i] = s.ahead ? __fmaf_rn(s.beta, f.m[i], f.g[i]) : f.m[i];
   }
 }
 
-constexpr unsigned kNormThreads = 256, kNormBatch = 4;
+constexpr unsigned kNormThreads = 256;
 
-// f(row, column, U's four values) for this CTA's share of a matrix, kNormBatch loads of each array in flight.  What lies behind a row's last
+// f(row, column, U's eight values) for this CTA's share of a matrix, BATCH loads of each array in flight.  What lies behind a row's last
 // column is zero.
 template <int KIND, bool FIRST, typename T, typename F>
-__device__ __forceinline__ void each_four(const Source& s, size_t matrix, F f) {
-  const unsigned fours = (s.cols + 3) / 4, total = fours * s.rows, step = gridDim.x * kNormThreads;
-  for (unsigned i0 = blockIdx.x * kNormThreads + threadIdx.x; i0 < total; i0 += kNormBatch * step) {
-    Fetched v[kNormBatch];
-    unsigned row[kNormBatch];
+__device__ __forceinline__ void each_eight(const Source& s, size_t matrix, F f) {
+  constexpr unsigned kBatch = KIND == kMomentum ? 2 : 4;
+  const unsigned eights = (s.cols + 7) / 8, total = eights * s.rows, step = gridDim.x * kNormThreads;
+  for (unsigned i0 = blockIdx.x * kNormThreads + threadIdx.x; i0 < total; i0 += kBatch * step) {
+    Fetched v[kBatch];
+    unsigned row[kBatch];
 #pragma unroll
-    for (unsigned b = 0; b < kNormBatch; ++b) {
+    for (unsigned b = 0; b < kBatch; ++b) {
       const unsigned i = i0 + b * step;
-      row[b] = i / fours;
-      if (i < total) source_fetch<KIND, FIRST, T>(s, matrix, row[b], (i - row[b] * fours) * 4, v[b]);
+      row[b] = i / eights;
+      if (i < total) source_fetch<KIND, FIRST, T>(s, matrix, row[b], (i - row[b] * eights) * 8, v[b]);
     }
 #pragma unroll
-    for (unsigned b = 0; b < kNormBatch; ++b) {
+    for (unsigned b = 0; b < kBatch; ++b) {
       const unsigned i = i0 + b * step;
       if (i >= total) break;
-      const unsigned column = (i - row[b] * fours) * 4;
-      float u[4];
+      const unsigned column = (i - row[b] * eights) * 8;
+      float u[8];
       source_values<KIND, FIRST>(s, matrix, row[b], column, v[b], u);
       f(row[b], column, u);
     }
@@ -372,9 +383,9 @@ orthogonal_norm_kernel(const Source s, double* __restrict__ partial) {
   pdl_launch_dependents();
   pdl_wait();
   double sum = 0.0;
-  each_four<KIND, true, T>(s, blockIdx.y, [&](unsigned, unsigned column, const float (&u)[4]) {
+  each_eight<KIND, true, T>(s, blockIdx.y, [&](unsigned, unsigned column, const float (&u)[8]) {
 #pragma unroll
-    for (unsigned k = 0; k < 4; ++k)
+    for (unsigned k = 0; k < 8; ++k)
       if (column + k < s.cols) sum = fma((double)u[k], (double)u[k], sum);
   });
 #pragma unroll
@@ -412,14 +423,14 @@ orthogonal_split_kernel(const Source s, const double* __restrict__ partial, unsi
   }
   __syncthreads();
   const Inverse inverse = inverse_of(sqrt(norm2), kScale);
-  each_four<KIND, false, T>(s, blockIdx.y, [&](unsigned row, unsigned column, const float (&u)[4]) {
-    unsigned high[2], low[2];
+  each_eight<KIND, false, T>(s, blockIdx.y, [&](unsigned row, unsigned column, const float (&u)[8]) {
+    unsigned high[4], low[4];
 #pragma unroll
-    for (unsigned k = 0; k < 2; ++k)
+    for (unsigned k = 0; k < 4; ++k)
       split_pair(u[2 * k] * inverse.first * inverse.rest, u[2 * k + 1] * inverse.first * inverse.rest, high[k], low[k]);
     const size_t at = blockIdx.y * x.stride + (size_t)row * x.ld + column;
-    *reinterpret_cast<uint2*>(x.high + at) = make_uint2(high[0], high[1]);
-    *reinterpret_cast<uint2*>(x.low + at) = make_uint2(low[0], low[1]);
+    *reinterpret_cast<uint4*>(x.high + at) = make_uint4(high[0], high[1], high[2], high[3]);
+    *reinterpret_cast<uint4*>(x.low + at) = make_uint4(low[0], low[1], low[2], low[3]);
   });
 }
 
@@ -942,9 +953,9 @@ inline bool layout_of(size_t n, size_t rows, size_t cols, Layout* l) {
   l->lds = round_up(l->side, 64);
   l->x_elements = rows * l->ldx;
   l->e_elements = l->side * l->lds;
-  const size_t work = rows * ((cols + 3) / 4);
-  l->norm_parts = (unsigned)((work + 8 * kNormThreads - 1) / (8 * kNormThreads));
-  const unsigned most = n >= 16 ? 64 : 592;             // CTAs of one matrix
+  const size_t work = rows * ((cols + 7) / 8);
+  l->norm_parts = (unsigned)((work + 4 * kNormThreads - 1) / (4 * kNormThreads));
+  const unsigned most = n >= 16 ? 96 : 1184;            // CTAs of one matrix
   if (l->norm_parts > most) l->norm_parts = most;
   l->square_parts = (unsigned)(16 * ((rows + 127) / 128) * ((cols + 63) / 64));
   size_t at = 0;
@@ -1181,8 +1192,9 @@ ssgd_status by_cluster(const Problem& p, const Layout& l, const Buffers& b, unsi
   }
 }
 
-inline bool fours_of(const void* p, size_t element, size_t ld, size_t stride, size_t n) {
-  return reinterpret_cast<uintptr_t>(p) % (4 * element) == 0 && ld % 4 == 0 && (n == 1 || stride % 4 == 0);
+inline bool eights_of(const void* p, size_t element, size_t ld, size_t stride, size_t n) {
+  const size_t of = 16 / element;               // elements of 16 bytes
+  return aligned16(p) && ld % of == 0 && (n == 1 || stride % of == 0);
 }
 
 // One batch of matrices: rows of stride ld, matrices of stride `stride`, in elements of `type`.
@@ -1254,7 +1266,7 @@ ssgd_status checked_orthogonalise(const void* u, int u_type, size_t n, size_t ro
   Problem p = {};
   p.source.u = u; p.source.ldu = ldu; p.source.u_stride = stride_u;
   p.source.rows = (unsigned)rows; p.source.cols = (unsigned)cols;
-  p.source.fours = fours_of(u, dtype_bytes((unsigned)u_type), ldu, stride_u, n);
+  p.source.eights = eights_of(u, dtype_bytes((unsigned)u_type), ldu, stride_u, n);
   p.source_type = u_type;
   p.n = n; p.rows = rows; p.cols = cols; p.steps = steps; p.terms = products;
   p.out = out; p.out_type = out_type; p.ldo = ldo; p.out_stride = stride_o;
@@ -1298,7 +1310,7 @@ ssgd_status ssgd_orthogonal_step(float* x, size_t ldx, size_t stride_x, const vo
   p.source.m = m; p.source.ldm = ldm; p.source.m_stride = stride_m;
   p.source.beta = beta; p.source.ahead = nesterov != 0;
   p.source.rows = (unsigned)rows; p.source.cols = (unsigned)cols;
-  p.source.fours = fours_of(g, dtype_bytes((unsigned)g_type), ldg, stride_g, n) && fours_of(m, 4, ldm, stride_m, n);
+  p.source.eights = eights_of(g, dtype_bytes((unsigned)g_type), ldg, stride_g, n) && eights_of(m, 4, ldm, stride_m, n);
   p.source_type = g_type;
   p.momentum = true;
   p.n = n; p.rows = rows; p.cols = cols; p.steps = steps; p.terms = products;
