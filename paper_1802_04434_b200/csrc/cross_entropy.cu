@@ -511,10 +511,10 @@ inline bool head_sizes(size_t T, size_t V, size_t D, int sms, HeadSizes* s) {
   dh.P = T; dh.Q = D; dh.K = V; dh.batch = 1;
   s->splits = 1;
   unsigned long long least = 0;
-  (void)half_form(dh, 1, 1, sms, 256, &least);
+  (void)half_form(dh, 1, 1, sms, &least);
   for (unsigned splits = 2; splits <= 16 && s->pieces == 1 && V >= 256 * (size_t)splits && splits * T * D <= kPieceElements; ++splits) {
     unsigned long long clocks = 0;
-    (void)half_form(dh, 1, splits, sms, 256, &clocks);
+    (void)half_form(dh, 1, splits, sms, &clocks);
     clocks += 8000 + 2 * splits * T * D * 4 / (22 * (size_t)sms);
     if (clocks < least) {
       least = clocks;

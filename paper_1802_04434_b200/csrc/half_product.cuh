@@ -624,13 +624,12 @@ inline unsigned long long half_tiles(const HalfProduct& h, unsigned rows, unsign
   for (unsigned long long i = 0; i < tp; ++i) n += tq > i * (rows / nt) ? tq - i * (rows / nt) : 0;
   return n;
 }
-// most: columns of the widest tile that the epilogue's boxes leave room for.
-inline HalfForm half_form(const HalfProduct& h, int terms, unsigned splits, int sms, unsigned most = 256, unsigned long long* clocks = nullptr) {
+inline HalfForm half_form(const HalfProduct& h, int terms, unsigned splits, int sms, unsigned long long* clocks = nullptr) {
   const unsigned long long stages = (h.K + 63) / 64 / splits + 1, batch = h.batch * splits, pairs = (unsigned)sms / 2;
   const unsigned long long r256 = (half_tiles(h, 256, 256) * batch + pairs - 1) / pairs, r128 = (half_tiles(h, 256, 128) * batch + pairs - 1) / pairs,
                            r64 = (half_tiles(h, 128, 64) * batch + sms - 1) / (unsigned)sms;
   const unsigned s256 = terms == 3 ? 1560 : 530, s128 = terms == 3 ? 980 : 400, s64 = terms == 3 ? 1000 : 390;
-  const unsigned long long c256 = most < 256 ? ~0ull : r256 * (stages * s256 + 1500) + 6500, c128 = r128 * (stages * s128 + 1200) + 5500, c64 = r64 * (stages * s64 + 1000) + 5000;
+  const unsigned long long c256 = r256 * (stages * s256 + 1500) + 6500, c128 = r128 * (stages * s128 + 1200) + 5500, c64 = r64 * (stages * s64 + 1000) + 5000;
   HalfForm best = c256 <= c128 && c256 <= c64 ? HalfForm{true, 256, 1} : c128 <= c64 ? HalfForm{true, 128, 1} : HalfForm{false, 64, 1};
   unsigned long long least = c256 < c128 ? c256 : c128;
   if (c64 < least) least = c64;
@@ -696,18 +695,17 @@ ssgd_status launch_half_form(const HalfProduct& h, const typename Epilogue::Args
   return launch_status();
 }
 
-// Whether three stages of 256 columns fit beside the epilogue's boxes.
-template <class Epilogue, int TERMS, int CHUNK>
-constexpr bool half_fits() { return (232448 - 8 * Epilogue::kBox - 512) / ((TERMS == 3 ? 2 : 1) * 32768) >= 3; }
-
 // LAYOUT says what h.p.by_rows and h.q.by_rows say.
 template <class Epilogue, int TERMS, int CHUNK, int LAYOUT>
-ssgd_status launch_half(const HalfProduct& h, const typename Epilogue::Args& args, const HalfForm& form, unsigned splits, int sms, cudaStream_t s) {
+ssgd_status launch_narrow(const HalfProduct& h, const typename Epilogue::Args& args, const HalfForm& form, unsigned splits, int sms, cudaStream_t s) {
   if (form.split > 1) return launch_half_form<Epilogue, false, 64, TERMS, CHUNK, LAYOUT, true>(h, args, form.split, sms, s);
   if (!form.pairs) return launch_half_form<Epilogue, false, 64, TERMS, CHUNK, LAYOUT, false>(h, args, splits, sms, s);
-  if constexpr (half_fits<Epilogue, TERMS, CHUNK>())
-    if (form.nt == 256) return launch_half_form<Epilogue, true, 256, TERMS, CHUNK, LAYOUT, false>(h, args, splits, sms, s);
   return launch_half_form<Epilogue, true, 128, TERMS, CHUNK, LAYOUT, false>(h, args, splits, sms, s);
+}
+template <class Epilogue, int TERMS, int CHUNK, int LAYOUT>
+ssgd_status launch_half(const HalfProduct& h, const typename Epilogue::Args& args, const HalfForm& form, unsigned splits, int sms, cudaStream_t s) {
+  if (form.nt == 256) return launch_half_form<Epilogue, true, 256, TERMS, CHUNK, LAYOUT, false>(h, args, splits, sms, s);
+  return launch_narrow<Epilogue, TERMS, CHUNK, LAYOUT>(h, args, form, splits, sms, s);
 }
 
 }  // namespace

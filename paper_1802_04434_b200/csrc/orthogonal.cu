@@ -3,14 +3,14 @@
 //
 //   X = U / |U|_F, then `steps` times  X <- a X + (b A + c A^2) X,  A = X X^T       (rows <= columns; else from the right)
 //
-// Three products a step, on the tensor cores, A and A^2 by the tiles on and above their diagonals alone.  An fp16 operand has
-// eleven bits, and what a step loses, the next ones multiply by up to a (a direction whose singular value is still small grows
-// by that).  Two ways:
-//   TERMS = 3  every matrix is the sum of two fp16 matrices (22 bits), a product three: error 2e-7 .. 1e-6 of the result, products in fp32
-//              1e-6 .. 5e-6.  b A + c A^2 is had from the square of A + (b / 2 c) I, so that nothing is read beside the operands
-//   TERMS = 1  products of the high parts alone, X still kept in two.  With d = |X|_F^2 / s (s the shorter side) and A = d I + E the step
-//              is  X <- (a + b d + c d^2) X + ((b + 2 c d) E + c E^2) X:  the part along X is done in fp32, and what goes through fp16 shrinks as X
-//              approaches its goal (A near I, E small).  Error 4e-4 .. 1e-3, without this 2e-3 .. 3e-3; rounding to bf16 alone is 1.7e-3
+// Three products a step, on the tensor cores, A and A^2 by the tiles on and above their diagonals alone.  Operands are fp16, and what a
+// step loses, the next ones multiply by up to a (a direction whose singular value is still small grows by that), so the arithmetic is
+// arranged to lose little.  X is kept as the sum of two fp16 matrices (22 bits).  With d = |X|_F^2 / s (s the shorter side) and A = d I + E
+// the step is
+//   X <- (a + b d + c d^2) X + ((b + 2 c d) E + c E^2) X:
+// the part along X is done in fp32, and what goes through the products shrinks as X approaches its goal (A near I, E small).
+//   TERMS = 3  products of both parts of each operand: error 4e-7 .. 2e-6 of the result, products in fp32 1e-6 .. 5e-6
+//   TERMS = 1  products of the high parts: 4e-4 .. 1e-3, without d 2e-3 .. 3e-3; rounding to bf16 alone is 1.7e-3
 // All matrices are stored times 2^13: elements are at most 1.2 in size, and the smallest that count stay normal numbers of fp16.
 
 #include "half_product.cuh"
@@ -62,43 +62,40 @@ __device__ __forceinline__ void send_symmetric(const Box& box, unsigned offset, 
   if (mirrored) send_parts<LOW, true>(box, LOW ? offset : offset ^ 2048, to, row0, column, matrix, w);
 }
 
-// The product X X^T.  DEFLATED: E = A - d I, where d comes from the sums of squares that the last step left, added in a fixed order by each
-// warp; the first tile of each matrix leaves it for the other two products.  Else A + (b / 2 c) I, see below.
-template <bool LOW, bool DEFLATED>
+// E = X X^T - d I.  d comes from the sums of squares that the last step left, added in a fixed order by each warp; the first tile of each
+// matrix leaves it for the other two products.
+template <bool LOW>
 struct GramEpilogue {
   struct Args {
     Parts e;
     const float* squares;       // [matrix][count], or null: |X| is 1
     float* d;                   // [matrix]
     unsigned count, side;
-    float shift;
   };
   static constexpr unsigned kBox = 4096;
   static __device__ __forceinline__ void prefetch(const Args& a) { prefetch_parts(a.e); }
   Box box;
-  float diagonal;               // what is added there
+  float d;
   unsigned row0, seen, matrix, half;
   bool mirrored;
-  __device__ __forceinline__ GramEpilogue(const Args& a, const Box& b) : box(b), diagonal(a.shift * kScale), seen(~0u), half(0) {}
+  __device__ __forceinline__ GramEpilogue(const Args&, const Box& b) : box(b), seen(~0u), half(0) {}
   __device__ __forceinline__ void ahead(const Args&, unsigned) {}
   __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
     row0 = first_row;
     matrix = at.matrix;
     mirrored = at.q0 >= at.p0 + at.rows;
-    if (DEFLATED) {
-      if (matrix != seen) {
-        seen = matrix;
-        float sum = 1.0f;
-        if (a.squares) {
-          sum = 0.0f;
-          for (unsigned i = box.lane; i < a.count; i += 32) sum += a.squares[(size_t)matrix * a.count + i];
+    if (matrix != seen) {
+      seen = matrix;
+      float sum = 1.0f;
+      if (a.squares) {
+        sum = 0.0f;
+        for (unsigned i = box.lane; i < a.count; i += 32) sum += a.squares[(size_t)matrix * a.count + i];
 #pragma unroll
-          for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-        }
-        diagonal = -(sum / (float)a.side) * kScale;
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       }
-      if (at.tile == 0 && row0 + box.lane == 0) a.d[matrix] = diagonal * -kUnscale;      // two warps: the same value
+      d = sum / (float)a.side;
     }
+    if (at.tile == 0 && row0 + box.lane == 0) a.d[matrix] = d;      // two warps: the same value
   }
   __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned, float (&v)[32]) {
     const unsigned on = row0 + box.lane - column;
@@ -106,7 +103,7 @@ struct GramEpilogue {
     for (unsigned q = 0; q < 32; ++q) v[q] *= kUnscale;
     if (on < 32u) {
 #pragma unroll
-      for (unsigned q = 0; q < 32; ++q) v[q] = on == q ? v[q] + diagonal : v[q];
+      for (unsigned q = 0; q < 32; ++q) v[q] = on == q ? v[q] - d * kScale : v[q];
     }
     send_symmetric<LOW>(box, half, a.e, row0, column, matrix, mirrored, v);
     if (!LOW && !mirrored) half ^= 2048;        // an odd number has gone out
@@ -115,146 +112,140 @@ struct GramEpilogue {
   __device__ __forceinline__ void finish(const Args&) { box.finish(); }
 };
 
-// The polynomial from the square of what the first product left.
-//   DEFLATED   M = p E + c E^2 with p = b + 2 c d;  X' = (a + b d + c d^2) X + M X
-//   else       M = a I + b A + c A^2 = (a - b^2 / 4 c) I + c (A + (b / 2 c) I)^2, nothing to be read again;  X' = M X.  Where c is too
-//              small for that, shift = 0 and A is read
-template <bool LOW, bool DEFLATED>
+// What an epilogue reads, 32 x 32 elements of two parts at a time, by one or two boxes in which what it makes of them goes out again.  With two
+// the next is asked for before the last is taken; with one (where shared memory holds no more beside stages of three terms and 256
+// columns) when the last has gone, which the products that run on meanwhile hide.
+template <unsigned BOXES>
+struct Reader {
+  unsigned asks = 0, takes = 0, later = ~0u;    // later: a column that has to wait for the box
+  __device__ __forceinline__ void ask(Box& box, const CUtensorMap& high, const CUtensorMap* low, unsigned column, unsigned row, unsigned matrix) {
+    if (BOXES == 1 && asks != takes) {
+      later = column;
+      return;
+    }
+    box.sent();
+    const unsigned b = BOXES == 1 ? 0 : asks & 1u;
+    box.ask(b, b * 4096, high, low, column, row, matrix);
+    ++asks;
+  }
+  // Where the elements are; for one box it is taken until `done`.
+  __device__ __forceinline__ unsigned take(Box& box) {
+    const unsigned b = BOXES == 1 ? 0 : takes & 1u;
+    box.take(b);
+    if (BOXES == 2) ++takes;
+    return b * 4096;
+  }
+  __device__ __forceinline__ void done(Box& box, const CUtensorMap& high, const CUtensorMap* low, unsigned row, unsigned matrix) {
+    if (BOXES == 1) {
+      ++takes;
+      if (later != ~0u) {
+        const unsigned column = later;
+        later = ~0u;
+        ask(box, high, low, column, row, matrix);
+      }
+    }
+  }
+};
+
+// M = p E + c E^2, p = b + 2 c d.
+struct PolynomialArgs {
+  Parts e, m;
+  const float* d;
+  Polynomial f;
+};
+template <bool LOW, unsigned BOXES>
 struct PolynomialEpilogue {
-  struct Args {
-    Parts e, m;
-    const float* d;
-    Polynomial f;
-    float diagonal;             // not deflated: what is added there
-    unsigned shifted;
-  };
-  // two boxes for E's parts, in which M's go out
-  static constexpr unsigned kBox = DEFLATED ? 8192 : 4096;
+  using Args = PolynomialArgs;
+  static constexpr unsigned kBox = BOXES * 4096;
   static __device__ __forceinline__ void prefetch(const Args& a) {
     prefetch_parts(a.m);
-    if (DEFLATED || !a.shifted) prefetch_parts(a.e);
+    prefetch_parts(a.e);
   }
   Box box;
+  Reader<BOXES> reader;
   float p;
-  unsigned row0, matrix, asks, takes;
+  unsigned row0, matrix;
   bool mirrored;
-  __device__ __forceinline__ PolynomialEpilogue(const Args&, const Box& b) : box(b), asks(0), takes(0) {}
+  __device__ __forceinline__ PolynomialEpilogue(const Args&, const Box& b) : box(b) {}
   __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
     row0 = first_row;
     matrix = at.matrix;
     mirrored = at.q0 >= at.p0 + at.rows;
-    if (DEFLATED) p = a.f.b + 2.0f * a.f.c * a.d[matrix];
+    p = a.f.b + 2.0f * a.f.c * a.d[matrix];
   }
-  __device__ __forceinline__ void ahead(const Args& a, unsigned column) {
-    if (DEFLATED) {
-      box.sent();
-      box.ask(asks & 1u, (asks & 1u) * 4096, a.e.high, LOW ? &a.e.low : nullptr, column, row0, matrix);
-      ++asks;
-    }
-  }
+  __device__ __forceinline__ void ahead(const Args& a, unsigned column) { reader.ask(box, a.e.high, LOW ? &a.e.low : nullptr, column, row0, matrix); }
   __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned, float (&v)[32]) {
-    const float c = a.f.c * kUnscale, by = DEFLATED ? p : a.f.b;
-    unsigned from = 0;
-    if (DEFLATED || !a.shifted) {
-      const unsigned b = DEFLATED ? takes++ & 1u : 0;
-      from = b * 4096;
-      if (!DEFLATED) {
-        box.sent();
-        box.ask(0, 0, a.e.high, &a.e.low, column, row0, matrix);
+    const float c = a.f.c * kUnscale;
+    const unsigned from = reader.take(box);
+#pragma unroll
+    for (unsigned q = 0; q < 4; ++q) {
+      float e[8];
+      box.get8(from, q, e);
+      if (LOW) {
+        float low[8];
+        box.get8(from + 2048, q, low);
+#pragma unroll
+        for (unsigned i = 0; i < 8; ++i) e[i] += low[i];
       }
-      box.take(b);
 #pragma unroll
-      for (unsigned q = 0; q < 4; ++q) {
-        float e[8];
-        box.get8(from, q, e);
-        if (LOW) {
-          float low[8];
-          box.get8(from + 2048, q, low);
-#pragma unroll
-          for (unsigned i = 0; i < 8; ++i) e[i] += low[i];
-        }
-#pragma unroll
-        for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = fmaf(c, v[8 * q + i], by * e[i]);
-      }
-      __syncwarp();
-    } else {
-#pragma unroll
-      for (unsigned q = 0; q < 32; ++q) v[q] *= c;
+      for (unsigned i = 0; i < 8; ++i) v[8 * q + i] = fmaf(c, v[8 * q + i], p * e[i]);
     }
-    if (!DEFLATED) {
-      const unsigned on = row0 + box.lane - column;
-      if (on < 32u) {
-#pragma unroll
-        for (unsigned q = 0; q < 32; ++q) v[q] = on == q ? v[q] + a.diagonal : v[q];
-      }
-    }
+    __syncwarp();
     send_symmetric<LOW>(box, from, a.m, row0, column, matrix, mirrored, v);
+    reader.done(box, a.e.high, LOW ? &a.e.low : nullptr, row0, matrix);
   }
   __device__ __forceinline__ void end(const Args&, const HalfPlace&, unsigned) {}
   __device__ __forceinline__ void finish(const Args&) { box.finish(); }
 };
 
-// X' = M X, or deflated (a + b d + c d^2) X + M X: kept for the next step, with its sum of squares; or, behind the last, written
-// out as T; or x <- x - delta X'.
+// X' = q X + M X, q = a + b d + c d^2: kept for the next step, with its sum of squares; or, behind the last, written out as T; or
+// x <- x - delta X'.
 enum UpdateTo { kNextStep, kOut, kParameters };
-template <int TO, typename T, bool LOW, bool DEFLATED>
+template <typename T>
+struct UpdateArgs {
+  Parts x, next;
+  const float* d;
+  float* squares;               // [matrix][count]
+  T* out;
+  size_t ldo, out_stride;
+  Polynomial f;
+  float delta;
+  unsigned rows, count, slots;          // sums of squares of a matrix, and of a tile
+};
+template <int TO, typename T, unsigned BOXES>
 struct UpdateEpilogue {
-  struct Args {
-    Parts x, next;
-    const float* d;
-    float* squares;             // [matrix][count]
-    T* out;
-    size_t ldo, out_stride;
-    Polynomial f;
-    float delta;
-    unsigned rows, count, slots;        // sums of squares of a matrix, and of a tile
-  };
-  static constexpr unsigned kBox = DEFLATED ? 8192 : 4096;      // two boxes of X's parts, in which X' goes out again
+  using Args = UpdateArgs<T>;
+  static constexpr unsigned kBox = BOXES * 4096;
   static __device__ __forceinline__ void prefetch(const Args& a) {
     if (TO == kNextStep) prefetch_parts(a.next);
-    if (DEFLATED) prefetch_parts(a.x);
+    prefetch_parts(a.x);
   }
   Box box;
+  Reader<BOXES> reader;
   float q, sum;
-  unsigned row0, matrix, asks, takes;
-  __device__ __forceinline__ UpdateEpilogue(const Args&, const Box& b) : box(b), asks(0), takes(0) {}
+  unsigned row0, matrix;
+  __device__ __forceinline__ UpdateEpilogue(const Args&, const Box& b) : box(b) {}
   __device__ __forceinline__ void begin(const Args& a, const HalfPlace& at, unsigned first_row, unsigned) {
     row0 = first_row;
     matrix = at.matrix;
-    if (DEFLATED) {
-      const float d = a.d[matrix];
-      q = a.f.a + d * (a.f.b + d * a.f.c);
-      sum = 0.0f;
-    }
+    const float d = a.d[matrix];
+    q = a.f.a + d * (a.f.b + d * a.f.c);
+    sum = 0.0f;
   }
-  __device__ __forceinline__ void ahead(const Args& a, unsigned column) {
-    if (DEFLATED) {
-      if (TO == kNextStep) box.sent();
-      box.ask(asks & 1u, (asks & 1u) * 4096, a.x.high, &a.x.low, column, row0, matrix);
-      ++asks;
-    }
-  }
+  __device__ __forceinline__ void ahead(const Args& a, unsigned column) { reader.ask(box, a.x.high, &a.x.low, column, row0, matrix); }
   __device__ __forceinline__ void unit(const Args& a, unsigned column, unsigned left, float (&v)[32]) {
-    unsigned from = 0;
-    if (!DEFLATED) {
+    const unsigned from = reader.take(box);
 #pragma unroll
-      for (unsigned i = 0; i < 32; ++i) v[i] *= kUnscale;
-    } else {
-      const unsigned b = takes++ & 1u;
-      from = b * 4096;
-      box.take(b);
+    for (unsigned p = 0; p < 4; ++p) {
+      float high[8], low[8];
+      box.get8(from, p, high);
+      box.get8(from + 2048, p, low);
 #pragma unroll
-      for (unsigned p = 0; p < 4; ++p) {
-        float high[8], low[8];
-        box.get8(from, p, high);
-        box.get8(from + 2048, p, low);
-#pragma unroll
-        for (unsigned i = 0; i < 8; ++i) v[8 * p + i] = fmaf(q, high[i] + low[i], v[8 * p + i] * kUnscale);
-      }
-      __syncwarp();
+      for (unsigned i = 0; i < 8; ++i) v[8 * p + i] = fmaf(q, high[i] + low[i], v[8 * p + i] * kUnscale);
     }
+    __syncwarp();
     if constexpr (TO == kNextStep) {
-      if (DEFLATED && row0 + box.lane < a.rows) {   // behind the last column there are zeros
+      if (row0 + box.lane < a.rows) {           // behind the last column there are zeros
 #pragma unroll
         for (unsigned i = 0; i < 32; ++i) sum = fmaf(v[i], v[i], sum);
       }
@@ -263,15 +254,17 @@ struct UpdateEpilogue {
       const float by = TO == kOut ? kUnscale : -a.delta * kUnscale;
 #pragma unroll
       for (unsigned i = 0; i < 32; ++i) v[i] *= by;
-      Box whole(box.at + from, box.full, box.lane);
+      const Box whole(box.at + from, box.full, box.lane);
       T* o = a.out + matrix * a.out_stride + (size_t)row0 * a.ldo + column;
       const unsigned rows = min(32u, a.rows - row0);
       if constexpr (TO == kOut) whole.rows_out(o, a.ldo, rows, left, v);
       else whole.rows_join(o, a.ldo, o, a.ldo, rows, left, v, [](float x, float step) { return x + step; });
+      __syncwarp();
     }
+    reader.done(box, a.x.high, &a.x.low, row0, matrix);
   }
   __device__ __forceinline__ void end(const Args& a, const HalfPlace& at, unsigned warp) {
-    if constexpr (TO == kNextStep && DEFLATED) {
+    if constexpr (TO == kNextStep) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       if (box.lane == 0) a.squares[(size_t)matrix * a.count + at.tile * a.slots + warp] = sum * (kUnscale * kUnscale);
@@ -727,15 +720,17 @@ orthogonal_small_kernel(const SmallArgs a) {
 template <int TO, typename T>
 struct ClusterArgs {
   CUtensorMap x[2][2], e[2], m[2];              // operands in boxes of 64 x 64, high and low part; the same boxes serve either way round
-  typename GramEpilogue<true, true>::Args gram[2];          // of the first step, and of the others
-  typename PolynomialEpilogue<true, true>::Args polynomial;
-  typename UpdateEpilogue<kNextStep, float, true, true>::Args next[2];
-  typename UpdateEpilogue<TO, T, true, true>::Args last;
+  typename GramEpilogue<true>::Args gram[2];          // of the first step, and of the others
+  PolynomialArgs polynomial;
+  UpdateArgs<float> next[2];
+  UpdateArgs<T> last;
   unsigned rows, cols, steps, starve;
   unsigned* status;
 };
 
-using ClusterShape = HalfShape<false, 64, 3, 1, 8192>;
+// Stages between two times that a sum of three terms is taken; tiles of 256 columns, with fewer sums on their way, twice as many.
+constexpr int kChunk = 2;
+using ClusterShape = HalfShape<false, 64, 3, kChunk, 8192>;
 
 struct ClusterState {
   unsigned stage0, full, empty, acc_full, acc_free, tmem, warp, lane, rank, size, matrix, starve;
@@ -789,16 +784,20 @@ __device__ __forceinline__ void cluster_product(ClusterState& st, bool symmetric
       const uint64_t p_desc = half_descriptor(st.stage0, (LAYOUT & 2) != 0), q_desc = half_descriptor(st.stage0 + S::p_bytes, (LAYOUT & 1) != 0);
       const unsigned idesc = mma_half_descriptor(128, 64, false, (LAYOUT & 2) != 0, (LAYOUT & 1) != 0);
       each_tile([&](unsigned, unsigned) {
-        for (unsigned k = 0; k < stages; ++k, ++st.n, ++st.t) {
+        for (unsigned k = 0; k < stages; ++k, ++st.n) {
           const unsigned s = st.n % S::stages, acc = st.t % S::accs;
-          if (st.t >= S::accs) st.ok = mbarrier_wait(st.acc_free + 8 * acc, (st.t / S::accs - 1) & 1u, kHalfPolls);
+          const bool fresh = k % kChunk == 0, taken = k % kChunk == kChunk - 1 || k + 1 == stages;
+          if (fresh && st.t >= S::accs) st.ok = mbarrier_wait(st.acc_free + 8 * acc, (st.t / S::accs - 1) & 1u, kHalfPolls);
           st.ok = st.ok && mbarrier_wait(st.full + 8 * s, (st.n / S::stages) & 1u, kHalfPolls);
           if (!st.ok) break;
           tcgen05_fence_after();
           const unsigned at = s * (S::stage_bytes >> 4);
-          half_issue<false, 3, LAYOUT, low>(st.tmem + acc * 64, p_desc + at, q_desc + at, idesc, chunks - k * 4, false);
+          half_issue<false, 3, LAYOUT, low>(st.tmem + acc * 64, p_desc + at, q_desc + at, idesc, chunks - k * 4, !fresh);
           tcgen05_commit(st.empty + 8 * s);
-          tcgen05_commit(st.acc_full + 8 * acc);
+          if (taken) {
+            tcgen05_commit(st.acc_full + 8 * acc);
+            ++st.t;
+          }
         }
       });
     }
@@ -816,7 +815,7 @@ __device__ __forceinline__ void cluster_product(ClusterState& st, bool symmetric
 #pragma unroll
       for (unsigned q = 0; q < 32; ++q) sum[q] = 0.0f;
 #pragma unroll 1
-      for (unsigned k = 0; k < stages; ++k, ++st.t) {
+      for (unsigned k = 0; k < stages; k += kChunk, ++st.t) {
         const unsigned acc = st.t % S::accs;
         st.ok = __all_sync(0xFFFFFFFFu, mbarrier_wait(st.acc_full + 8 * acc, (st.t / S::accs) & 1u, 4 * kHalfPolls));
         if (!st.ok) break;
@@ -892,10 +891,10 @@ orthogonal_cluster_kernel(const __grid_constant__ ClusterArgs<TO, T> a) {
   const unsigned squares = (side + 127) / 128 * ((side + 63) / 64);
   const bool symmetric = squares > st.size;
   const Box box(st.stage0 + S::stages * S::stage_bytes + w * S::box_bytes, box_full + 16 * w, st.lane);
-  GramEpilogue<true, true> gram(a.gram[0], box);
-  PolynomialEpilogue<true, true> polynomial(a.polynomial, box);
-  UpdateEpilogue<kNextStep, float, true, true> next(a.next[0], box);
-  UpdateEpilogue<TO, T, true, true> last(a.last, box);
+  GramEpilogue<true> gram(a.gram[0], box);
+  PolynomialEpilogue<true, 2> polynomial(a.polynomial, box);
+  UpdateEpilogue<kNextStep, float, 2> next(a.next[0], box);
+  UpdateEpilogue<TO, T, 2> last(a.last, box);
   // All CTAs of the cluster have left a product behind.  A CTA that gave up keeps step and does nothing more.
   auto between = [&]() {
     if (!st.ok) atomicExch(&failed, 1u);
@@ -1002,23 +1001,31 @@ ssgd_status launch_source_typed(const Problem& p, const Layout& l, const Whole& 
   }
 }
 
-// Stages between two times that a sum of three terms is taken.
-constexpr int kChunk = 1;
-
 struct Buffers {
   Whole x[2], e, m;
   Parts x_parts[2], e_parts, m_parts;
   float *d, *squares;
 };
 
-// Three terms, deflated: boxes and stages leave room for tiles of 128 columns.
-template <int TERMS, bool DEFLATED>
-constexpr unsigned kMostColumns = TERMS == 3 && DEFLATED ? 128 : 256;
-// Shorter side up to which three-term steps are deflated too: what the tensor cores cut off of the sums along X counts for more there
-// (130 x 130: 3.4e-6 of the result, deflated 6e-7, in fp32 1.5e-6; 512 x 512 1.7e-6, fp32 2.3e-6).
-constexpr size_t kDeflatedSide = 255;
+// One product: tiles of 256 columns and three terms leave an epilogue one box.
+template <template <unsigned> class Epilogue, int TERMS, int LAYOUT, typename Args>
+ssgd_status launch_boxed(const HalfProduct& h, const Args& args, const HalfForm& form, int sms, cudaStream_t s) {
+  constexpr int chunk = TERMS == 3 ? kChunk : 0;
+  if (form.nt == 256) {
+    using Wide = Epilogue<TERMS == 3 ? 1 : 2>;
+    return launch_half_form<Wide, true, 256, TERMS, 2 * chunk, LAYOUT, false>(h, args, 1, sms, s);
+  }
+  using Other = Epilogue<2>;
+  return launch_narrow<Other, TERMS, chunk, LAYOUT>(h, args, form, 1, sms, s);
+}
+template <bool LOW>
+struct GramOf { template <unsigned> using Epilogue = GramEpilogue<LOW>; };
+template <bool LOW>
+struct PolynomialOf { template <unsigned BOXES> using Epilogue = PolynomialEpilogue<LOW, BOXES>; };
+template <int TO, typename T>
+struct UpdateOf { template <unsigned BOXES> using Epilogue = UpdateEpilogue<TO, T, BOXES>; };
 
-template <int TO, typename T, int TERMS, bool DEFLATED>
+template <int TO, typename T, int TERMS>
 ssgd_status launch_update(const Problem& p, const Layout& l, const Buffers& b, int now, unsigned* count, int sms, cudaStream_t s) {
   const Whole& x = b.x[now];
   const HalfOperand whole = {x.high, x.low, x.ld, x.stride, false}, square = {b.m.high, b.m.low, b.m.ld, b.m.stride, false};
@@ -1034,38 +1041,22 @@ ssgd_status launch_update(const Problem& p, const Layout& l, const Buffers& b, i
     h.p = whole;
     h.q = square;
   }
-  const HalfForm form = half_form(h, TERMS, 1, sms, kMostColumns<TERMS, DEFLATED>);
+  const HalfForm form = half_form(h, TERMS, 1, sms);
   const unsigned slots = form.pairs ? 16 : 8;                  // epilogue warps of a tile
   *count = slots * (unsigned)half_tiles(h, form.pairs ? 256 : 128, form.nt);
-  typename UpdateEpilogue<TO, T, TERMS == 3, DEFLATED>::Args a = {};
+  UpdateArgs<T> a = {};
   a.x = b.x_parts[now]; a.next = b.x_parts[1 - now]; a.d = b.d; a.squares = b.squares;
   a.out = static_cast<T*>(p.out); a.ldo = p.ldo; a.out_stride = p.out_stride;
   a.f = p.f; a.delta = p.delta; a.rows = (unsigned)p.rows; a.count = *count; a.slots = slots;
-  using Epilogue = UpdateEpilogue<TO, T, TERMS == 3, DEFLATED>;
-  constexpr int chunk = TERMS == 3 ? kChunk : 0;
-  return h.q.by_rows ? launch_half<Epilogue, TERMS, chunk, kQByRows>(h, a, form, 1, sms, s) : launch_half<Epilogue, TERMS, chunk, kBothByK>(h, a, form, 1, sms, s);
+  return h.q.by_rows ? launch_boxed<UpdateOf<TO, T>::template Epilogue, TERMS, kQByRows>(h, a, form, sms, s)
+                     : launch_boxed<UpdateOf<TO, T>::template Epilogue, TERMS, kBothByK>(h, a, form, sms, s);
 }
 
-// The largest |b / 2 c| that is added to A's diagonal: A + that, times 2^13, is an fp16 number, and little of A is lost beside it.
-constexpr float kMostShift = 4.0f;
-
-// b A + c A^2 + a I from the square of A + by I, or, where that is too far from A, of A.
-struct Shift { float by, diagonal; bool shifted; };
-inline Shift shift_of(const Polynomial& f) {
-  const float by = f.b / (2.0f * f.c);
-  if (f.c == 0.0f || !(fabsf(by) <= kMostShift)) return {0.0f, kScale * f.a, false};
-  return {by, kScale * (f.a - f.b * by * 0.5f), true};
-}
-
-template <int TERMS, bool DEFLATED>
+template <int TERMS>
 ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, int sms, cudaStream_t s) {
-  using Gram = GramEpilogue<TERMS == 3, DEFLATED>;
-  using Poly = PolynomialEpilogue<TERMS == 3, DEFLATED>;
-  constexpr int chunk = TERMS == 3 ? kChunk : 0;
-  constexpr unsigned most = kMostColumns<TERMS, DEFLATED>;
+  constexpr bool kLow = TERMS == 3;
   unsigned count = 0;
   int now = 0;
-  const Shift shift = shift_of(p.f);            // not deflated
   for (unsigned k = 0; k < p.steps; ++k) {
     const Whole& x = b.x[now];
     HalfProduct h = {};
@@ -1077,22 +1068,22 @@ ssgd_status newton_schulz(const Problem& p, const Layout& l, const Buffers& b, i
     h.symmetric = true;
     h.status = p.status;
     h.starve = p.starve;
-    const typename Gram::Args gram = {b.e_parts, k ? b.squares : nullptr, b.d, count, (unsigned)l.side, shift.by};
-    const HalfForm form = half_form(h, TERMS, 1, sms, most);
-    ssgd_status st = h.p.by_rows ? launch_half<Gram, TERMS, chunk, kBothByRows>(h, gram, form, 1, sms, s)
-                                 : launch_half<Gram, TERMS, chunk, kBothByK>(h, gram, form, 1, sms, s);
+    const typename GramEpilogue<kLow>::Args gram = {b.e_parts, k ? b.squares : nullptr, b.d, count, (unsigned)l.side};
+    const HalfForm form = half_form(h, TERMS, 1, sms);
+    ssgd_status st = h.p.by_rows ? launch_boxed<GramOf<kLow>::template Epilogue, TERMS, kBothByRows>(h, gram, form, sms, s)
+                                 : launch_boxed<GramOf<kLow>::template Epilogue, TERMS, kBothByK>(h, gram, form, sms, s);
     if (st != SSGD_OK) return st;
     h.p = {b.e.high, b.e.low, b.e.ld, b.e.stride, false};
     h.q = h.p;
     h.K = l.side;
-    const typename Poly::Args polynomial = {b.e_parts, b.m_parts, b.d, p.f, shift.diagonal, shift.shifted};
-    st = launch_half<Poly, TERMS, chunk, kBothByK>(h, polynomial, half_form(h, TERMS, 1, sms, most), 1, sms, s);
+    const PolynomialArgs polynomial = {b.e_parts, b.m_parts, b.d, p.f};
+    st = launch_boxed<PolynomialOf<kLow>::template Epilogue, TERMS, kBothByK>(h, polynomial, half_form(h, TERMS, 1, sms), sms, s);
     if (st != SSGD_OK) return st;
-    if (k + 1 < p.steps) st = launch_update<kNextStep, float, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
-    else if (p.momentum) st = launch_update<kParameters, float, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
-    else if (p.out_type == SSGD_F32) st = launch_update<kOut, float, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
-    else if (p.out_type == SSGD_BF16) st = launch_update<kOut, __nv_bfloat16, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
-    else st = launch_update<kOut, __half, TERMS, DEFLATED>(p, l, b, now, &count, sms, s);
+    if (k + 1 < p.steps) st = launch_update<kNextStep, float, TERMS>(p, l, b, now, &count, sms, s);
+    else if (p.momentum) st = launch_update<kParameters, float, TERMS>(p, l, b, now, &count, sms, s);
+    else if (p.out_type == SSGD_F32) st = launch_update<kOut, float, TERMS>(p, l, b, now, &count, sms, s);
+    else if (p.out_type == SSGD_BF16) st = launch_update<kOut, __nv_bfloat16, TERMS>(p, l, b, now, &count, sms, s);
+    else st = launch_update<kOut, __half, TERMS>(p, l, b, now, &count, sms, s);
     if (st != SSGD_OK) return st;
     now = 1 - now;
   }
@@ -1115,13 +1106,13 @@ inline unsigned cluster_ctas(const Problem& p, const Layout& l, int sms) {
   h.symmetric = true;
   const unsigned long long square_tiles = half_tiles(h, 128, 64);
   unsigned long long launches = 3 * 5000ull, least = 0;
-  (void)half_form(h, p.terms, 1, sms, 256, &least);
+  (void)half_form(h, p.terms, 1, sms, &least);
   launches += least;
   h.K = s;
-  (void)half_form(h, p.terms, 1, sms, 256, &least);
+  (void)half_form(h, p.terms, 1, sms, &least);
   launches += least;
   h.P = p.rows; h.Q = p.cols; h.symmetric = false;
-  (void)half_form(h, p.terms, 1, sms, 256, &least);
+  (void)half_form(h, p.terms, 1, sms, &least);
   launches += least;
   const unsigned long long tiles = half_tiles(h, 128, 64), most = tiles > square_tiles ? tiles : square_tiles;
   const unsigned ctas = most <= 2 ? 2 : most <= 4 ? 4 : most <= 8 ? 8 : 16, at_once = ctas == 16 ? 6 : 96 / ctas;
@@ -1143,9 +1134,9 @@ ssgd_status launch_cluster(const Problem& p, const Layout& l, const Buffers& b, 
       !operand(a.m, b.m, l.side, l.side))
     return SSGD_ERR_CUDA;
   const unsigned count = 8 * (unsigned)(((p.rows + 127) / 128) * ((p.cols + 63) / 64));
-  a.gram[0] = {b.e_parts, nullptr, b.d, count, (unsigned)l.side, 0.0f};
-  a.gram[1] = {b.e_parts, b.squares, b.d, count, (unsigned)l.side, 0.0f};
-  a.polynomial = {b.e_parts, b.m_parts, b.d, p.f, 0.0f, 0};
+  a.gram[0] = {b.e_parts, nullptr, b.d, count, (unsigned)l.side};
+  a.gram[1] = {b.e_parts, b.squares, b.d, count, (unsigned)l.side};
+  a.polynomial = {b.e_parts, b.m_parts, b.d, p.f};
   for (int i = 0; i < 2; ++i) {
     a.next[i].x = b.x_parts[i];
     a.next[i].next = b.x_parts[1 - i];
@@ -1250,8 +1241,7 @@ ssgd_status solve(Problem p, const float* coefficients, cudaStream_t s) {
   const ssgd_status st = p.momentum ? launch_source_typed<kMomentum>(p, l, b.x[0], s) : launch_source_typed<kPlainSource>(p, l, b.x[0], s);
   if (st != SSGD_OK) return st;
   if (const unsigned ctas = cluster_ctas(p, l, info.sms)) return by_cluster(p, l, b, ctas, s);
-  if (p.terms == 1) return newton_schulz<1, true>(p, l, b, info.sms, s);
-  return l.side <= kDeflatedSide ? newton_schulz<3, true>(p, l, b, info.sms, s) : newton_schulz<3, false>(p, l, b, info.sms, s);
+  return p.terms == 3 ? newton_schulz<3>(p, l, b, info.sms, s) : newton_schulz<1>(p, l, b, info.sms, s);
 }
 
 ssgd_status checked_orthogonalise(const void* u, int u_type, size_t n, size_t rows, size_t cols, size_t ldu, size_t stride_u, const float* coefficients,
