@@ -590,3 +590,77 @@ def test_orthogonal_in_graphs_and_on_streams(orthogonal):
     torch.cuda.synchronize()
     for got, expected in results:
         assert all(torch.equal(a, b) for a, b in zip(got, expected))
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# together
+
+
+def test_align(loss):
+    from paper_1802_04434_b200 import binding as B
+    a, b = torch.randn(37, 50, device="cuda").half(), torch.randn(61, 9, device="cuda").half()
+    out = torch.full((37 + 9, 56), 7.0, dtype=F16, device="cuda")
+    assert B.lib().ssgd_xent_align(a.data_ptr(), 50, 1, 37, out.data_ptr(), b.data_ptr(), 1, 9, 9, out[37:].data_ptr(), 50, 56,
+                                   torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(out[:37, :50], a) and torch.equal(out[37:, :50], b[:50].t()) and not out[:, 50:].any()
+
+
+@pytest.mark.parametrize("fmt", ["mx", "nv"])
+def test_the_example(fmt):
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import train_language_head as example
+    losses, norms, model = example.train(steps=3, vocab=301, width=64, blocks=2, size=200, fmt=fmt)
+    assert all(torch.isfinite(torch.tensor(v)).all() for v in (losses, norms)) and bool(torch.isfinite(model.flat).all())
+    # its gradients: the loss's products alone, the layers' in fp32 on operands that 4 bits hold are as they are
+    gen_ = gen(1)
+    permutation = torch.randperm(301, generator=gen_, device="cuda")
+    tokens, targets = example.batch(gen_, permutation, 200, "cuda")
+    model.blocks, model.hidden = 0, model.hidden[:0]
+    parameters = model.parameters()
+    value = model.loss(parameters, tokens, targets)
+    de, dw = torch.autograd.grad(value, parameters)
+    e, w = parameters[0].detach(), parameters[1].detach()
+    g = torch.full((200,), 1.0 / int((targets != -100).sum()), device="cuda")
+    want, tol = ref.loss_and_gradients(e[tokens], w, targets, g)
+    within(dw, want[2], tol[2], "head")
+    # rows of the embedding are sums of dh over their tokens, rounded to bf16 each time one is added
+    rows = torch.zeros(301, 64, dtype=torch.float64, device="cuda").index_add_(0, tokens, want[1])
+    most = torch.bincount(tokens, minlength=301)[:, None]
+    sizes = torch.zeros(301, 64, dtype=torch.float64, device="cuda").index_add_(0, tokens, want[1].abs() + tol[1])
+    bound = torch.zeros(301, 64, dtype=torch.float64, device="cuda").index_add_(0, tokens, tol[1]) + most * 2.0 ** -8 * sizes
+    within(de, rows, bound, "embedding")
+
+
+def test_a_step_of_everything(loss, orthogonal):
+    # a layer, the loss, one norm over all gradients, the orthogonalised step, against the same in fp64 on the layer's rounded operands
+    from paper_1802_04434_b200 import binding as B, fp4
+    r = gen(11)
+    held = torch.tensor([-4.0, -2.0, -1.0, 0.0, 1.0, 3.0], device="cuda")      # values that 4 bits hold beside a 6 in every block
+    x = held[torch.randint(0, 6, (96, 64), generator=r, device="cuda")]
+    w = held[torch.randint(0, 6, (160, 64), generator=r, device="cuda")]
+    for t in (x, w):
+        t[::16], t[:, ::16] = 6.0, 6.0
+    x, w = x.to(BF16), w * 2.0 ** -6
+    head = (torch.randn(500, 160, generator=r, device="cuda") * 0.1).to(BF16)
+    y = torch.where(torch.rand(96, generator=r, device="cuda") < 0.2, -100, torch.randint(0, 500, (96,), generator=r, device="cuda"))
+    hidden, kept = fp4.linear_forward(x, w, "mx")
+    losses, kept2 = loss.cross_entropy_forward(hidden, head, y)
+    g = torch.full((96,), 1.0 / int((y != -100).sum()), device="cuda")
+    dh, dhead = loss.cross_entropy_backward(kept2, g)
+    want, tol = ref.loss_and_gradients(hidden, head, y, g)
+    assert torch.equal(hidden, (x.float() @ w.t()).to(BF16))                   # exact in 4 bits, one rounding
+    within(losses, want[0], tol[0], "losses")
+    within(dh, want[1], tol[1], "dh")
+    dx, dw = fp4.linear_backward(kept, dh)
+    row = torch.zeros(160 * 64 + 500 * 160, device="cuda")
+    norm = torch.zeros(1, device="cuda")
+    B.tensors_clip(B.TensorTable([dw, dhead], [row[:160 * 64].view_as(dw), row[160 * 64:].view_as(dhead)]), 0.01, norm)
+    both = torch.cat([dw.double().flatten(), dhead.double().flatten()])
+    assert abs(float(norm) - float(both.norm())) <= 2.0 ** -22 * float(norm)
+    p, m = w.clone(), torch.zeros_like(w)
+    clipped = row[:160 * 64].view(160, 64)
+    orthogonal.momentum_step(p, clipped, m, 0.9, 0.05)
+    b32 = torch.tensor(0.9, dtype=F32)
+    assert ref.off(m, (1 - b32).item() * clipped.double()) <= 2.0 ** -23
+    move = ref.orthogonal(m)
+    assert ref.off(p, w.double() - 0.05 * move) <= 2.0 ** -24 + 1e-5 * 0.05 * float(move.norm() / w.double().norm()) * 1.1
