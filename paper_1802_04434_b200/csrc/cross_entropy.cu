@@ -406,23 +406,32 @@ struct TokensEpilogue {
   __device__ __forceinline__ void finish(const Args&) {}
 };
 
+// The planes' sums, in order; a thread's four elements a CTA's width apart, eight loads in flight.
 template <typename T>
 __global__ void __launch_bounds__(256)
 xent_planes_kernel(const float* __restrict__ sums, unsigned planes, size_t plane, const Prepared* __restrict__ prepared, unsigned width, T* __restrict__ out,
                    size_t ldo) {
   pdl_launch_dependents();
   pdl_wait();
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= plane) return;
-  float s = 0.0f;
-  for (unsigned p0 = 0; p0 < planes; p0 += 8) {
-    float v[8];
+  const size_t i0 = (size_t)blockIdx.x * 1024 + threadIdx.x;
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (unsigned p = 0; p < planes; p += 2) {
+    float v[2][4];
 #pragma unroll
-    for (unsigned u = 0; u < 8; ++u) v[u] = p0 + u < planes ? sums[(p0 + u) * plane + i] : 0.0f;
+    for (unsigned u = 0; u < 2; ++u)
 #pragma unroll
-    for (unsigned u = 0; u < 8; ++u) s += v[u];
+      for (unsigned k = 0; k < 4; ++k) v[u][k] = p + u < planes && i0 + 256 * k < plane ? __ldcs(sums + (p + u) * plane + i0 + 256 * k) : 0.0f;
+#pragma unroll
+    for (unsigned u = 0; u < 2; ++u)
+#pragma unroll
+      for (unsigned k = 0; k < 4; ++k) s[k] += v[u][k];
   }
-  out[i / width * ldo + i % width] = from_float<T>(s * prepared->unscale);
+  const float unscale = prepared->unscale;
+#pragma unroll
+  for (unsigned k = 0; k < 4; ++k) {
+    const size_t i = i0 + 256 * k;
+    if (i < plane) out[i / width * ldo + i % width] = from_float<T>(s[k] * unscale);
+  }
 }
 
 // dw: rows of the vocabulary.
@@ -487,7 +496,7 @@ constexpr int kSumStages = 8;
 constexpr size_t kFewTokens = 2, kFewCtas = 2;      // see xent_few_kernel; CTAs of an SM
 
 struct HeadSizes {
-  size_t parts;                             // most partial statistics of a token: two for each 64 columns
+  size_t parts;                             // partial statistics of a token
   size_t forward_bytes;
   size_t piece, pieces;                     // columns of the vocabulary at a time
   unsigned splits;                          // of dh's k, the vocabulary
@@ -496,9 +505,15 @@ struct HeadSizes {
 
 // Pieces: dz of a piece is at most 2^27 numbers (256 MB), in whole 256 columns.
 constexpr size_t kPieceElements = (size_t)1 << 27;
+inline HalfForm stats_form(size_t T, size_t V, size_t D, int sms) {
+  HalfProduct p = {};
+  p.P = T; p.Q = V; p.K = D; p.batch = 1;
+  return half_form(p, 1, 1, sms);
+}
 inline bool head_sizes(size_t T, size_t V, size_t D, int sms, HeadSizes* s) {
   if (T < 1 || V < 1 || D < 1 || T > kSide || V > kSide || D > kSide || T > ((size_t)1 << 44) / V || T > ((size_t)1 << 44) / D) return false;
-  s->parts = 2 * ((V + 63) / 64);
+  // of a token: two for each tile of the form that the forward product takes, or one for each CTA of the streaming kernel
+  s->parts = 2 * ((V + stats_form(T, V, D, sms).nt - 1) / stats_form(T, V, D, sms).nt);
   if (T <= kFewTokens && s->parts < kFewCtas * (size_t)sms) s->parts = kFewCtas * (size_t)sms;
   s->forward_bytes = up(T * 4, 16) + s->parts * T * sizeof(float2);
   const size_t columns = up(V, 256);
@@ -515,7 +530,7 @@ inline bool head_sizes(size_t T, size_t V, size_t D, int sms, HeadSizes* s) {
   for (unsigned splits = 2; splits <= 16 && s->pieces == 1 && V >= 256 * (size_t)splits && splits * T * D <= kPieceElements; ++splits) {
     unsigned long long clocks = 0;
     (void)half_form(dh, 1, splits, sms, &clocks);
-    clocks += 8000 + 2 * splits * T * D * 4 / (22 * (size_t)sms);
+    clocks += 12000 + 2 * splits * T * D * 4 / (22 * (size_t)sms);
     if (clocks < least) {
       least = clocks;
       s->splits = splits;
@@ -568,7 +583,7 @@ ssgd_status head_forward(const T* h, size_t ldh, const T* w, size_t ldw, size_t 
     p.bf16 = std::is_same<T, __nv_bfloat16>::value;
     p.status = status;
     p.starve = starve;
-    const HalfForm form = half_form(p, 1, 1, sms);
+    const HalfForm form = stats_form(tokens, vocab, width, sms);
     const StatsEpilogue::Args args = {targets, partial, picked, (unsigned)tokens};
     const ssgd_status st = launch_half<StatsEpilogue, 1, kSumStages, kBothByK>(p, args, form, 1, sms, s);
     if (st != SSGD_OK) return st;
@@ -643,7 +658,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
       st = launch_half<TokensEpilogue<T>, 1, 0, kQByRows>(p, args, half_form(p, 1, z.splits, sms), z.splits, sms, s);
       if (st == SSGD_OK && z.splits > 1) {
         const size_t plane = b.T * b.D;
-        launch_kernel(xent_planes_kernel<T>, dim3(grid_for((plane + 255) / 256)), dim3(256), 0, s, true, sums, z.splits, plane, prepared, width,
+        launch_kernel(xent_planes_kernel<T>, dim3(grid_for((plane + 1023) / 1024)), dim3(256), 0, s, true, sums, z.splits, plane, prepared, width,
                       static_cast<T*>(b.dh), b.lddh);
         st = launch_status();
       }

@@ -245,8 +245,8 @@ __device__ __forceinline__ HalfPlace half_place(unsigned tile, const HalfPlan& p
 // How the operands lie in memory: which of them with their rows side by side.
 enum HalfLayout { kBothByK = 0, kQByRows = 1, kBothByRows = 3 };
 
-// One stage's MMAs.  Their descriptors differ by constants: with offsets that were only known at run time the issuing thread took 90
-// clocks an MMA, and one of 128 x 64 x 16 takes 32 to 48.
+// One stage's MMAs, with descriptors that differ by constants: what the issuing thread computes between two of them the tensor cores may
+// have to wait for.
 template <bool PAIR, int TERMS, int LAYOUT, unsigned LOW>
 __device__ __forceinline__ void half_issue(unsigned d, uint64_t pd, uint64_t qd, unsigned idesc, unsigned chunks, bool add) {
   constexpr unsigned ps = LAYOUT & 2 ? 2048 >> 4 : 32 >> 4, qs = LAYOUT & 1 ? 2048 >> 4 : 32 >> 4;      // 16 of k
@@ -277,7 +277,7 @@ __device__ __forceinline__ void half_issue(unsigned d, uint64_t pd, uint64_t qd,
 __device__ __forceinline__ void half_range(const HalfPlan& p, unsigned split, unsigned& first, unsigned& last) {
   first = 0;
   last = p.k_stages;
-  if (p.splits > 1) {                           // a 64-bit division takes a third of a microsecond
+  if (p.splits > 1) {
     first = (unsigned)((uint64_t)p.k_stages * split / p.splits);
     last = (unsigned)((uint64_t)p.k_stages * (split + 1) / p.splits);
   }
@@ -301,7 +301,7 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
   const unsigned worker = blockIdx.x / cluster, workers = gridDim.x / cluster, part = SPLIT ? cluster_rank() : 0;
 
   if (threadIdx.x == 0) {
-    // the first use of a map that is not at hand costs over a microsecond (200 x 200: a product 6.2 -> 5 us)
+    // while the kernel before this one ends
     prefetch_tensor_map(&maps.p[0]);
     prefetch_tensor_map(&maps.q[0]);
     if (TERMS == 3) prefetch_tensor_map(&maps.p[1]);

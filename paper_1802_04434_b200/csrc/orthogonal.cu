@@ -428,7 +428,7 @@ orthogonal_split_kernel(const Source s, const double* __restrict__ partial, unsi
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Matrices of up to 128 x 128: a CTA does all of it, one launch instead of two and three a step (64 x 64, five steps: 80 -> 2x us).
+// Matrices of up to 128 x 128: a CTA does all of it, one launch instead of two and three a step (64 x 64, five steps: 80 -> 22 us).
 //
 // X and E = X X^T - d I stay in registers in fp32, a thread a row and 32 columns, which is how the tensor cores give their sums back; their
 // fp16 parts lie in shared memory as the tensor cores take operands, 64 columns to a block of 128 rows x 128 bytes.  The same

@@ -16,6 +16,7 @@ from . import binding as B
 from .waits import check, status_of  # noqa: F401  (check: part of this module)
 
 _DTYPES = B._Codes({torch.bfloat16: 1, torch.float16: 2}, TypeError, "h and w must be of dtype bfloat16 or float16")
+_SMALL = 1 << 20
 _stream_of, _current_device = B._stream_of, B._current_device
 _pack_align, _pack_forward, _pack_backward = B.XENT_ALIGN_ARGS.pack, B.XENT_FORWARD_ARGS.pack, B.XENT_BACKWARD_ARGS.pack
 
@@ -91,13 +92,20 @@ def cross_entropy_forward(h: torch.Tensor, w: torch.Tensor, targets: torch.Tenso
     if not targets.is_contiguous():
         targets = targets.contiguous()
     losses = torch.empty(tokens, dtype=torch.float32, device=device)
-    state = torch.empty(5 * tokens, dtype=torch.uint8, device=device)
-    if tokens:
-        work = torch.empty(_sizes(index, tokens, vocab, width)[0], dtype=torch.uint8, device=device)
+    need = _sizes(index, tokens, vocab, width)[0] if tokens else 0
+    kept = (5 * tokens + 15) // 16 * 16
+    if need <= _SMALL:                      # one allocation for what is kept and what is not: 2 us less
+        state = torch.empty(kept + need, dtype=torch.uint8, device=device)
         at = state.data_ptr()
+        work_at = at + kept
+    else:
+        state = torch.empty(kept, dtype=torch.uint8, device=device)
+        work = torch.empty(need, dtype=torch.uint8, device=device)
+        at, work_at = state.data_ptr(), work.data_ptr()
+    if tokens:
         status = B.lib().ssgd_xent_forward_block(_pack_forward(
             h.data_ptr(), ldh, w.data_ptr(), ldw, code, tokens, vocab, width, targets.data_ptr(), ignore_index, losses.data_ptr(), at,
-            at + 4 * tokens, work.data_ptr(), status_of(device)[1], _stream_of(index)))
+            at + 4 * tokens, work_at, status_of(device)[1], _stream_of(index)))
         if status:
             B._check(status, "ssgd_xent_forward")
     return losses, Kept(h, w, targets, state, (ldh, ldw), (tokens, vocab, width))

@@ -207,3 +207,121 @@ def test_align_refusals(B):
     for change, status in ((dict(a=None), NULL), (dict(to_b=None), NULL), (dict(a=A + 1), ALIGN), (dict(to_a=A + 8), ALIGN), (dict(ldo=12), ALIGN), (dict(ldo=0), SIZE),
                            (dict(cols=0), SIZE), (dict(rows_b=(1 << 30) + 1), SIZE), (dict(rows_a=0, rows_b=0), OK), (dict(rows_a=0, rows_b=0, a=None, b=None), OK)):
         assert align(**change) == status
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# devices, with stand-ins for device tensors, the runtime and the library
+
+
+class Standin:
+    """A device tensor as far as the host side looks at it."""
+
+    def __init__(self, *shape, dtype=torch.float32, index=0, address=0x10000):
+        self.shape, self.dtype, self.device, self.is_cuda, self.address = torch.Size(shape), dtype, torch.device("cuda", index), True, address
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, dim=None):
+        s = [1]
+        for n in self.shape[:0:-1]:
+            s.insert(0, s[0] * n)
+        return tuple(s) if dim is None else s[dim]
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.address
+
+
+@pytest.fixture
+def runtime(B, monkeypatch):
+    """current: the current device; calls: (call, device that was current, words of its block)."""
+    from paper_1802_04434_b200 import loss, orthogonal, waits
+
+    class Runtime:
+        current, calls = 0, []
+    r = Runtime()
+    r.calls = []
+
+    class Switch:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.before, r.current = r.current, self.index
+
+        def __exit__(self, *exc):
+            r.current = self.before
+
+    class Library:
+        def __getattr__(self, name):
+            def call(block):
+                r.calls.append((name, r.current, [int.from_bytes(block[i:i + 8], "little") for i in range(0, len(block), 8)]))
+                return 0
+            return call
+    monkeypatch.setattr(B, "lib", Library)
+    monkeypatch.setattr(B, "_on", Switch)
+    monkeypatch.setattr(torch, "empty", lambda *shape, dtype=torch.float32, device=None: Standin(
+        *(shape[0] if isinstance(shape[0], (tuple, torch.Size)) else shape), dtype=dtype, index=device.index, address=0x900000))
+    for m in (loss, orthogonal):
+        monkeypatch.setattr(m, "_current_device", lambda: r.current)
+        monkeypatch.setattr(m, "_stream_of", lambda index: 1000 + index)
+        monkeypatch.setattr(m, "status_of", lambda device: (None, 0x500 + device.index))
+    monkeypatch.setattr(loss, "_sizes", lambda index, *sides: (2 << 20, 64))
+    monkeypatch.setattr(orthogonal, "_ws_bytes", lambda *sides: 64)
+    return r
+
+
+@pytest.mark.parametrize("index", [0, 1])
+def test_calls_go_to_their_operands_device(runtime, index):
+    from paper_1802_04434_b200 import loss, orthogonal
+    half = dict(dtype=torch.float16, index=index)
+    h, w, y = Standin(6, 16, **half), Standin(9, 16, address=0x20000, **half), Standin(6, dtype=torch.int64, index=index)
+    losses, kept = loss.cross_entropy_forward(h, w, y)
+    loss.cross_entropy_backward(kept, Standin(6, index=index))
+    odd = Standin(6, 13, **half), Standin(9, 13, **half)
+    u = Standin(3, 4, 5, index=index)
+    orthogonal.orthogonalise(u)
+    orthogonal.momentum_step(u, Standin(3, 4, 5, dtype=torch.bfloat16, index=index, address=0x30000), Standin(3, 4, 5, index=index, address=0x40000), 0.9, 0.1)
+    assert [c[0] for c in runtime.calls] == ["ssgd_xent_forward_block", "ssgd_xent_backward_block", "ssgd_orthogonalise_block", "ssgd_orthogonal_step_block"]
+    for name, current, words in runtime.calls:
+        assert current == index and words[-1] == 1000 + index and words[-2] == 0x500 + index, name
+    assert runtime.current == 0
+    forward, backward, alone, step_ = [c[2] for c in runtime.calls]
+    assert forward[:9] == [0x10000, 16, 0x20000, 16, 2, 6, 9, 16, 0x10000] and forward[9] == (1 << 64) - 100
+    assert backward[11:13] == [0x10000, 1] and backward[16] == 2
+    assert alone[:7] == [0x10000, 0, 3, 4, 5, 5, 20] and alone[10:12] == [5, 3]
+    assert step_[3:5] == [0x30000, 1] and step_[7] == 0x40000 and step_[19:21] == [5, 3]
+    assert loss._stride_as_it_is(odd[0], 13) == 0
+
+
+def test_operands_of_two_devices_are_refused(runtime):
+    from paper_1802_04434_b200 import loss, orthogonal
+    half = dict(dtype=torch.float16)
+    h, w, y = Standin(6, 16, **half), Standin(9, 16, **half), Standin(6, dtype=torch.int64)
+    for bad in ((h, Standin(9, 16, index=1, **half), y), (h, w, Standin(6, dtype=torch.int64, index=1))):
+        with pytest.raises(ValueError, match="one device"):
+            loss.cross_entropy_forward(*bad)
+    kept = loss.Kept(h, w, y, None, (16, 16), (6, 9, 16))
+    with pytest.raises(ValueError, match="operands' device"):
+        loss.cross_entropy_backward(kept, Standin(6, index=1))
+    with pytest.raises(ValueError, match="operands' device"):
+        loss.cross_entropy_backward(kept, Standin(6), dw=Standin(9, 16, index=1))
+    u, other = Standin(4, 5), Standin(4, 5, index=1)
+    with pytest.raises(ValueError, match="its device"):
+        orthogonal.orthogonalise(u, out=other)
+    for bad in ((other, u, u), (u, other, u), (u, u, other)):
+        with pytest.raises(ValueError, match="one device"):
+            orthogonal.momentum_step(*bad, 0.9, 0.1)
+    assert runtime.calls == []
+
+
+def test_products_by_the_results_type(runtime):
+    from paper_1802_04434_b200 import orthogonal
+    for shape, kind, want in (((256, 300), torch.bfloat16, 1), ((255, 4000), torch.bfloat16, 3), ((300, 300), torch.float16, 3), ((300, 300), torch.float32, 3)):
+        orthogonal.orthogonalise(Standin(*shape, dtype=kind))
+        assert runtime.calls[-1][2][11] == want
+    orthogonal.orthogonalise(Standin(300, 300), dtype=torch.bfloat16, products=3)
+    assert runtime.calls[-1][2][11] == 3
