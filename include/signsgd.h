@@ -482,8 +482,8 @@ ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t*
  * The logits are never in memory: a tile at a time, forward and once more backward.  A token whose target is `ignore` has
  * loss 0 and no part in any gradient (its row of dh is 0), whatever its row of h and its g hold, NaN included.  Any
  * other target outside 0 .. V-1 gives NaN, the loss and the gradients that it reaches.  Logits, statistics, losses and sums are
- * fp32; dz is rounded to the type of h and w (fp16: times a power of two that brings the largest |g| to 2^14 .. 2^15)
- * before the products of the gradients.  Sums go in a fixed order: equal inputs give equal bits.
+ * fp32; dz, divided by the largest |g| (and times 2^14 in fp16), is rounded to the type of h and w before the
+ * products of the gradients, which are multiplied by it again.  Sums go in a fixed order: equal inputs give equal bits.
  *   h, w      DEVICE, SSGD_BF16 or SSGD_F16, both the same; 16-byte aligned, rows of stride ldh, ldw >= D, multiples of 8
  *   targets   DEVICE int64 [T], 8-byte aligned
  *   ws        DEVICE, bytes as ssgd_xent_sizes says (for the current device), 16-byte aligned; calls that may run at the same time need one each

@@ -8,8 +8,9 @@
 //             to the operands' type, which is what the two products take that follow: dh += dz w, dw = dz^T h (no operand
 //             is transposed in memory, the products read them either way)
 // Statistics, losses and all sums are fp32; dz is the one rounding to 16 bits, as large as that of the gradients
-// themselves.  An fp16 dz is scaled by a power of two, so that the largest |g| lies just below 2^15: a gradient of
-// 1/tokens times a probability would be below fp16's range.
+// themselves.  It is divided by the largest |g|, and the products' sums are multiplied by it: tokens that all have the same g (a
+// mean, a sum) have a 1 there, so that the target's entry, p - 1, is -1 or close to it and loses little or nothing, where
+// -g would be off by the same part of itself for all tokens, up to 2^-8.  In fp16 times 2^14 besides, to keep small probabilities.
 
 #include "half_product.cuh"
 
@@ -259,14 +260,14 @@ xent_join_kernel(const float2* __restrict__ partial, const float* __restrict__ p
 // ---------------------------------------------------------------------------------------------------------------------
 // Backward.
 
-// Before the products: the scale of an fp16 dz, and, only where an ignored token's row of h is not finite, a copy of h with the
+// Before the products: the scale of dz, and, only where an ignored token's row of h is not finite, a copy of h with the
 // ignored rows zero, which dw's product then takes for h.
 struct Prepared {
   unsigned copied;              // h's copy is to be taken
-  float scale, unscale;         // of dz: powers of two, 1 for bf16
+  float scale, unscale;         // of dz
   unsigned unused;
 };
-template <typename T, bool SCALED>
+template <typename T>
 __global__ void __launch_bounds__(256)
 xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__ g, size_t g_stride, unsigned tokens, const T* __restrict__ h, size_t ldh,
                     unsigned width, T* __restrict__ copy, size_t ldc, Prepared* __restrict__ out) {
@@ -278,23 +279,25 @@ xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__
   bad = __syncthreads_or((int)bad) != 0;
   if (blockIdx.x == 0) {
     unsigned top = 0;                                       // |g|'s bits are ordered as |g| is
-    if (SCALED) {
-      for (unsigned t = threadIdx.x; t < tokens; t += 256)
-        if (kinds[t] == kCounts) top = max(top, __float_as_uint(g[t * g_stride]) & 0x7FFFFFFFu);
-      top = __reduce_max_sync(0xFFFFFFFFu, top);
-      if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = top;
-      __syncthreads();
-      for (unsigned k = 0; k < 8; ++k) top = max(top, part[k]);
-    }
+    for (unsigned t = threadIdx.x; t < tokens; t += 256)
+      if (kinds[t] == kCounts) top = max(top, __float_as_uint(g[t * g_stride]) & 0x7FFFFFFFu);
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = top;
+    __syncthreads();
+    for (unsigned k = 0; k < 8; ++k) top = max(top, part[k]);
     if (threadIdx.x == 0) {
-      // top = m 2^e, 1 <= m < 2: times 2^(14 - e) it lies in [2^14, 2^15); exponents kept where both powers are fp32 numbers
-      int e = SCALED && top >= 0x00800000u && top < 0x7F800000u ? 14 - ((int)(top >> 23) - 127) : 0;
-      if (SCALED && top > 0 && top < 0x00800000u) e = 126;
-      e = max(-126, min(126, e));
-      out->copied = bad;
-      out->scale = __uint_as_float((unsigned)(127 + e) << 23);
-      out->unscale = __uint_as_float((unsigned)(127 - e) << 23);
-      out->unused = 0;
+      constexpr float kTop = std::is_same<T, __half>::value ? 16384.0f : 1.0f;
+      const float most = __uint_as_float(top);
+      Prepared p = {bad, 1.0f, 1.0f, 0};
+      if (most >= 7.9e-31f && most <= 1.3e36f) {            // 2^-100 .. 2^120: both factors are fp32 numbers
+        p.scale = __fdiv_rn(kTop, most);
+        p.unscale = most * (1.0f / kTop);
+      } else if (top > 0 && top < 0x7F800000u) {            // out there by a power of two
+        const int e = most < 1.0f ? 120 : -100;
+        p.scale = __uint_as_float((unsigned)(127 + e) << 23);
+        p.unscale = __uint_as_float((unsigned)(127 - e) << 23);
+      }
+      *out = p;
     }
   }
   if (!bad) return;
@@ -631,7 +634,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
   T *copy = reinterpret_cast<T*>(b.ws + z.copy), *dz = reinterpret_cast<T*>(b.ws + z.dz);
   float* sums = reinterpret_cast<float*>(b.ws + z.sums);
   const unsigned tokens = (unsigned)b.T, width = (unsigned)b.D;
-  launch_kernel(xent_prepare_kernel<T, !kBf16>, dim3(tokens < (unsigned)sms * 4 ? tokens : (unsigned)sms * 4), dim3(256), 0, s, true, b.kinds, b.g, b.g_stride,
+  launch_kernel(xent_prepare_kernel<T>, dim3(tokens < (unsigned)sms * 4 ? tokens : (unsigned)sms * 4), dim3(256), 0, s, true, b.kinds, b.g, b.g_stride,
                 tokens, h, b.ldh, width, copy, z.copy_ld, prepared);
   ssgd_status st = launch_status();
   for (size_t first = 0; st == SSGD_OK && first < b.V; first += z.piece) {
