@@ -89,7 +89,14 @@ struct GramEpilogue {
       float sum = 1.0f;
       if (a.squares) {
         sum = 0.0f;
-        for (unsigned i = box.lane; i < a.count; i += 32) sum += a.squares[(size_t)matrix * a.count + i];
+        const float* from = a.squares + (size_t)matrix * a.count;
+        for (unsigned i = box.lane; i < a.count; i += 16 * 32) {      // sixteen in flight: the products wait behind this
+          float v[16];
+#pragma unroll
+          for (unsigned u = 0; u < 16; ++u) v[u] = i + u * 32 < a.count ? from[i + u * 32] : 0.0f;
+#pragma unroll
+          for (unsigned u = 0; u < 16; ++u) sum += v[u];
+        }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       }
