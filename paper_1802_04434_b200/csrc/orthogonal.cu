@@ -299,51 +299,82 @@ struct Source {
 };
 enum { kPlainSource, kMomentum };
 
-// Eight elements of a row, `left` of them inside, zeros behind.
+// Eight elements of a row as they lie in memory, `left` of them inside, zeros behind; and their values.
 template <typename T>
-__device__ __forceinline__ void source_load(const T* p, unsigned left, bool eights, float (&v)[8]) {
+struct Eight { uint4 q[sizeof(T) / 2]; };
+template <typename T>
+__device__ __forceinline__ void source_load(const T* p, unsigned left, bool eights, Eight<T>& e) {
   if (eights && left >= 8) {
-    load8(p, v);
-  } else {
 #pragma unroll
-    for (unsigned i = 0; i < 8; ++i) v[i] = i < left ? to_float(p[i]) : 0.0f;
+    for (unsigned i = 0; i < sizeof(T) / 2; ++i) e.q[i] = reinterpret_cast<const uint4*>(p)[i];
+  } else {
+    unsigned w[2 * sizeof(T)];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (unsigned i = 0; i < 8; ++i) w[i] = i < left ? __float_as_uint(p[i]) : 0u;
+    } else {
+      const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+      for (unsigned i = 0; i < 4; ++i) w[i] = (2 * i < left ? h[2 * i] : 0u) | (2 * i + 1 < left ? (unsigned)h[2 * i + 1] << 16 : 0u);
+    }
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 2; ++i) e.q[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void eight_values(const Eight<T>& e, float (&v)[8]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (unsigned i = 0; i < 2; ++i) {
+      v[4 * i] = __uint_as_float(e.q[i].x); v[4 * i + 1] = __uint_as_float(e.q[i].y);
+      v[4 * i + 2] = __uint_as_float(e.q[i].z); v[4 * i + 3] = __uint_as_float(e.q[i].w);
+    }
+  } else {
+    v[0] = low_to_float(T(), e.q[0].x); v[1] = high_to_float(T(), e.q[0].x); v[2] = low_to_float(T(), e.q[0].y); v[3] = high_to_float(T(), e.q[0].y);
+    v[4] = low_to_float(T(), e.q[0].z); v[5] = high_to_float(T(), e.q[0].z); v[6] = low_to_float(T(), e.q[0].w); v[7] = high_to_float(T(), e.q[0].w);
   }
 }
 
 // U at eight columns of a row, in two halves, so that several can be on their way; FIRST: m is brought forward and written.
-struct Fetched { float m[8], g[8]; };
+template <typename T>
+struct Fetched {
+  Eight<float> m;
+  Eight<T> g;
+};
 template <int KIND, bool FIRST, typename T>
-__device__ __forceinline__ void source_fetch(const Source& s, size_t matrix, unsigned row, unsigned column, Fetched& f) {
+__device__ __forceinline__ void source_fetch(const Source& s, size_t matrix, unsigned row, unsigned column, Fetched<T>& f) {
   const unsigned left = s.cols - column;
   if (KIND == kMomentum) source_load(s.m + matrix * s.m_stride + (size_t)row * s.ldm + column, left, s.eights, f.m);
   if (KIND == kPlainSource || FIRST || s.ahead) source_load(static_cast<const T*>(s.u) + matrix * s.u_stride + (size_t)row * s.ldu + column, left, s.eights, f.g);
 }
-template <int KIND, bool FIRST>
-__device__ __forceinline__ void source_values(const Source& s, size_t matrix, unsigned row, unsigned column, Fetched& f, float (&u)[8]) {
+template <int KIND, bool FIRST, typename T>
+__device__ __forceinline__ void source_values(const Source& s, size_t matrix, unsigned row, unsigned column, const Fetched<T>& f, float (&u)[8]) {
   if constexpr (KIND == kPlainSource) {
-#pragma unroll
-    for (unsigned i = 0; i < 8; ++i) u[i] = f.g[i];
+    eight_values(f.g, u);
   } else {
+    float m[8], g[8];
+    eight_values(f.m, m);
     if (FIRST || s.ahead) {
+      eight_values(f.g, g);
 #pragma unroll
-      for (unsigned i = 0; i < 8; ++i) f.g[i] = __fmul_rn(1.0f - s.beta, f.g[i]);
+      for (unsigned i = 0; i < 8; ++i) g[i] = __fmul_rn(1.0f - s.beta, g[i]);
     }
     if (FIRST) {
       float* mp = s.m + matrix * s.m_stride + (size_t)row * s.ldm + column;
       const unsigned left = s.cols - column;
 #pragma unroll
-      for (unsigned i = 0; i < 8; ++i) f.m[i] = __fmaf_rn(s.beta, f.m[i], f.g[i]);
+      for (unsigned i = 0; i < 8; ++i) m[i] = __fmaf_rn(s.beta, m[i], g[i]);
       if (s.eights && left >= 8) {
-        *reinterpret_cast<float4*>(mp) = make_float4(f.m[0], f.m[1], f.m[2], f.m[3]);
-        *reinterpret_cast<float4*>(mp + 4) = make_float4(f.m[4], f.m[5], f.m[6], f.m[7]);
+        *reinterpret_cast<float4*>(mp) = make_float4(m[0], m[1], m[2], m[3]);
+        *reinterpret_cast<float4*>(mp + 4) = make_float4(m[4], m[5], m[6], m[7]);
       } else {
 #pragma unroll
         for (unsigned i = 0; i < 8; ++i)
-          if (i < left) mp[i] = f.m[i];
+          if (i < left) mp[i] = m[i];
       }
     }
 #pragma unroll
-    for (unsigned i = 0; i < 8; ++i) u[i] = s.ahead ? __fmaf_rn(s.beta, f.m[i], f.g[i]) : f.m[i];
+    for (unsigned i = 0; i < 8; ++i) u[i] = s.ahead ? __fmaf_rn(s.beta, m[i], g[i]) : m[i];
   }
 }
 
@@ -353,10 +384,10 @@ constexpr unsigned kNormThreads = 256;
 // column is zero.
 template <int KIND, bool FIRST, typename T, typename F>
 __device__ __forceinline__ void each_eight(const Source& s, size_t matrix, F f) {
-  constexpr unsigned kBatch = KIND == kMomentum ? 2 : 4;
+  constexpr unsigned kBatch = KIND == kMomentum ? 2 : sizeof(T) == 2 ? 8 : 4;
   const unsigned eights = (s.cols + 7) / 8, total = eights * s.rows, step = gridDim.x * kNormThreads;
   for (unsigned i0 = blockIdx.x * kNormThreads + threadIdx.x; i0 < total; i0 += kBatch * step) {
-    Fetched v[kBatch];
+    Fetched<T> v[kBatch];
     unsigned row[kBatch];
 #pragma unroll
     for (unsigned b = 0; b < kBatch; ++b) {
@@ -370,7 +401,7 @@ __device__ __forceinline__ void each_eight(const Source& s, size_t matrix, F f) 
       if (i >= total) break;
       const unsigned column = (i - row[b] * eights) * 8;
       float u[8];
-      source_values<KIND, FIRST>(s, matrix, row[b], column, v[b], u);
+      source_values<KIND, FIRST, T>(s, matrix, row[b], column, v[b], u);
       f(row[b], column, u);
     }
   }
