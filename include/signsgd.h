@@ -482,7 +482,7 @@ ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t*
  * The logits are never in memory: a tile at a time, forward and once more backward.  A token whose target is `ignore` has
  * loss 0 and no part in any gradient (its row of dh is 0), whatever its row of h and its g hold, NaN included.  Any
  * other target outside 0 .. V-1 gives NaN, the loss and the gradients that it reaches.  Logits, statistics, losses and sums are
- * fp32; dz, divided by the largest |g| (and times 2^14 in fp16), is rounded to the type of h and w before the
+ * fp32; dz, divided by its largest entry (and times 2^14 in fp16), is rounded to the type of h and w before the
  * products of the gradients, which are multiplied by it again.  Sums go in a fixed order: equal inputs give equal bits.
  *   h, w      DEVICE, SSGD_BF16 or SSGD_F16, both the same; 16-byte aligned, rows of stride ldh, ldw >= D, multiples of 8
  *   targets   DEVICE int64 [T], 8-byte aligned
@@ -496,7 +496,8 @@ ssgd_status ssgd_xent_sizes(size_t T, size_t V, size_t D, size_t* forward_bytes,
 ssgd_status ssgd_xent_align(const void* a, size_t lda, size_t step_a, size_t rows_a, void* to_a, const void* b, size_t ldb,
                             size_t step_b, size_t rows_b, void* to_b, size_t cols, size_t ldo, void* stream);
 
-/*   losses, lse  out DEVICE float [T];  lse: log sum exp, for the backward pass
+/*   losses       out DEVICE float [T]
+ *   lse          out DEVICE float [2][T], for the backward pass: log sum exp, and the losses once more
  *   kinds        out DEVICE uint8 [T], for the backward pass: 0, or 1 for an ignored token, 2 where its row of h is not finite */
 ssgd_status ssgd_xent_forward(const void* h, size_t ldh, const void* w, size_t ldw, int dtype, size_t T, size_t V,
                               size_t D, const int64_t* targets, int64_t ignore, float* losses, float* lse,

@@ -8,8 +8,8 @@
 //             to the operands' type, which is what the two products take that follow: dh += dz w, dw = dz^T h (no operand
 //             is transposed in memory, the products read them either way)
 // Statistics, losses and all sums are fp32; dz is the one rounding to 16 bits, as large as that of the gradients
-// themselves.  It is divided by the largest |g|, and the products' sums are multiplied by it: tokens that all have the same g (a
-// mean, a sum) have a 1 there, so that the target's entry, p - 1, is -1 or close to it and loses little or nothing, where
+// themselves.  It is divided by its largest entry, a target's g (1 - p), and the products' sums are multiplied by it: where tokens have
+// the same g (a mean, a sum) and little idea of their targets, those entries are -1 or close to it and lose little or nothing, where
 // -g would be off by the same part of itself for all tokens, up to 2^-8.  In fp16 times 2^14 besides, to keep small probabilities.
 
 #include "half_product.cuh"
@@ -241,8 +241,10 @@ xent_join_kernel(const float2* __restrict__ partial, const float* __restrict__ p
     const bool ignored = y == ignore, inside = y >= 0 && y < (int64_t)vocab;
     // a target that is neither ignored nor in the vocabulary: NaN, here and in the gradients
     const float log_sum = logf(sum.y), l = inside || ignored ? sum.x + log_sum : __uint_as_float(0x7FC00000u);
-    losses[t] = ignored ? 0.0f : inside ? (sum.x - picked[t]) + log_sum : l;
+    const float loss = ignored ? 0.0f : inside ? (sum.x - picked[t]) + log_sum : l;
+    losses[t] = loss;
     lse[t] = l;
+    lse[tokens + t] = loss;
     if (!ignored) kinds[t] = kCounts;
   }
   // a warp for each ignored token
@@ -269,8 +271,8 @@ struct Prepared {
 };
 template <typename T>
 __global__ void __launch_bounds__(256)
-xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__ g, size_t g_stride, unsigned tokens, const T* __restrict__ h, size_t ldh,
-                    unsigned width, T* __restrict__ copy, size_t ldc, Prepared* __restrict__ out) {
+xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__ lse, const float* __restrict__ g, size_t g_stride, unsigned tokens,
+                    const T* __restrict__ h, size_t ldh, unsigned width, T* __restrict__ copy, size_t ldc, Prepared* __restrict__ out) {
   __shared__ unsigned part[8];
   pdl_launch_dependents();
   pdl_wait();
@@ -278,9 +280,10 @@ xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__
   for (unsigned t = threadIdx.x; t < tokens; t += 256) bad |= kinds[t] == kIgnoredNotFinite;
   bad = __syncthreads_or((int)bad) != 0;
   if (blockIdx.x == 0) {
-    unsigned top = 0;                                       // |g|'s bits are ordered as |g| is
+    unsigned top = 0;                                       // a magnitude's bits are ordered as it is
     for (unsigned t = threadIdx.x; t < tokens; t += 256)
-      if (kinds[t] == kCounts) top = max(top, __float_as_uint(g[t * g_stride]) & 0x7FFFFFFFu);
+      if (kinds[t] == kCounts)                              // probabilities below 2^-24 may be missing from a sum of 1; a loss of NaN leaves the others' factor alone
+        top = max(top, __float_as_uint(g[t * g_stride] * fmaxf(-expm1f(-lse[tokens + t]), 2.4e-7f)) & 0x7FFFFFFFu);
     top = __reduce_max_sync(0xFFFFFFFFu, top);
     if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = top;
     __syncthreads();
@@ -312,7 +315,7 @@ struct GradEpilogue {
   struct Args {
     CUtensorMap dz;             // [tokens][columns of this piece]
     const int64_t* targets;
-    const float* lse;
+    const float* lse;           // [2][tokens], see the join
     const float* g;
     const uint8_t* kinds;
     const Prepared* prepared;
@@ -321,7 +324,7 @@ struct GradEpilogue {
   };
   static constexpr unsigned kBox = 4096;      // two boxes in turn
   Box box;
-  float lse, g;
+  float lse, g, miss;           // miss: the target's probability less one
   int64_t target;
   unsigned row0, half;
   bool counts;
@@ -335,6 +338,8 @@ struct GradEpilogue {
     if (row >= a.tokens) return;
     counts = a.kinds[row] == kCounts;
     lse = a.lse[row];
+    // from the loss, -log p: a difference of probabilities would keep nothing of a token that is sure of its target
+    miss = expm1f(-a.lse[a.tokens + row]);
     g = a.g[row * a.g_stride] * a.prepared->scale;
     target = a.targets[row] - (int64_t)a.first;
   }
@@ -345,7 +350,7 @@ struct GradEpilogue {
       const int64_t at = target - (int64_t)column;
       if (at >= 0 && at < 32) {
 #pragma unroll
-        for (unsigned q = 0; q < 32; ++q) v[q] = (unsigned)at == q ? v[q] - 1.0f : v[q];
+        for (unsigned q = 0; q < 32; ++q) v[q] = (unsigned)at == q ? miss : v[q];
       }
 #pragma unroll
       for (unsigned q = 0; q < 32; ++q) v[q] *= g;
@@ -634,7 +639,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
   T *copy = reinterpret_cast<T*>(b.ws + z.copy), *dz = reinterpret_cast<T*>(b.ws + z.dz);
   float* sums = reinterpret_cast<float*>(b.ws + z.sums);
   const unsigned tokens = (unsigned)b.T, width = (unsigned)b.D;
-  launch_kernel(xent_prepare_kernel<T>, dim3(tokens < (unsigned)sms * 4 ? tokens : (unsigned)sms * 4), dim3(256), 0, s, true, b.kinds, b.g, b.g_stride,
+  launch_kernel(xent_prepare_kernel<T>, dim3(tokens < (unsigned)sms * 4 ? tokens : (unsigned)sms * 4), dim3(256), 0, s, true, b.kinds, b.lse, b.g, b.g_stride,
                 tokens, h, b.ldh, width, copy, z.copy_ld, prepared);
   ssgd_status st = launch_status();
   for (size_t first = 0; st == SSGD_OK && first < b.V; first += z.piece) {

@@ -58,7 +58,7 @@ class Kept(NamedTuple):
     h: torch.Tensor             # [tokens][..], as the kernels read it
     w: torch.Tensor
     targets: torch.Tensor
-    state: torch.Tensor         # log sum exp and kind of each token
+    state: torch.Tensor         # log sum exp, loss and kind of each token
     ld: Tuple[int, int]         # row strides of h and w
     sides: Tuple[int, int, int]
 
@@ -93,7 +93,7 @@ def cross_entropy_forward(h: torch.Tensor, w: torch.Tensor, targets: torch.Tenso
         targets = targets.contiguous()
     losses = torch.empty(tokens, dtype=torch.float32, device=device)
     need = _sizes(index, tokens, vocab, width)[0] if tokens else 0
-    kept = (5 * tokens + 15) // 16 * 16
+    kept = (9 * tokens + 15) // 16 * 16
     if need <= _SMALL:                      # one allocation for what is kept and what is not: 2 us less
         state = torch.empty(kept + need, dtype=torch.uint8, device=device)
         at = state.data_ptr()
@@ -105,7 +105,7 @@ def cross_entropy_forward(h: torch.Tensor, w: torch.Tensor, targets: torch.Tenso
     if tokens:
         status = B.lib().ssgd_xent_forward_block(_pack_forward(
             h.data_ptr(), ldh, w.data_ptr(), ldw, code, tokens, vocab, width, targets.data_ptr(), ignore_index, losses.data_ptr(), at,
-            at + 4 * tokens, work_at, status_of(device)[1], _stream_of(index)))
+            at + 8 * tokens, work_at, status_of(device)[1], _stream_of(index)))
         if status:
             B._check(status, "ssgd_xent_forward")
     return losses, Kept(h, w, targets, state, (ldh, ldw), (tokens, vocab, width))
@@ -143,7 +143,7 @@ def cross_entropy_backward(kept: Kept, g: torch.Tensor, dw: Optional[torch.Tenso
         at = kept.state.data_ptr()
         status = B.lib().ssgd_xent_backward_block(_pack_backward(
             kept.h.data_ptr(), kept.ld[0], kept.w.data_ptr(), kept.ld[1], _DTYPES[kept.h.dtype], tokens, vocab, width, kept.targets.data_ptr(), at,
-            at + 4 * tokens, g.data_ptr(), g.stride(0), dh.data_ptr() if want_h else 0, width, dw.data_ptr() if want_w else 0, code,
+            at + 8 * tokens, g.data_ptr(), g.stride(0), dh.data_ptr() if want_h else 0, width, dw.data_ptr() if want_w else 0, code,
             (dw.stride(0) if vocab > 1 else width) if want_w else width, work.data_ptr(), status_of(device)[1], _stream_of(index)))
         if status:
             B._check(status, "ssgd_xent_backward")

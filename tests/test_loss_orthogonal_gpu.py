@@ -220,9 +220,69 @@ def test_extreme_logits(loss):
     assert bool(losses.isnan().all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("T", [1, 2, 6, 200])
+def test_tokens_that_are_sure(loss, T, dtype):
+    # 1 - p between 1e-3 and 1e-6: the loss and the target's entry of dz are that small, and still themselves
+    r = gen(T)
+    w = torch.randn(120, 256, generator=r, device="cuda").mul_(0.02)
+    y = torch.randint(0, 120, (T,), generator=r, device="cuda")
+    h = (14 + 4 * torch.rand(T, 1, generator=r, device="cuda")) * w[y] / w[y].square().sum(1, keepdim=True) + torch.randn(T, 256, generator=r, device="cuda") * 0.1
+    h, w = h.to(dtype), w.to(dtype)
+    one = torch.ones(T, device="cuda")
+    losses, kept = loss.cross_entropy_forward(h, w, y)
+    dh, dw = loss.cross_entropy_backward(kept, one, dw_dtype=F32)
+    z = h.double() @ w.double().t()
+    p = torch.softmax(z, 1)
+    p[torch.arange(T), y] = 0
+    miss = p.sum(1)
+    assert float(miss.max()) < 1e-3
+    # sums of exponentials are 1 and a little: 2^-24 of them for each of up to 120 terms is 120 * 2^-24 / miss of the little, at the worst; logits as in the bounds of ref
+    S = (h.double().abs() @ w.double().abs().t()).amax(1)
+    error = 32 * 2.0 ** -23 + 4 * (2 * 256 / 16 + 34) * 2.0 ** -23 * S + 2.0 ** -19
+    assert ((losses.double() + torch.log1p(-miss)).abs() <= error * miss + 120 * 2.0 ** -24).all()
+    p[torch.arange(T), y] = -miss
+    part = (error * miss + 120 * 2.0 ** -24)[:, None] + 0 * p
+    within(dw, p.t() @ h.double(), (part + ref.HALF_STEP[dtype] * p.abs() + 2.0 ** -38).t() @ h.double().abs() * 1.01, "dw")
+    if dtype == BF16:
+        dz_tol = torch.where(p < 0, part, error[:, None] * p) + 2.0 ** -8 * p.abs()
+        within(dh, p @ w.double(), dz_tol @ w.double().abs() * 1.01 + 2.0 ** -8 * (p @ w.double()).abs() + 2.0 ** -130, "dh")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_a_sure_token_of_large_gradient_beside_others(loss, dtype):
+    # the sure token's loss is 0 or next to it, so its entry says nothing of how large the others of its row are
+    T, V, D = 6, 300, 256
+    h, w, y, _ = problem(T, V, D, dtype)
+    h[0] = w[y[0]] * (17 / w[y[0]].double().square().sum()).to(dtype)
+    g = torch.full((T,), 1e-6, device="cuda")
+    g[0] = 1.0
+    losses, kept = loss.cross_entropy_forward(h, w, y)
+    dh, dw = loss.cross_entropy_backward(kept, g, dw_dtype=F32)
+    want, tol = ref.loss_and_gradients(h, w, y, g)
+    within(dh, want[1], tol[1], "dh")
+    within(dw, want[2], tol[2], "dw")
+
+
+def test_a_row_that_is_not_a_number_leaves_the_others(loss):
+    h, w, y, g = problem(9, 300, 64, F16)
+    _, kept = loss.cross_entropy_forward(h, w, y)
+    before = loss.cross_entropy_backward(kept, g)[0]
+    bad = h.clone()
+    bad[4, 3] = float("nan")
+    g[4] = 1e-3 * g[4]
+    _, kept = loss.cross_entropy_forward(bad, w, y)
+    dh, _ = loss.cross_entropy_backward(kept, g)
+    rest = [t for t in range(9) if t != 4]
+    assert dh[4].isnan().all() and not dh[rest].isnan().any()
+    want, tol = ref.loss_and_gradients(h, w, y, g)
+    within(dh[rest], want[1][rest], tol[1][rest], "dh")
+    within(before[rest], want[1][rest], tol[1][rest], "before")
+
+
 @pytest.mark.parametrize("scale", [1e-30, 1e-8, 1.0, 1e4, 1e30])
 def test_gradients_of_any_size_scale_fp16(loss, scale):
-    # dz in fp16 is scaled to the largest |g|; what comes out overflows or vanishes only where the result does
+    # dz in fp16 is scaled to its largest entry; what comes out overflows or vanishes only where the result does
     h, w, y, g = problem(50, 60, 64, F16)
     losses, kept = loss.cross_entropy_forward(h, w, y)
     _, dw = loss.cross_entropy_backward(kept, g * scale, dw_dtype=F32)
@@ -385,7 +445,7 @@ def test_waits_that_run_out(loss, orthogonal):
     from paper_1802_04434_b200 import binding as B
     h, w, y, g = problem(200, 200, 128, BF16, ignored=0.0)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
-    losses, lse, kinds = torch.zeros(200, device="cuda"), torch.zeros(200, device="cuda"), torch.zeros(200, dtype=torch.uint8, device="cuda")
+    losses, lse, kinds = torch.zeros(200, device="cuda"), torch.zeros(400, device="cuda"), torch.zeros(200, dtype=torch.uint8, device="cuda")
     ws = torch.zeros(B.xent_sizes(200, 200, 128)[0], dtype=torch.uint8, device="cuda")
     stream = torch.cuda.current_stream().cuda_stream
     assert B.lib().ssgd_xent_wait_selftest(h.data_ptr(), 128, w.data_ptr(), 128, 1, 200, 200, 128, y.data_ptr(), -100, losses.data_ptr(), lse.data_ptr(),
