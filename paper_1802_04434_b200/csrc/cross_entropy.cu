@@ -277,13 +277,25 @@ xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__
   pdl_launch_dependents();
   pdl_wait();
   unsigned bad = 0;
+#pragma unroll 8
   for (unsigned t = threadIdx.x; t < tokens; t += 256) bad |= kinds[t] == kIgnoredNotFinite;
   bad = __syncthreads_or((int)bad) != 0;
   if (blockIdx.x == 0) {
     unsigned top = 0;                                       // a magnitude's bits are ordered as it is
-    for (unsigned t = threadIdx.x; t < tokens; t += 256)
-      if (kinds[t] == kCounts)                              // probabilities below 2^-24 may be missing from a sum of 1; a loss of NaN leaves the others' factor alone
-        top = max(top, __float_as_uint(g[t * g_stride] * fmaxf(-expm1f(-lse[tokens + t]), 2.4e-7f)) & 0x7FFFFFFFu);
+    for (unsigned t0 = threadIdx.x; t0 < tokens; t0 += 8 * 256) {      // eight in flight: one CTA, and the products wait for it
+      float loss[8], of[8];
+      bool counts[8];
+#pragma unroll
+      for (unsigned u = 0; u < 8; ++u) {
+        const unsigned t = t0 + u * 256;
+        counts[u] = t < tokens && kinds[t] == kCounts;
+        loss[u] = t < tokens ? lse[tokens + t] : 0.0f;
+        of[u] = t < tokens ? g[t * g_stride] : 0.0f;
+      }
+#pragma unroll
+      for (unsigned u = 0; u < 8; ++u)                      // probabilities below 2^-24 may be missing from a sum of 1; a loss of NaN leaves the others' factor alone
+        if (counts[u]) top = max(top, __float_as_uint(of[u] * fmaxf(-expm1f(-loss[u]), 2.4e-7f)) & 0x7FFFFFFFu);
+    }
     top = __reduce_max_sync(0xFFFFFFFFu, top);
     if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = top;
     __syncthreads();
