@@ -266,7 +266,7 @@ struct UpdateEpilogue {
       const unsigned rows = min(32u, a.rows - row0);
       if constexpr (TO == kOut) whole.rows_out(o, a.ldo, rows, left, v);
       else whole.rows_join(o, a.ldo, o, a.ldo, rows, left, v, [](float x, float step) { return x + step; });
-      __syncwarp();
+      box.fence();                              // the threads' own writes come before the copy that is asked for next into the same bytes
     }
     reader.done(box, a.x.high, &a.x.low, row0, matrix);
   }
