@@ -7,8 +7,8 @@
 //   backward  by pieces of the vocabulary: the logits' tiles once more, this time to dz = g (exp(z - lse) - [v = y]), rounded
 //             to the operands' type, which is what the two products take that follow: dh += dz w, dw = dz^T h (no operand
 //             is transposed in memory, the products read them either way)
-// Statistics, losses and all sums are fp32; dz is the one rounding to 16 bits, as large as that of the gradients
-// themselves.  It is divided by its largest entry, a target's g (1 - p), and the products' sums are multiplied by it: where tokens have
+// Statistics, losses and all sums are fp32, sums in parts (kSumStages, kGradientStages); dz is the one rounding to 16 bits, as large as that of the
+// gradients themselves.  It is divided by its largest entry, a target's g (1 - p), and the products' sums are multiplied by it: where tokens have
 // the same g (a mean, a sum) and little idea of their targets, those entries are -1 or close to it and lose little or nothing, where
 // -g would be off by the same part of itself for all tokens, up to 2^-8.  In fp16 times 2^14 besides, to keep small probabilities.
 
@@ -512,7 +512,13 @@ constexpr size_t kSide = (size_t)1 << 30;
 inline size_t up(size_t n, size_t k) { return (n + k - 1) / k * k; }
 
 // Stages between two times that a logit's sum is taken (each takes the threads 1500 clocks of 256 columns; four: 102 us for 2048 x 30522 x 1024).
+// The backward pass makes its logits by the same parts: what they are off beyond the forward pass's, whose log sum exp is taken from them, would be
+// a factor of all probabilities (one part: 2e-3 for a width of 16384 and logits near 40, fp16's rounding 2.4e-4).
 constexpr int kSumStages = 8;
+// The same for the gradients' products, 2048 of the vocabulary or of the tokens: 2e-5 of a sum whose terms have one sign, a tenth of fp16's
+// rounding.  One part: 1e-3 of dh for 131072 words that share a direction, 5e-4 of dw for 65536 tokens.  Whole training passes with both kinds of
+// parts / without: 8192 x 32768 x 4096 6.9 / 6.7 ms, 2048 x 30522 x 1024 456 / 443 us, 777 x 5003 x 1111 105 / 103 us.
+constexpr int kGradientStages = 32;
 constexpr size_t kFewTokens = 2, kFewCtas = 2;      // see xent_few_kernel; CTAs of an SM
 
 struct HeadSizes {
@@ -638,7 +644,7 @@ struct HeadBackward {
 template <typename O>
 ssgd_status weight_product(const HalfProduct& p, const HeadBackward& b, const Prepared* prepared, size_t first, size_t rows, int sms, cudaStream_t s) {
   const typename WeightEpilogue<O>::Args args = {prepared, static_cast<O*>(b.dw) + first * b.lddw, b.lddw, (unsigned)rows};
-  return launch_half<WeightEpilogue<O>, 1, 0, kBothByRows>(p, args, half_form(p, 1, 1, sms), 1, sms, s);
+  return launch_half<WeightEpilogue<O>, 1, kGradientStages, kBothByRows>(p, args, half_form(p, 1, 1, sms), 1, sms, s);
 }
 
 template <typename T>
@@ -667,7 +673,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
     p.P = b.T; p.Q = columns; p.K = b.D;
     typename GradEpilogue<T>::Args grad = {{}, b.targets, b.lse, b.g, b.kinds, prepared, b.g_stride, tokens, (unsigned)first};
     if (!box_map(&grad.dz, dz, kBf16, b.T, columns, z.dz_ld, 1, 0)) return SSGD_ERR_CUDA;
-    st = launch_half<GradEpilogue<T>, 1, 0, kBothByK>(p, grad, half_form(p, 1, 1, sms), 1, sms, s);
+    st = launch_half<GradEpilogue<T>, 1, kSumStages, kBothByK>(p, grad, half_form(p, 1, 1, sms), 1, sms, s);
     if (st != SSGD_OK) break;
     if (b.dh) {
       p.p = {dz, nullptr, z.dz_ld, 0, false};
@@ -675,7 +681,7 @@ ssgd_status head_backward(const HeadBackward& b, int sms, cudaStream_t s) {
       p.P = b.T; p.Q = b.D; p.K = columns;
       T* out = last && z.splits == 1 ? static_cast<T*>(b.dh) : nullptr;
       const typename TokensEpilogue<T>::Args args = {b.kinds, prepared, z.pieces > 1 || z.splits > 1 ? sums : nullptr, out, b.lddh, tokens, width, first > 0};
-      st = launch_half<TokensEpilogue<T>, 1, 0, kQByRows>(p, args, half_form(p, 1, z.splits, sms), z.splits, sms, s);
+      st = launch_half<TokensEpilogue<T>, 1, kGradientStages, kQByRows>(p, args, half_form(p, 1, z.splits, sms), z.splits, sms, s);
       if (st == SSGD_OK && z.splits > 1) {
         const size_t plane = b.T * b.D;
         launch_kernel(xent_planes_kernel<T>, dim3(grid_for((plane + 1023) / 1024)), dim3(256), 0, s, true, sums, z.splits, plane, prepared, width,

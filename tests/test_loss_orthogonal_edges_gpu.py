@@ -63,3 +63,122 @@ def test_boxes_that_are_used_again(orthogonal, n, rows, cols):
             orthogonal.momentum_step(x, u, m, 0.0, -1.0, products=products)
             moved.append(x)
         assert torch.equal(*moved) and float((moved[0].double() - want).abs().max()) <= most
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# the loss's gradients
+
+
+def gradients(h, w, y, g, part=16384):
+    """dh and dw (as if in fp32) of sum_t g_t losses_t without ignored tokens, and bounds that take sums as sums of parts, all in float64.
+
+    A logit is off by (32 + D / 256) 2^-23 S, S = sum |h_d w_d|, a loss by 2^-19 (1 + lse) beside, forward and backward: dz by the two, and
+    by 2^-38 of the largest g where fp16 ends.  Entries of dz are rounded to 16 bits, each to either side: sums of those errors are held to six standard
+    deviations, half a step / sqrt(3) each.  Targets' entries lie close to the largest, which is kept, and are off by no more than they
+    differ from it.  A sum's parts are 2048 long: 128 steps of 2 * 2^-23 of a part each, and 2^-23 of the sum for each of the parts."""
+    T, D = h.shape
+    V = w.shape[0]
+    hd, half = h.double(), ref.HALF_STEP[h.dtype]
+    z = torch.cat([hd @ p.double().t() for p in w.split(part)], 1)
+    S = torch.stack([(hd.abs() @ p.double().abs().t()).amax(1) for p in w.split(part)]).amax(0)
+    lse = torch.logsumexp(z, 1)
+    gd, at = g.double()[:, None], (torch.arange(T, device=h.device), y)
+    dz = z.sub_(lse[:, None]).exp_()
+    z_tol = (2 * (32 + D / 256) * 2.0 ** -23 * S + 2.0 ** -19 * (1 + lse.abs()))[:, None]
+    tol = gd.abs() * dz * z_tol + gd.abs().max() * 2.0 ** -38
+    dz[at] -= 1
+    dz *= gd
+    target = dz[at].abs() / dz[at].abs().max()
+    tol[at] += torch.minimum(half * target, 1 - target) * dz[at].abs().max() + 2.0 ** -22 * dz[at].abs()
+    spread = (half * dz).square_() / 3
+    spread[at] = 0
+
+    def product(rows, k):
+        """f(dz or what is like it, by columns of the vocabulary): rows that it is multiplied by."""
+        value, loose, chance, size = (rows(t, f) for t, f in ((dz, lambda b: b), (tol, torch.abs), (spread, torch.square), (dz.abs(), torch.abs)))
+        return value, loose + 6 * chance.sqrt() + (2 * 128 + k / 2048 + 2) * 2.0 ** -23 * size
+    dh, dh_tol = product(lambda t, f: sum(t[:, i:i + part] @ f(w[i:i + part].double()) for i in range(0, V, part)), V)
+    dw, dw_tol = product(lambda t, f: t.t() @ f(hd), T)
+    return dh, dh_tol + half * dh.abs() + ref.SMALLEST[h.dtype], dw, dw_tol + 2.0 ** -24 * dw.abs()
+
+
+def long_problem(T, V, D, dtype, deviation, mean, words):
+    """Rows with a part that all of them share, several times their own, so that sums grow with every term: logits of `mean` and their `deviation`."""
+    r = gen(T + V + D)
+    def randn(*s):
+        return torch.randn(*s, generator=r, device="cuda")
+    shared = randn(D)
+    w = randn(V, D).add_(4 * shared)
+    h = randn(T, D)
+    if mean:
+        h += shared
+        w -= w.mean(0) - 4 * shared
+        h *= mean / (h @ w.mean(0))[:, None]
+        w -= 4 * shared
+        w *= deviation / float((h[:8] @ w.t()).std(1).mean())
+        w += 4 * shared
+    else:
+        h -= h @ shared[:, None] * shared / shared.square().sum()
+        h *= deviation / float((h[:8] @ w.t()).std(1).mean())
+    y = torch.randint(0, words, (T,), generator=r, device="cuda")
+    return h.to(dtype), w.to(dtype), y
+
+
+def within(got, want, tol, what):
+    got = got.double()
+    assert torch.isfinite(got).all(), what
+    off = (got - want).abs()
+    assert bool((off <= tol).all()), "%s: %g of its bound, off by %g of %g" % (what, (off / tol).nan_to_num().max(), off.max(), want.abs().max())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("T,V,D", [(700, 131072, 6000), (64, 200000, 256)])
+def test_gradients_over_a_long_vocabulary(loss, T, V, D, dtype):
+    # dh's sum is V long, in one accumulator where there are enough tiles (the first), with planes of their own where not
+    h, w, y = long_problem(T, V, D, dtype, 0.05, 0, V)
+    _, kept = loss.cross_entropy_forward(h, w, y)
+    g = torch.ones(T, device="cuda")
+    dh, dw = loss.cross_entropy_backward(kept, g, dw_dtype=F32)
+    want, tol, dw_want, dw_tol = gradients(h, w, y, g)
+    within(dh, want, tol, "dh")
+    within(dw, dw_want, dw_tol, "dw")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_weight_gradient_of_many_tokens(loss, dtype):
+    # dw's sum is T long: words that are no token's target have terms of one sign
+    w, h, _ = long_problem(2304, 65536, 2048, dtype, 0.1, 0, 10)
+    y = torch.randint(0, 10, (65536,), generator=gen(3), device="cuda")
+    _, kept = loss.cross_entropy_forward(h, w, y)
+    g = torch.ones(65536, device="cuda")
+    dh, dw = loss.cross_entropy_backward(kept, g, dw_dtype=F32)
+    want, tol, dw_want, dw_tol = gradients(h, w, y, g)
+    within(dw, dw_want, dw_tol, "dw")
+    within(dh, want, tol, "dh")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("T", [3, 300])
+def test_large_logits_over_a_long_width(loss, T, dtype):
+    # The backward pass makes its logits once more: what they are off from the forward pass's is a factor of the probabilities, and a row of dz
+    # does not sum to zero.  That sum is dh where w has a column of ones (and h of zeros); one token counts, whose target's entry is the scale of dz
+    # and is kept.  In it: the logits', twice, as in `gradients`; roundings of dz; the product's parts; the target's p, 2^-22.
+    V, D = 2000, 16384
+    h, w, y = long_problem(T, V, D, dtype, 0.3, 40.0, V)
+    h[:, -1], w[:, -1] = 0, 1
+    t = T // 2
+    y[torch.arange(T, device="cuda") != t] = -100
+    _, kept = loss.cross_entropy_forward(h, w, y)
+    g = torch.ones(T, device="cuda")
+    dh, dw = loss.cross_entropy_backward(kept, g, dw_dtype=F32)
+    z = h[t].double() @ w.double().t()
+    S = float((h[t].double().abs() @ w.double().abs().t()).max())
+    p = torch.softmax(z, 0)
+    tol = 2 * (32 + D / 256) * 2.0 ** -23 * S + 2.0 ** -19 * (1 + float(torch.logsumexp(z, 0))) + 6 * ref.HALF_STEP[dtype] * float(p.square().sum().sqrt()) / 3 ** 0.5 \
+        + 2 * (2 * 128 + 3) * 2.0 ** -23 + 2.0 ** -22
+    assert abs(float(dh[t, -1])) <= tol, (float(dh[t, -1]), tol)
+    want, dh_tol, dw_want, dw_tol = gradients(h[t:t + 1], w, y[t:t + 1], g[:1])
+    within(dw, dw_want, dw_tol, "dw")
+    within(dh[t:t + 1], want, dh_tol, "dh")
+    others = torch.arange(T, device="cuda") != t
+    assert not dh[others].any()
