@@ -307,8 +307,8 @@ xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__
       if (most >= 7.9e-31f && most <= 1.3e36f) {            // 2^-100 .. 2^120: both factors are fp32 numbers
         p.scale = __fdiv_rn(kTop, most);
         p.unscale = most * (1.0f / kTop);
-      } else if (top > 0 && top < 0x7F800000u) {            // out there by a power of two
-        const int e = most < 1.0f ? 120 : -100;
+      } else if (top > 0 && top < 0x7F800000u) {            // out there by a power of two that leaves at most 2^14, which fp16 holds
+        const int e = most < 1.0f ? 114 : -114;
         p.scale = __uint_as_float((unsigned)(127 + e) << 23);
         p.unscale = __uint_as_float((unsigned)(127 - e) << 23);
       }

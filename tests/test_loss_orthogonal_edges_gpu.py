@@ -182,3 +182,24 @@ def test_large_logits_over_a_long_width(loss, T, dtype):
     within(dh[t:t + 1], want, dh_tol, "dh")
     others = torch.arange(T, device="cuda") != t
     assert not dh[others].any()
+
+
+def problem(T, V, D, dtype, seed=0):
+    r = gen(seed * 7919 + T + 31 * V + 1009 * D)
+    w = torch.randn(V, D, generator=r, device="cuda").mul_(1.5 / D ** 0.5)
+    y = torch.randint(0, V, (T,), generator=r, device="cuda")
+    h = torch.randn(T, D, generator=r, device="cuda")
+    g = (torch.rand(T, generator=r, device="cuda") - 0.3) / T
+    return h.to(dtype), w.to(dtype), y, g
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("scale", [3e-30, 1e-29, 1.5e38, 3e38])
+def test_gradients_at_the_ends_of_fp32(loss, dtype, scale):
+    # dz is scaled by a power of two there, 2^114 or 2^-114: fp16 keeps it to 2^-25 of what that is the inverse of
+    h, w, y, g = problem(50, 60, 64, dtype)
+    _, kept = loss.cross_entropy_forward(h, w, y)
+    _, dw = loss.cross_entropy_backward(kept, g * scale, dw_dtype=F32)
+    want, tol = ref.loss_and_gradients(h, w, y, g)
+    kept_to = 2.0 ** -25 * (2.0 ** -114 if scale < 1 else 2.0 ** 114) / scale
+    within(dw.double() / scale, want[2], tol[2] + 2.0 ** -23 * want[2].abs() + kept_to * h.double().abs().sum(0), "dw")
