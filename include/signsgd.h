@@ -482,7 +482,7 @@ ssgd_status ssgd_fp4_matmul_wait_selftest(const uint8_t* a_codes, const uint8_t*
  * The logits are never in memory: a tile at a time, forward and once more backward.  A token whose target is `ignore` has
  * loss 0 and no part in any gradient (its row of dh is 0), whatever its row of h and its g hold, NaN included.  Any
  * other target outside 0 .. V-1 gives NaN, the loss and the gradients that it reaches.  Logits, statistics, losses and sums are
- * fp32; dz, divided by its largest entry (and times 2^14 in fp16), is rounded to the type of h and w before the
+ * fp32; dz, divided by its largest finite entry (and times 2^14 in fp16), is rounded to the type of h and w before the
  * products of the gradients, which are multiplied by it again.  In fp16 dz is thus kept to 2^-38 of its largest entry (of one
  * between 2^-100 and 2^120; to 2^-138 below, 2^90 above): the row of dh of a token whose g is 10^-6 of the largest
  * loses probabilities below 4 * 10^-6.  Sums go in a fixed order: equal inputs give equal bits.

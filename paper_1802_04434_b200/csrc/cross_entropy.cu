@@ -293,8 +293,10 @@ xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__
         of[u] = t < tokens ? g[t * g_stride] : 0.0f;
       }
 #pragma unroll
-      for (unsigned u = 0; u < 8; ++u)                      // probabilities below 2^-24 may be missing from a sum of 1; a loss of NaN leaves the others' factor alone
-        if (counts[u]) top = max(top, __float_as_uint(of[u] * fmaxf(-expm1f(-loss[u]), 2.4e-7f)) & 0x7FFFFFFFu);
+      for (unsigned u = 0; u < 8; ++u) {                    // probabilities below 2^-24 may be missing from a sum of 1; a loss or g that is not finite leaves the others' factor alone
+        const unsigned entry = __float_as_uint(of[u] * fmaxf(-expm1f(-loss[u]), 2.4e-7f)) & 0x7FFFFFFFu;
+        if (counts[u] && entry < 0x7F800000u) top = max(top, entry);
+      }
     }
     top = __reduce_max_sync(0xFFFFFFFFu, top);
     if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = top;
@@ -307,7 +309,7 @@ xent_prepare_kernel(const uint8_t* __restrict__ kinds, const float* __restrict__
       if (most >= 7.9e-31f && most <= 1.3e36f) {            // 2^-100 .. 2^120: both factors are fp32 numbers
         p.scale = __fdiv_rn(kTop, most);
         p.unscale = most * (1.0f / kTop);
-      } else if (top > 0 && top < 0x7F800000u) {            // out there by a power of two that leaves at most 2^14, which fp16 holds
+      } else if (top > 0) {                                 // out there by a power of two that leaves at most 2^14, which fp16 holds
         const int e = most < 1.0f ? 114 : -114;
         p.scale = __uint_as_float((unsigned)(127 + e) << 23);
         p.unscale = __uint_as_float((unsigned)(127 - e) << 23);

@@ -203,3 +203,21 @@ def test_gradients_at_the_ends_of_fp32(loss, dtype, scale):
     want, tol = ref.loss_and_gradients(h, w, y, g)
     kept_to = 2.0 ** -25 * (2.0 ** -114 if scale < 1 else 2.0 ** 114) / scale
     within(dw.double() / scale, want[2], tol[2] + 2.0 ** -23 * want[2].abs() + kept_to * h.double().abs().sum(0), "dw")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_a_gradient_that_is_not_finite_leaves_the_other_rows(loss, dtype, value):
+    # gradients of a mean over many tokens: in fp16 what is not scaled vanishes
+    h, w, y, _ = problem(40, 5000, 64, dtype)
+    g = torch.full((40,), 1.0 / 8192, device="cuda")
+    want, tol = ref.loss_and_gradients(h, w, y, g)
+    g[7] = value
+    _, kept = loss.cross_entropy_forward(h, w, y)
+    dh, dw = loss.cross_entropy_backward(kept, g)
+    rest = torch.arange(40, device="cuda") != 7
+    within(dh[rest], want[1][rest], tol[1][rest], "dh")
+    assert not torch.isfinite(dh[7]).all() and not torch.isfinite(dw).all()
+    # nothing but such gradients
+    dh, dw = loss.cross_entropy_backward(kept, torch.full_like(g, value))
+    assert not torch.isfinite(dh).any()
