@@ -8,6 +8,7 @@ device is current.
 from __future__ import annotations
 
 import functools
+import math
 from typing import Optional, Tuple
 
 import torch
@@ -37,12 +38,13 @@ def _batch(t: torch.Tensor, name: str, written: bool) -> Tuple[torch.Tensor, int
     if len(shape) < 2:
         raise ValueError("%s must be a matrix or a batch of them, got %d dimensions" % (name, len(shape)))
     if len(shape) > 3:
+        lead = math.prod(shape[:-2])
         try:
-            t = t.view(-1, *shape[-2:])
+            t = t.view(lead, *shape[-2:])
         except RuntimeError:
             if written:
                 raise ValueError("the leading sides of %s must be one in memory" % name) from None
-            t = t.reshape(-1, *shape[-2:])
+            t = t.reshape(lead, *shape[-2:])
         shape = t.shape
     rows, cols = shape[-2:]
     stride = t.stride()

@@ -65,6 +65,13 @@ def test_boxes_that_are_used_again(orthogonal, n, rows, cols):
         assert torch.equal(*moved) and float((moved[0].double() - want).abs().max()) <= most
 
 
+def test_batches_of_empty_matrices(orthogonal):
+    for shape in ((2, 3, 0, 5), (2, 3, 4, 0), (2, 0, 4, 5), (2, 3, 1, 0, 5)):
+        x = torch.zeros(shape, device="cuda")
+        assert orthogonal.orthogonalise(x).shape == shape and orthogonal.orthogonalise(x, out=torch.zeros_like(x)).shape == shape
+        orthogonal.momentum_step(x, x.clone(), x.clone(), 0.9, 0.1)
+
+
 # ---------------------------------------------------------------------------------------------------------------------
 # the loss's gradients
 
