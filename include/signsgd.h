@@ -533,7 +533,8 @@ ssgd_status ssgd_xent_wait_selftest(const void* h, size_t ldh, const void* w, si
  *              1: operands of 11 bits, sums in fp32: the result is off by about 10^-3 of its norm (less than bf16's rounding of it
  *                 for a side of 256 and more; up to 4 * 10^-3 for small matrices of low rank)
  *   coefficients  HOST float[3]: a, b, c, finite;  steps 1 .. 100
- *   a batch       first element, rows at a stride of ld >= cols, matrices at a stride (any where n = 1); in elements, aligned to one
+ *   a batch       first element, rows at a stride of ld >= cols, matrices at a stride (any where n = 1); in elements, aligned to one.
+ *                 Matrices that are written share no element: they lie behind one another, or their rows in turn
  *   ws            DEVICE, ssgd_orthogonal_ws_bytes(n, rows, cols), 16-byte aligned; calls that may run at the same time
  *                 need one each
  *   status        in/out DEVICE unsigned, as for ssgd_fp4_matmul

@@ -1236,8 +1236,10 @@ ssgd_status check_batch(const void* p, int type, size_t n, size_t rows, size_t c
   if (ld < cols || ld >= (size_t)1 << 44 || stride >= (size_t)1 << 44) return SSGD_ERR_SIZE;
   return SSGD_OK;
 }
-// Matrices that are written may not share elements.
-inline bool overlapping(size_t n, size_t rows, size_t cols, size_t ld, size_t stride) { return n > 1 && stride < (rows - 1) * ld + cols; }
+// Matrices that are written may not share elements: they lie behind one another, or their rows in turn.
+inline bool overlapping(size_t n, size_t rows, size_t cols, size_t ld, size_t stride) {
+  return n > 1 && stride < (rows - 1) * ld + cols && (stride < cols || ld < (n - 1) * stride + cols);
+}
 
 ssgd_status check_problem(size_t n, size_t rows, size_t cols, const float* coefficients, unsigned steps, int products, const void* ws, const unsigned* status) {
   if (rows < 1 || cols < 1 || rows > kMostSide || cols > kMostSide || n > 65535 || steps < 1 || steps > 100) return SSGD_ERR_SIZE;

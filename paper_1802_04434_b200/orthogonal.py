@@ -49,7 +49,9 @@ def _batch(t: torch.Tensor, name: str, written: bool) -> Tuple[torch.Tensor, int
     rows, cols = shape[-2:]
     stride = t.stride()
     n = shape[0] if len(shape) == 3 else 1
-    if (cols > 1 and stride[-1] != 1) or (rows > 1 and stride[-2] < cols) or (written and n > 1 and rows and cols and stride[0] < (rows - 1) * stride[-2] + cols):
+    # matrices behind one another, or their rows in turn
+    shared = written and n > 1 and rows and cols and stride[0] < (rows - 1) * stride[-2] + cols and (stride[0] < cols or stride[-2] < (n - 1) * stride[0] + cols)
+    if (cols > 1 and stride[-1] != 1) or (rows > 1 and stride[-2] < cols) or shared:
         if written:
             raise ValueError("the matrices of %s must have unit column stride and share no elements" % name)
         t = t.contiguous()

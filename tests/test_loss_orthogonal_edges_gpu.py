@@ -72,6 +72,28 @@ def test_batches_of_empty_matrices(orthogonal):
         orthogonal.momentum_step(x, x.clone(), x.clone(), 0.9, 0.1)
 
 
+@pytest.mark.parametrize("n,rows,cols,gap", [(3, 40, 33, 0), (2, 100, 128, 3), (3, 200, 140, 1), (2, 700, 500, 4)])
+def test_matrices_whose_rows_lie_in_turn(orthogonal, n, rows, cols, gap):
+    # one row of each matrix behind the other, as where several weights are one: in place, and as the parameters and momenta of a step
+    def in_turn(t):
+        big = torch.full((rows, n * (cols + gap)), 7.0, device="cuda")
+        view = big.as_strided((n, rows, cols), (cols + gap, n * (cols + gap), 1))
+        view.copy_(t)
+        return big, view
+    u, x0 = (torch.randn(n, rows, cols, generator=gen(rows + i), device="cuda") for i in (0, 1))
+    want = orthogonal.orthogonalise(u)
+    big, view = in_turn(u)
+    assert orthogonal.orthogonalise(view, out=view).data_ptr() == view.data_ptr() and torch.equal(view, want)
+    (_, x), (_, m) = in_turn(x0), in_turn(u)
+    xs, ms = x0.clone(), u.clone()
+    for a, b in ((x, m), (xs, ms)):
+        orthogonal.momentum_step(a, u, b, 0.9, 0.1)
+    assert torch.equal(x, xs) and torch.equal(m, ms)
+    for b, v in ((big, view), (x._base, x), (m._base, m)):
+        v.fill_(7.0)
+        assert bool((b == 7.0).all())
+
+
 # ---------------------------------------------------------------------------------------------------------------------
 # the loss's gradients
 

@@ -9,3 +9,25 @@ def test_batches_of_empty_matrices():
         for written in (False, True):
             t, n, ld, stride = _batch(torch.zeros(shape), "t", written)
             assert t.shape == (torch.Size(shape[:-2]).numel(), *shape[-2:]) and n == t.shape[0]
+
+
+def test_matrices_whose_rows_lie_in_turn():
+    from paper_1802_04434_b200.orthogonal import _batch
+    flat = torch.zeros(400)
+    for n, rows, cols, stride, ld in ((3, 4, 5, 5, 15), (3, 4, 5, 8, 24), (2, 7, 3, 4, 9), (3, 2, 5, 5, 15)):
+        t, *got = _batch(flat.as_strided((n, rows, cols), (stride, ld, 1)), "t", True)
+        assert t.data_ptr() == flat.data_ptr() and got == [n, ld, stride]
+    for n, rows, cols, stride, ld in ((3, 4, 5, 5, 14), (3, 4, 5, 4, 15), (2, 7, 3, 2, 9), (3, 2, 5, 0, 15), (3, 4, 5, 7, 7)):
+        with pytest.raises(ValueError, match="share no elements"):
+            _batch(flat.as_strided((n, rows, cols), (stride, ld, 1)), "t", True)
+
+
+def test_shared_elements_at_the_boundary():
+    import ctypes
+    from paper_1802_04434_b200 import _build, binding as B
+    _build.build()
+    A, f, SIZE = 0x10000, (ctypes.c_float * 3)(3.4445, -4.7750, 2.0315), 3       # a fake address: these calls fail before touching it
+    for n, rows, cols, stride, ld in ((3, 4, 5, 5, 14), (3, 4, 5, 4, 15), (2, 7, 3, 2, 9), (3, 2, 5, 0, 15), (3, 4, 5, 7, 7)):
+        assert B.lib().ssgd_orthogonalise(A, 0, n, rows, cols, cols, rows * cols, f, 5, 3, A, 0, ld, stride, A, A, None) == SIZE
+        assert B.lib().ssgd_orthogonal_step(A, ld, stride, A, 0, cols, rows * cols, A, cols, rows * cols, n, rows, cols, 0.9, 0.1, 0, f, 5, 3, A, A, None) == SIZE
+        assert B.lib().ssgd_orthogonal_step(A, cols, rows * cols, A, 0, cols, rows * cols, A, ld, stride, n, rows, cols, 0.9, 0.1, 0, f, 5, 3, A, A, None) == SIZE
