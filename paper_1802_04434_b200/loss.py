@@ -66,7 +66,8 @@ class Kept(NamedTuple):
 def cross_entropy_forward(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100) -> Tuple[torch.Tensor, Kept]:
     """losses[t] = log sum_v exp (h_t . w_v) - h_t . w_target (float32; 0 where the target is ignore_index, NaN where it is another number
     outside the vocabulary), with what `cross_entropy_backward` needs.  h [tokens][width] and w [vocabulary][width] of one type,
-    bfloat16 or float16, rows at any stride (rows that do not start at multiples of 16 bytes are copied); targets int64 [tokens]."""
+    bfloat16 or float16, rows at any stride (rows that do not start at multiples of 16 bytes are copied); targets int64 [tokens].  Autograd does not see
+    this pass: `cross_entropy` is the one that it differentiates."""
     code = _DTYPES[h.dtype]
     if w.dtype != h.dtype:
         raise TypeError("h and w must be of one dtype, got %s and %s" % (h.dtype, w.dtype))

@@ -69,11 +69,24 @@ def _options(steps, coefficients, products) -> Tuple[float, float, float]:
     return float(a), float(b), float(c)
 
 
+class _NoDerivative(torch.autograd.Function):
+    """Passes a result on; an error where somebody differentiates it."""
+
+    @staticmethod
+    def forward(ctx, result, u):
+        return result.view_as(result)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("orthogonal.orthogonalise has no derivative; detach() u where none is meant")
+
+
 def orthogonalise(u: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS, dtype: Optional[torch.dtype] = None,
                   out: Optional[torch.Tensor] = None, products: Optional[int] = None) -> torch.Tensor:
     """X = u / |u|, then `steps` times X <- a X + (b A + c A^2) X with A = X X^T, for each matrix of u (float32, bfloat16 or float16);
     of `dtype` (None: u's), or into `out`, which may be u.  products: 3, as exact as products in float32, or 1, off by about 1e-3 of
-    the result's norm; None: 1 for a bfloat16 result whose smaller side is 256 or more, else 3."""
+    the result's norm; None: 1 for a bfloat16 result whose smaller side is 256 or more, else 3.  There is no derivative: where autograd
+    would want one of a result (`out` is written as it is), its backward pass is an error."""
     code = _DTYPES[u.dtype]
     device = u.device
     index = device.index
@@ -86,6 +99,7 @@ def orthogonalise(u: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS, dt
         with B._on(index):
             return orthogonalise(u, steps, coefficients, dtype, out, products)
     us, n, ldu, su = _batch(u, "u", False)
+    wanted = out is None and torch.is_grad_enabled() and getattr(u, "requires_grad", False)
     if out is None:
         out = torch.empty(u.shape, dtype=dtype or u.dtype, device=device)
     os, _, ldo, so = _batch(out, "out", True)
@@ -100,14 +114,14 @@ def orthogonalise(u: torch.Tensor, steps: int = 5, coefficients=COEFFICIENTS, dt
             work.data_ptr(), status_of(device)[1], _stream_of(index)))
         if status:
             B._check(status, "ssgd_orthogonalise")
-    return out
+    return _NoDerivative.apply(out, u) if wanted else out
 
 
 def momentum_step(x: torch.Tensor, g: torch.Tensor, m: torch.Tensor, beta: float, delta: float, steps: int = 5,
                   coefficients=COEFFICIENTS, nesterov: bool = False, products: int = 3) -> None:
-    """In place: m <- beta m + (1 - beta) g, then x <- x - delta orthogonalise(m), or with nesterov of beta m + (1 - beta) g.  x and m float32,
-    g float32, bfloat16 or float16; matrices, or batches of one shape.  A factor for the shape (such as max(1, rows / cols) ** 0.5)
-    goes into delta."""
+    """In place, unseen by autograd: m <- beta m + (1 - beta) g, then x <- x - delta orthogonalise(m), or with nesterov of
+    beta m + (1 - beta) g.  x and m float32, g float32, bfloat16 or float16; matrices, or batches of one shape, no two of them in
+    the same memory.  A factor for the shape (such as max(1, rows / cols) ** 0.5) goes into delta."""
     if x.dtype != torch.float32 or m.dtype != torch.float32:
         raise TypeError("x and m must be of dtype float32")
     code = _DTYPES[g.dtype]

@@ -94,6 +94,18 @@ def test_matrices_whose_rows_lie_in_turn(orthogonal, n, rows, cols, gap):
         assert bool((b == 7.0).all())
 
 
+def test_results_that_autograd_would_differentiate(orthogonal):
+    for shape in ((20, 30), (2, 3, 200, 140), (4, 0, 5)):
+        u = torch.randn(shape, generator=gen(1), device="cuda").requires_grad_()
+        got = orthogonal.orthogonalise(u)
+        assert torch.equal(got, orthogonal.orthogonalise(u.detach()))
+        with pytest.raises(RuntimeError, match="no derivative"):
+            (got.sum() + u.sum()).backward()
+        x, m = u.detach().clone().requires_grad_(), torch.zeros(shape, device="cuda")
+        orthogonal.momentum_step(x, torch.ones(shape, device="cuda"), m, 0.9, 0.1)
+        assert x.is_leaf
+
+
 # ---------------------------------------------------------------------------------------------------------------------
 # the loss's gradients
 

@@ -31,3 +31,31 @@ def test_shared_elements_at_the_boundary():
         assert B.lib().ssgd_orthogonalise(A, 0, n, rows, cols, cols, rows * cols, f, 5, 3, A, 0, ld, stride, A, A, None) == SIZE
         assert B.lib().ssgd_orthogonal_step(A, ld, stride, A, 0, cols, rows * cols, A, cols, rows * cols, n, rows, cols, 0.9, 0.1, 0, f, 5, 3, A, A, None) == SIZE
         assert B.lib().ssgd_orthogonal_step(A, cols, rows * cols, A, 0, cols, rows * cols, A, ld, stride, n, rows, cols, 0.9, 0.1, 0, f, 5, 3, A, A, None) == SIZE
+
+
+def test_results_that_autograd_would_differentiate(monkeypatch):
+    # the library's call replaced: what torch is told of a result
+    import types
+    from paper_1802_04434_b200 import binding as B, orthogonal
+
+    class Device(torch.Tensor):
+        """A tensor that says that it lives in device memory."""
+        is_cuda = True
+        device = types.SimpleNamespace(index=0)
+    monkeypatch.setattr(B, "lib", lambda: types.SimpleNamespace(ssgd_orthogonalise_block=lambda block: 0))
+    monkeypatch.setattr(orthogonal, "_current_device", lambda: 0)
+    monkeypatch.setattr(orthogonal, "_stream_of", lambda index: 0)
+    monkeypatch.setattr(orthogonal, "status_of", lambda device: (None, 0))
+    monkeypatch.setattr(orthogonal, "_ws_bytes", lambda *sides: 64)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *s, dtype=None, device=None: empty(*s, dtype=dtype))
+    u = torch.zeros(4, 5).as_subclass(Device).requires_grad_()
+    got = orthogonal.orthogonalise(u)
+    assert got.requires_grad and got.shape == (4, 5)
+    with pytest.raises(RuntimeError, match="no derivative"):
+        got.sum().backward()
+    with torch.no_grad():
+        assert not orthogonal.orthogonalise(u).requires_grad
+    assert not orthogonal.orthogonalise(u.detach()).requires_grad
+    out = empty(4, 5).as_subclass(Device)
+    assert orthogonal.orthogonalise(u, out=out) is out and not out.requires_grad
