@@ -12,6 +12,7 @@ from typing import NamedTuple, Optional, Tuple
 import torch
 
 from . import binding as B
+from .waits import _status, check, status_of  # noqa: F401  (check: part of this module)
 
 _BLOCK = {"mx": 32, "nv": 16}
 _U8 = torch.uint8
@@ -68,31 +69,6 @@ class Packed:
         """A copy with some of codes, scales, tensor_scale, rows, cols, fmt replaced."""
         names = ("codes", "scales", "tensor_scale", "rows", "cols", "fmt")
         return Packed(*[parts.get(n, getattr(self, n)) for n in names])
-
-
-_status = {}
-
-
-def _status_of(device: torch.device) -> Tuple[torch.Tensor, int]:
-    """The word of a device in which a product reports a wait that ran out."""
-    s = _status.get(device)
-    if s is None:
-        if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("the first 4-bit product on a device must come before any stream capture")
-        t = torch.zeros(1, dtype=torch.int32, device=device)
-        torch.cuda.synchronize(device)      # zero before a product on any stream may use it
-        s = _status[device] = (t, t.data_ptr())
-    return s
-
-
-def check(device="cuda") -> None:
-    """Waits for the device and raises if a product since the last check had to give up a bounded wait."""
-    device = torch.device("cuda", torch.cuda.current_device()) if torch.device(device).index is None else torch.device(device)
-    s = _status_of(device)[0]
-    torch.cuda.synchronize(device)
-    if int(s.item()):
-        s.zero_()
-        raise RuntimeError("a 4-bit product did not receive its operands in time; its output is not valid")
 
 
 # These calls are a few microseconds of Python each, next to kernels of a few microseconds: what is below avoids calls,
@@ -225,7 +201,7 @@ def matmul(a: Packed, b: Packed, dtype: torch.dtype = torch.bfloat16, out: Optio
     if k == 0:
         return out.zero_()
     if rows and cols:
-        status = _status.get(device) or _status_of(device)
+        status = _status.get(device) or status_of(device)
         failed = B.lib().ssgd_fp4_matmul_block(_pack_matmul(
             *a.pointers, *b.pointers, rows, cols, k, _FORMATS[fmt], out.data_ptr(), code, ldo, status[1], _stream_of(index)))
         if failed:

@@ -1,22 +1,27 @@
-"""The word of a device in which products of 16-bit operands report a wait that ran out (see ``include/signsgd.h``, status)."""
+"""The word of a device in which products of 16-bit and of 4-bit operands report a wait that ran out (see ``include/signsgd.h``, status)."""
 from __future__ import annotations
 
+import threading
 from typing import Tuple
 
 import torch
 
 _status = {}
+_making = threading.Lock()
 
 
 def status_of(device: torch.device) -> Tuple[torch.Tensor, int]:
     """The word of a device, and its address."""
     s = _status.get(device)
     if s is None:
-        if torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("the first such call on a device must come before any stream capture")
-        t = torch.zeros(1, dtype=torch.int32, device=device)
-        torch.cuda.synchronize(device)      # zero before a product on any stream may use it
-        s = _status[device] = (t, t.data_ptr())
+        with _making:                           # one word for all threads: a kernel may hold the address of each that was given out
+            s = _status.get(device)
+            if s is None:
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("the first such call on a device must come before any stream capture")
+                t = torch.zeros(1, dtype=torch.int32, device=device)
+                torch.cuda.synchronize(device)  # zero before a product on any stream may use it
+                s = _status[device] = (t, t.data_ptr())
     return s
 
 

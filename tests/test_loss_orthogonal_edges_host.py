@@ -59,3 +59,31 @@ def test_results_that_autograd_would_differentiate(monkeypatch):
     assert not orthogonal.orthogonalise(u.detach()).requires_grad
     out = empty(4, 5).as_subclass(Device)
     assert orthogonal.orthogonalise(u, out=out) is out and not out.requires_grad
+
+
+def test_threads_share_a_devices_word(monkeypatch):
+    import threading
+    import time
+    from paper_1802_04434_b200 import fp4, loss, orthogonal, waits
+    made = []
+
+    def zeros(*a, **k):
+        time.sleep(0.05)
+        made.append(torch.ones(1))
+        return made[-1]
+    device = torch.device("cuda", 63)
+    monkeypatch.setattr(torch, "zeros", zeros)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device: None)
+    words = []
+    threads = [threading.Thread(target=lambda: words.append(waits.status_of(device))) for _ in range(8)]
+    try:
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        waits._status.pop(device, None)
+    assert len(made) == 1 and {w[1] for w in words} == {made[0].data_ptr()}
+    # one word and one check for the products of every kind
+    assert fp4._status is waits._status and fp4.check is loss.check is orthogonal.check is waits.check
