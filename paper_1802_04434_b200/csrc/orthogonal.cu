@@ -1134,8 +1134,9 @@ inline bool parts_of(Parts* parts, const Whole& w, size_t rows, size_t cols, siz
 }
 
 // A cluster for each matrix, where that is faster; the clocks of one step either way.  By launches: each product its own, and 5000 for the gap
-// between two.  By a cluster: tiles of 128 x 64 in rounds, 1000 a stage and 4500 beside (a trip through L2, the epilogue, the barrier); clusters
-// of 16 are there 6 times, of 8 12 times.  0: launches.
+// between two.  By a cluster: tiles of 128 x 64 in rounds, 1000 a stage and 4500 beside (a trip through L2, the epilogue, the barrier); on 148
+// SMs clusters of 16 are counted as 6 at one time, of 8 as 12, of 4 as 24, of 2 as 48, on others in proportion.  (Of 4 and 2 there is room for 32 and 72:
+// five steps of 24, 32, 36 and 64 matrices of 200 x 128 take 73, 74, 135 us by clusters and 110 by launches.)  0: launches.
 inline unsigned cluster_ctas(const Problem& p, const Layout& l, int sms) {
   const size_t s = l.side, other = p.rows > p.cols ? p.rows : p.cols;
   HalfProduct h = {};
@@ -1154,7 +1155,7 @@ inline unsigned cluster_ctas(const Problem& p, const Layout& l, int sms) {
   (void)half_form(h, p.terms, 1, sms, &least);
   launches += least;
   const unsigned long long tiles = half_tiles(h, 128, 64), most = tiles > square_tiles ? tiles : square_tiles;
-  const unsigned ctas = most <= 2 ? 2 : most <= 4 ? 4 : most <= 8 ? 8 : 16, at_once = ctas == 16 ? 6 : 96 / ctas;
+  const unsigned ctas = most <= 2 ? 2 : most <= 4 ? 4 : most <= 8 ? 8 : 16, counted = (ctas == 16 ? 6 : 96 / ctas) * (unsigned)sms / 148, at_once = counted ? counted : 1;
   const unsigned long long square_rounds = (square_tiles + ctas - 1) / ctas, rounds = (tiles + ctas - 1) / ctas;
   const unsigned long long stages = (other + 63) / 64, stages_s = (s + 63) / 64;
   const unsigned long long cluster = (square_rounds * (stages + stages_s) + rounds * stages_s) * 1000 + 3 * 4500;
