@@ -102,8 +102,9 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 }
 
 // A few tokens: the weight's bytes are all that counts, and a warp takes four rows of it at a time against tokens that lie in shared memory,
-// in fp32.  (Whole forward passes over 30522 x 1024 on B200, this kernel / tiles of tensor-core products: one token 12.5 / 22.7 us, two 15.1 /
-// 22.7, four 20.9 / 22.7, so up to two; more registers and conversions per byte from there on.)
+// in fp32.  (Whole forward passes on B200, weights from HBM, this kernel / tiles of tensor-core products: 30522 x 1024 with one token 16.5 /
+// 19.0 us, two 18.3 / 19.1, four 24.9 / 19.8; 131072 x 4096 165 / 197, 176 / 196, 222 / 191; so up to two: more registers and conversions
+// per byte from there on.  With the 62 MB of 30522 x 1024 in L2 12.5, 15.1, 20.9 / 22.7.)
 constexpr unsigned kFewRows = 4, kFewWarps = 8;
 constexpr size_t kFewSmem = 98304;
 
