@@ -532,7 +532,7 @@ struct HeadSizes {
   size_t prepared, copy, copy_ld, dz, dz_ld, sums, backward_bytes;       // offsets and row lengths
 };
 
-// Pieces: dz of a piece is at most 2^27 numbers (256 MB), in whole 256 columns.
+// Pieces: dz of a piece is at most 2^27 numbers (256 MB), in whole 256 columns; 256 columns where more than 2^19 tokens make that more.
 constexpr size_t kPieceElements = (size_t)1 << 27;
 inline HalfForm stats_form(size_t T, size_t V, size_t D, int sms) {
   HalfProduct p = {};

@@ -262,3 +262,29 @@ def test_a_gradient_that_is_not_finite_leaves_the_other_rows(loss, dtype, value)
     # nothing but such gradients
     dh, dw = loss.cross_entropy_backward(kept, torch.full_like(g, value))
     assert not torch.isfinite(dh).any()
+
+
+@pytest.mark.parametrize("T", [3, 300])
+def test_every_row_of_a_weight_beyond_32_bits(loss, T):
+    # 4.3e9 bytes of w and 8.6e9 of dw, each block of rows another one, targets all over the vocabulary: a share of it that is lost, repeated or
+    # another's shows in dh and in that block of dw.  In norm: roundings to bf16 of dz and of dh, 2^-8 each at most; logits as in `gradients`, that is
+    # 1e-3 for sums of magnitudes near 55.
+    V, D, part = 262_657, 8192, 16384
+    h = torch.randn(T, D, generator=gen(T), device="cuda").to(BF16)
+    w = torch.empty(V, D, dtype=BF16, device="cuda")
+    for i, block in enumerate(w.split(part)):
+        block.copy_(torch.randn(block.shape, generator=gen(1000 + i), device="cuda").mul_(0.01))
+    y = torch.randint(0, V, (T,), generator=gen(5), device="cuda")
+    y[0], y[1], y[2] = V - 1, 0, V // 2
+    losses, kept = loss.cross_entropy_forward(h, w, y)
+    dh, dw = loss.cross_entropy_backward(kept, torch.ones(T, device="cuda"), dw_dtype=F32)
+    z = torch.cat([h.double() @ block.double().t() for block in w.split(part)], 1)
+    lse = torch.logsumexp(z, 1)
+    at = torch.arange(T, device="cuda"), y
+    want = lse - z[at]
+    assert float((losses.double() - want).abs().max()) < 1e-3
+    dz = z.sub_(lse[:, None]).exp_()
+    dz[at] -= 1
+    assert ref.off(dh, sum(dz[:, i:i + part] @ w[i:i + part].double() for i in range(0, V, part))) < 2.0 ** -7 + 1e-3
+    for i in range(0, V, part):
+        assert ref.off(dw[i:i + part], dz[:, i:i + part].t() @ h.double()) < 2.0 ** -8 + 1e-3, i
