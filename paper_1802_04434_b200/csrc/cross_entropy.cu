@@ -516,10 +516,10 @@ inline size_t up(size_t n, size_t k) { return (n + k - 1) / k * k; }
 
 // Stages between two times that a logit's sum is taken (each takes the threads 1500 clocks of 256 columns; four: 102 us for 2048 x 30522 x 1024).
 // The backward pass makes its logits by the same parts: what they are off beyond the forward pass's, whose log sum exp is taken from them, would be
-// a factor of all probabilities (one part: 2e-3 for a width of 16384 and logits near 40, fp16's rounding 2.4e-4).
+// a factor of all probabilities (a row of dz for a width of 16384 and logits near 40 sums to 2e-3 with one part, to 3e-6 with these).
 constexpr int kSumStages = 8;
 // The same for the gradients' products, 2048 of the vocabulary or of the tokens: 2e-5 of a sum whose terms have one sign, a tenth of fp16's
-// rounding.  One part: 1e-3 of dh for 131072 words that share a direction, 5e-4 of dw for 65536 tokens.  Whole training passes with both kinds of
+// rounding.  In fp16, one part / these: dh over 131072 words that share a direction off by 2.1e-3 / 2.3e-4, dw of 65536 tokens by 4e-4 / 1.2e-5.  Whole training passes with both kinds of
 // parts / without: 8192 x 32768 x 4096 6.9 / 6.7 ms, 2048 x 30522 x 1024 456 / 443 us, 777 x 5003 x 1111 105 / 103 us.
 constexpr int kGradientStages = 32;
 constexpr size_t kFewTokens = 2, kFewCtas = 2;      // see xent_few_kernel; CTAs of an SM

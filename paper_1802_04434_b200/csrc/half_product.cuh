@@ -456,7 +456,8 @@ half_product_kernel(const __grid_constant__ HalfMaps maps, const HalfPlan p, con
           if (!ok) break;
           tcgen05_fence_after();
           const unsigned lanes = tmem + t % S::accs * NT + (quarter << 21);
-          // 16 columns at a time: beside the 128 sums of 256 columns a thread has 40 registers
+          // 16 columns at a time: beside the 128 sums of 256 columns a thread has 40 registers, and epilogues that need more of them keep
+          // some of what they hold in local memory (none with StatsEpilogue, 32 to 104 bytes with those of gradients, 92 to 272 with three terms)
 #pragma unroll
           for (unsigned j = 0; j < 2 * kUnits; ++j) {
             unsigned v[16];
