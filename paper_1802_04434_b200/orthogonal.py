@@ -74,7 +74,8 @@ class _NoDerivative(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, result, u):
-        return result.view_as(result)
+        ctx.mark_dirty(result)                  # the tensor itself: a view of it could not be changed in place
+        return result
 
     @staticmethod
     def backward(ctx, _):

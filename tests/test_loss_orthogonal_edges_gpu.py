@@ -99,6 +99,7 @@ def test_results_that_autograd_would_differentiate(orthogonal):
         u = torch.randn(shape, generator=gen(1), device="cuda").requires_grad_()
         got = orthogonal.orthogonalise(u)
         assert torch.equal(got, orthogonal.orthogonalise(u.detach()))
+        got.mul_(0.1)
         with pytest.raises(RuntimeError, match="no derivative"):
             (got.sum() + u.sum()).backward()
         x, m = u.detach().clone().requires_grad_(), torch.zeros(shape, device="cuda")

@@ -87,3 +87,15 @@ def test_threads_share_a_devices_word(monkeypatch):
     assert len(made) == 1 and {w[1] for w in words} == {made[0].data_ptr()}
     # one word and one check for the products of every kind
     assert fp4._status is waits._status and fp4.check is loss.check is orthogonal.check is waits.check
+
+
+def test_results_may_be_changed_in_place():
+    # scaled before it is added to something, as an update is
+    from paper_1802_04434_b200.orthogonal import _NoDerivative
+    u = torch.ones(3, 4, requires_grad=True)
+    result = torch.full((3, 4), 2.0)
+    got = _NoDerivative.apply(result, u)
+    got.mul_(0.5).add_(1.0)
+    assert got.data_ptr() == result.data_ptr() and bool((got == 2.0).all()) and got.requires_grad
+    with pytest.raises(RuntimeError, match="no derivative"):
+        got.sum().backward()
