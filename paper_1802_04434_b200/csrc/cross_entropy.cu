@@ -519,8 +519,9 @@ inline size_t up(size_t n, size_t k) { return (n + k - 1) / k * k; }
 // a factor of all probabilities (a row of dz for a width of 16384 and logits near 40 sums to 2e-3 with one part, to 3e-6 with these).
 constexpr int kSumStages = 8;
 // The same for the gradients' products, 2048 of the vocabulary or of the tokens: 2e-5 of a sum whose terms have one sign, a tenth of fp16's
-// rounding.  In fp16, one part / these: dh over 131072 words that share a direction off by 2.1e-3 / 2.3e-4, dw of 65536 tokens by 4e-4 / 1.2e-5.  Whole training passes with both kinds of
-// parts / without: 8192 x 32768 x 4096 6.9 / 6.7 ms, 2048 x 30522 x 1024 456 / 443 us, 777 x 5003 x 1111 105 / 103 us.
+// rounding.  In fp16, one part / these: dh over 131072 words that share a direction off by 2.1e-3 / 2.3e-4, dw of 65536 tokens by 4e-4 /
+// 1.2e-5.  Whole training passes with both kinds of parts / without: 8192 x 32768 x 4096 6.9 / 6.7 ms, 2048 x 30522 x 1024 456 / 443 us,
+// 777 x 5003 x 1111 105 / 103 us.
 constexpr int kGradientStages = 32;
 constexpr size_t kFewTokens = 2, kFewCtas = 2;      // see xent_few_kernel; CTAs of an SM
 
